@@ -498,6 +498,189 @@ ssd_status ssd_draft_predict(int32_t rows, int32_t d, int32_t m, int32_t V, cons
                              float eps, int32_t* out_tok, float* out_hidden, void* workspace,
                              size_t workspace_bytes, int32_t* status, ssd_stream_t stream);
 
+/* ---------------------------------------------------------------------------
+ * The paged 8-bit cache.  The paper says nothing about how a cache is kept;
+ * these entry points are this library's own, for programs that decode many
+ * images whose bf16 caches would not fit, token by token or draft by draft.
+ * A pool of num_blocks blocks holds `block` tokens of one sequence each; a
+ * sequence's block table names its blocks in token order, and token p of the
+ * sequence sits in slot table[p / block] * block + p % block.  Keys (rotated)
+ * and values are e4m3 (4 exponent bits, 3 mantissa bits, largest value 448)
+ * with one float32 scale per block and KV head: the value of an entry is
+ * scale * e4m3.
+ *   k, v              dev e4m3 [num_blocks][Hkv][block][d], 16-byte aligned
+ *   k_scale, v_scale  dev float32 [num_blocks][Hkv]
+ * Supported: d in {64, 128}; block in {16, 32, 64, 128}; num_blocks * Hkv *
+ * block < 2^31 (indexes of values are 64-bit).  Blocks may be shared by
+ * sequences that only read them; two sequences must not append to one block.
+ * ------------------------------------------------------------------------- */
+typedef struct {
+  int32_t num_blocks, block, Hkv, d;
+  void* k;
+  void* v;
+  float* k_scale;
+  float* v_scale;
+} ssd_block_cache;
+
+/* Block tables and slot maps from request lengths.  Sequence b holds held[b]
+ * blocks and wants room for its n_new[b] tokens behind cache_len[b]:
+ *     need = ceil((cache_len + n_new) / block), demand = max(0, need - held)
+ * Blocks are dealt in sequence order from a ring of free ids: with first[b] =
+ * sum of demand[b'] over b' < b, block_table[b][held[b] + i] =
+ * ring[(head + first[b] + i) mod ring_size], i < demand[b], as long as head +
+ * first[b] + demand[b] <= tail.  head counts the ids dealt so far, tail the
+ * ids put into the ring so far (both only grow); freed blocks go to
+ * ring[tail mod ring_size].  A sequence that the ring cannot serve gets no
+ * block, and neither does any later one that wants some: SSD_ERR_WORKSPACE is
+ * recorded, its n_blocks stays held[b] and its slots are -1.
+ *     slots[b][j] = slot of token cache_len[b] + j,    j < n_new[b], else -1
+ *     pos[b][j]   = its position on the axes (time, row, column) for the
+ *                   rotary embedding: (p, p, p) for token p of the text
+ *                   prefix, (P, P + y, P + x) for grid token (y, x) behind a
+ *                   prefix of P tokens (slots of end-of-line tokens: x = W);
+ *                   0 where slots is -1
+ * block_table is the only argument both read (entries below held) and written;
+ * a call leaves held, ring, head and tail alone, so repeating it gives the
+ * same results; the next call takes n_blocks as held and next_head as head.
+ *   grid        may be NULL if pos is: only pos depends on it
+ *   cache_len, n_new, held  dev int32 [B]; ring dev int32 [ring_size]
+ *   head, tail  dev int64 [1];  next_head dev int64 [1] (out)
+ *   block_table dev int32 [B][max_blocks];  n_blocks dev int32 [B] (out)
+ *   slots       dev int64 [B][N_max] (out); pos dev int32 [B][N_max][3] or NULL
+ * block: a power of two from 16 to 128.  Device errors: a negative length,
+ * n_new above N_max, need or held above max_blocks, tail - head outside [0,
+ * ring_size] -> DEVICE_BOUNDS (that sequence is not served).
+ * ------------------------------------------------------------------------- */
+ssd_status ssd_cache_plan(const ssd_grid* grid, int32_t B, int32_t block, int32_t max_blocks,
+                          int32_t N_max, const int32_t* cache_len, const int32_t* n_new,
+                          const int32_t* held, const int32_t* ring, int32_t ring_size,
+                          const int64_t* head, const int64_t* tail, int64_t* next_head,
+                          int32_t* block_table, int32_t* n_blocks, int64_t* slots, int32_t* pos,
+                          int32_t* status, ssd_stream_t stream);
+
+/* Rotary positions with three axes (time, row, column).  Pair i of a head (i
+ * < d/2) turns by pos[axis(i)] * freq[i], where the first sec[0] pairs belong
+ * to time, the next sec[1] to the row and the last sec[2] to the column.  Pair
+ * i is (x[i], x[i + d/2]), or (x[2i], x[2i + 1]) if interleaved.  One axis
+ * only: sec = {d/2, 0, 0}.
+ *   table  dev float32 [n_pos][d/2][2]: cos and sin, by ssd_rotary_table()
+ */
+typedef struct {
+  const float* table;
+  int32_t n_pos;
+  int32_t sec[3];
+  int32_t interleaved;
+} ssd_rotary;
+
+/* table[p][i] = (cos(p * freq[i]), sin(p * freq[i])), the angle and the
+ * functions in 64 bits, rounded once.  Laid out once per model.
+ *   freq dev float32 [pairs]; table dev float32 [n_pos][pairs][2] (out) */
+ssd_status ssd_rotary_table(int32_t n_pos, int32_t pairs, const float* freq, float* table,
+                            ssd_stream_t stream);
+
+/* One pass's new tokens into the cache: q and k rotated, k and v quantised.
+ * Token j of sequence b (j < n_new[b], slots[b][j] >= 0) has row b * N_max + j
+ * of q, k and v (bf16; its Hq, Hkv, Hkv heads of d values side by side), rows
+ * ld apart, so the three may be parts of one projection's output.
+ *     q_out[b][j] = rotated q, bf16 (rows of other tokens untouched)
+ * K (rotated, in float32) and V go to their slots.  Per block and head, with
+ * m the largest finite magnitude of the new values and s the block's scale:
+ *  - a block whose first new token is its first token starts over:
+ *    s' = max(m, 2^-100) / 448 (what the block held is not looked at);
+ *  - a block that holds earlier tokens keeps s while m <= 448 s; else
+ *    s' = m / 448 and the earlier tokens' entries become e4m3(old * (s / s')).
+ * New entries are e4m3(clamp(x * (1 / s'), -448, 448)), to nearest even (an
+ * infinity becomes +-448, a NaN stays one).  Writing the same tokens again
+ * changes nothing.  A block's scale covers every token written to it since it
+ * started over, drafts that were rejected among them.
+ *   n_new dev int32 [B]; slots dev int64 [B][N_max]: consecutive tokens of a
+ *   sequence, as ssd_cache_plan() gives them; pos dev int32 [B][N_max][3]
+ *   ldq, ldk, ldv  elements between rows, multiples of 8; q, k, v, q_out
+ *                  16-byte aligned; q_out dev bf16 [B][N_max][Hq][d] (may be q
+ *                  itself if ldq = Hq * d)
+ * Device errors (DEVICE_BOUNDS): n_new outside [0, N_max] (the sequence is
+ * skipped), a slot outside the pool or not the one after its predecessor (the
+ * token is not cached), a position outside [0, n_pos) (position 0 is used).
+ * ------------------------------------------------------------------------- */
+ssd_status ssd_cache_append(const ssd_block_cache* cache, const ssd_rotary* rotary, int32_t B,
+                            int32_t N_max, int32_t Hq, const int32_t* n_new, const int64_t* slots,
+                            const int32_t* pos, const void* q, int64_t ldq, const void* k,
+                            int64_t ldk, const void* v, int64_t ldv, void* q_out, int32_t* status,
+                            ssd_stream_t stream);
+
+/* Frontier attention (a2) over the paged 8-bit cache: the formula and the mask
+ * of ssd_verify_attention() with K and V the cache's values,
+ *     O[b][j][h] = softmax_s(scale * Q[b][j][h] . K[s] + M(s, j)) V[s],
+ * over the sequence's tokens s, key_start[b] <= s < cache_len[b] + n_drafts[b];
+ * M = 0 iff pos(key) <= pos(query).  Tokens [0, cache_len) are committed (flat
+ * position s); token cache_len + j' is draft j' (flat position of
+ * draft_pos[b][j'], or cache_len + j' if draft_pos is NULL: plain causal
+ * decoding, one token each with D_max = 1).  A query that sees no key gets
+ * o = 0 and lse = -inf.  Slots outside the sequence's tokens may hold anything.
+ *   q          dev bf16 [B][D_max][Hq][d] (rotated); scale 0 -> 1/sqrt(d)
+ *   cache_len, n_drafts  dev int32 [B]; draft_pos dev int32 [B][D_max] or NULL
+ *   key_start  dev int32 [B] or NULL (0): the first token that may be seen
+ *              (prompts padded on the left)
+ *   block_table dev int32 [B][max_blocks]
+ *   o          dev bf16 [B][D_max][Hq][d] (out; padding slots untouched)
+ *   lse        dev float32 [B][Hq][D_max] or NULL: log-sum-exp (natural)
+ *   workspace  dev, 16-byte aligned, >= ssd_cache_attention_workspace(...,
+ *              max_blocks * block) bytes; may be NULL if that is 0
+ * q, o: 16-byte aligned.  Supported: Hq % Hkv == 0, any D_max.  Device errors
+ * (DEVICE_BOUNDS): a negative length, n_drafts above D_max or more tokens than
+ * max_blocks * block (rows left untouched); a block id outside the pool (its
+ * tokens are masked); a draft position outside the grid (the draft is seen by
+ * no query and sees no key).
+ * ------------------------------------------------------------------------- */
+size_t ssd_cache_attention_workspace(int32_t B, int32_t Hq, int32_t Hkv, int32_t d, int32_t D_max,
+                                     int32_t L_max);
+ssd_status ssd_cache_attention(const ssd_grid* grid, const ssd_block_cache* cache, int32_t B,
+                               int32_t Hq, const int32_t* cache_len, const int32_t* n_drafts,
+                               const int32_t* draft_pos, const int32_t* key_start, int32_t D_max,
+                               const int32_t* block_table, int32_t max_blocks, const void* q,
+                               float scale, void* o, float* lse, void* workspace,
+                               size_t workspace_bytes, int32_t* status, ssd_stream_t stream);
+
+/* ---------------------------------------------------------------------------
+ * Sampling with temperature, top-k, top-p and min-p from given uniforms (the
+ * paper samples at temperature 1; visual-token models are served with top-k
+ * and top-p).  For row r, with M the largest logit and c = log2(e) / T:
+ *     w_v = 2^(-(M - x_v) c) in float32,  W_v = round(2^31 w_v), an integer,
+ *     so that no sum below depends on its order;
+ *     order: logits descending, the lower index first among equal ones;
+ *     top-k: the first top_k entries (0 or above V: all), their mass Z_k;
+ *     kept:  of those, W_v > 0, w_v >= min_p, and the mass before the entry
+ *            in the order < top_p * Z_k (the first is always kept);
+ *     out_tok = smallest v with sum of kept W_v' over v' <= v > u_res * Z,
+ *     Z the kept mass, u_res the row's second uniform (ssd_rng).
+ * T = 0 takes the first largest logit.  NaN logits count as -inf, +inf ones
+ * as equal weights of 1; a row with nothing above -inf gives out_tok = -1, prob = 0,
+ * kept = 0.  Weights below 2^-32 of the largest are never drawn.
+ *   logits  dev float32 (or bf16 if logits_bf16) row r at + r * ld; any V up
+ *           to 2^20, any alignment to the element
+ *   prob    dev float32 [rows] or NULL: W of the token / Z
+ *   kept    dev int32 [rows] or NULL: entries kept
+ * Settings: one for all rows, or dev arrays [rows] where not NULL (values as
+ * for the scalars: T >= 0 finite, 0 < top_p <= 1, 0 <= min_p <= 1; others
+ * record DEVICE_BOUNDS and give out_tok = -1).  n_drafts (may be NULL): rows
+ * b * D_max + j with j >= n_drafts[b] are padding (-1, 0, 0), not read.
+ * ------------------------------------------------------------------------- */
+typedef struct {
+  float temperature;
+  int32_t top_k;
+  float top_p;
+  float min_p;
+  const float* temperatures;
+  const int32_t* top_ks;
+  const float* top_ps;
+  const float* min_ps;
+  const int32_t* n_drafts;
+  int32_t D_max;
+} ssd_sampling;
+ssd_status ssd_sample(int32_t rows, int32_t V, const void* logits, int32_t logits_bf16, int64_t ld,
+                      const ssd_sampling* sampling, const ssd_rng* rng, int32_t* out_tok,
+                      float* prob, int32_t* kept, int32_t* status, ssd_stream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

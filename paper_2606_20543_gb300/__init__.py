@@ -30,7 +30,9 @@ EXPORTED = ["ssd_abi_version", "ssd_status_string", "ssd_set_wait_limit",
             "ssd_draft_predict",
             "ssd_lmhead_accept_workspace", "ssd_lmhead_accept",
             "ssd_verify_step_workspace", "ssd_verify_step_launches", "ssd_verify_step",
-            "ssd_verify_accept"]
+            "ssd_verify_accept",
+            "ssd_cache_plan", "ssd_rotary_table", "ssd_cache_append",
+            "ssd_cache_attention_workspace", "ssd_cache_attention", "ssd_sample"]
 
 
 STRATEGY_ACCEPT_REJECT, STRATEGY_GREEDY, STRATEGY_SAMPLE = 0, 1, 2
@@ -84,6 +86,26 @@ class VerifyOut(ctypes.Structure):
                 ("status", ctypes.c_void_p)]
 
 
+class BlockCache(ctypes.Structure):
+    _fields_ = [("num_blocks", ctypes.c_int32), ("block", ctypes.c_int32),
+                ("Hkv", ctypes.c_int32), ("d", ctypes.c_int32),
+                ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p)]
+
+
+class Rotary(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("n_pos", ctypes.c_int32),
+                ("sec", ctypes.c_int32 * 3), ("interleaved", ctypes.c_int32)]
+
+
+class Sampling(ctypes.Structure):
+    _fields_ = [("temperature", ctypes.c_float), ("top_k", ctypes.c_int32),
+                ("top_p", ctypes.c_float), ("min_p", ctypes.c_float),
+                ("temperatures", ctypes.c_void_p), ("top_ks", ctypes.c_void_p),
+                ("top_ps", ctypes.c_void_p), ("min_ps", ctypes.c_void_p),
+                ("n_drafts", ctypes.c_void_p), ("D_max", ctypes.c_int32)]
+
+
 _LIB: Optional[ctypes.CDLL] = None
 
 
@@ -130,6 +152,16 @@ def load(path: Optional[str] = None) -> ctypes.CDLL:
         "ssd_verify_step_launches": (I32, [ctypes.POINTER(VerifyArgs)]),
         "ssd_verify_step": (I32, [ctypes.POINTER(VerifyArgs), ctypes.POINTER(VerifyOut), P, SZ, P]),
         "ssd_verify_accept": (I32, [ctypes.POINTER(VerifyArgs), ctypes.POINTER(VerifyOut), P, SZ, P]),
+        "ssd_cache_plan": (I32, [ctypes.POINTER(Grid), I32, I32, I32, I32, P, P, P, P, I32, P, P, P,
+                                 P, P, P, P, P, P]),
+        "ssd_rotary_table": (I32, [I32, I32, P, P, P]),
+        "ssd_cache_append": (I32, [ctypes.POINTER(BlockCache), ctypes.POINTER(Rotary), I32, I32,
+                                   I32, P, P, P, P, I64, P, I64, P, I64, P, P, P]),
+        "ssd_cache_attention_workspace": (SZ, [I32, I32, I32, I32, I32, I32]),
+        "ssd_cache_attention": (I32, [ctypes.POINTER(Grid), ctypes.POINTER(BlockCache), I32, I32, P,
+                                      P, P, P, I32, P, I32, P, F, P, P, P, SZ, P, P]),
+        "ssd_sample": (I32, [I32, I32, P, I32, I64, ctypes.POINTER(Sampling), ctypes.POINTER(Rng),
+                             P, P, P, P, P]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -340,3 +372,89 @@ def ssd_verify_accept(args: VerifyArgs, out: VerifyOut, workspace, workspace_byt
                       stream=None) -> None:
     _check("ssd_verify_accept", load().ssd_verify_accept(
         ctypes.byref(args), ctypes.byref(out), _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+def cache(k, v, k_scale, v_scale) -> BlockCache:
+    """The paged 8-bit cache over device tensors: k, v float8_e4m3fn (or uint8)
+    [num_blocks, Hkv, block, d], scales float32 [num_blocks, Hkv]."""
+    n, Hkv, block, d = k.shape
+    if v.shape != k.shape or tuple(k_scale.shape) != (n, Hkv) or tuple(v_scale.shape) != (n, Hkv):
+        raise ValueError("k, v [num_blocks, Hkv, block, d], scales [num_blocks, Hkv]")
+    for t in (k, v, k_scale, v_scale):
+        if not t.is_contiguous():
+            raise ValueError("the cache's tensors are contiguous")
+    if k.element_size() != 1 or v.element_size() != 1 or k_scale.element_size() != 4 \
+            or v_scale.element_size() != 4:
+        raise ValueError("k and v hold 8-bit entries, the scales float32")
+    return BlockCache(n, block, Hkv, d, _ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale))
+
+
+def rotary(table, sections, interleaved: bool = False) -> Rotary:
+    """Rotary settings: table float32 [n_pos, d/2, 2] (ssd_rotary_table), the
+    pairs of the axes time, row and column."""
+    if not table.is_contiguous() or table.element_size() != 4 or table.shape[-1] != 2:
+        raise ValueError("table: contiguous float32 [n_pos, d/2, 2]")
+    if len(sections) != 3 or sum(sections) != table.shape[1]:
+        raise ValueError("three sections that add up to d/2")
+    return Rotary(_ptr(table), table.shape[0], (ctypes.c_int32 * 3)(*sections), int(interleaved))
+
+
+def sampling(temperature: float = 1.0, top_k: int = 0, top_p: float = 1.0, min_p: float = 0.0,
+             temperatures=None, top_ks=None, top_ps=None, min_ps=None, n_drafts=None,
+             D_max: int = 1) -> Sampling:
+    """Settings of ssd_sample: for all rows, or device arrays [rows]."""
+    return Sampling(temperature, top_k, top_p, min_p, _ptr(temperatures), _ptr(top_ks),
+                    _ptr(top_ps), _ptr(min_ps), _ptr(n_drafts), D_max)
+
+
+def ssd_cache_plan(g: Optional[Grid], B, block, max_blocks, N_max, cache_len, n_new, held, ring,
+                   ring_size, head, tail, next_head, block_table, n_blocks, slots, pos, status,
+                   stream=None) -> None:
+    """Block tables, slot maps and (pos not None) positions of the new tokens."""
+    _check("ssd_cache_plan", load().ssd_cache_plan(
+        None if g is None else ctypes.byref(g), B, block, max_blocks, N_max, _ptr(cache_len),
+        _ptr(n_new), _ptr(held), _ptr(ring), ring_size, _ptr(head), _ptr(tail), _ptr(next_head),
+        _ptr(block_table), _ptr(n_blocks), _ptr(slots), _ptr(pos), _ptr(status), _stream(stream)))
+
+
+def ssd_rotary_table(n_pos, pairs, freq, table, stream=None) -> None:
+    _check("ssd_rotary_table", load().ssd_rotary_table(n_pos, pairs, _ptr(freq), _ptr(table),
+                                                       _stream(stream)))
+
+
+def ssd_cache_append(c: BlockCache, r: Rotary, B, N_max, Hq, n_new, slots, pos, q, ldq, k, ldk, v,
+                     ldv, q_out, status, stream=None) -> None:
+    """Rotate q and k, quantise k and v into the new tokens' slots."""
+    _check("ssd_cache_append", load().ssd_cache_append(
+        ctypes.byref(c), ctypes.byref(r), B, N_max, Hq, _ptr(n_new), _ptr(slots), _ptr(pos),
+        _ptr(q), ldq, _ptr(k), ldk, _ptr(v), ldv, _ptr(q_out), _ptr(status), _stream(stream)))
+
+
+def ssd_cache_attention_workspace(B, Hq, Hkv, d, D_max, L_max) -> int:
+    return load().ssd_cache_attention_workspace(B, Hq, Hkv, d, D_max, L_max)
+
+
+def ssd_cache_attention(g: Grid, c: BlockCache, B, Hq, cache_len, n_drafts, draft_pos, key_start,
+                        D_max, block_table, max_blocks, q, scale, o, lse, workspace,
+                        workspace_bytes, status, stream=None) -> None:
+    """Frontier attention over the paged 8-bit cache."""
+    _check("ssd_cache_attention", load().ssd_cache_attention(
+        ctypes.byref(g), ctypes.byref(c), B, Hq, _ptr(cache_len), _ptr(n_drafts), _ptr(draft_pos),
+        _ptr(key_start), D_max, _ptr(block_table), max_blocks, _ptr(q), scale, _ptr(o), _ptr(lse),
+        _ptr(workspace), workspace_bytes, _ptr(status), _stream(stream)))
+
+
+def ssd_sample(rows, V, logits, ld, p: Sampling, r: Rng, out_tok, prob, kept, status,
+               stream=None) -> None:
+    """Temperature, top-k, top-p and min-p; logits float32 or bfloat16."""
+    if logits is None:
+        bf16 = 0
+    elif logits.element_size() == 4 and logits.is_floating_point():
+        bf16 = 0
+    elif str(logits.dtype) == "torch.bfloat16":
+        bf16 = 1
+    else:
+        raise ValueError("logits are float32 or bfloat16")
+    _check("ssd_sample", load().ssd_sample(
+        rows, V, _ptr(logits), bf16, ld, ctypes.byref(p), ctypes.byref(r), _ptr(out_tok),
+        _ptr(prob), _ptr(kept), _ptr(status), _stream(stream)))

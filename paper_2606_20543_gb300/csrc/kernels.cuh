@@ -384,6 +384,79 @@ bool predictor_supported(int32_t d, int32_t m, int32_t V);  // multiples of 128
 cudaError_t launch_predictor(const PredictorArgs& p, void* ws, size_t ws_bytes, int32_t* status,
                              cudaStream_t stream);
 
+// ---- cache.cu (the paged 8-bit cache: plan, rotary table, append)
+struct CachePlanArgs {
+  ssd_grid grid;
+  int32_t B, block_log, max_blocks, N_max;
+  const int32_t* cache_len;
+  const int32_t* n_new;
+  const int32_t* held;
+  const int32_t* ring;
+  int32_t ring_size;
+  const int64_t* head;
+  const int64_t* tail;
+  int64_t* next_head;
+  int32_t* block_table;
+  int32_t* n_blocks;
+  int64_t* slots;
+  int32_t* pos;  // nullable
+  int32_t* status;
+};
+cudaError_t launch_cache_plan(const CachePlanArgs& a, cudaStream_t stream);
+cudaError_t launch_rotary_table(int32_t n_pos, int32_t pairs, const float* freq, float* table,
+                                cudaStream_t stream);
+struct CacheAppendArgs {
+  ssd_block_cache cache;
+  ssd_rotary rot;
+  int32_t B, N_max, Hq;
+  const int32_t* n_new;
+  const int64_t* slots;
+  const int32_t* pos;
+  const void* q;
+  const void* k;
+  const void* v;
+  int64_t ldq, ldk, ldv;
+  void* q_out;
+  int32_t* status;
+};
+cudaError_t launch_cache_append(const CacheAppendArgs& a, cudaStream_t stream);
+
+// ---- cache_attention.cu
+struct CacheAttnArgs {
+  ssd_grid grid;
+  ssd_block_cache cache;
+  int32_t B, Hq, D_max, max_blocks;
+  const int32_t* cache_len;
+  const int32_t* n_drafts;
+  const int32_t* draft_pos;  // nullable
+  const int32_t* key_start;  // nullable
+  const int32_t* block_table;
+  const void* q;
+  float scale;
+  void* o;
+  float* lse;  // nullable
+  int32_t* status;
+};
+size_t cache_attention_workspace(int32_t B, int32_t Hq, int32_t Hkv, int32_t d, int32_t D_max,
+                                 int32_t L_max);
+cudaError_t launch_cache_attention(const CacheAttnArgs& a, void* ws, cudaStream_t stream);
+
+// ---- sample.cu
+struct SampleArgs {
+  int32_t rows, V;
+  const void* logits;
+  int32_t bf16;
+  int64_t ld;
+  ssd_sampling s;
+  ssd_rng rng;
+  int32_t* out_tok;
+  float* prob;    // nullable
+  int32_t* kept;  // nullable
+  int32_t* status;
+};
+constexpr int32_t kSampleMaxV = 1 << 20;
+cudaError_t launch_sample(const SampleArgs& a, cudaStream_t stream);
+
 int device_sm_count();
 
 // cuTensorMapEncodeTiled, reached through the runtime's driver entry point

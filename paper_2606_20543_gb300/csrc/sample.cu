@@ -28,21 +28,25 @@ namespace {
 constexpr int kSampleThreads = 512;
 constexpr int kSampleWarps = kSampleThreads / 32;
 constexpr int kChunk = 256;              // entries of a chunk, eight to a lane
-constexpr int kBinsLog = 6;              // bins per factor of two
+constexpr int kBinsLog = 6;              // log2 of the bins per factor of two
+constexpr float kBinsPerLog2 = 1 << kBinsLog;
 constexpr int kBins = 32 << kBinsLog;    // weights down to 2^-32: below they are 0
+constexpr float kMaxC = 0x1p100f;        // largest log2(e) / T
 constexpr int kList = 4096;
 constexpr float kLog2e = 1.4426950408889634f;
 typedef unsigned long long u64;
 
 struct SampleRow {
-  float top, c;  // largest logit, log2(e) / T
+  float top, c;  // largest logit; kBinsPerLog2 * log2(e) / T
   float min_p;
   int32_t V;
+  bool inf;      // the largest logit is infinite: logits count as 0 (infinite) or -inf
   const void* x;
 };
 
 // NaN counts as -inf, -0 as +0 (they compare equal).
 __device__ __forceinline__ float clean(float x) { return x != x ? -INFINITY : x + 0.f; }
+__device__ __forceinline__ float finite_or_not(float x) { return x == INFINITY ? 0.f : -INFINITY; }
 // Order-preserving bits.
 __device__ __forceinline__ uint32_t key_of(float x) {
   const uint32_t b = __float_as_uint(x);
@@ -51,11 +55,15 @@ __device__ __forceinline__ uint32_t key_of(float x) {
 __device__ __forceinline__ float of_key(uint32_t k) {
   return __uint_as_float(k ^ ((k >> 31) ? 0x80000000u : 0xffffffffu));
 }
-// log2 of the largest weight over that of x, each operation rounded by itself.
-__device__ __forceinline__ float z_of(const SampleRow& r, float x) {
-  return x == r.top ? 0.f : __fmul_rn(__fsub_rn(r.top, x), r.c);
+// Bins below the largest logit: z times a power of two, each operation of z rounded by
+// itself.  NaN for a NaN, which no comparison lets through.
+__device__ __forceinline__ float bins_of(const SampleRow& r, float x) {
+  return __fmul_rn(__fsub_rn(r.top, x), r.c);
 }
-__device__ __forceinline__ float weight_f(float z) { return exp2f(-z); }
+// 2^-z, 0 <= z <= 32.
+__device__ __forceinline__ float weight_f(float bins) {
+  return ex2_approx(bins * (-1.f / kBinsPerLog2));
+}
 __device__ __forceinline__ uint32_t weight_i(float w) { return __float2uint_rn(w * 0x1p31f); }
 
 // How a row is read: vectors of 16 bytes where it is aligned, else entry by
@@ -69,8 +77,15 @@ __device__ __forceinline__ int32_t index_of(int32_t ch, int u, int lane) {
 }
 template <int MODE>
 __device__ __forceinline__ float load1(const SampleRow& r, int32_t i) {
-  if (MODE == kF32Vec || MODE == kF32) return clean(static_cast<const float*>(r.x)[i]);
-  return clean(__uint_as_float((uint32_t) static_cast<const uint16_t*>(r.x)[i] << 16));
+  const float x = MODE == kF32Vec || MODE == kF32
+                      ? static_cast<const float*>(r.x)[i]
+                      : __uint_as_float((uint32_t) static_cast<const uint16_t*>(r.x)[i] << 16);
+  return r.inf ? finite_or_not(x) : x;
+}
+// The weight of any logit.
+__device__ __forceinline__ uint32_t weight_of(const SampleRow& r, float x) {
+  const float b = bins_of(r, x);
+  return b < (float)kBins ? weight_i(weight_f(b)) : 0;
 }
 template <int MODE>
 __device__ __forceinline__ void load8(const SampleRow& r, int32_t ch, int lane, float (&x)[8]) {
@@ -89,8 +104,10 @@ __device__ __forceinline__ void load8(const SampleRow& r, int32_t ch, int lane, 
         x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
       }
     }
+    if (r.inf) {
 #pragma unroll
-    for (int u = 0; u < 8; ++u) x[u] = clean(x[u]);
+      for (int u = 0; u < 8; ++u) x[u] = finite_or_not(x[u]);
+    }
   } else {
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
@@ -178,7 +195,7 @@ __device__ void select(const SampleRow& r, int32_t n, u64 need, SampleShared& sh
       if (shift < 24 && (k >> (shift + 8)) != prefix) continue;
       const uint32_t d = (k >> shift) & 255u;
       atomicAdd(&sh.rcnt[d], 1u);
-      const uint32_t w = weight_i(weight_f(z_of(r, of_key(k))));
+      const uint32_t w = weight_of(r, of_key(k));
       if (w != 0) atomicAdd(&sh.rmass[d], (u64)w);
     }
     __syncthreads();
@@ -221,7 +238,7 @@ __device__ void select(const SampleRow& r, int32_t n, u64 need, SampleShared& sh
   }
   __syncthreads();
   *key = sh.prefix;
-  const u64 w = weight_i(weight_f(z_of(r, of_key(sh.prefix))));
+  const u64 w = weight_of(r, of_key(sh.prefix));
   *n_eq = BY_COUNT ? sh.need : (w > 0 ? (sh.need + w - 1) / w : 0);
   *mass = sh.above + *n_eq * w;
 }
@@ -233,13 +250,16 @@ __device__ __forceinline__ int shift_of(int32_t b, int wide) {
 }
 
 template <int MODE>
-__global__ void __launch_bounds__(kSampleThreads, 3) sample_kernel(SampleArgs a) {
+__global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a) {
   extern __shared__ __align__(16) unsigned char smem_raw[];
   SampleShared& sh = *reinterpret_cast<SampleShared*>(smem_raw);
   u64* chunk = reinterpret_cast<u64*>(smem_raw + sizeof(SampleShared));
   pdl_wait();
   const int32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int32_t chunks = (a.V + kChunk - 1) / kChunk;
+  // this warp's last chunk (negative: none)
+  const int32_t last_chunk =
+      warp < chunks ? warp + (chunks - 1 - warp) / kSampleWarps * kSampleWarps : -1;
   const int wide = a.V > 65536;
 #pragma unroll 1
   for (int32_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
@@ -273,18 +293,20 @@ __global__ void __launch_bounds__(kSampleThreads, 3) sample_kernel(SampleArgs a)
     r.x = a.bf16 ? static_cast<const void*>(static_cast<const uint16_t*>(a.logits) + row * a.ld)
                  : static_cast<const void*>(static_cast<const float*>(a.logits) + row * a.ld);
     r.min_p = min_p;
-    r.c = T > 0.f ? kLog2e / T : 1.f;
+    r.c = T > 0.f ? fminf(kLog2e / T, kMaxC) * kBinsPerLog2 : 1.f;
+    r.inf = false;
     const bool greedy = T == 0.f || k == 1;
     const bool cut_k = k > 0 && k < r.V, cut_p = top_p < 1.f;
 
     // ---- A: the largest logit and its first index
+    // (a NaN loses every comparison; the lane's chunk that holds its first largest is kept)
     float m = -INFINITY;
-    int32_t mc = 0;  // chunk of this lane's first largest
+    int32_t mc = 0;
 #pragma unroll 2
     for (int32_t ch = warp; ch < chunks; ch += kSampleWarps) {
       float x[8];
       load8<MODE>(r, ch, lane, x);
-      float y = fmax3(fmax3(x[0], x[1], x[2]), fmax3(x[3], x[4], x[5]), fmaxf(x[6], x[7]));
+      const float y = fmax3(fmax3(x[0], x[1], x[2]), fmax3(x[3], x[4], x[5]), fmaxf(x[6], x[7]));
       if (y > m) {
         m = y;
         mc = ch;
@@ -313,13 +335,9 @@ __global__ void __launch_bounds__(kSampleThreads, 3) sample_kernel(SampleArgs a)
     if (greedy) {
       int32_t at = 0x7fffffff;
       if (m == r.top) {
-        float x[8];
-        // (this lane's own entries of the chunk; the load is per lane)
-        const int32_t ch = mc;
         for (int u = 7; u >= 0; --u) {
-          const int32_t i = index_of<MODE>(ch, u, lane);
-          x[u] = i < r.V ? load1<MODE>(r, i) : -INFINITY;
-          if (x[u] == r.top) at = i;
+          const int32_t i = index_of<MODE>(mc, u, lane);
+          if (i < r.V && load1<MODE>(r, i) == r.top) at = i;
         }
       }
       at = __reduce_min_sync(0xffffffffu, at);
@@ -334,26 +352,29 @@ __global__ void __launch_bounds__(kSampleThreads, 3) sample_kernel(SampleArgs a)
       continue;
     }
 
-    // ---- B: the bins of the cuts
-    constexpr float kScale = (float)(1 << kBinsLog);
+    if (r.top == INFINITY) {
+      r.inf = true;
+      r.top = 0.f;
+    }
+
+    // ---- B: the bins of the cuts.  From the row's end, which was read last.
+    u64 total = 0;  // mass of the row (with top-p)
     if (cut_k || cut_p) {
-      u64 total = 0;
 #pragma unroll 1
-      for (int32_t ch = warp; ch < chunks; ch += kSampleWarps) {
+      for (int32_t ch = last_chunk; ch >= 0; ch -= kSampleWarps) {
         float x[8];
         load8<MODE>(r, ch, lane, x);
 #pragma unroll
         for (int u = 0; u < 8; ++u) {
-          const float z = z_of(r, x[u]);
-          if (z < 32.f) {
-            const int32_t b = (int32_t)(z * kScale);
-            if (cut_p) {
-              const uint32_t w = weight_i(weight_f(z));
-              total += w;
-              atomicAdd(&sh.mass[b], w >> shift_of(b, wide));
-            }
-            if (cut_k) atomicAdd(&sh.cnt[b], 1u);
+          const float z = bins_of(r, x[u]);
+          const bool in = z < (float)kBins;
+          const int32_t b = (int32_t)fminf(z, (float)kBins);
+          if (cut_p) {
+            const uint32_t w = weight_i(weight_f(fminf(z, (float)kBins)));  // 0 at kBins
+            total += w;
+            if (in) atomicAdd(&sh.mass[b], w >> shift_of(b, wide));
           }
+          if (cut_k && in) atomicAdd(&sh.cnt[b], 1u);
         }
       }
       if (cut_p) total = block_sum64(total, sh.red);
@@ -436,41 +457,56 @@ __global__ void __launch_bounds__(kSampleThreads, 3) sample_kernel(SampleArgs a)
     const float sure = (float)min(bin_lo, bin_k);
     __syncthreads();
 
+    // entries between the top-p bins and the top-k one count for top-p's mass
+    const float gap = cut_p && bin_hi < bin_k && bin_k < kBins ? (float)(bin_hi + 1) : (float)kBins;
+    const float behind = (float)min(kBins, cut_k && bin_k < kBins ? bin_k + 1 : bin_hi + 1);
+    const float limit = cut_k || cut_p ? fmaxf(sure, behind) : (float)kBins;
+
     // ---- C: exact masses by chunk, and the list
-    u64 count = 0, upto = 0, mid = 0;  // masses before the listed bins, and between them
+    u64 upto = 0, mid = 0;  // masses before the listed bins, and between them
+    uint32_t count = 0;
 #pragma unroll 1
     for (int32_t ch = warp; ch < chunks; ch += kSampleWarps) {
       float x[8];
       load8<MODE>(r, ch, lane, x);
-      u64 s = 0;
+      float z[8], least = INFINITY;
 #pragma unroll
       for (int u = 0; u < 8; ++u) {
-        const float z = z_of(r, x[u]);
-        if (!(z < 32.f)) continue;
-        const float zb = z * kScale;
-        if (zb < sure) {
-          const float w = weight_f(z);
-          const uint32_t wi = weight_i(w);
+        z[u] = bins_of(r, x[u]);
+        least = fminf(least, z[u]);
+      }
+      u64 s = 0;
+      if (__any_sync(0xffffffffu, least < limit)) {
+        bool other = false;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+          const float w = weight_f(fminf(z[u], (float)kBins));
+          const bool in = z[u] < sure;
+          const uint32_t wi = in ? weight_i(w) : 0;
           upto += wi;
-          if (w >= r.min_p) {
-            s += wi;
-            count += wi != 0;
-          }
-        } else {
-          const int32_t b = (int32_t)zb;
-          if (b > bin_k) continue;
-          if (b == bin_k || (b >= bin_lo && b <= bin_hi)) {
-            const int32_t at = atomicAdd(&sh.n_list, 1);
-            if (at < kList) {
-              sh.key[at] = key_of(x[u]);
-              sh.idx[at] = index_of<MODE>(ch, u, lane);
+          const uint32_t wk = w >= r.min_p ? wi : 0;
+          s += wk;
+          count += wk != 0;
+          other |= !in && z[u] < limit;
+        }
+        if (other) {
+#pragma unroll
+          for (int u = 0; u < 8; ++u) {
+            if (!(z[u] >= sure && z[u] < limit)) continue;
+            const int32_t b = (int32_t)z[u];
+            if (b == bin_k || (b >= bin_lo && b <= bin_hi)) {
+              const int32_t at = atomicAdd(&sh.n_list, 1);
+              if (at < kList) {
+                sh.key[at] = key_of(clean(x[u]));
+                sh.idx[at] = index_of<MODE>(ch, u, lane);
+              }
+            } else if (z[u] >= gap) {
+              mid += weight_i(weight_f(z[u]));
             }
-          } else if (cut_p && b > bin_hi) {
-            mid += weight_i(weight_f(z));
           }
         }
+        s = warp_sum35(s);
       }
-      s = warp_sum35(s);
       if (lane == 0) chunk[ch] = s;
     }
     if (cut_p) {
@@ -484,15 +520,16 @@ __global__ void __launch_bounds__(kSampleThreads, 3) sample_kernel(SampleArgs a)
     if (n_list > kList) {
       // too many entries where a cut falls: the radix search over the whole row
       auto of_row = [&](int32_t i, uint32_t* key) {
-        *key = key_of(load1<MODE>(r, i));
+        *key = key_of(clean(load1<MODE>(r, i)));
         return true;
       };
-      u64 total = 0, mass;
+      u64 mass;
+      total = 0;
       if (cut_k) {
         select<true>(r, r.V, (u64)k, sh, of_row, &cut, &n_eq, &total);
       } else {
         for (int32_t i = tid; i < r.V; i += kSampleThreads)
-          total += weight_i(weight_f(z_of(r, load1<MODE>(r, i))));
+          total += weight_of(r, load1<MODE>(r, i));
         total = block_sum64(total, sh.red);
       }
       if (cut_p) {
@@ -504,7 +541,7 @@ __global__ void __launch_bounds__(kSampleThreads, 3) sample_kernel(SampleArgs a)
 #pragma unroll 1
       for (int32_t i0 = 0; i0 < r.V && seen < n_eq; i0 += kSampleThreads) {
         const int32_t i = i0 + tid;
-        const bool eq = i < r.V && key_of(load1<MODE>(r, i)) == cut;
+        const bool eq = i < r.V && key_of(clean(load1<MODE>(r, i))) == cut;
         const uint32_t ball = __ballot_sync(0xffffffffu, eq);
         __syncthreads();
         if (lane == 0) sh.redi[warp] = __popc(ball);
@@ -516,7 +553,7 @@ __global__ void __launch_bounds__(kSampleThreads, 3) sample_kernel(SampleArgs a)
       }
       __syncthreads();
     } else if (n_list > 0) {
-      auto bin = [&](uint32_t key) { return (int32_t)(z_of(r, of_key(key)) * kScale); };
+      auto bin = [&](uint32_t key) { return (int32_t)bins_of(r, of_key(key)); };
       u64 in_k = 0, mass;  // mass of the entries of the top-k bin within top-k
       if (cut_k && bin_k < kBins) {
         auto of_k = [&](int32_t i, uint32_t* key) {
@@ -529,11 +566,11 @@ __global__ void __launch_bounds__(kSampleThreads, 3) sample_kernel(SampleArgs a)
         // the k entries' mass: before, between and in the listed bins
         u64 s = 0;
         for (int32_t i = tid; i < n_list; i += kSampleThreads) {
-          const float z = z_of(r, of_key(sh.key[i]));
-          if ((int32_t)(z * kScale) != bin_k) s += weight_i(weight_f(z));
+          if (bin(sh.key[i]) != bin_k) s += weight_of(r, of_key(sh.key[i]));
         }
         s = block_sum64(s, sh.red);
-        const u64 need = (u64)ceil((double)top_p * (double)(upto + mid + s + in_k));
+        const u64 k_mass = bin_k < kBins ? upto + mid + s + in_k : total;
+        const u64 need = (u64)ceil((double)top_p * (double)k_mass);
         auto listed = [&](int32_t i, uint32_t* key) {
           *key = sh.key[i];
           return true;
@@ -556,9 +593,9 @@ __global__ void __launch_bounds__(kSampleThreads, 3) sample_kernel(SampleArgs a)
     const bool by_row = n_list > kList;
     const int32_t cut_idx = sh.cut_idx;
     auto kept_weight = [&](float x, int32_t i) -> uint32_t {
-      const uint32_t kx = key_of(x);
-      if (kx < cut || (kx == cut && i >= cut_idx)) return 0;
-      const float z = z_of(r, x);
+      const uint32_t kx = key_of(clean(x));
+      const float z = bins_of(r, x);
+      if (kx < cut || (kx == cut && i >= cut_idx) || !(z < (float)kBins)) return 0;
       const float w = weight_f(z);
       return w >= r.min_p ? weight_i(w) : 0;
     };
@@ -587,7 +624,7 @@ __global__ void __launch_bounds__(kSampleThreads, 3) sample_kernel(SampleArgs a)
         atomicAdd(&chunk[sh.idx[i] / kChunk], (u64)w);
       }
     }
-    count = block_sum64(count, sh.red);
+    const u64 n_kept = block_sum64(count, sh.red);
 
     // ---- the draw
     if (warp == 0) {
@@ -637,7 +674,7 @@ __global__ void __launch_bounds__(kSampleThreads, 3) sample_kernel(SampleArgs a)
       if (lane == 0) {
         a.out_tok[row] = pick;
         if (a.prob) a.prob[row] = (float)((double)wp / (double)Z);
-        if (a.kept) a.kept[row] = (int32_t)count;
+        if (a.kept) a.kept[row] = (int32_t)n_kept;
       }
     }
   }

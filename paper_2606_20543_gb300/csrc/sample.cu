@@ -4,19 +4,20 @@
 // Weights are 32-bit integers, W = round(2^31 * 2^(-(max - x) c)), so every sum
 // is exact and the result depends on no order of summation.  The entries kept
 // are a prefix of the order (logit descending, index ascending): top-k cuts it by count,
-// top-p by mass, min-p by weight.  One block of threads takes a row in three passes, the first
-// from HBM and the others from L2 (a row of 65536 logits is 256 KB):
-//  A the largest logit;
-//  B a histogram of z = (max - x) c in bins of 1/64: the entries of each bin where
-//    top-k cuts, its mass where top-p does (one 32-bit atomic for each: the weights
-//    of a bin are cut to about 15 bits, so its mass is known from below and above).  They give
-//    the bin of the k-th entry and the one or two bins that can hold the top-p cut;
-//  C the exact weights: the mass of what is kept for certain, by chunks of 256
+// top-p by mass, min-p by weight.  One block of threads takes a row, which it reads twice,
+// from HBM and then from L2 (a row of 65536 float32 logits is 256 KB):
+//  A the largest logit, and a histogram of the logits in bins of 1/128 of a factor of
+//    two of weight (one 32-bit atomic an entry; the bins hang on the largest of the row's first
+//    entries, since the largest of all is not known yet).  The counts give the bin of the
+//    k-th entry exactly, and, each entry taken at its bin's middle, the bins where the
+//    top-p cut falls, with a margin of five standard deviations of that estimate;
+//  B the exact weights: the mass of what is kept for certain, by chunks of 256
 //    entries, and a list of the few entries in the bins where a cut falls.
 // A radix search over the list (exact counts and masses) finds both cuts, ties are
 // resolved by index, the listed entries that are kept join their chunks, and the chunk
-// and the entry that hold u Z are found.  Where the bins of a cut hold more entries than
-// the list takes (equal logits, high temperatures), the radix search runs over the row.
+// and the entry that hold u Z are found.  Where the bins of a cut hold more entries than the
+// list takes (equal logits, high temperatures), the search runs over the row's entries
+// in those bins; where the exact masses show the cut to be elsewhere, over the whole row.
 #include <algorithm>
 
 #include "kernels.cuh"
@@ -27,21 +28,30 @@ namespace {
 
 constexpr int kSampleThreads = 512;
 constexpr int kSampleWarps = kSampleThreads / 32;
-constexpr int kChunk = 256;              // entries of a chunk, eight to a lane
-constexpr int kBinsLog = 6;              // log2 of the bins per factor of two
-constexpr float kBinsPerLog2 = 1 << kBinsLog;
-constexpr int kBins = 32 << kBinsLog;    // weights down to 2^-32: below they are 0
-constexpr float kMaxC = 0x1p100f;        // largest log2(e) / T
+constexpr int kChunk = 256;            // entries of a chunk, eight to a lane
+constexpr int kPerLog2 = 128;             // bins per factor of two
+constexpr float kBinsPerLog2 = kPerLog2;
+constexpr int kHead = 8 * kPerLog2;       // bins above the reference logit: 8 factors of two
+constexpr int kBins = kHead + 32 * kPerLog2;  // and below it: from 2^-32 on weights are 0
+constexpr float kMaxC = 0x1p100f;      // largest log2(e) / T
 constexpr int kList = 4096;
 constexpr float kLog2e = 1.4426950408889634f;
+// Standard deviation of log-uniform weights in a bin over their mean: ln 2 / 128 / sqrt(12)
+constexpr float kBinSpread = 0.00157f;
+constexpr int kFew = 32;                  // entries that one warp orders by itself
 typedef unsigned long long u64;
 
+// How a row is read: vectors of 16 bytes where it is aligned, else entry by
+// entry.  Lane l takes entries index_of(ch, u, l), u < 8, of chunk ch.
+enum Mode { kF32Vec, kBf16Vec, kF32, kBf16 };
+
 struct SampleRow {
-  float top, c;  // largest logit; kBinsPerLog2 * log2(e) / T
-  float min_p;
+  const void* x;
   int32_t V;
   bool inf;      // the largest logit is infinite: logits count as 0 (infinite) or -inf
-  const void* x;
+  float top;     // the largest logit
+  float c;       // bins per unit of logit: kBinsPerLog2 * log2(e) / T
+  float min_p;
 };
 
 // NaN counts as -inf, -0 as +0 (they compare equal).
@@ -55,20 +65,36 @@ __device__ __forceinline__ uint32_t key_of(float x) {
 __device__ __forceinline__ float of_key(uint32_t k) {
   return __uint_as_float(k ^ ((k >> 31) ? 0x80000000u : 0xffffffffu));
 }
-// Bins below the largest logit: z times a power of two, each operation of z rounded by
-// itself.  NaN for a NaN, which no comparison lets through.
-__device__ __forceinline__ float bins_of(const SampleRow& r, float x) {
-  return __fmul_rn(__fsub_rn(r.top, x), r.c);
+__device__ __forceinline__ float2 fmul2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n .reg .b64 ra, rb, rd;\n"
+      " mov.b64 ra, {%2, %3};\n mov.b64 rb, {%4, %5};\n"
+      " mul.rn.f32x2 rd, ra, rb;\n mov.b64 {%0, %1}, rd;\n}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
 }
-// 2^-z, 0 <= z <= 32.
-__device__ __forceinline__ float weight_f(float bins) {
-  return ex2_approx(bins * (-1.f / kBinsPerLog2));
+__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
+// top - x, one rounding.
+__device__ __forceinline__ float2 below2(float top, float x0, float x1) {
+  return ffma2(make_float2(x0, x1), both(-1.f), both(top));
 }
+// The integer weight of float32 weight 2^-z.
 __device__ __forceinline__ uint32_t weight_i(float w) { return __float2uint_rn(w * 0x1p31f); }
+// 2^-z, z the bins below the largest logit over 128: the difference, the product and the
+// power are rounded one by one (the division by 128 is exact).
+__device__ __forceinline__ float weight_f(const SampleRow& r, float x) {
+  const float z = __fmul_rn(__fsub_rn(r.top, x), r.c);
+  return z < 32.f * kBinsPerLog2 ? ex2_approx(z * (-1.f / kBinsPerLog2)) : 0.f;  // (NaN: 0)
+}
+__device__ __forceinline__ uint32_t weight_of(const SampleRow& r, float x) {
+  return weight_i(weight_f(r, x));
+}
+// A logit's bin under the reference logit `ref`, as a float: descending in x.
+__device__ __forceinline__ float bin_of(float ref, float c, float x) {
+  return fmaf(__fsub_rn(ref, x), c, (float)kHead);
+}
 
-// How a row is read: vectors of 16 bytes where it is aligned, else entry by
-// entry.  Lane l takes entries index(ch, u, l), u < 8, of chunk ch.
-enum Mode { kF32Vec, kBf16Vec, kF32, kBf16 };
 template <int MODE>
 __device__ __forceinline__ int32_t index_of(int32_t ch, int u, int lane) {
   if (MODE == kF32Vec) return ch * kChunk + (u >> 2) * 128 + lane * 4 + (u & 3);
@@ -76,16 +102,11 @@ __device__ __forceinline__ int32_t index_of(int32_t ch, int u, int lane) {
   return ch * kChunk + u * 32 + lane;
 }
 template <int MODE>
-__device__ __forceinline__ float load1(const SampleRow& r, int32_t i) {
-  const float x = MODE == kF32Vec || MODE == kF32
-                      ? static_cast<const float*>(r.x)[i]
-                      : __uint_as_float((uint32_t) static_cast<const uint16_t*>(r.x)[i] << 16);
-  return r.inf ? finite_or_not(x) : x;
-}
-// The weight of any logit.
-__device__ __forceinline__ uint32_t weight_of(const SampleRow& r, float x) {
-  const float b = bins_of(r, x);
-  return b < (float)kBins ? weight_i(weight_f(b)) : 0;
+__device__ __forceinline__ float load1(const void* x, bool inf, int32_t i) {
+  const float v = MODE == kF32Vec || MODE == kF32
+                      ? static_cast<const float*>(x)[i]
+                      : __uint_as_float((uint32_t) static_cast<const uint16_t*>(x)[i] << 16);
+  return inf ? finite_or_not(v) : v;
 }
 template <int MODE>
 __device__ __forceinline__ void load8(const SampleRow& r, int32_t ch, int lane, float (&x)[8]) {
@@ -112,27 +133,36 @@ __device__ __forceinline__ void load8(const SampleRow& r, int32_t ch, int lane, 
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
       const int32_t i = index_of<MODE>(ch, u, lane);
-      x[u] = i < r.V ? load1<MODE>(r, i) : -INFINITY;
+      x[u] = i < r.V ? load1<MODE>(r.x, r.inf, i) : -INFINITY;
     }
   }
 }
+__device__ __forceinline__ float max8(const float (&x)[8]) {  // NaN loses
+  return fmax3(fmax3(x[0], x[1], x[2]), fmax3(x[3], x[4], x[5]), fmaxf(x[6], x[7]));
+}
 
 struct SampleShared {
-  uint32_t mass[kBins];  // of a bin, in units of 2^shift_of(bin)
   uint32_t cnt[kBins];
-  uint32_t key[kList];   // the list
+  uint32_t key[kList];  // the list
   int32_t idx[kList];
-  u64 rmass[256];        // radix search
+  uint32_t rsum[3][256];  // radix search: the masses' 11, 11 and 10 bits, each summed
   uint32_t rcnt[256];
-  u64 red[kSampleWarps];
-  u64 red2[kSampleWarps];
-  float redf[kSampleWarps];
+  uint32_t few_key[kFew];
+  int32_t few_idx[kFew];
+  u64 red[kSampleWarps], red2[kSampleWarps];
+  float redf[kSampleWarps], redf2[kSampleWarps];
   int32_t redi[kSampleWarps];
-  uint32_t prefix;
+  uint32_t from, to;  // radix search: the keys left, how many entries, what is to be reached
+  uint32_t left, n_few;
   u64 need, above;
+  uint32_t cut;       // its results: the cut's key, the index behind the last entry equal to it
+  u64 n_eq, cut_mass; // that is kept (cut_idx) or how many are (n_eq, where cut_idx is not
+                      // known), and the mass up to and including them
   int32_t n_list, cut_idx;
-  int32_t bin_k, bin_lo, bin_hi;
-  u64 upto_k_lo, upto_k_hi;
+  int32_t bin_k, bin_lo, bin_hi, need_k;
+  float k_mass;               // estimated mass of the first k entries, and its error
+  float k_mass_err;
+  uint32_t edge[4];           // least keys above the bins' edges
 };
 
 __device__ __forceinline__ u64 block_sum64(u64 v, u64* red) {
@@ -146,74 +176,74 @@ __device__ __forceinline__ u64 block_sum64(u64 v, u64* red) {
   for (int w = 0; w < kSampleWarps; ++w) s += red[w];
   return s;
 }
-// Inclusive scan over the block's threads.
-__device__ __forceinline__ u64 block_scan64(u64 v, u64* red) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const u64 y = __shfl_up_sync(0xffffffffu, v, o);
-    if (lane >= o) v += y;
-  }
-  __syncthreads();
-  if (lane == 31) red[warp] = v;
-  __syncthreads();
-  for (int w = 0; w < warp; ++w) v += red[w];
-  return v;
-}
 // Sum of at most 35-bit values over a warp.
 __device__ __forceinline__ u64 warp_sum35(u64 v) {
   const uint32_t lo = __reduce_add_sync(0xffffffffu, (uint32_t)(v & 0xffffffu));
   const uint32_t hi = __reduce_add_sync(0xffffffffu, (uint32_t)(v >> 24));
   return ((u64)hi << 24) + lo;
 }
+__device__ __forceinline__ u64 add_wide(u64 s, uint32_t w) {
+  asm("mad.wide.u32 %0, %1, 1, %0;" : "+l"(s) : "r"(w));
+  return s;
+}
 
-// The entry of the order at which `need` entries (BY_COUNT) or a mass of `need`
-// is reached among entries 0 .. n - 1 (at(i, &key): whether entry i takes part): its key,
-// how many entries equal to it are within, and the mass of everything up to and including
-// those.  need is at least 1 and at most the entries' count or mass.
-template <bool BY_COUNT, typename At>
-__device__ void select(const SampleRow& r, int32_t n, u64 need, SampleShared& sh, At at,
-                       uint32_t* key, u64* n_eq, u64* mass) {
-  if (threadIdx.x == 0) {
-    sh.prefix = 0;
+// The entry of the order at which `need` entries (by_count) or a mass of `need`
+// is reached among the entries (of the list, or of the row) whose keys are in lo .. hi: its
+// key, the index behind it and the mass of everything up to and including it.  need is at
+// least 1 and at most the entries' count or mass.  Each round deals the keys left to 256 digits
+// and keeps one digit's; a few entries are then ordered by one warp, a lane each.  Where
+// more share one key, the entries of that key that are kept are counted instead (n_eq).
+template <int MODE>
+__device__ __noinline__ void select(SampleRow r, SampleShared& sh, bool of_row, bool by_count, u64 need,
+                                    uint32_t lo, uint32_t hi) {
+  const int32_t n = of_row ? r.V : sh.n_list, tid = threadIdx.x;
+  auto key_at = [&](int32_t i) { return of_row ? key_of(clean(load1<MODE>(r.x, r.inf, i))) : sh.key[i]; };
+  __syncthreads();
+  if (tid == 0) {
+    sh.from = lo;
+    sh.to = hi;
     sh.need = need;
     sh.above = 0;
+    sh.left = (uint32_t)n;
+    sh.n_few = 0;
   }
 #pragma unroll 1
-  for (int shift = 24; shift >= 0; shift -= 8) {
+  while (true) {
+    if (tid < 256) sh.rcnt[tid] = sh.rsum[0][tid] = sh.rsum[1][tid] = sh.rsum[2][tid] = 0;
     __syncthreads();
-    if (threadIdx.x < 256) {
-      sh.rmass[threadIdx.x] = 0;
-      sh.rcnt[threadIdx.x] = 0;
-    }
-    __syncthreads();
-    const uint32_t prefix = sh.prefix;
+    const uint32_t from = sh.from, to = sh.to;
+    if (from == to || sh.left <= kFew) break;
+    const int shift = max(0, 24 - __clz(to - from));
 #pragma unroll 1
-    for (int32_t i = threadIdx.x; i < n; i += kSampleThreads) {
-      uint32_t k;
-      if (!at(i, &k)) continue;
-      if (shift < 24 && (k >> (shift + 8)) != prefix) continue;
-      const uint32_t d = (k >> shift) & 255u;
-      atomicAdd(&sh.rcnt[d], 1u);
+    for (int32_t i = tid; i < n; i += kSampleThreads) {
+      const uint32_t k = key_at(i);
+      if (k < from || k > to) continue;
+      const uint32_t d = (k - from) >> shift;
       const uint32_t w = weight_of(r, of_key(k));
-      if (w != 0) atomicAdd(&sh.rmass[d], (u64)w);
+      atomicAdd(&sh.rcnt[d], 1u);
+      atomicAdd(&sh.rsum[0][d], w & 2047u);
+      atomicAdd(&sh.rsum[1][d], (w >> 11) & 2047u);
+      atomicAdd(&sh.rsum[2][d], w >> 22);
     }
     __syncthreads();
-    if (threadIdx.x < 32) {
+    if (tid < 32) {
       // lane l: digits 255 - 8 l .. 248 - 8 l, descending
-      const int lane = threadIdx.x;
+      auto mass_of = [&](int d) {
+        return (u64)sh.rsum[0][d] + ((u64)sh.rsum[1][d] << 11) + ((u64)sh.rsum[2][d] << 22);
+      };
       u64 v = 0, m = 0;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const int d = 255 - 8 * lane - i;
-        m += sh.rmass[d];
-        v += BY_COUNT ? (u64)sh.rcnt[d] : sh.rmass[d];
+        const int d = 255 - 8 * tid - i;
+        const u64 x = mass_of(d);
+        m += x;
+        v += by_count ? (u64)sh.rcnt[d] : x;
       }
       u64 vi = v, mi = m;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
         const u64 a = __shfl_up_sync(0xffffffffu, vi, o), b = __shfl_up_sync(0xffffffffu, mi, o);
-        if (lane >= o) {
+        if (tid >= o) {
           vi += a;
           mi += b;
         }
@@ -221,32 +251,194 @@ __device__ void select(const SampleRow& r, int32_t n, u64 need, SampleShared& sh
       const u64 left = sh.need, above = sh.above;
       __syncwarp();
       const uint32_t reach = __ballot_sync(0xffffffffu, vi >= left);
-      if (lane == (reach ? __ffs(reach) - 1 : 31)) {
+      if (tid == (reach ? __ffs(reach) - 1 : 31)) {
         u64 rest = left - (vi - v), over = above + (mi - m);
-        int d = 255 - 8 * lane;
+        int d = 255 - 8 * tid;
+#pragma unroll 1
         for (int i = 0; i < 7; ++i, --d) {
-          const u64 x = BY_COUNT ? (u64)sh.rcnt[d] : sh.rmass[d];
-          if (x >= rest) break;
-          rest -= x;
-          over += sh.rmass[d];
+          const u64 x = mass_of(d), y = by_count ? (u64)sh.rcnt[d] : x;
+          if (y >= rest) break;
+          rest -= y;
+          over += x;
         }
         sh.need = rest;
         sh.above = over;
-        sh.prefix = (prefix << 8) | (uint32_t)d;
+        sh.left = sh.rcnt[d];
+        const uint32_t base = from + ((uint32_t)d << shift);
+        sh.from = base;
+        sh.to = min(to, base + ((1u << shift) - 1u));
       }
     }
+    __syncthreads();
+  }
+  const uint32_t from = sh.from, to = sh.to;
+  if (sh.left <= kFew) {
+#pragma unroll 1
+    for (int32_t i = tid; i < n; i += kSampleThreads) {
+      const uint32_t k = key_at(i);
+      if (k < from || k > to) continue;
+      const uint32_t at = atomicAdd(&sh.n_few, 1u);
+      sh.few_key[at] = k;
+      sh.few_idx[at] = of_row ? i : sh.idx[i];
+    }
+    __syncthreads();
+    if (tid < 32) {
+      const int32_t n_few = (int32_t)sh.n_few;
+      const bool have = tid < n_few;
+      const uint32_t k = have ? sh.few_key[tid] : 0;
+      const int32_t i = have ? sh.few_idx[tid] : 0x7fffffff;
+      const uint32_t w = have ? weight_of(r, of_key(k)) : 0;
+      u64 before = 0;
+#pragma unroll 1
+      for (int j = 0; j < n_few; ++j) {
+        const uint32_t kj = __shfl_sync(0xffffffffu, k, j), wj = __shfl_sync(0xffffffffu, w, j);
+        const int32_t ij = __shfl_sync(0xffffffffu, i, j);
+        if (kj > k || (kj == k && ij < i)) before += by_count ? 1 : wj;
+      }
+      // the last entry that starts below the need
+      const bool kept = have && before < sh.need;
+      const u64 mine = kept ? before : 0;
+      u64 most = mine;
+      u64 mass = kept ? w : 0;
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) {
+        most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
+        mass += __shfl_xor_sync(0xffffffffu, mass, o);
+      }
+      // (entries of weight 0 may share a start: the last of them in the order)
+      uint32_t last_key = kept && mine == most ? k : 0xffffffffu;
+      last_key = __reduce_min_sync(0xffffffffu, last_key);
+      const int32_t last_idx =
+          __reduce_max_sync(0xffffffffu, kept && mine == most && k == last_key ? i : -1);
+      if (tid == 0) {
+        sh.cut = last_key;
+        sh.cut_idx = last_idx + 1;
+        sh.n_eq = 0;
+        sh.cut_mass = sh.above + mass;
+      }
+    }
+  } else if (tid == 0) {
+    const u64 w = weight_of(r, of_key(from));
+    sh.cut = from;
+    sh.n_eq = by_count ? sh.need : (w > 0 ? (sh.need + w - 1) / w : 1);
+    sh.cut_mass = sh.above + sh.n_eq * w;
   }
   __syncthreads();
-  *key = sh.prefix;
-  const u64 w = weight_of(r, of_key(sh.prefix));
-  *n_eq = BY_COUNT ? sh.need : (w > 0 ? (sh.need + w - 1) / w : 0);
-  *mass = sh.above + *n_eq * w;
 }
 
-// Bits cut off the weights of bin b so that a row's sum stays in 32 bits; the
-// sum of a bin is then short by less than 2^-kept of itself.
-__device__ __forceinline__ int shift_of(int32_t b, int wide) {
-  return max(0, (wide ? 20 : 16) - (b >> kBinsLog));
+// Index behind the n_eq-th entry of the row (in index order) that equals the cut.
+template <int MODE>
+__device__ __noinline__ void row_ties(SampleRow r, SampleShared& sh) {
+  const int32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const uint32_t cut = sh.cut;
+  const u64 n_eq = sh.n_eq;
+  if (threadIdx.x == 0) sh.cut_idx = 0x7fffffff;
+  u64 seen = 0;
+#pragma unroll 1
+  for (int32_t i0 = 0; i0 < r.V && seen < n_eq; i0 += kSampleThreads) {
+    const int32_t i = i0 + tid;
+    const bool eq = i < r.V && key_of(clean(load1<MODE>(r.x, r.inf, i))) == cut;
+    const uint32_t ball = __ballot_sync(0xffffffffu, eq);
+    __syncthreads();
+    if (lane == 0) sh.redi[warp] = __popc(ball);
+    __syncthreads();
+    u64 before = seen;
+    for (int w = 0; w < warp; ++w) before += sh.redi[w];
+    if (eq && before + __popc(ball & ((1u << lane) - 1u)) + 1 == n_eq) sh.cut_idx = i + 1;
+    for (int w = 0; w < kSampleWarps; ++w) seen += sh.redi[w];
+  }
+  __syncthreads();
+}
+
+// Sums over the row's entries (for certain kept, all), and the list, of pass B.
+struct PassB {
+  u64 sure, total;
+  uint32_t count;
+};
+
+// Pass B.  Entries x >= x_sure are kept for certain (as far as min-p lets them); those in
+// [x_p, x_sure) and [x_k, x_k1) go to the list; TOTAL: the mass of the rest of the
+// row counts too, else that of [x_k1, x_p).
+template <int MODE, bool TOTAL>
+__device__ __forceinline__ PassB pass_b(const SampleRow& r, SampleShared& sh, u64* chunk,
+                                        int32_t chunks, float x_sure, float x_p, float x_k1,
+                                        float x_k) {
+  const int32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const float end = fminf(x_p, x_k);
+  const bool all_kept = r.min_p <= 0x1p-32f;  // of the weights that are not 0
+  PassB out{0, 0, 0};
+#pragma unroll 1
+  for (int32_t ch = warp; ch < chunks; ch += kSampleWarps) {
+    float x[8];
+    load8<MODE>(r, ch, lane, x);
+    u64 s = 0;
+    if (TOTAL || __any_sync(0xffffffffu, max8(x) >= end)) {
+      uint32_t listed = 0;  // bit u: entry u goes to the list (or between its ranges)
+      u64 sum = 0;
+#pragma unroll
+      for (int u = 0; u < 8; u += 2) {
+        const float2 z = fmul2(below2(r.top, x[u], x[u + 1]), both(r.c));
+        const float2 e = fmul2(z, both(-1.f / kBinsPerLog2));
+        const float2 w = make_float2(ex2_approx(e.x), ex2_approx(e.y));
+        const float2 f = fmul2(w, both(0x1p31f));
+#pragma unroll
+        for (int v = 0; v < 2; ++v) {
+          const float xv = v ? x[u + 1] : x[u];
+          const uint32_t wi = __float2uint_rn(v ? f.y : f.x);  // 0 for a NaN and beyond 2^-32
+          const bool in = xv >= x_sure;
+          if (TOTAL) out.total = add_wide(out.total, wi);
+          uint32_t wk = in ? wi : 0;
+          if (!all_kept && !((v ? w.y : w.x) >= r.min_p)) {
+            out.sure = add_wide(out.sure, wk);  // mass that min-p drops
+            wk = 0;
+          }
+          sum = add_wide(sum, wk);
+          out.count += wk != 0 ? 1 : 0;
+          listed |= !in && xv >= end ? 1u << (u + v) : 0u;
+        }
+      }
+      out.sure += sum;
+      if (__any_sync(0xffffffffu, listed != 0)) {
+        // entries between the listed ranges only add their mass
+        uint32_t between = 0;
+        if (x_k1 < x_p) {
+#pragma unroll
+          for (int u = 0; u < 8; ++u)
+            if ((listed >> u & 1u) && x[u] < x_p && x[u] >= x_k1) between |= 1u << u;
+          listed &= ~between;
+        }
+        int32_t at = __popc(listed);
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const int32_t y = __shfl_up_sync(0xffffffffu, at, o);
+          if (lane >= o) at += y;
+        }
+        int32_t base = 0;
+        if (lane == 31 && at > 0) base = atomicAdd(&sh.n_list, at);
+        at += __shfl_sync(0xffffffffu, base, 31) - __popc(listed);
+        uint32_t left = listed | between;
+        while (left) {
+          const int u = __ffs(left) - 1;
+          left &= left - 1;
+          float xu = x[0];
+#pragma unroll
+          for (int i = 1; i < 8; ++i) xu = u == i ? x[i] : xu;
+          if (between >> u & 1u) {
+            out.total += weight_of(r, xu);
+            continue;
+          }
+          if (at < kList) {
+            sh.key[at] = key_of(clean(xu));
+            sh.idx[at] = index_of<MODE>(ch, u, lane);
+          }
+          ++at;
+        }
+      }
+      s = warp_sum35(sum);
+    }
+    if (lane == 0) chunk[ch] = s;
+  }
+  return out;
 }
 
 template <int MODE>
@@ -257,10 +449,17 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
   pdl_wait();
   const int32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int32_t chunks = (a.V + kChunk - 1) / kChunk;
-  // this warp's last chunk (negative: none)
-  const int32_t last_chunk =
-      warp < chunks ? warp + (chunks - 1 - warp) / kSampleWarps * kSampleWarps : -1;
-  const int wide = a.V > 65536;
+  auto block_max = [&](float m) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    __syncthreads();
+    if (lane == 0) sh.redf[warp] = m;
+    __syncthreads();
+    m = sh.redf[0];
+#pragma unroll
+    for (int w = 1; w < kSampleWarps; ++w) m = fmaxf(m, sh.redf[w]);
+    return m;
+  };
 #pragma unroll 1
   for (int32_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
     __syncthreads();
@@ -281,65 +480,87 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
     const float T = a.s.temperatures ? a.s.temperatures[row] : a.s.temperature;
     const int32_t k = a.s.top_ks ? a.s.top_ks[row] : a.s.top_k;
     const float top_p = a.s.top_ps ? a.s.top_ps[row] : a.s.top_p;
-    const float min_p = a.s.min_ps ? a.s.min_ps[row] : a.s.min_p;
+    SampleRow r;
+    r.min_p = a.s.min_ps ? a.s.min_ps[row] : a.s.min_p;
     if (!(T >= 0.f) || T == INFINITY || k < 0 || !(top_p > 0.f && top_p <= 1.f) ||
-        !(min_p >= 0.f && min_p <= 1.f)) {
+        !(r.min_p >= 0.f && r.min_p <= 1.f)) {
       if (tid == 0) record_status(a.status, SSD_ERR_DEVICE_BOUNDS);
       none();
       continue;
     }
-    SampleRow r;
     r.V = a.V;
     r.x = a.bf16 ? static_cast<const void*>(static_cast<const uint16_t*>(a.logits) + row * a.ld)
                  : static_cast<const void*>(static_cast<const float*>(a.logits) + row * a.ld);
-    r.min_p = min_p;
     r.c = T > 0.f ? fminf(kLog2e / T, kMaxC) * kBinsPerLog2 : 1.f;
     r.inf = false;
+    const float u_res = warp == 0 ? row_uniforms(a.rng, row).y : 0.f;
     const bool greedy = T == 0.f || k == 1;
-    const bool cut_k = k > 0 && k < r.V, cut_p = top_p < 1.f;
+    const bool cut_k = !greedy && k > 0 && k < r.V, cut_p = !greedy && top_p < 1.f;
 
-    // ---- A: the largest logit and its first index
-    // (a NaN loses every comparison; the lane's chunk that holds its first largest is kept)
-    float m = -INFINITY;
-    int32_t mc = 0;
-#pragma unroll 2
-    for (int32_t ch = warp; ch < chunks; ch += kSampleWarps) {
+    // ---- A: the largest logit, and the histogram under the largest of each warp's first
+    // chunk; once more where that one lies too far below the row's largest
+    float ref = 0.f;
+    if (cut_k || cut_p) {
       float x[8];
-      load8<MODE>(r, ch, lane, x);
-      const float y = fmax3(fmax3(x[0], x[1], x[2]), fmax3(x[3], x[4], x[5]), fmaxf(x[6], x[7]));
-      if (y > m) {
-        m = y;
-        mc = ch;
+      load8<MODE>(r, warp, lane, x);  // (beyond the row: -inf)
+      ref = block_max(max8(x));
+    }
+    float m;
+    int32_t mc = 0;  // this lane's chunk with its first largest
+#pragma unroll 1
+    while (true) {
+      m = -INFINITY;
+      const bool hist = (cut_k || cut_p) && ref > -INFINITY && ref < INFINITY;
+      if (hist) {
+#pragma unroll
+        for (int i = 0; i < kBins / kSampleThreads; ++i) sh.cnt[tid + i * kSampleThreads] = 0;
+        __syncthreads();
+#pragma unroll 2
+        for (int32_t ch = warp; ch < chunks; ch += kSampleWarps) {
+          float x[8];
+          load8<MODE>(r, ch, lane, x);
+          m = fmaxf(m, max8(x));
+#pragma unroll
+          for (int u = 0; u < 8; u += 2) {
+            const float2 b = ffma2(below2(ref, x[u], x[u + 1]), both(r.c), both((float)kHead));
+            // (bins above the first count as the first; a NaN fails the comparison)
+            if (b.x < (float)kBins) atomicAdd(&sh.cnt[__float2uint_rz(b.x)], 1u);
+            if (b.y < (float)kBins) atomicAdd(&sh.cnt[__float2uint_rz(b.y)], 1u);
+          }
+        }
+      } else {
+#pragma unroll 4
+        for (int32_t ch = warp; ch < chunks; ch += kSampleWarps) {
+          float x[8];
+          load8<MODE>(r, ch, lane, x);
+          const float y = max8(x);
+          if (y > m) {
+            m = y;
+            mc = ch;
+          }
+        }
       }
+      r.top = block_max(m);
+      if (!(cut_k || cut_p) || r.top == -INFINITY) break;
+      if (r.top == INFINITY && !r.inf) {
+        r.inf = true;  // from here on logits are 0 or -inf
+        ref = 0.f;
+        continue;
+      }
+      if (hist && bin_of(ref, r.c, r.top) >= 1.f) break;
+      ref = r.top;  // (bin_of is kHead for the reference itself)
     }
-    for (int i = tid; i < kBins; i += kSampleThreads) {
-      sh.mass[i] = 0;
-      sh.cnt[i] = 0;
-    }
-    if (tid == 0) {
-      sh.n_list = 0;
-      sh.cut_idx = 0x7fffffff;
-    }
-    float wm = m;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) wm = fmaxf(wm, __shfl_xor_sync(0xffffffffu, wm, o));
-    if (lane == 0) sh.redf[warp] = wm;
-    __syncthreads();
-    r.top = sh.redf[0];
-#pragma unroll
-    for (int w = 1; w < kSampleWarps; ++w) r.top = fmaxf(r.top, sh.redf[w]);
     if (r.top == -INFINITY) {
       none();
       continue;
     }
     if (greedy) {
       int32_t at = 0x7fffffff;
-      if (m == r.top) {
+      if (m == r.top)
         for (int u = 7; u >= 0; --u) {
           const int32_t i = index_of<MODE>(mc, u, lane);
-          if (i < r.V && load1<MODE>(r, i) == r.top) at = i;
+          if (i < r.V && load1<MODE>(r.x, false, i) == r.top) at = i;
         }
-      }
       at = __reduce_min_sync(0xffffffffu, at);
       if (lane == 0) sh.redi[warp] = at;
       __syncthreads();
@@ -351,252 +572,206 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
       }
       continue;
     }
-
-    if (r.top == INFINITY) {
+    if (r.top == INFINITY) {  // (without a cut)
       r.inf = true;
       r.top = 0.f;
     }
+    if (tid == 0) {
+      sh.n_list = 0;
+      sh.cut_idx = 0x7fffffff;
+      sh.cut = 0;
+      sh.n_eq = 0;
+      sh.bin_k = kBins;  // top-k takes every entry with a weight
+      sh.bin_lo = sh.bin_hi = kBins;
+    }
 
-    // ---- B: the bins of the cuts.  From the row's end, which was read last.
-    u64 total = 0;  // mass of the row (with top-p)
+    // ---- the bins of the cuts.  Thread t: bins kPer t .. and the sums before them.
+    // Keys: x >= of_key(edge[0]): kept for certain; edge[1]: end of the top-p bins;
+    // edge[2], edge[3]: start and end of the top-k bin
+    uint32_t key_sure = 0, key_p = 0xffffffffu, key_k1 = 0xffffffffu, key_k = 0xffffffffu;
     if (cut_k || cut_p) {
-#pragma unroll 1
-      for (int32_t ch = last_chunk; ch >= 0; ch -= kSampleWarps) {
-        float x[8];
-        load8<MODE>(r, ch, lane, x);
-#pragma unroll
-        for (int u = 0; u < 8; ++u) {
-          const float z = bins_of(r, x[u]);
-          const bool in = z < (float)kBins;
-          const int32_t b = (int32_t)fminf(z, (float)kBins);
-          if (cut_p) {
-            const uint32_t w = weight_i(weight_f(fminf(z, (float)kBins)));  // 0 at kBins
-            total += w;
-            if (in) atomicAdd(&sh.mass[b], w >> shift_of(b, wide));
-          }
-          if (cut_k && in) atomicAdd(&sh.cnt[b], 1u);
-        }
-      }
-      if (cut_p) total = block_sum64(total, sh.red);
-      __syncthreads();
-      // thread t: bins 4 t .. 4 t + 3 and the sums before them.  The mass up to a bin is
-      // known from below and above by what was cut off the weights before it, and, with the
-      // row's exact mass, by what was cut off behind it.
       constexpr int kPer = kBins / kSampleThreads;
       static_assert(kPer * kSampleThreads == kBins, "bins per thread");
-      const float over = wide ? 0x1p-9f : 0x1p-13f;  // a bin's mass is short by less than this
-      auto low_of = [&](int b) { return (u64)sh.mass[b] << shift_of(b, wide); };
-      auto high_of = [&](int b) {
-        const u64 q = low_of(b);
-        return shift_of(b, wide) == 0 || q == 0 ? q : q + (u64)((float)q * over) + 1;
-      };
-      u64 n = 0, lo = 0, hi = 0;
+      int32_t n = 0;
+      float mass = 0.f, var = 0.f;
+      const float w0 = exp2f(((float)kHead - 0.5f - (float)(tid * kPer)) / kBinsPerLog2);
+      constexpr float kStep = 0.99459942f;  // 2^(-1/128)
+      float w = w0;
 #pragma unroll
       for (int i = 0; i < kPer; ++i) {
-        const int b = tid * kPer + i;
-        n += sh.cnt[b];
-        lo += low_of(b);
-        hi += high_of(b);
+        const int32_t cn = sh.cnt[tid * kPer + i];
+        const float q = (float)cn * w;
+        n += cn;
+        mass += q;
+        var += q * q;
+        w *= kStep;
       }
-      u64 n0 = 0, lo0 = 0, hi0 = 0, lo_all = 0, hi_all = 0;
-      if (cut_k) n0 = block_scan64(n, sh.red) - n;
-      if (cut_p) {
-        lo0 = block_scan64(lo, sh.red) - lo;
-        hi0 = block_scan64(hi, sh.red2) - hi;
-        lo_all = block_sum64(lo, sh.red);
-        hi_all = block_sum64(hi, sh.red2);
+      int32_t n1 = n;
+      float m1 = mass;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int32_t y = __shfl_up_sync(0xffffffffu, n1, o);
+        const float z = __shfl_up_sync(0xffffffffu, m1, o);
+        if (lane >= o) {
+          n1 += y;
+          m1 += z;
+        }
       }
-      // mass up to a bin whose sums are l and h
-      auto least_upto = [&](u64 l, u64 h) { return max(l, total + h > hi_all ? total + h - hi_all : 0); };
-      auto most_upto = [&](u64 l, u64 h) { return min(h, total + l - lo_all); };
-      if (tid == 0) {
-        sh.bin_k = kBins;  // top-k takes every entry with a weight
-        sh.bin_lo = sh.bin_hi = kBins;
-        sh.upto_k_lo = sh.upto_k_hi = total;
+      var = warp_sum(var);
+      __syncthreads();
+      if (lane == 31) {
+        sh.redi[warp] = n1;
+        sh.redf[warp] = m1;
+        sh.redf2[warp] = var;
       }
       __syncthreads();
-      if (cut_k && n0 < (u64)k && (u64)k <= n0 + n) {
-        u64 s = n0, l = lo0, h = hi0;
+      float total = 0.f;
+      var = 0.f;
+#pragma unroll
+      for (int w2 = 0; w2 < kSampleWarps; ++w2) {
+        if (w2 < warp) {
+          n1 += sh.redi[w2];
+          m1 += sh.redf[w2];
+        }
+        total += sh.redf[w2];
+        var += sh.redf2[w2];
+      }
+      const int32_t n0 = n1 - n;
+      const float m0 = m1 - mass;
+      if (tid == 0) {
+        sh.k_mass = total;
+        sh.k_mass_err = 0.f;
+      }
+      __syncthreads();
+      if (cut_k && n0 < k && k <= n1) {
+        int32_t s = n0;
+        float before = m0;
+        w = w0;
         for (int i = 0; i < kPer; ++i) {
-          const int b = tid * kPer + i;
-          if (s + sh.cnt[b] >= (u64)k) {
-            sh.bin_k = b;
-            sh.need = k - s;  // entries of the bin within top-k
-            sh.upto_k_lo = least_upto(l, h);  // mass of the k entries, from below and above
-            sh.upto_k_hi = most_upto(l + low_of(b), h + high_of(b));
+          const int32_t cn = sh.cnt[tid * kPer + i];
+          if (s + cn >= k) {
+            sh.bin_k = tid * kPer + i;
+            sh.need_k = k - s;  // entries of the bin within top-k
+            sh.k_mass = before + (float)(k - s) * w;
+            sh.k_mass_err = (float)(k - s) * w * (2.f * kBinSpread);
             break;
           }
-          s += sh.cnt[b];
-          l += low_of(b);
-          h += high_of(b);
+          s += cn;
+          before += (float)cn * w;
+          w *= kStep;
         }
       }
       __syncthreads();
       if (cut_p) {
-        const double p = top_p;
-        const u64 least = (u64)ceil(p * (double)sh.upto_k_lo), most = (u64)ceil(p * (double)sh.upto_k_hi);
-        u64 l = lo0, h = hi0;
+        const float err = sh.k_mass_err + 5.f * kBinSpread * sqrtf(var) + 1e-4f * sh.k_mass;
+        const float least = top_p * sh.k_mass - err, most = top_p * sh.k_mass + err;
+        float before = m0;
+        w = w0;
+        if (tid == 0 && least <= 0.f) sh.bin_lo = 0;
+#pragma unroll 1
         for (int i = 0; i < kPer; ++i) {
-          const int b = tid * kPer + i;
-          const u64 l1 = l + low_of(b), h1 = h + high_of(b);
-          // the first bin by which the least wanted can be reached, and the first by
-          // which the most wanted is: the cut is in one of them or between
-          if (most_upto(l, h) < least && least <= most_upto(l1, h1)) sh.bin_lo = b;
-          if (least_upto(l, h) < most && most <= least_upto(l1, h1)) sh.bin_hi = b;
-          l = l1;
-          h = h1;
+          const float upto = before + (float)sh.cnt[tid * kPer + i] * w;
+          // (several threads may find one where sums are rounded: any will do)
+          if (before < least && least <= upto) sh.bin_lo = tid * kPer + i;
+          if (before < most && most <= upto) sh.bin_hi = tid * kPer + i;
+          before = upto;
+          w *= kStep;
         }
       }
       __syncthreads();
-    }
-    const int32_t bin_k = cut_k ? sh.bin_k : kBins;
-    const u64 need_k = cut_k && bin_k < kBins ? sh.need : 0;
-    const int32_t bin_lo = cut_p ? sh.bin_lo : kBins;
-    const int32_t bin_hi = cut_p ? min(sh.bin_hi, kBins - 1) : -1;
-    // entries kept for certain: z in bins below these
-    const float sure = (float)min(bin_lo, bin_k);
-    __syncthreads();
-
-    // entries between the top-p bins and the top-k one count for top-p's mass
-    const float gap = cut_p && bin_hi < bin_k && bin_k < kBins ? (float)(bin_hi + 1) : (float)kBins;
-    const float behind = (float)min(kBins, cut_k && bin_k < kBins ? bin_k + 1 : bin_hi + 1);
-    const float limit = cut_k || cut_p ? fmaxf(sure, behind) : (float)kBins;
-
-    // ---- C: exact masses by chunk, and the list
-    u64 upto = 0, mid = 0;  // masses before the listed bins, and between them
-    uint32_t count = 0;
-#pragma unroll 1
-    for (int32_t ch = warp; ch < chunks; ch += kSampleWarps) {
-      float x[8];
-      load8<MODE>(r, ch, lane, x);
-      float z[8], least = INFINITY;
-#pragma unroll
-      for (int u = 0; u < 8; ++u) {
-        z[u] = bins_of(r, x[u]);
-        least = fminf(least, z[u]);
-      }
-      u64 s = 0;
-      if (__any_sync(0xffffffffu, least < limit)) {
-        bool other = false;
-#pragma unroll
-        for (int u = 0; u < 8; ++u) {
-          const float w = weight_f(fminf(z[u], (float)kBins));
-          const bool in = z[u] < sure;
-          const uint32_t wi = in ? weight_i(w) : 0;
-          upto += wi;
-          const uint32_t wk = w >= r.min_p ? wi : 0;
-          s += wk;
-          count += wk != 0;
-          other |= !in && z[u] < limit;
+      const int32_t bin_k = sh.bin_k;
+      const int32_t bin_lo = min(cut_p ? sh.bin_lo : kBins, bin_k);
+      const int32_t bin_hi = cut_p ? min(max(sh.bin_hi, bin_lo), bin_k) : -1;
+      if (warp < 4) {
+        // least key whose bin is below the edge (bin_of is monotone): each step looks at 32
+        // keys of those left
+        const int32_t edge = warp == 0 ? bin_lo : warp == 1 ? bin_hi + 1
+                             : warp == 2 ? bin_k : bin_k + 1;
+        uint32_t lo = key_of(-INFINITY), hi = key_of(INFINITY);
+        while (lo < hi) {
+          const uint32_t step = (hi - lo) / 32 + 1;
+          const uint32_t at = lo + min((uint32_t)lane * step, hi - lo);
+          const uint32_t below =
+              __ballot_sync(0xffffffffu, at == hi || bin_of(ref, r.c, of_key(at)) < (float)edge);
+          const int f = below ? __ffs(below) - 1 : 32;  // the first of them
+          const uint32_t top = f < 32 ? lo + min((uint32_t)f * step, hi - lo) : hi;
+          if (f > 0) lo = lo + min((uint32_t)(f - 1) * step, hi - lo) + 1;
+          hi = top;
+          if (f == 0) break;
         }
-        if (other) {
-#pragma unroll
-          for (int u = 0; u < 8; ++u) {
-            if (!(z[u] >= sure && z[u] < limit)) continue;
-            const int32_t b = (int32_t)z[u];
-            if (b == bin_k || (b >= bin_lo && b <= bin_hi)) {
-              const int32_t at = atomicAdd(&sh.n_list, 1);
-              if (at < kList) {
-                sh.key[at] = key_of(clean(x[u]));
-                sh.idx[at] = index_of<MODE>(ch, u, lane);
-              }
-            } else if (z[u] >= gap) {
-              mid += weight_i(weight_f(z[u]));
-            }
+        if (lane == 0) sh.edge[warp] = hi;
+      }
+      __syncthreads();
+      key_sure = sh.edge[0];
+      if (cut_p) key_p = sh.edge[1];
+      if (bin_k < kBins) {
+        key_k1 = sh.edge[2];
+        key_k = sh.edge[3];
+      }
+    } else {
+      key_sure = key_of(-INFINITY);
+      __syncthreads();
+    }
+    // the k-th entry's bin ends the order; without one, every entry counts for top-p's mass
+    const bool has_k = key_k != 0xffffffffu;
+    key_p = min(key_p, key_sure);
+
+    // ---- B
+    auto at_key = [](uint32_t key) { return key == 0xffffffffu ? INFINITY : of_key(key); };
+    const PassB pb = cut_p && !has_k
+                         ? pass_b<MODE, true>(r, sh, chunk, chunks, at_key(key_sure), at_key(key_p),
+                                              INFINITY, INFINITY)
+                         : pass_b<MODE, false>(r, sh, chunk, chunks, at_key(key_sure), at_key(key_p),
+                                               at_key(key_k1), at_key(key_k));
+    uint32_t count = pb.count;
+    bool by_row = false;  // the chunks' masses are to be summed again
+    if (cut_k || cut_p) {
+      u64 sure = 0, rest = 0;  // rest: all of the row, or what lies between the listed bins
+      if (cut_p) {
+        sure = block_sum64(pb.sure, sh.red);
+        rest = block_sum64(pb.total, sh.red2);
+      }
+      __syncthreads();
+      const bool overflow = sh.n_list > kList;
+      by_row = overflow;
+      if (has_k) select<MODE>(r, sh, overflow, true, (u64)sh.need_k, key_k, key_k1 - 1);
+      if (cut_p) {
+        u64 k_mass = rest, listed = 0;
+        // mass of the listed entries before the top-k bin
+        if (!overflow) {
+          for (int32_t i = tid; i < sh.n_list; i += kSampleThreads)
+            if (sh.key[i] >= key_p && (!has_k || sh.key[i] >= key_k1)) listed += weight_of(r, of_key(sh.key[i]));
+        } else {
+#pragma unroll 1
+          for (int32_t i = tid; i < r.V; i += kSampleThreads) {
+            const float x = load1<MODE>(r.x, r.inf, i);
+            const uint32_t key = key_of(clean(x));
+            if (key >= key_p && key < key_sure && (!has_k || key >= key_k1)) listed += weight_of(r, x);
           }
         }
-        s = warp_sum35(s);
+        listed = block_sum64(listed, sh.red);
+        if (has_k) k_mass = sure + rest + listed + sh.cut_mass;
+        const u64 need = (u64)ceil((double)top_p * (double)k_mass);
+        // what the listed top-p bins reach: with the top-k bin among them, all of it
+        const bool with_k = has_k && key_p <= key_k;
+        const u64 reach = sure + listed + (with_k ? sh.cut_mass : 0);
+        if (need > sure && need <= reach) {
+          select<MODE>(r, sh, overflow, false, need - sure, with_k ? key_k : key_p, key_sure - 1);
+        } else {
+          // the estimate was off: the cut is not in the listed bins
+          by_row = true;
+          select<MODE>(r, sh, true, false, need, key_of(-INFINITY), key_of(r.top));
+        }
       }
-      if (lane == 0) chunk[ch] = s;
-    }
-    if (cut_p) {
-      upto = block_sum64(upto, sh.red);
-      mid = block_sum64(mid, sh.red2);
+      if (sh.n_eq != 0) row_ties<MODE>(r, sh);  // equal entries at the cut, too many for a warp
     }
     __syncthreads();
-    const int32_t n_list = sh.n_list;
-    uint32_t cut = 0;
-    u64 n_eq = ~0ull;
-    if (n_list > kList) {
-      // too many entries where a cut falls: the radix search over the whole row
-      auto of_row = [&](int32_t i, uint32_t* key) {
-        *key = key_of(clean(load1<MODE>(r, i)));
-        return true;
-      };
-      u64 mass;
-      total = 0;
-      if (cut_k) {
-        select<true>(r, r.V, (u64)k, sh, of_row, &cut, &n_eq, &total);
-      } else {
-        for (int32_t i = tid; i < r.V; i += kSampleThreads)
-          total += weight_of(r, load1<MODE>(r, i));
-        total = block_sum64(total, sh.red);
-      }
-      if (cut_p) {
-        const u64 need = (u64)ceil((double)top_p * (double)total);
-        select<false>(r, r.V, need, sh, of_row, &cut, &n_eq, &mass);
-      }
-      // index behind the last kept entry equal to the cut
-      u64 seen = 0;
-#pragma unroll 1
-      for (int32_t i0 = 0; i0 < r.V && seen < n_eq; i0 += kSampleThreads) {
-        const int32_t i = i0 + tid;
-        const bool eq = i < r.V && key_of(clean(load1<MODE>(r, i))) == cut;
-        const uint32_t ball = __ballot_sync(0xffffffffu, eq);
-        __syncthreads();
-        if (lane == 0) sh.redi[warp] = __popc(ball);
-        __syncthreads();
-        u64 before = seen;
-        for (int w = 0; w < warp; ++w) before += sh.redi[w];
-        if (eq && before + __popc(ball & ((1u << lane) - 1u)) + 1 == n_eq) sh.cut_idx = i + 1;
-        for (int w = 0; w < kSampleWarps; ++w) seen += sh.redi[w];
-      }
-      __syncthreads();
-    } else if (n_list > 0) {
-      auto bin = [&](uint32_t key) { return (int32_t)bins_of(r, of_key(key)); };
-      u64 in_k = 0, mass;  // mass of the entries of the top-k bin within top-k
-      if (cut_k && bin_k < kBins) {
-        auto of_k = [&](int32_t i, uint32_t* key) {
-          *key = sh.key[i];
-          return bin(*key) == bin_k;
-        };
-        select<true>(r, n_list, need_k, sh, of_k, &cut, &n_eq, &in_k);
-      }
-      if (cut_p) {
-        // the k entries' mass: before, between and in the listed bins
-        u64 s = 0;
-        for (int32_t i = tid; i < n_list; i += kSampleThreads) {
-          if (bin(sh.key[i]) != bin_k) s += weight_of(r, of_key(sh.key[i]));
-        }
-        s = block_sum64(s, sh.red);
-        const u64 k_mass = bin_k < kBins ? upto + mid + s + in_k : total;
-        const u64 need = (u64)ceil((double)top_p * (double)k_mass);
-        auto listed = [&](int32_t i, uint32_t* key) {
-          *key = sh.key[i];
-          return true;
-        };
-        // (need > upto: the bins before the listed ones cannot reach it; the k-th
-        // entry can, so no entry behind it gets in)
-        select<false>(r, n_list, need - upto, sh, listed, &cut, &n_eq, &mass);
-      }
-      if (n_eq != ~0ull) {
-        // the n_eq-th lowest index of the entries equal to the cut
-        for (int32_t i = tid; i < n_list; i += kSampleThreads) {
-          if (sh.key[i] != cut) continue;
-          u64 below = 0;
-          for (int32_t j = 0; j < n_list; ++j) below += sh.key[j] == cut && sh.idx[j] < sh.idx[i];
-          if (below + 1 == n_eq) sh.cut_idx = sh.idx[i] + 1;
-        }
-      }
-      __syncthreads();
-    }
-    const bool by_row = n_list > kList;
+    const uint32_t cut = sh.cut;
     const int32_t cut_idx = sh.cut_idx;
     auto kept_weight = [&](float x, int32_t i) -> uint32_t {
       const uint32_t kx = key_of(clean(x));
-      const float z = bins_of(r, x);
-      if (kx < cut || (kx == cut && i >= cut_idx) || !(z < (float)kBins)) return 0;
-      const float w = weight_f(z);
+      if (kx < cut || (kx == cut && i >= cut_idx)) return 0;
+      const float w = weight_f(r, x);
       return w >= r.min_p ? weight_i(w) : 0;
     };
     // the listed entries that are kept, into their chunks (or every entry again)
@@ -617,6 +792,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
         if (lane == 0) chunk[ch] = s;
       }
     } else {
+      const int32_t n_list = sh.n_list;
       for (int32_t i = tid; i < n_list; i += kSampleThreads) {
         const uint32_t w = kept_weight(of_key(sh.key[i]), sh.idx[i]);
         if (w == 0) continue;
@@ -624,10 +800,14 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
         atomicAdd(&chunk[sh.idx[i] / kChunk], (u64)w);
       }
     }
-    const u64 n_kept = block_sum64(count, sh.red);
+    count = __reduce_add_sync(0xffffffffu, count);
+    if (lane == 0) sh.redi[warp] = (int32_t)count;
+    __syncthreads();
 
     // ---- the draw
     if (warp == 0) {
+      count = lane < kSampleWarps ? sh.redi[lane] : 0;
+      count = __reduce_add_sync(0xffffffffu, count);
       const int32_t per = (chunks + 31) / 32;
       u64 s = 0;
       for (int32_t i = 0; i < per; ++i) s += lane * per + i < chunks ? chunk[lane * per + i] : 0;
@@ -638,7 +818,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
         if (lane >= o) incl += y;
       }
       const u64 Z = __shfl_sync(0xffffffffu, incl, 31);
-      const u64 aim = (u64)((double)row_uniforms(a.rng, row).y * (double)Z);
+      const u64 aim = (u64)((double)u_res * (double)Z);
       // sums are whole: sum > u Z iff sum > floor(u Z)
       const uint32_t reach = __ballot_sync(0xffffffffu, incl > aim);
       const int32_t l0 = reach ? __ffs(reach) - 1 : 31;
@@ -652,29 +832,40 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
       }
       ch = __shfl_sync(0xffffffffu, ch, l0);
       before = __shfl_sync(0xffffffffu, before, l0);
+      // the chunk, eight entries in a row to a lane
+      uint32_t w[8];
+      u64 c = 0;
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const int32_t i = ch * kChunk + lane * 8 + u;
+        w[u] = i < r.V ? kept_weight(load1<MODE>(r.x, r.inf, i), i) : 0;
+        c += w[u];
+      }
+      u64 ci = c;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const u64 y = __shfl_up_sync(0xffffffffu, ci, o);
+        if (lane >= o) ci += y;
+      }
+      const uint32_t hit = __ballot_sync(0xffffffffu, before + ci > aim);
+      const int32_t l1 = hit ? __ffs(hit) - 1 : 31;
+      before += ci - c;
       int32_t pick = -1;
       uint32_t wp = 0;
-#pragma unroll 1
-      for (int32_t u = 0; u < 8 && pick < 0; ++u) {
-        const int32_t i = ch * kChunk + u * 32 + lane;
-        const uint32_t w = i < r.V ? kept_weight(load1<MODE>(r, i), i) : 0;
-        u64 c = w;
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-          const u64 y = __shfl_up_sync(0xffffffffu, c, o);
-          if (lane >= o) c += y;
+      for (int u = 0; u < 8; ++u) {
+        before += w[u];
+        if (pick < 0 && before > aim) {
+          pick = ch * kChunk + lane * 8 + u;
+          wp = w[u];
         }
-        const uint32_t hit = __ballot_sync(0xffffffffu, before + c > aim);
-        if (hit) {
-          pick = __shfl_sync(0xffffffffu, i, __ffs(hit) - 1);
-          wp = __shfl_sync(0xffffffffu, w, __ffs(hit) - 1);
-        }
-        before += __shfl_sync(0xffffffffu, c, 31);
       }
+      pick = __shfl_sync(0xffffffffu, pick, l1);
+      wp = __shfl_sync(0xffffffffu, wp, l1);
       if (lane == 0) {
         a.out_tok[row] = pick;
         if (a.prob) a.prob[row] = (float)((double)wp / (double)Z);
-        if (a.kept) a.kept[row] = (int32_t)n_kept;
+        if (a.kept) a.kept[row] = (int32_t)count;
       }
     }
   }

@@ -19,6 +19,7 @@
 // list takes (equal logits, high temperatures), the search runs over the row's entries
 // in those bins; where the exact masses show the cut to be elsewhere, over the whole row.
 #include <algorithm>
+#include <type_traits>
 
 #include "kernels.cuh"
 
@@ -163,6 +164,7 @@ struct SampleShared {
   float k_mass;               // estimated mass of the first k entries, and its error
   float k_mass_err;
   uint32_t edge[4];           // least keys above the bins' edges
+  uint32_t floor_key;         // least key with a weight
 };
 
 __device__ __forceinline__ u64 block_sum64(u64 v, u64* red) {
@@ -350,6 +352,25 @@ __device__ __noinline__ void row_ties(SampleRow r, SampleShared& sh) {
   __syncthreads();
 }
 
+// The least key above which a condition on the logit, monotone, holds (one warp: each
+// step looks at 32 keys of those left).
+template <typename F>
+__device__ __forceinline__ uint32_t least_key(int lane, F holds) {
+  uint32_t lo = key_of(-INFINITY), hi = key_of(INFINITY);
+#pragma unroll 1
+  while (lo < hi) {
+    const uint32_t step = (hi - lo) / 32 + 1;
+    const uint32_t at = lo + min((uint32_t)lane * step, hi - lo);
+    const uint32_t yes = __ballot_sync(0xffffffffu, at == hi || holds(of_key(at)));
+    const int f = yes ? __ffs(yes) - 1 : 32;  // the first of them
+    const uint32_t top = f < 32 ? lo + min((uint32_t)f * step, hi - lo) : hi;
+    if (f > 0) lo += min((uint32_t)(f - 1) * step, hi - lo) + 1;
+    hi = top;
+    if (f == 0) break;
+  }
+  return hi;
+}
+
 // Sums over the row's entries (for certain kept, all), and the list, of pass B.
 struct PassB {
   u64 sure, total;
@@ -373,32 +394,46 @@ __device__ __forceinline__ PassB pass_b(const SampleRow& r, SampleShared& sh, u6
     load8<MODE>(r, ch, lane, x);
     u64 s = 0;
     if (TOTAL || __any_sync(0xffffffffu, max8(x) >= end)) {
-      uint32_t listed = 0;  // bit u: entry u goes to the list (or between its ranges)
       u64 sum = 0;
+      int32_t n_in = 0, n_end = 0;
+      // (x_sure is at least the least logit with a weight: what is kept has one)
+      auto entries = [&](auto min_p) {
 #pragma unroll
-      for (int u = 0; u < 8; u += 2) {
-        const float2 z = fmul2(below2(r.top, x[u], x[u + 1]), both(r.c));
-        const float2 e = fmul2(z, both(-1.f / kBinsPerLog2));
-        const float2 w = make_float2(ex2_approx(e.x), ex2_approx(e.y));
-        const float2 f = fmul2(w, both(0x1p31f));
+        for (int u = 0; u < 8; u += 2) {
+          const float2 z = fmul2(below2(r.top, x[u], x[u + 1]), both(r.c));
+          const float2 e = fmul2(z, both(-1.f / kBinsPerLog2));
+          const float2 w = make_float2(ex2_approx(e.x), ex2_approx(e.y));
+          const float2 f = fmul2(w, both(0x1p31f));
 #pragma unroll
-        for (int v = 0; v < 2; ++v) {
-          const float xv = v ? x[u + 1] : x[u];
-          const uint32_t wi = __float2uint_rn(v ? f.y : f.x);  // 0 for a NaN and beyond 2^-32
-          const bool in = xv >= x_sure;
-          if (TOTAL) out.total = add_wide(out.total, wi);
-          uint32_t wk = in ? wi : 0;
-          if (!all_kept && !((v ? w.y : w.x) >= r.min_p)) {
-            out.sure = add_wide(out.sure, wk);  // mass that min-p drops
-            wk = 0;
+          for (int v = 0; v < 2; ++v) {
+            const float xv = v ? x[u + 1] : x[u];
+            const uint32_t wi = __float2uint_rn(v ? f.y : f.x);  // 0 for a NaN and beyond 2^-32
+            bool in = xv >= x_sure;
+            n_end += xv >= end ? 1 : 0;
+            if (TOTAL) out.total = add_wide(out.total, wi);
+            if constexpr (decltype(min_p)::value) {
+              out.sure = add_wide(out.sure, in ? wi : 0);
+              n_end -= in ? 1 : 0;
+              in = in && (v ? w.y : w.x) >= r.min_p;
+              n_end += in ? 1 : 0;
+            }
+            sum = add_wide(sum, in ? wi : 0);
+            n_in += in ? 1 : 0;
           }
-          sum = add_wide(sum, wk);
-          out.count += wk != 0 ? 1 : 0;
-          listed |= !in && xv >= end ? 1u << (u + v) : 0u;
         }
+      };
+      if (all_kept) {
+        entries(std::false_type());
+        out.sure += sum;
+      } else {
+        entries(std::true_type());
       }
-      out.sure += sum;
-      if (__any_sync(0xffffffffu, listed != 0)) {
+      out.count += n_in;
+      if (__any_sync(0xffffffffu, n_end != n_in)) {
+        // the entries of this chunk that go to the list, or lie between its ranges (bit u)
+        uint32_t listed = 0;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) listed |= x[u] >= end && x[u] < x_sure ? 1u << u : 0u;
         // entries between the listed ranges only add their mass
         uint32_t between = 0;
         if (x_k1 < x_p) {
@@ -585,6 +620,12 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
       sh.bin_lo = sh.bin_hi = kBins;
     }
 
+    if (warp == kSampleWarps - 1) {
+      // the least logit with a weight: rounding makes the others 0
+      const uint32_t at = least_key(lane, [&](float x) { return weight_of(r, x) != 0; });
+      if (lane == 0) sh.floor_key = at;
+    }
+
     // ---- the bins of the cuts.  Thread t: bins kPer t .. and the sums before them.
     // Keys: x >= of_key(edge[0]): kept for certain; edge[1]: end of the top-p bins;
     // edge[2], edge[3]: start and end of the top-k bin
@@ -683,23 +724,11 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
       const int32_t bin_lo = min(cut_p ? sh.bin_lo : kBins, bin_k);
       const int32_t bin_hi = cut_p ? min(max(sh.bin_hi, bin_lo), bin_k) : -1;
       if (warp < 4) {
-        // least key whose bin is below the edge (bin_of is monotone): each step looks at 32
-        // keys of those left
         const int32_t edge = warp == 0 ? bin_lo : warp == 1 ? bin_hi + 1
                              : warp == 2 ? bin_k : bin_k + 1;
-        uint32_t lo = key_of(-INFINITY), hi = key_of(INFINITY);
-        while (lo < hi) {
-          const uint32_t step = (hi - lo) / 32 + 1;
-          const uint32_t at = lo + min((uint32_t)lane * step, hi - lo);
-          const uint32_t below =
-              __ballot_sync(0xffffffffu, at == hi || bin_of(ref, r.c, of_key(at)) < (float)edge);
-          const int f = below ? __ffs(below) - 1 : 32;  // the first of them
-          const uint32_t top = f < 32 ? lo + min((uint32_t)f * step, hi - lo) : hi;
-          if (f > 0) lo = lo + min((uint32_t)(f - 1) * step, hi - lo) + 1;
-          hi = top;
-          if (f == 0) break;
-        }
-        if (lane == 0) sh.edge[warp] = hi;
+        const uint32_t at =
+            least_key(lane, [&](float x) { return bin_of(ref, r.c, x) < (float)edge; });
+        if (lane == 0) sh.edge[warp] = at;
       }
       __syncthreads();
       key_sure = sh.edge[0];
@@ -709,12 +738,13 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
         key_k = sh.edge[3];
       }
     } else {
-      key_sure = key_of(-INFINITY);
       __syncthreads();
     }
+    const uint32_t key_floor = sh.floor_key;
+    key_sure = max(key_sure, key_floor);
     // the k-th entry's bin ends the order; without one, every entry counts for top-p's mass
     const bool has_k = key_k != 0xffffffffu;
-    key_p = min(key_p, key_sure);
+    key_p = max(min(key_p, key_sure), key_floor);
 
     // ---- B
     auto at_key = [](uint32_t key) { return key == 0xffffffffu ? INFINITY : of_key(key); };

@@ -7,10 +7,10 @@
 // top-p by mass, min-p by weight.  One block of threads takes a row, which it reads twice,
 // from HBM and then from L2 (a row of 65536 float32 logits is 256 KB):
 //  A the largest logit, and a histogram of the logits in bins of 1/128 of a factor of
-//    two of weight (one 32-bit atomic an entry; the bins hang on the largest of the row's first
-//    entries, since the largest of all is not known yet).  The counts give the bin of the
-//    k-th entry exactly, and, each entry taken at its bin's middle, the bins where the
-//    top-p cut falls, with a margin of five standard deviations of that estimate;
+//    two of weight: the entries of a bin and the sum of their places in it, in 1/256 of the bin
+//    (the bins hang on the largest of the row's first entries, since the largest of all is not
+//    known yet).  The counts give the bin of the k-th entry exactly; with the places a bin's
+//    mass is known to 2^-16, which gives the one or two bins where the top-p cut falls;
 //  B the exact weights: the mass of what is kept for certain, by chunks of 256
 //    entries, and a list of the few entries in the bins where a cut falls.
 // A radix search over the list (exact counts and masses) finds both cuts, ties are
@@ -37,8 +37,11 @@ constexpr int kBins = kHead + 32 * kPerLog2;  // and below it: from 2^-32 on wei
 constexpr float kMaxC = 0x1p100f;      // largest log2(e) / T
 constexpr int kList = 4096;
 constexpr float kLog2e = 1.4426950408889634f;
-// Standard deviation of log-uniform weights in a bin over their mean: ln 2 / 128 / sqrt(12)
-constexpr float kBinSpread = 0.00157f;
+constexpr int kPlaces = 256;              // places in a bin
+constexpr float kBinLn = 0.0054152123f;   // ln 2 / 128: log of the ratio of a bin's edges
+// A bin's mass is taken at its entries' mean place: off by half a place's width (2^-17) and
+// by the curvature of the exponential (kBinLn^2 / 8), and the sums by their roundings.
+constexpr float kMassErr = 0x1p-15f;
 constexpr int kFew = 32;                  // entries that one warp orders by itself
 typedef unsigned long long u64;
 
@@ -91,9 +94,12 @@ __device__ __forceinline__ float weight_f(const SampleRow& r, float x) {
 __device__ __forceinline__ uint32_t weight_of(const SampleRow& r, float x) {
   return weight_i(weight_f(r, x));
 }
-// A logit's bin under the reference logit `ref`, as a float: descending in x.
+// A logit's bin under the reference logit `ref`, times kPlaces: descending in x.
+__device__ __forceinline__ float2 bin2_of(float ref, float c, float x0, float x1) {
+  return ffma2(below2(ref, x0, x1), both(c * kPlaces), both((float)(kHead * kPlaces)));
+}
 __device__ __forceinline__ float bin_of(float ref, float c, float x) {
-  return fmaf(__fsub_rn(ref, x), c, (float)kHead);
+  return fmaf(__fsub_rn(ref, x), c * kPlaces, (float)(kHead * kPlaces));
 }
 
 template <int MODE>
@@ -144,6 +150,7 @@ __device__ __forceinline__ float max8(const float (&x)[8]) {  // NaN loses
 
 struct SampleShared {
   uint32_t cnt[kBins];
+  uint32_t place[kBins];
   uint32_t key[kList];  // the list
   int32_t idx[kList];
   uint32_t rsum[3][256];  // radix search: the masses' 11, 11 and 10 bits, each summed
@@ -151,7 +158,7 @@ struct SampleShared {
   uint32_t few_key[kFew];
   int32_t few_idx[kFew];
   u64 red[kSampleWarps], red2[kSampleWarps];
-  float redf[kSampleWarps], redf2[kSampleWarps];
+  float redf[kSampleWarps];
   int32_t redi[kSampleWarps];
   uint32_t from, to;  // radix search: the keys left, how many entries, what is to be reached
   uint32_t left, n_few;
@@ -548,7 +555,8 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
       const bool hist = (cut_k || cut_p) && ref > -INFINITY && ref < INFINITY;
       if (hist) {
 #pragma unroll
-        for (int i = 0; i < kBins / kSampleThreads; ++i) sh.cnt[tid + i * kSampleThreads] = 0;
+        for (int i = 0; i < kBins / kSampleThreads; ++i)
+          sh.cnt[tid + i * kSampleThreads] = sh.place[tid + i * kSampleThreads] = 0;
         __syncthreads();
 #pragma unroll 2
         for (int32_t ch = warp; ch < chunks; ch += kSampleWarps) {
@@ -557,10 +565,17 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
           m = fmaxf(m, max8(x));
 #pragma unroll
           for (int u = 0; u < 8; u += 2) {
-            const float2 b = ffma2(below2(ref, x[u], x[u + 1]), both(r.c), both((float)kHead));
+            const float2 b = bin2_of(ref, r.c, x[u], x[u + 1]);
             // (bins above the first count as the first; a NaN fails the comparison)
-            if (b.x < (float)kBins) atomicAdd(&sh.cnt[__float2uint_rz(b.x)], 1u);
-            if (b.y < (float)kBins) atomicAdd(&sh.cnt[__float2uint_rz(b.y)], 1u);
+#pragma unroll
+            for (int v = 0; v < 2; ++v) {
+              const float bv = v ? b.y : b.x;
+              if (bv < (float)(kBins * kPlaces)) {
+                const uint32_t at = __float2uint_rz(bv);
+                atomicAdd(&sh.cnt[at / kPlaces], 1u);
+                if (cut_p) atomicAdd(&sh.place[at / kPlaces], at % kPlaces);
+              }
+            }
           }
         }
       } else {
@@ -582,7 +597,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
         ref = 0.f;
         continue;
       }
-      if (hist && bin_of(ref, r.c, r.top) >= 1.f) break;
+      if (hist && bin_of(ref, r.c, r.top) >= (float)kPlaces) break;
       ref = r.top;  // (bin_of is kHead for the reference itself)
     }
     if (r.top == -INFINITY) {
@@ -633,18 +648,23 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
     if (cut_k || cut_p) {
       constexpr int kPer = kBins / kSampleThreads;
       static_assert(kPer * kSampleThreads == kBins, "bins per thread");
-      int32_t n = 0;
-      float mass = 0.f, var = 0.f;
-      const float w0 = exp2f(((float)kHead - 0.5f - (float)(tid * kPer)) / kBinsPerLog2);
+      // 2^((kHead - b) / 128) of a bin's upper edge
+      const float w0 = exp2f((float)(kHead - tid * kPer) / kBinsPerLog2);
       constexpr float kStep = 0.99459942f;  // 2^(-1/128)
-      float w = w0;
+      auto mass_of = [&](int b, float w) {
+        const uint32_t cn = sh.cnt[b];
+        if (cn == 0) return 0.f;
+        const float mean = kBinLn / kPlaces * (__fdividef((float)sh.place[b], (float)cn) + 0.5f);
+        return (float)cn * w * (1.f - mean + 0.5f * mean * mean);
+      };
+      int32_t n = 0;
+      float mass = 0.f, w = w0;
+      float q[kPer];  // mass of each bin
 #pragma unroll
       for (int i = 0; i < kPer; ++i) {
-        const int32_t cn = sh.cnt[tid * kPer + i];
-        const float q = (float)cn * w;
-        n += cn;
-        mass += q;
-        var += q * q;
+        n += sh.cnt[tid * kPer + i];
+        q[i] = cut_p ? mass_of(tid * kPer + i, w) : 0.f;
+        mass += q[i];
         w *= kStep;
       }
       int32_t n1 = n;
@@ -658,16 +678,13 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
           m1 += z;
         }
       }
-      var = warp_sum(var);
       __syncthreads();
       if (lane == 31) {
         sh.redi[warp] = n1;
         sh.redf[warp] = m1;
-        sh.redf2[warp] = var;
       }
       __syncthreads();
       float total = 0.f;
-      var = 0.f;
 #pragma unroll
       for (int w2 = 0; w2 < kSampleWarps; ++w2) {
         if (w2 < warp) {
@@ -675,7 +692,6 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
           m1 += sh.redf[w2];
         }
         total += sh.redf[w2];
-        var += sh.redf2[w2];
       }
       const int32_t n0 = n1 - n;
       const float m0 = m1 - mass;
@@ -688,35 +704,33 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
         int32_t s = n0;
         float before = m0;
         w = w0;
+#pragma unroll
         for (int i = 0; i < kPer; ++i) {
           const int32_t cn = sh.cnt[tid * kPer + i];
-          if (s + cn >= k) {
+          if (s < k && s + cn >= k) {
             sh.bin_k = tid * kPer + i;
             sh.need_k = k - s;  // entries of the bin within top-k
             sh.k_mass = before + (float)(k - s) * w;
-            sh.k_mass_err = (float)(k - s) * w * (2.f * kBinSpread);
-            break;
+            sh.k_mass_err = (float)(k - s) * w * kBinLn;
           }
           s += cn;
-          before += (float)cn * w;
+          before += q[i];
           w *= kStep;
         }
       }
       __syncthreads();
       if (cut_p) {
-        const float err = sh.k_mass_err + 5.f * kBinSpread * sqrtf(var) + 1e-4f * sh.k_mass;
+        const float err = sh.k_mass_err + kMassErr * sh.k_mass;
         const float least = top_p * sh.k_mass - err, most = top_p * sh.k_mass + err;
         float before = m0;
-        w = w0;
         if (tid == 0 && least <= 0.f) sh.bin_lo = 0;
-#pragma unroll 1
+#pragma unroll
         for (int i = 0; i < kPer; ++i) {
-          const float upto = before + (float)sh.cnt[tid * kPer + i] * w;
+          const float upto = before + q[i];
           // (several threads may find one where sums are rounded: any will do)
           if (before < least && least <= upto) sh.bin_lo = tid * kPer + i;
           if (before < most && most <= upto) sh.bin_hi = tid * kPer + i;
           before = upto;
-          w *= kStep;
         }
       }
       __syncthreads();
@@ -727,7 +741,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
         const int32_t edge = warp == 0 ? bin_lo : warp == 1 ? bin_hi + 1
                              : warp == 2 ? bin_k : bin_k + 1;
         const uint32_t at =
-            least_key(lane, [&](float x) { return bin_of(ref, r.c, x) < (float)edge; });
+            least_key(lane, [&](float x) { return bin_of(ref, r.c, x) < (float)(edge * kPlaces); });
         if (lane == 0) sh.edge[warp] = at;
       }
       __syncthreads();

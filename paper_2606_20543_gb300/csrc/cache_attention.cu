@@ -21,7 +21,7 @@
 
 #include <algorithm>
 
-#include "kernels.cuh"
+#include "cache_attention.cuh"
 
 namespace ssd {
 
@@ -30,8 +30,8 @@ namespace {
 constexpr int kWarps = 4;
 constexpr int kStages = 4;          // steps in flight per warp
 constexpr int kStep = 16;           // keys per step
-constexpr int kMaxKps = 8192;       // most keys of a part
-constexpr int kMinStepsPerWarp = 4; // a part's fewest steps per warp
+constexpr int kMinTiles = 2;        // a part's fewest tiles (times the warps that share its rows / 4)
+constexpr int kMaxPartTiles = 256;  // 16384 keys: at most 1024 block ids and scales in shared memory
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 // log2 growth of the running maximum (and growth of the V scale) that moves the
@@ -39,32 +39,25 @@ constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kGrowth = 8.f, kVGrowth = 16.f;
 
 struct Plan {
-  int32_t wr, rowgroups, splits, kps;
+  int32_t wr, rowgroups, splits, min_tiles;
 };
 
 Plan make_plan(int32_t B, int32_t Hq, int32_t Hkv, int32_t D_max, int32_t L_max) {
   Plan p;
   const int64_t rows = (int64_t)D_max * (Hq / Hkv);
-  const int64_t tiles = (rows + 15) / 16;
-  p.wr = tiles >= 3 ? 4 : (int32_t)tiles;
-  p.rowgroups = (int32_t)((tiles + p.wr - 1) / p.wr);
+  const int64_t row_tiles = (rows + 15) / 16;
+  p.wr = row_tiles >= 3 ? 4 : (int32_t)row_tiles;
+  p.rowgroups = (int32_t)((row_tiles + p.wr - 1) / p.wr);
   const int64_t base = (int64_t)B * Hkv * p.rowgroups;
   const int64_t target = 3 * (int64_t)device_sm_count();
-  const int32_t least = kStep * kMinStepsPerWarp * (kWarps / p.wr);
-  int64_t splits = (target + base - 1) / base;
-  splits = std::max<int64_t>(1, std::min<int64_t>(splits, (L_max + least - 1) / least));
-  int64_t kps = (L_max + splits - 1) / splits;
-  kps = std::min<int64_t>(kMaxKps, (kps + 127) / 128 * 128);
-  p.kps = (int32_t)kps;
-  p.splits = (int32_t)((L_max + kps - 1) / kps);
+  p.min_tiles = kMinTiles * (kWarps / p.wr);
+  const int64_t tiles = (L_max + kCacheTile - 1) / kCacheTile;
+  const int64_t most = std::max<int64_t>(1, tiles / p.min_tiles);
+  // (and no part longer than the room for its block ids)
+  const int64_t least = (tiles + kMaxPartTiles - 1) / kMaxPartTiles;
+  p.splits = (int32_t)std::max<int64_t>(least, std::min<int64_t>((target + base - 1) / base, most));
   return p;
 }
-
-struct Launch {
-  int32_t wr, splits, kps;
-  float* part_o;   // [B * Hkv * D_max * G][splits][d]
-  float2* part_ml; // [...][splits]: reference maximum (log2) and sum
-};
 
 size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 
@@ -108,19 +101,9 @@ __device__ __forceinline__ void cp_wait() {
   asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 
-// Flat position of draft j of sequence b; -1 outside the grid.
-__device__ __forceinline__ int32_t flat_pos(const CacheAttnArgs& a, int32_t b, int32_t cache,
-                                            int32_t j) {
-  if (a.draft_pos == nullptr) return cache + j;
-  const int32_t i = a.draft_pos[(int64_t)b * a.D_max + j];
-  if (i < 0 || i >= a.grid.grid_h * a.grid.grid_w) return -1;
-  const int32_t y = i / a.grid.grid_w;
-  return a.grid.prefix_len + y * a.grid.row_stride + (i - y * a.grid.grid_w);
-}
-
 template <int D>
 __global__ void __launch_bounds__(kWarps * 32, 3)
-cache_attn_kernel(CacheAttnArgs a, Launch L) {
+cache_attn_kernel(CacheAttnArgs a, CacheAttnLaunch L, int32_t row_warps) {
   constexpr int NT = D / 8;           // output tiles of 8 columns
   constexpr int KG = D / 64;          // groups of four mma steps of QK^T
   constexpr int VB = D / 8;           // bytes of V a lane takes per key
@@ -129,30 +112,34 @@ cache_attn_kernel(CacheAttnArgs a, Launch L) {
   static_assert(kWarpBytes >= 16 * D * 4 + 16 * 8, "a warp's partial rows fit its ring");
   extern __shared__ __align__(16) unsigned char smem[];
   int32_t* s_id = reinterpret_cast<int32_t*>(smem + kWarps * kWarpBytes);
-  float* s_ks = reinterpret_cast<float*>(s_id + L.kps / 16);
-  float* s_vs = s_ks + L.kps / 16;
+  float* s_ks = reinterpret_cast<float*>(s_id + L.max_blocks);
+  float* s_vs = s_ks + L.max_blocks;
   pdl_wait();
 
   const int32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int32_t split = blockIdx.x, b = blockIdx.y / a.cache.Hkv, g = blockIdx.y % a.cache.Hkv;
   const int32_t S = a.cache.block, S_log = 31 - __clz(S), G = a.Hq / a.cache.Hkv;
   const int32_t cache = a.cache_len[b], nd = a.n_drafts[b];
-  const int32_t most = a.max_blocks * S;
-  if (cache < 0 || nd < 0 || nd > a.D_max || cache > most - nd) {
+  if (!cache_lengths_ok(a, cache, nd)) {
     if (tid == 0 && split == 0 && g == 0 && blockIdx.z == 0)
       record_status(a.status, SSD_ERR_DEVICE_BOUNDS);
     return;
   }
   const int32_t Lk = cache + nd, rows_total = nd * G;
-  const int32_t k_lo = split * L.kps, k_hi = min(Lk, k_lo + L.kps);
-  const int32_t row_g0 = blockIdx.z * L.wr * 16;
-  if (row_g0 >= rows_total || k_lo >= Lk) return;
+  const int32_t tiles = (Lk + kCacheTile - 1) / kCacheTile;
+  const int32_t parts = cache_parts(L.splits, L.min_tiles, tiles);
+  const int32_t row_g0 = blockIdx.z * row_warps * 16;
+  if (row_g0 >= rows_total || split >= parts) return;
+  const int32_t t_lo = (int32_t)((int64_t)tiles * split / parts);
+  const int32_t t_hi = (int32_t)((int64_t)tiles * (split + 1) / parts);
+  const int32_t k_lo = t_lo * kCacheTile, k_hi = min(Lk, t_hi * kCacheTile);
   const int32_t start = a.key_start != nullptr ? min(Lk, max(0, a.key_start[b])) : 0;
 
   // ---- the part's block ids and scales
-  const int32_t nb = (k_hi - k_lo + S - 1) >> S_log;
+  const int32_t b_lo = k_lo >> S_log;  // (a part may start inside a block of 128)
+  const int32_t nb = ((k_hi - 1) >> S_log) + 1 - b_lo;
   for (int32_t i = tid; i < nb; i += blockDim.x) {
-    int32_t id = a.block_table[(int64_t)b * a.max_blocks + (k_lo >> S_log) + i];
+    int32_t id = a.block_table[(int64_t)b * a.max_blocks + b_lo + i];
     if (id < 0 || id >= a.cache.num_blocks) {
       record_status(a.status, SSD_ERR_DEVICE_BOUNDS);
       id = -1;
@@ -164,7 +151,7 @@ cache_attn_kernel(CacheAttnArgs a, Launch L) {
   }
 
   // ---- this warp's rows and its share of the steps
-  const int32_t wk_n = kWarps / L.wr, wr = warp % L.wr, wk = warp / L.wr;
+  const int32_t wk_n = kWarps / row_warps, wr = warp % row_warps, wk = warp / row_warps;
   const int32_t q = lane & 3, r8 = lane >> 2;
   const int32_t row0 = row_g0 + wr * 16;
   int32_t qpos[2];
@@ -174,7 +161,7 @@ cache_attn_kernel(CacheAttnArgs a, Launch L) {
     const int32_t r = row0 + r8 + 8 * i;
     qpos[i] = -1;
     if (r < rows_total) {
-      qpos[i] = flat_pos(a, b, cache, r / G);
+      qpos[i] = cache_flat_pos(a, b, cache, r / G);
       if (qpos[i] < 0 && split == 0 && g == 0) record_status(a.status, SSD_ERR_DEVICE_BOUNDS);
       minq = min(minq, qpos[i]);
     }
@@ -233,7 +220,7 @@ cache_attn_kernel(CacheAttnArgs a, Launch L) {
   auto issue = [&](int32_t t) {
     const int32_t k0 = key_of(t);
     if (k0 < k_hi && row0 < rows_total) {
-      const int32_t i = (k0 - k_lo) >> S_log, id = s_id[i];
+      const int32_t i = (k0 >> S_log) - b_lo, id = s_id[i];
       const int64_t at =
           (((int64_t)max(id, 0) * a.cache.Hkv + g) * S + (k0 & (S - 1))) * D;
       const uint32_t dst = ring + (t % kStages) * kStageBytes;
@@ -269,7 +256,7 @@ cache_attn_kernel(CacheAttnArgs a, Launch L) {
     for (int32_t t = 0; key_of(t) < k_hi; ++t) {
       cp_wait<kStages - 2>();
       issue(t + kStages - 1);
-      const int32_t k0 = key_of(t), bi = (k0 - k_lo) >> S_log;
+      const int32_t k0 = key_of(t), bi = (k0 >> S_log) - b_lo;
       const unsigned char* st = smem + warp * kWarpBytes + (t % kStages) * kStageBytes;
       // ---- S = Q K^T
       float sc[2][4];
@@ -300,7 +287,7 @@ cache_attn_kernel(CacheAttnArgs a, Launch L) {
             if (key >= start && key < k_hi && s_id[bi] >= 0) {
               kp = key;
               if (key >= cache) {
-                kp = flat_pos(a, b, cache, key - cache);
+                kp = cache_flat_pos(a, b, cache, key - cache);
                 if (kp < 0) kp = 0x7fffffff;
               }
             }
@@ -415,13 +402,13 @@ cache_attn_kernel(CacheAttnArgs a, Launch L) {
       const int32_t r = r8 + 8 * i;
       float M = -INFINITY;
       for (int w = 0; w < wk_n; ++w)
-        M = fmaxf(M, reinterpret_cast<const float2*>(smem + (wr + w * L.wr) * kWarpBytes +
+        M = fmaxf(M, reinterpret_cast<const float2*>(smem + (wr + w * row_warps) * kWarpBytes +
                                                      16 * D * 4)[r].x);
       float sum = 0.f;
 #pragma unroll
       for (int n = 0; n < NT; ++n) o[n][2 * i] = o[n][2 * i + 1] = 0.f;
       for (int w = 0; w < wk_n; ++w) {
-        const unsigned char* at = smem + (wr + w * L.wr) * kWarpBytes;
+        const unsigned char* at = smem + (wr + w * row_warps) * kWarpBytes;
         const float2 x = reinterpret_cast<const float2*>(at + 16 * D * 4)[r];
         const float f = x.x == -INFINITY ? 0.f : exp2f(x.x - M);
         sum += x.y * f;
@@ -438,7 +425,7 @@ cache_attn_kernel(CacheAttnArgs a, Launch L) {
   }
 
   // ---- the rows, or the part's share of them
-  const bool direct = Lk <= L.kps;
+  const bool direct = parts == 1;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     const int32_t r = row0 + r8 + 8 * i;
@@ -474,7 +461,7 @@ cache_attn_kernel(CacheAttnArgs a, Launch L) {
 // One warp per (sequence, draft, head): the parts of its row, weighted by their
 // reference maxima.
 template <int D>
-__global__ void __launch_bounds__(256) cache_attn_combine_kernel(CacheAttnArgs a, Launch L) {
+__global__ void __launch_bounds__(256) cache_attn_combine_kernel(CacheAttnArgs a, CacheAttnLaunch L) {
   pdl_wait();
   const int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
   const int32_t lane = threadIdx.x & 31;
@@ -483,10 +470,10 @@ __global__ void __launch_bounds__(256) cache_attn_combine_kernel(CacheAttnArgs a
   const int64_t bj = row / a.Hq;
   const int32_t b = (int32_t)(bj / a.D_max), j = (int32_t)(bj - (int64_t)b * a.D_max);
   const int32_t cache = a.cache_len[b], nd = a.n_drafts[b];
-  if (cache < 0 || nd < 0 || nd > a.D_max || cache > a.max_blocks * a.cache.block - nd) return;
-  const int32_t Lk = cache + nd;
-  if (j >= nd || Lk <= L.kps) return;  // padding, or written by the attention kernel
-  const int32_t parts = (Lk + L.kps - 1) / L.kps;
+  if (!cache_lengths_ok(a, cache, nd) || j >= nd) return;
+  const int32_t parts =
+      cache_parts(L.splits, L.min_tiles, (cache + nd + kCacheTile - 1) / kCacheTile);
+  if (parts == 1) return;  // written by the attention kernel
   const int64_t at = row * L.splits;
   if (!dbg_in(at + parts - 1, (int64_t)a.B * a.D_max * a.Hq * L.splits, a.status)) return;
   float M = -INFINITY;
@@ -515,39 +502,56 @@ __global__ void __launch_bounds__(256) cache_attn_combine_kernel(CacheAttnArgs a
 }
 
 template <int D>
-cudaError_t launch(const CacheAttnArgs& a, const Plan& p, const Launch& L, cudaStream_t stream) {
-  const size_t smem = (size_t)kWarps * kStages * 2 * kStep * D + (size_t)p.kps / 16 * 12;
-  cudaError_t e = cudaFuncSetAttribute(cache_attn_kernel<D>,
-                                       cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+cudaError_t launch_mma(const CacheAttnArgs& a, const Plan& p, const CacheAttnLaunch& L,
+                       cudaStream_t stream) {
+  const size_t smem = (size_t)kWarps * kStages * 2 * kStep * D + (size_t)L.max_blocks * 12;
+  const cudaError_t e = cudaFuncSetAttribute(
+      cache_attn_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;
-  e = launch_kernel(cache_attn_kernel<D>, dim3(p.splits, a.B * a.cache.Hkv, p.rowgroups),
-                    dim3(kWarps * 32), smem, stream, true, a, L);
-  if (e != cudaSuccess || p.splits == 1) return e;
-  const int64_t rows = (int64_t)a.B * a.D_max * a.Hq;
-  return launch_kernel(cache_attn_combine_kernel<D>, dim3((unsigned)((rows + 7) / 8)), dim3(256), 0,
-                       stream, true, a, L);
+  return launch_kernel(cache_attn_kernel<D>, dim3(p.splits, a.B * a.cache.Hkv, p.rowgroups),
+                       dim3(kWarps * 32), smem, stream, true, a, L, p.wr);
+}
+
+size_t part_bytes(int64_t rows, int32_t splits, int32_t d) {
+  if (splits == 1) return 0;
+  return align256((size_t)rows * splits * d * sizeof(float)) +
+         align256((size_t)rows * splits * sizeof(float2));
 }
 
 }  // namespace
 
+// Enough for either kernel: which one runs depends on arguments that the
+// query does not have.
 size_t cache_attention_workspace(int32_t B, int32_t Hq, int32_t Hkv, int32_t d, int32_t D_max,
                                  int32_t L_max) {
-  const Plan p = make_plan(B, Hq, Hkv, D_max, L_max);
-  if (p.splits == 1) return 0;
-  const size_t rows = (size_t)B * D_max * Hq * p.splits;
-  return align256(rows * d * sizeof(float)) + align256(rows * sizeof(float2));
+  int32_t splits, min_tiles;
+  cache_attention_tc_plan(B, Hq, Hkv, D_max, L_max, &splits, &min_tiles);
+  splits = std::max(splits, make_plan(B, Hq, Hkv, D_max, L_max).splits);
+  return part_bytes((int64_t)B * D_max * Hq, splits, d);
 }
 
 cudaError_t launch_cache_attention(const CacheAttnArgs& a, void* ws, cudaStream_t stream) {
-  const Plan p = make_plan(a.B, a.Hq, a.cache.Hkv, a.D_max, a.max_blocks * a.cache.block);
-  Launch L{p.wr, p.splits, p.kps, nullptr, nullptr};
-  if (p.splits > 1) {
-    const size_t rows = (size_t)a.B * a.D_max * a.Hq * p.splits;
+  const int32_t L_max = a.max_blocks * a.cache.block, d = a.cache.d;
+  const bool tc = cache_attention_tc_runs(a);
+  const Plan p = make_plan(a.B, a.Hq, a.cache.Hkv, a.D_max, L_max);
+  CacheAttnLaunch L{p.splits, p.min_tiles, 0, nullptr, nullptr};
+  if (tc)
+    cache_attention_tc_plan(a.B, a.Hq, a.cache.Hkv, a.D_max, L_max, &L.splits, &L.min_tiles);
+  const int32_t tiles = (L_max + kCacheTile - 1) / kCacheTile;
+  L.max_blocks =
+      cache_part_tiles(L.splits, L.min_tiles, tiles) * (kCacheTile / std::min(a.cache.block, 64)) + 1;
+  const int64_t rows = (int64_t)a.B * a.D_max * a.Hq;
+  if (L.splits > 1) {
     L.part_o = static_cast<float*>(ws);
-    L.part_ml = reinterpret_cast<float2*>(static_cast<unsigned char*>(ws) +
-                                          align256(rows * a.cache.d * sizeof(float)));
+    L.part_ml = reinterpret_cast<float2*>(
+        static_cast<unsigned char*>(ws) + align256((size_t)rows * L.splits * d * sizeof(float)));
   }
-  return a.cache.d == 128 ? launch<128>(a, p, L, stream) : launch<64>(a, p, L, stream);
+  cudaError_t e = tc ? launch_cache_attention_tc(a, L, stream)
+                     : (d == 128 ? launch_mma<128>(a, p, L, stream) : launch_mma<64>(a, p, L, stream));
+  if (e != cudaSuccess || L.splits == 1) return e;
+  const dim3 grid((unsigned)((rows + 7) / 8));
+  return d == 128 ? launch_kernel(cache_attn_combine_kernel<128>, grid, dim3(256), 0, stream, true, a, L)
+                  : launch_kernel(cache_attn_combine_kernel<64>, grid, dim3(256), 0, stream, true, a, L);
 }
 
 }  // namespace ssd

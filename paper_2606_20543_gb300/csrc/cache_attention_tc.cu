@@ -1,0 +1,630 @@
+// cache_attention_tc.cu — frontier attention over the paged 8-bit cache on the
+// 5th-generation tensor cores (include/ssd.h, ssd_cache_attention; 128-wide heads):
+//   O[b][j][h] = softmax_s(scale * Q[b][j][h] . (sk K[s]) + M(s, j)) (sv V[s]).
+//
+// K and V stay e4m3 from the cache to the products (kind::f8f6f4): they are
+// copied once by TMA, 128 bytes a key, and never widened.  Q and P are split in two
+// e4m3 terms each, x = hi + lo with hi the nearest e4m3 and lo the nearest to the rest:
+// 8 significant bits, as many as bf16 has, at the cost of twice the products, which run at twice
+// the rate of bf16's.  Q's rows are scaled by a power of two first (largest entry in
+// [128, 256)), P by 2^6 times its block's V scale over a reference scale, so that hi and lo use
+// e4m3's range; the K scale multiplies the scores.
+//
+// One CTA (8 warps, two CTAs per SM) per tile of 128 query rows (drafts x the query
+// heads of a KV head) and part of the sequence's keys, longest sequences first:
+//  warp 4 streams K and V in tiles of 64 keys through rings of kNS stages, a
+//    copy per cache block (TMA, 128-byte swizzle);
+//  warp 5 issues S = (Qhi + Qlo) K^T into one of two TMEM buffers, warp 6 O +=
+//    (Phi + Plo) V with P read from TMEM, where it replaced S;
+//  warps 0-3 (a thread a row) turn S into P.  The running maximum moves only when
+//    it grows by more than a factor of two; O is rescaled in TMEM when it does, or
+//    when a block's V scale is above twice the reference.
+#include <cuda_fp16.h>
+
+#include <algorithm>
+
+#include "cache_attention.cuh"
+
+namespace ssd {
+
+namespace {
+
+constexpr int kD = 128;
+constexpr int kBM = 128;
+constexpr int KT = kCacheTile;
+constexpr int kNS = 4;                       // K and V stages
+constexpr int kTileBytes = KT * kD;          // one K (or V) tile
+constexpr int kQBytes = kBM * kD;            // one term of Q
+constexpr uint32_t kCols = 256;              // S/P x 2 (64 columns each), O at 128
+constexpr int kThreadsTC = 256;
+constexpr int kCtasPerSm = 2;
+constexpr int kMinTiles = 6;                 // a part's fewest tiles
+constexpr int kMaxPartTiles = 256;           // at most 1024 block ids and scales in shared memory
+constexpr int kMaxDrafts = 512;              // with positions of their own (kept in shared memory)
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kGrowth = 1.f;               // log2 growth of the maximum that moves it
+constexpr float kPScale = 64.f;              // P <= 2^kGrowth: hi <= 64 * 2 * 2 = 256
+
+// kind::f8f6f4, e4m3 A and B, fp32 D.
+__host__ __device__ constexpr uint32_t idesc_e4m3(int m, int n, bool b_mn_major) {
+  return (1u << 4) | ((b_mn_major ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) |
+         ((uint32_t)(m >> 4) << 24);
+}
+__device__ __forceinline__ void mma8_ss(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc,
+                                        uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+      " tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n}\n" ::"r"(d_tmem),
+      "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void mma8_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc,
+                                        uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+      " tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], [%1], %2, %3, p;\n}\n" ::"r"(d_tmem),
+      "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+
+// float16 pairs to e4m3 pairs and back (exactly).
+__device__ __forceinline__ uint32_t e4m3_of_f16(uint32_t h) {
+  uint16_t r;
+  asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(r) : "r"(h));
+  return r;
+}
+__device__ __forceinline__ uint32_t f16_of_e4m3(uint32_t w) {
+  uint32_t h;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)w));
+  return h;
+}
+// A pair as hi and lo terms (16 bits each).
+__device__ __forceinline__ void split2(float2 x, uint32_t& hi, uint32_t& lo) {
+  const __half2 h = __floats2half2_rn(x.x, x.y);
+  const uint32_t hb = *reinterpret_cast<const uint32_t*>(&h);
+  hi = e4m3_of_f16(hb);
+  const uint32_t back = f16_of_e4m3(hi);
+  const __half2 rest = __hsub2(h, *reinterpret_cast<const __half2*>(&back));
+  lo = e4m3_of_f16(*reinterpret_cast<const uint32_t*>(&rest));
+}
+
+// 64 consecutive 32-bit columns of this thread's TMEM lane (warp-collective).
+__device__ __forceinline__ void tmem_ld64(uint32_t taddr, float* v) {
+  uint32_t r[64];
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x64.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,"
+      "%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32,%33,%34,%35,%36,"
+      "%37,%38,%39,%40,%41,%42,%43,%44,%45,%46,%47,%48,%49,%50,%51,%52,%53,%54,%55,%56,%57,%58,"
+      "%59,%60,%61,%62,%63}, [%64];\n"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
+        "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]),
+        "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]),
+        "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]),
+        "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31]),
+        "=r"(r[32]), "=r"(r[33]), "=r"(r[34]), "=r"(r[35]), "=r"(r[36]), "=r"(r[37]),
+        "=r"(r[38]), "=r"(r[39]), "=r"(r[40]), "=r"(r[41]), "=r"(r[42]), "=r"(r[43]),
+        "=r"(r[44]), "=r"(r[45]), "=r"(r[46]), "=r"(r[47]), "=r"(r[48]), "=r"(r[49]),
+        "=r"(r[50]), "=r"(r[51]), "=r"(r[52]), "=r"(r[53]), "=r"(r[54]), "=r"(r[55]),
+        "=r"(r[56]), "=r"(r[57]), "=r"(r[58]), "=r"(r[59]), "=r"(r[60]), "=r"(r[61]),
+        "=r"(r[62]), "=r"(r[63])
+      : "r"(taddr)
+      : "memory");
+#pragma unroll
+  for (int i = 0; i < 64; ++i) v[i] = __uint_as_float(r[i]);
+}
+
+__device__ __forceinline__ uint64_t low_bits(int32_t n) {
+  return n <= 0 ? 0ull : (n >= 64 ? ~0ull : ((1ull << n) - 1ull));
+}
+
+struct Shared {
+  uint64_t k_full[kNS], k_empty[kNS], v_full[kNS], v_empty[kNS];
+  uint64_t s_full[2], p_ready[2], pv_done[2];
+  uint32_t tmem;
+  int32_t seq;
+  int32_t bad;  // a draft position outside the grid, or a block outside the pool
+  int32_t kflat[kMaxDrafts];
+};
+
+__global__ void __launch_bounds__(kThreadsTC, kCtasPerSm)
+cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
+                     CacheAttnArgs a, CacheAttnLaunch L, int32_t mtiles) {
+  extern __shared__ __align__(1024) unsigned char smem_raw[];
+  unsigned char* smem = reinterpret_cast<unsigned char*>(
+      (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  unsigned char* sQ = smem;                        // hi, lo
+  unsigned char* sK = sQ + 2 * kQBytes;
+  unsigned char* sV = sK + kNS * kTileBytes;
+  Shared& sh = *reinterpret_cast<Shared*>(sV + kNS * kTileBytes);
+  int32_t* s_id = reinterpret_cast<int32_t*>(&sh + 1);
+  float* s_ks = reinterpret_cast<float*>(s_id + L.max_blocks);
+  float* s_vs = s_ks + L.max_blocks;
+  pdl_wait();
+
+  const int32_t tid = threadIdx.x, lane = tid & 31, warp = (int32_t)warp_uniform(tid >> 5);
+  const int32_t S = a.cache.block, S_log = 31 - __clz(S), Hkv = a.cache.Hkv, G = a.Hq / Hkv;
+  int32_t unit = blockIdx.x;
+  const int32_t split = unit % L.splits;
+  unit /= L.splits;
+  const int32_t mtile = unit % mtiles;
+  unit /= mtiles;
+  const int32_t g = unit % Hkv, rank = unit / Hkv;
+
+  // ---- the sequence: the rank-th longest (batches above 256 keep their order)
+  int32_t b = rank;
+  if (a.B > 1 && a.B <= kThreadsTC) {
+    int32_t* keys = sh.kflat;  // (not in use yet)
+    int32_t mine = 0;
+    if (tid < a.B) {
+      const int32_t c = a.cache_len[tid], n = a.n_drafts[tid];
+      mine = cache_lengths_ok(a, c, n) && n > 0 ? c + n : 0;
+      keys[tid] = mine;
+    }
+    __syncthreads();
+    if (tid < a.B) {
+      int32_t r = 0;
+#pragma unroll 4
+      for (int32_t j = 0; j < a.B; ++j) {
+        const int32_t kj = keys[j];
+        r += kj > mine || (kj == mine && j < tid);
+      }
+      if (r == rank) sh.seq = tid;
+    }
+    __syncthreads();
+    b = sh.seq;
+  }
+  const int32_t cache = a.cache_len[b], nd = a.n_drafts[b];
+  if (!cache_lengths_ok(a, cache, nd)) {
+    if (tid == 0 && split == 0 && g == 0 && mtile == 0) record_status(a.status, SSD_ERR_DEVICE_BOUNDS);
+    return;
+  }
+  const int32_t Lk = cache + nd, rows_total = nd * G, row0 = mtile * kBM;
+  const int32_t tiles = (Lk + KT - 1) / KT;
+  const int32_t parts = cache_parts(L.splits, L.min_tiles, tiles);
+  if (row0 >= rows_total || split >= parts) return;
+  const int32_t t_lo = (int32_t)((int64_t)tiles * split / parts);
+  const int32_t t_hi = (int32_t)((int64_t)tiles * (split + 1) / parts);
+  const int32_t k_lo = t_lo * KT, k_hi = min(Lk, t_hi * KT), ntiles = t_hi - t_lo;
+  const int32_t start = a.key_start != nullptr ? min(Lk, max(0, a.key_start[b])) : 0;
+  const int32_t b_lo = k_lo >> S_log, nb = ((k_hi - 1) >> S_log) + 1 - b_lo;
+
+  // ---- set-up
+  __syncthreads();  // kflat is free again
+  if (tid == 0) {
+    for (int i = 0; i < kNS; ++i) {
+      mbar_init(&sh.k_full[i], 1);
+      mbar_init(&sh.k_empty[i], 1);
+      mbar_init(&sh.v_full[i], 1);
+      mbar_init(&sh.v_empty[i], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&sh.s_full[i], 1);
+      mbar_init(&sh.p_ready[i], 4);
+      mbar_init(&sh.pv_done[i], 1);
+    }
+    fence_barrier_init();
+    sh.bad = 0;
+  }
+  if (warp == 7) {
+    tmem_alloc(&sh.tmem, kCols);
+    tmem_relinquish();
+  }
+  if (warp == 4 && lane < 2) prefetch_tensormap(lane == 0 ? &tmK : &tmV);
+  for (int32_t i = tid; i < nb; i += kThreadsTC) {
+    int32_t id = a.block_table[(int64_t)b * a.max_blocks + b_lo + i];
+    if (id < 0 || id >= a.cache.num_blocks) {
+      record_status(a.status, SSD_ERR_DEVICE_BOUNDS);
+      id = -1;
+    }
+    s_id[i] = id;
+    const int64_t at = (int64_t)max(id, 0) * Hkv + g;
+    s_ks[i] = a.cache.k_scale[at];
+    s_vs[i] = id < 0 ? 0.f : a.cache.v_scale[at];
+  }
+  if (a.draft_pos != nullptr) {
+    for (int32_t j = tid; j < nd; j += kThreadsTC) {
+      const int32_t p = cache_flat_pos(a, b, cache, j);
+      if (p < 0 && split == 0 && g == 0 && mtile == 0) record_status(a.status, SSD_ERR_DEVICE_BOUNDS);
+      sh.kflat[j] = p;
+    }
+  }
+  // Q: row `tid` of the tile, as two terms of a row scaled to [128, 256)
+  float rowc = 0.f;
+  if (tid < kBM) {
+    const int32_t r = row0 + tid;
+    const bool live = r < rows_total;
+    const int32_t j = live ? r / G : 0, h = g * G + (live ? r - j * G : 0);
+    const uint4* src = reinterpret_cast<const uint4*>(
+        static_cast<const __nv_bfloat16*>(a.q) + (((int64_t)b * a.D_max + j) * a.Hq + h) * kD);
+    uint4 w[kD / 8];
+    float m = 0.f;
+#pragma unroll
+    for (int i = 0; i < kD / 8; ++i) {
+      w[i] = live ? src[i] : make_uint4(0, 0, 0, 0);
+      const uint32_t v[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        m = fmaxf(m, fmaxf(fabsf(__uint_as_float(v[e] << 16)), fabsf(__uint_as_float(v[e] & 0xffff0000u))));
+    }
+    // 2^(7 - e), e the exponent of the largest entry: in two factors, each in range
+    const int32_t e = min(127, max(-126, (int32_t)(__float_as_uint(m) >> 23) - 127));
+    const int32_t up = 7 - e, u1 = up / 2, u2 = up - u1;
+    const float f1 = __uint_as_float((uint32_t)(u1 + 127) << 23), f2 = __uint_as_float((uint32_t)(u2 + 127) << 23);
+    const float c2 = (a.scale != 0.f ? a.scale : rsqrtf((float)kD)) * kLog2e;
+    rowc = c2 * __uint_as_float((uint32_t)(127 - u1) << 23) * __uint_as_float((uint32_t)(127 - u2) << 23);
+#pragma unroll
+    for (int c = 0; c < kD / 16; ++c) {
+      uint32_t hi[4], lo[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint4& x = w[2 * c + (i >> 1)];
+        const uint32_t p0 = (i & 1) ? x.z : x.x, p1 = (i & 1) ? x.w : x.y;
+        uint32_t h0, l0, h1, l1;
+        split2(make_float2(__uint_as_float(p0 << 16) * f1 * f2, __uint_as_float(p0 & 0xffff0000u) * f1 * f2), h0, l0);
+        split2(make_float2(__uint_as_float(p1 << 16) * f1 * f2, __uint_as_float(p1 & 0xffff0000u) * f1 * f2), h1, l1);
+        hi[i] = h0 | (h1 << 16);
+        lo[i] = l0 | (l1 << 16);
+      }
+      const uint32_t off = (uint32_t)tid * 128 + (uint32_t)((c ^ (tid & 7)) << 4);
+      *reinterpret_cast<uint4*>(sQ + off) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+      *reinterpret_cast<uint4*>(sQ + kQBytes + off) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+    }
+    fence_proxy_async_shared();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = sh.tmem, tO = tmem + 128;
+
+  // Rows of tile t that hold no key of the sequence (behind its end, before its
+  // start, of a block outside the pool), as a bit mask of the others
+  auto live_keys = [&](int32_t c0) -> uint64_t {
+    uint64_t m = low_bits(k_hi - c0) & ~low_bits(start - c0);
+    if (m == 0) return 0;
+#pragma unroll 1
+    for (int32_t k = 0; k < KT; k += min(S, KT))
+      if (c0 + k < k_hi && s_id[((c0 + k) >> S_log) - b_lo] < 0)
+        m &= ~(low_bits(min(S, KT)) << k);
+    return m;
+  };
+
+  if (warp == 4) {
+    // ------------------------------------------------------------ producer
+    const bool leader = elect_one();
+    const uint64_t pol = policy_evict_first();
+    const int32_t rows = min(S, KT);
+    bool ok = true;
+    int32_t t = 0;
+#pragma unroll 1
+    for (; t < ntiles && ok; ++t) {
+      const int s = t % kNS;
+      if (t >= kNS) {
+        ok = mbar_wait_warp(&sh.k_empty[s], ((t / kNS) - 1) & 1, a.status) &&
+             mbar_wait_warp(&sh.v_empty[s], ((t / kNS) - 1) & 1, a.status);
+        if (!ok) break;
+      }
+      const int32_t c0 = k_lo + t * KT;
+      if (leader) {
+        // (blocks behind the last key are not copied: their rows stay what they were)
+        const int32_t n = min(KT, k_hi - c0);
+        const uint32_t bytes = (uint32_t)((n + rows - 1) / rows * rows * kD);
+        mbar_arrive_expect_tx(&sh.k_full[s], bytes);
+        mbar_arrive_expect_tx(&sh.v_full[s], bytes);
+#pragma unroll 1
+        for (int32_t k = 0; k < n; k += rows) {
+          const int32_t id = max(s_id[((c0 + k) >> S_log) - b_lo], 0);
+          const int32_t row = (id * Hkv + g) * S + ((c0 + k) & (S - 1));
+          tma_load_2d(sK + s * kTileBytes + k * kD, &tmK, 0, row, &sh.k_full[s], pol);
+          tma_load_2d(sV + s * kTileBytes + k * kD, &tmV, 0, row, &sh.v_full[s], pol);
+        }
+      }
+      __syncwarp();
+    }
+    // after a wait that gave up, the copies in flight still land here
+    if (!ok)
+      for (int32_t u = max(0, t - kNS); u < t; ++u) {
+        mbar_drain(&sh.k_full[u % kNS], (u / kNS) & 1);
+        mbar_drain(&sh.v_full[u % kNS], (u / kNS) & 1);
+      }
+  } else if (warp == 5) {
+    // ----------------------------------------------------------- S products
+    const uint32_t tSu = warp_uniform(tmem), aQ = warp_uniform(smem_u32(sQ));
+    const uint32_t aK = warp_uniform(smem_u32(sK));
+    const bool leader = elect_one();
+    const uint64_t dq = smem_desc(aQ, 16, 1024);
+    constexpr uint32_t kIdesc = idesc_e4m3(kBM, KT, false);
+    int32_t t = 0;
+    bool ok = true;
+#pragma unroll 1
+    for (; t < ntiles; ++t) {
+      const int s = t % kNS, sb = t & 1;
+      ok = mbar_wait_warp(&sh.k_full[s], (t / kNS) & 1, a.status);
+      // the S/P buffer is free once PV of tile t - 2 is done
+      if (ok && t >= 2) ok = mbar_wait_warp(&sh.pv_done[sb], ((t >> 1) - 1) & 1, a.status);
+      if (!ok) break;
+      tc_fence_after();
+      const uint64_t dk = smem_desc(aK + s * kTileBytes, 16, 1024);
+      if (leader) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int ks = 0; ks < kD / 32; ++ks)
+            mma8_ss(tSu + sb * KT, smem_desc_at(dq, u * kQBytes + ks * 32), smem_desc_at(dk, ks * 32),
+                    kIdesc, u + ks > 0 ? 1u : 0u);
+        mma_commit(&sh.s_full[sb]);
+        mma_commit(&sh.k_empty[s]);
+      }
+      __syncwarp();
+    }
+    if (!ok && t > 0) mbar_drain(&sh.s_full[(t - 1) & 1], ((t - 1) >> 1) & 1);
+  } else if (warp == 6) {
+    // ---------------------------------------------------------- PV products
+    const uint32_t tSu = warp_uniform(tmem), tOu = warp_uniform(tO);
+    const uint32_t aV = warp_uniform(smem_u32(sV));
+    const bool leader = elect_one();
+    constexpr uint32_t kIdesc = idesc_e4m3(kBM, kD, true);
+    int32_t t = 0;
+    bool ok = true;
+#pragma unroll 1
+    for (; t < ntiles; ++t) {
+      const int s = t % kNS, sb = t & 1;
+      const int32_t c0 = k_lo + t * KT;
+      ok = mbar_wait_warp(&sh.v_full[s], (t / kNS) & 1, a.status);
+      if (!ok) break;
+      const uint64_t live = live_keys(c0);
+      if (live != ~0ull) {
+        // rows without a key hold whatever the pool holds, and their P of 0 times a NaN
+        // would be one: cleared (whole rows, so the swizzle does not matter)
+#pragma unroll 1
+        for (int32_t i = lane; i < KT * 8; i += 32)
+          if (!(live >> (i >> 3) & 1ull))
+            *reinterpret_cast<uint4*>(sV + s * kTileBytes + i * 16) = make_uint4(0u, 0u, 0u, 0u);
+        fence_proxy_async_shared();
+        __syncwarp();
+      }
+      ok = mbar_wait_warp(&sh.p_ready[sb], (t >> 1) & 1, a.status);
+      if (!ok) break;
+      tc_fence_after();
+      // A = P in TMEM (32 keys = 8 columns a step; lo 16 columns behind hi), B = V
+      // (MN-major: 8-key groups 1 KB apart; 32 keys = 4 KB)
+      const uint64_t dv = smem_desc(aV + s * kTileBytes, kTileBytes, 1024);
+      if (leader) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int kk = 0; kk < KT / 32; ++kk)
+            mma8_ts(tOu, tSu + sb * KT + u * 16 + kk * 8, smem_desc_at(dv, kk * 4096), kIdesc,
+                    t + u + kk > 0 ? 1u : 0u);
+        mma_commit(&sh.pv_done[sb]);
+        mma_commit(&sh.v_empty[s]);
+      }
+      __syncwarp();
+    }
+    if (!ok && t > 0) mbar_drain(&sh.pv_done[(t - 1) & 1], ((t - 1) >> 1) & 1);
+  } else if (warp < 4) {
+    // ------------------------------------------------------------- softmax
+    const uint32_t lane_off = (uint32_t)(warp * 32) << 16;
+    const int32_t r = row0 + tid;
+    const bool warp_live = row0 + warp * 32 < rows_total;
+    const int32_t j = r < rows_total ? r / G : 0;
+    int32_t qpos = 0x7fffffff;
+    if (r < rows_total) qpos = a.draft_pos != nullptr ? sh.kflat[j] : cache + j;
+    // keys below this one are visible to every row of the warp
+    const int32_t mask_from = min(cache, __reduce_min_sync(0xffffffffu, qpos) + 1);
+    float m_run = -INFINITY, l_run = 0.f, v_ref = 0.f;
+    bool ok = true;
+    int32_t t = 0;
+#pragma unroll 1
+    for (; t < ntiles; ++t) {
+      const int sb = t & 1;
+      const int32_t c0 = k_lo + t * KT;
+      if (!mbar_wait(&sh.s_full[sb], (t >> 1) & 1, a.status)) ok = false;
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) break;
+      tc_fence_after();
+      if (warp_live) {
+        float sv[64];
+        tmem_ld64(tmem + lane_off + sb * KT, sv);
+        // scales of the tile's four groups of 16 keys
+        float f[4], vs[4], v_max = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int32_t k = min(c0 + 16 * i, k_hi - 1);
+          const int32_t at = (k >> S_log) - b_lo;
+          f[i] = fmaxf(rowc * s_ks[at], 1e-37f);
+          vs[i] = c0 + 16 * i < k_hi ? s_vs[at] : 0.f;
+          v_max = fmaxf(v_max, vs[i]);
+        }
+        const uint64_t live = c0 + KT > mask_from || c0 < start ||  c0 + KT > k_hi ||
+                              !(fminf(fminf(vs[0], vs[1]), fminf(vs[2], vs[3])) > 0.f)
+                                  ? live_keys(c0) : ~0ull;
+        if (live != ~0ull || c0 + KT > mask_from) {
+          uint64_t keep;
+          if (a.draft_pos == nullptr) {
+            keep = low_bits(qpos < 0x7fffffff ? qpos + 1 - c0 : KT);
+          } else {
+            keep = low_bits(min(cache, qpos < 0x7fffffff ? qpos + 1 : cache) - c0);
+#pragma unroll 1
+            for (int32_t k = max(0, cache - c0); k < min(KT, k_hi - c0); ++k) {
+              const int32_t p = sh.kflat[c0 + k - cache];
+              if (p >= 0 && p <= qpos) keep |= 1ull << k;
+            }
+          }
+          keep &= live;
+#pragma unroll
+          for (int i = 0; i < 64; ++i)
+            if (!(keep >> i & 1ull)) sv[i] = -INFINITY;
+        }
+        float mx = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float* x = sv + 16 * i;
+          float y = fmax3(x[0], x[1], x[2]);
+#pragma unroll
+          for (int e = 3; e < 15; e += 2) y = fmax3(y, x[e], x[e + 1]);
+          mx = fmaxf(mx, fmaxf(y, x[15]) * f[i]);
+        }
+        float alpha = 1.f;
+        bool moved = false;
+        if (mx > m_run + kGrowth || (m_run == -INFINITY && mx > -INFINITY)) {
+          alpha = m_run == -INFINITY ? 0.f : ex2_approx(m_run - mx);
+          m_run = mx;
+          moved = true;
+        }
+        l_run *= alpha;
+        if (!(v_max <= 2.f * v_ref)) {  // the same in every thread
+          alpha *= v_ref / v_max;
+          v_ref = v_max;
+          moved = true;
+        }
+        if (t > 0 && __any_sync(0xffffffffu, moved)) {
+          // O may be rescaled once PV of the tile before is done
+          ok = mbar_wait_warp(&sh.pv_done[(t - 1) & 1], ((t - 1) >> 1) & 1, a.status);
+          tc_fence_after();
+#pragma unroll 1
+          for (int c = 0; c < kD / 32; ++c) {
+            float ov[32];
+            tmem_ld32(tO + lane_off + c * 32, ov);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) ov[i] *= alpha;
+            tmem_st32(tO + lane_off + c * 32, ov);
+          }
+        }
+        const float m = m_run == -INFINITY ? 0.f : m_run;
+        uint32_t pk[32];  // hi, lo
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          // P times 2^6 vs / v_ref, in the exponent.  A block whose scale is next to nothing beside
+          // the reference (and one outside the pool) adds to the sum alone.
+          const float ratio = vs[i] / v_ref;
+          const bool tiny = !(ratio > 0x1p-60f);
+          const float off = tiny ? -m : log2f(ratio * kPScale) - m;
+          const float inv = tiny ? 1.f : 1.f / (ratio * kPScale);
+          float2 s2[2];
+#pragma unroll
+          for (int e = 0; e < 8; e += 2) {
+            uint32_t hi[2], lo[2];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+              const float2 x = ffma2(make_float2(sv[16 * i + 2 * (e + u)], sv[16 * i + 2 * (e + u) + 1]),
+                                     make_float2(f[i], f[i]), make_float2(off, off));
+              const float2 p = make_float2(ex2_approx(x.x), ex2_approx(x.y));
+              s2[u] = e == 0 ? p : fadd2(s2[u], p);
+              if (tiny) hi[u] = lo[u] = 0;
+              else split2(p, hi[u], lo[u]);
+            }
+            pk[4 * i + e / 2] = hi[0] | (hi[1] << 16);
+            pk[16 + 4 * i + e / 2] = lo[0] | (lo[1] << 16);
+          }
+          const float2 ss = fadd2(s2[0], s2[1]);
+          l_run += (ss.x + ss.y) * inv;
+        }
+        tmem_st32(tmem + lane_off + sb * KT, pk);
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sh.p_ready[sb]);
+    }
+    // ---- epilogue
+    if (ok) ok = mbar_wait_warp(&sh.pv_done[(ntiles - 1) & 1], ((ntiles - 1) >> 1) & 1, a.status);
+    tc_fence_after();
+    if (ok && warp_live) {
+      const bool live = r < rows_total;
+      const int32_t h = g * G + (r - j * G);
+      const int64_t orow = ((int64_t)b * a.D_max + j) * a.Hq + h;
+      const bool direct = parts == 1;
+      const int64_t prow = orow * L.splits + split;
+      const bool store = live && (direct ? dbg_in(orow, (int64_t)a.B * a.D_max * a.Hq, a.status)
+                                         : dbg_in(prow, (int64_t)a.B * a.D_max * a.Hq * L.splits, a.status));
+      const float of = v_ref / kPScale;
+      const float inv = l_run > 0.f ? of / l_run : 0.f;
+#pragma unroll 1
+      for (int c = 0; c < kD / 32; ++c) {
+        float ov[32];
+        tmem_ld32(tO + lane_off + c * 32, ov);
+        if (!store) continue;
+        if (direct) {
+          uint4* ob = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(a.o) + orow * kD + c * 32);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            // (a row that sees no key: 0, whatever its products are)
+            float x[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = l_run > 0.f ? ov[8 * i + e] * inv : 0.f;
+            ob[i] = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]),
+                               pack_bf16x2(x[6], x[7]));
+          }
+        } else {
+          float4* po = reinterpret_cast<float4*>(L.part_o + prow * kD + c * 32);
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            po[i] = make_float4(ov[4 * i] * of, ov[4 * i + 1] * of, ov[4 * i + 2] * of, ov[4 * i + 3] * of);
+        }
+      }
+      if (store) {
+        if (!direct) L.part_ml[prow] = make_float2(m_run, l_run);
+        else if (a.lse != nullptr)
+          a.lse[((int64_t)b * a.Hq + h) * a.D_max + j] =
+              l_run > 0.f ? (m_run + log2f(l_run)) * kLn2 : -INFINITY;
+      }
+    }
+  }
+  // ---- teardown
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 7) {
+    tc_fence_after();
+    tmem_dealloc(tmem, kCols);
+  }
+}
+
+// 2D view of a cache: {128 bytes, rows}, box {128, rows of a copy}.
+bool cache_map(CUtensorMap* map, const void* base, int64_t rows, int32_t box_rows) {
+  EncodeTiledFn fn = tensor_map_encoder();
+  if (fn == nullptr) return false;
+  const cuuint64_t dims[2] = {kD, (cuuint64_t)rows}, strides[1] = {kD};
+  const cuuint32_t box[2] = {kD, (cuuint32_t)box_rows}, estr[2] = {1, 1};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, estr,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+}  // namespace
+
+bool cache_attention_tc_runs(const CacheAttnArgs& a) {
+  const int64_t rows = (int64_t)a.D_max * (a.Hq / a.cache.Hkv);
+  return a.cache.d == kD && rows > 16 && (a.draft_pos == nullptr || a.D_max <= kMaxDrafts);
+}
+
+void cache_attention_tc_plan(int32_t B, int32_t Hq, int32_t Hkv, int32_t D_max, int32_t L_max,
+                             int32_t* splits, int32_t* min_tiles) {
+  const int64_t mtiles = ((int64_t)D_max * (Hq / Hkv) + kBM - 1) / kBM;
+  const int64_t base = (int64_t)B * Hkv * mtiles, tiles = (L_max + KT - 1) / KT;
+  const int64_t target = (int64_t)kCtasPerSm * device_sm_count();
+  const int64_t most = std::max<int64_t>(1, tiles / kMinTiles);
+  const int64_t least = (tiles + kMaxPartTiles - 1) / kMaxPartTiles;
+  *min_tiles = kMinTiles;
+  *splits = (int32_t)std::max<int64_t>(least, std::min<int64_t>(target / base, most));
+}
+
+cudaError_t launch_cache_attention_tc(const CacheAttnArgs& a, const CacheAttnLaunch& L,
+                                      cudaStream_t stream) {
+  const int32_t mtiles = (int32_t)(((int64_t)a.D_max * (a.Hq / a.cache.Hkv) + kBM - 1) / kBM);
+  const int64_t rows = (int64_t)a.cache.num_blocks * a.cache.Hkv * a.cache.block;
+  const int32_t box = std::min(a.cache.block, KT);
+  CUtensorMap tk, tv;
+  if (!cache_map(&tk, a.cache.k, rows, box) || !cache_map(&tv, a.cache.v, rows, box))
+    return cudaErrorInvalidValue;
+  const size_t smem = 1024 + 2 * kQBytes + 2 * kNS * kTileBytes + sizeof(Shared) + (size_t)L.max_blocks * 12;
+  const cudaError_t e = cudaFuncSetAttribute(
+      cache_attn_tc_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (e != cudaSuccess) return e;
+  const int64_t grid = (int64_t)a.B * a.cache.Hkv * mtiles * L.splits;
+  if (grid > INT32_MAX) return cudaErrorInvalidValue;
+  return launch_kernel(cache_attn_tc_kernel, dim3((unsigned)grid), dim3(kThreadsTC), smem, stream, true,
+                       tk, tv, a, L, mtiles);
+}
+
+}  // namespace ssd

@@ -2,23 +2,25 @@
 // 5th-generation tensor cores (include/ssd.h, ssd_cache_attention; 128-wide heads):
 //   O[b][j][h] = softmax_s(scale * Q[b][j][h] . (sk K[s]) + M(s, j)) (sv V[s]).
 //
-// K and V stay e4m3 from the cache to the products (kind::f8f6f4): they are
-// copied once by TMA, 128 bytes a key, and never widened.  Q and P are split in two
-// e4m3 terms each, x = hi + lo with hi the nearest e4m3 and lo the nearest to the rest:
-// 8 significant bits, as many as bf16 has, at the cost of twice the products, which run at twice
-// the rate of bf16's.  Q's rows are scaled by a power of two first (largest entry in
-// [128, 256)), P by 2^6 times its block's V scale over a reference scale, so that hi and lo use
-// e4m3's range; the K scale multiplies the scores.
+// K stays e4m3 from the cache to the products (kind::f8f6f4): it is copied by TMA, 128 bytes
+// a key, and never widened; Q is split in two e4m3 terms, x = hi + lo with hi the nearest
+// e4m3 and lo the nearest to the rest (8 significant bits, as many as bf16 has, at the cost of
+// twice the products, which run at twice the rate of bf16's), after its rows are scaled by a
+// power of two (largest entry in [128, 256)).  P, which changes with every tile, is rounded to
+// float16 instead (a split takes six instructions a pair, and the softmax is what bounds this
+// kernel): one warp widens V to float16, exactly, and the second product is kind::f16.  The K
+// scale of a block multiplies the scores, its V scale over a reference the probabilities.
 //
 // One CTA (8 warps, two CTAs per SM) per tile of 128 query rows (drafts x the query
 // heads of a KV head) and part of the sequence's keys, longest sequences first:
-//  warp 4 streams K and V in tiles of 64 keys through rings of kNS stages, a
-//    copy per cache block (TMA, 128-byte swizzle);
-//  warp 5 issues S = (Qhi + Qlo) K^T into one of two TMEM buffers, warp 6 O +=
-//    (Phi + Plo) V with P read from TMEM, where it replaced S;
+//  warp 4 streams K and V in tiles of 64 keys through rings of kNK and kNV
+//    stages, a copy per cache block (TMA, 128-byte swizzle);
+//  warp 5 issues S = (Qhi + Qlo) K^T into one of two TMEM buffers, warp 6 O += P V
+//    with P read from TMEM, where it replaced S; warp 7 widens V into one of two buffers
+//    (and clears the rows that hold no key);
 //  warps 0-3 (a thread a row) turn S into P.  The running maximum moves only when
-//    it grows by more than a factor of two; O is rescaled in TMEM when it does, or
-//    when a block's V scale is above twice the reference.
+//    it grows by more than 2^8; O is rescaled in TMEM when it does, or when a
+//    block's V scale is above 16 times the reference.
 #include <cuda_fp16.h>
 
 #include <algorithm>
@@ -32,7 +34,7 @@ namespace {
 constexpr int kD = 128;
 constexpr int kBM = 128;
 constexpr int KT = kCacheTile;
-constexpr int kNS = 4;                       // K and V stages
+constexpr int kNK = 3, kNV = 2;              // K and V stages
 constexpr int kTileBytes = KT * kD;          // one K (or V) tile
 constexpr int kQBytes = kBM * kD;            // one term of Q
 constexpr uint32_t kCols = 256;              // S/P x 2 (64 columns each), O at 128
@@ -43,8 +45,10 @@ constexpr int kMaxPartTiles = 256;           // at most 1024 block ids and scale
 constexpr int kMaxDrafts = 512;              // with positions of their own (kept in shared memory)
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
-constexpr float kGrowth = 1.f;               // log2 growth of the maximum that moves it
-constexpr float kPScale = 64.f;              // P <= 2^kGrowth: hi <= 64 * 2 * 2 = 256
+// log2 growth of the maximum, and of the V scale over its reference, that moves them: P
+// stays below 2^12 in float16
+constexpr float kGrowth = 8.f, kVGrowth = 4.f;
+constexpr int kWideBytes = 2 * kTileBytes;   // a V tile in float16
 
 // kind::f8f6f4, e4m3 A and B, fp32 D.
 __host__ __device__ constexpr uint32_t idesc_e4m3(int m, int n, bool b_mn_major) {
@@ -59,13 +63,10 @@ __device__ __forceinline__ void mma8_ss(uint32_t d_tmem, uint64_t adesc, uint64_
       "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
       : "memory");
 }
-__device__ __forceinline__ void mma8_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc,
-                                        uint32_t idesc, uint32_t accumulate) {
-  asm volatile(
-      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
-      " tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], [%1], %2, %3, p;\n}\n" ::"r"(d_tmem),
-      "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate)
-      : "memory");
+// kind::f16, float16 A and B, fp32 D.
+__host__ __device__ constexpr uint32_t idesc_f16(int m, int n, bool b_mn_major) {
+  return (1u << 4) | ((b_mn_major ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) |
+         ((uint32_t)(m >> 4) << 24);
 }
 
 // float16 pairs to e4m3 pairs and back (exactly).
@@ -115,16 +116,45 @@ __device__ __forceinline__ void tmem_ld64(uint32_t taddr, float* v) {
   for (int i = 0; i < 64; ++i) v[i] = __uint_as_float(r[i]);
 }
 
+// 16 consecutive 32-bit columns of this thread's TMEM lane (warp-collective).
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, float* v) {
+  uint32_t r[16];
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,"
+      "%15}, [%16];\n"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
+        "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]),
+        "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr)
+      : "memory");
+#pragma unroll
+  for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const float* v) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,"
+      "%14,%15,%16};\n"
+      "tcgen05.wait::st.sync.aligned;" ::"r"(taddr),
+      "r"(__float_as_uint(v[0])), "r"(__float_as_uint(v[1])), "r"(__float_as_uint(v[2])),
+      "r"(__float_as_uint(v[3])), "r"(__float_as_uint(v[4])), "r"(__float_as_uint(v[5])),
+      "r"(__float_as_uint(v[6])), "r"(__float_as_uint(v[7])), "r"(__float_as_uint(v[8])),
+      "r"(__float_as_uint(v[9])), "r"(__float_as_uint(v[10])), "r"(__float_as_uint(v[11])),
+      "r"(__float_as_uint(v[12])), "r"(__float_as_uint(v[13])), "r"(__float_as_uint(v[14])),
+      "r"(__float_as_uint(v[15]))
+      : "memory");
+}
+
 __device__ __forceinline__ uint64_t low_bits(int32_t n) {
   return n <= 0 ? 0ull : (n >= 64 ? ~0ull : ((1ull << n) - 1ull));
 }
 
 struct Shared {
-  uint64_t k_full[kNS], k_empty[kNS], v_full[kNS], v_empty[kNS];
+  uint64_t k_full[kNK], k_empty[kNK], v_full[kNV], v_empty[kNV];
+  uint64_t w_full[2];  // V widened
   uint64_t s_full[2], p_ready[2], pv_done[2];
   uint32_t tmem;
   int32_t seq;
-  int32_t bad;  // a draft position outside the grid, or a block outside the pool
   int32_t kflat[kMaxDrafts];
 };
 
@@ -136,11 +166,14 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   unsigned char* sQ = smem;                        // hi, lo
   unsigned char* sK = sQ + 2 * kQBytes;
-  unsigned char* sV = sK + kNS * kTileBytes;
-  Shared& sh = *reinterpret_cast<Shared*>(sV + kNS * kTileBytes);
+  unsigned char* sV = sK + kNK * kTileBytes;
+  unsigned char* sW = sV + kNV * kTileBytes;       // V in float16 [2][d / 64][KT][128 bytes]
+  Shared& sh = *reinterpret_cast<Shared*>(sW + 2 * kWideBytes);
+  // the part's blocks: id (-1: outside the pool), K scale, log2 of the V scale, its inverse
   int32_t* s_id = reinterpret_cast<int32_t*>(&sh + 1);
   float* s_ks = reinterpret_cast<float*>(s_id + L.max_blocks);
-  float* s_vs = s_ks + L.max_blocks;
+  float* s_lv = s_ks + L.max_blocks;
+  float* s_iv = s_lv + L.max_blocks;
   pdl_wait();
 
   const int32_t tid = threadIdx.x, lane = tid & 31, warp = (int32_t)warp_uniform(tid >> 5);
@@ -193,35 +226,41 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
   // ---- set-up
   __syncthreads();  // kflat is free again
   if (tid == 0) {
-    for (int i = 0; i < kNS; ++i) {
+    for (int i = 0; i < kNK; ++i) {
       mbar_init(&sh.k_full[i], 1);
       mbar_init(&sh.k_empty[i], 1);
+    }
+    for (int i = 0; i < kNV; ++i) {
       mbar_init(&sh.v_full[i], 1);
       mbar_init(&sh.v_empty[i], 1);
     }
     for (int i = 0; i < 2; ++i) {
+      mbar_init(&sh.w_full[i], 1);
       mbar_init(&sh.s_full[i], 1);
       mbar_init(&sh.p_ready[i], 4);
       mbar_init(&sh.pv_done[i], 1);
     }
     fence_barrier_init();
-    sh.bad = 0;
   }
   if (warp == 7) {
     tmem_alloc(&sh.tmem, kCols);
     tmem_relinquish();
   }
   if (warp == 4 && lane < 2) prefetch_tensormap(lane == 0 ? &tmK : &tmV);
+  bool bad = false;  // a block outside the pool
   for (int32_t i = tid; i < nb; i += kThreadsTC) {
     int32_t id = a.block_table[(int64_t)b * a.max_blocks + b_lo + i];
     if (id < 0 || id >= a.cache.num_blocks) {
       record_status(a.status, SSD_ERR_DEVICE_BOUNDS);
       id = -1;
+      bad = true;
     }
     s_id[i] = id;
     const int64_t at = (int64_t)max(id, 0) * Hkv + g;
     s_ks[i] = a.cache.k_scale[at];
-    s_vs[i] = id < 0 ? 0.f : a.cache.v_scale[at];
+    const float vs = a.cache.v_scale[at];
+    s_lv[i] = id < 0 ? -INFINITY : log2f(vs);
+    s_iv[i] = 1.f / vs;
   }
   if (a.draft_pos != nullptr) {
     for (int32_t j = tid; j < nd; j += kThreadsTC) {
@@ -274,7 +313,7 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
     fence_proxy_async_shared();
   }
   tc_fence_before();
-  __syncthreads();
+  const bool any_bad = __syncthreads_or(bad) != 0;
   tc_fence_after();
   const uint32_t tmem = sh.tmem, tO = tmem + 128;
 
@@ -296,38 +335,39 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
     const uint64_t pol = policy_evict_first();
     const int32_t rows = min(S, KT);
     bool ok = true;
-    int32_t t = 0;
+    int32_t t = 0, nk = 0, nv = 0;  // tiles; K and V copies issued
 #pragma unroll 1
     for (; t < ntiles && ok; ++t) {
-      const int s = t % kNS;
-      if (t >= kNS) {
-        ok = mbar_wait_warp(&sh.k_empty[s], ((t / kNS) - 1) & 1, a.status) &&
-             mbar_wait_warp(&sh.v_empty[s], ((t / kNS) - 1) & 1, a.status);
-        if (!ok) break;
-      }
       const int32_t c0 = k_lo + t * KT;
-      if (leader) {
-        // (blocks behind the last key are not copied: their rows stay what they were)
-        const int32_t n = min(KT, k_hi - c0);
-        const uint32_t bytes = (uint32_t)((n + rows - 1) / rows * rows * kD);
-        mbar_arrive_expect_tx(&sh.k_full[s], bytes);
-        mbar_arrive_expect_tx(&sh.v_full[s], bytes);
+      // (blocks behind the last key are not copied: their rows stay what they were)
+      const int32_t n = min(KT, k_hi - c0);
+      const uint32_t bytes = (uint32_t)((n + rows - 1) / rows * rows * kD);
+      auto copy = [&](unsigned char* dst, const CUtensorMap* map, uint64_t* full) {
+        if (leader) {
+          mbar_arrive_expect_tx(full, bytes);
 #pragma unroll 1
-        for (int32_t k = 0; k < n; k += rows) {
-          const int32_t id = max(s_id[((c0 + k) >> S_log) - b_lo], 0);
-          const int32_t row = (id * Hkv + g) * S + ((c0 + k) & (S - 1));
-          tma_load_2d(sK + s * kTileBytes + k * kD, &tmK, 0, row, &sh.k_full[s], pol);
-          tma_load_2d(sV + s * kTileBytes + k * kD, &tmV, 0, row, &sh.v_full[s], pol);
+          for (int32_t k = 0; k < n; k += rows) {
+            const int32_t id = max(s_id[((c0 + k) >> S_log) - b_lo], 0);
+            const int32_t row = (id * Hkv + g) * S + ((c0 + k) & (S - 1));
+            tma_load_2d(dst + k * kD, map, 0, row, full, pol);
+          }
         }
-      }
-      __syncwarp();
+        __syncwarp();
+      };
+      if (t >= kNK) ok = mbar_wait_warp(&sh.k_empty[t % kNK], ((t / kNK) - 1) & 1, a.status);
+      if (!ok) break;
+      copy(sK + t % kNK * kTileBytes, &tmK, &sh.k_full[t % kNK]);
+      nk = t + 1;
+      if (t >= kNV) ok = mbar_wait_warp(&sh.v_empty[t % kNV], ((t / kNV) - 1) & 1, a.status);
+      if (!ok) break;
+      copy(sV + t % kNV * kTileBytes, &tmV, &sh.v_full[t % kNV]);
+      nv = t + 1;
     }
     // after a wait that gave up, the copies in flight still land here
-    if (!ok)
-      for (int32_t u = max(0, t - kNS); u < t; ++u) {
-        mbar_drain(&sh.k_full[u % kNS], (u / kNS) & 1);
-        mbar_drain(&sh.v_full[u % kNS], (u / kNS) & 1);
-      }
+    if (!ok) {
+      for (int32_t u = max(0, nk - kNK); u < nk; ++u) mbar_drain(&sh.k_full[u % kNK], (u / kNK) & 1);
+      for (int32_t u = max(0, nv - kNV); u < nv; ++u) mbar_drain(&sh.v_full[u % kNV], (u / kNV) & 1);
+    }
   } else if (warp == 5) {
     // ----------------------------------------------------------- S products
     const uint32_t tSu = warp_uniform(tmem), aQ = warp_uniform(smem_u32(sQ));
@@ -339,8 +379,8 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
     bool ok = true;
 #pragma unroll 1
     for (; t < ntiles; ++t) {
-      const int s = t % kNS, sb = t & 1;
-      ok = mbar_wait_warp(&sh.k_full[s], (t / kNS) & 1, a.status);
+      const int s = t % kNK, sb = t & 1;
+      ok = mbar_wait_warp(&sh.k_full[s], (t / kNK) & 1, a.status);
       // the S/P buffer is free once PV of tile t - 2 is done
       if (ok && t >= 2) ok = mbar_wait_warp(&sh.pv_done[sb], ((t >> 1) - 1) & 1, a.status);
       if (!ok) break;
@@ -362,47 +402,65 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
   } else if (warp == 6) {
     // ---------------------------------------------------------- PV products
     const uint32_t tSu = warp_uniform(tmem), tOu = warp_uniform(tO);
-    const uint32_t aV = warp_uniform(smem_u32(sV));
+    const uint32_t aW = warp_uniform(smem_u32(sW));
     const bool leader = elect_one();
-    constexpr uint32_t kIdesc = idesc_e4m3(kBM, kD, true);
+    constexpr uint32_t kIdesc = idesc_f16(kBM, kD, true);
     int32_t t = 0;
     bool ok = true;
 #pragma unroll 1
     for (; t < ntiles; ++t) {
-      const int s = t % kNS, sb = t & 1;
-      const int32_t c0 = k_lo + t * KT;
-      ok = mbar_wait_warp(&sh.v_full[s], (t / kNS) & 1, a.status);
-      if (!ok) break;
-      const uint64_t live = live_keys(c0);
-      if (live != ~0ull) {
-        // rows without a key hold whatever the pool holds, and their P of 0 times a NaN
-        // would be one: cleared (whole rows, so the swizzle does not matter)
-#pragma unroll 1
-        for (int32_t i = lane; i < KT * 8; i += 32)
-          if (!(live >> (i >> 3) & 1ull))
-            *reinterpret_cast<uint4*>(sV + s * kTileBytes + i * 16) = make_uint4(0u, 0u, 0u, 0u);
-        fence_proxy_async_shared();
-        __syncwarp();
-      }
-      ok = mbar_wait_warp(&sh.p_ready[sb], (t >> 1) & 1, a.status);
+      const int sb = t & 1;
+      ok = mbar_wait_warp(&sh.w_full[sb], (t >> 1) & 1, a.status) &&
+           mbar_wait_warp(&sh.p_ready[sb], (t >> 1) & 1, a.status);
       if (!ok) break;
       tc_fence_after();
-      // A = P in TMEM (32 keys = 8 columns a step; lo 16 columns behind hi), B = V
-      // (MN-major: 8-key groups 1 KB apart; 32 keys = 4 KB)
-      const uint64_t dv = smem_desc(aV + s * kTileBytes, kTileBytes, 1024);
+      // A = P in TMEM (16 keys = 8 columns a step), B = V in float16 (MN-major: blocks of 64
+      // columns KT * 128 bytes apart, 8-key groups 1 KB apart; 16 keys = 2 KB)
+      const uint64_t dv = smem_desc(aW + sb * kWideBytes, KT * 128, 1024);
       if (leader) {
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-          for (int kk = 0; kk < KT / 32; ++kk)
-            mma8_ts(tOu, tSu + sb * KT + u * 16 + kk * 8, smem_desc_at(dv, kk * 4096), kIdesc,
-                    t + u + kk > 0 ? 1u : 0u);
+        for (int kk = 0; kk < KT / 16; ++kk)
+          mma_ts(tOu, tSu + sb * KT + kk * 8, smem_desc_at(dv, kk * 2048), kIdesc, t + kk > 0 ? 1u : 0u);
         mma_commit(&sh.pv_done[sb]);
-        mma_commit(&sh.v_empty[s]);
       }
       __syncwarp();
     }
     if (!ok && t > 0) mbar_drain(&sh.pv_done[(t - 1) & 1], ((t - 1) >> 1) & 1);
+  } else if (warp == 7) {
+    // ------------------------------------------------------------- V widened
+    // Rows without a key hold whatever the pool holds, and their P of 0 times a NaN would
+    // be one: cleared.  A lane takes 16 values of a key; of its two 16-byte halves the lanes of
+    // the upper columns store the second first, so that eight lanes fill all the banks.
+#pragma unroll 1
+    for (int32_t t = 0; t < ntiles; ++t) {
+      const int s = t % kNV, sb = t & 1;
+      const int32_t c0 = k_lo + t * KT;
+      bool ok = mbar_wait_warp(&sh.v_full[s], (t / kNV) & 1, a.status);
+      if (ok && t >= 2) ok = mbar_wait_warp(&sh.pv_done[sb], ((t >> 1) - 1) & 1, a.status);
+      if (!ok) break;
+      const uint64_t live = c0 >= start && c0 + KT <= k_hi && !any_bad ? ~0ull : live_keys(c0);
+      const int c = lane & 7;
+      const unsigned char* from = sV + s * kTileBytes;
+      unsigned char* to = sW + sb * kWideBytes + (c >> 2) * (KT * 128);
+#pragma unroll 4
+      for (int i = 0; i < KT / 4; ++i) {
+        const int key = i * 4 + (lane >> 3);
+        uint4 w = *reinterpret_cast<const uint4*>(from + key * 128 + ((c ^ (key & 7)) << 4));
+        if (!(live >> key & 1ull)) w = make_uint4(0u, 0u, 0u, 0u);
+        uint4 h[2];
+        h[0] = make_uint4(f16_of_e4m3(w.x), f16_of_e4m3(w.x >> 16), f16_of_e4m3(w.y), f16_of_e4m3(w.y >> 16));
+        h[1] = make_uint4(f16_of_e4m3(w.z), f16_of_e4m3(w.z >> 16), f16_of_e4m3(w.w), f16_of_e4m3(w.w >> 16));
+        const int first = c >> 2, c2 = 2 * (c & 3);
+        *reinterpret_cast<uint4*>(to + key * 128 + (((c2 + first) ^ (key & 7)) << 4)) = first ? h[1] : h[0];
+        *reinterpret_cast<uint4*>(to + key * 128 + (((c2 + 1 - first) ^ (key & 7)) << 4)) = first ? h[0] : h[1];
+      }
+      fence_proxy_async_shared();
+      __syncwarp();
+      if (lane == 0) {
+        mbar_arrive(&sh.w_full[sb]);
+        mbar_arrive(&sh.v_empty[s]);
+      }
+    }
   } else if (warp < 4) {
     // ------------------------------------------------------------- softmax
     const uint32_t lane_off = (uint32_t)(warp * 32) << 16;
@@ -413,13 +471,24 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
     if (r < rows_total) qpos = a.draft_pos != nullptr ? sh.kflat[j] : cache + j;
     // keys below this one are visible to every row of the warp
     const int32_t mask_from = min(cache, __reduce_min_sync(0xffffffffu, qpos) + 1);
-    float m_run = -INFINITY, l_run = 0.f, v_ref = 0.f;
+    float m_run = -INFINITY, l_run = 0.f;
+    float lg_ref = -INFINITY, v_ref = 0.f;  // reference of the V scales and its log2
     bool ok = true;
     int32_t t = 0;
 #pragma unroll 1
     for (; t < ntiles; ++t) {
       const int sb = t & 1;
       const int32_t c0 = k_lo + t * KT;
+      // scales of the tile's groups of 16 keys: K's, V's log2 and inverse
+      float f[4], lg[4], iv[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int32_t at = (min(c0 + 16 * i, k_hi - 1) >> S_log) - b_lo;
+        f[i] = fmaxf(rowc * s_ks[at], 1e-37f);
+        lg[i] = s_lv[at];
+        iv[i] = s_iv[at];
+      }
+      const float lg_max = fmaxf(fmaxf(lg[0], lg[1]), fmaxf(lg[2], lg[3]));
       if (!mbar_wait(&sh.s_full[sb], (t >> 1) & 1, a.status)) ok = false;
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
@@ -427,20 +496,7 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
       if (warp_live) {
         float sv[64];
         tmem_ld64(tmem + lane_off + sb * KT, sv);
-        // scales of the tile's four groups of 16 keys
-        float f[4], vs[4], v_max = 0.f;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int32_t k = min(c0 + 16 * i, k_hi - 1);
-          const int32_t at = (k >> S_log) - b_lo;
-          f[i] = fmaxf(rowc * s_ks[at], 1e-37f);
-          vs[i] = c0 + 16 * i < k_hi ? s_vs[at] : 0.f;
-          v_max = fmaxf(v_max, vs[i]);
-        }
-        const uint64_t live = c0 + KT > mask_from || c0 < start ||  c0 + KT > k_hi ||
-                              !(fminf(fminf(vs[0], vs[1]), fminf(vs[2], vs[3])) > 0.f)
-                                  ? live_keys(c0) : ~0ull;
-        if (live != ~0ull || c0 + KT > mask_from) {
+        if (c0 + KT > mask_from || c0 < start || c0 + KT > k_hi || any_bad) {
           uint64_t keep;
           if (a.draft_pos == nullptr) {
             keep = low_bits(qpos < 0x7fffffff ? qpos + 1 - c0 : KT);
@@ -452,7 +508,7 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
               if (p >= 0 && p <= qpos) keep |= 1ull << k;
             }
           }
-          keep &= live;
+          keep &= live_keys(c0);
 #pragma unroll
           for (int i = 0; i < 64; ++i)
             if (!(keep >> i & 1ull)) sv[i] = -INFINITY;
@@ -461,10 +517,13 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const float* x = sv + 16 * i;
-          float y = fmax3(x[0], x[1], x[2]);
+          float y = fmax3(x[0], x[1], x[2]), z = fmax3(x[3], x[4], x[5]);
 #pragma unroll
-          for (int e = 3; e < 15; e += 2) y = fmax3(y, x[e], x[e + 1]);
-          mx = fmaxf(mx, fmaxf(y, x[15]) * f[i]);
+          for (int e = 6; e < 14; e += 4) {
+            y = fmax3(y, x[e], x[e + 1]);
+            z = fmax3(z, x[e + 2], x[e + 3]);
+          }
+          mx = fmaxf(mx, fmax3(fmaxf(y, z), x[14], x[15]) * f[i]);
         }
         float alpha = 1.f;
         bool moved = false;
@@ -474,9 +533,11 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
           moved = true;
         }
         l_run *= alpha;
-        if (!(v_max <= 2.f * v_ref)) {  // the same in every thread
-          alpha *= v_ref / v_max;
-          v_ref = v_max;
+        if (lg_max > lg_ref + kVGrowth || (lg_ref == -INFINITY && lg_max > -INFINITY)) {
+          // (the same in every thread)
+          alpha *= lg_ref == -INFINITY ? 0.f : exp2f(lg_ref - lg_max);
+          lg_ref = lg_max;
+          v_ref = exp2f(lg_ref);
           moved = true;
         }
         if (t > 0 && __any_sync(0xffffffffu, moved)) {
@@ -484,42 +545,38 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
           ok = mbar_wait_warp(&sh.pv_done[(t - 1) & 1], ((t - 1) >> 1) & 1, a.status);
           tc_fence_after();
 #pragma unroll 1
-          for (int c = 0; c < kD / 32; ++c) {
-            float ov[32];
-            tmem_ld32(tO + lane_off + c * 32, ov);
+          for (int c = 0; c < kD / 16; ++c) {
+            float ov[16];
+            tmem_ld16(tO + lane_off + c * 16, ov);
 #pragma unroll
-            for (int i = 0; i < 32; ++i) ov[i] *= alpha;
-            tmem_st32(tO + lane_off + c * 32, ov);
+            for (int i = 0; i < 16; ++i) ov[i] *= alpha;
+            tmem_st16(tO + lane_off + c * 16, ov);
           }
         }
         const float m = m_run == -INFINITY ? 0.f : m_run;
-        uint32_t pk[32];  // hi, lo
+        uint32_t pk[32];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          // P times 2^6 vs / v_ref, in the exponent.  A block whose scale is next to nothing beside
-          // the reference (and one outside the pool) adds to the sum alone.
-          const float ratio = vs[i] / v_ref;
-          const bool tiny = !(ratio > 0x1p-60f);
-          const float off = tiny ? -m : log2f(ratio * kPScale) - m;
-          const float inv = tiny ? 1.f : 1.f / (ratio * kPScale);
+          // P times its V scale over the reference, in the exponent.  A block whose scale is
+          // next to nothing beside the reference (and one outside the pool) adds to the sum alone.
+          const bool tiny = !(lg[i] - lg_ref > -60.f);
+          const float off = tiny ? -m : lg[i] - lg_ref - m;
           float2 s2[2];
 #pragma unroll
-          for (int e = 0; e < 8; e += 2) {
-            uint32_t hi[2], lo[2];
+          for (int e = 0; e < 8; ++e) {
+            const float2 x = ffma2(make_float2(sv[16 * i + 2 * e], sv[16 * i + 2 * e + 1]),
+                                   make_float2(f[i], f[i]), make_float2(off, off));
+            const float2 p = make_float2(ex2_approx(x.x), ex2_approx(x.y));
+            s2[e & 1] = e < 2 ? p : fadd2(s2[e & 1], p);
+            const __half2 h = __floats2half2_rn(p.x, p.y);
+            pk[8 * i + e] = *reinterpret_cast<const uint32_t*>(&h);
+          }
+          if (tiny) {
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-              const float2 x = ffma2(make_float2(sv[16 * i + 2 * (e + u)], sv[16 * i + 2 * (e + u) + 1]),
-                                     make_float2(f[i], f[i]), make_float2(off, off));
-              const float2 p = make_float2(ex2_approx(x.x), ex2_approx(x.y));
-              s2[u] = e == 0 ? p : fadd2(s2[u], p);
-              if (tiny) hi[u] = lo[u] = 0;
-              else split2(p, hi[u], lo[u]);
-            }
-            pk[4 * i + e / 2] = hi[0] | (hi[1] << 16);
-            pk[16 + 4 * i + e / 2] = lo[0] | (lo[1] << 16);
+            for (int e = 0; e < 8; ++e) pk[8 * i + e] = 0;
           }
           const float2 ss = fadd2(s2[0], s2[1]);
-          l_run += (ss.x + ss.y) * inv;
+          l_run += (ss.x + ss.y) * (tiny ? 1.f : v_ref * iv[i]);
         }
         tmem_st32(tmem + lane_off + sb * KT, pk);
       }
@@ -538,8 +595,7 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
       const int64_t prow = orow * L.splits + split;
       const bool store = live && (direct ? dbg_in(orow, (int64_t)a.B * a.D_max * a.Hq, a.status)
                                          : dbg_in(prow, (int64_t)a.B * a.D_max * a.Hq * L.splits, a.status));
-      const float of = v_ref / kPScale;
-      const float inv = l_run > 0.f ? of / l_run : 0.f;
+      const float inv = l_run > 0.f ? v_ref / l_run : 0.f;
 #pragma unroll 1
       for (int c = 0; c < kD / 32; ++c) {
         float ov[32];
@@ -560,7 +616,7 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
           float4* po = reinterpret_cast<float4*>(L.part_o + prow * kD + c * 32);
 #pragma unroll
           for (int i = 0; i < 8; ++i)
-            po[i] = make_float4(ov[4 * i] * of, ov[4 * i + 1] * of, ov[4 * i + 2] * of, ov[4 * i + 3] * of);
+            po[i] = make_float4(ov[4 * i] * v_ref, ov[4 * i + 1] * v_ref, ov[4 * i + 2] * v_ref, ov[4 * i + 3] * v_ref);
         }
       }
       if (store) {
@@ -617,7 +673,8 @@ cudaError_t launch_cache_attention_tc(const CacheAttnArgs& a, const CacheAttnLau
   CUtensorMap tk, tv;
   if (!cache_map(&tk, a.cache.k, rows, box) || !cache_map(&tv, a.cache.v, rows, box))
     return cudaErrorInvalidValue;
-  const size_t smem = 1024 + 2 * kQBytes + 2 * kNS * kTileBytes + sizeof(Shared) + (size_t)L.max_blocks * 12;
+  const size_t smem = 1024 + 2 * kQBytes + (kNK + kNV) * kTileBytes + 2 * kWideBytes + sizeof(Shared) +
+                      (size_t)L.max_blocks * 16;
   const cudaError_t e = cudaFuncSetAttribute(
       cache_attn_tc_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;

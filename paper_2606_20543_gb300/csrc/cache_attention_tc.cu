@@ -428,9 +428,14 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
     if (!ok && t > 0) mbar_drain(&sh.pv_done[(t - 1) & 1], ((t - 1) >> 1) & 1);
   } else if (warp == 7) {
     // ------------------------------------------------------------- V widened
-    // Rows without a key hold whatever the pool holds, and their P of 0 times a NaN would
-    // be one: cleared.  A lane takes 16 values of a key; of its two 16-byte halves the lanes of
-    // the upper columns store the second first, so that eight lanes fill all the banks.
+    // A lane takes 16 values (a 16-byte chunk) of a key, eight keys by four chunks a step:
+    // then a lane's places in the swizzled tiles are fixed, and eight lanes' stores fill all
+    // banks (with eight chunks of a key a step and the halves swapped to avoid conflicts the
+    // warp took 2600 cycles a tile).  Rows without a key hold whatever the pool holds, and
+    // their P of 0 times a NaN would be one: cleared.
+    const int c = lane & 3, k8 = lane >> 2;
+    const uint32_t src0 = k8 * 128 + ((c ^ k8) << 4), src1 = k8 * 128 + (((c + 4) ^ k8) << 4);
+    const uint32_t dst0 = k8 * 128 + (((2 * c) ^ k8) << 4), dst1 = k8 * 128 + (((2 * c + 1) ^ k8) << 4);
 #pragma unroll 1
     for (int32_t t = 0; t < ntiles; ++t) {
       const int s = t % kNV, sb = t & 1;
@@ -438,21 +443,22 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
       bool ok = mbar_wait_warp(&sh.v_full[s], (t / kNV) & 1, a.status);
       if (ok && t >= 2) ok = mbar_wait_warp(&sh.pv_done[sb], ((t >> 1) - 1) & 1, a.status);
       if (!ok) break;
-      const uint64_t live = c0 >= start && c0 + KT <= k_hi && !any_bad ? ~0ull : live_keys(c0);
-      const int c = lane & 7;
       const unsigned char* from = sV + s * kTileBytes;
-      unsigned char* to = sW + sb * kWideBytes + (c >> 2) * (KT * 128);
+      unsigned char* to = sW + sb * kWideBytes;
+      const bool whole = c0 >= start && c0 + KT <= k_hi && !any_bad;
+      const uint64_t live = whole ? ~0ull : live_keys(c0);
 #pragma unroll 4
-      for (int i = 0; i < KT / 4; ++i) {
-        const int key = i * 4 + (lane >> 3);
-        uint4 w = *reinterpret_cast<const uint4*>(from + key * 128 + ((c ^ (key & 7)) << 4));
-        if (!(live >> key & 1ull)) w = make_uint4(0u, 0u, 0u, 0u);
-        uint4 h[2];
-        h[0] = make_uint4(f16_of_e4m3(w.x), f16_of_e4m3(w.x >> 16), f16_of_e4m3(w.y), f16_of_e4m3(w.y >> 16));
-        h[1] = make_uint4(f16_of_e4m3(w.z), f16_of_e4m3(w.z >> 16), f16_of_e4m3(w.w), f16_of_e4m3(w.w >> 16));
-        const int first = c >> 2, c2 = 2 * (c & 3);
-        *reinterpret_cast<uint4*>(to + key * 128 + (((c2 + first) ^ (key & 7)) << 4)) = first ? h[1] : h[0];
-        *reinterpret_cast<uint4*>(to + key * 128 + (((c2 + 1 - first) ^ (key & 7)) << 4)) = first ? h[0] : h[1];
+      for (int i = 0; i < KT / 8; ++i) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {  // blocks of 64 columns
+          uint4 w = *reinterpret_cast<const uint4*>(from + i * 1024 + (h ? src1 : src0));
+          if (!whole && !(live >> (8 * i + k8) & 1ull)) w = make_uint4(0u, 0u, 0u, 0u);
+          unsigned char* at = to + h * (KT * 128) + i * 1024;
+          *reinterpret_cast<uint4*>(at + dst0) = make_uint4(
+              f16_of_e4m3(w.x), f16_of_e4m3(w.x >> 16), f16_of_e4m3(w.y), f16_of_e4m3(w.y >> 16));
+          *reinterpret_cast<uint4*>(at + dst1) = make_uint4(
+              f16_of_e4m3(w.z), f16_of_e4m3(w.z >> 16), f16_of_e4m3(w.w), f16_of_e4m3(w.w >> 16));
+        }
       }
       fence_proxy_async_shared();
       __syncwarp();
@@ -481,12 +487,19 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
       const int32_t c0 = k_lo + t * KT;
       // scales of the tile's groups of 16 keys: K's, V's log2 and inverse
       float f[4], lg[4], iv[4];
+      if (S_log >= 6) {  // the tile is of one block
+        const int32_t at = (c0 >> S_log) - b_lo;
+        f[0] = f[1] = f[2] = f[3] = fmaxf(rowc * s_ks[at], 1e-37f);
+        lg[0] = lg[1] = lg[2] = lg[3] = s_lv[at];
+        iv[0] = iv[1] = iv[2] = iv[3] = s_iv[at];
+      } else {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int32_t at = (min(c0 + 16 * i, k_hi - 1) >> S_log) - b_lo;
-        f[i] = fmaxf(rowc * s_ks[at], 1e-37f);
-        lg[i] = s_lv[at];
-        iv[i] = s_iv[at];
+        for (int i = 0; i < 4; ++i) {
+          const int32_t at = (min(c0 + 16 * i, k_hi - 1) >> S_log) - b_lo;
+          f[i] = fmaxf(rowc * s_ks[at], 1e-37f);
+          lg[i] = s_lv[at];
+          iv[i] = s_iv[at];
+        }
       }
       const float lg_max = fmaxf(fmaxf(lg[0], lg[1]), fmaxf(lg[2], lg[3]));
       if (!mbar_wait(&sh.s_full[sb], (t >> 1) & 1, a.status)) ok = false;

@@ -8,17 +8,18 @@
 // twice the products, which run at twice the rate of bf16's), after its rows are scaled by a
 // power of two (largest entry in [128, 256)).  P, which changes with every tile, is rounded to
 // float16 instead (a split takes six instructions a pair, and the softmax is what bounds this
-// kernel): one warp widens V to float16, exactly, and the second product is kind::f16.  The K
+// kernel): four warps widen V to float16, exactly, and the second product is kind::f16.  The K
 // scale of a block multiplies the scores, its V scale over a reference the probabilities.
 //
-// One CTA (8 warps, two CTAs per SM) per tile of 128 query rows (drafts x the query
+// One CTA (12 warps, two CTAs per SM) per tile of 128 query rows (drafts x the query
 // heads of a KV head) and part of the sequence's keys, longest sequences first:
 //  warp 4 streams K and V in tiles of 64 keys through rings of kNK and kNV
 //    stages, a copy per cache block (TMA, 128-byte swizzle);
 //  warp 5 issues S = (Qhi + Qlo) K^T into one of two TMEM buffers, warp 6 O += P V
-//    with P read from TMEM, where it replaced S; warp 7 widens V into one of two buffers
-//    (and clears the rows that hold no key);
-//  warps 0-3 (a thread a row) turn S into P.  The running maximum moves only when
+//    with P read from TMEM, where it replaced S; warps 8-11 widen V into one of two buffers
+//    (and clear the rows that hold no key; one warp alone took 2300 cycles a tile, twice the
+//    softmax);
+//  warps 0-3 (a thread a row, with the registers that the other warps give up) turn S into P.  The running maximum moves only when
 //    it grows by more than 2^8; O is rescaled in TMEM when it does, or when a
 //    block's V scale is above 16 times the reference.
 #include <cuda_fp16.h>
@@ -38,7 +39,10 @@ constexpr int kNK = 3, kNV = 2;              // K and V stages
 constexpr int kTileBytes = KT * kD;          // one K (or V) tile
 constexpr int kQBytes = kBM * kD;            // one term of Q
 constexpr uint32_t kCols = 256;              // S/P x 2 (64 columns each), O at 128
-constexpr int kThreadsTC = 256;
+constexpr int kThreadsTC = 384;
+// Registers of a thread: 80 at launch (two CTAs per SM), then 144 for the softmax's warps and
+// 48 for the eight others: 144 + 2 * 48 = 3 * 80.
+constexpr int kRegsSoftmax = 144, kRegsOther = 48;
 constexpr int kCtasPerSm = 2;
 constexpr int kMinTiles = 6;                 // a part's fewest tiles
 constexpr int kMaxPartTiles = 256;           // at most 1024 block ids and scales in shared memory
@@ -90,32 +94,6 @@ __device__ __forceinline__ void split2(float2 x, uint32_t& hi, uint32_t& lo) {
   lo = e4m3_of_f16(*reinterpret_cast<const uint32_t*>(&rest));
 }
 
-// 64 consecutive 32-bit columns of this thread's TMEM lane (warp-collective).
-__device__ __forceinline__ void tmem_ld64(uint32_t taddr, float* v) {
-  uint32_t r[64];
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x64.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,"
-      "%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32,%33,%34,%35,%36,"
-      "%37,%38,%39,%40,%41,%42,%43,%44,%45,%46,%47,%48,%49,%50,%51,%52,%53,%54,%55,%56,%57,%58,"
-      "%59,%60,%61,%62,%63}, [%64];\n"
-      "tcgen05.wait::ld.sync.aligned;"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
-        "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]),
-        "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]),
-        "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]),
-        "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31]),
-        "=r"(r[32]), "=r"(r[33]), "=r"(r[34]), "=r"(r[35]), "=r"(r[36]), "=r"(r[37]),
-        "=r"(r[38]), "=r"(r[39]), "=r"(r[40]), "=r"(r[41]), "=r"(r[42]), "=r"(r[43]),
-        "=r"(r[44]), "=r"(r[45]), "=r"(r[46]), "=r"(r[47]), "=r"(r[48]), "=r"(r[49]),
-        "=r"(r[50]), "=r"(r[51]), "=r"(r[52]), "=r"(r[53]), "=r"(r[54]), "=r"(r[55]),
-        "=r"(r[56]), "=r"(r[57]), "=r"(r[58]), "=r"(r[59]), "=r"(r[60]), "=r"(r[61]),
-        "=r"(r[62]), "=r"(r[63])
-      : "r"(taddr)
-      : "memory");
-#pragma unroll
-  for (int i = 0; i < 64; ++i) v[i] = __uint_as_float(r[i]);
-}
-
 // 16 consecutive 32-bit columns of this thread's TMEM lane (warp-collective).
 __device__ __forceinline__ void tmem_ld16(uint32_t taddr, float* v) {
   uint32_t r[16];
@@ -145,8 +123,28 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const float* v) {
       : "memory");
 }
 
+// Store 8 columns, without the wait.
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t* v) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(taddr),
+               "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+               : "memory");
+}
+
 __device__ __forceinline__ uint64_t low_bits(int32_t n) {
   return n <= 0 ? 0ull : (n >= 64 ? ~0ull : ((1ull << n) - 1ull));
+}
+
+// mbar_drain(), inlined: a call has no place beside setmaxnreg.
+__device__ __forceinline__ void drain(uint64_t* bar, uint32_t parity) {
+#pragma unroll 1
+  for (int i = 0; i < (1 << 14) && !mbar_try_wait(bar, parity); ++i) __nanosleep(256);
+}
+
+__device__ __forceinline__ void take_registers() {
+  asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
+}
+__device__ __forceinline__ void give_registers() {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOther));
 }
 
 struct Shared {
@@ -154,7 +152,8 @@ struct Shared {
   uint64_t w_full[2];  // V widened
   uint64_t s_full[2], p_ready[2], pv_done[2];
   uint32_t tmem;
-  int32_t seq;
+  int3 seq;             // the sequence, its cache length and drafts
+  float rowc[kBM];      // a row's factor of the scores
   int32_t kflat[kMaxDrafts];
 };
 
@@ -186,12 +185,13 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
   const int32_t g = unit % Hkv, rank = unit / Hkv;
 
   // ---- the sequence: the rank-th longest (batches above 256 keep their order)
-  int32_t b = rank;
-  if (a.B > 1 && a.B <= kThreadsTC) {
+  int32_t b = rank, cache, nd;
+  if (a.B > 1 && a.B <= kLptMax) {
     int32_t* keys = sh.kflat;  // (not in use yet)
-    int32_t mine = 0;
+    int32_t mine = 0, c = 0, n = 0;
     if (tid < a.B) {
-      const int32_t c = a.cache_len[tid], n = a.n_drafts[tid];
+      c = a.cache_len[tid];
+      n = a.n_drafts[tid];
       mine = cache_lengths_ok(a, c, n) && n > 0 ? c + n : 0;
       keys[tid] = mine;
     }
@@ -203,12 +203,16 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
         const int32_t kj = keys[j];
         r += kj > mine || (kj == mine && j < tid);
       }
-      if (r == rank) sh.seq = tid;
+      if (r == rank) sh.seq = make_int3(tid, c, n);
     }
     __syncthreads();
-    b = sh.seq;
+    b = sh.seq.x;
+    cache = sh.seq.y;
+    nd = sh.seq.z;
+  } else {
+    cache = a.cache_len[b];
+    nd = a.n_drafts[b];
   }
-  const int32_t cache = a.cache_len[b], nd = a.n_drafts[b];
   if (!cache_lengths_ok(a, cache, nd)) {
     if (tid == 0 && split == 0 && g == 0 && mtile == 0) record_status(a.status, SSD_ERR_DEVICE_BOUNDS);
     return;
@@ -232,10 +236,10 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
     }
     for (int i = 0; i < kNV; ++i) {
       mbar_init(&sh.v_full[i], 1);
-      mbar_init(&sh.v_empty[i], 1);
+      mbar_init(&sh.v_empty[i], 4);
     }
     for (int i = 0; i < 2; ++i) {
-      mbar_init(&sh.w_full[i], 1);
+      mbar_init(&sh.w_full[i], 4);
       mbar_init(&sh.s_full[i], 1);
       mbar_init(&sh.p_ready[i], 4);
       mbar_init(&sh.pv_done[i], 1);
@@ -248,7 +252,9 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
   }
   if (warp == 4 && lane < 2) prefetch_tensormap(lane == 0 ? &tmK : &tmV);
   bool bad = false;  // a block outside the pool
-  for (int32_t i = tid; i < nb; i += kThreadsTC) {
+  // warps 4-7: the part's blocks and the drafts' positions; the others: Q
+  const bool stages = warp >= 4 && warp < 8;
+  for (int32_t i = stages ? tid - 128 : nb; i < nb; i += 128) {
     int32_t id = a.block_table[(int64_t)b * a.max_blocks + b_lo + i];
     if (id < 0 || id >= a.cache.num_blocks) {
       record_status(a.status, SSD_ERR_DEVICE_BOUNDS);
@@ -263,50 +269,55 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
     s_iv[i] = 1.f / vs;
   }
   if (a.draft_pos != nullptr) {
-    for (int32_t j = tid; j < nd; j += kThreadsTC) {
+    for (int32_t j = stages ? tid - 128 : nd; j < nd; j += 128) {
       const int32_t p = cache_flat_pos(a, b, cache, j);
       if (p < 0 && split == 0 && g == 0 && mtile == 0) record_status(a.status, SSD_ERR_DEVICE_BOUNDS);
       sh.kflat[j] = p;
     }
   }
-  // Q: row `tid` of the tile, as two terms of a row scaled to [128, 256)
-  float rowc = 0.f;
-  if (tid < kBM) {
-    const int32_t r = row0 + tid;
+  // Q as two terms, two threads a row, the row scaled to [128, 256) (rows behind the last
+  // one stay what they were: they reach no other row)
+  const int32_t q_row = warp < 4 ? tid >> 1 : (tid - 128) >> 1;
+  if (!stages && row0 + (q_row & ~15) < rows_total) {
+    const int32_t r = row0 + q_row, half = tid & 1;
     const bool live = r < rows_total;
     const int32_t j = live ? r / G : 0, h = g * G + (live ? r - j * G : 0);
     const uint4* src = reinterpret_cast<const uint4*>(
-        static_cast<const __nv_bfloat16*>(a.q) + (((int64_t)b * a.D_max + j) * a.Hq + h) * kD);
-    uint4 w[kD / 8];
+                           static_cast<const __nv_bfloat16*>(a.q) +
+                           (((int64_t)b * a.D_max + j) * a.Hq + h) * kD) + half * (kD / 16);
+    uint4 w[kD / 16];
     float m = 0.f;
 #pragma unroll
-    for (int i = 0; i < kD / 8; ++i) {
-      w[i] = live ? src[i] : make_uint4(0, 0, 0, 0);
+    for (int i = 0; i < kD / 16; ++i) w[i] = live ? src[i] : make_uint4(0, 0, 0, 0);
+#pragma unroll
+    for (int i = 0; i < kD / 16; ++i) {
       const uint32_t v[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        m = fmaxf(m, fmaxf(fabsf(__uint_as_float(v[e] << 16)), fabsf(__uint_as_float(v[e] & 0xffff0000u))));
+        m = fmax3(m, fabsf(__uint_as_float(v[e] << 16)), fabsf(__uint_as_float(v[e] & 0xffff0000u)));
     }
-    // 2^(7 - e), e the exponent of the largest entry: in two factors, each in range
-    const int32_t e = min(127, max(-126, (int32_t)(__float_as_uint(m) >> 23) - 127));
-    const int32_t up = 7 - e, u1 = up / 2, u2 = up - u1;
-    const float f1 = __uint_as_float((uint32_t)(u1 + 127) << 23), f2 = __uint_as_float((uint32_t)(u2 + 127) << 23);
-    const float c2 = (a.scale != 0.f ? a.scale : rsqrtf((float)kD)) * kLog2e;
-    rowc = c2 * __uint_as_float((uint32_t)(127 - u1) << 23) * __uint_as_float((uint32_t)(127 - u2) << 23);
+    m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 1));
+    // 2^(7 - e), e the exponent of the largest entry
+    const int32_t e = (int32_t)(__float_as_uint(m) >> 23) - 127, up = max(-120, min(126, 7 - e));
+    const float f = __uint_as_float((uint32_t)(up + 127) << 23);
+    if (half == 0)
+      sh.rowc[q_row] = (a.scale != 0.f ? a.scale : rsqrtf((float)kD)) * kLog2e *
+                       __uint_as_float((uint32_t)(127 - up) << 23);
 #pragma unroll
-    for (int c = 0; c < kD / 16; ++c) {
+    for (int c = 0; c < kD / 32; ++c) {
       uint32_t hi[4], lo[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const uint4& x = w[2 * c + (i >> 1)];
         const uint32_t p0 = (i & 1) ? x.z : x.x, p1 = (i & 1) ? x.w : x.y;
         uint32_t h0, l0, h1, l1;
-        split2(make_float2(__uint_as_float(p0 << 16) * f1 * f2, __uint_as_float(p0 & 0xffff0000u) * f1 * f2), h0, l0);
-        split2(make_float2(__uint_as_float(p1 << 16) * f1 * f2, __uint_as_float(p1 & 0xffff0000u) * f1 * f2), h1, l1);
+        split2(make_float2(__uint_as_float(p0 << 16) * f, __uint_as_float(p0 & 0xffff0000u) * f), h0, l0);
+        split2(make_float2(__uint_as_float(p1 << 16) * f, __uint_as_float(p1 & 0xffff0000u) * f), h1, l1);
         hi[i] = h0 | (h1 << 16);
         lo[i] = l0 | (l1 << 16);
       }
-      const uint32_t off = (uint32_t)tid * 128 + (uint32_t)((c ^ (tid & 7)) << 4);
+      const int ch = half * 4 + c;
+      const uint32_t off = (uint32_t)q_row * 128 + (uint32_t)((ch ^ (q_row & 7)) << 4);
       *reinterpret_cast<uint4*>(sQ + off) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
       *reinterpret_cast<uint4*>(sQ + kQBytes + off) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
     }
@@ -331,6 +342,7 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
 
   if (warp == 4) {
     // ------------------------------------------------------------ producer
+    give_registers();
     const bool leader = elect_one();
     const uint64_t pol = policy_evict_first();
     const int32_t rows = min(S, KT);
@@ -365,11 +377,12 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
     }
     // after a wait that gave up, the copies in flight still land here
     if (!ok) {
-      for (int32_t u = max(0, nk - kNK); u < nk; ++u) mbar_drain(&sh.k_full[u % kNK], (u / kNK) & 1);
-      for (int32_t u = max(0, nv - kNV); u < nv; ++u) mbar_drain(&sh.v_full[u % kNV], (u / kNV) & 1);
+      for (int32_t u = max(0, nk - kNK); u < nk; ++u) drain(&sh.k_full[u % kNK], (u / kNK) & 1);
+      for (int32_t u = max(0, nv - kNV); u < nv; ++u) drain(&sh.v_full[u % kNV], (u / kNV) & 1);
     }
   } else if (warp == 5) {
     // ----------------------------------------------------------- S products
+    give_registers();
     const uint32_t tSu = warp_uniform(tmem), aQ = warp_uniform(smem_u32(sQ));
     const uint32_t aK = warp_uniform(smem_u32(sK));
     const bool leader = elect_one();
@@ -398,9 +411,10 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
       }
       __syncwarp();
     }
-    if (!ok && t > 0) mbar_drain(&sh.s_full[(t - 1) & 1], ((t - 1) >> 1) & 1);
+    if (!ok && t > 0) drain(&sh.s_full[(t - 1) & 1], ((t - 1) >> 1) & 1);
   } else if (warp == 6) {
     // ---------------------------------------------------------- PV products
+    give_registers();
     const uint32_t tSu = warp_uniform(tmem), tOu = warp_uniform(tO);
     const uint32_t aW = warp_uniform(smem_u32(sW));
     const bool leader = elect_one();
@@ -425,9 +439,10 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
       }
       __syncwarp();
     }
-    if (!ok && t > 0) mbar_drain(&sh.pv_done[(t - 1) & 1], ((t - 1) >> 1) & 1);
-  } else if (warp == 7) {
-    // ------------------------------------------------------------- V widened
+    if (!ok && t > 0) drain(&sh.pv_done[(t - 1) & 1], ((t - 1) >> 1) & 1);
+  } else if (warp >= 8) {
+    // ------------------------------------------------- V widened, 16 keys a warp
+    give_registers();
     // A lane takes 16 values (a 16-byte chunk) of a key, eight keys by four chunks a step:
     // then a lane's places in the swizzled tiles are fixed, and eight lanes' stores fill all
     // banks (with eight chunks of a key a step and the halves swapped to avoid conflicts the
@@ -447,8 +462,8 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
       unsigned char* to = sW + sb * kWideBytes;
       const bool whole = c0 >= start && c0 + KT <= k_hi && !any_bad;
       const uint64_t live = whole ? ~0ull : live_keys(c0);
-#pragma unroll 4
-      for (int i = 0; i < KT / 8; ++i) {
+#pragma unroll
+      for (int i = 2 * (warp - 8); i < 2 * (warp - 8) + 2; ++i) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {  // blocks of 64 columns
           uint4 w = *reinterpret_cast<const uint4*>(from + i * 1024 + (h ? src1 : src0));
@@ -469,9 +484,11 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
     }
   } else if (warp < 4) {
     // ------------------------------------------------------------- softmax
+    take_registers();
     const uint32_t lane_off = (uint32_t)(warp * 32) << 16;
     const int32_t r = row0 + tid;
     const bool warp_live = row0 + warp * 32 < rows_total;
+    const float rowc = sh.rowc[tid];
     const int32_t j = r < rows_total ? r / G : 0;
     int32_t qpos = 0x7fffffff;
     if (r < rows_total) qpos = a.draft_pos != nullptr ? sh.kflat[j] : cache + j;
@@ -508,7 +525,8 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
       tc_fence_after();
       if (warp_live) {
         float sv[64];
-        tmem_ld64(tmem + lane_off + sb * KT, sv);
+        tmem_ld32(tmem + lane_off + sb * KT, sv);
+        tmem_ld32(tmem + lane_off + sb * KT + 32, sv + 32);
         if (c0 + KT > mask_from || c0 < start || c0 + KT > k_hi || any_bad) {
           uint64_t keep;
           if (a.draft_pos == nullptr) {
@@ -567,9 +585,9 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
           }
         }
         const float m = m_run == -INFINITY ? 0.f : m_run;
-        uint32_t pk[32];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
+          uint32_t pk[8];
           // P times its V scale over the reference, in the exponent.  A block whose scale is
           // next to nothing beside the reference (and one outside the pool) adds to the sum alone.
           const bool tiny = !(lg[i] - lg_ref > -60.f);
@@ -582,16 +600,17 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
             const float2 p = make_float2(ex2_approx(x.x), ex2_approx(x.y));
             s2[e & 1] = e < 2 ? p : fadd2(s2[e & 1], p);
             const __half2 h = __floats2half2_rn(p.x, p.y);
-            pk[8 * i + e] = *reinterpret_cast<const uint32_t*>(&h);
+            pk[e] = *reinterpret_cast<const uint32_t*>(&h);
           }
           if (tiny) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) pk[8 * i + e] = 0;
+            for (int e = 0; e < 8; ++e) pk[e] = 0;
           }
           const float2 ss = fadd2(s2[0], s2[1]);
           l_run += (ss.x + ss.y) * (tiny ? 1.f : v_ref * iv[i]);
+          tmem_st8(tmem + lane_off + sb * KT + 8 * i, pk);  // (waited for below)
         }
-        tmem_st32(tmem + lane_off + sb * KT, pk);
+        asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
       }
       tc_fence_before();
       __syncwarp();
@@ -639,6 +658,8 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
               l_run > 0.f ? (m_run + log2f(l_run)) * kLn2 : -INFINITY;
       }
     }
+  } else {
+    give_registers();  // (warp 7: the whole group of four gives)
   }
   // ---- teardown
   tc_fence_before();

@@ -7,15 +7,18 @@
 // with float32 accumulation and the scales stay outside: sk multiplies the
 // scores, sv the probabilities before they are rounded to float16.
 //
-// A warp takes 16 query rows (drafts x the query heads that share the KV head)
-// and walks steps of 16 keys.  The order of an mma's inner index and of its
-// columns is free as long as both operands agree, so each lane reads the 16
-// bytes it needs from global memory in one piece: of K, 16 consecutive values
-// of a key for four mma steps; of V, 16 consecutive columns of a key for sixteen
-// output tiles.  The copies go through a ring of shared memory that only the
-// lane itself reads (cp.async; no barrier), four steps deep.
+// The products are turned round, S^T = K Q^T and O^T = V^T P^T: the keys (and then
+// the columns of V) fill the 16 rows of an mma, and the query rows its 8 columns, so
+// the few rows of a token under grouped heads (drafts x the query heads that share
+// the KV head) fill it better.  A warp takes 8 or 16 query rows and walks steps of
+// 16 keys.  The order of an mma's inner index and of its rows is free as long as
+// both operands agree, so each lane reads what it needs from a step in pieces of 16
+// bytes: of K, 16 consecutive values of two keys; of V, 16 consecutive columns of
+// four keys.  A step's K and V come by TMA (swizzled, so those reads meet no bank
+// conflicts) into a ring of the warp's own, four steps deep; a stage is asked for
+// again as soon as it is in registers.  P turns round in registers (movmatrix).
 // The warps of a CTA split 16-key steps among them where the rows are few (and
-// merge at the end), else they take four row tiles of the same keys.
+// merge at the end), else they take other rows of the same keys.
 
 #include <cuda_fp16.h>
 
@@ -30,8 +33,8 @@ namespace {
 constexpr int kWarps = 4;
 constexpr int kStages = 4;          // steps in flight per warp
 constexpr int kStep = 16;           // keys per step
+constexpr int kCtas = 3;            // per SM
 constexpr int kMinTiles = 2;        // a part's fewest tiles (times the warps that share its rows / 4)
-constexpr int kMaxPartTiles = 256;  // 16384 keys: at most 1024 block ids and scales in shared memory
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 // log2 growth of the running maximum (and growth of the V scale) that moves the
@@ -39,23 +42,37 @@ constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kGrowth = 8.f, kVGrowth = 16.f;
 
 struct Plan {
-  int32_t wr, rowgroups, splits, min_tiles;
+  int32_t rows, row_warps, row_groups;  // rows of a warp, its CTA's warps with other rows
+  int32_t per_head, goal, uniform, min_tiles;
+  int32_t group_rows() const { return rows * row_warps; }
+  bool cut(int32_t B) const { return per_head > B; }
 };
 
 Plan make_plan(int32_t B, int32_t Hq, int32_t Hkv, int32_t D_max, int32_t L_max) {
   Plan p;
   const int64_t rows = (int64_t)D_max * (Hq / Hkv);
-  const int64_t row_tiles = (rows + 15) / 16;
-  p.wr = row_tiles >= 3 ? 4 : (int32_t)row_tiles;
-  p.rowgroups = (int32_t)((row_tiles + p.wr - 1) / p.wr);
-  const int64_t base = (int64_t)B * Hkv * p.rowgroups;
-  const int64_t target = 3 * (int64_t)device_sm_count();
-  p.min_tiles = kMinTiles * (kWarps / p.wr);
+  const int64_t sms = device_sm_count();
+  // few rows, or so few CTAs that the longest warp's steps are the time: 8 rows of all
+  // four warps
+  const bool few = (int64_t)B * Hkv * ((rows + 7) / 8) <= sms;
+  p.rows = rows <= 8 || few ? 8 : 16;
+  const int64_t row_tiles = (rows + p.rows - 1) / p.rows;
+  p.row_warps = few ? 1 : row_tiles >= 3 ? 4 : (int32_t)row_tiles;
+  p.row_groups = (int32_t)((row_tiles + p.row_warps - 1) / p.row_warps);
+  p.min_tiles = kMinTiles * (kWarps / p.row_warps);
   const int64_t tiles = (L_max + kCacheTile - 1) / kCacheTile;
+  // CTAs a sequence and head may take; a part has room for so many block ids
   const int64_t most = std::max<int64_t>(1, tiles / p.min_tiles);
-  // (and no part longer than the room for its block ids)
-  const int64_t least = (tiles + kMaxPartTiles - 1) / kMaxPartTiles;
-  p.splits = (int32_t)std::max<int64_t>(least, std::min<int64_t>((target + base - 1) / base, most));
+  const int64_t least = (tiles + kWorkTiles - 1) / kWorkTiles;
+  const int64_t target = kCtas * sms / ((int64_t)Hkv * p.row_groups);
+  if (target <= B || most == 1) {
+    p.goal = p.uniform = (int32_t)least;
+    p.per_head = (int32_t)(B * least);
+  } else {
+    p.uniform = 0;
+    p.goal = (int32_t)std::min(target, B * most);
+    p.per_head = (int32_t)std::max<int64_t>(p.goal, B * least);
+  }
   return p;
 }
 
@@ -84,62 +101,89 @@ __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
   __half2 v = __floats2half2_rn(lo, hi);
   return *reinterpret_cast<uint32_t*>(&v);
 }
-template <int BYTES>
-__device__ __forceinline__ void cp_async(uint32_t dst, const void* src, bool valid) {
-  const uint32_t n = valid ? BYTES : 0;  // the rest is filled with zeros
-  if constexpr (BYTES == 16)
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n)
-                 : "memory");
-  else
-    asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(dst), "l"(src), "n"(BYTES),
-                 "r"(n)
-                 : "memory");
-}
-__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void cp_wait() {
-  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+// 8 x 8 values of 16 bits, lane (r, q) holding (r, 2 q) and (r, 2 q + 1), turned round.
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
+  uint32_t y;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
 }
 
-template <int D>
-__global__ void __launch_bounds__(kWarps * 32, 3)
-cache_attn_kernel(CacheAttnArgs a, CacheAttnLaunch L, int32_t row_warps) {
-  constexpr int NT = D / 8;           // output tiles of 8 columns
-  constexpr int KG = D / 64;          // groups of four mma steps of QK^T
+// NR: groups of 8 query rows of a warp.
+template <int D, int NR>
+__global__ void __launch_bounds__(kWarps * 32, kCtas)
+cache_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
+                  CacheAttnArgs a, CacheAttnLaunch L, int32_t row_warps) {
+  constexpr int RW = 8 * NR;          // rows of a warp
+  constexpr int NT = D / 16;          // output tiles of 16 columns
+  constexpr int KG = D / 64;          // groups of four mma steps of K Q^T
   constexpr int VB = D / 8;           // bytes of V a lane takes per key
   constexpr int kStageBytes = 2 * kStep * D;
   constexpr int kWarpBytes = kStages * kStageBytes;
-  static_assert(kWarpBytes >= 16 * D * 4 + 16 * 8, "a warp's partial rows fit its ring");
-  extern __shared__ __align__(16) unsigned char smem[];
+  constexpr int kRowFloats = D + 4;   // of the partial rows, which take the ring's place
+  static_assert(kWarpBytes >= RW * kRowFloats * 4, "a warp's partial rows fit its ring");
+  extern __shared__ __align__(1024) unsigned char smem_raw[];
+  unsigned char* smem = reinterpret_cast<unsigned char*>(
+      (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   int32_t* s_id = reinterpret_cast<int32_t*>(smem + kWarps * kWarpBytes);
   float* s_ks = reinterpret_cast<float*>(s_id + L.max_blocks);
   float* s_vs = s_ks + L.max_blocks;
+  __shared__ uint64_t s_full[kWarps][kStages];
+  __shared__ float2 s_ml[kWarps][RW];
+  if (threadIdx.x < 2) prefetch_tensormap(threadIdx.x == 0 ? &tmK : &tmV);
   pdl_wait();
 
-  const int32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int32_t split = blockIdx.x, b = blockIdx.y / a.cache.Hkv, g = blockIdx.y % a.cache.Hkv;
-  const int32_t S = a.cache.block, S_log = 31 - __clz(S), G = a.Hq / a.cache.Hkv;
+  const int32_t tid = threadIdx.x, lane = tid & 31, warp = (int32_t)warp_uniform(tid >> 5);
+  const int32_t g = blockIdx.y, S = a.cache.block, S_log = 31 - __clz(S), G = a.Hq / a.cache.Hkv;
+  const bool first_of = g == 0 && blockIdx.z == 0;
+  const CacheWork work = cache_work(a, L, blockIdx.x, first_of && tid < 32);
+  if (work.b < 0) return;
+  const int32_t b = work.b, split = work.split, parts = work.parts;
   const int32_t cache = a.cache_len[b], nd = a.n_drafts[b];
-  if (!cache_lengths_ok(a, cache, nd)) {
-    if (tid == 0 && split == 0 && g == 0 && blockIdx.z == 0)
-      record_status(a.status, SSD_ERR_DEVICE_BOUNDS);
-    return;
-  }
+  if (!cache_lengths_ok(a, cache, nd)) return;
   const int32_t Lk = cache + nd, rows_total = nd * G;
   const int32_t tiles = (Lk + kCacheTile - 1) / kCacheTile;
-  const int32_t parts = cache_parts(L.splits, L.min_tiles, tiles);
-  const int32_t row_g0 = blockIdx.z * row_warps * 16;
-  if (row_g0 >= rows_total || split >= parts) return;
+  const int32_t row_g0 = blockIdx.z * row_warps * RW;
+  if (row_g0 >= rows_total) return;
   const int32_t t_lo = (int32_t)((int64_t)tiles * split / parts);
   const int32_t t_hi = (int32_t)((int64_t)tiles * (split + 1) / parts);
   const int32_t k_lo = t_lo * kCacheTile, k_hi = min(Lk, t_hi * kCacheTile);
   const int32_t start = a.key_start != nullptr ? min(Lk, max(0, a.key_start[b])) : 0;
 
+  // ---- this warp's rows and its share of the steps, and the copies of the first ones
+  const int32_t wk_n = kWarps / row_warps, wr = warp % row_warps, wk = warp / row_warps;
+  const int32_t q = lane & 3, r8 = lane >> 2;
+  const int32_t row0 = row_g0 + wr * RW;
+  const int32_t first = max(k_lo, start & ~(kStep - 1));  // multiple of 16
+  unsigned char* ring = smem + warp * kWarpBytes;
+  const int32_t n_steps =
+      row0 >= rows_total || first >= k_hi ? 0 : (k_hi - first + kStep - 1) / kStep;
+  const int32_t steps = n_steps > wk ? (n_steps - wk + wk_n - 1) / wk_n : 0;
+  auto key_of = [&](int32_t t) { return first + (t * wk_n + wk) * kStep; };
+  auto issue = [&](int32_t t, int32_t id) {  // by one lane
+    const int32_t k0 = key_of(t), z = max(id, 0) * a.cache.Hkv + g;
+    unsigned char* dst = ring + (t % kStages) * kStageBytes;
+    uint64_t* bar = &s_full[warp][t % kStages];
+    const uint64_t once = policy_evict_first();
+    mbar_arrive_expect_tx(bar, kStageBytes);
+    tma_load_3d(dst, &tmK, 0, k0 & (S - 1), z, bar, once);
+    tma_load_3d(dst + kStep * D, &tmV, 0, k0 & (S - 1), z, bar, once);
+  };
+  const int32_t* table = a.block_table + (int64_t)b * a.max_blocks;
+  if (lane == 0) {
+    for (int t = 0; t < kStages; ++t) mbar_init(&s_full[warp][t], 1);
+    fence_barrier_init();
+    for (int t = 0; t < kStages && t < steps; ++t) {
+      const int32_t id = table[key_of(t) >> S_log];
+      issue(t, id < a.cache.num_blocks ? id : -1);
+    }
+  }
+  __syncwarp();
+
   // ---- the part's block ids and scales
   const int32_t b_lo = k_lo >> S_log;  // (a part may start inside a block of 128)
   const int32_t nb = ((k_hi - 1) >> S_log) + 1 - b_lo;
   for (int32_t i = tid; i < nb; i += blockDim.x) {
-    int32_t id = a.block_table[(int64_t)b * a.max_blocks + b_lo + i];
+    int32_t id = table[b_lo + i];
     if (id < 0 || id >= a.cache.num_blocks) {
       record_status(a.status, SSD_ERR_DEVICE_BOUNDS);
       id = -1;
@@ -150,44 +194,31 @@ cache_attn_kernel(CacheAttnArgs a, CacheAttnLaunch L, int32_t row_warps) {
     s_vs[i] = id < 0 ? 0.f : a.cache.v_scale[at];
   }
 
-  // ---- this warp's rows and its share of the steps
-  const int32_t wk_n = kWarps / row_warps, wr = warp % row_warps, wk = warp / row_warps;
-  const int32_t q = lane & 3, r8 = lane >> 2;
-  const int32_t row0 = row_g0 + wr * 16;
-  int32_t qpos[2];
-  int32_t minq = 0x7fffffff;
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int32_t r = row0 + r8 + 8 * i;
-    qpos[i] = -1;
-    if (r < rows_total) {
-      qpos[i] = cache_flat_pos(a, b, cache, r / G);
-      if (qpos[i] < 0 && split == 0 && g == 0) record_status(a.status, SSD_ERR_DEVICE_BOUNDS);
-      minq = min(minq, qpos[i]);
-    }
-  }
-  minq = __reduce_min_sync(0xffffffffu, minq);
-  // keys below this one are visible to every row of the warp
-  const int32_t mask_from = min(cache, minq + 1);
-
-  // Q as float16 with its row's power of two taken out; column order of K's reads
-  uint32_t qf[KG][4][4];
-  float rowc[2];
+  // Q as float16 with its row's power of two taken out; column order of K's reads.  A
+  // lane holds row 8 n + r8.
+  uint32_t qf[NR][KG][4][2];
+  float rowc_of[NR];
+  int32_t qpos_of[NR];
   const float c2 = (a.scale != 0.f ? a.scale : rsqrtf((float)D)) * kLog2e;
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int32_t r = row0 + r8 + 8 * i;
+  for (int n = 0; n < NR; ++n) {
+    const int32_t r = row0 + r8 + 8 * n;
     const bool live = r < rows_total;
     const int32_t j = live ? r / G : 0, h = g * G + (live ? r - j * G : 0);
     const uint4* src = reinterpret_cast<const uint4*>(
         static_cast<const __nv_bfloat16*>(a.q) + (((int64_t)b * a.D_max + j) * a.Hq + h) * D);
+    qpos_of[n] = 0x7fffffff;
+    if (live) {
+      qpos_of[n] = cache_flat_pos(a, b, cache, j);
+      if (qpos_of[n] < 0 && split == 0 && g == 0) record_status(a.status, SSD_ERR_DEVICE_BOUNDS);
+    }
     float x[KG][16];
     float m = 0.f;
 #pragma unroll
     for (int kg = 0; kg < KG; ++kg)
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        const uint4 w = live ? src[kg * 8 + q * 2 + u] : make_uint4(0, 0, 0, 0);
+        const uint4 w = live ? src[(q * KG + kg) * 2 + u] : make_uint4(0, 0, 0, 0);
         const uint32_t v[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -201,259 +232,269 @@ cache_attn_kernel(CacheAttnArgs a, CacheAttnLaunch L, int32_t row_warps) {
     // 2^e with m / 2^e in [1, 2) (or less, for the smallest; 4, for the largest)
     const int32_t e = min(126, max(-126, (int32_t)(__float_as_uint(m) >> 23) - 127));
     const float down = __uint_as_float((uint32_t)(127 - e) << 23);
-    rowc[i] = c2 * __uint_as_float((uint32_t)(127 + e) << 23);
+    rowc_of[n] = c2 * __uint_as_float((uint32_t)(127 + e) << 23);
 #pragma unroll
     for (int kg = 0; kg < KG; ++kg)
 #pragma unroll
       for (int s = 0; s < 4; ++s) {
-        qf[kg][s][i] = pack_f16x2(x[kg][4 * s] * down, x[kg][4 * s + 1] * down);
-        qf[kg][s][2 + i] = pack_f16x2(x[kg][4 * s + 2] * down, x[kg][4 * s + 3] * down);
+        qf[n][kg][s][0] = pack_f16x2(x[kg][4 * s] * down, x[kg][4 * s + 1] * down);
+        qf[n][kg][s][1] = pack_f16x2(x[kg][4 * s + 2] * down, x[kg][4 * s + 3] * down);
       }
   }
+  // keys below this one are visible to every row of the warp
+  int32_t mask_from;
+  {
+    int32_t minq = qpos_of[0];
+    if (NR == 2) minq = min(minq, qpos_of[NR - 1]);
+    mask_from = min(cache, min(0x7ffffffe, __reduce_min_sync(0xffffffffu, minq)) + 1);
+  }
+  // From here on a lane's rows are 8 n + 2 q + u: those of its scores and of O.
+  float rowc[NR][2];
+  int32_t qpos[NR][2];
+#pragma unroll
+  for (int n = 0; n < NR; ++n)
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      rowc[n][u] = __shfl_sync(0xffffffffu, rowc_of[n], (2 * q + u) * 4);
+      qpos[n][u] = __shfl_sync(0xffffffffu, qpos_of[n], (2 * q + u) * 4);
+    }
   __syncthreads();  // ids and scales
 
-  const int32_t first = max(k_lo, start & ~(kStep - 1));  // multiple of 16
-  const uint32_t ring = smem_u32(smem) + warp * kWarpBytes;
-  const uint8_t* kbase = static_cast<const uint8_t*>(a.cache.k);
-  const uint8_t* vbase = static_cast<const uint8_t*>(a.cache.v);
-  auto key_of = [&](int32_t t) { return first + (t * wk_n + wk) * kStep; };
-  auto issue = [&](int32_t t) {
-    const int32_t k0 = key_of(t);
-    if (k0 < k_hi && row0 < rows_total) {
-      const int32_t i = (k0 >> S_log) - b_lo, id = s_id[i];
-      const int64_t at =
-          (((int64_t)max(id, 0) * a.cache.Hkv + g) * S + (k0 & (S - 1))) * D;
-      const uint32_t dst = ring + (t % kStages) * kStageBytes;
-      auto valid = [&](int32_t k) { return id >= 0 && k0 + k >= start && k0 + k < k_hi; };
+  // offsets of the lane's pieces in a stage (the swizzle: of 16-byte pieces, by the row)
+  uint32_t k_off[KG], v_off[2];
 #pragma unroll
-      for (int n = 0; n < 2; ++n)
+  for (int kg = 0; kg < KG; ++kg) {
+    const int32_t sw = D == 128 ? r8 : (r8 >> 1) & 3;
+    k_off[kg] = r8 * D + (((q * KG + kg) ^ sw) << 4);
+  }
 #pragma unroll
-        for (int kg = 0; kg < KG; ++kg) {
-          const int32_t k = n * 8 + r8;
-          cp_async<16>(dst + (n * KG + kg) * 512 + lane * 16, kbase + at + k * D + kg * 64 + q * 16,
-                       valid(k));
-        }
+  for (int u = 0; u < 2; ++u) {
+    const int32_t key = 2 * q + u;
+    v_off[u] = kStep * D + key * D + (D == 128 ? (r8 ^ key) << 4 : (((r8 >> 1) ^ q) << 4) + (r8 & 1) * 8);
+  }
+
+  float o[NR][NT][4];
+  float m_ref[NR][2], l[NR][2];
 #pragma unroll
-      for (int n = 0; n < 4; ++n) {
-        const int32_t k = (n >> 1) * 8 + 2 * q + (n & 1);
-        cp_async<VB>(dst + kStep * D + n * 32 * VB + lane * VB, vbase + at + k * D + r8 * VB,
-                     valid(k));
+  for (int n = 0; n < NR; ++n) {
+#pragma unroll
+    for (int t = 0; t < NT; ++t) o[n][t][0] = o[n][t][1] = o[n][t][2] = o[n][t][3] = 0.f;
+    m_ref[n][0] = m_ref[n][1] = -INFINITY;
+    l[n][0] = l[n][1] = 0.f;
+  }
+  float v_ref = 0.f, v_inv = 0.f;
+  bool ok = true;
+  int32_t t = 0;
+#pragma unroll 1
+  for (; t < steps; ++t) {
+    ok = mbar_wait_warp(&s_full[warp][t % kStages], (t / kStages) & 1, a.status);
+    if (!ok) break;
+    const unsigned char* st = ring + (t % kStages) * kStageBytes;
+    uint4 kw[2][KG];
+    uint32_t v[4][VB / 4];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int kg = 0; kg < KG; ++kg)
+        kw[h][kg] = *reinterpret_cast<const uint4*>(st + k_off[kg] + h * 8 * D);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const unsigned char* at = st + v_off[i & 1] + (i >> 1) * 8 * D;
+      if constexpr (VB == 16) {
+        const uint4 w = *reinterpret_cast<const uint4*>(at);
+        v[i][0] = w.x;
+        v[i][1] = w.y;
+        v[i][2] = w.z;
+        v[i][3] = w.w;
+      } else {
+        const uint2 w = *reinterpret_cast<const uint2*>(at);
+        v[i][0] = w.x;
+        v[i][1] = w.y;
       }
     }
-    cp_commit();
-  };
-#pragma unroll
-  for (int t = 0; t < kStages - 1; ++t) issue(t);
+    const int32_t k0 = key_of(t), bi = (k0 >> S_log) - b_lo;
+    const float ks = s_ks[bi], vs = s_vs[bi];
+    __syncwarp();
+    if (lane == 0 && t + kStages < steps)
+      issue(t + kStages, s_id[(key_of(t + kStages) >> S_log) - b_lo]);
 
-  float o[NT][4];
+    // ---- S^T = K Q^T
+    float x[NR][4];  // keys r8 and r8 + 8 (by 2) of the lane's rows
+    {
+      float sc[KG][NR][4];
 #pragma unroll
-  for (int n = 0; n < NT; ++n) o[n][0] = o[n][1] = o[n][2] = o[n][3] = 0.f;
-  float m_ref[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
-  float v_ref = 0.f, v_inv = 0.f;
-
-  if (row0 < rows_total) {
-#pragma unroll 1
-    for (int32_t t = 0; key_of(t) < k_hi; ++t) {
-      cp_wait<kStages - 2>();
-      issue(t + kStages - 1);
-      const int32_t k0 = key_of(t), bi = (k0 >> S_log) - b_lo;
-      const unsigned char* st = smem + warp * kWarpBytes + (t % kStages) * kStageBytes;
-      // ---- S = Q K^T
-      float sc[2][4];
+      for (int kg = 0; kg < KG; ++kg) {
 #pragma unroll
-      for (int n = 0; n < 2; ++n) {
-        sc[n][0] = sc[n][1] = sc[n][2] = sc[n][3] = 0.f;
+        for (int n = 0; n < NR; ++n) sc[kg][n][0] = sc[kg][n][1] = sc[kg][n][2] = sc[kg][n][3] = 0.f;
 #pragma unroll
-        for (int kg = 0; kg < KG; ++kg) {
-          const uint4 w = *reinterpret_cast<const uint4*>(st + (n * KG + kg) * 512 + lane * 16);
-          mma_f16(sc[n], qf[kg][0], f16_lo(w.x), f16_hi(w.x));
-          mma_f16(sc[n], qf[kg][1], f16_lo(w.y), f16_hi(w.y));
-          mma_f16(sc[n], qf[kg][2], f16_lo(w.z), f16_hi(w.z));
-          mma_f16(sc[n], qf[kg][3], f16_lo(w.w), f16_hi(w.w));
+        for (int s = 0; s < 4; ++s) {
+          const uint32_t w0 = s == 0 ? kw[0][kg].x : s == 1 ? kw[0][kg].y : s == 2 ? kw[0][kg].z : kw[0][kg].w;
+          const uint32_t w1 = s == 0 ? kw[1][kg].x : s == 1 ? kw[1][kg].y : s == 2 ? kw[1][kg].z : kw[1][kg].w;
+          const uint32_t kf[4] = {f16_lo(w0), f16_lo(w1), f16_hi(w0), f16_hi(w1)};
+#pragma unroll
+          for (int n = 0; n < NR; ++n) mma_f16(sc[kg][n], kf, qf[n][kg][s][0], qf[n][kg][s][1]);
         }
       }
-      const float ks = s_ks[bi], vs = s_vs[bi];
 #pragma unroll
-      for (int n = 0; n < 2; ++n)
+      for (int n = 0; n < NR; ++n)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) sc[n][e] *= rowc[e >> 1] * ks;
-      if (k0 < start || k0 + kStep > min(mask_from, k_hi) || s_id[bi] < 0) {
+        for (int e = 0; e < 4; ++e)
+          x[n][e] = (KG == 2 ? sc[0][n][e] + sc[KG - 1][n][e] : sc[0][n][e]) * (rowc[n][e & 1] * ks);
+    }
+    if (k0 < start || k0 + kStep > min(mask_from, k_hi) || s_id[bi] < 0) {
+      const bool in_pool = s_id[bi] >= 0;
 #pragma unroll
-        for (int n = 0; n < 2; ++n)
-#pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            const int32_t key = k0 + n * 8 + 2 * q + u;
-            int32_t kp = 0x7fffffff;
-            if (key >= start && key < k_hi && s_id[bi] >= 0) {
-              kp = key;
-              if (key >= cache) {
-                kp = cache_flat_pos(a, b, cache, key - cache);
-                if (kp < 0) kp = 0x7fffffff;
-              }
-            }
-            if (kp > qpos[0]) sc[n][u] = -INFINITY;
-            if (kp > qpos[1]) sc[n][2 + u] = -INFINITY;
+      for (int h = 0; h < 2; ++h) {
+        const int32_t key = k0 + r8 + 8 * h;
+        int32_t kp = 0x7fffffff;
+        if (key >= start && key < k_hi && in_pool) {
+          kp = key;
+          if (key >= cache) {
+            kp = cache_flat_pos(a, b, cache, key - cache);
+            if (kp < 0) kp = 0x7fffffff;
           }
-      }
-      // ---- softmax against a reference maximum that moves when it falls behind
-      float mx[2];
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        mx[i] = fmaxf(fmaxf(sc[0][2 * i], sc[0][2 * i + 1]), fmaxf(sc[1][2 * i], sc[1][2 * i + 1]));
-        mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], 1));
-        mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], 2));
-      }
-      const bool behind = mx[0] > m_ref[0] + kGrowth || mx[1] > m_ref[1] + kGrowth;
-      const bool v_behind = !(vs <= v_ref * kVGrowth);  // the same in every lane
-      if (__any_sync(0xffffffffu, behind) || v_behind) {
-        float f = 1.f;
-        if (v_behind) {
-          const float to = fmaxf(vs, 0x1p-120f);
-          f = v_ref / to;
-          v_ref = to;
-          v_inv = 1.f / to;
         }
+#pragma unroll
+        for (int n = 0; n < NR; ++n)
+#pragma unroll
+          for (int u = 0; u < 2; ++u)
+            if (kp > qpos[n][u] || kp == 0x7fffffff) x[n][2 * h + u] = -INFINITY;
+      }
+      // what lies in no key's place may be anything
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int32_t key = k0 + 2 * q + (i & 1) + 8 * (i >> 1);
+        if (!(key >= start && key < k_hi && in_pool)) {
+#pragma unroll
+          for (int w = 0; w < VB / 4; ++w) v[i][w] = 0;
+        }
+      }
+    }
+    // ---- softmax against a reference maximum that moves when it falls behind
+    bool behind = !(vs <= v_ref * kVGrowth);  // the same in every lane
+#pragma unroll
+    for (int n = 0; n < NR; ++n)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) behind |= fmaxf(x[n][u], x[n][2 + u]) > m_ref[n][u] + kGrowth;
+    if (__any_sync(0xffffffffu, behind)) {
+      float f = 1.f;
+      if (!(vs <= v_ref * kVGrowth)) {
+        const float to = fmaxf(vs, 0x1p-120f);
+        f = v_ref / to;
+        v_ref = to;
+        v_inv = 1.f / to;
+      }
+#pragma unroll
+      for (int n = 0; n < NR; ++n) {
         float al[2];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const float m = fmaxf(m_ref[i], mx[i]);
-          al[i] = m == -INFINITY ? 1.f : exp2f(m_ref[i] - m);
-          m_ref[i] = m;
-          l[i] *= al[i];
-          al[i] *= f;
+        for (int u = 0; u < 2; ++u) {
+          float m = fmaxf(x[n][u], x[n][2 + u]);
+#pragma unroll
+          for (int s = 4; s < 32; s <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, s));
+          m = fmaxf(m_ref[n][u], m);
+          al[u] = m == -INFINITY ? 1.f : exp2f(m_ref[n][u] - m);
+          m_ref[n][u] = m;
+          l[n][u] *= al[u];
+          al[u] *= f;
         }
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          o[n][0] *= al[0];
-          o[n][1] *= al[0];
-          o[n][2] *= al[1];
-          o[n][3] *= al[1];
-        }
-      }
-      const float ratio = vs * v_inv;
-      uint32_t pf[4];
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const float m = m_ref[i] == -INFINITY ? 0.f : m_ref[i];
-#pragma unroll
-        for (int n = 0; n < 2; ++n) {
-          const float p0 = ex2_approx(sc[n][2 * i] - m), p1 = ex2_approx(sc[n][2 * i + 1] - m);
-          l[i] += p0 + p1;
-          pf[2 * n + i] = pack_f16x2(p0 * ratio, p1 * ratio);
+        for (int c = 0; c < NT; ++c) {
+          o[n][c][0] *= al[0];
+          o[n][c][1] *= al[1];
+          o[n][c][2] *= al[0];
+          o[n][c][3] *= al[1];
         }
       }
-      // ---- O += P V: output tile nt holds column n * VB + nt as its n-th
-      uint32_t v[4][VB / 4];
-#pragma unroll
-      for (int n = 0; n < 4; ++n) {
-        const unsigned char* at = st + kStep * D + n * 32 * VB + lane * VB;
-        if constexpr (VB == 16) {
-          const uint4 w = *reinterpret_cast<const uint4*>(at);
-          v[n][0] = w.x;
-          v[n][1] = w.y;
-          v[n][2] = w.z;
-          v[n][3] = w.w;
-        } else {
-          const uint2 w = *reinterpret_cast<const uint2*>(at);
-          v[n][0] = w.x;
-          v[n][1] = w.y;
-        }
-      }
-#pragma unroll
-      for (int w = 0; w < VB / 4; ++w)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const uint32_t sel = h == 0 ? 0x5140u : 0x7362u;
-          const uint32_t x0 = __byte_perm(v[0][w], v[1][w], sel);
-          const uint32_t x1 = __byte_perm(v[2][w], v[3][w], sel);
-          mma_f16(o[4 * w + 2 * h], pf, f16_lo(x0), f16_lo(x1));
-          mma_f16(o[4 * w + 2 * h + 1], pf, f16_hi(x0), f16_hi(x1));
-        }
     }
-  }
-  cp_wait<0>();
-
+    const float ratio = vs * v_inv;
+    uint32_t pf[NR][2];
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
-    l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
-  }
-
-  // ---- merge the warps that shared the rows
-  // a lane's columns of a row: q * 2 * VB + (0 .. VB - 1), then VB more
-  if (wk_n > 1) {
-    __syncwarp();
-    unsigned char* mine = smem + warp * kWarpBytes;
-    float2* ml = reinterpret_cast<float2*>(mine + 16 * D * 4);
+    for (int n = 0; n < NR; ++n) {
+      const float m0 = m_ref[n][0] == -INFINITY ? 0.f : m_ref[n][0];
+      const float m1 = m_ref[n][1] == -INFINITY ? 0.f : m_ref[n][1];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      float* po = reinterpret_cast<float*>(mine) + (r8 + 8 * i) * D;
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int n = 0; n < NT; ++n) po[q * 2 * VB + u * VB + n] = o[n][2 * i + u] * v_ref;
-      if (q == 0) ml[r8 + 8 * i] = make_float2(m_ref[i], l[i]);
-    }
-    __syncthreads();
-    if (wk != 0) return;
-    v_ref = 1.f;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int32_t r = r8 + 8 * i;
-      float M = -INFINITY;
-      for (int w = 0; w < wk_n; ++w)
-        M = fmaxf(M, reinterpret_cast<const float2*>(smem + (wr + w * row_warps) * kWarpBytes +
-                                                     16 * D * 4)[r].x);
-      float sum = 0.f;
-#pragma unroll
-      for (int n = 0; n < NT; ++n) o[n][2 * i] = o[n][2 * i + 1] = 0.f;
-      for (int w = 0; w < wk_n; ++w) {
-        const unsigned char* at = smem + (wr + w * row_warps) * kWarpBytes;
-        const float2 x = reinterpret_cast<const float2*>(at + 16 * D * 4)[r];
-        const float f = x.x == -INFINITY ? 0.f : exp2f(x.x - M);
-        sum += x.y * f;
-        const float* po = reinterpret_cast<const float*>(at) + r * D + q * 2 * VB;
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          o[n][2 * i] += po[n] * f;
-          o[n][2 * i + 1] += po[VB + n] * f;
-        }
+      for (int h = 0; h < 2; ++h) {
+        const float p0 = ex2_approx(x[n][2 * h] - m0), p1 = ex2_approx(x[n][2 * h + 1] - m1);
+        l[n][0] += p0;
+        l[n][1] += p1;
+        pf[n][h] = transpose8x8(pack_f16x2(p0 * ratio, p1 * ratio));
       }
-      m_ref[i] = M;
-      l[i] = sum;
     }
+    // ---- O^T += V^T P^T: output tile c holds columns r8 * VB + 2 c and the next
+#pragma unroll
+    for (int w = 0; w < VB / 4; ++w)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint32_t sel = h == 0 ? 0x5140u : 0x7362u;
+        const uint32_t x0 = __byte_perm(v[0][w], v[1][w], sel);
+        const uint32_t x1 = __byte_perm(v[2][w], v[3][w], sel);
+        const uint32_t vf[4] = {f16_lo(x0), f16_hi(x0), f16_lo(x1), f16_hi(x1)};
+#pragma unroll
+        for (int n = 0; n < NR; ++n) mma_f16(o[n][2 * w + h], vf, pf[n][0], pf[n][1]);
+      }
   }
+  if (!ok)  // the copies still in flight land before the CTA is let go
+    for (; t < steps; ++t) mbar_drain(&s_full[warp][t % kStages], (t / kStages) & 1);
+  __syncwarp();
 
-  // ---- the rows, or the part's share of them
+  // ---- every warp's rows to its ring's place, then the rows (or the part's share of
+  // them), each by a warp that merges what the warps of its rows hold
+  {
+    float* mine = reinterpret_cast<float*>(ring);
+#pragma unroll
+    for (int n = 0; n < NR; ++n)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int32_t r = 8 * n + 2 * q + u;
+#pragma unroll
+        for (int s = 4; s < 32; s <<= 1) l[n][u] += __shfl_xor_sync(0xffffffffu, l[n][u], s);
+#pragma unroll
+        for (int c = 0; c < NT; c += 2)
+          *reinterpret_cast<float4*>(mine + r * kRowFloats + r8 * VB + 2 * c) =
+              make_float4(o[n][c][u] * v_ref, o[n][c][2 + u] * v_ref, o[n][c + 1][u] * v_ref,
+                          o[n][c + 1][2 + u] * v_ref);
+        if (r8 == 0) s_ml[warp][r] = make_float2(m_ref[n][u], l[n][u]);
+      }
+  }
+  if (__syncthreads_or(!ok)) return;
+  constexpr int PER = D / 32;
   const bool direct = parts == 1;
+  for (int32_t rr = warp; rr < row_warps * RW && row_g0 + rr < rows_total; rr += kWarps) {
+    const int32_t w0 = rr / RW, r = rr - w0 * RW;
+    float M = -INFINITY;
+    for (int32_t w = w0; w < kWarps; w += row_warps) M = fmaxf(M, s_ml[w][r].x);
+    float sum = 0.f, acc[PER];
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int32_t r = row0 + r8 + 8 * i;
-    if (r >= rows_total) continue;
-    const int32_t j = r / G, h = g * G + (r - j * G);
+    for (int k = 0; k < PER; ++k) acc[k] = 0.f;
+    for (int32_t w = w0; w < kWarps; w += row_warps) {
+      const float2 ml = s_ml[w][r];
+      const float f = ml.x == -INFINITY ? 0.f : exp2f(ml.x - M);
+      sum += ml.y * f;
+      const float* po =
+          reinterpret_cast<const float*>(smem + w * kWarpBytes) + r * kRowFloats + lane * PER;
+#pragma unroll
+      for (int k = 0; k < PER; ++k) acc[k] += po[k] * f;
+    }
+    const int32_t row = row_g0 + rr, j = row / G, h = g * G + (row - j * G);
     if (direct) {
       const int64_t at = ((int64_t)b * a.D_max + j) * a.Hq + h;
       if (!dbg_in(at, (int64_t)a.B * a.D_max * a.Hq, a.status)) continue;
-      const float f = l[i] > 0.f ? v_ref / l[i] : 0.f;
-      uint32_t* ob = reinterpret_cast<uint32_t*>(static_cast<__nv_bfloat16*>(a.o) + at * D + q * 2 * VB);
+      const float inv = sum > 0.f ? 1.f / sum : 0.f;
+      uint32_t* ob = reinterpret_cast<uint32_t*>(static_cast<__nv_bfloat16*>(a.o) + at * D + lane * PER);
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int n = 0; n < NT; n += 2)
-          ob[(u * VB + n) / 2] = pack_bf16x2(o[n][2 * i + u] * f, o[n + 1][2 * i + u] * f);
-      if (a.lse != nullptr && q == 0)
+      for (int k = 0; k < PER; k += 2) ob[k / 2] = pack_bf16x2(acc[k] * inv, acc[k + 1] * inv);
+      if (a.lse != nullptr && lane == 0)
         a.lse[((int64_t)b * a.Hq + h) * a.D_max + j] =
-            l[i] > 0.f ? (m_ref[i] + log2f(l[i])) * kLn2 : -INFINITY;
+            sum > 0.f ? (M + log2f(sum)) * kLn2 : -INFINITY;
     } else {
-      const int64_t at = (((int64_t)b * a.D_max + j) * a.Hq + h) * L.splits + split;
-      if (!dbg_in(at, (int64_t)a.B * a.D_max * a.Hq * L.splits, a.status)) continue;
-      float2* po = reinterpret_cast<float2*>(L.part_o + at * D + q * 2 * VB);
+      const int64_t at =
+          (((int64_t)g * L.row_groups + blockIdx.z) * L.per_head + blockIdx.x) * L.group_rows + rr;
+      if (!dbg_in(at, (int64_t)a.cache.Hkv * L.row_groups * L.per_head * L.group_rows, a.status)) continue;
+      float* po = L.part_o + at * D + lane * PER;
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int n = 0; n < NT; n += 2)
-          po[(u * VB + n) / 2] = make_float2(o[n][2 * i + u] * v_ref, o[n + 1][2 * i + u] * v_ref);
-      if (q == 0) L.part_ml[at] = make_float2(m_ref[i], l[i]);
+      for (int k = 0; k < PER; ++k) po[k] = acc[k];
+      if (lane == 0) L.part_ml[at] = make_float2(M, sum);
     }
   }
 }
@@ -471,27 +512,49 @@ __global__ void __launch_bounds__(256) cache_attn_combine_kernel(CacheAttnArgs a
   const int32_t b = (int32_t)(bj / a.D_max), j = (int32_t)(bj - (int64_t)b * a.D_max);
   const int32_t cache = a.cache_len[b], nd = a.n_drafts[b];
   if (!cache_lengths_ok(a, cache, nd) || j >= nd) return;
-  const int32_t parts =
-      cache_parts(L.splits, L.min_tiles, (cache + nd + kCacheTile - 1) / kCacheTile);
-  if (parts == 1) return;  // written by the attention kernel
-  const int64_t at = row * L.splits;
-  if (!dbg_in(at + parts - 1, (int64_t)a.B * a.D_max * a.Hq * L.splits, a.status)) return;
+  int32_t parts;
+  int64_t at, step = 1, room;
+  if (L.info != nullptr) {
+    const int2 x = L.info[b];
+    const int32_t G = a.Hq / a.cache.Hkv, g = h / G, r = j * G + (h - g * G);
+    const int32_t z = r / L.group_rows;
+    parts = x.y;
+    step = L.group_rows;
+    at = (((int64_t)g * L.row_groups + z) * L.per_head + x.x) * step + (r - z * L.group_rows);
+    room = (int64_t)a.cache.Hkv * L.row_groups * L.per_head * step;
+  } else {
+    parts = cache_parts(L.splits, L.min_tiles, (cache + nd + kCacheTile - 1) / kCacheTile);
+    at = row * L.splits;
+    room = (int64_t)a.B * a.D_max * a.Hq * L.splits;
+  }
+  if (parts <= 1) return;  // written by the attention kernel
+  if (!dbg_in(at + (parts - 1) * step, room, a.status)) return;
   float M = -INFINITY;
-  for (int32_t s = lane; s < parts; s += 32) M = fmaxf(M, L.part_ml[at + s].x);
+  for (int32_t s = lane; s < parts; s += 32) M = fmaxf(M, L.part_ml[at + s * step].x);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
   constexpr int PER = D / 32;
   float acc[PER], sum = 0.f;
 #pragma unroll
   for (int k = 0; k < PER; ++k) acc[k] = 0.f;
-  for (int32_t s = 0; s < parts; ++s) {
-    const float2 x = L.part_ml[at + s];
-    const float f = x.x == -INFINITY ? 0.f : exp2f(x.x - M);
-    sum += x.y * f;
-    const float* po = L.part_o + (at + s) * D + lane * PER;
+  for (int32_t s0 = 0; s0 < parts; s0 += 32) {
+    float mine = 0.f;  // the factor of part s0 + lane
+    if (s0 + lane < parts) {
+      const float2 x = L.part_ml[at + (s0 + lane) * step];
+      mine = x.x == -INFINITY ? 0.f : exp2f(x.x - M);
+      sum += x.y * mine;
+    }
+    const int32_t n = min(32, parts - s0);
+#pragma unroll 4
+    for (int32_t s = 0; s < n; ++s) {
+      const float f = __shfl_sync(0xffffffffu, mine, s);
+      const float* po = L.part_o + (at + (s0 + s) * step) * D + lane * PER;
 #pragma unroll
-    for (int k = 0; k < PER; ++k) acc[k] += po[k] * f;
+      for (int k = 0; k < PER; ++k) acc[k] += po[k] * f;
+    }
   }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
   const float inv = sum > 0.f ? 1.f / sum : 0.f;
   __nv_bfloat16* ob = static_cast<__nv_bfloat16*>(a.o) + row * D + lane * PER;
 #pragma unroll
@@ -501,21 +564,43 @@ __global__ void __launch_bounds__(256) cache_attn_combine_kernel(CacheAttnArgs a
     a.lse[((int64_t)b * a.Hq + h) * a.D_max + j] = sum > 0.f ? (M + log2f(sum)) * kLn2 : -INFINITY;
 }
 
-template <int D>
-cudaError_t launch_mma(const CacheAttnArgs& a, const Plan& p, const CacheAttnLaunch& L,
-                       cudaStream_t stream) {
-  const size_t smem = (size_t)kWarps * kStages * 2 * kStep * D + (size_t)L.max_blocks * 12;
-  const cudaError_t e = cudaFuncSetAttribute(
-      cache_attn_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-  if (e != cudaSuccess) return e;
-  return launch_kernel(cache_attn_kernel<D>, dim3(p.splits, a.B * a.cache.Hkv, p.rowgroups),
-                       dim3(kWarps * 32), smem, stream, true, a, L, p.wr);
+// 3D view of a cache: {d bytes, tokens of a block, blocks x heads}, box {d, a step, 1}.
+bool step_map(CUtensorMap* map, const void* base, const ssd_block_cache& c) {
+  EncodeTiledFn fn = tensor_map_encoder();
+  if (fn == nullptr) return false;
+  const cuuint64_t dims[3] = {(cuuint64_t)c.d, (cuuint64_t)c.block,
+                              (cuuint64_t)c.num_blocks * (cuuint64_t)c.Hkv};
+  const cuuint64_t strides[2] = {(cuuint64_t)c.d, (cuuint64_t)c.d * (cuuint64_t)c.block};
+  const cuuint32_t box[3] = {(cuuint32_t)c.d, kStep, 1}, estr[3] = {1, 1, 1};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void*>(base), dims, strides, box, estr,
+            CU_TENSOR_MAP_INTERLEAVE_NONE,
+            c.d == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-size_t part_bytes(int64_t rows, int32_t splits, int32_t d) {
-  if (splits == 1) return 0;
-  return align256((size_t)rows * splits * d * sizeof(float)) +
-         align256((size_t)rows * splits * sizeof(float2));
+template <int D, int NR>
+cudaError_t launch_mma(const CacheAttnArgs& a, const Plan& p, const CacheAttnLaunch& L,
+                       cudaStream_t stream) {
+  CUtensorMap tk, tv;
+  if (!step_map(&tk, a.cache.k, a.cache) || !step_map(&tv, a.cache.v, a.cache))
+    return cudaErrorInvalidValue;
+  const size_t smem = 1024 + (size_t)kWarps * kStages * 2 * kStep * D + (size_t)L.max_blocks * 12;
+  const cudaError_t e = cudaFuncSetAttribute(
+      cache_attn_kernel<D, NR>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (e != cudaSuccess) return e;
+  return launch_kernel(cache_attn_kernel<D, NR>, dim3(p.per_head, a.cache.Hkv, p.row_groups),
+                       dim3(kWarps * 32), smem, stream, true, tk, tv, a, L, p.row_warps);
+}
+
+size_t part_bytes(int64_t rows, int32_t d) {
+  return align256((size_t)rows * d * sizeof(float)) + align256((size_t)rows * sizeof(float2));
+}
+// Part rows of the tensor-core kernel and of the other one (0: nothing is cut).
+int64_t tc_part_rows(int32_t B, int32_t Hq, int32_t D_max, int32_t splits) {
+  return splits == 1 ? 0 : (int64_t)B * D_max * Hq * splits;
+}
+int64_t mma_part_rows(int32_t B, int32_t Hkv, const Plan& p) {
+  return p.cut(B) ? (int64_t)Hkv * p.row_groups * p.per_head * p.group_rows() : 0;
 }
 
 }  // namespace
@@ -526,30 +611,48 @@ size_t cache_attention_workspace(int32_t B, int32_t Hq, int32_t Hkv, int32_t d, 
                                  int32_t L_max) {
   int32_t splits, min_tiles;
   cache_attention_tc_plan(B, Hq, Hkv, D_max, L_max, &splits, &min_tiles);
-  splits = std::max(splits, make_plan(B, Hq, Hkv, D_max, L_max).splits);
-  return part_bytes((int64_t)B * D_max * Hq, splits, d);
+  const Plan p = make_plan(B, Hq, Hkv, D_max, L_max);
+  const int64_t rows = std::max(tc_part_rows(B, Hq, D_max, splits), mma_part_rows(B, Hkv, p));
+  return rows == 0 ? 0 : part_bytes(rows, d) + align256((size_t)B * sizeof(int2));
 }
 
 cudaError_t launch_cache_attention(const CacheAttnArgs& a, void* ws, cudaStream_t stream) {
   const int32_t L_max = a.max_blocks * a.cache.block, d = a.cache.d;
+  const int32_t tiles = (L_max + kCacheTile - 1) / kCacheTile;
   const bool tc = cache_attention_tc_runs(a);
   const Plan p = make_plan(a.B, a.Hq, a.cache.Hkv, a.D_max, L_max);
-  CacheAttnLaunch L{p.splits, p.min_tiles, 0, nullptr, nullptr};
-  if (tc)
+  CacheAttnLaunch L{};
+  int64_t rows;
+  int32_t part_tiles;
+  if (tc) {
     cache_attention_tc_plan(a.B, a.Hq, a.cache.Hkv, a.D_max, L_max, &L.splits, &L.min_tiles);
-  const int32_t tiles = (L_max + kCacheTile - 1) / kCacheTile;
-  L.max_blocks =
-      cache_part_tiles(L.splits, L.min_tiles, tiles) * (kCacheTile / std::min(a.cache.block, 64)) + 1;
-  const int64_t rows = (int64_t)a.B * a.D_max * a.Hq;
-  if (L.splits > 1) {
-    L.part_o = static_cast<float*>(ws);
-    L.part_ml = reinterpret_cast<float2*>(
-        static_cast<unsigned char*>(ws) + align256((size_t)rows * L.splits * d * sizeof(float)));
+    rows = tc_part_rows(a.B, a.Hq, a.D_max, L.splits);
+    part_tiles = cache_part_tiles(L.splits, L.min_tiles, tiles);
+  } else {
+    L.min_tiles = p.min_tiles;
+    L.per_head = p.per_head;
+    L.goal = p.goal;
+    L.uniform = p.uniform;
+    L.row_groups = p.row_groups;
+    L.group_rows = p.group_rows();
+    rows = mma_part_rows(a.B, a.cache.Hkv, p);
+    part_tiles = std::min(tiles, kWorkTiles);
   }
-  cudaError_t e = tc ? launch_cache_attention_tc(a, L, stream)
-                     : (d == 128 ? launch_mma<128>(a, p, L, stream) : launch_mma<64>(a, p, L, stream));
-  if (e != cudaSuccess || L.splits == 1) return e;
-  const dim3 grid((unsigned)((rows + 7) / 8));
+  L.max_blocks = part_tiles * (kCacheTile / std::min(a.cache.block, 64)) + 1;
+  if (rows > 0) {
+    unsigned char* at = static_cast<unsigned char*>(ws);
+    L.part_o = reinterpret_cast<float*>(at);
+    at += align256((size_t)rows * d * sizeof(float));
+    L.part_ml = reinterpret_cast<float2*>(at);
+    at += align256((size_t)rows * sizeof(float2));
+    if (!tc) L.info = reinterpret_cast<int2*>(at);
+  }
+  cudaError_t e;
+  if (tc) e = launch_cache_attention_tc(a, L, stream);
+  else if (d == 128) e = p.rows == 8 ? launch_mma<128, 1>(a, p, L, stream) : launch_mma<128, 2>(a, p, L, stream);
+  else e = p.rows == 8 ? launch_mma<64, 1>(a, p, L, stream) : launch_mma<64, 2>(a, p, L, stream);
+  if (e != cudaSuccess || rows == 0) return e;
+  const dim3 grid((unsigned)(((int64_t)a.B * a.D_max * a.Hq + 7) / 8));
   return d == 128 ? launch_kernel(cache_attn_combine_kernel<128>, grid, dim3(256), 0, stream, true, a, L)
                   : launch_kernel(cache_attn_combine_kernel<64>, grid, dim3(256), 0, stream, true, a, L);
 }

@@ -234,41 +234,64 @@ __device__ __forceinline__ void turn(float& x, float& y, float2 cs) {
   x = u;
 }
 
+// The eight pairs' cos and sin that 16 values of a token need (positions out of the table:
+// recorded, and position 0).  The eight are two runs of four; `wide`: a run lies in one
+// section and its table entries on a 16-byte boundary.
 template <int D>
-__device__ __forceinline__ void rotate16(const CacheAppendArgs& a, int64_t token, int32_t c8,
-                                         float (&xa)[8], float (&xb)[8]) {
-  const int32_t* p = a.pos + 3 * token;
+__device__ __forceinline__ void load_turns(const CacheAppendArgs& a, const int32_t (&pos)[3],
+                                           int32_t c8, bool wide, float2 (&cs)[8]) {
   int32_t at[3];
 #pragma unroll
   for (int i = 0; i < 3; ++i) {
-    at[i] = p[i];
+    at[i] = pos[i];
     if (at[i] < 0 || at[i] >= a.rot.n_pos) {
       record_status(a.status, SSD_ERR_DEVICE_BOUNDS);
       at[i] = 0;
     }
   }
   const int32_t s0 = a.rot.sec[0], s1 = s0 + a.rot.sec[1];
-  auto cs = [&](int32_t pair) {
+  auto entry = [&](int32_t pair) {
     const int32_t row = pair < s0 ? at[0] : (pair < s1 ? at[1] : at[2]);
-    return __ldg(reinterpret_cast<const float2*>(a.rot.table) + (int64_t)row * (D / 2) + pair);
+    return reinterpret_cast<const float2*>(a.rot.table) + (int64_t)row * (D / 2) + pair;
   };
-  if (a.rot.interleaved) {
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const int32_t pair = a.rot.interleaved ? (c8 + u * (D / 2)) / 2 : c8 + 4 * u;
+    if (wide) {
+      const float4* p = reinterpret_cast<const float4*>(entry(pair));
+      const float4 x = __ldg(p), y = __ldg(p + 1);
+      cs[4 * u] = make_float2(x.x, x.y);
+      cs[4 * u + 1] = make_float2(x.z, x.w);
+      cs[4 * u + 2] = make_float2(y.x, y.y);
+      cs[4 * u + 3] = make_float2(y.z, y.w);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) cs[4 * u + i] = __ldg(entry(pair + i));
+    }
+  }
+}
+__device__ __forceinline__ void rotate16(bool interleaved, const float2 (&cs)[8], float (&xa)[8],
+                                         float (&xb)[8]) {
+  if (interleaved) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      turn(xa[2 * i], xa[2 * i + 1], cs(c8 / 2 + i));
-      turn(xb[2 * i], xb[2 * i + 1], cs((c8 + D / 2) / 2 + i));
+      turn(xa[2 * i], xa[2 * i + 1], cs[i]);
+      turn(xb[2 * i], xb[2 * i + 1], cs[4 + i]);
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) turn(xa[i], xb[i], cs(c8 + i));
+    for (int i = 0; i < 8; ++i) turn(xa[i], xb[i], cs[i]);
   }
 }
 
 // A thread holds 16 values of a row, a row takes D / 16 lanes, and a block of
-// threads covers a cache block of S tokens of one head in four passes (at
-// least a warp): the new values stay in registers (64) between the search for
-// their largest and the rounding, so they are read once.
-constexpr int kPasses = 4;
+// threads covers a cache block of S tokens of one head in kPasses passes (at
+// least a warp): the new values stay in registers between the search for their
+// largest and the rounding, so they are read once.
+// What bounds it is the chain of dependent loads (lengths and the first slot; rows,
+// slots and positions; the table), so each link is asked for by all passes at once.
+constexpr int kPasses = 2;
+constexpr int kHeads = 4;  // heads of q that share a thread's cos and sin
 constexpr int append_threads(int d, int block) {
   return block * (d / 16) / kPasses < 32 ? 32 : block * (d / 16) / kPasses;
 }
@@ -276,23 +299,43 @@ constexpr int append_threads(int d, int block) {
 // x: new tokens' rows of one head; kIsK: rotated first.
 template <int D, bool kIsK>
 __device__ __forceinline__ void append_block(const CacheAppendArgs& a, int32_t b, int32_t i,
-                                             int32_t g, float* red) {
+                                             int32_t g, bool wide, float* red) {
   constexpr int LPR = D / 16;  // lanes of a row
   const int32_t S = a.cache.block, tid = threadIdx.x;
+  const int64_t row0 = (int64_t)b * a.N_max;
   const int32_t n = a.n_new[b];
+  const int64_t slot0 = a.slots[row0];
   if (n <= 0 || n > a.N_max) {
     if (n != 0 && tid == 0) record_status(a.status, SSD_ERR_DEVICE_BOUNDS);
     return;
   }
-  const int64_t row0 = (int64_t)b * a.N_max;
-  const int64_t slot0 = a.slots[row0];
   if (slot0 < 0) return;  // a sequence that the plan could not serve
   const int32_t off0 = (int32_t)(slot0 & (S - 1));
   const int32_t j0 = i == 0 ? 0 : i * S - off0;  // the block's first new token
   if (j0 >= n) return;
   const int32_t first = i == 0 ? off0 : 0;       // tokens it holds already
   const int32_t count = min(n - j0, S - first);
-  const int64_t slot = a.slots[row0 + j0];
+  const __nv_bfloat16* x =
+      static_cast<const __nv_bfloat16*>(kIsK ? a.k : a.v) + (row0 + j0) * (kIsK ? a.ldk : a.ldv) +
+      (int64_t)g * D;
+  const int64_t ld = kIsK ? a.ldk : a.ldv;
+  const int32_t c8 = (tid % LPR) * 8, r0 = tid / LPR, rows = blockDim.x / LPR;
+
+  uint4 wa[kPasses], wb[kPasses];
+  int64_t at[kPasses];
+  int32_t pos[kPasses][3];
+#pragma unroll
+  for (int u = 0; u < kPasses; ++u) {
+    const int32_t r = r0 + u * rows;  // of the new tokens
+    if (r >= count) continue;
+    wa[u] = *reinterpret_cast<const uint4*>(x + r * ld + c8);
+    wb[u] = *reinterpret_cast<const uint4*>(x + r * ld + c8 + D / 2);
+    at[u] = a.slots[row0 + j0 + r];
+    if (kIsK)
+#pragma unroll
+      for (int e = 0; e < 3; ++e) pos[u][e] = a.pos[3 * (row0 + j0 + r) + e];
+  }
+  const int64_t slot = i == 0 ? slot0 : a.slots[row0 + j0];
   if (slot < 0 || slot >= (int64_t)a.cache.num_blocks * S || (int32_t)(slot & (S - 1)) != first) {
     if (tid == 0) record_status(a.status, SSD_ERR_DEVICE_BOUNDS);
     return;
@@ -300,27 +343,27 @@ __device__ __forceinline__ void append_block(const CacheAppendArgs& a, int32_t b
   const int64_t head = slot / S * a.cache.Hkv + g;
   uint8_t* out = static_cast<uint8_t*>(kIsK ? a.cache.k : a.cache.v) + head * S * D;
   float* scale = (kIsK ? a.cache.k_scale : a.cache.v_scale) + head;
-  const __nv_bfloat16* x =
-      static_cast<const __nv_bfloat16*>(kIsK ? a.k : a.v) + (row0 + j0) * (kIsK ? a.ldk : a.ldv) +
-      (int64_t)g * D;
-  const int64_t ld = kIsK ? a.ldk : a.ldv;
-  const int32_t c8 = (tid % LPR) * 8, r0 = tid / LPR, rows = blockDim.x / LPR;
+  const float old = *scale;
 
   float xa[kPasses][8], xb[kPasses][8];
   bool have[kPasses];
   float m = 0.f;
 #pragma unroll
   for (int u = 0; u < kPasses; ++u) {
-    const int32_t r = r0 + u * rows;  // of the new tokens
+    const int32_t r = r0 + u * rows;
     have[u] = r < count;
-    if (have[u] && a.slots[row0 + j0 + r] != slot + r) {
+    if (have[u] && at[u] != slot + r) {
       record_status(a.status, SSD_ERR_DEVICE_BOUNDS);
       have[u] = false;
     }
     if (!have[u]) continue;
-    unpack8(*reinterpret_cast<const uint4*>(x + r * ld + c8), xa[u]);
-    unpack8(*reinterpret_cast<const uint4*>(x + r * ld + c8 + D / 2), xb[u]);
-    if (kIsK) rotate16<D>(a, row0 + j0 + r, c8, xa[u], xb[u]);
+    unpack8(wa[u], xa[u]);
+    unpack8(wb[u], xb[u]);
+    if (kIsK) {
+      float2 cs[8];
+      load_turns<D>(a, pos[u], c8, wide, cs);
+      rotate16(a.rot.interleaved, cs, xa[u], xb[u]);
+    }
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const float p = fabsf(xa[u][e]), q = fabsf(xb[u][e]);
@@ -335,7 +378,6 @@ __device__ __forceinline__ void append_block(const CacheAppendArgs& a, int32_t b
     __syncthreads();
     for (int w = 0; w < (int)blockDim.x / 32; ++w) m = fmaxf(m, red[w]);
   }
-  const float old = *scale;
   const bool grown = first == 0 || m > kTop8 * old;
   const float s = grown ? fmaxf(m, kLeast) / kTop8 : old;
   const float inv = 1.0f / s;
@@ -368,13 +410,13 @@ __device__ __forceinline__ void append_block(const CacheAppendArgs& a, int32_t b
   }
 }
 
-// Grid: first the (sequence, touched block, head) units of K, then those of V,
-// then the rows of q in pieces of kPasses passes.
+// Grid: first the (sequence, touched block, head) units of K, then those of V, then
+// those of q: a thread takes 16 columns of up to kHeads heads of a token.
 template <int D>
 __global__ void __launch_bounds__(128 * (D / 16) / kPasses)
-cache_append_kernel(CacheAppendArgs a, int32_t touched, int64_t kv_units) {
+cache_append_kernel(CacheAppendArgs a, int32_t touched, int64_t kv_units, bool wide) {
   constexpr int LPR = D / 16;
-  __shared__ float red[8];
+  __shared__ float red[128 * LPR / kPasses / 32];
   pdl_wait();
   int64_t unit = blockIdx.x;
   if (unit < 2 * kv_units) {
@@ -383,29 +425,44 @@ cache_append_kernel(CacheAppendArgs a, int32_t touched, int64_t kv_units) {
     const int32_t g = (int32_t)(unit % a.cache.Hkv);
     const int32_t bi = (int32_t)(unit / a.cache.Hkv);
     const int32_t b = bi / touched, i = bi - b * touched;
-    if (is_k) append_block<D, true>(a, b, i, g, red);
-    else append_block<D, false>(a, b, i, g, red);
+    if (is_k) append_block<D, true>(a, b, i, g, wide, red);
+    else append_block<D, false>(a, b, i, g, wide, red);
     return;
   }
   unit -= 2 * kv_units;
   const int32_t rows = blockDim.x / LPR, c8 = (threadIdx.x % LPR) * 8;
-  const int64_t total = (int64_t)a.B * a.N_max * a.Hq;
+  const int32_t groups = (a.Hq + kHeads - 1) / kHeads;
+  const int64_t r = unit * rows + threadIdx.x / LPR;
+  if (r >= (int64_t)a.B * a.N_max * groups) return;
+  const int32_t token = (int32_t)r / groups, h0 = ((int32_t)r - token * groups) * kHeads;
+  const int32_t b = token / a.N_max, n = a.n_new[b];
+  if (token - b * a.N_max >= n || n > a.N_max) return;
+  int32_t pos[3];
 #pragma unroll
-  for (int u = 0; u < kPasses; ++u) {
-    const int64_t r = unit * rows * kPasses + u * rows + threadIdx.x / LPR;
-    if (r >= total) return;
-    const int32_t token = (int32_t)(r / a.Hq), h = (int32_t)(r - (int64_t)token * a.Hq);
-    const int32_t b = token / a.N_max, n = a.n_new[b];
-    if (token - b * a.N_max >= n || n > a.N_max || a.slots[token] < 0) continue;
-    const __nv_bfloat16* x =
-        static_cast<const __nv_bfloat16*>(a.q) + token * a.ldq + (int64_t)h * D + c8;
+  for (int e = 0; e < 3; ++e) pos[e] = a.pos[3 * (int64_t)token + e];
+  const int64_t slot = a.slots[token];
+  const __nv_bfloat16* x =
+      static_cast<const __nv_bfloat16*>(a.q) + token * a.ldq + (int64_t)h0 * D + c8;
+  uint4 wa[kHeads], wb[kHeads];
+#pragma unroll
+  for (int u = 0; u < kHeads; ++u) {
+    if (h0 + u >= a.Hq) continue;
+    wa[u] = *reinterpret_cast<const uint4*>(x + u * D);
+    wb[u] = *reinterpret_cast<const uint4*>(x + u * D + D / 2);
+  }
+  if (slot < 0) return;
+  float2 cs[8];
+  load_turns<D>(a, pos, c8, wide, cs);
+  __nv_bfloat16* y = static_cast<__nv_bfloat16*>(a.q_out) + ((int64_t)token * a.Hq + h0) * D + c8;
+#pragma unroll
+  for (int u = 0; u < kHeads; ++u) {
+    if (h0 + u >= a.Hq) continue;
     float xa[8], xb[8];
-    unpack8(*reinterpret_cast<const uint4*>(x), xa);
-    unpack8(*reinterpret_cast<const uint4*>(x + D / 2), xb);
-    rotate16<D>(a, token, c8, xa, xb);
-    __nv_bfloat16* y = static_cast<__nv_bfloat16*>(a.q_out) + r * D + c8;
-    *reinterpret_cast<uint4*>(y) = pack8(xa);
-    *reinterpret_cast<uint4*>(y + D / 2) = pack8(xb);
+    unpack8(wa[u], xa);
+    unpack8(wb[u], xb);
+    rotate16(a.rot.interleaved, cs, xa, xb);
+    *reinterpret_cast<uint4*>(y + u * D) = pack8(xa);
+    *reinterpret_cast<uint4*>(y + u * D + D / 2) = pack8(xb);
   }
 }
 
@@ -433,13 +490,17 @@ cudaError_t launch_cache_append(const CacheAppendArgs& a, cudaStream_t stream) {
   // blocks that N_max tokens can touch: from the last token of one on
   const int32_t touched = 1 + (a.N_max - 1 + S - 1) / S;
   const int64_t kv_units = (int64_t)a.B * touched * a.cache.Hkv;
-  const int64_t q_rows = (int64_t)a.B * a.N_max * a.Hq, per = (int64_t)threads / (d / 16) * kPasses;
+  const int64_t q_rows = (int64_t)a.B * a.N_max * ((a.Hq + kHeads - 1) / kHeads);
+  const int32_t per = threads / (d / 16);
   const int64_t grid = 2 * kv_units + (q_rows + per - 1) / per;
   if (grid > INT32_MAX) return cudaErrorInvalidValue;
+  const int32_t s0 = a.rot.sec[0], s1 = s0 + a.rot.sec[1];
+  const bool wide =
+      s0 % 4 == 0 && s1 % 4 == 0 && (reinterpret_cast<uintptr_t>(a.rot.table) & 15) == 0;
   return d == 128 ? launch_kernel(cache_append_kernel<128>, dim3((unsigned)grid), dim3(threads), 0,
-                                  stream, true, a, touched, kv_units)
+                                  stream, true, a, touched, kv_units, wide)
                   : launch_kernel(cache_append_kernel<64>, dim3((unsigned)grid), dim3(threads), 0,
-                                  stream, true, a, touched, kv_units);
+                                  stream, true, a, touched, kv_units, wide);
 }
 
 }  // namespace ssd

@@ -102,6 +102,24 @@ __device__ __forceinline__ float bin_of(float ref, float c, float x) {
   return fmaf(__fsub_rn(ref, x), c * kPlaces, (float)(kHead * kPlaces));
 }
 
+// An entry into the histogram (not those below the last bin, nor a NaN).  Predicated: a
+// branch per entry took more than the additions.
+template <bool PLACES>
+__device__ __forceinline__ void add_to_bin(uint32_t cnt0, uint32_t place0, float b) {
+  const uint32_t at = __float2uint_rz(b), off = at / kPlaces * 4;
+  if constexpr (PLACES)
+    asm volatile(
+        "{\n .reg .pred p;\n setp.lt.f32 p, %0, %1;\n"
+        " @p red.shared.add.u32 [%2], 1;\n @p red.shared.add.u32 [%3], %4;\n}" ::"f"(b),
+        "f"((float)(kBins * kPlaces)), "r"(cnt0 + off), "r"(place0 + off), "r"(at % kPlaces)
+        : "memory");
+  else
+    asm volatile(
+        "{\n .reg .pred p;\n setp.lt.f32 p, %0, %1;\n @p red.shared.add.u32 [%2], 1;\n}" ::"f"(b),
+        "f"((float)(kBins * kPlaces)), "r"(cnt0 + off)
+        : "memory");
+}
+
 template <int MODE>
 __device__ __forceinline__ int32_t index_of(int32_t ch, int u, int lane) {
   if (MODE == kF32Vec) return ch * kChunk + (u >> 2) * 128 + lane * 4 + (u & 3);
@@ -335,26 +353,93 @@ __device__ __noinline__ void select(SampleRow r, SampleShared& sh, bool of_row, 
   __syncthreads();
 }
 
-// Index behind the n_eq-th entry of the row (in index order) that equals the cut.
+// Index behind the n_eq-th entry (in index order) that equals the cut, to cut_idx.
+// From the list, which holds all of them: a radix search over their indices.
+__device__ __noinline__ void list_ties(SampleShared& sh) {
+  const int32_t n = sh.n_list, tid = threadIdx.x;
+  const uint32_t cut = sh.cut;
+  uint32_t left = (uint32_t)sh.n_eq;  // (at most kList)
+  int32_t base = 0;                   // the index's digits found
+#pragma unroll 1
+  for (int shift = 16; shift >= 0; shift -= 8) {
+    __syncthreads();
+    if (tid < 256) sh.rcnt[tid] = 0;
+    __syncthreads();
+#pragma unroll 1
+    for (int32_t i = tid; i < n; i += kSampleThreads)
+      if (sh.key[i] == cut && ((sh.idx[i] ^ base) >> shift) < 256)
+        atomicAdd(&sh.rcnt[(sh.idx[i] >> shift) & 255], 1u);
+    __syncthreads();
+    // (every warp for itself) lane l: digits 8 l .. 8 l + 7
+    const int32_t lane = tid & 31;
+    uint32_t mine = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) mine += sh.rcnt[8 * lane + i];
+    uint32_t upto = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t y = __shfl_up_sync(0xffffffffu, upto, o);
+      if (lane >= o) upto += y;
+    }
+    const uint32_t reach = __ballot_sync(0xffffffffu, upto >= left);
+    const int src = reach ? __ffs(reach) - 1 : 31;
+    int32_t d = 8 * src;
+    left -= __shfl_sync(0xffffffffu, upto - mine, src);
+#pragma unroll 1
+    for (int i = 0; i < 7 && sh.rcnt[d] < left; ++i, ++d) left -= sh.rcnt[d];
+    base |= d << shift;
+  }
+  __syncthreads();
+  if (tid == 0) sh.cut_idx = base + 1;
+  __syncthreads();
+}
+// From the row: counts by chunks (where the chunks' masses will stand), then the chunk's.
 template <int MODE>
-__device__ __noinline__ void row_ties(SampleRow r, SampleShared& sh) {
+__device__ __noinline__ void row_ties(SampleRow r, SampleShared& sh, u64* chunk, int32_t chunks) {
   const int32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const uint32_t cut = sh.cut;
-  const u64 n_eq = sh.n_eq;
-  if (threadIdx.x == 0) sh.cut_idx = 0x7fffffff;
-  u64 seen = 0;
+  __syncthreads();
+  if (tid == 0) sh.cut_idx = 0x7fffffff;
+#pragma unroll 2
+  for (int32_t ch = warp; ch < chunks; ch += kSampleWarps) {
+    float x[8];
+    load8<MODE>(r, ch, lane, x);
+    uint32_t n = 0;
+#pragma unroll
+    for (int u = 0; u < 8; ++u)  // (behind the row: -inf, which is no cut)
+      n += key_of(clean(x[u])) == cut ? 1 : 0;
+    n = __reduce_add_sync(0xffffffffu, n);
+    if (lane == 0) chunk[ch] = n;
+  }
+  __syncthreads();
+  if (warp == 0) {
+    u64 left = sh.n_eq;
+    int32_t ch = 0;
+    for (; ch < chunks; ch += 32) {  // 32 chunks at a time
+      const uint32_t n = ch + lane < chunks ? (uint32_t)chunk[ch + lane] : 0;
+      uint32_t upto = n;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t y = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += y;
+      }
+      const uint32_t reach = __ballot_sync(0xffffffffu, upto >= left);
+      if (reach) {
+        const int src = __ffs(reach) - 1;
+        left -= __shfl_sync(0xffffffffu, upto - n, src);
+        ch += src;
+        break;
+      }
+      left -= __shfl_sync(0xffffffffu, upto, 31);
+    }
 #pragma unroll 1
-  for (int32_t i0 = 0; i0 < r.V && seen < n_eq; i0 += kSampleThreads) {
-    const int32_t i = i0 + tid;
-    const bool eq = i < r.V && key_of(clean(load1<MODE>(r.x, r.inf, i))) == cut;
-    const uint32_t ball = __ballot_sync(0xffffffffu, eq);
-    __syncthreads();
-    if (lane == 0) sh.redi[warp] = __popc(ball);
-    __syncthreads();
-    u64 before = seen;
-    for (int w = 0; w < warp; ++w) before += sh.redi[w];
-    if (eq && before + __popc(ball & ((1u << lane) - 1u)) + 1 == n_eq) sh.cut_idx = i + 1;
-    for (int w = 0; w < kSampleWarps; ++w) seen += sh.redi[w];
+    for (int u = 0; u < kChunk / 32 && left > 0; ++u) {
+      const int32_t i = ch * kChunk + u * 32 + lane;
+      const bool eq = i < r.V && key_of(clean(load1<MODE>(r.x, r.inf, i))) == cut;
+      const uint32_t ball = __ballot_sync(0xffffffffu, eq);
+      if (eq && (u64)__popc(ball & ((1u << lane) - 1u)) + 1 == left) sh.cut_idx = i + 1;
+      left = (u64)__popc(ball) >= left ? 0 : left - __popc(ball);
+    }
   }
   __syncthreads();
 }
@@ -558,26 +643,25 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
         for (int i = 0; i < kBins / kSampleThreads; ++i)
           sh.cnt[tid + i * kSampleThreads] = sh.place[tid + i * kSampleThreads] = 0;
         __syncthreads();
+        const uint32_t cnt0 = smem_u32(sh.cnt), place0 = smem_u32(sh.place);
+        auto count = [&](auto places) {
 #pragma unroll 2
-        for (int32_t ch = warp; ch < chunks; ch += kSampleWarps) {
-          float x[8];
-          load8<MODE>(r, ch, lane, x);
-          m = fmaxf(m, max8(x));
+          for (int32_t ch = warp; ch < chunks; ch += kSampleWarps) {
+            float x[8];
+            load8<MODE>(r, ch, lane, x);
+            m = fmaxf(m, max8(x));
 #pragma unroll
-          for (int u = 0; u < 8; u += 2) {
-            const float2 b = bin2_of(ref, r.c, x[u], x[u + 1]);
-            // (bins above the first count as the first; a NaN fails the comparison)
+            for (int u = 0; u < 8; u += 2) {
+              const float2 b = bin2_of(ref, r.c, x[u], x[u + 1]);
+              // (bins above the first count as the first)
 #pragma unroll
-            for (int v = 0; v < 2; ++v) {
-              const float bv = v ? b.y : b.x;
-              if (bv < (float)(kBins * kPlaces)) {
-                const uint32_t at = __float2uint_rz(bv);
-                atomicAdd(&sh.cnt[at / kPlaces], 1u);
-                if (cut_p) atomicAdd(&sh.place[at / kPlaces], at % kPlaces);
-              }
+              for (int v = 0; v < 2; ++v)
+                add_to_bin<decltype(places)::value>(cnt0, place0, v ? b.y : b.x);
             }
           }
-        }
+        };
+        if (cut_p) count(std::true_type());
+        else count(std::false_type());
       } else {
 #pragma unroll 4
         for (int32_t ch = warp; ch < chunks; ch += kSampleWarps) {
@@ -807,7 +891,11 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
           select<MODE>(r, sh, true, false, need, key_of(-INFINITY), key_of(r.top));
         }
       }
-      if (sh.n_eq != 0) row_ties<MODE>(r, sh);  // equal entries at the cut, too many for a warp
+      // equal entries at the cut, too many for a warp
+      if (sh.n_eq != 0) {
+        if (by_row) row_ties<MODE>(r, sh, chunk, chunks);
+        else list_ties(sh);
+      }
     }
     __syncthreads();
     const uint32_t cut = sh.cut;

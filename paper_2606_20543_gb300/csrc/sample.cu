@@ -45,13 +45,13 @@ constexpr float kMassErr = 0x1p-15f;
 constexpr int kFew = 32;                  // entries that one warp orders by itself
 typedef unsigned long long u64;
 
-// How a row is read: vectors of 16 bytes where it is aligned, else entry by
-// entry.  Lane l takes entries index_of(ch, u, l), u < 8, of chunk ch.
-enum Mode { kF32Vec, kBf16Vec, kF32, kBf16 };
-
+// A row is read in vectors of 16 bytes from the boundary at or before its first entry, so
+// chunk 0 may begin `off` entries before the row: chunk ch holds entries ch * kChunk - off
+// and on.  Chunks that the row does not fill are read entry by entry.
+// Lane l takes entries index_of(r, ch, u, l), u < 8, of chunk ch.
 struct SampleRow {
   const void* x;
-  int32_t V;
+  int32_t V, off;
   bool inf;      // the largest logit is infinite: logits count as 0 (infinite) or -inf
   float top;     // the largest logit
   float c;       // bins per unit of logit: kBinsPerLog2 * log2(e) / T
@@ -120,29 +120,28 @@ __device__ __forceinline__ void add_to_bin(uint32_t cnt0, uint32_t place0, float
         : "memory");
 }
 
-template <int MODE>
-__device__ __forceinline__ int32_t index_of(int32_t ch, int u, int lane) {
-  if (MODE == kF32Vec) return ch * kChunk + (u >> 2) * 128 + lane * 4 + (u & 3);
-  if (MODE == kBf16Vec) return ch * kChunk + lane * 8 + u;
-  return ch * kChunk + u * 32 + lane;
+template <bool BF16>
+__device__ __forceinline__ int32_t index_of(const SampleRow& r, int32_t ch, int u, int lane) {
+  return ch * kChunk - r.off + (BF16 ? lane * 8 + u : (u >> 2) * 128 + lane * 4 + (u & 3));
 }
-template <int MODE>
+template <bool BF16>
 __device__ __forceinline__ float load1(const void* x, bool inf, int32_t i) {
-  const float v = MODE == kF32Vec || MODE == kF32
-                      ? static_cast<const float*>(x)[i]
-                      : __uint_as_float((uint32_t) static_cast<const uint16_t*>(x)[i] << 16);
+  const float v = BF16 ? __uint_as_float((uint32_t) static_cast<const uint16_t*>(x)[i] << 16)
+                       : static_cast<const float*>(x)[i];
   return inf ? finite_or_not(v) : v;
 }
-template <int MODE>
+template <bool BF16>
 __device__ __forceinline__ void load8(const SampleRow& r, int32_t ch, int lane, float (&x)[8]) {
-  if ((MODE == kF32Vec || MODE == kBf16Vec) && (ch + 1) * kChunk <= r.V) {
-    if constexpr (MODE == kF32Vec) {
-      const float4* p = static_cast<const float4*>(r.x) + ch * (kChunk / 4) + lane;
+  const int32_t first = ch * kChunk - r.off;
+  if (first >= 0 && first + kChunk <= r.V) {
+    if constexpr (!BF16) {
+      const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(r.x) + first) + lane;
       const float4 a = p[0], b = p[32];
       x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w;
       x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
     } else {
-      const uint4 a = static_cast<const uint4*>(r.x)[ch * (kChunk / 8) + lane];
+      const uint4 a =
+          reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(r.x) + first)[lane];
       const uint32_t w[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -157,8 +156,8 @@ __device__ __forceinline__ void load8(const SampleRow& r, int32_t ch, int lane, 
   } else {
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
-      const int32_t i = index_of<MODE>(ch, u, lane);
-      x[u] = i < r.V ? load1<MODE>(r.x, r.inf, i) : -INFINITY;
+      const int32_t i = index_of<BF16>(r, ch, u, lane);
+      x[u] = i >= 0 && i < r.V ? load1<BF16>(r.x, r.inf, i) : -INFINITY;
     }
   }
 }
@@ -220,11 +219,11 @@ __device__ __forceinline__ u64 add_wide(u64 s, uint32_t w) {
 // least 1 and at most the entries' count or mass.  Each round deals the keys left to 256 digits
 // and keeps one digit's; a few entries are then ordered by one warp, a lane each.  Where
 // more share one key, the entries of that key that are kept are counted instead (n_eq).
-template <int MODE>
+template <bool BF16>
 __device__ __noinline__ void select(SampleRow r, SampleShared& sh, bool of_row, bool by_count, u64 need,
                                     uint32_t lo, uint32_t hi) {
   const int32_t n = of_row ? r.V : sh.n_list, tid = threadIdx.x;
-  auto key_at = [&](int32_t i) { return of_row ? key_of(clean(load1<MODE>(r.x, r.inf, i))) : sh.key[i]; };
+  auto key_at = [&](int32_t i) { return of_row ? key_of(clean(load1<BF16>(r.x, r.inf, i))) : sh.key[i]; };
   __syncthreads();
   if (tid == 0) {
     sh.from = lo;
@@ -394,7 +393,7 @@ __device__ __noinline__ void list_ties(SampleShared& sh) {
   __syncthreads();
 }
 // From the row: counts by chunks (where the chunks' masses will stand), then the chunk's.
-template <int MODE>
+template <bool BF16>
 __device__ __noinline__ void row_ties(SampleRow r, SampleShared& sh, u64* chunk, int32_t chunks) {
   const int32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const uint32_t cut = sh.cut;
@@ -403,7 +402,7 @@ __device__ __noinline__ void row_ties(SampleRow r, SampleShared& sh, u64* chunk,
 #pragma unroll 2
   for (int32_t ch = warp; ch < chunks; ch += kSampleWarps) {
     float x[8];
-    load8<MODE>(r, ch, lane, x);
+    load8<BF16>(r, ch, lane, x);
     uint32_t n = 0;
 #pragma unroll
     for (int u = 0; u < 8; ++u)  // (behind the row: -inf, which is no cut)
@@ -434,8 +433,8 @@ __device__ __noinline__ void row_ties(SampleRow r, SampleShared& sh, u64* chunk,
     }
 #pragma unroll 1
     for (int u = 0; u < kChunk / 32 && left > 0; ++u) {
-      const int32_t i = ch * kChunk + u * 32 + lane;
-      const bool eq = i < r.V && key_of(clean(load1<MODE>(r.x, r.inf, i))) == cut;
+      const int32_t i = ch * kChunk - r.off + u * 32 + lane;
+      const bool eq = i >= 0 && i < r.V && key_of(clean(load1<BF16>(r.x, r.inf, i))) == cut;
       const uint32_t ball = __ballot_sync(0xffffffffu, eq);
       if (eq && (u64)__popc(ball & ((1u << lane) - 1u)) + 1 == left) sh.cut_idx = i + 1;
       left = (u64)__popc(ball) >= left ? 0 : left - __popc(ball);
@@ -472,7 +471,7 @@ struct PassB {
 // Pass B.  Entries x >= x_sure are kept for certain (as far as min-p lets them); those in
 // [x_p, x_sure) and [x_k, x_k1) go to the list; TOTAL: the mass of the rest of the
 // row counts too, else that of [x_k1, x_p).
-template <int MODE, bool TOTAL>
+template <bool BF16, bool TOTAL>
 __device__ __forceinline__ PassB pass_b(const SampleRow& r, SampleShared& sh, u64* chunk,
                                         int32_t chunks, float x_sure, float x_p, float x_k1,
                                         float x_k) {
@@ -483,7 +482,7 @@ __device__ __forceinline__ PassB pass_b(const SampleRow& r, SampleShared& sh, u6
 #pragma unroll 1
   for (int32_t ch = warp; ch < chunks; ch += kSampleWarps) {
     float x[8];
-    load8<MODE>(r, ch, lane, x);
+    load8<BF16>(r, ch, lane, x);
     u64 s = 0;
     if (TOTAL || __any_sync(0xffffffffu, max8(x) >= end)) {
       u64 sum = 0;
@@ -556,7 +555,7 @@ __device__ __forceinline__ PassB pass_b(const SampleRow& r, SampleShared& sh, u6
           }
           if (at < kList) {
             sh.key[at] = key_of(clean(xu));
-            sh.idx[at] = index_of<MODE>(ch, u, lane);
+            sh.idx[at] = index_of<BF16>(r, ch, u, lane);
           }
           ++at;
         }
@@ -568,14 +567,13 @@ __device__ __forceinline__ PassB pass_b(const SampleRow& r, SampleShared& sh, u6
   return out;
 }
 
-template <int MODE>
+template <bool BF16>
 __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a) {
   extern __shared__ __align__(16) unsigned char smem_raw[];
   SampleShared& sh = *reinterpret_cast<SampleShared*>(smem_raw);
   u64* chunk = reinterpret_cast<u64*>(smem_raw + sizeof(SampleShared));
   pdl_wait();
   const int32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int32_t chunks = (a.V + kChunk - 1) / kChunk;
   auto block_max = [&](float m) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
@@ -616,8 +614,10 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
       continue;
     }
     r.V = a.V;
-    r.x = a.bf16 ? static_cast<const void*>(static_cast<const uint16_t*>(a.logits) + row * a.ld)
-                 : static_cast<const void*>(static_cast<const float*>(a.logits) + row * a.ld);
+    r.x = BF16 ? static_cast<const void*>(static_cast<const uint16_t*>(a.logits) + row * a.ld)
+               : static_cast<const void*>(static_cast<const float*>(a.logits) + row * a.ld);
+    r.off = (int32_t)((reinterpret_cast<uintptr_t>(r.x) & 15u) / (BF16 ? 2 : 4));
+    const int32_t chunks = (a.V + r.off + kChunk - 1) / kChunk;
     r.c = T > 0.f ? fminf(kLog2e / T, kMaxC) * kBinsPerLog2 : 1.f;
     r.inf = false;
     const float u_res = warp == 0 ? row_uniforms(a.rng, row).y : 0.f;
@@ -629,7 +629,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
     float ref = 0.f;
     if (cut_k || cut_p) {
       float x[8];
-      load8<MODE>(r, warp, lane, x);  // (beyond the row: -inf)
+      load8<BF16>(r, warp, lane, x);  // (beyond the row: -inf)
       ref = block_max(max8(x));
     }
     float m;
@@ -648,7 +648,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
 #pragma unroll 2
           for (int32_t ch = warp; ch < chunks; ch += kSampleWarps) {
             float x[8];
-            load8<MODE>(r, ch, lane, x);
+            load8<BF16>(r, ch, lane, x);
             m = fmaxf(m, max8(x));
 #pragma unroll
             for (int u = 0; u < 8; u += 2) {
@@ -666,7 +666,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
 #pragma unroll 4
         for (int32_t ch = warp; ch < chunks; ch += kSampleWarps) {
           float x[8];
-          load8<MODE>(r, ch, lane, x);
+          load8<BF16>(r, ch, lane, x);
           const float y = max8(x);
           if (y > m) {
             m = y;
@@ -692,8 +692,8 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
       int32_t at = 0x7fffffff;
       if (m == r.top)
         for (int u = 7; u >= 0; --u) {
-          const int32_t i = index_of<MODE>(mc, u, lane);
-          if (i < r.V && load1<MODE>(r.x, false, i) == r.top) at = i;
+          const int32_t i = index_of<BF16>(r, mc, u, lane);
+          if (i >= 0 && i < r.V && load1<BF16>(r.x, false, i) == r.top) at = i;
         }
       at = __reduce_min_sync(0xffffffffu, at);
       if (lane == 0) sh.redi[warp] = at;
@@ -847,9 +847,9 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
     // ---- B
     auto at_key = [](uint32_t key) { return key == 0xffffffffu ? INFINITY : of_key(key); };
     const PassB pb = cut_p && !has_k
-                         ? pass_b<MODE, true>(r, sh, chunk, chunks, at_key(key_sure), at_key(key_p),
+                         ? pass_b<BF16, true>(r, sh, chunk, chunks, at_key(key_sure), at_key(key_p),
                                               INFINITY, INFINITY)
-                         : pass_b<MODE, false>(r, sh, chunk, chunks, at_key(key_sure), at_key(key_p),
+                         : pass_b<BF16, false>(r, sh, chunk, chunks, at_key(key_sure), at_key(key_p),
                                                at_key(key_k1), at_key(key_k));
     uint32_t count = pb.count;
     bool by_row = false;  // the chunks' masses are to be summed again
@@ -862,7 +862,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
       __syncthreads();
       const bool overflow = sh.n_list > kList;
       by_row = overflow;
-      if (has_k) select<MODE>(r, sh, overflow, true, (u64)sh.need_k, key_k, key_k1 - 1);
+      if (has_k) select<BF16>(r, sh, overflow, true, (u64)sh.need_k, key_k, key_k1 - 1);
       if (cut_p) {
         u64 k_mass = rest, listed = 0;
         // mass of the listed entries before the top-k bin
@@ -872,7 +872,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
         } else {
 #pragma unroll 1
           for (int32_t i = tid; i < r.V; i += kSampleThreads) {
-            const float x = load1<MODE>(r.x, r.inf, i);
+            const float x = load1<BF16>(r.x, r.inf, i);
             const uint32_t key = key_of(clean(x));
             if (key >= key_p && key < key_sure && (!has_k || key >= key_k1)) listed += weight_of(r, x);
           }
@@ -884,16 +884,16 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
         const bool with_k = has_k && key_p <= key_k;
         const u64 reach = sure + listed + (with_k ? sh.cut_mass : 0);
         if (need > sure && need <= reach) {
-          select<MODE>(r, sh, overflow, false, need - sure, with_k ? key_k : key_p, key_sure - 1);
+          select<BF16>(r, sh, overflow, false, need - sure, with_k ? key_k : key_p, key_sure - 1);
         } else {
           // the estimate was off: the cut is not in the listed bins
           by_row = true;
-          select<MODE>(r, sh, true, false, need, key_of(-INFINITY), key_of(r.top));
+          select<BF16>(r, sh, true, false, need, key_of(-INFINITY), key_of(r.top));
         }
       }
       // equal entries at the cut, too many for a warp
       if (sh.n_eq != 0) {
-        if (by_row) row_ties<MODE>(r, sh, chunk, chunks);
+        if (by_row) row_ties<BF16>(r, sh, chunk, chunks);
         else list_ties(sh);
       }
     }
@@ -912,11 +912,11 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
 #pragma unroll 1
       for (int32_t ch = warp; ch < chunks; ch += kSampleWarps) {
         float x[8];
-        load8<MODE>(r, ch, lane, x);
+        load8<BF16>(r, ch, lane, x);
         u64 s = 0;
 #pragma unroll
         for (int u = 0; u < 8; ++u) {
-          const uint32_t w = kept_weight(x[u], index_of<MODE>(ch, u, lane));
+          const uint32_t w = kept_weight(x[u], index_of<BF16>(r, ch, u, lane));
           s += w;
           count += w != 0;
         }
@@ -929,7 +929,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
         const uint32_t w = kept_weight(of_key(sh.key[i]), sh.idx[i]);
         if (w == 0) continue;
         ++count;
-        atomicAdd(&chunk[sh.idx[i] / kChunk], (u64)w);
+        atomicAdd(&chunk[(sh.idx[i] + r.off) / kChunk], (u64)w);
       }
     }
     count = __reduce_add_sync(0xffffffffu, count);
@@ -969,8 +969,8 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
       u64 c = 0;
 #pragma unroll
       for (int u = 0; u < 8; ++u) {
-        const int32_t i = ch * kChunk + lane * 8 + u;
-        w[u] = i < r.V ? kept_weight(load1<MODE>(r.x, r.inf, i), i) : 0;
+        const int32_t i = ch * kChunk - r.off + lane * 8 + u;
+        w[u] = i >= 0 && i < r.V ? kept_weight(load1<BF16>(r.x, r.inf, i), i) : 0;
         c += w[u];
       }
       u64 ci = c;
@@ -988,7 +988,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
       for (int u = 0; u < 8; ++u) {
         before += w[u];
         if (pick < 0 && before > aim) {
-          pick = ch * kChunk + lane * 8 + u;
+          pick = ch * kChunk - r.off + lane * 8 + u;
           wp = w[u];
         }
       }
@@ -1003,25 +1003,24 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
   }
 }
 
-template <int MODE>
+template <bool BF16>
 cudaError_t launch(const SampleArgs& a, cudaStream_t stream) {
-  const size_t smem = sizeof(SampleShared) + (size_t)((a.V + kChunk - 1) / kChunk) * sizeof(u64);
+  // (a row may begin up to 7 entries behind its first chunk's begin)
+  const size_t smem =
+      sizeof(SampleShared) + (size_t)((a.V + 7 + kChunk - 1) / kChunk) * sizeof(u64);
   const cudaError_t e = cudaFuncSetAttribute(
-      sample_kernel<MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+      sample_kernel<BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;
   // a row per CTA, dealt by the hardware as CTAs end
   const unsigned blocks = (unsigned)std::min<int64_t>(a.rows, 1 << 20);
-  return launch_kernel(sample_kernel<MODE>, dim3(blocks), dim3(kSampleThreads), smem, stream, true,
+  return launch_kernel(sample_kernel<BF16>, dim3(blocks), dim3(kSampleThreads), smem, stream, true,
                        a);
 }
 
 }  // namespace
 
 cudaError_t launch_sample(const SampleArgs& a, cudaStream_t stream) {
-  const int64_t bytes = a.bf16 ? 2 : 4;
-  const bool vec = (reinterpret_cast<uintptr_t>(a.logits) & 15u) == 0 && a.ld * bytes % 16 == 0;
-  if (a.bf16) return vec ? launch<kBf16Vec>(a, stream) : launch<kBf16>(a, stream);
-  return vec ? launch<kF32Vec>(a, stream) : launch<kF32>(a, stream);
+  return a.bf16 ? launch<true>(a, stream) : launch<false>(a, stream);
 }
 
 }  // namespace ssd

@@ -105,18 +105,18 @@ __device__ __forceinline__ float bin_of(float ref, float c, float x) {
 // An entry into the histogram (not those below the last bin, nor a NaN).  Predicated: a
 // branch per entry took more than the additions.
 template <bool PLACES>
-__device__ __forceinline__ void add_to_bin(uint32_t cnt0, uint32_t place0, float b) {
-  const uint32_t at = __float2uint_rz(b), off = at / kPlaces * 4;
+__device__ __forceinline__ void add_to_bin(uint32_t cnt0, float b) {
+  const uint32_t at = __float2uint_rz(b), to = cnt0 + at / kPlaces * 4;
   if constexpr (PLACES)
     asm volatile(
         "{\n .reg .pred p;\n setp.lt.f32 p, %0, %1;\n"
-        " @p red.shared.add.u32 [%2], 1;\n @p red.shared.add.u32 [%3], %4;\n}" ::"f"(b),
-        "f"((float)(kBins * kPlaces)), "r"(cnt0 + off), "r"(place0 + off), "r"(at % kPlaces)
+        " @p red.shared.add.u32 [%2], 1;\n @p red.shared.add.u32 [%2 + %4], %3;\n}" ::"f"(b),
+        "f"((float)(kBins * kPlaces)), "r"(to), "r"(at % kPlaces), "n"(kBins * 4)
         : "memory");
   else
     asm volatile(
         "{\n .reg .pred p;\n setp.lt.f32 p, %0, %1;\n @p red.shared.add.u32 [%2], 1;\n}" ::"f"(b),
-        "f"((float)(kBins * kPlaces)), "r"(cnt0 + off)
+        "f"((float)(kBins * kPlaces)), "r"(to)
         : "memory");
 }
 
@@ -167,7 +167,7 @@ __device__ __forceinline__ float max8(const float (&x)[8]) {  // NaN loses
 
 struct SampleShared {
   uint32_t cnt[kBins];
-  uint32_t place[kBins];
+  uint32_t place[kBins];  // (right behind cnt)
   uint32_t key[kList];  // the list
   int32_t idx[kList];
   uint32_t rsum[3][256];  // radix search: the masses' 11, 11 and 10 bits, each summed
@@ -491,8 +491,8 @@ __device__ __forceinline__ PassB pass_b(const SampleRow& r, SampleShared& sh, u6
       auto entries = [&](auto min_p) {
 #pragma unroll
         for (int u = 0; u < 8; u += 2) {
-          const float2 z = fmul2(below2(r.top, x[u], x[u + 1]), both(r.c));
-          const float2 e = fmul2(z, both(-1.f / kBinsPerLog2));
+          // (as weight_f: a power of two changes no rounding)
+          const float2 e = fmul2(below2(r.top, x[u], x[u + 1]), both(r.c * (-1.f / kBinsPerLog2)));
           const float2 w = make_float2(ex2_approx(e.x), ex2_approx(e.y));
           const float2 f = fmul2(w, both(0x1p31f));
 #pragma unroll
@@ -643,7 +643,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
         for (int i = 0; i < kBins / kSampleThreads; ++i)
           sh.cnt[tid + i * kSampleThreads] = sh.place[tid + i * kSampleThreads] = 0;
         __syncthreads();
-        const uint32_t cnt0 = smem_u32(sh.cnt), place0 = smem_u32(sh.place);
+        const uint32_t cnt0 = smem_u32(sh.cnt);
         auto count = [&](auto places) {
 #pragma unroll 2
           for (int32_t ch = warp; ch < chunks; ch += kSampleWarps) {
@@ -656,7 +656,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
               // (bins above the first count as the first)
 #pragma unroll
               for (int v = 0; v < 2; ++v)
-                add_to_bin<decltype(places)::value>(cnt0, place0, v ? b.y : b.x);
+                add_to_bin<decltype(places)::value>(cnt0, v ? b.y : b.x);
             }
           }
         };

@@ -42,7 +42,7 @@ constexpr float kBinLn = 0.0054152123f;   // ln 2 / 128: log of the ratio of a b
 // A bin's mass is taken at its entries' mean place: off by half a place's width (2^-17) and
 // by the curvature of the exponential (kBinLn^2 / 8), and the sums by their roundings.
 constexpr float kMassErr = 0x1p-15f;
-constexpr int kFew = 32;                  // entries that one warp orders by itself
+constexpr int kFew = 128;                 // entries that are ordered by comparing each with all
 typedef unsigned long long u64;
 
 // A row is read in vectors of 16 bytes from the boundary at or before its first entry, so
@@ -172,8 +172,7 @@ struct SampleShared {
   int32_t idx[kList];
   uint32_t rsum[3][256];  // radix search: the masses' 11, 11 and 10 bits, each summed
   uint32_t rcnt[256];
-  uint32_t few_key[kFew];
-  int32_t few_idx[kFew];
+  uint4 few[kFew];        // ~index, key (a number that orders entries), weight
   u64 red[kSampleWarps], red2[kSampleWarps];
   float redf[kSampleWarps];
   int32_t redi[kSampleWarps];
@@ -217,8 +216,9 @@ __device__ __forceinline__ u64 add_wide(u64 s, uint32_t w) {
 // is reached among the entries (of the list, or of the row) whose keys are in lo .. hi: its
 // key, the index behind it and the mass of everything up to and including it.  need is at
 // least 1 and at most the entries' count or mass.  Each round deals the keys left to 256 digits
-// and keeps one digit's; a few entries are then ordered by one warp, a lane each.  Where
-// more share one key, the entries of that key that are kept are counted instead (n_eq).
+// and keeps one digit's, until a few entries are left (most lists are short from the start):
+// then each is compared with all, a thread per entry.  Where more share one key, the
+// entries of that key that are kept are counted instead (n_eq).
 template <bool BF16>
 __device__ __noinline__ void select(SampleRow r, SampleShared& sh, bool of_row, bool by_count, u64 need,
                                     uint32_t lo, uint32_t hi) {
@@ -235,10 +235,11 @@ __device__ __noinline__ void select(SampleRow r, SampleShared& sh, bool of_row, 
   }
 #pragma unroll 1
   while (true) {
-    if (tid < 256) sh.rcnt[tid] = sh.rsum[0][tid] = sh.rsum[1][tid] = sh.rsum[2][tid] = 0;
     __syncthreads();
     const uint32_t from = sh.from, to = sh.to;
     if (from == to || sh.left <= kFew) break;
+    if (tid < 256) sh.rcnt[tid] = sh.rsum[0][tid] = sh.rsum[1][tid] = sh.rsum[2][tid] = 0;
+    __syncthreads();
     const int shift = max(0, 24 - __clz(to - from));
 #pragma unroll 1
     for (int32_t i = tid; i < n; i += kSampleThreads) {
@@ -304,43 +305,30 @@ __device__ __noinline__ void select(SampleRow r, SampleShared& sh, bool of_row, 
       const uint32_t k = key_at(i);
       if (k < from || k > to) continue;
       const uint32_t at = atomicAdd(&sh.n_few, 1u);
-      sh.few_key[at] = k;
-      sh.few_idx[at] = of_row ? i : sh.idx[i];
+      sh.few[at] = make_uint4(~(uint32_t)(of_row ? i : sh.idx[i]), k, weight_of(r, of_key(k)), 0);
     }
     __syncthreads();
-    if (tid < 32) {
-      const int32_t n_few = (int32_t)sh.n_few;
-      const bool have = tid < n_few;
-      const uint32_t k = have ? sh.few_key[tid] : 0;
-      const int32_t i = have ? sh.few_idx[tid] : 0x7fffffff;
-      const uint32_t w = have ? weight_of(r, of_key(k)) : 0;
-      u64 before = 0;
-#pragma unroll 1
-      for (int j = 0; j < n_few; ++j) {
-        const uint32_t kj = __shfl_sync(0xffffffffu, k, j), wj = __shfl_sync(0xffffffffu, w, j);
-        const int32_t ij = __shfl_sync(0xffffffffu, i, j);
-        if (kj > k || (kj == k && ij < i)) before += by_count ? 1 : wj;
+    const int32_t n_few = (int32_t)sh.n_few;
+    if (tid < n_few) {
+      const u64 left = sh.need;
+      auto order = [](const uint4& x) { return ((u64)x.y << 32) | x.x; };
+      const uint4 me = sh.few[tid];
+      u64 mass = 0;  // of the entries before this one in the order, and their count
+      uint32_t count = 0;
+#pragma unroll 4
+      for (int32_t j = 0; j < n_few; ++j) {
+        const uint4 x = sh.few[j];
+        const bool first = order(x) > order(me);
+        mass = add_wide(mass, first ? x.z : 0);
+        count += first ? 1 : 0;
       }
-      // the last entry that starts below the need
-      const bool kept = have && before < sh.need;
-      const u64 mine = kept ? before : 0;
-      u64 most = mine;
-      u64 mass = kept ? w : 0;
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) {
-        most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
-        mass += __shfl_xor_sync(0xffffffffu, mass, o);
-      }
-      // (entries of weight 0 may share a start: the last of them in the order)
-      uint32_t last_key = kept && mine == most ? k : 0xffffffffu;
-      last_key = __reduce_min_sync(0xffffffffu, last_key);
-      const int32_t last_idx =
-          __reduce_max_sync(0xffffffffu, kept && mine == most && k == last_key ? i : -1);
-      if (tid == 0) {
-        sh.cut = last_key;
-        sh.cut_idx = last_idx + 1;
+      // the one entry that reaches the need
+      const u64 before = by_count ? (u64)count : mass;
+      if (before < left && before + (by_count ? 1 : me.z) >= left) {
+        sh.cut = me.y;
+        sh.cut_idx = (int32_t)~me.x + 1;
         sh.n_eq = 0;
-        sh.cut_mass = sh.above + mass;
+        sh.cut_mass = sh.above + mass + me.z;
       }
     }
   } else if (tid == 0) {
@@ -460,6 +448,15 @@ __device__ __forceinline__ uint32_t least_key(int lane, F holds) {
     if (f == 0) break;
   }
   return hi;
+}
+
+// The same with a guess: mostly within 16 steps of it.
+template <typename F>
+__device__ __forceinline__ uint32_t least_key(int lane, float guess, F holds) {
+  const uint32_t base = key_of(guess) - 16;
+  const uint32_t yes = __ballot_sync(0xffffffffu, holds(of_key(base + lane)));
+  if (fabsf(guess) < 0x1p126f && yes != 0 && !(yes & 1u)) return base + __ffs(yes) - 1;
+  return least_key(lane, holds);
 }
 
 // Sums over the row's entries (for certain kept, all), and the list, of pass B.
@@ -721,7 +718,8 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
 
     if (warp == kSampleWarps - 1) {
       // the least logit with a weight: rounding makes the others 0
-      const uint32_t at = least_key(lane, [&](float x) { return weight_of(r, x) != 0; });
+      const uint32_t at = least_key(lane, r.top - 32.f * kBinsPerLog2 / r.c,
+                                    [&](float x) { return weight_of(r, x) != 0; });
       if (lane == 0) sh.floor_key = at;
     }
 
@@ -825,7 +823,8 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
         const int32_t edge = warp == 0 ? bin_lo : warp == 1 ? bin_hi + 1
                              : warp == 2 ? bin_k : bin_k + 1;
         const uint32_t at =
-            least_key(lane, [&](float x) { return bin_of(ref, r.c, x) < (float)(edge * kPlaces); });
+            least_key(lane, ref - (float)(edge - kHead) / r.c,
+                      [&](float x) { return bin_of(ref, r.c, x) < (float)(edge * kPlaces); });
         if (lane == 0) sh.edge[warp] = at;
       }
       __syncthreads();

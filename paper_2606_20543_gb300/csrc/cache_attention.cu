@@ -135,366 +135,382 @@ cache_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
   const int32_t tid = threadIdx.x, lane = tid & 31, warp = (int32_t)warp_uniform(tid >> 5);
   const int32_t g = blockIdx.y, S = a.cache.block, S_log = 31 - __clz(S), G = a.Hq / a.cache.Hkv;
   const bool first_of = g == 0 && blockIdx.z == 0;
-  const CacheWork work = cache_work(a, L, blockIdx.x, first_of && tid < 32);
-  if (work.b < 0) return;
-  const int32_t b = work.b, split = work.split, parts = work.parts;
-  const int32_t cache = a.cache_len[b], nd = a.n_drafts[b];
-  if (!cache_lengths_ok(a, cache, nd)) return;
-  const int32_t Lk = cache + nd, rows_total = nd * G;
-  const int32_t tiles = (Lk + kCacheTile - 1) / kCacheTile;
-  const int32_t row_g0 = blockIdx.z * row_warps * RW;
-  if (row_g0 >= rows_total) return;
-  const int32_t t_lo = (int32_t)((int64_t)tiles * split / parts);
-  const int32_t t_hi = (int32_t)((int64_t)tiles * (split + 1) / parts);
-  const int32_t k_lo = t_lo * kCacheTile, k_hi = min(Lk, t_hi * kCacheTile);
-  const int32_t start = a.key_start != nullptr ? min(Lk, max(0, a.key_start[b])) : 0;
-
-  // ---- this warp's rows and its share of the steps, and the copies of the first ones
-  const int32_t wk_n = kWarps / row_warps, wr = warp % row_warps, wk = warp / row_warps;
-  const int32_t q = lane & 3, r8 = lane >> 2;
-  const int32_t row0 = row_g0 + wr * RW;
-  const int32_t first = max(k_lo, start & ~(kStep - 1));  // multiple of 16
-  unsigned char* ring = smem + warp * kWarpBytes;
-  const int32_t n_steps =
-      row0 >= rows_total || first >= k_hi ? 0 : (k_hi - first + kStep - 1) / kStep;
-  const int32_t steps = n_steps > wk ? (n_steps - wk + wk_n - 1) / wk_n : 0;
-  auto key_of = [&](int32_t t) { return first + (t * wk_n + wk) * kStep; };
-  auto issue = [&](int32_t t, int32_t id) {  // by one lane
-    const int32_t k0 = key_of(t), z = max(id, 0) * a.cache.Hkv + g;
-    unsigned char* dst = ring + (t % kStages) * kStageBytes;
-    uint64_t* bar = &s_full[warp][t % kStages];
-    const uint64_t once = policy_evict_first();
-    mbar_arrive_expect_tx(bar, kStageBytes);
-    tma_load_3d(dst, &tmK, 0, k0 & (S - 1), z, bar, once);
-    tma_load_3d(dst + kStep * D, &tmV, 0, k0 & (S - 1), z, bar, once);
-  };
-  const int32_t* table = a.block_table + (int64_t)b * a.max_blocks;
   if (lane == 0) {
     for (int t = 0; t < kStages; ++t) mbar_init(&s_full[warp][t], 1);
     fence_barrier_init();
-    for (int t = 0; t < kStages && t < steps; ++t) {
-      const int32_t id = table[key_of(t) >> S_log];
-      issue(t, id < a.cache.num_blocks ? id : -1);
-    }
   }
-  __syncwarp();
-
-  // ---- the part's block ids and scales
-  const int32_t b_lo = k_lo >> S_log;  // (a part may start inside a block of 128)
-  const int32_t nb = ((k_hi - 1) >> S_log) + 1 - b_lo;
-  for (int32_t i = tid; i < nb; i += blockDim.x) {
-    int32_t id = table[b_lo + i];
-    if (id < 0 || id >= a.cache.num_blocks) {
-      record_status(a.status, SSD_ERR_DEVICE_BOUNDS);
-      id = -1;
-    }
-    s_id[i] = id;
-    const int64_t at = (int64_t)id * a.cache.Hkv + g;
-    s_ks[i] = id < 0 ? 0.f : a.cache.k_scale[at];
-    s_vs[i] = id < 0 ? 0.f : a.cache.v_scale[at];
-  }
-
-  // Q as float16 with its row's power of two taken out; column order of K's reads.  A
-  // lane holds row 8 n + r8.
-  uint32_t qf[NR][KG][4][2];
-  float rowc_of[NR];
-  int32_t qpos_of[NR];
-  const float c2 = (a.scale != 0.f ? a.scale : rsqrtf((float)D)) * kLog2e;
-#pragma unroll
-  for (int n = 0; n < NR; ++n) {
-    const int32_t r = row0 + r8 + 8 * n;
-    const bool live = r < rows_total;
-    const int32_t j = live ? r / G : 0, h = g * G + (live ? r - j * G : 0);
-    const uint4* src = reinterpret_cast<const uint4*>(
-        static_cast<const __nv_bfloat16*>(a.q) + (((int64_t)b * a.D_max + j) * a.Hq + h) * D);
-    qpos_of[n] = 0x7fffffff;
-    if (live) {
-      qpos_of[n] = cache_flat_pos(a, b, cache, j);
-      if (qpos_of[n] < 0 && split == 0 && g == 0) record_status(a.status, SSD_ERR_DEVICE_BOUNDS);
-    }
-    float x[KG][16];
-    float m = 0.f;
-#pragma unroll
-    for (int kg = 0; kg < KG; ++kg)
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const uint4 w = live ? src[(q * KG + kg) * 2 + u] : make_uint4(0, 0, 0, 0);
-        const uint32_t v[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          x[kg][u * 8 + 2 * e] = __uint_as_float(v[e] << 16);
-          x[kg][u * 8 + 2 * e + 1] = __uint_as_float(v[e] & 0xffff0000u);
-          m = fmaxf(m, fmaxf(fabsf(x[kg][u * 8 + 2 * e]), fabsf(x[kg][u * 8 + 2 * e + 1])));
-        }
-      }
-    m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 1));
-    m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2));
-    // 2^e with m / 2^e in [1, 2) (or less, for the smallest; 4, for the largest)
-    const int32_t e = min(126, max(-126, (int32_t)(__float_as_uint(m) >> 23) - 127));
-    const float down = __uint_as_float((uint32_t)(127 - e) << 23);
-    rowc_of[n] = c2 * __uint_as_float((uint32_t)(127 + e) << 23);
-#pragma unroll
-    for (int kg = 0; kg < KG; ++kg)
-#pragma unroll
-      for (int s = 0; s < 4; ++s) {
-        qf[n][kg][s][0] = pack_f16x2(x[kg][4 * s] * down, x[kg][4 * s + 1] * down);
-        qf[n][kg][s][1] = pack_f16x2(x[kg][4 * s + 2] * down, x[kg][4 * s + 3] * down);
-      }
-  }
-  // keys below this one are visible to every row of the warp
-  int32_t mask_from;
-  {
-    int32_t minq = qpos_of[0];
-    if (NR == 2) minq = min(minq, qpos_of[NR - 1]);
-    mask_from = min(cache, min(0x7ffffffe, __reduce_min_sync(0xffffffffu, minq)) + 1);
-  }
-  // From here on a lane's rows are 8 n + 2 q + u: those of its scores and of O.
-  float rowc[NR][2];
-  int32_t qpos[NR][2];
-#pragma unroll
-  for (int n = 0; n < NR; ++n)
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      rowc[n][u] = __shfl_sync(0xffffffffu, rowc_of[n], (2 * q + u) * 4);
-      qpos[n][u] = __shfl_sync(0xffffffffu, qpos_of[n], (2 * q + u) * 4);
-    }
-  __syncthreads();  // ids and scales
-
-  // offsets of the lane's pieces in a stage (the swizzle: of 16-byte pieces, by the row)
-  uint32_t k_off[KG], v_off[2];
-#pragma unroll
-  for (int kg = 0; kg < KG; ++kg) {
-    const int32_t sw = D == 128 ? r8 : (r8 >> 1) & 3;
-    k_off[kg] = r8 * D + (((q * KG + kg) ^ sw) << 4);
-  }
-#pragma unroll
-  for (int u = 0; u < 2; ++u) {
-    const int32_t key = 2 * q + u;
-    v_off[u] = kStep * D + key * D + (D == 128 ? (r8 ^ key) << 4 : (((r8 >> 1) ^ q) << 4) + (r8 & 1) * 8);
-  }
-
-  float o[NR][NT][4];
-  float m_ref[NR][2], l[NR][2];
-#pragma unroll
-  for (int n = 0; n < NR; ++n) {
-#pragma unroll
-    for (int t = 0; t < NT; ++t) o[n][t][0] = o[n][t][1] = o[n][t][2] = o[n][t][3] = 0.f;
-    m_ref[n][0] = m_ref[n][1] = -INFINITY;
-    l[n][0] = l[n][1] = 0.f;
-  }
-  float v_ref = 0.f, v_inv = 0.f;
-  bool ok = true;
-  int32_t t = 0;
+  uint32_t stage = 0, phase = 0;  // of the warp's next step
+  CacheWork work;
+  bool more = work.first(a, L, blockIdx.x, first_of && tid < 32);
 #pragma unroll 1
-  for (; t < steps; ++t) {
-    ok = mbar_wait_warp(&s_full[warp][t % kStages], (t / kStages) & 1, a.status);
-    if (!ok) break;
-    const unsigned char* st = ring + (t % kStages) * kStageBytes;
-    uint4 kw[2][KG];
-    uint32_t v[4][VB / 4];
+  for (; more; more = work.next(a)) {
+    // (the rows of the part before have left the ring's place, and the copies may know it)
+    fence_proxy_async_shared();
+    __syncthreads();
+    const int32_t b = work.b;
+    const int32_t cache = a.cache_len[b], nd = a.n_drafts[b];
+    const int32_t Lk = cache + nd, rows_total = nd * G;
+    const int32_t row_g0 = blockIdx.z * row_warps * RW;
+    if (L.info != nullptr && first_of && tid == 0) {
+      if (work.t_lo == 0) L.info[b].x = blockIdx.x;
+      if (work.t_hi == work.tiles) L.info[b].y = blockIdx.x;
+    }
+    if (row_g0 >= rows_total) continue;
+    const bool whole = work.t_lo == 0 && work.t_hi == work.tiles, begins = work.t_lo == 0;
+    const int32_t k_lo = work.t_lo * kCacheTile, k_hi = min(Lk, work.t_hi * kCacheTile);
+    const int32_t start = a.key_start != nullptr ? min(Lk, max(0, a.key_start[b])) : 0;
+
+    // ---- this warp's rows and its share of the steps, and the copies of the first ones
+    const int32_t wk_n = kWarps / row_warps, wr = warp % row_warps, wk = warp / row_warps;
+    const int32_t q = lane & 3, r8 = lane >> 2;
+    const int32_t row0 = row_g0 + wr * RW;
+    const int32_t first = max(k_lo, start & ~(kStep - 1));  // multiple of 16
+    unsigned char* ring = smem + warp * kWarpBytes;
+    const int32_t n_steps =
+        row0 >= rows_total || first >= k_hi ? 0 : (k_hi - first + kStep - 1) / kStep;
+    const int32_t steps = n_steps > wk ? (n_steps - wk + wk_n - 1) / wk_n : 0;
+    auto key_of = [&](int32_t t) { return first + (t * wk_n + wk) * kStep; };
+    auto issue = [&](int32_t t, uint32_t to, int32_t id) {  // by one lane
+      const int32_t k0 = key_of(t), z = max(id, 0) * a.cache.Hkv + g;
+      unsigned char* dst = ring + to * kStageBytes;
+      uint64_t* bar = &s_full[warp][to];
+      const uint64_t once = policy_evict_first();
+      mbar_arrive_expect_tx(bar, kStageBytes);
+      tma_load_3d(dst, &tmK, 0, k0 & (S - 1), z, bar, once);
+      tma_load_3d(dst + kStep * D, &tmV, 0, k0 & (S - 1), z, bar, once);
+    };
+    const int32_t* table = a.block_table + (int64_t)b * a.max_blocks;
+    if (lane == 0) {
+      for (int t = 0; t < kStages && t < steps; ++t) {
+        const int32_t id = table[key_of(t) >> S_log];
+        issue(t, (stage + t) % kStages, id < a.cache.num_blocks ? id : -1);
+      }
+    }
+    __syncwarp();
+
+    // ---- the part's block ids and scales
+    const int32_t b_lo = k_lo >> S_log;  // (a part may start inside a block of 128)
+    const int32_t nb = ((k_hi - 1) >> S_log) + 1 - b_lo;
+    for (int32_t i = tid; i < nb; i += blockDim.x) {
+      int32_t id = table[b_lo + i];
+      if (id < 0 || id >= a.cache.num_blocks) {
+        record_status(a.status, SSD_ERR_DEVICE_BOUNDS);
+        id = -1;
+      }
+      s_id[i] = id;
+      const int64_t at = (int64_t)id * a.cache.Hkv + g;
+      s_ks[i] = id < 0 ? 0.f : a.cache.k_scale[at];
+      s_vs[i] = id < 0 ? 0.f : a.cache.v_scale[at];
+    }
+
+    // Q as float16 with its row's power of two taken out; column order of K's reads.  A
+    // lane holds row 8 n + r8.
+    uint32_t qf[NR][KG][4][2];
+    float rowc_of[NR];
+    int32_t qpos_of[NR];
+    const float c2 = (a.scale != 0.f ? a.scale : rsqrtf((float)D)) * kLog2e;
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+    for (int n = 0; n < NR; ++n) {
+      const int32_t r = row0 + r8 + 8 * n;
+      const bool live = r < rows_total;
+      const int32_t j = live ? r / G : 0, h = g * G + (live ? r - j * G : 0);
+      const uint4* src = reinterpret_cast<const uint4*>(
+          static_cast<const __nv_bfloat16*>(a.q) + (((int64_t)b * a.D_max + j) * a.Hq + h) * D);
+      qpos_of[n] = 0x7fffffff;
+      if (live) {
+        qpos_of[n] = cache_flat_pos(a, b, cache, j);
+        if (qpos_of[n] < 0 && begins && g == 0) record_status(a.status, SSD_ERR_DEVICE_BOUNDS);
+      }
+      float x[KG][16];
+      float m = 0.f;
 #pragma unroll
       for (int kg = 0; kg < KG; ++kg)
-        kw[h][kg] = *reinterpret_cast<const uint4*>(st + k_off[kg] + h * 8 * D);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const unsigned char* at = st + v_off[i & 1] + (i >> 1) * 8 * D;
-      if constexpr (VB == 16) {
-        const uint4 w = *reinterpret_cast<const uint4*>(at);
-        v[i][0] = w.x;
-        v[i][1] = w.y;
-        v[i][2] = w.z;
-        v[i][3] = w.w;
-      } else {
-        const uint2 w = *reinterpret_cast<const uint2*>(at);
-        v[i][0] = w.x;
-        v[i][1] = w.y;
-      }
-    }
-    const int32_t k0 = key_of(t), bi = (k0 >> S_log) - b_lo;
-    const float ks = s_ks[bi], vs = s_vs[bi];
-    __syncwarp();
-    if (lane == 0 && t + kStages < steps)
-      issue(t + kStages, s_id[(key_of(t + kStages) >> S_log) - b_lo]);
-
-    // ---- S^T = K Q^T
-    float x[NR][4];  // keys r8 and r8 + 8 (by 2) of the lane's rows
-    {
-      float sc[KG][NR][4];
+        for (int u = 0; u < 2; ++u) {
+          const uint4 w = live ? src[(q * KG + kg) * 2 + u] : make_uint4(0, 0, 0, 0);
+          const uint32_t v[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-      for (int kg = 0; kg < KG; ++kg) {
+          for (int e = 0; e < 4; ++e) {
+            x[kg][u * 8 + 2 * e] = __uint_as_float(v[e] << 16);
+            x[kg][u * 8 + 2 * e + 1] = __uint_as_float(v[e] & 0xffff0000u);
+            m = fmaxf(m, fmaxf(fabsf(x[kg][u * 8 + 2 * e]), fabsf(x[kg][u * 8 + 2 * e + 1])));
+          }
+        }
+      m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 1));
+      m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2));
+      // 2^e with m / 2^e in [1, 2) (or less, for the smallest; 4, for the largest)
+      const int32_t e = min(126, max(-126, (int32_t)(__float_as_uint(m) >> 23) - 127));
+      const float down = __uint_as_float((uint32_t)(127 - e) << 23);
+      rowc_of[n] = c2 * __uint_as_float((uint32_t)(127 + e) << 23);
 #pragma unroll
-        for (int n = 0; n < NR; ++n) sc[kg][n][0] = sc[kg][n][1] = sc[kg][n][2] = sc[kg][n][3] = 0.f;
+      for (int kg = 0; kg < KG; ++kg)
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
-          const uint32_t w0 = s == 0 ? kw[0][kg].x : s == 1 ? kw[0][kg].y : s == 2 ? kw[0][kg].z : kw[0][kg].w;
-          const uint32_t w1 = s == 0 ? kw[1][kg].x : s == 1 ? kw[1][kg].y : s == 2 ? kw[1][kg].z : kw[1][kg].w;
-          const uint32_t kf[4] = {f16_lo(w0), f16_lo(w1), f16_hi(w0), f16_hi(w1)};
+          qf[n][kg][s][0] = pack_f16x2(x[kg][4 * s] * down, x[kg][4 * s + 1] * down);
+          qf[n][kg][s][1] = pack_f16x2(x[kg][4 * s + 2] * down, x[kg][4 * s + 3] * down);
+        }
+    }
+    // keys below this one are visible to every row of the warp
+    int32_t mask_from;
+    {
+      int32_t minq = qpos_of[0];
+      if (NR == 2) minq = min(minq, qpos_of[NR - 1]);
+      mask_from = min(cache, min(0x7ffffffe, __reduce_min_sync(0xffffffffu, minq)) + 1);
+    }
+    // From here on a lane's rows are 8 n + 2 q + u: those of its scores and of O.
+    float rowc[NR][2];
+    int32_t qpos[NR][2];
 #pragma unroll
-          for (int n = 0; n < NR; ++n) mma_f16(sc[kg][n], kf, qf[n][kg][s][0], qf[n][kg][s][1]);
+    for (int n = 0; n < NR; ++n)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        rowc[n][u] = __shfl_sync(0xffffffffu, rowc_of[n], (2 * q + u) * 4);
+        qpos[n][u] = __shfl_sync(0xffffffffu, qpos_of[n], (2 * q + u) * 4);
+      }
+    __syncthreads();  // ids and scales
+
+    // offsets of the lane's pieces in a stage (the swizzle: of 16-byte pieces, by the row)
+    uint32_t k_off[KG], v_off[2];
+#pragma unroll
+    for (int kg = 0; kg < KG; ++kg) {
+      const int32_t sw = D == 128 ? r8 : (r8 >> 1) & 3;
+      k_off[kg] = r8 * D + (((q * KG + kg) ^ sw) << 4);
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int32_t key = 2 * q + u;
+      v_off[u] = kStep * D + key * D + (D == 128 ? (r8 ^ key) << 4 : (((r8 >> 1) ^ q) << 4) + (r8 & 1) * 8);
+    }
+
+    float o[NR][NT][4];
+    float m_ref[NR][2], l[NR][2];
+#pragma unroll
+    for (int n = 0; n < NR; ++n) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t) o[n][t][0] = o[n][t][1] = o[n][t][2] = o[n][t][3] = 0.f;
+      m_ref[n][0] = m_ref[n][1] = -INFINITY;
+      l[n][0] = l[n][1] = 0.f;
+    }
+    float v_ref = 0.f, v_inv = 0.f;
+    bool ok = true;
+    int32_t t = 0;
+#pragma unroll 1
+    for (; t < steps; ++t) {
+      ok = mbar_wait_warp(&s_full[warp][stage], phase, a.status);
+      if (!ok) break;
+      const unsigned char* st = ring + stage * kStageBytes;
+      uint4 kw[2][KG];
+      uint32_t v[4][VB / 4];
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int kg = 0; kg < KG; ++kg)
+          kw[h][kg] = *reinterpret_cast<const uint4*>(st + k_off[kg] + h * 8 * D);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const unsigned char* at = st + v_off[i & 1] + (i >> 1) * 8 * D;
+        if constexpr (VB == 16) {
+          const uint4 w = *reinterpret_cast<const uint4*>(at);
+          v[i][0] = w.x;
+          v[i][1] = w.y;
+          v[i][2] = w.z;
+          v[i][3] = w.w;
+        } else {
+          const uint2 w = *reinterpret_cast<const uint2*>(at);
+          v[i][0] = w.x;
+          v[i][1] = w.y;
         }
       }
+      const int32_t k0 = key_of(t), bi = (k0 >> S_log) - b_lo;
+      const float ks = s_ks[bi], vs = s_vs[bi];
+      __syncwarp();
+      if (lane == 0 && t + kStages < steps)
+        issue(t + kStages, stage, s_id[(key_of(t + kStages) >> S_log) - b_lo]);
+      stage = (stage + 1) % kStages;
+      phase ^= stage == 0 ? 1u : 0u;
+
+      // ---- S^T = K Q^T
+      float x[NR][4];  // keys r8 and r8 + 8 (by 2) of the lane's rows
+      {
+        float sc[KG][NR][4];
 #pragma unroll
-      for (int n = 0; n < NR; ++n)
+        for (int kg = 0; kg < KG; ++kg) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          x[n][e] = (KG == 2 ? sc[0][n][e] + sc[KG - 1][n][e] : sc[0][n][e]) * (rowc[n][e & 1] * ks);
-    }
-    if (k0 < start || k0 + kStep > min(mask_from, k_hi) || s_id[bi] < 0) {
-      const bool in_pool = s_id[bi] >= 0;
+          for (int n = 0; n < NR; ++n) sc[kg][n][0] = sc[kg][n][1] = sc[kg][n][2] = sc[kg][n][3] = 0.f;
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int32_t key = k0 + r8 + 8 * h;
-        int32_t kp = 0x7fffffff;
-        if (key >= start && key < k_hi && in_pool) {
-          kp = key;
-          if (key >= cache) {
-            kp = cache_flat_pos(a, b, cache, key - cache);
-            if (kp < 0) kp = 0x7fffffff;
+          for (int s = 0; s < 4; ++s) {
+            const uint32_t w0 = s == 0 ? kw[0][kg].x : s == 1 ? kw[0][kg].y : s == 2 ? kw[0][kg].z : kw[0][kg].w;
+            const uint32_t w1 = s == 0 ? kw[1][kg].x : s == 1 ? kw[1][kg].y : s == 2 ? kw[1][kg].z : kw[1][kg].w;
+            const uint32_t kf[4] = {f16_lo(w0), f16_lo(w1), f16_hi(w0), f16_hi(w1)};
+#pragma unroll
+            for (int n = 0; n < NR; ++n) mma_f16(sc[kg][n], kf, qf[n][kg][s][0], qf[n][kg][s][1]);
           }
         }
 #pragma unroll
         for (int n = 0; n < NR; ++n)
 #pragma unroll
-          for (int u = 0; u < 2; ++u)
-            if (kp > qpos[n][u] || kp == 0x7fffffff) x[n][2 * h + u] = -INFINITY;
+          for (int e = 0; e < 4; ++e)
+            x[n][e] = (KG == 2 ? sc[0][n][e] + sc[KG - 1][n][e] : sc[0][n][e]) * (rowc[n][e & 1] * ks);
       }
-      // what lies in no key's place may be anything
+      if (k0 < start || k0 + kStep > min(mask_from, k_hi) || s_id[bi] < 0) {
+        const bool in_pool = s_id[bi] >= 0;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int32_t key = k0 + 2 * q + (i & 1) + 8 * (i >> 1);
-        if (!(key >= start && key < k_hi && in_pool)) {
+        for (int h = 0; h < 2; ++h) {
+          const int32_t key = k0 + r8 + 8 * h;
+          int32_t kp = 0x7fffffff;
+          if (key >= start && key < k_hi && in_pool) {
+            kp = key;
+            if (key >= cache) {
+              kp = cache_flat_pos(a, b, cache, key - cache);
+              if (kp < 0) kp = 0x7fffffff;
+            }
+          }
 #pragma unroll
-          for (int w = 0; w < VB / 4; ++w) v[i][w] = 0;
+          for (int n = 0; n < NR; ++n)
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+              if (kp > qpos[n][u] || kp == 0x7fffffff) x[n][2 * h + u] = -INFINITY;
+        }
+        // what lies in no key's place may be anything
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int32_t key = k0 + 2 * q + (i & 1) + 8 * (i >> 1);
+          if (!(key >= start && key < k_hi && in_pool)) {
+#pragma unroll
+            for (int w = 0; w < VB / 4; ++w) v[i][w] = 0;
+          }
         }
       }
-    }
-    // ---- softmax against a reference maximum that moves when it falls behind
-    bool behind = !(vs <= v_ref * kVGrowth);  // the same in every lane
+      // ---- softmax against a reference maximum that moves when it falls behind
+      bool behind = !(vs <= v_ref * kVGrowth);  // the same in every lane
 #pragma unroll
-    for (int n = 0; n < NR; ++n)
+      for (int n = 0; n < NR; ++n)
 #pragma unroll
-      for (int u = 0; u < 2; ++u) behind |= fmaxf(x[n][u], x[n][2 + u]) > m_ref[n][u] + kGrowth;
-    if (__any_sync(0xffffffffu, behind)) {
-      float f = 1.f;
-      if (!(vs <= v_ref * kVGrowth)) {
-        const float to = fmaxf(vs, 0x1p-120f);
-        f = v_ref / to;
-        v_ref = to;
-        v_inv = 1.f / to;
+        for (int u = 0; u < 2; ++u) behind |= fmaxf(x[n][u], x[n][2 + u]) > m_ref[n][u] + kGrowth;
+      if (__any_sync(0xffffffffu, behind)) {
+        float f = 1.f;
+        if (!(vs <= v_ref * kVGrowth)) {
+          const float to = fmaxf(vs, 0x1p-120f);
+          f = v_ref / to;
+          v_ref = to;
+          v_inv = 1.f / to;
+        }
+#pragma unroll
+        for (int n = 0; n < NR; ++n) {
+          float al[2];
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            float m = fmaxf(x[n][u], x[n][2 + u]);
+#pragma unroll
+            for (int s = 4; s < 32; s <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, s));
+            m = fmaxf(m_ref[n][u], m);
+            al[u] = m == -INFINITY ? 1.f : exp2f(m_ref[n][u] - m);
+            m_ref[n][u] = m;
+            l[n][u] *= al[u];
+            al[u] *= f;
+          }
+#pragma unroll
+          for (int c = 0; c < NT; ++c) {
+            o[n][c][0] *= al[0];
+            o[n][c][1] *= al[1];
+            o[n][c][2] *= al[0];
+            o[n][c][3] *= al[1];
+          }
+        }
       }
+      const float ratio = vs * v_inv;
+      uint32_t pf[NR][2];
 #pragma unroll
       for (int n = 0; n < NR; ++n) {
-        float al[2];
+        const float m0 = m_ref[n][0] == -INFINITY ? 0.f : m_ref[n][0];
+        const float m1 = m_ref[n][1] == -INFINITY ? 0.f : m_ref[n][1];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const float p0 = ex2_approx(x[n][2 * h] - m0), p1 = ex2_approx(x[n][2 * h + 1] - m1);
+          l[n][0] += p0;
+          l[n][1] += p1;
+          pf[n][h] = transpose8x8(pack_f16x2(p0 * ratio, p1 * ratio));
+        }
+      }
+      // ---- O^T += V^T P^T: output tile c holds columns r8 * VB + 2 c and the next
+#pragma unroll
+      for (int w = 0; w < VB / 4; ++w)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const uint32_t sel = h == 0 ? 0x5140u : 0x7362u;
+          const uint32_t x0 = __byte_perm(v[0][w], v[1][w], sel);
+          const uint32_t x1 = __byte_perm(v[2][w], v[3][w], sel);
+          const uint32_t vf[4] = {f16_lo(x0), f16_hi(x0), f16_lo(x1), f16_hi(x1)};
+#pragma unroll
+          for (int n = 0; n < NR; ++n) mma_f16(o[n][2 * w + h], vf, pf[n][0], pf[n][1]);
+        }
+    }
+    if (!ok)  // the copies still in flight land before the CTA is let go
+      for (int i = 0; i < kStages && t < steps; ++i, ++t) {
+        mbar_drain(&s_full[warp][stage], phase);
+        stage = (stage + 1) % kStages;
+        phase ^= stage == 0 ? 1u : 0u;
+      }
+    __syncwarp();
+
+    // ---- every warp's rows to its ring's place, then the rows (or the part's share of
+    // them), each by a warp that merges what the warps of its rows hold
+    {
+      float* mine = reinterpret_cast<float*>(ring);
+#pragma unroll
+      for (int n = 0; n < NR; ++n)
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-          float m = fmaxf(x[n][u], x[n][2 + u]);
+          const int32_t r = 8 * n + 2 * q + u;
 #pragma unroll
-          for (int s = 4; s < 32; s <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, s));
-          m = fmaxf(m_ref[n][u], m);
-          al[u] = m == -INFINITY ? 1.f : exp2f(m_ref[n][u] - m);
-          m_ref[n][u] = m;
-          l[n][u] *= al[u];
-          al[u] *= f;
+          for (int s = 4; s < 32; s <<= 1) l[n][u] += __shfl_xor_sync(0xffffffffu, l[n][u], s);
+#pragma unroll
+          for (int c = 0; c < NT; c += 2)
+            *reinterpret_cast<float4*>(mine + r * kRowFloats + r8 * VB + 2 * c) =
+                make_float4(o[n][c][u] * v_ref, o[n][c][2 + u] * v_ref, o[n][c + 1][u] * v_ref,
+                            o[n][c + 1][2 + u] * v_ref);
+          if (r8 == 0) s_ml[warp][r] = make_float2(m_ref[n][u], l[n][u]);
         }
-#pragma unroll
-        for (int c = 0; c < NT; ++c) {
-          o[n][c][0] *= al[0];
-          o[n][c][1] *= al[1];
-          o[n][c][2] *= al[0];
-          o[n][c][3] *= al[1];
-        }
-      }
     }
-    const float ratio = vs * v_inv;
-    uint32_t pf[NR][2];
+    if (__syncthreads_or(!ok)) return;
+    constexpr int PER = D / 32;
+    for (int32_t rr = warp; rr < row_warps * RW && row_g0 + rr < rows_total; rr += kWarps) {
+      const int32_t w0 = rr / RW, r = rr - w0 * RW;
+      float M = -INFINITY;
+      for (int32_t w = w0; w < kWarps; w += row_warps) M = fmaxf(M, s_ml[w][r].x);
+      float sum = 0.f, acc[PER];
 #pragma unroll
-    for (int n = 0; n < NR; ++n) {
-      const float m0 = m_ref[n][0] == -INFINITY ? 0.f : m_ref[n][0];
-      const float m1 = m_ref[n][1] == -INFINITY ? 0.f : m_ref[n][1];
+      for (int k = 0; k < PER; ++k) acc[k] = 0.f;
+      for (int32_t w = w0; w < kWarps; w += row_warps) {
+        const float2 ml = s_ml[w][r];
+        const float f = ml.x == -INFINITY ? 0.f : exp2f(ml.x - M);
+        sum += ml.y * f;
+        const float* po =
+            reinterpret_cast<const float*>(smem + w * kWarpBytes) + r * kRowFloats + lane * PER;
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const float p0 = ex2_approx(x[n][2 * h] - m0), p1 = ex2_approx(x[n][2 * h + 1] - m1);
-        l[n][0] += p0;
-        l[n][1] += p1;
-        pf[n][h] = transpose8x8(pack_f16x2(p0 * ratio, p1 * ratio));
+        for (int k = 0; k < PER; ++k) acc[k] += po[k] * f;
       }
-    }
-    // ---- O^T += V^T P^T: output tile c holds columns r8 * VB + 2 c and the next
+      const int32_t row = row_g0 + rr, j = row / G, h = g * G + (row - j * G);
+      if (whole) {
+        const int64_t at = ((int64_t)b * a.D_max + j) * a.Hq + h;
+        if (!dbg_in(at, (int64_t)a.B * a.D_max * a.Hq, a.status)) continue;
+        const float inv = sum > 0.f ? 1.f / sum : 0.f;
+        uint32_t* ob = reinterpret_cast<uint32_t*>(static_cast<__nv_bfloat16*>(a.o) + at * D + lane * PER);
 #pragma unroll
-    for (int w = 0; w < VB / 4; ++w)
+        for (int k = 0; k < PER; k += 2) ob[k / 2] = pack_bf16x2(acc[k] * inv, acc[k + 1] * inv);
+        if (a.lse != nullptr && lane == 0)
+          a.lse[((int64_t)b * a.Hq + h) * a.D_max + j] =
+              sum > 0.f ? (M + log2f(sum)) * kLn2 : -INFINITY;
+      } else {
+        // (a CTA leaves a share of several sequences, but of neighbours: slot x + b)
+        const int64_t slots = L.per_head + a.B;
+        const int64_t at = (((int64_t)g * L.row_groups + blockIdx.z) * slots + blockIdx.x + b) * L.group_rows + rr;
+        if (!dbg_in(at, (int64_t)a.cache.Hkv * L.row_groups * slots * L.group_rows, a.status)) continue;
+        float* po = L.part_o + at * D + lane * PER;
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const uint32_t sel = h == 0 ? 0x5140u : 0x7362u;
-        const uint32_t x0 = __byte_perm(v[0][w], v[1][w], sel);
-        const uint32_t x1 = __byte_perm(v[2][w], v[3][w], sel);
-        const uint32_t vf[4] = {f16_lo(x0), f16_hi(x0), f16_lo(x1), f16_hi(x1)};
-#pragma unroll
-        for (int n = 0; n < NR; ++n) mma_f16(o[n][2 * w + h], vf, pf[n][0], pf[n][1]);
+        for (int k = 0; k < PER; ++k) po[k] = acc[k];
+        if (lane == 0) L.part_ml[at] = make_float2(M, sum);
       }
-  }
-  if (!ok)  // the copies still in flight land before the CTA is let go
-    for (; t < steps; ++t) mbar_drain(&s_full[warp][t % kStages], (t / kStages) & 1);
-  __syncwarp();
-
-  // ---- every warp's rows to its ring's place, then the rows (or the part's share of
-  // them), each by a warp that merges what the warps of its rows hold
-  {
-    float* mine = reinterpret_cast<float*>(ring);
-#pragma unroll
-    for (int n = 0; n < NR; ++n)
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const int32_t r = 8 * n + 2 * q + u;
-#pragma unroll
-        for (int s = 4; s < 32; s <<= 1) l[n][u] += __shfl_xor_sync(0xffffffffu, l[n][u], s);
-#pragma unroll
-        for (int c = 0; c < NT; c += 2)
-          *reinterpret_cast<float4*>(mine + r * kRowFloats + r8 * VB + 2 * c) =
-              make_float4(o[n][c][u] * v_ref, o[n][c][2 + u] * v_ref, o[n][c + 1][u] * v_ref,
-                          o[n][c + 1][2 + u] * v_ref);
-        if (r8 == 0) s_ml[warp][r] = make_float2(m_ref[n][u], l[n][u]);
-      }
-  }
-  if (__syncthreads_or(!ok)) return;
-  constexpr int PER = D / 32;
-  const bool direct = parts == 1;
-  for (int32_t rr = warp; rr < row_warps * RW && row_g0 + rr < rows_total; rr += kWarps) {
-    const int32_t w0 = rr / RW, r = rr - w0 * RW;
-    float M = -INFINITY;
-    for (int32_t w = w0; w < kWarps; w += row_warps) M = fmaxf(M, s_ml[w][r].x);
-    float sum = 0.f, acc[PER];
-#pragma unroll
-    for (int k = 0; k < PER; ++k) acc[k] = 0.f;
-    for (int32_t w = w0; w < kWarps; w += row_warps) {
-      const float2 ml = s_ml[w][r];
-      const float f = ml.x == -INFINITY ? 0.f : exp2f(ml.x - M);
-      sum += ml.y * f;
-      const float* po =
-          reinterpret_cast<const float*>(smem + w * kWarpBytes) + r * kRowFloats + lane * PER;
-#pragma unroll
-      for (int k = 0; k < PER; ++k) acc[k] += po[k] * f;
-    }
-    const int32_t row = row_g0 + rr, j = row / G, h = g * G + (row - j * G);
-    if (direct) {
-      const int64_t at = ((int64_t)b * a.D_max + j) * a.Hq + h;
-      if (!dbg_in(at, (int64_t)a.B * a.D_max * a.Hq, a.status)) continue;
-      const float inv = sum > 0.f ? 1.f / sum : 0.f;
-      uint32_t* ob = reinterpret_cast<uint32_t*>(static_cast<__nv_bfloat16*>(a.o) + at * D + lane * PER);
-#pragma unroll
-      for (int k = 0; k < PER; k += 2) ob[k / 2] = pack_bf16x2(acc[k] * inv, acc[k + 1] * inv);
-      if (a.lse != nullptr && lane == 0)
-        a.lse[((int64_t)b * a.Hq + h) * a.D_max + j] =
-            sum > 0.f ? (M + log2f(sum)) * kLn2 : -INFINITY;
-    } else {
-      const int64_t at =
-          (((int64_t)g * L.row_groups + blockIdx.z) * L.per_head + blockIdx.x) * L.group_rows + rr;
-      if (!dbg_in(at, (int64_t)a.cache.Hkv * L.row_groups * L.per_head * L.group_rows, a.status)) continue;
-      float* po = L.part_o + at * D + lane * PER;
-#pragma unroll
-      for (int k = 0; k < PER; ++k) po[k] = acc[k];
-      if (lane == 0) L.part_ml[at] = make_float2(M, sum);
     }
   }
 }
@@ -518,10 +534,11 @@ __global__ void __launch_bounds__(256) cache_attn_combine_kernel(CacheAttnArgs a
     const int2 x = L.info[b];
     const int32_t G = a.Hq / a.cache.Hkv, g = h / G, r = j * G + (h - g * G);
     const int32_t z = r / L.group_rows;
-    parts = x.y;
+    const int64_t slots = L.per_head + a.B;
+    parts = x.y - x.x + 1;
     step = L.group_rows;
-    at = (((int64_t)g * L.row_groups + z) * L.per_head + x.x) * step + (r - z * L.group_rows);
-    room = (int64_t)a.cache.Hkv * L.row_groups * L.per_head * step;
+    at = (((int64_t)g * L.row_groups + z) * slots + x.x + b) * step + (r - z * L.group_rows);
+    room = (int64_t)a.cache.Hkv * L.row_groups * slots * step;
   } else {
     parts = cache_parts(L.splits, L.min_tiles, (cache + nd + kCacheTile - 1) / kCacheTile);
     at = row * L.splits;
@@ -600,7 +617,7 @@ int64_t tc_part_rows(int32_t B, int32_t Hq, int32_t D_max, int32_t splits) {
   return splits == 1 ? 0 : (int64_t)B * D_max * Hq * splits;
 }
 int64_t mma_part_rows(int32_t B, int32_t Hkv, const Plan& p) {
-  return p.cut(B) ? (int64_t)Hkv * p.row_groups * p.per_head * p.group_rows() : 0;
+  return p.cut(B) ? (int64_t)Hkv * p.row_groups * (p.per_head + B) * p.group_rows() : 0;
 }
 
 }  // namespace
@@ -636,7 +653,7 @@ cudaError_t launch_cache_attention(const CacheAttnArgs& a, void* ws, cudaStream_
     L.row_groups = p.row_groups;
     L.group_rows = p.group_rows();
     rows = mma_part_rows(a.B, a.cache.Hkv, p);
-    part_tiles = std::min(tiles, kWorkTiles);
+    part_tiles = std::min(tiles, kWorkRoom);
   }
   L.max_blocks = part_tiles * (kCacheTile / std::min(a.cache.block, 64)) + 1;
   if (rows > 0) {

@@ -13,19 +13,20 @@ constexpr int kCacheTile = 64;  // keys: parts of a sequence are whole tiles
 // kernel, else the attention writes the rows itself.  The tensor-core kernel cuts
 // a sequence of `tiles` tiles into parts of about equal length, at most `splits`,
 // none shorter than min_tiles (but the only one); part p holds tiles
-// [tiles * p / n, tiles * (p + 1) / n).  The other one gives the CTAs of a KV head
-// (per_head of them) to the sequences by their lengths: cache_work().
+// [tiles * p / n, tiles * (p + 1) / n).  The other one deals all sequences' tiles to the
+// CTAs of a KV head: CacheWork.
 struct CacheAttnLaunch {
   int32_t splits, min_tiles;
   int32_t max_blocks;  // most blocks of a part (room for their ids and scales)
-  float* part_o;       // [B][D_max][Hq][splits][d]; or [Hkv][row groups][per_head][rows][d]
+  float* part_o;       // [B][D_max][Hq][splits][d]; or [Hkv][row groups][per_head + B][rows][d]
   float2* part_ml;     // the same without d: reference maximum (log2) and sum
-  // cache_work()
+  // CacheWork
   int32_t per_head, goal, uniform, row_groups, group_rows;
-  int2* info;          // [B]: first CTA and parts of a sequence
+  int2* info;          // [B]: first and last CTA of a sequence
 };
 
-constexpr int kWorkTiles = 128;  // most tiles of a part of cache_work()
+constexpr int kWorkTiles = 128;  // a CTA's most tiles of one sequence, about (kWorkRoom: at most)
+constexpr int kWorkRoom = kWorkTiles + 8;
 
 __host__ __device__ __forceinline__ int32_t cache_parts(int32_t splits, int32_t min_tiles,
                                                         int32_t tiles) {
@@ -53,87 +54,165 @@ __device__ __forceinline__ bool cache_lengths_ok(const CacheAttnArgs& a, int32_t
   return cache >= 0 && nd >= 0 && nd <= a.D_max && cache <= a.max_blocks * a.cache.block - nd;
 }
 
-// What CTA x of a KV head's per_head works on: part `split` of `parts` of sequence b
-// (b < 0: nothing).  Called by converged warps; every lane gets the same answer.
-// uniform > 0: as many CTAs for every sequence.  Else a sequence gets one for every
-// `chunk` tiles, with the least chunk for which `goal` of them (those that run at
-// once) suffice, so lengths that differ leave no CTA with more than `chunk` tiles.
+// What CTA x of a KV head's per_head works on: parts of sequences, one after the other.
+//  - The sequences alone fill the GPU (uniform > 0): as many CTAs for every sequence.
+//  - Else a sequence gets a CTA for every `chunk` tiles, with the least chunk for which `goal`
+//    CTAs (those that run at once) suffice, so lengths that differ leave no CTA with more than
+//    `chunk` tiles.
+//  - Where that is more than kEvenTiles tiles above an even share (8 sequences for 14 CTAs),
+//    the tiles of all sequences, in one line, are cut evenly, and a CTA may work on the end of
+//    one sequence and the beginning of the next.  A cut that would leave a sliver of a sequence
+//    moves to the sequence's end.  8 sequences of 8000 keys, 32 heads: 108 -> 92 us; with 16
+//    sequences of 2000 keys for 57 CTAs, a tile or two from even, the second part's
+//    set-up costs more than it gives (20 -> 22 us).
+// Called by converged warps; every lane holds the same.
+constexpr int kEvenTiles = 8;
 struct CacheWork {
-  int32_t b, split, parts;
-};
-// report: the launch's first CTA of a sequence, which records bad lengths.
-__device__ __forceinline__ CacheWork cache_work(const CacheAttnArgs& a, const CacheAttnLaunch& L,
-                                                int32_t x, bool report) {
-  const int32_t lane = threadIdx.x & 31;
-  constexpr uint32_t kAll = 0xffffffffu;
-  auto tiles_of = [&](int32_t b) -> int32_t {
+  int32_t b, t_lo, t_hi, tiles;  // the part: tiles t_lo .. t_hi - 1 of the tiles of sequence b
+  // the line: the CTA's tiles left, and where sequence b begins
+  int64_t at, end, start;
+
+  // Tiles of a sequence; report: bad lengths are recorded.
+  static __device__ __forceinline__ int32_t tiles_of(const CacheAttnArgs& a, int32_t b, bool report) {
     const int32_t c = a.cache_len[b], n = a.n_drafts[b];
     if (!cache_lengths_ok(a, c, n)) {
       if (report) record_status(a.status, SSD_ERR_DEVICE_BOUNDS);
       return 0;
     }
     return n == 0 ? 0 : (c + n + kCacheTile - 1) / kCacheTile;
-  };
-  auto parts_of = [&](int32_t tiles, int32_t chunk) {
-    return min((tiles + chunk - 1) / chunk, tiles == 0 ? 0 : max(1, tiles / L.min_tiles));
-  };
-  if (L.uniform > 0) {
-    const int32_t b = x / L.uniform, split = x - b * L.uniform;
-    report = report && split == 0;
-    const int32_t parts = L.uniform == 1 ? 1 : parts_of(tiles_of(b), kWorkTiles);
-    if (L.uniform == 1) report = report && tiles_of(b) >= 0;
-    if (report && L.info != nullptr && lane == 0) L.info[b] = make_int2(b * L.uniform, parts);
-    return CacheWork{split < parts ? b : -1, split, parts};
   }
-  report = report && x == 0;
-  const int32_t mine = lane < a.B ? tiles_of(lane) : 0;  // (what a batch of up to 32 needs)
-  int64_t total = mine;
-  int32_t most = mine;
-  for (int32_t b = lane + 32; b < a.B; b += 32) {
-    const int32_t t = tiles_of(b);
-    total += t;
-    most = max(most, t);
-  }
+
+  // The sequence that holds tile x of the line, from sequence b0 = a multiple of 32 on, which
+  // begins at `begin`: false if none.
+  __device__ __noinline__ bool find(const CacheAttnArgs& a, int64_t x) {
+    const int32_t lane = threadIdx.x & 31;
+    int64_t before = 0;
+    for (int32_t b0 = 0; b0 < a.B; b0 += 32) {
+      const int32_t n = b0 + lane < a.B ? tiles_of(a, b0 + lane, false) : 0;
+      int64_t upto = n;
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(kAll, total, o);
-  most = __reduce_max_sync(kAll, most);
-  report = false;
-  // (lo - 1 is too few, hi enough; a part longer than kWorkTiles has no room)
-  int32_t hi = (int32_t)min((int64_t)min(most, kWorkTiles), total / (L.goal - a.B) + 1);
-  int32_t lo = max(1, (int32_t)min((int64_t)hi, (total + L.goal - 1) / L.goal));
-  while (lo < hi) {
-    const int32_t chunk = (lo + hi) >> 1;
-    int32_t n = parts_of(mine, chunk);
-    for (int32_t b = lane + 32; b < a.B; b += 32) n += parts_of(tiles_of(b), chunk);
-    if (__reduce_add_sync(kAll, n) <= L.goal) hi = chunk;
-    else lo = chunk + 1;
+      for (int o = 1; o < 32; o <<= 1) {
+        const int64_t y = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += y;
+      }
+      upto += before;
+      const uint32_t here = __ballot_sync(0xffffffffu, x < upto);
+      if (here != 0) {
+        const int32_t src = __ffs(here) - 1;
+        b = b0 + src;
+        tiles = __shfl_sync(0xffffffffu, n, src);
+        start = __shfl_sync(0xffffffffu, upto, src) - tiles;
+        return true;
+      }
+      before = __shfl_sync(0xffffffffu, upto, 31);
+    }
+    return false;
   }
-  const int32_t chunk = max(1, hi);
-  CacheWork w{-1, 0, 0};
-  int32_t before = 0;
-  for (int32_t b0 = 0; b0 < a.B; b0 += 32) {
-    const int32_t b = b0 + lane;
-    const int32_t n = b >= a.B ? 0 : parts_of(b0 == 0 ? mine : tiles_of(b), chunk);
-    int32_t end = n;
+  // The cut at tile x, and with it the sequence it lies in.
+  __device__ __forceinline__ int64_t cut(const CacheAttnArgs& a, int64_t x, int32_t sliver) {
+    if (!find(a, x)) return x;
+    if (x - start <= sliver) return start;
+    return start + tiles - x <= sliver ? start + tiles : x;
+  }
+  // The CTA's first part; false: none.  report: the launch's first CTAs, which record bad
+  // lengths.
+  __device__ __forceinline__ bool first(const CacheAttnArgs& a, const CacheAttnLaunch& L, int32_t x,
+                                        bool report) {
+    if (L.uniform > 0) {
+      b = x / L.uniform;
+      const int32_t split = x - b * L.uniform;
+      tiles = tiles_of(a, b, report && split == 0);
+      const int32_t parts = (tiles + kWorkTiles - 1) / kWorkTiles;
+      if (split >= parts) return false;
+      t_lo = 0;
+      t_hi = tiles;
+      if (parts > 1) {
+        t_lo = (int32_t)((int64_t)tiles * split / parts);
+        t_hi = (int32_t)((int64_t)tiles * (split + 1) / parts);
+      }
+      at = end = start = 0;
+      return true;
+    }
+    const int32_t lane = threadIdx.x & 31;
+    // (the first 32 lengths stay in a register)
+    const int32_t mine = lane < a.B ? tiles_of(a, lane, report && x == 0) : 0;
+    int64_t total = mine;
+    int32_t most = mine;
+    for (int32_t i = lane + 32; i < a.B; i += 32) {
+      const int32_t t = tiles_of(a, i, report && x == 0);
+      total += t;
+      most = max(most, t);
+    }
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int32_t y = __shfl_up_sync(kAll, end, o);
-      if (lane >= o) end += y;
+    for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+    // the chunk: lo - 1 is too small, hi enough (or as long as a part may be)
+    most = __reduce_max_sync(0xffffffffu, most);
+    auto parts_of = [&](int32_t t, int32_t chunk) {
+      return min((t + chunk - 1) / chunk, t == 0 ? 0 : max(1, t / L.min_tiles));
+    };
+    int32_t hi = (int32_t)min((int64_t)min(most, kWorkTiles), total / (L.goal - a.B) + 1);
+    int32_t lo = max(1, (int32_t)min((int64_t)hi, (total + L.goal - 1) / L.goal));
+    while (lo < hi) {
+      const int32_t chunk = (lo + hi) >> 1;
+      int32_t n = parts_of(mine, chunk);
+      for (int32_t i = lane + 32; i < a.B; i += 32) n += parts_of(tiles_of(a, i, false), chunk);
+      if (__reduce_add_sync(0xffffffffu, n) <= L.goal) hi = chunk;
+      else lo = chunk + 1;
     }
-    end += before;
-    if (L.info != nullptr && x == 0 && blockIdx.y == 0 && blockIdx.z == 0 && threadIdx.x < 32 && b < a.B)
-      L.info[b] = make_int2(end - n, n);
-    const uint32_t here = __ballot_sync(kAll, x >= end - n && x < end);
-    if (here != 0) {
-      const int32_t src = __ffs(here) - 1;
-      w = CacheWork{b0 + src, x - __shfl_sync(kAll, end - n, src), __shfl_sync(kAll, n, src)};
-      if (x > 0) break;  // (CTA 0 writes every sequence's info)
+    if (total == 0) return false;
+    if (hi <= total / L.goal + kEvenTiles) {
+      int32_t before = 0;
+      for (int32_t b0 = 0; b0 < a.B; b0 += 32) {
+        const int32_t t = b0 == 0 ? mine : b0 + lane < a.B ? tiles_of(a, b0 + lane, false) : 0;
+        const int32_t n = parts_of(t, hi);
+        int32_t upto = n;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const int32_t y = __shfl_up_sync(0xffffffffu, upto, o);
+          if (lane >= o) upto += y;
+        }
+        upto += before;
+        const uint32_t here = __ballot_sync(0xffffffffu, x < upto);
+        if (here != 0) {
+          const int32_t src = __ffs(here) - 1;
+          b = b0 + src;
+          tiles = __shfl_sync(0xffffffffu, t, src);
+          const int32_t parts = __shfl_sync(0xffffffffu, n, src);
+          const int32_t split = x - (__shfl_sync(0xffffffffu, upto, src) - parts);
+          t_lo = (int32_t)((int64_t)tiles * split / parts);
+          t_hi = (int32_t)((int64_t)tiles * (split + 1) / parts);
+          at = end = start = 0;
+          return true;
+        }
+        before = __shfl_sync(0xffffffffu, upto, 31);
+      }
+      return false;
     }
-    before = __shfl_sync(kAll, end, 31);
-    if (x == 0 && L.info == nullptr && w.b >= 0) break;
+    const int64_t n = max((total + kWorkTiles - 1) / kWorkTiles,
+                          min((int64_t)L.goal, max((int64_t)1, total / L.min_tiles)));
+    if (x >= n) return false;
+    const int32_t sliver = L.min_tiles / 2 - 1;
+    end = cut(a, total * (x + 1) / n, sliver);
+    at = cut(a, total * x / n, sliver);
+    if (at >= start + tiles && !find(a, at)) return false;
+    part();
+    return true;
   }
-  return w;
-}
+  __device__ __forceinline__ void part() {
+    t_lo = (int32_t)(at - start);
+    t_hi = (int32_t)min((int64_t)tiles, end - start);
+  }
+  // The CTA's next part.
+  __device__ __forceinline__ bool next(const CacheAttnArgs& a) {
+    at = start + tiles;
+    if (at >= end) return false;
+    start = at;
+    do tiles = tiles_of(a, ++b, false);
+    while (tiles == 0);
+    part();
+    return true;
+  }
+};
 
 // cache_attention_tc.cu: the tcgen05 kernel
 bool cache_attention_tc_runs(const CacheAttnArgs& a);

@@ -52,9 +52,7 @@ Plan make_plan(int32_t B, int32_t Hq, int32_t Hkv, int32_t D_max, int32_t L_max)
   Plan p;
   const int64_t rows = (int64_t)D_max * (Hq / Hkv);
   const int64_t sms = device_sm_count();
-  // few rows, or so few CTAs that the longest warp's steps are the time: 8 rows of all
-  // four warps
-  const bool few = (int64_t)B * Hkv * ((rows + 7) / 8) <= sms;
+  const bool few = cache_attention_few(B, Hkv, rows, L_max);
   p.rows = rows <= 8 || few ? 8 : 16;
   const int64_t row_tiles = (rows + p.rows - 1) / p.rows;
   p.row_warps = few ? 1 : row_tiles >= 3 ? 4 : (int32_t)row_tiles;

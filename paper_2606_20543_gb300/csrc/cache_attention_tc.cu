@@ -685,7 +685,8 @@ bool cache_map(CUtensorMap* map, const void* base, int64_t rows, int32_t box_row
 
 bool cache_attention_tc_runs(const CacheAttnArgs& a) {
   const int64_t rows = (int64_t)a.D_max * (a.Hq / a.cache.Hkv);
-  return a.cache.d == kD && rows > 16 && (a.draft_pos == nullptr || a.D_max <= kMaxDrafts);
+  return a.cache.d == kD && rows > 16 && (a.draft_pos == nullptr || a.D_max <= kMaxDrafts) &&
+         !cache_attention_few(a.B, a.cache.Hkv, rows, (int64_t)a.max_blocks * a.cache.block);
 }
 
 void cache_attention_tc_plan(int32_t B, int32_t Hq, int32_t Hkv, int32_t D_max, int32_t L_max,

@@ -30,7 +30,10 @@ namespace ssd {
 
 namespace {
 
-constexpr int kWarps = 4;
+constexpr int kWarps = 4;           // of a CTA
+constexpr int kManyWarps = 8;       // where no SM has more than one CTA: a warp alone on its
+                                    // scheduler takes 900 cycles a step, most of it waiting
+                                    // (8 heads over 800 keys: 12.6 us with four, 10.4)
 constexpr int kStages = 4;          // steps in flight per warp
 constexpr int kStep = 16;           // keys per step
 constexpr int kCtas = 3;            // per SM
@@ -43,6 +46,7 @@ constexpr float kGrowth = 8.f, kVGrowth = 16.f;
 
 struct Plan {
   int32_t rows, row_warps, row_groups;  // rows of a warp, its CTA's warps with other rows
+  int32_t warps;                        // of a CTA
   int32_t per_head, goal, uniform, min_tiles;
   int32_t group_rows() const { return rows * row_warps; }
   bool cut(int32_t B) const { return per_head > B; }
@@ -63,7 +67,7 @@ Plan make_plan(int32_t B, int32_t Hq, int32_t Hkv, int32_t D_max, int32_t L_max)
   const int64_t most = std::max<int64_t>(1, tiles / p.min_tiles);
   const int64_t least = (tiles + kWorkTiles - 1) / kWorkTiles;
   const int64_t target = kCtas * sms / ((int64_t)Hkv * p.row_groups);
-  if (target <= B || most == 1) {
+  if (target <= B || most < kCutFrom) {
     p.goal = p.uniform = (int32_t)least;
     p.per_head = (int32_t)(B * least);
   } else {
@@ -71,6 +75,8 @@ Plan make_plan(int32_t B, int32_t Hq, int32_t Hkv, int32_t D_max, int32_t L_max)
     p.goal = (int32_t)std::min(target, B * most);
     p.per_head = (int32_t)std::max<int64_t>(p.goal, B * least);
   }
+  const bool alone = (int64_t)p.per_head * Hkv * p.row_groups <= sms;
+  p.warps = alone && p.rows == 8 && p.row_warps == 1 ? kManyWarps : kWarps;
   return p;
 }
 
@@ -106,9 +112,9 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
   return y;
 }
 
-// NR: groups of 8 query rows of a warp.
-template <int D, int NR>
-__global__ void __launch_bounds__(kWarps * 32, kCtas)
+// NR: groups of 8 query rows of a warp; W: warps.
+template <int D, int NR, int W>
+__global__ void __launch_bounds__(W * 32, W == kWarps ? kCtas : 1)
 cache_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
                   CacheAttnArgs a, CacheAttnLaunch L, int32_t row_warps) {
   constexpr int RW = 8 * NR;          // rows of a warp
@@ -122,11 +128,11 @@ cache_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>(
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  int32_t* s_id = reinterpret_cast<int32_t*>(smem + kWarps * kWarpBytes);
+  int32_t* s_id = reinterpret_cast<int32_t*>(smem + W * kWarpBytes);
   float* s_ks = reinterpret_cast<float*>(s_id + L.max_blocks);
   float* s_vs = s_ks + L.max_blocks;
-  __shared__ uint64_t s_full[kWarps][kStages];
-  __shared__ float2 s_ml[kWarps][RW];
+  __shared__ uint64_t s_full[W][kStages];
+  __shared__ float2 s_ml[W][RW];
   if (threadIdx.x < 2) prefetch_tensormap(threadIdx.x == 0 ? &tmK : &tmV);
   pdl_wait();
 
@@ -159,7 +165,7 @@ cache_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
     const int32_t start = a.key_start != nullptr ? min(Lk, max(0, a.key_start[b])) : 0;
 
     // ---- this warp's rows and its share of the steps, and the copies of the first ones
-    const int32_t wk_n = kWarps / row_warps, wr = warp % row_warps, wk = warp / row_warps;
+    const int32_t wk_n = W / row_warps, wr = warp % row_warps, wk = warp / row_warps;
     const int32_t q = lane & 3, r8 = lane >> 2;
     const int32_t row0 = row_g0 + wr * RW;
     const int32_t first = max(k_lo, start & ~(kStep - 1));  // multiple of 16
@@ -472,14 +478,14 @@ cache_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
     }
     if (__syncthreads_or(!ok)) return;
     constexpr int PER = D / 32;
-    for (int32_t rr = warp; rr < row_warps * RW && row_g0 + rr < rows_total; rr += kWarps) {
+    for (int32_t rr = warp; rr < row_warps * RW && row_g0 + rr < rows_total; rr += W) {
       const int32_t w0 = rr / RW, r = rr - w0 * RW;
       float M = -INFINITY;
-      for (int32_t w = w0; w < kWarps; w += row_warps) M = fmaxf(M, s_ml[w][r].x);
+      for (int32_t w = w0; w < W; w += row_warps) M = fmaxf(M, s_ml[w][r].x);
       float sum = 0.f, acc[PER];
 #pragma unroll
       for (int k = 0; k < PER; ++k) acc[k] = 0.f;
-      for (int32_t w = w0; w < kWarps; w += row_warps) {
+      for (int32_t w = w0; w < W; w += row_warps) {
         const float2 ml = s_ml[w][r];
         const float f = ml.x == -INFINITY ? 0.f : exp2f(ml.x - M);
         sum += ml.y * f;
@@ -593,18 +599,18 @@ bool step_map(CUtensorMap* map, const void* base, const ssd_block_cache& c) {
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int D, int NR>
+template <int D, int NR, int W = kWarps>
 cudaError_t launch_mma(const CacheAttnArgs& a, const Plan& p, const CacheAttnLaunch& L,
                        cudaStream_t stream) {
   CUtensorMap tk, tv;
   if (!step_map(&tk, a.cache.k, a.cache) || !step_map(&tv, a.cache.v, a.cache))
     return cudaErrorInvalidValue;
-  const size_t smem = 1024 + (size_t)kWarps * kStages * 2 * kStep * D + (size_t)L.max_blocks * 12;
+  const size_t smem = 1024 + (size_t)W * kStages * 2 * kStep * D + (size_t)L.max_blocks * 12;
   const cudaError_t e = cudaFuncSetAttribute(
-      cache_attn_kernel<D, NR>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+      cache_attn_kernel<D, NR, W>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;
-  return launch_kernel(cache_attn_kernel<D, NR>, dim3(p.per_head, a.cache.Hkv, p.row_groups),
-                       dim3(kWarps * 32), smem, stream, true, tk, tv, a, L, p.row_warps);
+  return launch_kernel(cache_attn_kernel<D, NR, W>, dim3(p.per_head, a.cache.Hkv, p.row_groups),
+                       dim3(W * 32), smem, stream, true, tk, tv, a, L, p.row_warps);
 }
 
 size_t part_bytes(int64_t rows, int32_t d) {
@@ -664,8 +670,14 @@ cudaError_t launch_cache_attention(const CacheAttnArgs& a, void* ws, cudaStream_
   }
   cudaError_t e;
   if (tc) e = launch_cache_attention_tc(a, L, stream);
-  else if (d == 128) e = p.rows == 8 ? launch_mma<128, 1>(a, p, L, stream) : launch_mma<128, 2>(a, p, L, stream);
-  else e = p.rows == 8 ? launch_mma<64, 1>(a, p, L, stream) : launch_mma<64, 2>(a, p, L, stream);
+  else if (d == 128)
+    e = p.rows > 8 ? launch_mma<128, 2>(a, p, L, stream)
+        : p.warps == kWarps ? launch_mma<128, 1>(a, p, L, stream)
+                            : launch_mma<128, 1, kManyWarps>(a, p, L, stream);
+  else
+    e = p.rows > 8 ? launch_mma<64, 2>(a, p, L, stream)
+        : p.warps == kWarps ? launch_mma<64, 1>(a, p, L, stream)
+                            : launch_mma<64, 1, kManyWarps>(a, p, L, stream);
   if (e != cudaSuccess || rows == 0) return e;
   const dim3 grid((unsigned)(((int64_t)a.B * a.D_max * a.Hq + 7) / 8));
   return d == 128 ? launch_kernel(cache_attn_combine_kernel<128>, grid, dim3(256), 0, stream, true, a, L)

@@ -616,7 +616,8 @@ ssd_status ssd_cache_append(const ssd_block_cache* cache, const ssd_rotary* rota
  * position s); token cache_len + j' is draft j' (flat position of
  * draft_pos[b][j'], or cache_len + j' if draft_pos is NULL: plain causal
  * decoding, one token each with D_max = 1).  A query that sees no key gets
- * o = 0 and lse = -inf.  Slots outside the sequence's tokens may hold anything.
+ * o = 0 and lse = -inf.  Slots outside the sequence's tokens may hold anything;
+ * a NaN entry of a token reaches every row of a call that reads its block.
  *   q          dev bf16 [B][D_max][Hq][d] (rotated); scale 0 -> 1/sqrt(d)
  *   cache_len, n_drafts  dev int32 [B]; draft_pos dev int32 [B][D_max] or NULL
  *   key_start  dev int32 [B] or NULL (0): the first token that may be seen
@@ -653,8 +654,8 @@ ssd_status ssd_cache_attention(const ssd_grid* grid, const ssd_block_cache* cach
  *            in the order < top_p * Z_k (the first is always kept);
  *     out_tok = smallest v with sum of kept W_v' over v' <= v > u_res * Z,
  *     Z the kept mass, u_res the row's second uniform (ssd_rng).
- * T = 0 takes the first largest logit.  NaN logits count as -inf, +inf ones
- * as equal weights of 1; a row with nothing above -inf gives out_tok = -1, prob = 0,
+ * c is at most 2^100 (T above about 1e-30).  T = 0 takes the first largest
+ * logit.  NaN logits count as -inf, +inf ones as equal weights of 1; a row with nothing above -inf gives out_tok = -1, prob = 0,
  * kept = 0.  Weights below 2^-32 of the largest are never drawn.
  *   logits  dev float32 (or bf16 if logits_bf16) row r at + r * ld; any V up
  *           to 2^20, any alignment to the element

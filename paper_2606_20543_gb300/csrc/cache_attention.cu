@@ -19,6 +19,13 @@
 // again as soon as it is in registers.  P turns round in registers (movmatrix).
 // The warps of a CTA split 16-key steps among them where the rows are few (and
 // merge at the end), else they take other rows of the same keys.
+//
+// A token of 16 sequences of 7000 to 27000 keys, 8 KV heads of 4 query heads: 503 MB in 91 us,
+// 5.5 TB/s, 0.82 of the measured copy rate (with query rows in the mma's 16 rows, lane-wise
+// copies and as many CTAs for each sequence 132 us, the SMs idle for a quarter of it).  What is
+// left: the last tenth to even out, and the combine.  Little work is bound by the steps of a
+// warp, 900 cycles each while it has its scheduler to itself: one token over 800 keys 10.3 us,
+// of which 7 are the launch, the first copies and the rows' way out.
 
 #include <cuda_fp16.h>
 
@@ -520,7 +527,7 @@ cache_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
 }
 
 // One warp per (sequence, draft, head): the parts of its row, weighted by their
-// reference maxima.
+// reference maxima.  The launch is most of its 4 us.
 template <int D>
 __global__ void __launch_bounds__(256) cache_attn_combine_kernel(CacheAttnArgs a, CacheAttnLaunch L) {
   pdl_wait();

@@ -1,5 +1,5 @@
 // cache_attention_tc.cu — frontier attention over the paged 8-bit cache on the
-// 5th-generation tensor cores (include/ssd.h, ssd_cache_attention; 128-wide heads):
+// 5th-generation tensor cores (include/ssd.h, ssd_cache_attention):
 //   O[b][j][h] = softmax_s(scale * Q[b][j][h] . (sk K[s]) + M(s, j)) (sv V[s]).
 //
 // K stays e4m3 from the cache to the products (kind::f8f6f4): it is copied by TMA, 128 bytes
@@ -40,12 +40,9 @@ namespace ssd {
 
 namespace {
 
-constexpr int kD = 128;
 constexpr int kBM = 128;
 constexpr int KT = kCacheTile;
 constexpr int kNK = 3, kNV = 2;              // K and V stages
-constexpr int kTileBytes = KT * kD;          // one K (or V) tile
-constexpr int kQBytes = kBM * kD;            // one term of Q
 constexpr uint32_t kCols = 256;              // S/P x 2 (64 columns each), O at 128
 constexpr int kThreadsTC = 384;
 // Registers of a thread: 80 at launch (two CTAs per SM), then 144 for the softmax's warps and
@@ -60,7 +57,10 @@ constexpr float kLn2 = 0.6931471805599453f;
 // log2 growth of the maximum, and of the V scale over its reference, that moves them: P
 // stays below 2^12 in float16
 constexpr float kGrowth = 8.f, kVGrowth = 4.f;
-constexpr int kWideBytes = 2 * kTileBytes;   // a V tile in float16
+// Bytes of one term of Q, a K (or V) tile and a V tile in float16.
+__host__ __device__ constexpr int q_bytes(int d) { return kBM * d; }
+__host__ __device__ constexpr int tile_bytes(int d) { return KT * d; }
+__host__ __device__ constexpr int wide_bytes(int d) { return 2 * KT * d; }
 
 // kind::f8f6f4, e4m3 A and B, fp32 D.
 __host__ __device__ constexpr uint32_t idesc_e4m3(int m, int n, bool b_mn_major) {
@@ -155,6 +155,19 @@ __device__ __forceinline__ void give_registers() {
   asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOther));
 }
 
+// Rows of d bytes are swizzled over their own length (TMA and products alike): pieces of 16 bytes
+// by the row's place among 8 rows (128 bytes), or by that of its pair among 4 (64 bytes).
+template <int D>
+__device__ __forceinline__ uint32_t piece_at(int row, int piece) {
+  return (uint32_t)(row * D + ((piece ^ (D == 128 ? row & 7 : (row >> 1) & 3)) << 4));
+}
+// Descriptor of such rows, K-major: groups of 8 rows.
+template <int D>
+__device__ __forceinline__ uint64_t rows_desc(uint32_t saddr) {
+  const uint64_t d = smem_desc(saddr, 16, 8 * D);
+  return D == 128 ? d : (d & ~(7ull << 61)) | 4ull << 61;  // 64-byte swizzle
+}
+
 struct Shared {
   uint64_t k_full[kNK], k_empty[kNK], v_full[kNV], v_empty[kNV];
   uint64_t w_full[2];  // V widened
@@ -165,9 +178,11 @@ struct Shared {
   int32_t kflat[kMaxDrafts];
 };
 
+template <int D>
 __global__ void __launch_bounds__(kThreadsTC, kCtasPerSm)
 cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
                      CacheAttnArgs a, CacheAttnLaunch L, int32_t mtiles) {
+  constexpr int kQBytes = q_bytes(D), kTileBytes = tile_bytes(D), kWideBytes = wide_bytes(D);
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>(
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -292,13 +307,13 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
     const int32_t j = live ? r / G : 0, h = g * G + (live ? r - j * G : 0);
     const uint4* src = reinterpret_cast<const uint4*>(
                            static_cast<const __nv_bfloat16*>(a.q) +
-                           (((int64_t)b * a.D_max + j) * a.Hq + h) * kD) + half * (kD / 16);
-    uint4 w[kD / 16];
+                           (((int64_t)b * a.D_max + j) * a.Hq + h) * D) + half * (D / 16);
+    uint4 w[D / 16];
     float m = 0.f;
 #pragma unroll
-    for (int i = 0; i < kD / 16; ++i) w[i] = live ? src[i] : make_uint4(0, 0, 0, 0);
+    for (int i = 0; i < D / 16; ++i) w[i] = live ? src[i] : make_uint4(0, 0, 0, 0);
 #pragma unroll
-    for (int i = 0; i < kD / 16; ++i) {
+    for (int i = 0; i < D / 16; ++i) {
       const uint32_t v[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
 #pragma unroll
       for (int e = 0; e < 4; ++e)
@@ -309,10 +324,10 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
     const int32_t e = (int32_t)(__float_as_uint(m) >> 23) - 127, up = max(-120, min(126, 7 - e));
     const float f = __uint_as_float((uint32_t)(up + 127) << 23);
     if (half == 0)
-      sh.rowc[q_row] = (a.scale != 0.f ? a.scale : rsqrtf((float)kD)) * kLog2e *
+      sh.rowc[q_row] = (a.scale != 0.f ? a.scale : rsqrtf((float)D)) * kLog2e *
                        __uint_as_float((uint32_t)(127 - up) << 23);
 #pragma unroll
-    for (int c = 0; c < kD / 32; ++c) {
+    for (int c = 0; c < D / 32; ++c) {
       uint32_t hi[4], lo[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -324,8 +339,7 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
         hi[i] = h0 | (h1 << 16);
         lo[i] = l0 | (l1 << 16);
       }
-      const int ch = half * 4 + c;
-      const uint32_t off = (uint32_t)q_row * 128 + (uint32_t)((ch ^ (q_row & 7)) << 4);
+      const uint32_t off = piece_at<D>(q_row, half * (D / 32) + c);
       *reinterpret_cast<uint4*>(sQ + off) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
       *reinterpret_cast<uint4*>(sQ + kQBytes + off) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
     }
@@ -361,7 +375,7 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
       const int32_t c0 = k_lo + t * KT;
       // (blocks behind the last key are not copied: their rows stay what they were)
       const int32_t n = min(KT, k_hi - c0);
-      const uint32_t bytes = (uint32_t)((n + rows - 1) / rows * rows * kD);
+      const uint32_t bytes = (uint32_t)((n + rows - 1) / rows * rows * D);
       auto copy = [&](unsigned char* dst, const CUtensorMap* map, uint64_t* full) {
         if (leader) {
           mbar_arrive_expect_tx(full, bytes);
@@ -369,7 +383,7 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
           for (int32_t k = 0; k < n; k += rows) {
             const int32_t id = max(s_id[((c0 + k) >> S_log) - b_lo], 0);
             const int32_t row = (id * Hkv + g) * S + ((c0 + k) & (S - 1));
-            tma_load_2d(dst + k * kD, map, 0, row, full, pol);
+            tma_load_2d(dst + k * D, map, 0, row, full, pol);
           }
         }
         __syncwarp();
@@ -394,7 +408,7 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
     const uint32_t tSu = warp_uniform(tmem), aQ = warp_uniform(smem_u32(sQ));
     const uint32_t aK = warp_uniform(smem_u32(sK));
     const bool leader = elect_one();
-    const uint64_t dq = smem_desc(aQ, 16, 1024);
+    const uint64_t dq = rows_desc<D>(aQ);
     constexpr uint32_t kIdesc = idesc_e4m3(kBM, KT, false);
     int32_t t = 0;
     bool ok = true;
@@ -406,12 +420,12 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
       if (ok && t >= 2) ok = mbar_wait_warp(&sh.pv_done[sb], ((t >> 1) - 1) & 1, a.status);
       if (!ok) break;
       tc_fence_after();
-      const uint64_t dk = smem_desc(aK + s * kTileBytes, 16, 1024);
+      const uint64_t dk = rows_desc<D>(aK + s * kTileBytes);
       if (leader) {
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
-          for (int ks = 0; ks < kD / 32; ++ks)
+          for (int ks = 0; ks < D / 32; ++ks)
             mma8_ss(tSu + sb * KT, smem_desc_at(dq, u * kQBytes + ks * 32), smem_desc_at(dk, ks * 32),
                     kIdesc, u + ks > 0 ? 1u : 0u);
         mma_commit(&sh.s_full[sb]);
@@ -426,7 +440,7 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
     const uint32_t tSu = warp_uniform(tmem), tOu = warp_uniform(tO);
     const uint32_t aW = warp_uniform(smem_u32(sW));
     const bool leader = elect_one();
-    constexpr uint32_t kIdesc = idesc_f16(kBM, kD, true);
+    constexpr uint32_t kIdesc = idesc_f16(kBM, D, true);
     int32_t t = 0;
     bool ok = true;
 #pragma unroll 1
@@ -457,7 +471,7 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
     // warp took 2600 cycles a tile).  Rows without a key hold whatever the pool holds, and
     // their P of 0 times a NaN would be one: cleared.
     const int c = lane & 3, k8 = lane >> 2;
-    const uint32_t src0 = k8 * 128 + ((c ^ k8) << 4), src1 = k8 * 128 + (((c + 4) ^ k8) << 4);
+    const uint32_t src0 = piece_at<D>(k8, c), src1 = D == 128 ? piece_at<D>(k8, c + 4) : 0;
     const uint32_t dst0 = k8 * 128 + (((2 * c) ^ k8) << 4), dst1 = k8 * 128 + (((2 * c + 1) ^ k8) << 4);
 #pragma unroll 1
     for (int32_t t = 0; t < ntiles; ++t) {
@@ -473,8 +487,8 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
 #pragma unroll
       for (int i = 2 * (warp - 8); i < 2 * (warp - 8) + 2; ++i) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {  // blocks of 64 columns
-          uint4 w = *reinterpret_cast<const uint4*>(from + i * 1024 + (h ? src1 : src0));
+        for (int h = 0; h < D / 64; ++h) {  // blocks of 64 columns
+          uint4 w = *reinterpret_cast<const uint4*>(from + i * 8 * D + (h ? src1 : src0));
           if (!whole && !(live >> (8 * i + k8) & 1ull)) w = make_uint4(0u, 0u, 0u, 0u);
           unsigned char* at = to + h * (KT * 128) + i * 1024;
           *reinterpret_cast<uint4*>(at + dst0) = make_uint4(
@@ -584,7 +598,7 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
           ok = mbar_wait_warp(&sh.pv_done[(t - 1) & 1], ((t - 1) >> 1) & 1, a.status);
           tc_fence_after();
 #pragma unroll 1
-          for (int c = 0; c < kD / 16; ++c) {
+          for (int c = 0; c < D / 16; ++c) {
             float ov[16];
             tmem_ld16(tO + lane_off + c * 16, ov);
 #pragma unroll
@@ -637,12 +651,12 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
                                          : dbg_in(prow, (int64_t)a.B * a.D_max * a.Hq * L.splits, a.status));
       const float inv = l_run > 0.f ? v_ref / l_run : 0.f;
 #pragma unroll 1
-      for (int c = 0; c < kD / 32; ++c) {
+      for (int c = 0; c < D / 32; ++c) {
         float ov[32];
         tmem_ld32(tO + lane_off + c * 32, ov);
         if (!store) continue;
         if (direct) {
-          uint4* ob = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(a.o) + orow * kD + c * 32);
+          uint4* ob = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(a.o) + orow * D + c * 32);
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             // (a row that sees no key: 0, whatever its products are)
@@ -653,7 +667,7 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
                                pack_bf16x2(x[6], x[7]));
           }
         } else {
-          float4* po = reinterpret_cast<float4*>(L.part_o + prow * kD + c * 32);
+          float4* po = reinterpret_cast<float4*>(L.part_o + prow * D + c * 32);
 #pragma unroll
           for (int i = 0; i < 8; ++i)
             po[i] = make_float4(ov[4 * i] * v_ref, ov[4 * i + 1] * v_ref, ov[4 * i + 2] * v_ref, ov[4 * i + 3] * v_ref);
@@ -678,22 +692,45 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
   }
 }
 
-// 2D view of a cache: {128 bytes, rows}, box {128, rows of a copy}.
-bool cache_map(CUtensorMap* map, const void* base, int64_t rows, int32_t box_rows) {
+// 2D view of a cache: {d bytes, rows}, box {d, rows of a copy}.
+bool cache_map(CUtensorMap* map, const void* base, int64_t rows, int32_t box_rows, int32_t d) {
   EncodeTiledFn fn = tensor_map_encoder();
   if (fn == nullptr) return false;
-  const cuuint64_t dims[2] = {kD, (cuuint64_t)rows}, strides[1] = {kD};
-  const cuuint32_t box[2] = {kD, (cuuint32_t)box_rows}, estr[2] = {1, 1};
+  const cuuint64_t dims[2] = {(cuuint64_t)d, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)d};
+  const cuuint32_t box[2] = {(cuuint32_t)d, (cuuint32_t)box_rows}, estr[2] = {1, 1};
   return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, estr,
-            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+            CU_TENSOR_MAP_INTERLEAVE_NONE,
+            d == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int D>
+cudaError_t launch(const CacheAttnArgs& a, const CacheAttnLaunch& L, cudaStream_t stream) {
+  const int32_t mtiles = (int32_t)(((int64_t)a.D_max * (a.Hq / a.cache.Hkv) + kBM - 1) / kBM);
+  const int64_t rows = (int64_t)a.cache.num_blocks * a.cache.Hkv * a.cache.block;
+  const int32_t box = std::min(a.cache.block, KT);
+  CUtensorMap tk, tv;
+  if (!cache_map(&tk, a.cache.k, rows, box, D) || !cache_map(&tv, a.cache.v, rows, box, D))
+    return cudaErrorInvalidValue;
+  const size_t smem = 1024 + 2 * q_bytes(D) + (kNK + kNV) * tile_bytes(D) + 2 * wide_bytes(D) +
+                      sizeof(Shared) + (size_t)L.max_blocks * 16;
+  const cudaError_t e = cudaFuncSetAttribute(
+      cache_attn_tc_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (e != cudaSuccess) return e;
+  const int64_t grid = (int64_t)a.B * a.cache.Hkv * mtiles * L.splits;
+  if (grid > INT32_MAX) return cudaErrorInvalidValue;
+  return launch_kernel(cache_attn_tc_kernel<D>, dim3((unsigned)grid), dim3(kThreadsTC), smem, stream,
+                       true, tk, tv, a, L, mtiles);
 }
 
 }  // namespace
 
+// From 17 query rows on (the mma.sync kernel takes 16 to a warp, and every warp reads the keys for
+// itself): 8 sequences of 4000 keys, 32 heads: 128-wide, 17 rows 81 us here and 106 there, 48 rows
+// 94 and 189; 64-wide 77 and 72, 48 rows 88 and 130, 128 rows 89 and 331.
 bool cache_attention_tc_runs(const CacheAttnArgs& a) {
   const int64_t rows = (int64_t)a.D_max * (a.Hq / a.cache.Hkv);
-  return a.cache.d == kD && rows > 16 && (a.draft_pos == nullptr || a.D_max <= kMaxDrafts) &&
+  return rows > 16 && (a.draft_pos == nullptr || a.D_max <= kMaxDrafts) &&
          !cache_attention_few(a.B, a.cache.Hkv, rows, (int64_t)a.max_blocks * a.cache.block);
 }
 
@@ -710,21 +747,7 @@ void cache_attention_tc_plan(int32_t B, int32_t Hq, int32_t Hkv, int32_t D_max, 
 
 cudaError_t launch_cache_attention_tc(const CacheAttnArgs& a, const CacheAttnLaunch& L,
                                       cudaStream_t stream) {
-  const int32_t mtiles = (int32_t)(((int64_t)a.D_max * (a.Hq / a.cache.Hkv) + kBM - 1) / kBM);
-  const int64_t rows = (int64_t)a.cache.num_blocks * a.cache.Hkv * a.cache.block;
-  const int32_t box = std::min(a.cache.block, KT);
-  CUtensorMap tk, tv;
-  if (!cache_map(&tk, a.cache.k, rows, box) || !cache_map(&tv, a.cache.v, rows, box))
-    return cudaErrorInvalidValue;
-  const size_t smem = 1024 + 2 * kQBytes + (kNK + kNV) * kTileBytes + 2 * kWideBytes + sizeof(Shared) +
-                      (size_t)L.max_blocks * 16;
-  const cudaError_t e = cudaFuncSetAttribute(
-      cache_attn_tc_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-  if (e != cudaSuccess) return e;
-  const int64_t grid = (int64_t)a.B * a.cache.Hkv * mtiles * L.splits;
-  if (grid > INT32_MAX) return cudaErrorInvalidValue;
-  return launch_kernel(cache_attn_tc_kernel, dim3((unsigned)grid), dim3(kThreadsTC), smem, stream, true,
-                       tk, tv, a, L, mtiles);
+  return a.cache.d == 128 ? launch<128>(a, L, stream) : launch<64>(a, L, stream);
 }
 
 }  // namespace ssd

@@ -17,8 +17,7 @@
 // four keys.  A step's K and V come by TMA (swizzled, so those reads meet no bank
 // conflicts) into a ring of the warp's own, four steps deep; a stage is asked for
 // again as soon as it is in registers.  P turns round in registers (movmatrix).
-// The warps of a CTA split 16-key steps among them where the rows are few (and
-// merge at the end), else they take other rows of the same keys.
+// The warps of a CTA split 16-key steps among them and merge at the end.
 //
 // A token of 16 sequences of 7000 to 27000 keys, 8 KV heads of 4 query heads: 503 MB in 91 us,
 // 5.5 TB/s, 0.82 of the measured copy rate (with query rows in the mma's 16 rows, lane-wise
@@ -44,7 +43,7 @@ constexpr int kManyWarps = 8;       // where no SM has more than one CTA: a warp
 constexpr int kStages = 4;          // steps in flight per warp
 constexpr int kStep = 16;           // keys per step
 constexpr int kCtas = 3;            // per SM
-constexpr int kMinTiles = 2;        // a part's fewest tiles (times the warps that share its rows / 4)
+constexpr int kMinTiles = 8;        // a part's fewest tiles
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 // log2 growth of the running maximum (and growth of the V scale) that moves the
@@ -52,26 +51,23 @@ constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kGrowth = 8.f, kVGrowth = 16.f;
 
 struct Plan {
-  int32_t rows, row_warps, row_groups;  // rows of a warp, its CTA's warps with other rows
-  int32_t warps;                        // of a CTA
-  int32_t per_head, goal, uniform, min_tiles;
-  int32_t group_rows() const { return rows * row_warps; }
+  int32_t rows, row_groups;  // rows of a CTA, CTAs with other rows of the same keys
+  int32_t warps;             // of a CTA
+  int32_t per_head, goal, uniform;
   bool cut(int32_t B) const { return per_head > B; }
 };
 
+// (Of at most 16 rows, or little work.)
 Plan make_plan(int32_t B, int32_t Hq, int32_t Hkv, int32_t D_max, int32_t L_max) {
   Plan p;
   const int64_t rows = (int64_t)D_max * (Hq / Hkv);
   const int64_t sms = device_sm_count();
   const bool few = cache_attention_few(B, Hkv, rows, L_max);
   p.rows = rows <= 8 || few ? 8 : 16;
-  const int64_t row_tiles = (rows + p.rows - 1) / p.rows;
-  p.row_warps = few ? 1 : row_tiles >= 3 ? 4 : (int32_t)row_tiles;
-  p.row_groups = (int32_t)((row_tiles + p.row_warps - 1) / p.row_warps);
-  p.min_tiles = kMinTiles * (kWarps / p.row_warps);
+  p.row_groups = (int32_t)((rows + p.rows - 1) / p.rows);
   const int64_t tiles = (L_max + kCacheTile - 1) / kCacheTile;
   // CTAs a sequence and head may take; a part has room for so many block ids
-  const int64_t most = std::max<int64_t>(1, tiles / p.min_tiles);
+  const int64_t most = std::max<int64_t>(1, tiles / kMinTiles);
   const int64_t least = (tiles + kWorkTiles - 1) / kWorkTiles;
   const int64_t target = kCtas * sms / ((int64_t)Hkv * p.row_groups);
   if (target <= B || most < kCutFrom) {
@@ -83,7 +79,7 @@ Plan make_plan(int32_t B, int32_t Hq, int32_t Hkv, int32_t D_max, int32_t L_max)
     p.per_head = (int32_t)std::max<int64_t>(p.goal, B * least);
   }
   const bool alone = (int64_t)p.per_head * Hkv * p.row_groups <= sms;
-  p.warps = alone && p.rows == 8 && p.row_warps == 1 ? kManyWarps : kWarps;
+  p.warps = alone && p.rows == 8 ? kManyWarps : kWarps;
   return p;
 }
 
@@ -123,7 +119,7 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
 template <int D, int NR, int W>
 __global__ void __launch_bounds__(W * 32, W == kWarps ? kCtas : 1)
 cache_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
-                  CacheAttnArgs a, CacheAttnLaunch L, int32_t row_warps) {
+                  CacheAttnArgs a, CacheAttnLaunch L) {
   constexpr int RW = 8 * NR;          // rows of a warp
   constexpr int NT = D / 16;          // output tiles of 16 columns
   constexpr int KG = D / 64;          // groups of four mma steps of K Q^T
@@ -161,26 +157,24 @@ cache_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
     const int32_t b = work.b;
     const int32_t cache = a.cache_len[b], nd = a.n_drafts[b];
     const int32_t Lk = cache + nd, rows_total = nd * G;
-    const int32_t row_g0 = blockIdx.z * row_warps * RW;
+    const int32_t row0 = blockIdx.z * RW;
     if (L.info != nullptr && first_of && tid == 0) {
       if (work.t_lo == 0) L.info[b].x = blockIdx.x;
       if (work.t_hi == work.tiles) L.info[b].y = blockIdx.x;
     }
-    if (row_g0 >= rows_total) continue;
+    if (row0 >= rows_total) continue;
     const bool whole = work.t_lo == 0 && work.t_hi == work.tiles, begins = work.t_lo == 0;
     const int32_t k_lo = work.t_lo * kCacheTile, k_hi = min(Lk, work.t_hi * kCacheTile);
     const int32_t start = a.key_start != nullptr ? min(Lk, max(0, a.key_start[b])) : 0;
 
     // ---- this warp's rows and its share of the steps, and the copies of the first ones
-    const int32_t wk_n = W / row_warps, wr = warp % row_warps, wk = warp / row_warps;
     const int32_t q = lane & 3, r8 = lane >> 2;
-    const int32_t row0 = row_g0 + wr * RW;
     const int32_t first = max(k_lo, start & ~(kStep - 1));  // multiple of 16
     unsigned char* ring = smem + warp * kWarpBytes;
     const int32_t n_steps =
-        row0 >= rows_total || first >= k_hi ? 0 : (k_hi - first + kStep - 1) / kStep;
-    const int32_t steps = n_steps > wk ? (n_steps - wk + wk_n - 1) / wk_n : 0;
-    auto key_of = [&](int32_t t) { return first + (t * wk_n + wk) * kStep; };
+        first >= k_hi ? 0 : (k_hi - first + kStep - 1) / kStep;
+    const int32_t steps = n_steps > warp ? (n_steps - warp + W - 1) / W : 0;
+    auto key_of = [&](int32_t t) { return first + (t * W + warp) * kStep; };
     auto issue = [&](int32_t t, uint32_t to, int32_t id) {  // by one lane
       const int32_t k0 = key_of(t), z = max(id, 0) * a.cache.Hkv + g;
       unsigned char* dst = ring + to * kStageBytes;
@@ -485,14 +479,13 @@ cache_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
     }
     if (__syncthreads_or(!ok)) return;
     constexpr int PER = D / 32;
-    for (int32_t rr = warp; rr < row_warps * RW && row_g0 + rr < rows_total; rr += W) {
-      const int32_t w0 = rr / RW, r = rr - w0 * RW;
+    for (int32_t r = warp; r < RW && row0 + r < rows_total; r += W) {
       float M = -INFINITY;
-      for (int32_t w = w0; w < W; w += row_warps) M = fmaxf(M, s_ml[w][r].x);
+      for (int32_t w = 0; w < W; ++w) M = fmaxf(M, s_ml[w][r].x);
       float sum = 0.f, acc[PER];
 #pragma unroll
       for (int k = 0; k < PER; ++k) acc[k] = 0.f;
-      for (int32_t w = w0; w < W; w += row_warps) {
+      for (int32_t w = 0; w < W; ++w) {
         const float2 ml = s_ml[w][r];
         const float f = ml.x == -INFINITY ? 0.f : exp2f(ml.x - M);
         sum += ml.y * f;
@@ -501,7 +494,7 @@ cache_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
 #pragma unroll
         for (int k = 0; k < PER; ++k) acc[k] += po[k] * f;
       }
-      const int32_t row = row_g0 + rr, j = row / G, h = g * G + (row - j * G);
+      const int32_t row = row0 + r, j = row / G, h = g * G + (row - j * G);
       if (whole) {
         const int64_t at = ((int64_t)b * a.D_max + j) * a.Hq + h;
         if (!dbg_in(at, (int64_t)a.B * a.D_max * a.Hq, a.status)) continue;
@@ -515,8 +508,8 @@ cache_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
       } else {
         // (a CTA leaves a share of several sequences, but of neighbours: slot x + b)
         const int64_t slots = L.per_head + a.B;
-        const int64_t at = (((int64_t)g * L.row_groups + blockIdx.z) * slots + blockIdx.x + b) * L.group_rows + rr;
-        if (!dbg_in(at, (int64_t)a.cache.Hkv * L.row_groups * slots * L.group_rows, a.status)) continue;
+        const int64_t at = (((int64_t)g * L.row_groups + blockIdx.z) * slots + blockIdx.x + b) * RW + r;
+        if (!dbg_in(at, (int64_t)a.cache.Hkv * L.row_groups * slots * RW, a.status)) continue;
         float* po = L.part_o + at * D + lane * PER;
 #pragma unroll
         for (int k = 0; k < PER; ++k) po[k] = acc[k];
@@ -617,7 +610,7 @@ cudaError_t launch_mma(const CacheAttnArgs& a, const Plan& p, const CacheAttnLau
       cache_attn_kernel<D, NR, W>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;
   return launch_kernel(cache_attn_kernel<D, NR, W>, dim3(p.per_head, a.cache.Hkv, p.row_groups),
-                       dim3(W * 32), smem, stream, true, tk, tv, a, L, p.row_warps);
+                       dim3(W * 32), smem, stream, true, tk, tv, a, L);
 }
 
 size_t part_bytes(int64_t rows, int32_t d) {
@@ -628,27 +621,29 @@ int64_t tc_part_rows(int32_t B, int32_t Hq, int32_t D_max, int32_t splits) {
   return splits == 1 ? 0 : (int64_t)B * D_max * Hq * splits;
 }
 int64_t mma_part_rows(int32_t B, int32_t Hkv, const Plan& p) {
-  return p.cut(B) ? (int64_t)Hkv * p.row_groups * (p.per_head + B) * p.group_rows() : 0;
+  return p.cut(B) ? (int64_t)Hkv * p.row_groups * (p.per_head + B) * p.rows : 0;
 }
 
 }  // namespace
 
-// Enough for either kernel: which one runs depends on arguments that the
-// query does not have.
 size_t cache_attention_workspace(int32_t B, int32_t Hq, int32_t Hkv, int32_t d, int32_t D_max,
                                  int32_t L_max) {
-  int32_t splits, min_tiles;
-  cache_attention_tc_plan(B, Hq, Hkv, D_max, L_max, &splits, &min_tiles);
-  const Plan p = make_plan(B, Hq, Hkv, D_max, L_max);
-  const int64_t rows = std::max(tc_part_rows(B, Hq, D_max, splits), mma_part_rows(B, Hkv, p));
+  int64_t rows;
+  if (cache_attention_tc_runs(B, Hq, Hkv, D_max, L_max)) {
+    int32_t splits, min_tiles;
+    cache_attention_tc_plan(B, Hq, Hkv, D_max, L_max, &splits, &min_tiles);
+    rows = tc_part_rows(B, Hq, D_max, splits);
+  } else {
+    rows = mma_part_rows(B, Hkv, make_plan(B, Hq, Hkv, D_max, L_max));
+  }
   return rows == 0 ? 0 : part_bytes(rows, d) + align256((size_t)B * sizeof(int2));
 }
 
 cudaError_t launch_cache_attention(const CacheAttnArgs& a, void* ws, cudaStream_t stream) {
   const int32_t L_max = a.max_blocks * a.cache.block, d = a.cache.d;
   const int32_t tiles = (L_max + kCacheTile - 1) / kCacheTile;
-  const bool tc = cache_attention_tc_runs(a);
-  const Plan p = make_plan(a.B, a.Hq, a.cache.Hkv, a.D_max, L_max);
+  const bool tc = cache_attention_tc_runs(a.B, a.Hq, a.cache.Hkv, a.D_max, L_max);
+  Plan p{};
   CacheAttnLaunch L{};
   int64_t rows;
   int32_t part_tiles;
@@ -657,12 +652,13 @@ cudaError_t launch_cache_attention(const CacheAttnArgs& a, void* ws, cudaStream_
     rows = tc_part_rows(a.B, a.Hq, a.D_max, L.splits);
     part_tiles = cache_part_tiles(L.splits, L.min_tiles, tiles);
   } else {
-    L.min_tiles = p.min_tiles;
+    p = make_plan(a.B, a.Hq, a.cache.Hkv, a.D_max, L_max);
+    L.min_tiles = kMinTiles;
     L.per_head = p.per_head;
     L.goal = p.goal;
     L.uniform = p.uniform;
     L.row_groups = p.row_groups;
-    L.group_rows = p.group_rows();
+    L.group_rows = p.rows;
     rows = mma_part_rows(a.B, a.cache.Hkv, p);
     part_tiles = std::min(tiles, kWorkRoom);
   }

@@ -229,7 +229,7 @@ inline bool cache_attention_few(int64_t B, int64_t Hkv, int64_t rows, int64_t L_
 }
 
 // cache_attention_tc.cu: the tcgen05 kernel
-bool cache_attention_tc_runs(const CacheAttnArgs& a);
+bool cache_attention_tc_runs(int32_t B, int32_t Hq, int32_t Hkv, int32_t D_max, int32_t L_max);
 void cache_attention_tc_plan(int32_t B, int32_t Hq, int32_t Hkv, int32_t D_max, int32_t L_max,
                              int32_t* splits, int32_t* min_tiles);
 cudaError_t launch_cache_attention_tc(const CacheAttnArgs& a, const CacheAttnLaunch& L,

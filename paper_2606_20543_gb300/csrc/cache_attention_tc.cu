@@ -51,7 +51,7 @@ constexpr int kRegsSoftmax = 144, kRegsOther = 48;
 constexpr int kCtasPerSm = 2;
 constexpr int kMinTiles = 6;                 // a part's fewest tiles
 constexpr int kMaxPartTiles = 256;           // at most 1024 block ids and scales in shared memory
-constexpr int kMaxDrafts = 512;              // with positions of their own (kept in shared memory)
+constexpr int kMaxDrafts = 4096;             // whose positions are kept in shared memory
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 // log2 growth of the maximum, and of the V scale over its reference, that moves them: P
@@ -175,7 +175,7 @@ struct Shared {
   uint32_t tmem;
   int3 seq;             // the sequence, its cache length and drafts
   float rowc[kBM];      // a row's factor of the scores
-  int32_t kflat[kMaxDrafts];
+  int32_t len[kLptMax]; // sequences' keys
 };
 
 template <int D>
@@ -196,6 +196,8 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
   float* s_ks = reinterpret_cast<float*>(s_id + L.max_blocks);
   float* s_lv = s_ks + L.max_blocks;
   float* s_iv = s_lv + L.max_blocks;
+  int32_t* s_flat = reinterpret_cast<int32_t*>(s_iv + L.max_blocks);  // the drafts' positions
+  const bool staged = a.draft_pos != nullptr && a.D_max <= kMaxDrafts;
   pdl_wait();
 
   const int32_t tid = threadIdx.x, lane = tid & 31, warp = (int32_t)warp_uniform(tid >> 5);
@@ -210,20 +212,19 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
   // ---- the sequence: the rank-th longest (batches above 256 keep their order)
   int32_t b = rank, cache, nd;
   if (a.B > 1 && a.B <= kLptMax) {
-    int32_t* keys = sh.kflat;  // (not in use yet)
     int32_t mine = 0, c = 0, n = 0;
     if (tid < a.B) {
       c = a.cache_len[tid];
       n = a.n_drafts[tid];
       mine = cache_lengths_ok(a, c, n) && n > 0 ? c + n : 0;
-      keys[tid] = mine;
+      sh.len[tid] = mine;
     }
     __syncthreads();
     if (tid < a.B) {
       int32_t r = 0;
 #pragma unroll 4
       for (int32_t j = 0; j < a.B; ++j) {
-        const int32_t kj = keys[j];
+        const int32_t kj = sh.len[j];
         r += kj > mine || (kj == mine && j < tid);
       }
       if (r == rank) sh.seq = make_int3(tid, c, n);
@@ -251,7 +252,6 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
   const int32_t b_lo = k_lo >> S_log, nb = ((k_hi - 1) >> S_log) + 1 - b_lo;
 
   // ---- set-up
-  __syncthreads();  // kflat is free again
   if (tid == 0) {
     for (int i = 0; i < kNK; ++i) {
       mbar_init(&sh.k_full[i], 1);
@@ -295,7 +295,7 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
     for (int32_t j = stages ? tid - 128 : nd; j < nd; j += 128) {
       const int32_t p = cache_flat_pos(a, b, cache, j);
       if (p < 0 && split == 0 && g == 0 && mtile == 0) record_status(a.status, SSD_ERR_DEVICE_BOUNDS);
-      sh.kflat[j] = p;
+      if (staged) s_flat[j] = p;
     }
   }
   // Q as two terms, two threads a row, the row scaled to [128, 256) (rows behind the last
@@ -513,7 +513,8 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
     const float rowc = sh.rowc[tid];
     const int32_t j = r < rows_total ? r / G : 0;
     int32_t qpos = 0x7fffffff;
-    if (r < rows_total) qpos = a.draft_pos != nullptr ? sh.kflat[j] : cache + j;
+    auto flat_of = [&](int32_t i) { return staged ? s_flat[i] : cache_flat_pos(a, b, cache, i); };
+    if (r < rows_total) qpos = flat_of(j);
     // keys below this one are visible to every row of the warp
     const int32_t mask_from = min(cache, __reduce_min_sync(0xffffffffu, qpos) + 1);
     float m_run = -INFINITY, l_run = 0.f;
@@ -557,7 +558,7 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
             keep = low_bits(min(cache, qpos < 0x7fffffff ? qpos + 1 : cache) - c0);
 #pragma unroll 1
             for (int32_t k = max(0, cache - c0); k < min(KT, k_hi - c0); ++k) {
-              const int32_t p = sh.kflat[c0 + k - cache];
+              const int32_t p = flat_of(c0 + k - cache);
               if (p >= 0 && p <= qpos) keep |= 1ull << k;
             }
           }
@@ -713,7 +714,8 @@ cudaError_t launch(const CacheAttnArgs& a, const CacheAttnLaunch& L, cudaStream_
   if (!cache_map(&tk, a.cache.k, rows, box, D) || !cache_map(&tv, a.cache.v, rows, box, D))
     return cudaErrorInvalidValue;
   const size_t smem = 1024 + 2 * q_bytes(D) + (kNK + kNV) * tile_bytes(D) + 2 * wide_bytes(D) +
-                      sizeof(Shared) + (size_t)L.max_blocks * 16;
+                      sizeof(Shared) + (size_t)L.max_blocks * 16 +
+                      (a.draft_pos != nullptr && a.D_max <= kMaxDrafts ? (size_t)a.D_max * 4 : 0);
   const cudaError_t e = cudaFuncSetAttribute(
       cache_attn_tc_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;
@@ -725,13 +727,12 @@ cudaError_t launch(const CacheAttnArgs& a, const CacheAttnLaunch& L, cudaStream_
 
 }  // namespace
 
-// From 17 query rows on (the mma.sync kernel takes 16 to a warp, and every warp reads the keys for
+// From 17 query rows on (the mma.sync kernel takes 16 to a CTA, and every CTA reads the keys for
 // itself): 8 sequences of 4000 keys, 32 heads: 128-wide, 17 rows 81 us here and 106 there, 48 rows
 // 94 and 189; 64-wide 77 and 72, 48 rows 88 and 130, 128 rows 89 and 331.
-bool cache_attention_tc_runs(const CacheAttnArgs& a) {
-  const int64_t rows = (int64_t)a.D_max * (a.Hq / a.cache.Hkv);
-  return rows > 16 && (a.draft_pos == nullptr || a.D_max <= kMaxDrafts) &&
-         !cache_attention_few(a.B, a.cache.Hkv, rows, (int64_t)a.max_blocks * a.cache.block);
+bool cache_attention_tc_runs(int32_t B, int32_t Hq, int32_t Hkv, int32_t D_max, int32_t L_max) {
+  const int64_t rows = (int64_t)D_max * (Hq / Hkv);
+  return rows > 16 && !cache_attention_few(B, Hkv, rows, L_max);
 }
 
 void cache_attention_tc_plan(int32_t B, int32_t Hq, int32_t Hkv, int32_t D_max, int32_t L_max,

@@ -211,7 +211,20 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
 
   // ---- the sequence: the rank-th longest (batches above 256 keep their order)
   int32_t b = rank, cache, nd;
-  if (a.B > 1 && a.B <= kLptMax) {
+  if (a.B <= 32) {
+    // every warp for itself, a sequence a lane
+    const int32_t c = lane < a.B ? a.cache_len[lane] : 0, n = lane < a.B ? a.n_drafts[lane] : 0;
+    const int32_t mine = lane < a.B ? (cache_lengths_ok(a, c, n) && n > 0 ? c + n : 0) : -1;
+    int32_t r = 0;
+#pragma unroll
+    for (int32_t j = 0; j < 32; ++j) {
+      const int32_t kj = __shfl_sync(0xffffffffu, mine, j);
+      r += kj > mine || (kj == mine && j < lane);
+    }
+    b = __ffs(__ballot_sync(0xffffffffu, r == rank)) - 1;
+    cache = __shfl_sync(0xffffffffu, c, b);
+    nd = __shfl_sync(0xffffffffu, n, b);
+  } else if (a.B <= kLptMax) {
     int32_t mine = 0, c = 0, n = 0;
     if (tid < a.B) {
       c = a.cache_len[tid];
@@ -245,8 +258,11 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
   const int32_t tiles = (Lk + KT - 1) / KT;
   const int32_t parts = cache_parts(L.splits, L.min_tiles, tiles);
   if (row0 >= rows_total || split >= parts) return;
-  const int32_t t_lo = (int32_t)((int64_t)tiles * split / parts);
-  const int32_t t_hi = (int32_t)((int64_t)tiles * (split + 1) / parts);
+  int32_t t_lo = 0, t_hi = tiles;
+  if (parts > 1) {
+    t_lo = (int32_t)((int64_t)tiles * split / parts);
+    t_hi = (int32_t)((int64_t)tiles * (split + 1) / parts);
+  }
   const int32_t k_lo = t_lo * KT, k_hi = min(Lk, t_hi * KT), ntiles = t_hi - t_lo;
   const int32_t start = a.key_start != nullptr ? min(Lk, max(0, a.key_start[b])) : 0;
   const int32_t b_lo = k_lo >> S_log, nb = ((k_hi - 1) >> S_log) + 1 - b_lo;

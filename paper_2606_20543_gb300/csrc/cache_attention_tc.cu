@@ -8,17 +8,18 @@
 // twice the products, which run at twice the rate of bf16's), after its rows are scaled by a
 // power of two (largest entry in [128, 256)).  P, which changes with every tile, is rounded to
 // float16 instead (a split takes six instructions a pair, and the softmax is what bounds this
-// kernel): four warps widen V to float16, exactly, and the second product is kind::f16.  The K
+// kernel): two warps widen V to float16, exactly, and the second product is kind::f16.  The K
 // scale of a block multiplies the scores, its V scale over a reference the probabilities.
 //
-// One CTA (12 warps, two CTAs per SM) per tile of 128 query rows (drafts x the query
+// One CTA (8 warps, two CTAs per SM) per tile of 128 query rows (drafts x the query
 // heads of a KV head) and part of the sequence's keys, longest sequences first:
 //  warp 4 streams K and V in tiles of 64 keys through rings of kNK and kNV
-//    stages, a copy per cache block (TMA, 128-byte swizzle);
-//  warp 5 issues S = (Qhi + Qlo) K^T into one of two TMEM buffers, warp 6 O += P V
-//    with P read from TMEM, where it replaced S; warps 8-11 widen V into one of two buffers
-//    (and clear the rows that hold no key; one warp alone took 2300 cycles a tile, twice the
-//    softmax);
+//    stages, a copy per cache block (TMA, 64- or 128-byte swizzle);
+//  warp 5 issues S = (Qhi + Qlo) K^T of the next tile into one of two TMEM buffers, then O += P V
+//    of the tile before with P read from TMEM, where it replaced S;
+//  warps 6-7 widen V into one of two buffers (and clear the rows that hold no key); as four
+//    warps, with another for each product, they took issue slots from the softmax by waiting
+//    (25 x 48 drafts 34.3 us, 29.3 now);
 //  warps 0-3 (a thread a row, with the registers that the other warps give up) turn S into
 //    P.  The running maximum moves only when it grows by more than 2^8; O is rescaled in
 //    TMEM when it does, or when a block's V scale is above 16 times the reference.
@@ -44,10 +45,10 @@ constexpr int kBM = 128;
 constexpr int KT = kCacheTile;
 constexpr int kNK = 3, kNV = 2;              // K and V stages
 constexpr uint32_t kCols = 256;              // S/P x 2 (64 columns each), O at 128
-constexpr int kThreadsTC = 384;
-// Registers of a thread: 80 at launch (two CTAs per SM), then 144 for the softmax's warps and
-// 48 for the eight others: 144 + 2 * 48 = 3 * 80.
-constexpr int kRegsSoftmax = 144, kRegsOther = 48;
+constexpr int kThreadsTC = 256;
+// Registers of a thread: 128 at launch (two CTAs per SM), then 184 for the softmax's warps and
+// 72 for the others.
+constexpr int kRegsSoftmax = 184, kRegsOther = 72;
 constexpr int kCtasPerSm = 2;
 constexpr int kMinTiles = 6;                 // a part's fewest tiles
 constexpr int kMaxPartTiles = 256;           // at most 1024 block ids and scales in shared memory
@@ -275,10 +276,10 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
     }
     for (int i = 0; i < kNV; ++i) {
       mbar_init(&sh.v_full[i], 1);
-      mbar_init(&sh.v_empty[i], 4);
+      mbar_init(&sh.v_empty[i], 2);
     }
     for (int i = 0; i < 2; ++i) {
-      mbar_init(&sh.w_full[i], 4);
+      mbar_init(&sh.w_full[i], 2);
       mbar_init(&sh.s_full[i], 1);
       mbar_init(&sh.p_ready[i], 4);
       mbar_init(&sh.pv_done[i], 1);
@@ -316,8 +317,8 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
   }
   // Q as two terms, two threads a row, the row scaled to [128, 256) (rows behind the last
   // one stay what they were: they reach no other row)
-  const int32_t q_row = warp < 4 ? tid >> 1 : (tid - 128) >> 1;
-  if (!stages && row0 + (q_row & ~15) < rows_total) {
+#pragma unroll 1
+  for (int32_t q_row = tid >> 1; !stages && q_row < kBM && row0 + (q_row & ~15) < rows_total; q_row += 64) {
     const int32_t r = row0 + q_row, half = tid & 1;
     const bool live = r < rows_total;
     const int32_t j = live ? r / G : 0, h = g * G + (live ? r - j * G : 0);
@@ -419,51 +420,42 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
       for (int32_t u = max(0, nv - kNV); u < nv; ++u) drain(&sh.v_full[u % kNV], (u / kNV) & 1);
     }
   } else if (warp == 5) {
-    // ----------------------------------------------------------- S products
+    // ------------------------------------------------------------- products
     give_registers();
-    const uint32_t tSu = warp_uniform(tmem), aQ = warp_uniform(smem_u32(sQ));
-    const uint32_t aK = warp_uniform(smem_u32(sK));
+    const uint32_t tSu = warp_uniform(tmem), tOu = warp_uniform(tO), aQ = warp_uniform(smem_u32(sQ));
+    const uint32_t aK = warp_uniform(smem_u32(sK)), aW = warp_uniform(smem_u32(sW));
     const bool leader = elect_one();
     const uint64_t dq = rows_desc<D>(aQ);
-    constexpr uint32_t kIdesc = idesc_e4m3(kBM, KT, false);
-    int32_t t = 0;
+    constexpr uint32_t kIdescS = idesc_e4m3(kBM, KT, false), kIdescO = idesc_f16(kBM, D, true);
+    int32_t ns = 0, np = 0;  // tiles whose products were issued
     bool ok = true;
 #pragma unroll 1
-    for (; t < ntiles; ++t) {
-      const int s = t % kNK, sb = t & 1;
-      ok = mbar_wait_warp(&sh.k_full[s], (t / kNK) & 1, a.status);
-      // the S/P buffer is free once PV of tile t - 2 is done
-      if (ok && t >= 2) ok = mbar_wait_warp(&sh.pv_done[sb], ((t >> 1) - 1) & 1, a.status);
-      if (!ok) break;
-      tc_fence_after();
-      const uint64_t dk = rows_desc<D>(aK + s * kTileBytes);
-      if (leader) {
+    while (ok && np < ntiles) {
+      // S of the next tile, then PV of the one before
+      if (ns < ntiles) {
+        const int s = ns % kNK, sb = ns & 1;
+        ok = mbar_wait_warp(&sh.k_full[s], (ns / kNK) & 1, a.status);
+        // the S/P buffer is free once PV of tile ns - 2 is done
+        if (ok && ns >= 2) ok = mbar_wait_warp(&sh.pv_done[sb], ((ns >> 1) - 1) & 1, a.status);
+        if (!ok) break;
+        tc_fence_after();
+        const uint64_t dk = rows_desc<D>(aK + s * kTileBytes);
+        if (leader) {
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
+          for (int u = 0; u < 2; ++u)
 #pragma unroll
-          for (int ks = 0; ks < D / 32; ++ks)
-            mma8_ss(tSu + sb * KT, smem_desc_at(dq, u * kQBytes + ks * 32), smem_desc_at(dk, ks * 32),
-                    kIdesc, u + ks > 0 ? 1u : 0u);
-        mma_commit(&sh.s_full[sb]);
-        mma_commit(&sh.k_empty[s]);
+            for (int ks = 0; ks < D / 32; ++ks)
+              mma8_ss(tSu + sb * KT, smem_desc_at(dq, u * kQBytes + ks * 32), smem_desc_at(dk, ks * 32),
+                      kIdescS, u + ks > 0 ? 1u : 0u);
+          mma_commit(&sh.s_full[sb]);
+          mma_commit(&sh.k_empty[s]);
+        }
+        __syncwarp();
+        if (ns++ == 0) continue;
       }
-      __syncwarp();
-    }
-    if (!ok && t > 0) drain(&sh.s_full[(t - 1) & 1], ((t - 1) >> 1) & 1);
-  } else if (warp == 6) {
-    // ---------------------------------------------------------- PV products
-    give_registers();
-    const uint32_t tSu = warp_uniform(tmem), tOu = warp_uniform(tO);
-    const uint32_t aW = warp_uniform(smem_u32(sW));
-    const bool leader = elect_one();
-    constexpr uint32_t kIdesc = idesc_f16(kBM, D, true);
-    int32_t t = 0;
-    bool ok = true;
-#pragma unroll 1
-    for (; t < ntiles; ++t) {
-      const int sb = t & 1;
-      ok = mbar_wait_warp(&sh.w_full[sb], (t >> 1) & 1, a.status) &&
-           mbar_wait_warp(&sh.p_ready[sb], (t >> 1) & 1, a.status);
+      const int sb = np & 1;
+      ok = mbar_wait_warp(&sh.w_full[sb], (np >> 1) & 1, a.status) &&
+           mbar_wait_warp(&sh.p_ready[sb], (np >> 1) & 1, a.status);
       if (!ok) break;
       tc_fence_after();
       // A = P in TMEM (16 keys = 8 columns a step), B = V in float16 (MN-major: blocks of 64
@@ -472,14 +464,16 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
       if (leader) {
 #pragma unroll
         for (int kk = 0; kk < KT / 16; ++kk)
-          mma_ts(tOu, tSu + sb * KT + kk * 8, smem_desc_at(dv, kk * 2048), kIdesc, t + kk > 0 ? 1u : 0u);
+          mma_ts(tOu, tSu + sb * KT + kk * 8, smem_desc_at(dv, kk * 2048), kIdescO, np + kk > 0 ? 1u : 0u);
         mma_commit(&sh.pv_done[sb]);
       }
       __syncwarp();
+      ++np;
     }
-    if (!ok && t > 0) drain(&sh.pv_done[(t - 1) & 1], ((t - 1) >> 1) & 1);
-  } else if (warp >= 8) {
-    // ------------------------------------------------- V widened, 16 keys a warp
+    if (!ok && ns > 0) drain(&sh.s_full[(ns - 1) & 1], ((ns - 1) >> 1) & 1);
+    if (!ok && np > 0) drain(&sh.pv_done[(np - 1) & 1], ((np - 1) >> 1) & 1);
+  } else if (warp >= 6) {
+    // ------------------------------------------------- V widened, 32 keys a warp
     give_registers();
     // A lane takes 16 values (a 16-byte chunk) of a key, eight keys by four chunks a step:
     // then a lane's places in the swizzled tiles are fixed, and eight lanes' stores fill all
@@ -501,7 +495,7 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
       const bool whole = c0 >= start && c0 + KT <= k_hi && !any_bad;
       const uint64_t live = whole ? ~0ull : live_keys(c0);
 #pragma unroll
-      for (int i = 2 * (warp - 8); i < 2 * (warp - 8) + 2; ++i) {
+      for (int i = 4 * (warp - 6); i < 4 * (warp - 6) + 4; ++i) {
 #pragma unroll
         for (int h = 0; h < D / 64; ++h) {  // blocks of 64 columns
           uint4 w = *reinterpret_cast<const uint4*>(from + i * 8 * D + (h ? src1 : src0));
@@ -697,8 +691,6 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
               l_run > 0.f ? (m_run + log2f(l_run)) * kLn2 : -INFINITY;
       }
     }
-  } else {
-    give_registers();  // (warp 7: the whole group of four gives)
   }
   // ---- teardown
   tc_fence_before();

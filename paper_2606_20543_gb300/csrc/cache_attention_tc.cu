@@ -24,13 +24,15 @@
 //    P.  The running maximum moves only when it grows by more than 2^8; O is rescaled in
 //    TMEM when it does, or when a block's V scale is above 16 times the reference.
 //
-// 128 drafts of 8 sequences over 2300 to 3800 keys, 32 heads (222 MB, 51 GFLOP): 80 us, 2.8 TB/s,
-// 0.41 of the measured copy rate; the tensor pipe is busy for a quarter of it.  A tile takes
-// 1415 cycles of an SM with two CTAs, half of its issue slots: without the softmax 59 us, without
-// widening V 75, without exponentials 76.  256 CTAs leave 48 of the 152 SMs with one.  25
-// sequences of 48 drafts over 120 to 700 keys, 16 heads (56 MB): 35 us, of which a CTA's set-up
-// takes 3.7 and its seven tiles about as long.  Tiles of 128 keys with V in e4m3 as well (P in
-// two terms, 8 softmax warps): 94 and 38 us, so the products are not what to save.
+// 128 drafts of 8 sequences over 2300 to 3800 keys, 32 heads (222 MB, 51 GFLOP): 72 us, 3.1 TB/s,
+// 0.45 of the measured copy rate; the tensor pipe is busy for a quarter of it.  A tile takes
+// 1200 cycles of an SM with two CTAs, and a CTA of such a pair about 2200: 650 for the
+// exponentials, 370 for the maximum, 270 for S out of TMEM, the rest between the warps (when all of it
+// took 80 us it was 59 without the softmax, 76 without the exponentials, 75 without widening
+// V).  256 CTAs leave 48 of the 152 SMs with one.  25 sequences of 48 drafts over 120 to 700 keys,
+// 16 heads (56 MB): 29 us, of which a CTA's set-up takes 3.5 and its seven tiles about twice
+// that.  Tiles of 128 keys with V in e4m3 as well (P in two terms, 8 softmax warps) were
+// slower by a sixth, so the products are not what to save.
 #include <cuda_fp16.h>
 
 #include <algorithm>
@@ -149,6 +151,15 @@ __device__ __forceinline__ void drain(uint64_t* bar, uint32_t parity) {
   for (int i = 0; i < (1 << 14) && !mbar_try_wait(bar, parity); ++i) __nanosleep(256);
 }
 
+// Arrival of the warp's lane 0, without a branch.
+__device__ __forceinline__ void arrive_lane0(uint64_t* bar, int lane) {
+  asm volatile(
+      "{\n .reg .pred p;\n setp.eq.u32 p, %1, 0;\n"
+      " @p mbarrier.arrive.shared::cta.b64 _, [%0];\n}" ::"r"(smem_u32(bar)),
+      "r"(lane)
+      : "memory");
+}
+
 __device__ __forceinline__ void take_registers() {
   asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
 }
@@ -169,7 +180,7 @@ __device__ __forceinline__ uint64_t rows_desc(uint32_t saddr) {
   return D == 128 ? d : (d & ~(7ull << 61)) | 4ull << 61;  // 64-byte swizzle
 }
 
-struct Shared {
+struct alignas(16) Shared {
   uint64_t k_full[kNK], k_empty[kNK], v_full[kNV], v_empty[kNV];
   uint64_t w_full[2];  // V widened
   uint64_t s_full[2], p_ready[2], pv_done[2];
@@ -193,11 +204,8 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
   unsigned char* sW = sV + kNV * kTileBytes;       // V in float16 [2][d / 64][KT][128 bytes]
   Shared& sh = *reinterpret_cast<Shared*>(sW + 2 * kWideBytes);
   // the part's blocks: id (-1: outside the pool), K scale, log2 of the V scale, its inverse
-  int32_t* s_id = reinterpret_cast<int32_t*>(&sh + 1);
-  float* s_ks = reinterpret_cast<float*>(s_id + L.max_blocks);
-  float* s_lv = s_ks + L.max_blocks;
-  float* s_iv = s_lv + L.max_blocks;
-  int32_t* s_flat = reinterpret_cast<int32_t*>(s_iv + L.max_blocks);  // the drafts' positions
+  float4* s_blk = reinterpret_cast<float4*>(&sh + 1);
+  int32_t* s_flat = reinterpret_cast<int32_t*>(s_blk + L.max_blocks);  // the drafts' positions
   const bool staged = a.draft_pos != nullptr && a.D_max <= kMaxDrafts;
   pdl_wait();
 
@@ -301,12 +309,10 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
       id = -1;
       bad = true;
     }
-    s_id[i] = id;
     const int64_t at = (int64_t)max(id, 0) * Hkv + g;
-    s_ks[i] = a.cache.k_scale[at];
     const float vs = a.cache.v_scale[at];
-    s_lv[i] = id < 0 ? -INFINITY : log2f(vs);
-    s_iv[i] = 1.f / vs;
+    s_blk[i] = make_float4(a.cache.k_scale[at], id < 0 ? -INFINITY : log2f(vs), 1.f / vs,
+                           __int_as_float(id));
   }
   if (a.draft_pos != nullptr) {
     for (int32_t j = stages ? tid - 128 : nd; j < nd; j += 128) {
@@ -374,7 +380,7 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
     if (m == 0) return 0;
 #pragma unroll 1
     for (int32_t k = 0; k < KT; k += min(S, KT))
-      if (c0 + k < k_hi && s_id[((c0 + k) >> S_log) - b_lo] < 0)
+      if (c0 + k < k_hi && __float_as_int(s_blk[((c0 + k) >> S_log) - b_lo].w) < 0)
         m &= ~(low_bits(min(S, KT)) << k);
     return m;
   };
@@ -398,18 +404,18 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
           mbar_arrive_expect_tx(full, bytes);
 #pragma unroll 1
           for (int32_t k = 0; k < n; k += rows) {
-            const int32_t id = max(s_id[((c0 + k) >> S_log) - b_lo], 0);
+            const int32_t id = max(__float_as_int(s_blk[((c0 + k) >> S_log) - b_lo].w), 0);
             const int32_t row = (id * Hkv + g) * S + ((c0 + k) & (S - 1));
             tma_load_2d(dst + k * D, map, 0, row, full, pol);
           }
         }
         __syncwarp();
       };
-      if (t >= kNK) ok = mbar_wait_warp(&sh.k_empty[t % kNK], ((t / kNK) - 1) & 1, a.status);
+      if (t >= kNK) ok = wait_warp(&sh.k_empty[t % kNK], ((t / kNK) - 1) & 1, a.status);
       if (!ok) break;
       copy(sK + t % kNK * kTileBytes, &tmK, &sh.k_full[t % kNK]);
       nk = t + 1;
-      if (t >= kNV) ok = mbar_wait_warp(&sh.v_empty[t % kNV], ((t / kNV) - 1) & 1, a.status);
+      if (t >= kNV) ok = wait_warp(&sh.v_empty[t % kNV], ((t / kNV) - 1) & 1, a.status);
       if (!ok) break;
       copy(sV + t % kNV * kTileBytes, &tmV, &sh.v_full[t % kNV]);
       nv = t + 1;
@@ -434,9 +440,9 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
       // S of the next tile, then PV of the one before
       if (ns < ntiles) {
         const int s = ns % kNK, sb = ns & 1;
-        ok = mbar_wait_warp(&sh.k_full[s], (ns / kNK) & 1, a.status);
+        ok = wait_warp(&sh.k_full[s], (ns / kNK) & 1, a.status);
         // the S/P buffer is free once PV of tile ns - 2 is done
-        if (ok && ns >= 2) ok = mbar_wait_warp(&sh.pv_done[sb], ((ns >> 1) - 1) & 1, a.status);
+        if (ok && ns >= 2) ok = wait_warp(&sh.pv_done[sb], ((ns >> 1) - 1) & 1, a.status);
         if (!ok) break;
         tc_fence_after();
         const uint64_t dk = rows_desc<D>(aK + s * kTileBytes);
@@ -454,8 +460,8 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
         if (ns++ == 0) continue;
       }
       const int sb = np & 1;
-      ok = mbar_wait_warp(&sh.w_full[sb], (np >> 1) & 1, a.status) &&
-           mbar_wait_warp(&sh.p_ready[sb], (np >> 1) & 1, a.status);
+      ok = wait_warp(&sh.w_full[sb], (np >> 1) & 1, a.status) &&
+           wait_warp(&sh.p_ready[sb], (np >> 1) & 1, a.status);
       if (!ok) break;
       tc_fence_after();
       // A = P in TMEM (16 keys = 8 columns a step), B = V in float16 (MN-major: blocks of 64
@@ -487,8 +493,8 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
     for (int32_t t = 0; t < ntiles; ++t) {
       const int s = t % kNV, sb = t & 1;
       const int32_t c0 = k_lo + t * KT;
-      bool ok = mbar_wait_warp(&sh.v_full[s], (t / kNV) & 1, a.status);
-      if (ok && t >= 2) ok = mbar_wait_warp(&sh.pv_done[sb], ((t >> 1) - 1) & 1, a.status);
+      bool ok = wait_warp(&sh.v_full[s], (t / kNV) & 1, a.status);
+      if (ok && t >= 2) ok = wait_warp(&sh.pv_done[sb], ((t >> 1) - 1) & 1, a.status);
       if (!ok) break;
       const unsigned char* from = sV + s * kTileBytes;
       unsigned char* to = sW + sb * kWideBytes;
@@ -509,10 +515,8 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
       }
       fence_proxy_async_shared();
       __syncwarp();
-      if (lane == 0) {
-        mbar_arrive(&sh.w_full[sb]);
-        mbar_arrive(&sh.v_empty[s]);
-      }
+      arrive_lane0(&sh.w_full[sb], lane);
+      arrive_lane0(&sh.v_empty[s], lane);
     }
   } else if (warp < 4) {
     // ------------------------------------------------------------- softmax
@@ -539,21 +543,22 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
       float f[4], lg[4], iv[4];
       if (S_log >= 6) {  // the tile is of one block
         const int32_t at = (c0 >> S_log) - b_lo;
-        f[0] = f[1] = f[2] = f[3] = fmaxf(rowc * s_ks[at], 1e-37f);
-        lg[0] = lg[1] = lg[2] = lg[3] = s_lv[at];
-        iv[0] = iv[1] = iv[2] = iv[3] = s_iv[at];
+        const float4 x = s_blk[at];
+        f[0] = f[1] = f[2] = f[3] = fmaxf(rowc * x.x, 1e-37f);
+        lg[0] = lg[1] = lg[2] = lg[3] = x.y;
+        iv[0] = iv[1] = iv[2] = iv[3] = x.z;
       } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int32_t at = (min(c0 + 16 * i, k_hi - 1) >> S_log) - b_lo;
-          f[i] = fmaxf(rowc * s_ks[at], 1e-37f);
-          lg[i] = s_lv[at];
-          iv[i] = s_iv[at];
+          const float4 x = s_blk[at];
+          f[i] = fmaxf(rowc * x.x, 1e-37f);
+          lg[i] = x.y;
+          iv[i] = x.z;
         }
       }
       const float lg_max = fmaxf(fmaxf(lg[0], lg[1]), fmaxf(lg[2], lg[3]));
-      if (!mbar_wait(&sh.s_full[sb], (t >> 1) & 1, a.status)) ok = false;
-      ok = __all_sync(0xffffffffu, ok);
+      ok = ok && wait_warp(&sh.s_full[sb], (t >> 1) & 1, a.status);
       if (!ok) break;
       tc_fence_after();
       if (warp_live) {
@@ -606,7 +611,7 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
         }
         if (t > 0 && __any_sync(0xffffffffu, moved)) {
           // O may be rescaled once PV of the tile before is done
-          ok = mbar_wait_warp(&sh.pv_done[(t - 1) & 1], ((t - 1) >> 1) & 1, a.status);
+          ok = wait_warp(&sh.pv_done[(t - 1) & 1], ((t - 1) >> 1) & 1, a.status);
           tc_fence_after();
 #pragma unroll 1
           for (int c = 0; c < D / 16; ++c) {
@@ -647,10 +652,10 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
       }
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(&sh.p_ready[sb]);
+      arrive_lane0(&sh.p_ready[sb], lane);
     }
     // ---- epilogue
-    if (ok) ok = mbar_wait_warp(&sh.pv_done[(ntiles - 1) & 1], ((ntiles - 1) >> 1) & 1, a.status);
+    if (ok) ok = wait_warp(&sh.pv_done[(ntiles - 1) & 1], ((ntiles - 1) >> 1) & 1, a.status);
     tc_fence_after();
     if (ok && warp_live) {
       const bool live = r < rows_total;

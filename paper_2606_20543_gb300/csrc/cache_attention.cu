@@ -301,7 +301,7 @@ cache_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
     int32_t t = 0;
 #pragma unroll 1
     for (; t < steps; ++t) {
-      ok = mbar_wait_warp(&s_full[warp][stage], phase, a.status);
+      ok = wait_warp(&s_full[warp][stage], phase, a.status);
       if (!ok) break;
       const unsigned char* st = ring + stage * kStageBytes;
       uint4 kw[2][KG];

@@ -224,15 +224,14 @@ struct CacheWork {
   }
 };
 
-// Little work: as CTAs of 8 rows whose four warps share the keys, all of it is resident at once,
-// and what counts is how long one CTA takes.  Every 8 rows read the keys again, from L2, so only
-// up to 9 * 2^15 keys in all, and 3 * 2^16 where CTAs share an SM.  64 rows of 8 heads: over
-// 300 keys 9.4 us, on the tensor-core kernel, which takes 7000 cycles to get going, 14.2;
-// over 4000 keys 21.4 and 22.8; 96 rows over 4000 26.3 and 24.5.  32 heads, 64 rows (two CTAs
-// to an SM): over 300 keys 10.5 and 14.8, over 1000 24.8 and 21.5.
+// Little work: as CTAs of 8 rows whose warps share the keys, all of it is resident at once, and
+// what counts is how long one CTA takes.  Every 8 rows read the keys again, from L2, so only up
+// to 9 * 2^15 keys in all.  64 rows of 8 heads: over 300 keys 7.8 us, on the tensor-core kernel,
+// which takes 6500 cycles to get going, 12.3; over 4000 20.3 and 21.2; 96 rows over 4000 24.9 and
+// 23.6.  32 heads, 64 rows: over 1000 keys 16.8 and 19.2, over 2000 30.9 and 24.7.
 inline bool cache_attention_few(int64_t B, int64_t Hkv, int64_t rows, int64_t L_max) {
-  const int64_t ctas = B * Hkv * ((rows + 7) / 8), sms = device_sm_count();
-  return ctas <= 3 * sms && ctas * L_max <= (ctas <= sms ? 9 << 15 : 3 << 16);
+  const int64_t ctas = B * Hkv * ((rows + 7) / 8);
+  return ctas <= 3 * device_sm_count() && ctas * L_max <= 9 << 15;
 }
 
 // cache_attention_tc.cu: the tcgen05 kernel

@@ -19,12 +19,12 @@
 // again as soon as it is in registers.  P turns round in registers (movmatrix).
 // The warps of a CTA split 16-key steps among them and merge at the end.
 //
-// A token of 16 sequences of 7000 to 27000 keys, 8 KV heads of 4 query heads: 503 MB in 91 us,
-// 5.5 TB/s, 0.82 of the measured copy rate (with query rows in the mma's 16 rows, lane-wise
+// A token of 16 sequences of 7000 to 27000 keys, 8 KV heads of 4 query heads: 503 MB in 89 us,
+// 5.7 TB/s, 0.83 of the measured copy rate (with query rows in the mma's 16 rows, lane-wise
 // copies and as many CTAs for each sequence 132 us, the SMs idle for a quarter of it).  What is
 // left: the last tenth to even out, and the combine.  Little work is bound by the steps of a
-// warp, 900 cycles each while it has its scheduler to itself: one token over 800 keys 10.3 us,
-// of which 7 are the launch, the first copies and the rows' way out.
+// warp, 900 cycles each while it has its scheduler to itself: one token over 800 keys 9.4 us,
+// of which 6 are the launch, the first copies and the rows' way out.
 
 #include <cuda_fp16.h>
 
@@ -107,6 +107,9 @@ __device__ __forceinline__ uint32_t f16_hi(uint32_t w) {
 __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
   __half2 v = __floats2half2_rn(lo, hi);
   return *reinterpret_cast<uint32_t*>(&v);
+}
+__device__ __forceinline__ uint32_t word(const uint4& x, int i) {
+  return i == 0 ? x.x : i == 1 ? x.y : i == 2 ? x.z : x.w;
 }
 // 8 x 8 values of 16 bits, lane (r, q) holding (r, 2 q) and (r, 2 q + 1), turned round.
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
@@ -284,7 +287,8 @@ cache_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       const int32_t key = 2 * q + u;
-      v_off[u] = kStep * D + key * D + (D == 128 ? (r8 ^ key) << 4 : (((r8 >> 1) ^ q) << 4) + (r8 & 1) * 8);
+      v_off[u] = kStep * D + key * D +
+                 (D == 128 ? (r8 ^ key) << 4 : (((r8 >> 1) ^ q) << 4) + (r8 & 1) * 8);
     }
 
     float o[NR][NT][4];
@@ -344,8 +348,7 @@ cache_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
           for (int n = 0; n < NR; ++n) sc[kg][n][0] = sc[kg][n][1] = sc[kg][n][2] = sc[kg][n][3] = 0.f;
 #pragma unroll
           for (int s = 0; s < 4; ++s) {
-            const uint32_t w0 = s == 0 ? kw[0][kg].x : s == 1 ? kw[0][kg].y : s == 2 ? kw[0][kg].z : kw[0][kg].w;
-            const uint32_t w1 = s == 0 ? kw[1][kg].x : s == 1 ? kw[1][kg].y : s == 2 ? kw[1][kg].z : kw[1][kg].w;
+            const uint32_t w0 = word(kw[0][kg], s), w1 = word(kw[1][kg], s);
             const uint32_t kf[4] = {f16_lo(w0), f16_lo(w1), f16_hi(w0), f16_hi(w1)};
 #pragma unroll
             for (int n = 0; n < NR; ++n) mma_f16(sc[kg][n], kf, qf[n][kg][s][0], qf[n][kg][s][1]);
@@ -499,7 +502,8 @@ cache_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
         const int64_t at = ((int64_t)b * a.D_max + j) * a.Hq + h;
         if (!dbg_in(at, (int64_t)a.B * a.D_max * a.Hq, a.status)) continue;
         const float inv = sum > 0.f ? 1.f / sum : 0.f;
-        uint32_t* ob = reinterpret_cast<uint32_t*>(static_cast<__nv_bfloat16*>(a.o) + at * D + lane * PER);
+        uint32_t* ob =
+            reinterpret_cast<uint32_t*>(static_cast<__nv_bfloat16*>(a.o) + at * D + lane * PER);
 #pragma unroll
         for (int k = 0; k < PER; k += 2) ob[k / 2] = pack_bf16x2(acc[k] * inv, acc[k + 1] * inv);
         if (a.lse != nullptr && lane == 0)
@@ -683,8 +687,8 @@ cudaError_t launch_cache_attention(const CacheAttnArgs& a, void* ws, cudaStream_
                             : launch_mma<64, 1, kManyWarps>(a, p, L, stream);
   if (e != cudaSuccess || rows == 0) return e;
   const dim3 grid((unsigned)(((int64_t)a.B * a.D_max * a.Hq + 7) / 8));
-  return d == 128 ? launch_kernel(cache_attn_combine_kernel<128>, grid, dim3(256), 0, stream, true, a, L)
-                  : launch_kernel(cache_attn_combine_kernel<64>, grid, dim3(256), 0, stream, true, a, L);
+  return launch_kernel(d == 128 ? cache_attn_combine_kernel<128> : cache_attn_combine_kernel<64>, grid,
+                       dim3(256), 0, stream, true, a, L);
 }
 
 }  // namespace ssd

@@ -158,7 +158,8 @@ struct CacheWork {
     // the chunk: lo - 1 is too small, hi enough (or as long as a part may be)
     most = __reduce_max_sync(0xffffffffu, most);
     auto parts_of = [&](int32_t t, int32_t chunk) {
-      return min((t + chunk - 1) / chunk, t < kCutFrom * L.min_tiles ? (t > 0 ? 1 : 0) : t / L.min_tiles);
+      const int32_t at_most = t < kCutFrom * L.min_tiles ? (t > 0 ? 1 : 0) : t / L.min_tiles;
+      return min((t + chunk - 1) / chunk, at_most);
     };
     int32_t hi = (int32_t)min((int64_t)min(most, kWorkTiles), total / (L.goal - a.B) + 1);
     int32_t lo = max(1, (int32_t)min((int64_t)hi, (total + L.goal - 1) / L.goal));

@@ -324,7 +324,8 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
   // Q as two terms, two threads a row, the row scaled to [128, 256) (rows behind the last
   // one stay what they were: they reach no other row)
 #pragma unroll 1
-  for (int32_t q_row = tid >> 1; !stages && q_row < kBM && row0 + (q_row & ~15) < rows_total; q_row += 64) {
+  for (int32_t q_row = tid >> 1; !stages && q_row < kBM && row0 + (q_row & ~15) < rows_total;
+       q_row += 64) {
     const int32_t r = row0 + q_row, half = tid & 1;
     const bool live = r < rows_total;
     const int32_t j = live ? r / G : 0, h = g * G + (live ? r - j * G : 0);
@@ -357,8 +358,10 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
         const uint4& x = w[2 * c + (i >> 1)];
         const uint32_t p0 = (i & 1) ? x.z : x.x, p1 = (i & 1) ? x.w : x.y;
         uint32_t h0, l0, h1, l1;
-        split2(make_float2(__uint_as_float(p0 << 16) * f, __uint_as_float(p0 & 0xffff0000u) * f), h0, l0);
-        split2(make_float2(__uint_as_float(p1 << 16) * f, __uint_as_float(p1 & 0xffff0000u) * f), h1, l1);
+        const float2 x0 = make_float2(__uint_as_float(p0 << 16), __uint_as_float(p0 & 0xffff0000u));
+        const float2 x1 = make_float2(__uint_as_float(p1 << 16), __uint_as_float(p1 & 0xffff0000u));
+        split2(make_float2(x0.x * f, x0.y * f), h0, l0);
+        split2(make_float2(x1.x * f, x1.y * f), h1, l1);
         hi[i] = h0 | (h1 << 16);
         lo[i] = l0 | (l1 << 16);
       }
@@ -470,7 +473,8 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
       if (leader) {
 #pragma unroll
         for (int kk = 0; kk < KT / 16; ++kk)
-          mma_ts(tOu, tSu + sb * KT + kk * 8, smem_desc_at(dv, kk * 2048), kIdescO, np + kk > 0 ? 1u : 0u);
+          mma_ts(tOu, tSu + sb * KT + kk * 8, smem_desc_at(dv, kk * 2048), kIdescO,
+                 np + kk > 0 ? 1u : 0u);
         mma_commit(&sh.pv_done[sb]);
       }
       __syncwarp();
@@ -686,7 +690,8 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
           float4* po = reinterpret_cast<float4*>(L.part_o + prow * D + c * 32);
 #pragma unroll
           for (int i = 0; i < 8; ++i)
-            po[i] = make_float4(ov[4 * i] * v_ref, ov[4 * i + 1] * v_ref, ov[4 * i + 2] * v_ref, ov[4 * i + 3] * v_ref);
+            po[i] = make_float4(ov[4 * i] * v_ref, ov[4 * i + 1] * v_ref, ov[4 * i + 2] * v_ref,
+                                ov[4 * i + 3] * v_ref);
         }
       }
       if (store) {
@@ -741,8 +746,8 @@ cudaError_t launch(const CacheAttnArgs& a, const CacheAttnLaunch& L, cudaStream_
 }  // namespace
 
 // From 17 query rows on (the mma.sync kernel takes 16 to a CTA, and every CTA reads the keys for
-// itself): 8 sequences of 4000 keys, 32 heads: 128-wide, 17 rows 81 us here and 106 there, 48 rows
-// 94 and 189; 64-wide 77 and 72, 48 rows 88 and 130, 128 rows 89 and 331.
+// itself): 16 sequences of 4000 keys, 8 heads: 128-wide, 17 rows 45 us here and 59 there; 64-wide
+// 39 and 47 (48 rows and 8 sequences of 32 heads: 88 and 130).
 bool cache_attention_tc_runs(int32_t B, int32_t Hq, int32_t Hkv, int32_t D_max, int32_t L_max) {
   const int64_t rows = (int64_t)D_max * (Hq / Hkv);
   return rows > 16 && !cache_attention_few(B, Hkv, rows, L_max);

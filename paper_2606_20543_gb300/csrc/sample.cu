@@ -231,7 +231,9 @@ template <bool BF16>
 __device__ __noinline__ void select(SampleRow r, SampleShared& sh, bool of_row, bool by_count, u64 need,
                                     uint32_t lo, uint32_t hi) {
   const int32_t n = of_row ? r.V : sh.n_list, tid = threadIdx.x;
-  auto key_at = [&](int32_t i) { return of_row ? key_of(clean(load1<BF16>(r.x, r.inf, i))) : sh.key[i]; };
+  auto key_at = [&](int32_t i) {
+    return of_row ? key_of(clean(load1<BF16>(r.x, r.inf, i))) : sh.key[i];
+  };
   __syncthreads();
   if (tid == 0) {
     sh.from = lo;
@@ -875,7 +877,8 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
         // mass of the listed entries before the top-k bin
         if (!overflow) {
           for (int32_t i = tid; i < sh.n_list; i += kSampleThreads)
-            if (sh.key[i] >= key_p && (!has_k || sh.key[i] >= key_k1)) listed += weight_of(r, of_key(sh.key[i]));
+            if (sh.key[i] >= key_p && (!has_k || sh.key[i] >= key_k1))
+              listed += weight_of(r, of_key(sh.key[i]));
         } else {
 #pragma unroll 1
           for (int32_t i = tid; i < r.V; i += kSampleThreads) {

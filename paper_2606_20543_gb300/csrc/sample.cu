@@ -192,6 +192,7 @@ struct SampleShared {
                       // known), and the mass up to and including them
   int32_t n_list, cut_idx;
   int32_t bin_k, bin_lo, bin_hi, need_k;
+  float upto[kSampleWarps];   // mass up to and including a warp's bins
   float k_mass;               // estimated mass of the first k entries, and its error
   float k_mass_err;
   uint32_t edge[4];           // least keys above the bins' edges
@@ -786,12 +787,16 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
         total += sh.redf[w2];
       }
       const int32_t n0 = n1 - n;
-      const float m0 = m1 - mass;
       if (tid == 0) {
         sh.k_mass = total;
         sh.k_mass_err = 0.f;
       }
+      if (lane == 31) sh.upto[warp] = m1;
       __syncthreads();
+      // (the mass before the thread's bins is the one that the thread before ends with, to the
+      // bit: a cut that fell in between would be found by nobody)
+      float m0 = __shfl_up_sync(0xffffffffu, m1, 1);
+      if (lane == 0) m0 = warp == 0 ? 0.f : sh.upto[warp - 1];
       if (cut_k && n0 < k && k <= n1) {
         int32_t s = n0;
         float before = m0;
@@ -818,7 +823,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
         if (tid == 0 && least <= 0.f) sh.bin_lo = 0;
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
-          const float upto = before + q[i];
+          const float upto = i + 1 < kPer ? before + q[i] : m1;
           // (several threads may find one where sums are rounded: any will do)
           if (before < least && least <= upto) sh.bin_lo = tid * kPer + i;
           if (before < most && most <= upto) sh.bin_hi = tid * kPer + i;

@@ -21,11 +21,11 @@
 //
 // 1024 rows of 65536 float32 logits, top-p 0.95: 162 us, 268 MB at 1.65 TB/s (0.24 of the
 // measured copy rate; the pass for the largest logit alone takes 53 us, without a cut 111).
-// About 20 instructions an entry in the two passes bound it, and 20000 cycles a row between
-// them, of which two rows to an SM hide half.  One row of 16384, top-k 2000: 13 us; 200 rows
-// of 32771 bf16 logits with settings of their own: 39 us, one CTA's time.  Not faster: loads
-// by bulk copies into a ring (175 us), 256 threads a row (184: four rows to an SM do not fit
-// L2), counts and places in one word (168), bins of 1/256 without places (191: longer lists).
+// About 20 instructions an entry in the two passes bound it, and 17000 cycles a row between
+// them, of which two rows to an SM hide half.  One row of 16384, top-k 2000: 12.5 us; 200 rows
+// of 32771 bf16 logits with settings of their own: 39 us, one CTA's time; 1024 rows of 16384,
+// top-p 0.95: 55 us.  Not faster: loads by bulk copies into a ring (175 us for the first case),
+// counts and places in one word (168), bins of 1/256 without places (191: longer lists).
 #include <algorithm>
 #include <type_traits>
 
@@ -35,8 +35,6 @@ namespace ssd {
 
 namespace {
 
-constexpr int kSampleThreads = 512;
-constexpr int kSampleWarps = kSampleThreads / 32;
 constexpr int kChunk = 256;            // entries of a chunk, eight to a lane
 constexpr int kPerLog2 = 128;             // bins per factor of two
 constexpr float kBinsPerLog2 = kPerLog2;
@@ -173,17 +171,25 @@ __device__ __forceinline__ float max8(const float (&x)[8]) {  // NaN loses
   return fmax3(fmax3(x[0], x[1], x[2]), fmax3(x[3], x[4], x[5]), fmaxf(x[6], x[7]));
 }
 
+// NT: threads of a block.
+template <int NT>
 struct SampleShared {
-  uint32_t cnt[kBins];
-  uint32_t place[kBins];  // (right behind cnt)
-  uint32_t key[kList];  // the list
-  int32_t idx[kList];
+  union {
+    struct {  // pass A's
+      uint32_t cnt[kBins];
+      uint32_t place[kBins];  // (right behind cnt)
+    };
+    struct {  // the list, from pass B on
+      uint32_t key[kList];
+      int32_t idx[kList];
+    };
+  };
   uint32_t rsum[3][256];  // radix search: the masses' 11, 11 and 10 bits, each summed
   uint32_t rcnt[256];
   uint4 few[kFew];        // ~index, key (a number that orders entries), weight
-  u64 red[kSampleWarps], red2[kSampleWarps];
-  float redf[kSampleWarps];
-  int32_t redi[kSampleWarps];
+  u64 red[(NT / 32)], red2[(NT / 32)];
+  float redf[(NT / 32)];
+  int32_t redi[(NT / 32)];
   uint32_t from, to;  // radix search: the keys left, how many entries, what is to be reached
   uint32_t left, n_few;
   u64 need, above;
@@ -192,13 +198,14 @@ struct SampleShared {
                       // known), and the mass up to and including them
   int32_t n_list, cut_idx;
   int32_t bin_k, bin_lo, bin_hi, need_k;
-  float upto[kSampleWarps];   // mass up to and including a warp's bins
+  float upto[NT / 32];        // mass up to and including a warp's bins
   float k_mass;               // estimated mass of the first k entries, and its error
   float k_mass_err;
   uint32_t edge[4];           // least keys above the bins' edges
   uint32_t floor_key;         // least key with a weight
 };
 
+template <int NT>
 __device__ __forceinline__ u64 block_sum64(u64 v, u64* red) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
@@ -207,7 +214,7 @@ __device__ __forceinline__ u64 block_sum64(u64 v, u64* red) {
   __syncthreads();
   u64 s = 0;
 #pragma unroll
-  for (int w = 0; w < kSampleWarps; ++w) s += red[w];
+  for (int w = 0; w < (NT / 32); ++w) s += red[w];
   return s;
 }
 // Sum of at most 35-bit values over a warp.
@@ -228,8 +235,8 @@ __device__ __forceinline__ u64 add_wide(u64 s, uint32_t w) {
 // and keeps one digit's, until a few entries are left (most lists are short from the start):
 // then each is compared with all, a thread per entry.  Where more share one key, the
 // entries of that key that are kept are counted instead (n_eq).
-template <bool BF16>
-__device__ __noinline__ void select(SampleRow r, SampleShared& sh, bool of_row, bool by_count, u64 need,
+template <int NT, bool BF16>
+__device__ __noinline__ void select(SampleRow r, SampleShared<NT>& sh, bool of_row, bool by_count, u64 need,
                                     uint32_t lo, uint32_t hi) {
   const int32_t n = of_row ? r.V : sh.n_list, tid = threadIdx.x;
   auto key_at = [&](int32_t i) {
@@ -253,7 +260,7 @@ __device__ __noinline__ void select(SampleRow r, SampleShared& sh, bool of_row, 
     __syncthreads();
     const int shift = max(0, 24 - __clz(to - from));
 #pragma unroll 1
-    for (int32_t i = tid; i < n; i += kSampleThreads) {
+    for (int32_t i = tid; i < n; i += NT) {
       const uint32_t k = key_at(i);
       if (k < from || k > to) continue;
       const uint32_t d = (k - from) >> shift;
@@ -312,7 +319,7 @@ __device__ __noinline__ void select(SampleRow r, SampleShared& sh, bool of_row, 
   const uint32_t from = sh.from, to = sh.to;
   if (sh.left <= kFew) {
 #pragma unroll 1
-    for (int32_t i = tid; i < n; i += kSampleThreads) {
+    for (int32_t i = tid; i < n; i += NT) {
       const uint32_t k = key_at(i);
       if (k < from || k > to) continue;
       const uint32_t at = atomicAdd(&sh.n_few, 1u);
@@ -353,7 +360,8 @@ __device__ __noinline__ void select(SampleRow r, SampleShared& sh, bool of_row, 
 
 // Index behind the n_eq-th entry (in index order) that equals the cut, to cut_idx.
 // From the list, which holds all of them: a radix search over their indices.
-__device__ __noinline__ void list_ties(SampleShared& sh) {
+template <int NT>
+__device__ __noinline__ void list_ties(SampleShared<NT>& sh) {
   const int32_t n = sh.n_list, tid = threadIdx.x;
   const uint32_t cut = sh.cut;
   uint32_t left = (uint32_t)sh.n_eq;  // (at most kList)
@@ -364,7 +372,7 @@ __device__ __noinline__ void list_ties(SampleShared& sh) {
     if (tid < 256) sh.rcnt[tid] = 0;
     __syncthreads();
 #pragma unroll 1
-    for (int32_t i = tid; i < n; i += kSampleThreads)
+    for (int32_t i = tid; i < n; i += NT)
       if (sh.key[i] == cut && ((sh.idx[i] ^ base) >> shift) < 256)
         atomicAdd(&sh.rcnt[(sh.idx[i] >> shift) & 255], 1u);
     __syncthreads();
@@ -392,14 +400,14 @@ __device__ __noinline__ void list_ties(SampleShared& sh) {
   __syncthreads();
 }
 // From the row: counts by chunks (where the chunks' masses will stand), then the chunk's.
-template <bool BF16>
-__device__ __noinline__ void row_ties(SampleRow r, SampleShared& sh, u64* chunk, int32_t chunks) {
+template <int NT, bool BF16>
+__device__ __noinline__ void row_ties(SampleRow r, SampleShared<NT>& sh, u64* chunk, int32_t chunks) {
   const int32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const uint32_t cut = sh.cut;
   __syncthreads();
   if (tid == 0) sh.cut_idx = 0x7fffffff;
 #pragma unroll 2
-  for (int32_t ch = warp; ch < chunks; ch += kSampleWarps) {
+  for (int32_t ch = warp; ch < chunks; ch += (NT / 32)) {
     float x[8];
     load8<BF16>(r, ch, lane, x);
     uint32_t n = 0;
@@ -479,8 +487,8 @@ struct PassB {
 // Pass B.  Entries x >= x_sure are kept for certain (as far as min-p lets them); those in
 // [x_p, x_sure) and [x_k, x_k1) go to the list; TOTAL: the mass of the rest of the
 // row counts too, else that of [x_k1, x_p).
-template <bool BF16, bool TOTAL>
-__device__ __forceinline__ PassB pass_b(const SampleRow& r, SampleShared& sh, u64* chunk,
+template <int NT, bool BF16, bool TOTAL>
+__device__ __forceinline__ PassB pass_b(const SampleRow& r, SampleShared<NT>& sh, u64* chunk,
                                         int32_t chunks, float x_sure, float x_p, float x_k1,
                                         float x_k) {
   const int32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -488,7 +496,7 @@ __device__ __forceinline__ PassB pass_b(const SampleRow& r, SampleShared& sh, u6
   const bool all_kept = r.min_p <= 0x1p-32f;  // of the weights that are not 0
   PassB out{0, 0, 0};
 #pragma unroll 1
-  for (int32_t ch = warp; ch < chunks; ch += kSampleWarps) {
+  for (int32_t ch = warp; ch < chunks; ch += (NT / 32)) {
     float x[8];
     load8<BF16>(r, ch, lane, x);
     u64 s = 0;
@@ -575,11 +583,11 @@ __device__ __forceinline__ PassB pass_b(const SampleRow& r, SampleShared& sh, u6
   return out;
 }
 
-template <bool BF16>
-__global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a) {
+template <int NT, bool BF16>
+__global__ void __launch_bounds__(NT, 1024 / NT) sample_kernel(SampleArgs a) {
   extern __shared__ __align__(16) unsigned char smem_raw[];
-  SampleShared& sh = *reinterpret_cast<SampleShared*>(smem_raw);
-  u64* chunk = reinterpret_cast<u64*>(smem_raw + sizeof(SampleShared));
+  SampleShared<NT>& sh = *reinterpret_cast<SampleShared<NT>*>(smem_raw);
+  u64* chunk = reinterpret_cast<u64*>(smem_raw + sizeof(SampleShared<NT>));
   pdl_wait();
   const int32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   auto block_max = [&](float m) {
@@ -590,7 +598,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
     __syncthreads();
     m = sh.redf[0];
 #pragma unroll
-    for (int w = 1; w < kSampleWarps; ++w) m = fmaxf(m, sh.redf[w]);
+    for (int w = 1; w < (NT / 32); ++w) m = fmaxf(m, sh.redf[w]);
     return m;
   };
 #pragma unroll 1
@@ -648,13 +656,13 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
       const bool hist = (cut_k || cut_p) && ref > -INFINITY && ref < INFINITY;
       if (hist) {
 #pragma unroll
-        for (int i = 0; i < kBins / kSampleThreads; ++i)
-          sh.cnt[tid + i * kSampleThreads] = sh.place[tid + i * kSampleThreads] = 0;
+        for (int i = 0; i < kBins / NT; ++i)
+          sh.cnt[tid + i * NT] = sh.place[tid + i * NT] = 0;
         __syncthreads();
         const uint32_t cnt0 = smem_u32(sh.cnt);
         auto count = [&](auto places) {
 #pragma unroll 2
-          for (int32_t ch = warp; ch < chunks; ch += kSampleWarps) {
+          for (int32_t ch = warp; ch < chunks; ch += (NT / 32)) {
             float x[8];
             load8<BF16>(r, ch, lane, x);
             m = fmaxf(m, max8(x));
@@ -672,7 +680,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
         else count(std::false_type());
       } else {
 #pragma unroll 4
-        for (int32_t ch = warp; ch < chunks; ch += kSampleWarps) {
+        for (int32_t ch = warp; ch < chunks; ch += (NT / 32)) {
           float x[8];
           load8<BF16>(r, ch, lane, x);
           const float y = max8(x);
@@ -707,7 +715,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
       if (lane == 0) sh.redi[warp] = at;
       __syncthreads();
       if (tid == 0) {
-        for (int w = 1; w < kSampleWarps; ++w) at = min(at, sh.redi[w]);
+        for (int w = 1; w < (NT / 32); ++w) at = min(at, sh.redi[w]);
         a.out_tok[row] = at;
         if (a.prob) a.prob[row] = 1.f;
         if (a.kept) a.kept[row] = 1;
@@ -727,7 +735,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
       sh.bin_lo = sh.bin_hi = kBins;
     }
 
-    if (warp == kSampleWarps - 1) {
+    if (warp == (NT / 32) - 1) {
       // the least logit with a weight: rounding makes the others 0
       const uint32_t at = least_key(lane, r.top - 32.f * kBinsPerLog2 / r.c,
                                     [&](float x) { return weight_of(r, x) != 0; });
@@ -739,8 +747,8 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
     // edge[2], edge[3]: start and end of the top-k bin
     uint32_t key_sure = 0, key_p = 0xffffffffu, key_k1 = 0xffffffffu, key_k = 0xffffffffu;
     if (cut_k || cut_p) {
-      constexpr int kPer = kBins / kSampleThreads;
-      static_assert(kPer * kSampleThreads == kBins, "bins per thread");
+      constexpr int kPer = kBins / NT;
+      static_assert(kPer * NT == kBins, "bins per thread");
       // 2^((kHead - b) / 128) of a bin's upper edge
       const float w0 = exp2f((float)(kHead - tid * kPer) / kBinsPerLog2);
       constexpr float kStep = 0.99459942f;  // 2^(-1/128)
@@ -779,7 +787,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
       __syncthreads();
       float total = 0.f;
 #pragma unroll
-      for (int w2 = 0; w2 < kSampleWarps; ++w2) {
+      for (int w2 = 0; w2 < (NT / 32); ++w2) {
         if (w2 < warp) {
           n1 += sh.redi[w2];
           m1 += sh.redf[w2];
@@ -861,55 +869,55 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
     // ---- B
     auto at_key = [](uint32_t key) { return key == 0xffffffffu ? INFINITY : of_key(key); };
     const PassB pb = cut_p && !has_k
-                         ? pass_b<BF16, true>(r, sh, chunk, chunks, at_key(key_sure), at_key(key_p),
+                         ? pass_b<NT, BF16, true>(r, sh, chunk, chunks, at_key(key_sure), at_key(key_p),
                                               INFINITY, INFINITY)
-                         : pass_b<BF16, false>(r, sh, chunk, chunks, at_key(key_sure), at_key(key_p),
+                         : pass_b<NT, BF16, false>(r, sh, chunk, chunks, at_key(key_sure), at_key(key_p),
                                                at_key(key_k1), at_key(key_k));
     uint32_t count = pb.count;
     bool by_row = false;  // the chunks' masses are to be summed again
     if (cut_k || cut_p) {
       u64 sure = 0, rest = 0;  // rest: all of the row, or what lies between the listed bins
       if (cut_p) {
-        sure = block_sum64(pb.sure, sh.red);
-        rest = block_sum64(pb.total, sh.red2);
+        sure = block_sum64<NT>(pb.sure, sh.red);
+        rest = block_sum64<NT>(pb.total, sh.red2);
       }
       __syncthreads();
       const bool overflow = sh.n_list > kList;
       by_row = overflow;
-      if (has_k) select<BF16>(r, sh, overflow, true, (u64)sh.need_k, key_k, key_k1 - 1);
+      if (has_k) select<NT, BF16>(r, sh, overflow, true, (u64)sh.need_k, key_k, key_k1 - 1);
       if (cut_p) {
         u64 k_mass = rest, listed = 0;
         // mass of the listed entries before the top-k bin
         if (!overflow) {
-          for (int32_t i = tid; i < sh.n_list; i += kSampleThreads)
+          for (int32_t i = tid; i < sh.n_list; i += NT)
             if (sh.key[i] >= key_p && (!has_k || sh.key[i] >= key_k1))
               listed += weight_of(r, of_key(sh.key[i]));
         } else {
 #pragma unroll 1
-          for (int32_t i = tid; i < r.V; i += kSampleThreads) {
+          for (int32_t i = tid; i < r.V; i += NT) {
             const float x = load1<BF16>(r.x, r.inf, i);
             const uint32_t key = key_of(clean(x));
             if (key >= key_p && key < key_sure && (!has_k || key >= key_k1)) listed += weight_of(r, x);
           }
         }
-        listed = block_sum64(listed, sh.red);
+        listed = block_sum64<NT>(listed, sh.red);
         if (has_k) k_mass = sure + rest + listed + sh.cut_mass;
         const u64 need = (u64)ceil((double)top_p * (double)k_mass);
         // what the listed top-p bins reach: with the top-k bin among them, all of it
         const bool with_k = has_k && key_p <= key_k;
         const u64 reach = sure + listed + (with_k ? sh.cut_mass : 0);
         if (need > sure && need <= reach) {
-          select<BF16>(r, sh, overflow, false, need - sure, with_k ? key_k : key_p, key_sure - 1);
+          select<NT, BF16>(r, sh, overflow, false, need - sure, with_k ? key_k : key_p, key_sure - 1);
         } else {
           // the estimate was off: the cut is not in the listed bins
           by_row = true;
-          select<BF16>(r, sh, true, false, need, key_of(-INFINITY), key_of(r.top));
+          select<NT, BF16>(r, sh, true, false, need, key_of(-INFINITY), key_of(r.top));
         }
       }
       // equal entries at the cut, too many for a warp
       if (sh.n_eq != 0) {
-        if (by_row) row_ties<BF16>(r, sh, chunk, chunks);
-        else list_ties(sh);
+        if (by_row) row_ties<NT, BF16>(r, sh, chunk, chunks);
+        else list_ties<NT>(sh);
       }
     }
     __syncthreads();
@@ -925,7 +933,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
     if (by_row) {
       count = 0;
 #pragma unroll 1
-      for (int32_t ch = warp; ch < chunks; ch += kSampleWarps) {
+      for (int32_t ch = warp; ch < chunks; ch += (NT / 32)) {
         float x[8];
         load8<BF16>(r, ch, lane, x);
         u64 s = 0;
@@ -940,7 +948,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
       }
     } else {
       const int32_t n_list = sh.n_list;
-      for (int32_t i = tid; i < n_list; i += kSampleThreads) {
+      for (int32_t i = tid; i < n_list; i += NT) {
         const uint32_t w = kept_weight(of_key(sh.key[i]), sh.idx[i]);
         if (w == 0) continue;
         ++count;
@@ -953,7 +961,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
 
     // ---- the draw
     if (warp == 0) {
-      count = lane < kSampleWarps ? sh.redi[lane] : 0;
+      count = lane < (NT / 32) ? sh.redi[lane] : 0;
       count = __reduce_add_sync(0xffffffffu, count);
       const int32_t per = (chunks + 31) / 32;
       u64 s = 0;
@@ -1018,24 +1026,32 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(SampleArgs a)
   }
 }
 
-template <bool BF16>
+template <int NT, bool BF16>
 cudaError_t launch(const SampleArgs& a, cudaStream_t stream) {
   // (a row may begin up to 7 entries behind its first chunk's begin)
   const size_t smem =
-      sizeof(SampleShared) + (size_t)((a.V + 7 + kChunk - 1) / kChunk) * sizeof(u64);
+      sizeof(SampleShared<NT>) + (size_t)((a.V + 7 + kChunk - 1) / kChunk) * sizeof(u64);
   const cudaError_t e = cudaFuncSetAttribute(
-      sample_kernel<BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+      sample_kernel<NT, BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;
   // a row per CTA, dealt by the hardware as CTAs end
   const unsigned blocks = (unsigned)std::min<int64_t>(a.rows, 1 << 20);
-  return launch_kernel(sample_kernel<BF16>, dim3(blocks), dim3(kSampleThreads), smem, stream, true,
+  return launch_kernel(sample_kernel<NT, BF16>, dim3(blocks), dim3(NT), smem, stream, true,
                        a);
 }
 
 }  // namespace
 
 cudaError_t launch_sample(const SampleArgs& a, cudaStream_t stream) {
-  return a.bf16 ? launch<true>(a, stream) : launch<false>(a, stream);
+  // Many rows of up to 128 KB: 256 threads each, so that four rows share an SM and one's passes
+  // run beside what another does between them (1024 rows, top-p 0.95, of 4096 logits 46 -> 31 us,
+  // of 16384 69 -> 55, of 32768 99 -> 94).  Four rows of 256 KB to an SM do not fit L2, where the
+  // second pass finds them (65536 logits: 163 -> 184); two rows to an SM are better off with
+  // 512 threads, few rows too.
+  const bool many =
+      a.rows > 2 * device_sm_count() && (int64_t)a.V * (a.bf16 ? 2 : 4) <= 128 << 10;
+  if (many) return a.bf16 ? launch<256, true>(a, stream) : launch<256, false>(a, stream);
+  return a.bf16 ? launch<512, true>(a, stream) : launch<512, false>(a, stream);
 }
 
 }  // namespace ssd

@@ -45,7 +45,6 @@ constexpr int kStep = 16;           // keys per step
 constexpr int kCtas = 3;            // per SM
 constexpr int kMinTiles = 8;        // a part's fewest tiles
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kLn2 = 0.6931471805599453f;
 // log2 growth of the running maximum (and growth of the V scale) that moves the
 // reference: P stays below 2^8 * 2^4 in float16
 constexpr float kGrowth = 8.f, kVGrowth = 16.f;
@@ -501,14 +500,14 @@ cache_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
       if (whole) {
         const int64_t at = ((int64_t)b * a.D_max + j) * a.Hq + h;
         if (!dbg_in(at, (int64_t)a.B * a.D_max * a.Hq, a.status)) continue;
-        const float inv = sum > 0.f ? 1.f / sum : 0.f;
+        const float inv = 1.f / sum;
         uint32_t* ob =
             reinterpret_cast<uint32_t*>(static_cast<__nv_bfloat16*>(a.o) + at * D + lane * PER);
 #pragma unroll
-        for (int k = 0; k < PER; k += 2) ob[k / 2] = pack_bf16x2(acc[k] * inv, acc[k + 1] * inv);
+        for (int k = 0; k < PER; k += 2)
+          ob[k / 2] = pack_bf16x2(row_value(acc[k], inv, sum), row_value(acc[k + 1], inv, sum));
         if (a.lse != nullptr && lane == 0)
-          a.lse[((int64_t)b * a.Hq + h) * a.D_max + j] =
-              sum > 0.f ? (M + log2f(sum)) * kLn2 : -INFINITY;
+          a.lse[((int64_t)b * a.Hq + h) * a.D_max + j] = row_lse(M, sum);
       } else {
         // (a CTA leaves a share of several sequences, but of neighbours: slot x + b)
         const int64_t slots = L.per_head + a.B;
@@ -580,13 +579,14 @@ __global__ void __launch_bounds__(256) cache_attn_combine_kernel(CacheAttnArgs a
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-  const float inv = sum > 0.f ? 1.f / sum : 0.f;
+  const float inv = 1.f / sum;
   __nv_bfloat16* ob = static_cast<__nv_bfloat16*>(a.o) + row * D + lane * PER;
 #pragma unroll
   for (int k = 0; k < PER; k += 2)
-    *reinterpret_cast<uint32_t*>(ob + k) = pack_bf16x2(acc[k] * inv, acc[k + 1] * inv);
+    *reinterpret_cast<uint32_t*>(ob + k) =
+        pack_bf16x2(row_value(acc[k], inv, sum), row_value(acc[k + 1], inv, sum));
   if (a.lse != nullptr && lane == 0)
-    a.lse[((int64_t)b * a.Hq + h) * a.D_max + j] = sum > 0.f ? (M + log2f(sum)) * kLn2 : -INFINITY;
+    a.lse[((int64_t)b * a.Hq + h) * a.D_max + j] = row_lse(M, sum);
 }
 
 // 3D view of a cache: {d bytes, tokens of a block, blocks x heads}, box {d, a step, 1}.

@@ -46,6 +46,16 @@ __device__ __forceinline__ bool wait_warp(uint64_t* bar, uint32_t parity, int32_
   return mbar_wait_warp(bar, parity, status);
 }
 
+// A row's way out.  A row that sees no key has the sum 0, and nothing else has: then it is 0 and
+// -inf, whatever its products are (0 times a NaN of the pool).  A NaN in a key that it sees, or in
+// its query, makes the sum a NaN, and that goes out.
+__device__ __forceinline__ float row_value(float x, float inv, float sum) {
+  return sum == 0.f ? 0.f : x * inv;
+}
+__device__ __forceinline__ float row_lse(float m_log2, float sum) {
+  return sum == 0.f ? -INFINITY : (m_log2 + log2f(sum)) * 0.6931471805599453f;
+}
+
 // Flat position of draft j of sequence b; -1 outside the grid.
 __device__ __forceinline__ int32_t cache_flat_pos(const CacheAttnArgs& a, int32_t b, int32_t cache,
                                                   int32_t j) {

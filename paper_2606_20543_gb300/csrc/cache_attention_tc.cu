@@ -56,7 +56,6 @@ constexpr int kMinTiles = 6;                 // a part's fewest tiles
 constexpr int kMaxPartTiles = 256;           // at most 1024 block ids and scales in shared memory
 constexpr int kMaxDrafts = 4096;             // whose positions are kept in shared memory
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kLn2 = 0.6931471805599453f;
 // log2 growth of the maximum, and of the V scale over its reference, that moves them: P
 // stays below 2^12 in float16
 constexpr float kGrowth = 8.f, kVGrowth = 4.f;
@@ -669,7 +668,7 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
       const int64_t prow = orow * L.splits + split;
       const bool store = live && (direct ? dbg_in(orow, (int64_t)a.B * a.D_max * a.Hq, a.status)
                                          : dbg_in(prow, (int64_t)a.B * a.D_max * a.Hq * L.splits, a.status));
-      const float inv = l_run > 0.f ? v_ref / l_run : 0.f;
+      const float inv = v_ref / l_run;
 #pragma unroll 1
       for (int c = 0; c < D / 32; ++c) {
         float ov[32];
@@ -679,10 +678,9 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
           uint4* ob = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(a.o) + orow * D + c * 32);
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            // (a row that sees no key: 0, whatever its products are)
             float x[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = l_run > 0.f ? ov[8 * i + e] * inv : 0.f;
+            for (int e = 0; e < 8; ++e) x[e] = row_value(ov[8 * i + e], inv, l_run);
             ob[i] = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]),
                                pack_bf16x2(x[6], x[7]));
           }
@@ -697,8 +695,7 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
       if (store) {
         if (!direct) L.part_ml[prow] = make_float2(m_run, l_run);
         else if (a.lse != nullptr)
-          a.lse[((int64_t)b * a.Hq + h) * a.D_max + j] =
-              l_run > 0.f ? (m_run + log2f(l_run)) * kLn2 : -INFINITY;
+          a.lse[((int64_t)b * a.Hq + h) * a.D_max + j] = row_lse(m_run, l_run);
       }
     }
   }

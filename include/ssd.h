@@ -617,9 +617,10 @@ ssd_status ssd_cache_append(const ssd_block_cache* cache, const ssd_rotary* rota
  * draft_pos[b][j'], or cache_len + j' if draft_pos is NULL: plain causal
  * decoding, one token each with D_max = 1).  A query that sees no key gets
  * o = 0 and lse = -inf.  Slots outside the sequence's tokens may hold anything.
- * A NaN in a query or in a token's key gives NaN (o and lse) in the rows that
- * see it and in no other; a NaN in a token's value gives NaN in its column of o
- * in those rows, and may in the rows of its head that see other tokens only.
+ * A NaN or an infinity in a query and a NaN in a token's key give NaN (o and
+ * lse) in the rows that see a token, and that token, and in no other; a NaN in
+ * a token's value gives NaN in its column of o in the rows that see the token,
+ * and may in the rows of its head that see other tokens only.
  *   q          dev bf16 [B][D_max][Hq][d] (rotated); scale 0 -> 1/sqrt(d)
  *   cache_len, n_drafts  dev int32 [B]; draft_pos dev int32 [B][D_max] or NULL
  *   key_start  dev int32 [B] or NULL (0): the first token that may be seen

@@ -247,7 +247,8 @@ cache_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
       m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2));
       // 2^e with m / 2^e in [1, 2) (or less, for the smallest; 4, for the largest)
       const int32_t e = min(126, max(-126, (int32_t)(__float_as_uint(m) >> 23) - 127));
-      const float down = __uint_as_float((uint32_t)(127 - e) << 23);
+      // (an infinity: every product of the row is NaN, as its softmax is)
+      const float down = m == INFINITY ? NAN : __uint_as_float((uint32_t)(127 - e) << 23);
       rowc_of[n] = c2 * __uint_as_float((uint32_t)(127 + e) << 23);
 #pragma unroll
       for (int kg = 0; kg < KG; ++kg)

@@ -345,7 +345,8 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
     m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 1));
     // 2^(7 - e), e the exponent of the largest entry
     const int32_t e = (int32_t)(__float_as_uint(m) >> 23) - 127, up = max(-120, min(126, 7 - e));
-    const float f = __uint_as_float((uint32_t)(up + 127) << 23);
+    // (an infinity, which e4m3 would clamp: every product of the row is NaN, as its softmax is)
+    const float f = m == INFINITY ? NAN : __uint_as_float((uint32_t)(up + 127) << 23);
     if (half == 0)
       sh.rowc[q_row] = (a.scale != 0.f ? a.scale : rsqrtf((float)D)) * kLog2e *
                        __uint_as_float((uint32_t)(127 - up) << 23);

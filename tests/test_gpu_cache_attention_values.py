@@ -1,9 +1,9 @@
-"""ssd_cache_attention where what a row sees is not a number.  Every kernel and cut: a CTA's 8 or 16 rows and the
-tensor-core kernel (from 17 rows under a table for many tokens), sequences that are whole
-and sequences cut into parts.
+"""ssd_cache_attention where what a row sees is not finite.  Every kernel and cut: a CTA's
+8 or 16 rows and the tensor-core kernel (from 17 rows under a table for many tokens), sequences
+that are whole and sequences cut into parts.
 
 A NaN in a key's K reaches the rows that see the key, one in its V that column of them (and may
-reach it in rows of the head that see other keys only); one in a query its row.
+reach it in rows of the head that see other keys only); a NaN or an infinity in a query its row.
 Their log-sum-exp is NaN for K and the query.  A row that sees nothing is 0 and -inf all the same.
 
 Tolerances of the others, per entry: bf16 of the output (2^-8 of it) and of a probability (2^-8 of
@@ -173,7 +173,7 @@ def test_nan_in_a_value(ssd, path, d):  # noqa: F811
 
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("path", PATHS)
-@pytest.mark.parametrize("what", ["nan"])
+@pytest.mark.parametrize("what", ["nan", "inf", "-inf"])
 def test_a_query_that_is_not_finite(ssd, path, d, what):  # noqa: F811
     c = Call(path, d)
     j, h = c.D // 2, c.Hq - 1

@@ -509,7 +509,7 @@ ssd_status ssd_draft_predict(int32_t rows, int32_t d, int32_t m, int32_t V, cons
  * with one float32 scale per block and KV head: the value of an entry is
  * scale * e4m3.
  *   k, v              dev e4m3 [num_blocks][Hkv][block][d], 16-byte aligned
- *   k_scale, v_scale  dev float32 [num_blocks][Hkv]
+ *   k_scale, v_scale  dev float32 [num_blocks][Hkv], finite and not negative
  * Supported: d in {64, 128}; block in {16, 32, 64, 128}; num_blocks * Hkv *
  * block < 2^31 (indexes of values are 64-bit).  Blocks may be shared by
  * sequences that only read them; two sequences must not append to one block.

@@ -45,9 +45,8 @@ constexpr int kStep = 16;           // keys per step
 constexpr int kCtas = 3;            // per SM
 constexpr int kMinTiles = 8;        // a part's fewest tiles
 constexpr float kLog2e = 1.4426950408889634f;
-// log2 growth of the running maximum (and growth of the V scale) that moves the
-// reference: P stays below 2^8 * 2^4 in float16
-constexpr float kGrowth = 8.f, kVGrowth = 16.f;
+constexpr float kMostP = 256.f;     // a probability beyond it moves its reference
+constexpr float kUnseen = -3.402823466e38f;  // reference of a row that has seen no key
 
 struct Plan {
   int32_t rows, row_groups;  // rows of a CTA, CTAs with other rows of the same keys
@@ -292,15 +291,19 @@ cache_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
     }
 
     float o[NR][NT][4];
-    float m_ref[NR][2], l[NR][2];
+    // A row's two references: m_ref (log2) of its scores, for the sum, and 1 / v_inv, a power of
+    // two, of its probabilities times their V scales.  Those go into the product as float16,
+    // below kMostP and with the largest at least 1, whatever the scales of keys that the row
+    // does not see or hardly weighs.
+    float m_ref[NR][2], v_inv[NR][2], l[NR][2];
 #pragma unroll
     for (int n = 0; n < NR; ++n) {
 #pragma unroll
       for (int t = 0; t < NT; ++t) o[n][t][0] = o[n][t][1] = o[n][t][2] = o[n][t][3] = 0.f;
-      m_ref[n][0] = m_ref[n][1] = -INFINITY;
+      m_ref[n][0] = m_ref[n][1] = kUnseen;
+      v_inv[n][0] = v_inv[n][1] = 1.f;
       l[n][0] = l[n][1] = 0.f;
     }
-    float v_ref = 0.f, v_inv = 0.f;
     bool ok = true;
     int32_t t = 0;
 #pragma unroll 1
@@ -389,20 +392,28 @@ cache_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
           }
         }
       }
-      // ---- softmax against a reference maximum that moves when it falls behind
-      bool behind = !(vs <= v_ref * kVGrowth);  // the same in every lane
+      // ---- softmax against references that move when they fall behind
+      float p[NR][4], ratio[NR][2];
+      auto weigh = [&]() {
+#pragma unroll
+        for (int n = 0; n < NR; ++n) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) p[n][e] = ex2_approx(x[n][e] - m_ref[n][e & 1]);
+          ratio[n][0] = vs * v_inv[n][0];
+          ratio[n][1] = vs * v_inv[n][1];
+        }
+      };
+      weigh();
+      bool behind = false;
 #pragma unroll
       for (int n = 0; n < NR; ++n)
 #pragma unroll
-        for (int u = 0; u < 2; ++u) behind |= fmaxf(x[n][u], x[n][2 + u]) > m_ref[n][u] + kGrowth;
-      if (__any_sync(0xffffffffu, behind)) {
-        float f = 1.f;
-        if (!(vs <= v_ref * kVGrowth)) {
-          const float to = fmaxf(vs, 0x1p-120f);
-          f = v_ref / to;
-          v_ref = to;
-          v_inv = 1.f / to;
+        for (int u = 0; u < 2; ++u) {
+          const float top = fmaxf(p[n][u], p[n][2 + u]);
+          behind |= fmaxf(top, top * ratio[n][u]) > kMostP;
         }
+      if (__any_sync(0xffffffffu, behind)) {
+        const float lg = fmaxf(log2f(vs), -120.f);
 #pragma unroll
         for (int n = 0; n < NR; ++n) {
           float al[2];
@@ -411,11 +422,15 @@ cache_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
             float m = fmaxf(x[n][u], x[n][2 + u]);
 #pragma unroll
             for (int s = 4; s < 32; s <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, s));
-            m = fmaxf(m_ref[n][u], m);
-            al[u] = m == -INFINITY ? 1.f : exp2f(m_ref[n][u] - m);
+            const float old = m_ref[n][u];
+            const int32_t dv_old = 127 - (int32_t)(__float_as_uint(v_inv[n][u]) >> 23);
+            const float m_v = fmaxf(old + (float)dv_old, m + lg);
+            m = fmaxf(old, m);
+            const int32_t dv = min(126, max(-126, __float2int_rd(m_v - m)));
             m_ref[n][u] = m;
-            l[n][u] *= al[u];
-            al[u] *= f;
+            v_inv[n][u] = __uint_as_float((uint32_t)(127 - dv) << 23);
+            l[n][u] *= exp2f(old - m);
+            al[u] = exp2f(old - m + (float)(dv_old - dv));
           }
 #pragma unroll
           for (int c = 0; c < NT; ++c) {
@@ -425,21 +440,18 @@ cache_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
             o[n][c][3] *= al[1];
           }
         }
+        weigh();
       }
-      const float ratio = vs * v_inv;
       uint32_t pf[NR][2];
 #pragma unroll
-      for (int n = 0; n < NR; ++n) {
-        const float m0 = m_ref[n][0] == -INFINITY ? 0.f : m_ref[n][0];
-        const float m1 = m_ref[n][1] == -INFINITY ? 0.f : m_ref[n][1];
+      for (int n = 0; n < NR; ++n)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const float p0 = ex2_approx(x[n][2 * h] - m0), p1 = ex2_approx(x[n][2 * h + 1] - m1);
+          const float p0 = p[n][2 * h], p1 = p[n][2 * h + 1];
           l[n][0] += p0;
           l[n][1] += p1;
-          pf[n][h] = transpose8x8(pack_f16x2(p0 * ratio, p1 * ratio));
+          pf[n][h] = transpose8x8(pack_f16x2(p0 * ratio[n][0], p1 * ratio[n][1]));
         }
-      }
       // ---- O^T += V^T P^T: output tile c holds columns r8 * VB + 2 c and the next
 #pragma unroll
       for (int w = 0; w < VB / 4; ++w)
@@ -472,6 +484,7 @@ cache_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
           const int32_t r = 8 * n + 2 * q + u;
 #pragma unroll
           for (int s = 4; s < 32; s <<= 1) l[n][u] += __shfl_xor_sync(0xffffffffu, l[n][u], s);
+          const float v_ref = 1.f / v_inv[n][u];
 #pragma unroll
           for (int c = 0; c < NT; c += 2)
             *reinterpret_cast<float4*>(mine + r * kRowFloats + r8 * VB + 2 * c) =

@@ -9,7 +9,7 @@
 // power of two (largest entry in [128, 256)).  P, which changes with every tile, is rounded to
 // float16 instead (a split takes six instructions a pair, and the softmax is what bounds this
 // kernel): two warps widen V to float16, exactly, and the second product is kind::f16.  The K
-// scale of a block multiplies the scores, its V scale over a reference the probabilities.
+// scale of a block multiplies the scores, its V scale over the row's reference the probabilities.
 //
 // One CTA (8 warps, two CTAs per SM) per tile of 128 query rows (drafts x the query
 // heads of a KV head) and part of the sequence's keys, longest sequences first:
@@ -21,8 +21,10 @@
 //    warps, with another for each product, they took issue slots from the softmax by waiting
 //    (25 x 48 drafts 34.3 us, 29.3 now);
 //  warps 0-3 (a thread a row, with the registers that the other warps give up) turn S into
-//    P.  The running maximum moves only when it grows by more than 2^8; O is rescaled in
-//    TMEM when it does, or when a block's V scale is above 16 times the reference.
+//    P.  A row has two references, of its scores (for the sum) and of its scores times their
+//    V scales (for P), so P's float16 holds the row whatever the scales of keys that it does not
+//    see or hardly weighs.  A reference moves only when its maximum grows by more than 2^8; O is
+//    rescaled in TMEM when the second one does.
 //
 // 128 drafts of 8 sequences over 2300 to 3800 keys, 32 heads (222 MB, 51 GFLOP): 72 us, 3.1 TB/s,
 // 0.45 of the measured copy rate; the tensor pipe is busy for a quarter of it.  A tile takes
@@ -56,9 +58,9 @@ constexpr int kMinTiles = 6;                 // a part's fewest tiles
 constexpr int kMaxPartTiles = 256;           // at most 1024 block ids and scales in shared memory
 constexpr int kMaxDrafts = 4096;             // whose positions are kept in shared memory
 constexpr float kLog2e = 1.4426950408889634f;
-// log2 growth of the maximum, and of the V scale over its reference, that moves them: P
-// stays below 2^12 in float16
-constexpr float kGrowth = 8.f, kVGrowth = 4.f;
+// log2 growth of a row's maxima that moves their references: P stays below 2^8 in float16
+constexpr float kGrowth = 8.f;
+constexpr float kLeastVScale = 0x1p-110f;    // lesser ones count as this (an append's is 2^-109)
 // Bytes of one term of Q, a K (or V) tile and a V tile in float16.
 __host__ __device__ constexpr int q_bytes(int d) { return kBM * d; }
 __host__ __device__ constexpr int tile_bytes(int d) { return KT * d; }
@@ -202,7 +204,7 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
   unsigned char* sV = sK + kNK * kTileBytes;
   unsigned char* sW = sV + kNV * kTileBytes;       // V in float16 [2][d / 64][KT][128 bytes]
   Shared& sh = *reinterpret_cast<Shared*>(sW + 2 * kWideBytes);
-  // the part's blocks: id (-1: outside the pool), K scale, log2 of the V scale, its inverse
+  // the part's blocks: K scale, log2 of the V scale, its inverse, id (-1: outside the pool)
   float4* s_blk = reinterpret_cast<float4*>(&sh + 1);
   int32_t* s_flat = reinterpret_cast<int32_t*>(s_blk + L.max_blocks);  // the drafts' positions
   const bool staged = a.draft_pos != nullptr && a.D_max <= kMaxDrafts;
@@ -309,9 +311,9 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
       bad = true;
     }
     const int64_t at = (int64_t)max(id, 0) * Hkv + g;
-    const float vs = a.cache.v_scale[at];
-    s_blk[i] = make_float4(a.cache.k_scale[at], id < 0 ? -INFINITY : log2f(vs), 1.f / vs,
-                           __int_as_float(id));
+    const float vs = a.cache.v_scale[at], least = fmaxf(vs, kLeastVScale);
+    s_blk[i] = make_float4(a.cache.k_scale[at], id >= 0 && vs > 0.f ? log2f(least) : -INFINITY,
+                           1.f / least, __int_as_float(id));
   }
   if (a.draft_pos != nullptr) {
     for (int32_t j = stages ? tid - 128 : nd; j < nd; j += 128) {
@@ -535,8 +537,9 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
     if (r < rows_total) qpos = flat_of(j);
     // keys below this one are visible to every row of the warp
     const int32_t mask_from = min(cache, __reduce_min_sync(0xffffffffu, qpos) + 1);
-    float m_run = -INFINITY, l_run = 0.f;
-    float lg_ref = -INFINITY, v_ref = 0.f;  // reference of the V scales and its log2
+    // references (log2) of the scores, for the sum, and of the scores times their V scales, for
+    // P; v_ref = 2^(m_v - m_run)
+    float m_run = -INFINITY, m_v = -INFINITY, v_ref = 0.f, l_run = 0.f;
     bool ok = true;
     int32_t t = 0;
 #pragma unroll 1
@@ -561,7 +564,6 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
           iv[i] = x.z;
         }
       }
-      const float lg_max = fmaxf(fmaxf(lg[0], lg[1]), fmaxf(lg[2], lg[3]));
       ok = ok && wait_warp(&sh.s_full[sb], (t >> 1) & 1, a.status);
       if (!ok) break;
       tc_fence_after();
@@ -586,7 +588,7 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
           for (int i = 0; i < 64; ++i)
             if (!(keep >> i & 1ull)) sv[i] = -INFINITY;
         }
-        float mx = -INFINITY;
+        float mx = -INFINITY, mxv = -INFINITY;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const float* x = sv + 16 * i;
@@ -596,21 +598,19 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
             y = fmax3(y, x[e], x[e + 1]);
             z = fmax3(z, x[e + 2], x[e + 3]);
           }
-          mx = fmaxf(mx, fmax3(fmaxf(y, z), x[14], x[15]) * f[i]);
+          const float top = fmax3(fmaxf(y, z), x[14], x[15]) * f[i];
+          mx = fmaxf(mx, top);
+          mxv = fmaxf(mxv, top + lg[i]);
         }
         float alpha = 1.f;
         bool moved = false;
-        if (mx > m_run + kGrowth || (m_run == -INFINITY && mx > -INFINITY)) {
-          alpha = m_run == -INFINITY ? 0.f : ex2_approx(m_run - mx);
+        if (mx > m_run + kGrowth) {  // (of nothing: -inf, and a factor of 0)
+          l_run *= ex2_approx(m_run - mx);
           m_run = mx;
-          moved = true;
         }
-        l_run *= alpha;
-        if (lg_max > lg_ref + kVGrowth || (lg_ref == -INFINITY && lg_max > -INFINITY)) {
-          // (the same in every thread)
-          alpha *= lg_ref == -INFINITY ? 0.f : exp2f(lg_ref - lg_max);
-          lg_ref = lg_max;
-          v_ref = exp2f(lg_ref);
+        if (mxv > m_v + kGrowth) {
+          alpha = ex2_approx(m_v - mxv);
+          m_v = mxv;
           moved = true;
         }
         if (t > 0 && __any_sync(0xffffffffu, moved)) {
@@ -626,14 +626,16 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
             tmem_st16(tO + lane_off + c * 16, ov);
           }
         }
-        const float m = m_run == -INFINITY ? 0.f : m_run;
+        const float m = m_run == -INFINITY ? 0.f : m_run, v_lg = m_v - m_run;
+        v_ref = m_run == -INFINITY ? 0.f : ex2_approx(v_lg);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           uint32_t pk[8];
           // P times its V scale over the reference, in the exponent.  A block whose scale is
-          // next to nothing beside the reference (and one outside the pool) adds to the sum alone.
-          const bool tiny = !(lg[i] - lg_ref > -60.f);
-          const float off = tiny ? -m : lg[i] - lg_ref - m;
+          // next to nothing beside the reference (or 0, a block outside the pool, a row that has
+          // seen no key) adds to the sum alone.
+          const bool tiny = !(lg[i] - v_lg > -60.f);
+          const float off = tiny ? -m : lg[i] - m_v;
           float2 s2[2];
 #pragma unroll
           for (int e = 0; e < 8; ++e) {

@@ -1,6 +1,7 @@
-"""ssd_cache_attention where what a row sees is not finite.  Every kernel and cut: a CTA's
-8 or 16 rows and the tensor-core kernel (from 17 rows under a table for many tokens), sequences
-that are whole and sequences cut into parts.
+"""ssd_cache_attention where the values are awkward: NaN and infinities in what a row sees,
+and V scales that lie far apart.  Every kernel and cut: a CTA's 8 or 16 rows and the
+tensor-core kernel (from 17 rows under a table for many tokens), sequences that are whole
+and sequences cut into parts.
 
 A NaN in a key's K reaches the rows that see the key, one in its V that column of them (and may
 reach it in rows of the head that see other keys only); a NaN or an infinity in a query its row.
@@ -186,3 +187,53 @@ def test_a_query_that_is_not_finite(ssd, path, d, what):  # noqa: F811
     c.start = 2 ** 30  # (sees no key)
     o, lse = c.run(ssd)
     assert bool((o == 0).all()) and bool((lse == -torch.inf).all())
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("path", PATHS)
+@pytest.mark.parametrize("log2", [20, 40, 90])
+def test_large_values_that_hardly_weigh(ssd, path, d, log2):  # noqa: F811
+    """The first block's V are 2^log2 times the others', and its keys' scores 100 below: the row
+    is what the others give (their weights are e^100 = 2^144 times as large)."""
+    c = Call(path, d)
+    first = c.ids[0]
+    c.vs *= 2.0 ** -30
+    c.vs[first] *= 2.0 ** log2
+    c.q[..., 0] = 8.0
+    c.k[..., 0] = 0
+    c.ks[first] = 100 * d ** 0.5 / 8 / 448
+    c.k[first] = 0
+    c.k[first, :, :, 0] = 0xfe  # -448
+    o, lse = c.run(ssd)
+    c.check(o, lse)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("path", PATHS)
+@pytest.mark.parametrize("step", [-5.0, 5.0, 0.0])
+def test_value_scales_that_rise_and_fall(ssd, path, d, step):  # noqa: F811
+    """By 2^step from block to block (up to 2^60), or zero for every other block."""
+    c = Call(path, d)
+    i = torch.arange(c.need, device="cuda")
+    c.vs[c.ids[:c.need]] *= torch.exp2(step * i.clamp(max=12))[:, None]
+    if step == 0.0:
+        c.vs[c.ids[:c.need:2]] = 0.0
+    o, lse = c.run(ssd)
+    c.check(o, lse)
+    c.vs[c.ids[:c.need]] = 0.0
+    o, lse = c.run(ssd)
+    assert bool((o == 0).all())
+    c.check(o, lse)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("path", [p for p in PATHS if PATHS[p][0] > BLOCK])
+def test_large_values_of_drafts_that_are_not_seen(ssd, path, d):  # noqa: F811
+    """The first 16 drafts come behind the others in the grid and have V 2^40 times as large."""
+    c = Call(path, d)
+    n = c.D - BLOCK
+    c.draft_pos = list(range(c.cache + n, c.cache + c.D)) + list(range(c.cache, c.cache + n))
+    c.vs *= 2.0 ** -30
+    c.vs[c.ids[c.cache // BLOCK]] *= 2.0 ** 40
+    o, lse = c.run(ssd)
+    c.check(o, lse)

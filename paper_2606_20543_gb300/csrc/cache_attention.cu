@@ -552,20 +552,18 @@ __global__ void __launch_bounds__(256) cache_attn_combine_kernel(CacheAttnArgs a
   int32_t parts;
   int64_t at, step = 1, room;
   if (L.info != nullptr) {
-    const int2 x = L.info[b];
-    const int32_t G = a.Hq / a.cache.Hkv, g = h / G, r = j * G + (h - g * G);
-    const int32_t z = r / L.group_rows;
-    const int64_t slots = L.per_head + a.B;
-    parts = x.y - x.x + 1;
+    const int32_t G = a.Hq / a.cache.Hkv, g = h / G;
+    const CacheShares x = cache_shares(L, a.B, b, L.info[b], g, j * G + (h - g * G));
+    parts = x.parts;
     step = L.group_rows;
-    at = (((int64_t)g * L.row_groups + z) * slots + x.x + b) * step + (r - z * L.group_rows);
-    room = (int64_t)a.cache.Hkv * L.row_groups * slots * step;
+    at = x.at;
+    room = (int64_t)a.cache.Hkv * L.row_groups * (L.per_head + a.B) * step;
   } else {
     parts = cache_parts(L.splits, L.min_tiles, (cache + nd + kCacheTile - 1) / kCacheTile);
     at = row * L.splits;
     room = (int64_t)a.B * a.D_max * a.Hq * L.splits;
   }
-  if (parts <= 1) return;  // written by the attention kernel
+  if (parts <= 1) return;  // written by the attention kernel (or no part is known)
   if (!dbg_in(at + (parts - 1) * step, room, a.status)) return;
   float M = -INFINITY;
   for (int32_t s = lane; s < parts; s += 32) M = fmaxf(M, L.part_ml[at + s * step].x);

@@ -39,6 +39,25 @@ inline int32_t cache_part_tiles(int32_t splits, int32_t min_tiles, int32_t tiles
   return splits == 1 ? tiles : (even > few ? even : few);
 }
 
+// A row's shares that the CTAs of CacheWork left: the first one's place among the part rows (the
+// next is group_rows on), and how many.  `row`: of the KV head's rows of sequence b; `cut`:
+// L.info[b].  A CTA that gave up on a wait leaves the info of its later sequences unwritten, so
+// what is no range of CTAs stands for none.
+struct CacheShares {
+  int64_t at;
+  int32_t parts;
+};
+__host__ __device__ __forceinline__ CacheShares cache_shares(const CacheAttnLaunch& L, int32_t B,
+                                                             int32_t b, int2 cut, int32_t g,
+                                                             int32_t row) {
+  if (cut.x < 0 || cut.y < cut.x || cut.y >= L.per_head) return CacheShares{0, 0};
+  const int32_t z = row / L.group_rows;
+  const int64_t slots = L.per_head + B;
+  return CacheShares{(((int64_t)g * L.row_groups + z) * slots + cut.x + b) * L.group_rows +
+                         (row - z * L.group_rows),
+                     cut.y - cut.x + 1};
+}
+
 // mbar_wait_warp() with one try ahead of the loop: a wait for what is there already takes a try
 // and a vote (through the loop 220 cycles on a busy SM, of the 2200 that a tile of 64 keys takes).
 __device__ __forceinline__ bool wait_warp(uint64_t* bar, uint32_t parity, int32_t* status) {

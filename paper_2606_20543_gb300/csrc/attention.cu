@@ -20,6 +20,8 @@
 // Long caches are split over CTAs; a combine kernel merges the splits by
 // their log-sum-exp.
 
+#include <atomic>
+
 #include "kernels.cuh"
 
 namespace ssd {
@@ -447,19 +449,41 @@ Plan make_plan(int32_t B, int32_t Hq, int32_t Hkv, int32_t d, int32_t D_max, int
 
 size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 
+std::atomic<EncodeTiledFn> encode_tiled_driver{nullptr};
+
+// cuTensorMapEncodeTiled, also from a host thread that has made no CUDA call yet: the driver
+// wants a current context, which the runtime gives the thread.  (Only where there is none, so a
+// context that the caller made current stays.)
+CUresult encode_tiled(CUtensorMap* map, CUtensorMapDataType type, cuuint32_t rank, void* base,
+                      const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box,
+                      const cuuint32_t* elements, CUtensorMapInterleave interleave,
+                      CUtensorMapSwizzle swizzle, CUtensorMapL2promotion promotion,
+                      CUtensorMapFloatOOBfill fill) {
+  EncodeTiledFn fn = encode_tiled_driver.load(std::memory_order_relaxed);
+  auto encode = [&]() {
+    return fn(map, type, rank, base, dims, strides, box, elements, interleave, swizzle, promotion,
+              fill);
+  };
+  const CUresult r = encode();
+  if (r != CUDA_ERROR_INVALID_CONTEXT && r != CUDA_ERROR_NOT_INITIALIZED) return r;
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaSetDevice(dev) != cudaSuccess) return r;
+  return encode();
+}
+
 }  // namespace
 
 EncodeTiledFn tensor_map_encoder() {
-  static EncodeTiledFn fn = nullptr;
-  if (fn == nullptr) {
+  if (encode_tiled_driver.load(std::memory_order_relaxed) == nullptr) {
     void* p = nullptr;
     cudaDriverEntryPointQueryResult q;
     if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault,
-                                         &q) == cudaSuccess &&
-        q == cudaDriverEntryPointSuccess)
-      fn = reinterpret_cast<EncodeTiledFn>(p);
+                                         &q) != cudaSuccess ||
+        q != cudaDriverEntryPointSuccess)
+      return nullptr;
+    encode_tiled_driver.store(reinterpret_cast<EncodeTiledFn>(p), std::memory_order_relaxed);
   }
-  return fn;
+  return encode_tiled;
 }
 
 bool bf16_tensor_map(CUtensorMap* map, const void* base, uint32_t rank, const uint64_t* dims,

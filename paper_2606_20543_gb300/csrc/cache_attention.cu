@@ -621,12 +621,14 @@ cudaError_t launch_mma(const CacheAttnArgs& a, const Plan& p, const CacheAttnLau
   CUtensorMap tk, tv;
   if (!step_map(&tk, a.cache.k, a.cache) || !step_map(&tv, a.cache.v, a.cache))
     return cudaErrorInvalidValue;
-  const size_t smem = 1024 + (size_t)W * kStages * 2 * kStep * D + (size_t)L.max_blocks * 12;
-  const cudaError_t e = cudaFuncSetAttribute(
-      cache_attn_kernel<D, NR, W>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  auto smem = [](int32_t blocks) {
+    return 1024 + (size_t)W * kStages * 2 * kStep * D + (size_t)blocks * 12;
+  };
+  const cudaError_t e =
+      allow_smem(cache_attn_kernel<D, NR, W>, smem(part_blocks(kWorkRoom, kLeastBlock)));
   if (e != cudaSuccess) return e;
   return launch_kernel(cache_attn_kernel<D, NR, W>, dim3(p.per_head, a.cache.Hkv, p.row_groups),
-                       dim3(W * 32), smem, stream, true, tk, tv, a, L);
+                       dim3(W * 32), smem(L.max_blocks), stream, true, tk, tv, a, L);
 }
 
 size_t part_bytes(int64_t rows, int32_t d) {
@@ -678,7 +680,7 @@ cudaError_t launch_cache_attention(const CacheAttnArgs& a, void* ws, cudaStream_
     rows = mma_part_rows(a.B, a.cache.Hkv, p);
     part_tiles = std::min(tiles, kWorkRoom);
   }
-  L.max_blocks = part_tiles * (kCacheTile / std::min(a.cache.block, 64)) + 1;
+  L.max_blocks = part_blocks(part_tiles, a.cache.block);
   if (rows > 0) {
     unsigned char* at = static_cast<unsigned char*>(ws);
     L.part_o = reinterpret_cast<float*>(at);

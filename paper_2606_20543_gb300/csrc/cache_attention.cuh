@@ -33,6 +33,11 @@ __host__ __device__ __forceinline__ int32_t cache_parts(int32_t splits, int32_t 
   const int32_t n = tiles / min_tiles;
   return n < 1 ? 1 : (n < splits ? n : splits);
 }
+constexpr int kLeastBlock = 16;  // tokens
+// Most blocks that so many tiles lie in (a part may start inside a block of 128 tokens).
+inline int32_t part_blocks(int32_t tiles, int32_t block) {
+  return tiles * (kCacheTile / (block < kCacheTile ? block : kCacheTile)) + 1;
+}
 // Most tiles of a part of any sequence of at most `tiles` tiles.
 inline int32_t cache_part_tiles(int32_t splits, int32_t min_tiles, int32_t tiles) {
   const int32_t even = tiles / splits + 1, few = 2 * min_tiles;  // n < splits: tiles / n < 2 min

@@ -731,16 +731,19 @@ cudaError_t launch(const CacheAttnArgs& a, const CacheAttnLaunch& L, cudaStream_
   CUtensorMap tk, tv;
   if (!cache_map(&tk, a.cache.k, rows, box, D) || !cache_map(&tv, a.cache.v, rows, box, D))
     return cudaErrorInvalidValue;
-  const size_t smem = 1024 + 2 * q_bytes(D) + (kNK + kNV) * tile_bytes(D) + 2 * wide_bytes(D) +
-                      sizeof(Shared) + (size_t)L.max_blocks * 16 +
-                      (a.draft_pos != nullptr && a.D_max <= kMaxDrafts ? (size_t)a.D_max * 4 : 0);
-  const cudaError_t e = cudaFuncSetAttribute(
-      cache_attn_tc_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  auto smem = [](int32_t blocks, int32_t drafts) {
+    return 1024 + 2 * q_bytes(D) + (kNK + kNV) * tile_bytes(D) + 2 * wide_bytes(D) + sizeof(Shared) +
+           (size_t)blocks * 16 + (size_t)drafts * 4;
+  };
+  // (a part has at most a tile more than kMaxPartTiles)
+  const cudaError_t e = allow_smem(cache_attn_tc_kernel<D>,
+                                   smem(part_blocks(kMaxPartTiles + 1, kLeastBlock), kMaxDrafts));
   if (e != cudaSuccess) return e;
   const int64_t grid = (int64_t)a.B * a.cache.Hkv * mtiles * L.splits;
   if (grid > INT32_MAX) return cudaErrorInvalidValue;
-  return launch_kernel(cache_attn_tc_kernel<D>, dim3((unsigned)grid), dim3(kThreadsTC), smem, stream,
-                       true, tk, tv, a, L, mtiles);
+  return launch_kernel(cache_attn_tc_kernel<D>, dim3((unsigned)grid), dim3(kThreadsTC),
+                       smem(L.max_blocks, a.draft_pos != nullptr && a.D_max <= kMaxDrafts ? a.D_max : 0),
+                       stream, true, tk, tv, a, L, mtiles);
 }
 
 }  // namespace

@@ -30,6 +30,14 @@ __device__ __forceinline__ int32_t frontier_drafts(const ssd_grid& g, int32_t ca
   return n > D_max ? -1 : n;  // the host checks D_max >= (k_v + 1) W; keep the guard
 }
 
+// Let launches of `kernel` take up to `most` bytes of dynamic shared memory.  The limit belongs to
+// the process: `most` is what any call takes, not this one, or a call could lower it between
+// another host thread's call of this and its launch, which is then refused.
+template <typename Kernel>
+cudaError_t allow_smem(Kernel kernel, size_t most) {
+  return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most);
+}
+
 // Launch `kernel`, optionally as a programmatic dependent of the kernel
 // before it on `stream` (cudaLaunchAttributeProgrammaticStreamSerialization).
 // Every kernel but the cooperative ones and the mma.sync attention is launched so.

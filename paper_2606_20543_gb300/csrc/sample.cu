@@ -1029,15 +1029,15 @@ __global__ void __launch_bounds__(NT, 1024 / NT) sample_kernel(SampleArgs a) {
 template <int NT, bool BF16>
 cudaError_t launch(const SampleArgs& a, cudaStream_t stream) {
   // (a row may begin up to 7 entries behind its first chunk's begin)
-  const size_t smem =
-      sizeof(SampleShared<NT>) + (size_t)((a.V + 7 + kChunk - 1) / kChunk) * sizeof(u64);
-  const cudaError_t e = cudaFuncSetAttribute(
-      sample_kernel<NT, BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  auto smem = [](int32_t V) {
+    return sizeof(SampleShared<NT>) + (size_t)((V + 7 + kChunk - 1) / kChunk) * sizeof(u64);
+  };
+  const cudaError_t e = allow_smem(sample_kernel<NT, BF16>, smem(kSampleMaxV));
   if (e != cudaSuccess) return e;
   // a row per CTA, dealt by the hardware as CTAs end
   const unsigned blocks = (unsigned)std::min<int64_t>(a.rows, 1 << 20);
-  return launch_kernel(sample_kernel<NT, BF16>, dim3(blocks), dim3(NT), smem, stream, true,
-                       a);
+  return launch_kernel(sample_kernel<NT, BF16>, dim3(blocks), dim3(NT), smem(a.V), stream,
+                       true, a);
 }
 
 }  // namespace

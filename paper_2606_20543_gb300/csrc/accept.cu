@@ -816,15 +816,16 @@ bool accept_supported(int32_t V) { return V <= kMaxV; }
 
 cudaError_t launch_accept(const AcceptArgs& a, cudaStream_t stream) {
   if (a.rows == 0) return cudaSuccess;
-  const int32_t nch = (a.V + kChunk - 1) / kChunk;
-  const size_t smem = (size_t)kStages * 2 * kChunk * sizeof(float) +
-                      (size_t)nch * kBlocksPerChunk * sizeof(float);
+  auto smem = [](int32_t V) {
+    return (size_t)kStages * 2 * kChunk * sizeof(float) +
+           (size_t)((V + kChunk - 1) / kChunk) * kBlocksPerChunk * sizeof(float);
+  };
   const int64_t grid = std::min<int64_t>(a.rows, (int64_t)kCtasPerSm * device_sm_count());
   auto launch = [&](auto kernel) {
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                         (int)smem);
+    const cudaError_t e = allow_smem(kernel, smem(kMaxV));
     if (e != cudaSuccess) return e;
-    return launch_kernel(kernel, dim3((unsigned)grid), dim3(kThreads), smem, stream, /*pdl=*/true, a);
+    return launch_kernel(kernel, dim3((unsigned)grid), dim3(kThreads), smem(a.V), stream, /*pdl=*/true,
+                         a);
   };
   switch (a.strategy) {
     case SSD_STRATEGY_GREEDY: return launch(accept_kernel<SSD_STRATEGY_GREEDY, false>);

@@ -828,14 +828,12 @@ ssd_status lmhead_check(int32_t rows, int32_t V, int32_t K) {
   int64_t resident = 0;
   if (row_pairs(rows)) {
     LmConfig c(rows, V, smem, nullptr);
-    if (cudaFuncSetAttribute(lmhead_accept_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                             (int)smem) != cudaSuccess ||
+    if (allow_smem(lmhead_accept_kernel<true>, kMaxSmem) != cudaSuccess ||
         cudaOccupancyMaxActiveClusters(&n, lmhead_accept_kernel<true>, &c.cfg) != cudaSuccess)
       return SSD_ERR_CUDA;
     resident = 2 * (int64_t)n;
   } else {
-    if (cudaFuncSetAttribute(lmhead_accept_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                             (int)smem) != cudaSuccess ||
+    if (allow_smem(lmhead_accept_kernel<false>, kMaxSmem) != cudaSuccess ||
         cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, lmhead_accept_kernel<false>, kThreadsL,
                                                       smem) != cudaSuccess)
       return SSD_ERR_CUDA;
@@ -876,7 +874,7 @@ cudaError_t launch_lmhead(const LmHeadArgs& a, void* ws, size_t ws_bytes, cudaSt
   }
   const size_t smem = smem_bytes(a.rows, L.ku, L.stages);
   auto launch = [&](auto kernel) {
-    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    e = allow_smem(kernel, kMaxSmem);
     if (e != cudaSuccess) return e;
     LmConfig c(a.rows, a.V, smem, stream);
     return cudaLaunchKernelEx(&c.cfg, kernel, ht, hd, wt, wd, a, L);

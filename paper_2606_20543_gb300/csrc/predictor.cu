@@ -72,6 +72,7 @@ constexpr int kEpiWarp0 = 4;         // warps 4-7: TMEM lane quarters 0-3
 constexpr int kEpiThreads = 128;
 constexpr int kUnitBytes = 32768;    // weights per unit
 constexpr int kMaxRows = 128;
+constexpr size_t kMaxSmem = 232448;  // 227 KB
 constexpr int kPhases = 4;
 constexpr int kBarEpi = 1;           // named barrier of the epilogue warps
 constexpr int kMaxSlots = 8;         // most CTAs sharing one feature tile
@@ -865,8 +866,7 @@ PredPlan make_plan(int32_t rows, int32_t d, int32_t m, int32_t V, int32_t sm_cou
   P.part_odd = (part_max[0] + 63) / 64 * 64;
   P.part_floats = P.part_odd + part_max[1];
   const size_t slot = (size_t)kUnitBytes + (size_t)P.nn * 256;
-  const size_t budget = 232448;  // 227 KB of dynamic shared memory per CTA
-  P.stages = (int32_t)std::min<size_t>(8, (budget - 1024 - 2048) / slot);
+  P.stages = (int32_t)std::min<size_t>(8, (kMaxSmem - 1024 - 2048) / slot);
   P.smem = 1024 + (size_t)P.stages * slot + (2 * P.stages + 5) * 8 + 32 + kMaxRows * 4;
   return P;
 }
@@ -988,8 +988,7 @@ cudaError_t launch_rows(const PredictorArgs& a, void* ws, size_t ws_bytes, int32
   if (!ok) return cudaErrorInvalidValue;
   cudaError_t e = launch_zero(w.ctr, (int32_t)(w.zero_bytes / 4), stream);
   if (e != cudaSuccess) return e;
-  e = cudaFuncSetAttribute(predictor_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                           (int)P.smem);
+  e = allow_smem(predictor_kernel, kMaxSmem);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)P.ncta, 1, 1);

@@ -94,3 +94,20 @@ def test_cache_attention(ssd, D, Hq, tokens):  # noqa: F811
         calls.append(call)
         outputs.append([o, st])
     together(calls, outputs)
+
+
+def test_acceptance(ssd):  # noqa: F811
+    gen = torch.Generator("cuda").manual_seed(2)
+    calls, outputs = [], []
+    for V in (256, 131072):
+        t, r = (torch.randn((1, V), generator=gen, device="cuda") for _ in range(2))
+        u = torch.rand((1, 2), generator=gen, device="cuda")
+        tok, st = (torch.zeros(1, dtype=torch.int32, device="cuda") for _ in range(2))
+        acc = torch.zeros(1, dtype=torch.uint8, device="cuda")
+        rng = ssd.rng(uniforms=u)
+
+        def call(stream, V=V, t=t, r=r, u=u, rng=rng, tok=tok, acc=acc, st=st):
+            ssd.ssd_accept(1, V, t, r, V, None, 1.0, rng, tok, acc, None, None, st, stream=stream)
+        calls.append(call)
+        outputs.append([tok, acc, st])
+    together(calls, outputs)

@@ -50,6 +50,11 @@ class PagedDecode:
         self.table = new((n_pos, d // 2, 2), torch.float32)
         ssd_rotary_table(n_pos, d // 2, freq, self.table)
         self.rotary = make_rotary(self.table, sections, interleaved)
+        # positions of the grid's tokens on the axes; before and behind them one that is refused
+        P, W, cells = grid.prefix_len, grid.grid_w, grid.grid_h * grid.grid_w
+        i = torch.arange(cells, device=device)
+        self._grid_pos = new((cells + 2, 3), torch.int32, -1)
+        self._grid_pos[1:-1] = torch.stack([torch.full_like(i, P), P + i // W, P + i % W], 1)
         # every block is free; the ring's last place takes what release() does not move
         self.ring = torch.arange(num_blocks + 1, dtype=torch.int32, device=device)
         self.head, self.next_head = new((1,), torch.int64), new((1,), torch.int64)
@@ -58,7 +63,7 @@ class PagedDecode:
                                                                 for _ in range(4))
         self.block_table = new((B, max_blocks), torch.int32, -1)
         self._slots = new((B * N_max,), torch.int64, -1)
-        self._pos = new((B * N_max * 3,), torch.int32)
+        self._pos, self._draft_pos = (new((B * N_max, 3), torch.int32) for _ in range(2))
         self._q = new((B * N_max * Hq * d,), torch.bfloat16)
         self._o = new((B * N_max * Hq * d,), torch.bfloat16)
         self.out_tok = new((B * N_max,), torch.int32, -1)
@@ -80,7 +85,7 @@ class PagedDecode:
             raise ValueError("N is between 1 and N_max")
         self.n_new.copy_(n_new)
         rows = self.B * self.N
-        self.slots, self.pos = self._slots[:rows], self._pos[:3 * rows]
+        self.slots, self.pos = self._slots[:rows], self._pos[:rows]
         ssd_cache_plan(self.g, self.B, self.block, self.max_blocks, self.N, self.cache_len,
                        self.n_new, self.held, self.ring, self.num_blocks, self.head, self.tail,
                        self.next_head, self.block_table, self.n_blocks, self.slots, self.pos,
@@ -90,16 +95,27 @@ class PagedDecode:
     def attend(self, layer, q, k, v, draft_pos=None, key_start=None, scale=0.0):
         """q bf16 [B * N, Hq * d], k and v bf16 [B * N, Hkv * d]: row b * N + j is new
         token j of sequence b; rows may lie apart (slices of one projection's output).
-        draft_pos int32 [B, N]: the new tokens are drafts.  Returns o bf16 [B * N, Hq * d]
-        (valid until the next call; rows without a token hold what they held)."""
+        draft_pos int32 [B, N]: the new tokens are drafts of these grid indices (y * W + x),
+        which give their rotary positions and what they see (without it: the next tokens of the
+        flat sequence).  The drafts that advance() keeps become the tokens that follow, so those
+        have to be the next ones, in order.  Returns o bf16 [B * N, Hq * d] (valid until the next
+        call; rows without a token hold what they held)."""
         rows, width = self.B * self.N, self.Hq * self.d
         for x, heads in ((q, self.Hq), (k, self.Hkv), (v, self.Hkv)):
             if tuple(x.shape) != (rows, heads * self.d) or x.stride(1) != 1 \
                     or x.dtype != torch.bfloat16:
                 raise ValueError("q, k, v: bfloat16 [B * N, heads * d], heads side by side")
+        pos = self.pos
+        if draft_pos is not None:
+            if draft_pos.dtype != torch.int32 or draft_pos.numel() != rows \
+                    or not draft_pos.is_contiguous():
+                raise ValueError("draft_pos: int32 [B, N], contiguous")
+            cells = self.g.grid_h * self.g.grid_w
+            pos = self._draft_pos[:rows]
+            torch.index_select(self._grid_pos, 0, draft_pos.view(-1).clamp(-1, cells).add_(1), out=pos)
         q_rot, o = self._q[:rows * width], self._o[:rows * width]
         ssd_cache_append(self.caches[layer], self.rotary, self.B, self.N, self.Hq, self.n_new,
-                         self.slots, self.pos, q, q.stride(0), k, k.stride(0), v, v.stride(0),
+                         self.slots, pos, q, q.stride(0), k, k.stride(0), v, v.stride(0),
                          q_rot, self.status)
         ws, n = self._workspace(self.N)
         ssd_cache_attention(self.g, self.caches[layer], self.B, self.Hq, self.cache_len, self.n_new,

@@ -532,7 +532,9 @@ typedef struct {
  * ids put into the ring so far (both only grow); freed blocks go to
  * ring[tail mod ring_size].  A sequence that the ring cannot serve gets no
  * block, and neither does any later one that wants some: SSD_ERR_WORKSPACE is
- * recorded, its n_blocks stays held[b] and its slots are -1.
+ * recorded, its n_blocks stays held[b] and its slots are -1.  It has no new
+ * tokens in this pass: ssd_cache_append() leaves it out by its slots, and the
+ * caller passes n_drafts 0 for it to ssd_cache_attention().
  *     slots[b][j] = slot of token cache_len[b] + j,    j < n_new[b], else -1
  *     pos[b][j]   = its position on the axes (time, row, column) for the
  *                   rotary embedding: (p, p, p) for token p of the text

@@ -26,7 +26,10 @@ class PagedDecode:
         sample(logits, ...)      the next tokens
         advance(n)               n of the new tokens of every sequence stay
 
-    Tokens that do not stay (rejected drafts) are overwritten by the next pass.
+    Tokens that do not stay (rejected drafts) are overwritten by the next pass.  A sequence that
+    plan() cannot serve (the pool has no block for it, or its lengths are out of range: ``status``
+    says so) is left out of the pass, on the device: n_new is 0, it attends to nothing, its rows of
+    o hold what they held and it does not advance.
     ``release(mask)`` gives the blocks of finished sequences back; their next
     pass starts at length 0."""
 
@@ -83,13 +86,14 @@ class PagedDecode:
         self.N = self.N_max if N is None else N
         if not 0 < self.N <= self.N_max:
             raise ValueError("N is between 1 and N_max")
-        self.n_new.copy_(n_new)
+        want = n_new.to(self.n_new).expand(self.B).contiguous()  # (mostly n_new itself)
         rows = self.B * self.N
         self.slots, self.pos = self._slots[:rows], self._pos[:rows]
         ssd_cache_plan(self.g, self.B, self.block, self.max_blocks, self.N, self.cache_len,
-                       self.n_new, self.held, self.ring, self.num_blocks, self.head, self.tail,
+                       want, self.held, self.ring, self.num_blocks, self.head, self.tail,
                        self.next_head, self.block_table, self.n_blocks, self.slots, self.pos,
                        self.status)
+        torch.mul(want, self.slots.view(self.B, self.N)[:, 0] >= 0, out=self.n_new)  # (if served)
         self._workspace(self.N)  # (allocated here, not in the middle of a pass)
 
     def attend(self, layer, q, k, v, draft_pos=None, key_start=None, scale=0.0):
@@ -134,9 +138,8 @@ class PagedDecode:
         return tok
 
     def advance(self, n=None) -> None:
-        """n int32 [B] (default: all) of the pass's new tokens stay.  A sequence that got
-        no blocks must not advance: its slots are -1."""
-        self.cache_len.add_(self.n_new if n is None else n)
+        """n int32 [B] (default, and at most: all) of the pass's new tokens stay."""
+        self.cache_len.add_(self.n_new if n is None else self.n_new.clamp(max=n))
         self.held.copy_(self.n_blocks)
         self.head.copy_(self.next_head)
 
@@ -148,5 +151,6 @@ class PagedDecode:
         place = torch.where(own.flatten(), place, self.num_blocks)
         self.ring.scatter_(0, place, self.block_table.flatten())
         self.tail.add_(own.sum())
+        self.block_table.masked_fill_(mask[:, None], -1)
         self.cache_len.masked_fill_(mask, 0)
         self.held.masked_fill_(mask, 0)

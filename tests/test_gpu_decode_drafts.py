@@ -1,4 +1,5 @@
-"""PagedDecode with drafts that are not the next tokens of the flat sequence.
+"""PagedDecode with drafts that are not the next tokens of the flat sequence, and with a pool that
+cannot serve everyone.
 
 The rotated query and the cached entries are compared with float64 rotations by the drafts' own
 grid positions: bf16's rounding (2^-8 of the value) and e4m3's (half a step times the scale), each
@@ -14,6 +15,7 @@ from tests.test_gpu_cache_attention import i32, ssd  # noqa: F401
 pytestmark = pytest.mark.gpu
 
 H, W, PREFIX = 6, 7, 10
+SSD_ERR_WORKSPACE = 7
 
 
 class Batch:
@@ -130,3 +132,82 @@ def test_the_frontier_s_drafts(ssd):  # noqa: F811
     ssd.ssd_frontier(dec.g, 2, dec.cache_len, 2 * W, nd, pos, dec.status)
     t.one_pass(nd.tolist(), 2 * W, pos.tolist())
     assert nd.tolist() == [2 * W, 2 * W - 4] and int(dec.status.item()) == 0
+
+
+def test_a_pool_that_runs_dry(ssd):  # noqa: F811
+    """The sequence that gets no blocks is left out of the pass and does not advance, whatever
+    advance() is told; once blocks are back it is served like any other."""
+    t = Batch(ssd, 3, 4, 2, 64, 16, W, 5, 32)
+    dec = t.dec
+    dec.k.view(torch.uint8).fill_(0x7f)
+    dec.v.view(torch.uint8).fill_(0x7f)
+    t.one_pass([32, 20, 17], 32, served=[True, True, False])
+    assert int(dec.status.item()) == SSD_ERR_WORKSPACE
+    dec.advance()
+    assert dec.cache_len.tolist() == [32, 20, 0] and dec.held.tolist() == [2, 2, 0]
+    # one block is left: the next to ask takes it, the one behind it waits
+    dec.status.zero_()
+    t.one_pass([1, 1, 1], 1, served=[True, True, False])
+    assert int(dec.status.item()) == SSD_ERR_WORKSPACE
+    dec.advance(i32([1, 0, 1]))
+    assert dec.cache_len.tolist() == [33, 20, 0] and dec.held.tolist() == [3, 2, 0]
+    # sequence 0 ends; sequence 2 takes its blocks
+    dec.release(torch.tensor([True, False, False], device="cuda"))
+    dec.status.zero_()
+    assert dec.block_table[0].tolist() == [-1] * dec.max_blocks
+    t.one_pass([0, 3, 25], 25)
+    dec.advance()
+    assert int(dec.status.item()) == 0
+    assert dec.cache_len.tolist() == [0, 23, 25] and dec.held.tolist() == [0, 2, 2]
+    # and a sequence that was released and is not served holds nothing of another's
+    dec.status.zero_()
+    t.one_pass([17, 1, 1], 17, served=[False, True, True])
+    assert int(dec.status.item()) == SSD_ERR_WORKSPACE
+    dec.advance()
+    assert dec.cache_len.tolist() == [0, 24, 26]
+
+
+def test_more_tokens_than_a_sequence_has_room_for(ssd):  # noqa: F811
+    """Lengths beyond the table are recorded, and that sequence is left out in the same way."""
+    t = Batch(ssd, 2, 2, 1, 64, 16, W, 0, 16)
+    dec = t.dec
+    room = dec.max_blocks * dec.block
+    dec.cache_len.copy_(i32([room - 3, 0]))
+    dec.held.copy_(i32([dec.max_blocks, 0]))
+    dec.block_table[0] = torch.arange(dec.max_blocks, dtype=torch.int32, device="cuda")
+    dec.head.fill_(dec.max_blocks)
+    t.one_pass([4, 5], 16, served=[False, True])
+    assert int(dec.status.item()) == 6
+    dec.advance()
+    assert dec.cache_len.tolist() == [room - 3, 5]
+
+
+def test_a_dry_pool_in_a_graph(ssd):  # noqa: F811
+    """Nobody can look between the passes of a captured graph: a token each until the pool is
+    empty, and two more."""
+    t = Batch(ssd, 2, 2, 1, 64, 16, W, 3, 1)
+    dec = t.dec
+    x = torch.randn((2, 4 * 64), device="cuda").to(torch.bfloat16)
+    one = i32([1, 1])
+
+    def step():
+        dec.plan(one, 1)
+        dec.attend(0, x[:, :128], x[:, 128:192], x[:, 192:])
+        dec.advance()
+
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for _ in range(15):
+        graph.replay()
+    torch.cuda.synchronize()
+    assert int(dec.status.item()) == 0 and dec.cache_len.tolist() == [16, 16]
+    for _ in range(3):
+        graph.replay()
+    torch.cuda.synchronize()
+    assert int(dec.status.item()) == SSD_ERR_WORKSPACE
+    assert dec.cache_len.tolist() == [19, 16] and dec.held.tolist() == [2, 1]

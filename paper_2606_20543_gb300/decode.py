@@ -14,6 +14,11 @@ from . import (Grid, Rng, Sampling, cache as make_cache, rotary as make_rotary,
                ssd_cache_plan, ssd_rotary_table, ssd_sample)
 
 
+def _row_stride(x):
+    """Elements from row to row; of a single row, whose stride may be anything, its width."""
+    return x.stride(0) if x.shape[0] > 1 else x.shape[1]
+
+
 class PagedDecode:
     """B sequences over a pool of ``num_blocks`` blocks of ``block`` tokens for
     each of ``layers`` layers; all layers share the block tables.
@@ -119,7 +124,7 @@ class PagedDecode:
             torch.index_select(self._grid_pos, 0, draft_pos.view(-1).clamp(-1, cells).add_(1), out=pos)
         q_rot, o = self._q[:rows * width], self._o[:rows * width]
         ssd_cache_append(self.caches[layer], self.rotary, self.B, self.N, self.Hq, self.n_new,
-                         self.slots, pos, q, q.stride(0), k, k.stride(0), v, v.stride(0),
+                         self.slots, pos, q, _row_stride(q), k, _row_stride(k), v, _row_stride(v),
                          q_rot, self.status)
         ws, n = self._workspace(self.N)
         ssd_cache_attention(self.g, self.caches[layer], self.B, self.Hq, self.cache_len, self.n_new,
@@ -133,7 +138,7 @@ class PagedDecode:
         if rows > self.out_tok.shape[0] or logits.stride(1) != 1:
             raise ValueError("logits: at most B * N_max rows, entries side by side")
         tok = self.out_tok[:rows]
-        ssd_sample(rows, V, logits, logits.stride(0), settings, rng, tok, self.prob[:rows],
+        ssd_sample(rows, V, logits, _row_stride(logits), settings, rng, tok, self.prob[:rows],
                    self.kept[:rows], self.status)
         return tok
 

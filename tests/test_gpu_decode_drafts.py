@@ -211,3 +211,22 @@ def test_a_dry_pool_in_a_graph(ssd):  # noqa: F811
     torch.cuda.synchronize()
     assert int(dec.status.item()) == SSD_ERR_WORKSPACE
     assert dec.cache_len.tolist() == [19, 16] and dec.held.tolist() == [2, 1]
+
+
+def test_one_row_with_any_stride(ssd):  # noqa: F811
+    """A tensor of one row may have any row stride: one new token of one sequence."""
+    def one(width, stride):
+        x = torch.randn(width, generator=torch.Generator("cuda").manual_seed(width), device="cuda")
+        return x.to(torch.bfloat16).as_strided((1, width), (stride, 1))
+
+    out = []
+    for stride in (4096, 1, 0):
+        dec = Batch(ssd, 1, 2, 1, 64, 16, W, 0, 1).dec
+        dec.plan(i32([1]), 1)
+        o = dec.attend(0, one(128, stride), one(64, stride), one(64, stride)).clone()
+        x = one(100, stride)
+        tok = dec.sample(x, ssd.sampling(1.0, 10), ssd.rng(3, 4)).clone()
+        assert int(dec.status.item()) == 0
+        out.append((o, tok))
+    for o, tok in out[1:]:
+        assert torch.equal(o, out[0][0]) and torch.equal(tok, out[0][1])

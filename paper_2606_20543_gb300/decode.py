@@ -107,18 +107,19 @@ class PagedDecode:
         draft_pos int32 [B, N]: the new tokens are drafts of these grid indices (y * W + x),
         which give their rotary positions and what they see (without it: the next tokens of the
         flat sequence).  The drafts that advance() keeps become the tokens that follow, so those
-        have to be the next ones, in order.  Returns o bf16 [B * N, Hq * d] (valid until the next
+        have to be the next ones, in order.  key_start int32 [B]: the first token of a sequence
+        that may be seen.  Returns o bf16 [B * N, Hq * d] (valid until the next
         call; rows without a token hold what they held)."""
         rows, width = self.B * self.N, self.Hq * self.d
         for x, heads in ((q, self.Hq), (k, self.Hkv), (v, self.Hkv)):
             if tuple(x.shape) != (rows, heads * self.d) or x.stride(1) != 1 \
                     or x.dtype != torch.bfloat16:
                 raise ValueError("q, k, v: bfloat16 [B * N, heads * d], heads side by side")
+        for x, n in ((draft_pos, rows), (key_start, self.B)):
+            if x is not None and (x.dtype != torch.int32 or x.numel() != n or not x.is_contiguous()):
+                raise ValueError("draft_pos: int32 [B, N], key_start: int32 [B], contiguous")
         pos = self.pos
         if draft_pos is not None:
-            if draft_pos.dtype != torch.int32 or draft_pos.numel() != rows \
-                    or not draft_pos.is_contiguous():
-                raise ValueError("draft_pos: int32 [B, N], contiguous")
             cells = self.g.grid_h * self.g.grid_w
             pos = self._draft_pos[:rows]
             torch.index_select(self._grid_pos, 0, draft_pos.view(-1).clamp(-1, cells).add_(1), out=pos)

@@ -230,3 +230,19 @@ def test_one_row_with_any_stride(ssd):  # noqa: F811
         out.append((o, tok))
     for o, tok in out[1:]:
         assert torch.equal(o, out[0][0]) and torch.equal(tok, out[0][1])
+
+
+def test_refused_positions_and_starts(ssd):  # noqa: F811
+    dec = Batch(ssd, 2, 2, 1, 64, 16, W, 0, 4).dec
+    dec.plan(i32([1, 1]), 2)
+    q = torch.zeros((4, 128), dtype=torch.bfloat16, device="cuda")
+    k = torch.zeros((4, 64), dtype=torch.bfloat16, device="cuda")
+    pos, start = i32([[0, 1], [0, 1]]), i32([0, 0])
+    for bad in (pos.long(), pos[:1], pos.t(), pos.float()):
+        with pytest.raises(ValueError):
+            dec.attend(0, q, k, k, bad)
+    for bad in (start.long(), start[:1], i32([0, 0, 0, 0])[::2]):
+        with pytest.raises(ValueError):
+            dec.attend(0, q, k, k, key_start=bad)
+    dec.attend(0, q, k, k, pos, start)
+    assert int(dec.status.item()) == 0

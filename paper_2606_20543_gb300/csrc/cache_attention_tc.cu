@@ -66,8 +66,8 @@ __host__ __device__ constexpr int q_bytes(int d) { return kBM * d; }
 __host__ __device__ constexpr int tile_bytes(int d) { return KT * d; }
 __host__ __device__ constexpr int wide_bytes(int d) { return 2 * KT * d; }
 
-// kind::f8f6f4, e4m3 A and B, fp32 D.
-__host__ __device__ constexpr uint32_t idesc_e4m3(int m, int n, bool b_mn_major) {
+// fp32 D; A and B e4m3 (kind::f8f6f4) or float16 (kind::f16), whose codes are both 0.
+__host__ __device__ constexpr uint32_t idesc_of(int m, int n, bool b_mn_major) {
   return (1u << 4) | ((b_mn_major ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) |
          ((uint32_t)(m >> 4) << 24);
 }
@@ -78,11 +78,6 @@ __device__ __forceinline__ void mma8_ss(uint32_t d_tmem, uint64_t adesc, uint64_
       " tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n}\n" ::"r"(d_tmem),
       "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
       : "memory");
-}
-// kind::f16, float16 A and B, fp32 D.
-__host__ __device__ constexpr uint32_t idesc_f16(int m, int n, bool b_mn_major) {
-  return (1u << 4) | ((b_mn_major ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) |
-         ((uint32_t)(m >> 4) << 24);
 }
 
 // float16 pairs to e4m3 pairs and back (exactly).
@@ -437,7 +432,7 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
     const uint32_t aK = warp_uniform(smem_u32(sK)), aW = warp_uniform(smem_u32(sW));
     const bool leader = elect_one();
     const uint64_t dq = rows_desc<D>(aQ);
-    constexpr uint32_t kIdescS = idesc_e4m3(kBM, KT, false), kIdescO = idesc_f16(kBM, D, true);
+    constexpr uint32_t kIdescS = idesc_of(kBM, KT, false), kIdescO = idesc_of(kBM, D, true);
     int32_t ns = 0, np = 0;  // tiles whose products were issued
     bool ok = true;
 #pragma unroll 1

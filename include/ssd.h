@@ -660,8 +660,8 @@ ssd_status ssd_cache_attention(const ssd_grid* grid, const ssd_block_cache* cach
  *     out_tok = smallest v with sum of kept W_v' over v' <= v > u_res * Z,
  *     Z the kept mass, u_res the row's second uniform (ssd_rng).
  * c is at most 2^100 (T above about 1e-30).  T = 0 takes the first largest
- * logit.  NaN logits count as -inf, +inf ones as equal weights of 1; a row with nothing above -inf gives out_tok = -1, prob = 0,
- * kept = 0.  Weights below 2^-32 of the largest are never drawn.
+ * logit.  NaN logits count as -inf, +inf ones as equal weights of 1; a row with
+ * nothing above -inf gives out_tok = -1, prob = 0, kept = 0.  Weights below 2^-32 of the largest are never drawn.
  *   logits  dev float32 (or bf16 if logits_bf16) row r at + r * ld; any V up
  *           to 2^20, any alignment to the element
  *   prob    dev float32 [rows] or NULL: W of the token / Z

@@ -103,7 +103,7 @@ __device__ __forceinline__ bool cache_lengths_ok(const CacheAttnArgs& a, int32_t
 //  - Where that is more than kEvenTiles tiles above an even share (8 sequences for 14 CTAs),
 //    the tiles of all sequences, in one line, are cut evenly, and a CTA may work on the end of
 //    one sequence and the beginning of the next.  A cut that would leave a sliver of a sequence
-//    moves to the sequence's end.  8 sequences of 8000 keys, 32 heads: 108 -> 96 us; with 16
+//    moves to the sequence's end.  8 sequences of 8000 keys, 32 heads: 108 -> 95 us; with 16
 //    sequences of 2000 keys for 57 CTAs, a tile or two from even, the second part's
 //    set-up costs more than it gives (20 -> 22 us).
 // Called by converged warps; every lane holds the same.

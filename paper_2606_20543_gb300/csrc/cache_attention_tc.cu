@@ -4,9 +4,10 @@
 //
 // K stays e4m3 from the cache to the products (kind::f8f6f4): it is copied by TMA, 128 bytes
 // a key, and never widened; Q is split in two e4m3 terms, x = hi + lo with hi the nearest
-// e4m3 and lo the nearest to the rest (8 significant bits, as many as bf16 has, at the cost of
-// twice the products, which run at twice the rate of bf16's), after its rows are scaled by a
-// power of two (largest entry in [128, 256)).  P, which changes with every tile, is rounded to
+// e4m3 and lo the nearest to the rest, at the cost of twice the products, which run at twice the
+// rate of bf16's, after its rows are scaled by a power of two (largest entry in [128, 256)).  That
+// keeps bf16's 8 significant bits of entries down to 2^-10 of the row's largest; below, lo's least
+// step is absolute, and the error 2^-18 of that largest.  P, which changes with every tile, is rounded to
 // float16 instead (a split takes six instructions a pair, and the softmax is what bounds this
 // kernel): two warps widen V to float16, exactly, and the second product is kind::f16.  The K
 // scale of a block multiplies the scores, its V scale over the row's reference the probabilities.
@@ -26,14 +27,19 @@
 //    see or hardly weighs.  A reference moves only when its maximum grows by more than 2^8; O is
 //    rescaled in TMEM when the second one does.
 //
-// 128 drafts of 8 sequences over 2300 to 3800 keys, 32 heads (222 MB, 51 GFLOP): 72 us, 3.1 TB/s,
+// 128 drafts of 8 sequences over 2300 to 3800 keys, 32 heads (222 MB, 51 GFLOP): 73 us, 3.0 TB/s,
 // 0.45 of the measured copy rate; the tensor pipe is busy for a quarter of it.  A tile takes
 // 1200 cycles of an SM with two CTAs, and a CTA of such a pair about 2200: 650 for the
 // exponentials, 370 for the maximum, 270 for S out of TMEM, the rest between the warps (when all of it
 // took 80 us it was 59 without the softmax, 76 without the exponentials, 75 without widening
-// V).  256 CTAs leave 48 of the 152 SMs with one.  25 sequences of 48 drafts over 120 to 700 keys,
-// 16 heads (56 MB): 29 us, of which a CTA's set-up takes 3.5 and its seven tiles about twice
-// that.  Tiles of 128 keys with V in e4m3 as well (P in two terms, 8 softmax warps) were
+// V).  All tiles at the first rate are 48 us; the 60 of the longest sequence at the second are
+// 65, and units are not cut here (256 for 304 places, 48 of the 152 SMs with one), so that
+// sequence bounds it.  With draft_pos 78 us: a tile that holds drafts reads a position per key
+// and row.  25 sequences of 48 drafts over 120 to 700 keys,
+// 16 heads (56 MB): 29 us (with draft_pos 33), of which a CTA's set-up takes 3.5 and its seven
+// tiles about twice that; 48 rows fill three eighths of a tile, and 400 units take a second
+// round in 304 places.  The attention over a bf16 cache takes 67 and 20 us for the two: this one
+// saves memory, not time.  Tiles of 128 keys with V in e4m3 as well (P in two terms, 8 softmax warps) were
 // slower by a sixth, so the products are not what to save.
 #include <cuda_fp16.h>
 
@@ -744,8 +750,8 @@ cudaError_t launch(const CacheAttnArgs& a, const CacheAttnLaunch& L, cudaStream_
 }  // namespace
 
 // From 17 query rows on (the mma.sync kernel takes 16 to a CTA, and every CTA reads the keys for
-// itself): 16 sequences of 4000 keys, 8 heads: 128-wide, 17 rows 45 us here and 59 there; 64-wide
-// 39 and 47 (48 rows and 8 sequences of 32 heads: 88 and 130).
+// itself): 16 sequences of 4000 keys, 8 heads: 128-wide, 17 rows 44 us here and 59 there; 64-wide
+// 35 and 47 (48 rows and 8 sequences of 32 heads: 66 and 130).
 bool cache_attention_tc_runs(int32_t B, int32_t Hq, int32_t Hkv, int32_t D_max, int32_t L_max) {
   const int64_t rows = (int64_t)D_max * (Hq / Hkv);
   return rows > 16 && !cache_attention_few(B, Hkv, rows, L_max);

@@ -19,7 +19,7 @@
 // list takes (equal logits, high temperatures), the search runs over the row's entries
 // in those bins; where the exact masses show the cut to be elsewhere, over the whole row.
 //
-// 1024 rows of 65536 float32 logits, top-p 0.95: 162 us, 268 MB at 1.65 TB/s (0.24 of the
+// 1024 rows of 65536 float32 logits, top-p 0.95: 164 to 167 us, 268 MB at 1.6 TB/s (0.24 of the
 // measured copy rate; the pass for the largest logit alone takes 53 us, without a cut 111).
 // About 20 instructions an entry in the two passes bound it, and 17000 cycles a row between
 // them, of which two rows to an SM hide half.  One row of 16384, top-k 2000: 12.5 us; 200 rows

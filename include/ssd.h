@@ -610,6 +610,37 @@ ssd_status ssd_cache_append(const ssd_block_cache* cache, const ssd_rotary* rota
                             int64_t ldk, const void* v, int64_t ldv, void* q_out, int32_t* status,
                             ssd_stream_t stream);
 
+/* Norms of the query and key heads, between projection and rotation:
+ *   SSD_NORM_RMS    y = x / sqrt(mean(x^2) + eps) * gain + bias
+ *   SSD_NORM_LAYER  y = (x - mean(x)) / sqrt(mean((x - mean(x))^2) + eps) * gain + bias
+ * over the d values of a head, in float32 (so a head's squares have to stay
+ * below 2^127), not rounded before the rotation.
+ *   eps  above 0, finite
+ *   q_gain, q_bias  dev float32 [q_heads][d] (a row for every head: q_heads =
+ *           Hq), or [d] if q_heads is 0 (one row for all); NULL: 1 and 0;
+ *           16-byte aligned.  k_gain, k_bias the same over the Hkv heads. */
+typedef enum { SSD_NORM_RMS = 1, SSD_NORM_LAYER = 2 } ssd_norm_kind;
+typedef struct {
+  int32_t kind; /* an ssd_norm_kind */
+  float eps;
+  const float* q_gain;
+  const float* q_bias;
+  const float* k_gain;
+  const float* k_bias;
+  int32_t q_heads, k_heads;
+} ssd_head_norm;
+
+/* ssd_cache_append() of q and k that are normalised head by head first (v is
+ * not).  A NaN in a head makes all of it NaN; in an RMS norm an infinity is a
+ * NaN in its own pair and the head's other entries 0 (times gain plus bias).
+ * A NaN goes into the cache as NaN and leaves the block's scale to the rest. */
+ssd_status ssd_cache_append_norm(const ssd_block_cache* cache, const ssd_rotary* rotary,
+                                 const ssd_head_norm* norm, int32_t B, int32_t N_max, int32_t Hq,
+                                 const int32_t* n_new, const int64_t* slots, const int32_t* pos,
+                                 const void* q, int64_t ldq, const void* k, int64_t ldk,
+                                 const void* v, int64_t ldv, void* q_out, int32_t* status,
+                                 ssd_stream_t stream);
+
 /* Frontier attention (a2) over the paged 8-bit cache: the formula and the mask
  * of ssd_verify_attention() with K and V the cache's values,
  *     O[b][j][h] = softmax_s(scale * Q[b][j][h] . K[s] + M(s, j)) V[s],
@@ -686,6 +717,25 @@ typedef struct {
 ssd_status ssd_sample(int32_t rows, int32_t V, const void* logits, int32_t logits_bf16, int64_t ld,
                       const ssd_sampling* sampling, const ssd_rng* rng, int32_t* out_tok,
                       float* prob, int32_t* kept, int32_t* status, ssd_stream_t stream);
+
+/* ---------------------------------------------------------------------------
+ * 8-bit matrix products: the projections around the cache on e4m3 inputs and
+ * weights, with a float32 scale for every 128 entries of the inner length (and,
+ * of a weight, for 128 of its rows).  As the cache, not of the paper.
+ *
+ * x[rows][K] as e4m3 and scales.  With m the largest finite magnitude of a
+ * block of block_rows rows x 128 columns (fewer at the ends):
+ *     s = max(m, 2^-100) / 448;   entry = e4m3(clamp(x * (1 / s), -448, 448))
+ * to nearest even; an infinity becomes +-448, a NaN stays one.
+ *   x      dev float32, or bf16 if x_bf16; rows ldx elements apart
+ *   out    dev e4m3, rows ldo bytes apart (columns from K on untouched)
+ *   scale  dev float32 [ceil(K / 128)][lds]: entry [k / 128][row / block_rows]
+ * block_rows: 1 (activations) or 128 (weights).  ldx a multiple of 8, ldo of
+ * 16; x, out 16-byte aligned; lds >= ceil(rows / block_rows).
+ * ------------------------------------------------------------------------- */
+ssd_status ssd_quantize(int32_t rows, int32_t K, int32_t block_rows, const void* x, int32_t x_bf16,
+                        int64_t ldx, void* out, int64_t ldo, float* scale, int64_t lds,
+                        ssd_stream_t stream);
 
 #ifdef __cplusplus
 }

@@ -131,3 +131,13 @@ def attention(q, k, v, visible, scale, vscale):
             lse[j, h] = m + np.log(z)
             mag[j, h] = np.abs(q[j, h]).max() * np.abs(kk).sum(-1).max() * scale
     return o, lse, A, F, mag
+
+
+def head_norm(x, kind, eps, gain=None, bias=None):
+    """x [N, H, d] float64: every head over its d values; gain, bias [d] or [H, d]."""
+    if kind == "layer":
+        x = x - x.mean(-1, keepdims=True)
+    y = x / np.sqrt((x * x).mean(-1, keepdims=True) + eps)
+    if gain is not None:
+        y = y * gain
+    return y if bias is None else y + bias

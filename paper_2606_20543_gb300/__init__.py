@@ -31,14 +31,17 @@ EXPORTED = ["ssd_abi_version", "ssd_status_string", "ssd_set_wait_limit",
             "ssd_lmhead_accept_workspace", "ssd_lmhead_accept",
             "ssd_verify_step_workspace", "ssd_verify_step_launches", "ssd_verify_step",
             "ssd_verify_accept",
-            "ssd_cache_plan", "ssd_rotary_table", "ssd_cache_append",
-            "ssd_cache_attention_workspace", "ssd_cache_attention", "ssd_sample"]
+            "ssd_cache_plan", "ssd_rotary_table", "ssd_cache_append", "ssd_cache_append_norm",
+            "ssd_cache_attention_workspace", "ssd_cache_attention", "ssd_sample",
+            "ssd_quantize"]
 
 
 STRATEGY_ACCEPT_REJECT, STRATEGY_GREEDY, STRATEGY_SAMPLE = 0, 1, 2
 COMMIT_PREFIX, COMMIT_NONE, COMMIT_BLOCK, COMMIT_FIRST_ROW, COMMIT_PREFIX_BONUS = 0, 1, 2, 3, 4
 COMMITS = {"prefix": COMMIT_PREFIX, "none": COMMIT_NONE, "block": COMMIT_BLOCK,
            "first_row": COMMIT_FIRST_ROW, "prefix_bonus": COMMIT_PREFIX_BONUS}
+NORM_RMS, NORM_LAYER = 1, 2
+NORMS = {"rms": NORM_RMS, "layer": NORM_LAYER}
 STRATEGIES = {"accept_reject": STRATEGY_ACCEPT_REJECT, "greedy": STRATEGY_GREEDY,
               "sample": STRATEGY_SAMPLE}
 
@@ -96,6 +99,13 @@ class BlockCache(ctypes.Structure):
 class Rotary(ctypes.Structure):
     _fields_ = [("table", ctypes.c_void_p), ("n_pos", ctypes.c_int32),
                 ("sec", ctypes.c_int32 * 3), ("interleaved", ctypes.c_int32)]
+
+
+class HeadNorm(ctypes.Structure):
+    _fields_ = [("kind", ctypes.c_int32), ("eps", ctypes.c_float),
+                ("q_gain", ctypes.c_void_p), ("q_bias", ctypes.c_void_p),
+                ("k_gain", ctypes.c_void_p), ("k_bias", ctypes.c_void_p),
+                ("q_heads", ctypes.c_int32), ("k_heads", ctypes.c_int32)]
 
 
 class Sampling(ctypes.Structure):
@@ -157,11 +167,15 @@ def load(path: Optional[str] = None) -> ctypes.CDLL:
         "ssd_rotary_table": (I32, [I32, I32, P, P, P]),
         "ssd_cache_append": (I32, [ctypes.POINTER(BlockCache), ctypes.POINTER(Rotary), I32, I32,
                                    I32, P, P, P, P, I64, P, I64, P, I64, P, P, P]),
+        "ssd_cache_append_norm": (I32, [ctypes.POINTER(BlockCache), ctypes.POINTER(Rotary),
+                                        ctypes.POINTER(HeadNorm), I32, I32, I32, P, P, P, P, I64, P,
+                                        I64, P, I64, P, P, P]),
         "ssd_cache_attention_workspace": (SZ, [I32, I32, I32, I32, I32, I32]),
         "ssd_cache_attention": (I32, [ctypes.POINTER(Grid), ctypes.POINTER(BlockCache), I32, I32, P,
                                       P, P, P, I32, P, I32, P, F, P, P, P, SZ, P, P]),
         "ssd_sample": (I32, [I32, I32, P, I32, I64, ctypes.POINTER(Sampling), ctypes.POINTER(Rng),
                              P, P, P, P, P]),
+        "ssd_quantize": (I32, [I32, I32, I32, P, I32, I64, P, I64, P, I64, P]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -399,6 +413,30 @@ def rotary(table, sections, interleaved: bool = False) -> Rotary:
     return Rotary(_ptr(table), table.shape[0], (ctypes.c_int32 * 3)(*sections), int(interleaved))
 
 
+def head_norm(kind, eps, q_gain=None, q_bias=None, k_gain=None, k_bias=None) -> HeadNorm:
+    """Norms of the query and key heads: kind "rms" or "layer"; gains and biases float32 [d], one
+    row for all heads, or [heads, d] (both of a side alike), or None (1 and 0)."""
+    rows = []
+    for side in ((q_gain, q_bias), (k_gain, k_bias)):
+        shape = None
+        for t in side:
+            if t is None:
+                continue
+            if str(t.dtype) != "torch.float32" or not t.is_contiguous() or t.dim() not in (1, 2):
+                raise ValueError("gains and biases: contiguous float32 [d] or [heads, d]")
+            if shape is not None and t.shape != shape:
+                raise ValueError("gain and bias have one shape")
+            shape = t.shape
+        if shape is not None and rows and rows[-1][1] not in (None, shape[-1]):
+            raise ValueError("q and k heads have one width")
+        rows.append((0 if shape is None or len(shape) == 1 else shape[0],
+                     None if shape is None else shape[-1]))
+    n = HeadNorm(NORMS.get(kind, kind), eps, _ptr(q_gain), _ptr(q_bias), _ptr(k_gain), _ptr(k_bias),
+                 rows[0][0], rows[1][0])
+    n.d = rows[0][1] or rows[1][1]  # (checked against the cache's at the call)
+    return n
+
+
 def sampling(temperature: float = 1.0, top_k: int = 0, top_p: float = 1.0, min_p: float = 0.0,
              temperatures=None, top_ks=None, top_ps=None, min_ps=None, n_drafts=None,
              D_max: int = 1) -> Sampling:
@@ -430,6 +468,17 @@ def ssd_cache_append(c: BlockCache, r: Rotary, B, N_max, Hq, n_new, slots, pos, 
         _ptr(q), ldq, _ptr(k), ldk, _ptr(v), ldv, _ptr(q_out), _ptr(status), _stream(stream)))
 
 
+def ssd_cache_append_norm(c: BlockCache, r: Rotary, norm: HeadNorm, B, N_max, Hq, n_new, slots, pos,
+                          q, ldq, k, ldk, v, ldv, q_out, status, stream=None) -> None:
+    """ssd_cache_append() of q and k whose heads are normalised first."""
+    if getattr(norm, "d", None) not in (None, c.d):
+        raise ValueError("gains and biases of another head width")
+    _check("ssd_cache_append_norm", load().ssd_cache_append_norm(
+        ctypes.byref(c), ctypes.byref(r), ctypes.byref(norm), B, N_max, Hq, _ptr(n_new),
+        _ptr(slots), _ptr(pos), _ptr(q), ldq, _ptr(k), ldk, _ptr(v), ldv, _ptr(q_out), _ptr(status),
+        _stream(stream)))
+
+
 def ssd_cache_attention_workspace(B, Hq, Hkv, d, D_max, L_max) -> int:
     return load().ssd_cache_attention_workspace(B, Hq, Hkv, d, D_max, L_max)
 
@@ -442,6 +491,22 @@ def ssd_cache_attention(g: Grid, c: BlockCache, B, Hq, cache_len, n_drafts, draf
         ctypes.byref(g), ctypes.byref(c), B, Hq, _ptr(cache_len), _ptr(n_drafts), _ptr(draft_pos),
         _ptr(key_start), D_max, _ptr(block_table), max_blocks, _ptr(q), scale, _ptr(o), _ptr(lse),
         _ptr(workspace), workspace_bytes, _ptr(status), _stream(stream)))
+
+
+def _is_bf16(t, what: str) -> int:
+    """1 for bfloat16 (or nothing at all), 0 for float32."""
+    if t is None or str(t.dtype) == "torch.bfloat16":
+        return 1
+    if str(t.dtype) == "torch.float32":
+        return 0
+    raise ValueError(what + " is float32 or bfloat16")
+
+
+def ssd_quantize(rows, K, block_rows, x, ldx, out, ldo, scale, lds, stream=None) -> None:
+    """x float32 or bf16 [rows, K] as e4m3 with a scale for block_rows x 128 entries."""
+    _check("ssd_quantize", load().ssd_quantize(
+        rows, K, block_rows, _ptr(x), _is_bf16(x, "x"), ldx, _ptr(out), ldo, _ptr(scale), lds,
+        _stream(stream)))
 
 
 def ssd_sample(rows, V, logits, ld, p: Sampling, r: Rng, out_tok, prob, kept, status,

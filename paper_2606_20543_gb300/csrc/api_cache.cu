@@ -41,6 +41,64 @@ ssd_status check_cache(const ssd_block_cache* c) {
   return SSD_OK;
 }
 
+// (norm may be null)
+ssd_status append(const ssd_block_cache* cache, const ssd_rotary* rotary, const ssd_head_norm* norm,
+                  int32_t B, int32_t N_max, int32_t Hq, const int32_t* n_new, const int64_t* slots,
+                  const int32_t* pos, const void* q, int64_t ldq, const void* k, int64_t ldk,
+                  const void* v, int64_t ldv, void* q_out, int32_t* status, ssd_stream_t stream) {
+  ssd_status s = check_cache(cache);
+  if (s != SSD_OK) return s;
+  if (rotary == nullptr) return SSD_ERR_INVALID_ARG;
+  if (B < 0 || N_max <= 0 || Hq <= 0) return SSD_ERR_SHAPE;
+  const int32_t d = cache->d, Hkv = cache->Hkv;
+  if (Hq % Hkv != 0 || rotary->n_pos <= 0) return SSD_ERR_SHAPE;
+  int64_t pairs = 0;
+  for (int i = 0; i < 3; ++i) {
+    if (rotary->sec[i] < 0) return SSD_ERR_SHAPE;
+    pairs += rotary->sec[i];
+  }
+  if (pairs != d / 2) return SSD_ERR_SHAPE;
+  if (ldq < (int64_t)Hq * d || ldk < (int64_t)Hkv * d || ldv < (int64_t)Hkv * d) return SSD_ERR_SHAPE;
+  if (ldq % 8 != 0 || ldk % 8 != 0 || ldv % 8 != 0) return SSD_ERR_SHAPE;
+  if ((int64_t)Hq * d > INT32_MAX / 2 || (int64_t)B * N_max > INT32_MAX / Hq)
+    return SSD_ERR_UNSUPPORTED;
+  if (norm != nullptr) {
+    if (norm->kind != SSD_NORM_RMS && norm->kind != SSD_NORM_LAYER) return SSD_ERR_INVALID_ARG;
+    if (!(norm->eps > 0.f) || !isfinite(norm->eps)) return SSD_ERR_INVALID_ARG;
+    if ((norm->q_heads != 0 && norm->q_heads != Hq) || (norm->k_heads != 0 && norm->k_heads != Hkv))
+      return SSD_ERR_SHAPE;
+    for (const float* p : {norm->q_gain, norm->q_bias, norm->k_gain, norm->k_bias})
+      if (!aligned(p, 16)) return SSD_ERR_INVALID_ARG;
+  }
+  if (B == 0) return SSD_OK;
+  for (const void* p : {(const void*)n_new, (const void*)slots, (const void*)pos, q, k, v,
+                        (const void*)q_out, (const void*)rotary->table, (const void*)status})
+    if (p == nullptr) return SSD_ERR_INVALID_ARG;
+  for (const void* p : {q, k, v, (const void*)q_out})
+    if (!aligned(p, 16)) return SSD_ERR_INVALID_ARG;
+  if (!aligned(slots, 8) || !aligned(rotary->table, 8)) return SSD_ERR_INVALID_ARG;
+  if (q_out == q && ldq != (int64_t)Hq * d) return SSD_ERR_INVALID_ARG;
+  CacheAppendArgs a{};
+  a.cache = *cache;
+  a.rot = *rotary;
+  a.B = B;
+  a.N_max = N_max;
+  a.Hq = Hq;
+  a.n_new = n_new;
+  a.slots = slots;
+  a.pos = pos;
+  a.q = q;
+  a.k = k;
+  a.v = v;
+  a.ldq = ldq;
+  a.ldk = ldk;
+  a.ldv = ldv;
+  a.q_out = q_out;
+  a.status = status;
+  if (norm != nullptr) a.norm = *norm;
+  return from_cuda(launch_cache_append(a, (cudaStream_t)stream));
+}
+
 }  // namespace
 
 extern "C" {
@@ -103,48 +161,19 @@ ssd_status ssd_cache_append(const ssd_block_cache* cache, const ssd_rotary* rota
                             const int32_t* pos, const void* q, int64_t ldq, const void* k,
                             int64_t ldk, const void* v, int64_t ldv, void* q_out, int32_t* status,
                             ssd_stream_t stream) {
-  ssd_status s = check_cache(cache);
-  if (s != SSD_OK) return s;
-  if (rotary == nullptr) return SSD_ERR_INVALID_ARG;
-  if (B < 0 || N_max <= 0 || Hq <= 0) return SSD_ERR_SHAPE;
-  const int32_t d = cache->d, Hkv = cache->Hkv;
-  if (Hq % Hkv != 0 || rotary->n_pos <= 0) return SSD_ERR_SHAPE;
-  int64_t pairs = 0;
-  for (int i = 0; i < 3; ++i) {
-    if (rotary->sec[i] < 0) return SSD_ERR_SHAPE;
-    pairs += rotary->sec[i];
-  }
-  if (pairs != d / 2) return SSD_ERR_SHAPE;
-  if (ldq < (int64_t)Hq * d || ldk < (int64_t)Hkv * d || ldv < (int64_t)Hkv * d) return SSD_ERR_SHAPE;
-  if (ldq % 8 != 0 || ldk % 8 != 0 || ldv % 8 != 0) return SSD_ERR_SHAPE;
-  if ((int64_t)Hq * d > INT32_MAX / 2 || (int64_t)B * N_max > INT32_MAX / Hq)
-    return SSD_ERR_UNSUPPORTED;
-  if (B == 0) return SSD_OK;
-  for (const void* p : {(const void*)n_new, (const void*)slots, (const void*)pos, q, k, v,
-                        (const void*)q_out, (const void*)rotary->table, (const void*)status})
-    if (p == nullptr) return SSD_ERR_INVALID_ARG;
-  for (const void* p : {q, k, v, (const void*)q_out})
-    if (!aligned(p, 16)) return SSD_ERR_INVALID_ARG;
-  if (!aligned(slots, 8) || !aligned(rotary->table, 8)) return SSD_ERR_INVALID_ARG;
-  if (q_out == q && ldq != (int64_t)Hq * d) return SSD_ERR_INVALID_ARG;
-  CacheAppendArgs a{};
-  a.cache = *cache;
-  a.rot = *rotary;
-  a.B = B;
-  a.N_max = N_max;
-  a.Hq = Hq;
-  a.n_new = n_new;
-  a.slots = slots;
-  a.pos = pos;
-  a.q = q;
-  a.k = k;
-  a.v = v;
-  a.ldq = ldq;
-  a.ldk = ldk;
-  a.ldv = ldv;
-  a.q_out = q_out;
-  a.status = status;
-  return from_cuda(launch_cache_append(a, (cudaStream_t)stream));
+  return append(cache, rotary, nullptr, B, N_max, Hq, n_new, slots, pos, q, ldq, k, ldk, v, ldv,
+                q_out, status, stream);
+}
+
+ssd_status ssd_cache_append_norm(const ssd_block_cache* cache, const ssd_rotary* rotary,
+                                 const ssd_head_norm* norm, int32_t B, int32_t N_max, int32_t Hq,
+                                 const int32_t* n_new, const int64_t* slots, const int32_t* pos,
+                                 const void* q, int64_t ldq, const void* k, int64_t ldk,
+                                 const void* v, int64_t ldv, void* q_out, int32_t* status,
+                                 ssd_stream_t stream) {
+  if (norm == nullptr) return SSD_ERR_INVALID_ARG;
+  return append(cache, rotary, norm, B, N_max, Hq, n_new, slots, pos, q, ldq, k, ldk, v, ldv, q_out,
+                status, stream);
 }
 
 size_t ssd_cache_attention_workspace(int32_t B, int32_t Hq, int32_t Hkv, int32_t d, int32_t D_max,

@@ -1,11 +1,9 @@
 // cache.cu — the paged 8-bit cache (include/ssd.h): the plan (block tables,
 // slot maps and positions from request lengths), the rotary table and the
 // append (rotary positions with three axes, e4m3 blocks with a scale per head).
-#include <cuda_fp8.h>
-
 #include <algorithm>
 
-#include "kernels.cuh"
+#include "e4m3.cuh"
 
 namespace ssd {
 
@@ -195,39 +193,6 @@ __global__ void rotary_table_kernel(int32_t n, int32_t pairs, const float* freq,
 }
 
 // ----------------------------------------------------------------- append
-constexpr float kTop8 = 448.f;       // largest e4m3 value
-constexpr float kLeast = 0x1p-100f;  // least magnitude a block is scaled by
-
-__device__ __forceinline__ void unpack8(const uint4& w, float* x) {
-  const uint32_t v[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    x[2 * i] = __uint_as_float(v[i] << 16);
-    x[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u);
-  }
-}
-__device__ __forceinline__ uint4 pack8(const float* x) {
-  return make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]),
-                    pack_bf16x2(x[6], x[7]));
-}
-// Two float32 to e4m3, to nearest even; +-448 beyond, NaN for NaN.
-__device__ __forceinline__ uint32_t to_e4m3x2(float lo, float hi) {
-  uint16_t r;
-  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
-  return r;
-}
-__device__ __forceinline__ uint2 to_e4m3x8(const float* x, float f) {
-  uint32_t h[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) h[i] = to_e4m3x2(x[2 * i] * f, x[2 * i + 1] * f);
-  return make_uint2(h[0] | (h[1] << 16), h[2] | (h[3] << 16));
-}
-__device__ __forceinline__ float2 from_e4m3x2(uint16_t w) {
-  uint32_t h;
-  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(w));
-  return __half22float2(*reinterpret_cast<const __half2*>(&h));
-}
-
 // Rotation of 16 values of a head: 8 from column c8 on in a, 8 from column c8 +
 // d/2 on in b.  Products and sums are rounded one by one (no fused
 // multiply-add), so the result does not depend on how a compiler pairs them.
@@ -287,6 +252,57 @@ __device__ __forceinline__ void rotate16(bool interleaved, const float2 (&cs)[8]
   }
 }
 
+// Gains (or biases) of the 16 values that a thread holds of head h; heads 0: one row for all.
+template <int D>
+__device__ __forceinline__ void load_gain(const float* gain, int32_t heads, int32_t h, int32_t c8,
+                                          float none, float (&ga)[8], float (&gb)[8]) {
+  if (gain == nullptr) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) ga[i] = gb[i] = none;
+    return;
+  }
+  const float4* p = reinterpret_cast<const float4*>(gain + (heads != 0 ? h * D : 0) + c8);
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const float4 x = __ldg(p + i), y = __ldg(p + D / 8 + i);
+    ga[4 * i] = x.x, ga[4 * i + 1] = x.y, ga[4 * i + 2] = x.z, ga[4 * i + 3] = x.w;
+    gb[4 * i] = y.x, gb[4 * i + 1] = y.y, gb[4 * i + 2] = y.z, gb[4 * i + 3] = y.w;
+  }
+}
+// A head's norm over its D / 16 lanes: kNorm 1, x / sqrt(mean x^2 + eps); 2, the same of x less its
+// mean (squares of the differences, so a large mean costs no digits); times gain plus bias.  In
+// float32, and not rounded before the rotation.  Called by all lanes of a head together, whatever
+// the warp's other lanes do.
+template <int D, int kNorm>
+__device__ __forceinline__ void normalise16(float eps, const float (&ga)[8], const float (&gb)[8],
+                                            const float (&ba)[8], const float (&bb)[8],
+                                            float (&xa)[8], float (&xb)[8]) {
+  constexpr int LPR = D / 16;
+  const uint32_t lanes = ((1u << LPR) - 1u) << (threadIdx.x & 31 & ~(LPR - 1));
+  auto sum = [&](float v) {
+#pragma unroll
+    for (int o = LPR / 2; o > 0; o >>= 1) v += __shfl_xor_sync(lanes, v, o);
+    return v;
+  };
+  if constexpr (kNorm == 2) {
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s += xa[i] + xb[i];
+    const float mean = sum(s) * (1.f / D);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) xa[i] -= mean, xb[i] -= mean;
+  }
+  float s = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) s = fmaf(xa[i], xa[i], fmaf(xb[i], xb[i], s));
+  const float r = rsqrtf(fmaf(sum(s), 1.f / D, eps));
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    xa[i] = fmaf(xa[i] * r, ga[i], ba[i]);
+    xb[i] = fmaf(xb[i] * r, gb[i], bb[i]);
+  }
+}
+
 // A thread holds 16 values of a row, a row takes D / 16 lanes, and a block of
 // threads covers a cache block of S tokens of one head in kPasses passes (at
 // least a warp): the new values stay in registers between the search for their
@@ -304,7 +320,7 @@ constexpr int append_threads(int d, int block) {
 }
 
 // x: new tokens' rows of one head; kIsK: rotated first.
-template <int D, bool kIsK>
+template <int D, bool kIsK, int kNorm>
 __device__ __forceinline__ void append_block(const CacheAppendArgs& a, int32_t b, int32_t i,
                                              int32_t g, bool wide, float* red) {
   constexpr int LPR = D / 16;  // lanes of a row
@@ -367,6 +383,12 @@ __device__ __forceinline__ void append_block(const CacheAppendArgs& a, int32_t b
     unpack8(wa[u], xa[u]);
     unpack8(wb[u], xb[u]);
     if (kIsK) {
+      if constexpr (kNorm != 0) {
+        float ga[8], gb[8], ba[8], bb[8];
+        load_gain<D>(a.norm.k_gain, a.norm.k_heads, g, c8, 1.f, ga, gb);
+        load_gain<D>(a.norm.k_bias, a.norm.k_heads, g, c8, 0.f, ba, bb);
+        normalise16<D, kNorm>(a.norm.eps, ga, gb, ba, bb, xa[u], xb[u]);
+      }
       float2 cs[8];
       load_turns<D>(a, pos[u], c8, wide, cs);
       rotate16(a.rot.interleaved, cs, xa[u], xb[u]);
@@ -419,7 +441,7 @@ __device__ __forceinline__ void append_block(const CacheAppendArgs& a, int32_t b
 
 // Grid: first the (sequence, touched block, head) units of K, then those of V, then
 // those of q: a thread takes 16 columns of up to kHeads heads of a token.
-template <int D>
+template <int D, int kNorm>
 __global__ void __launch_bounds__(128 * (D / 16) / kPasses)
 cache_append_kernel(CacheAppendArgs a, int32_t touched, int64_t kv_units, bool wide) {
   constexpr int LPR = D / 16;
@@ -432,8 +454,8 @@ cache_append_kernel(CacheAppendArgs a, int32_t touched, int64_t kv_units, bool w
     const int32_t g = (int32_t)(unit % a.cache.Hkv);
     const int32_t bi = (int32_t)(unit / a.cache.Hkv);
     const int32_t b = bi / touched, i = bi - b * touched;
-    if (is_k) append_block<D, true>(a, b, i, g, wide, red);
-    else append_block<D, false>(a, b, i, g, wide, red);
+    if (is_k) append_block<D, true, kNorm>(a, b, i, g, wide, red);
+    else append_block<D, false, kNorm>(a, b, i, g, wide, red);
     return;
   }
   unit -= 2 * kv_units;
@@ -460,6 +482,7 @@ cache_append_kernel(CacheAppendArgs a, int32_t touched, int64_t kv_units, bool w
   if (slot < 0) return;
   float2 cs[8];
   load_turns<D>(a, pos, c8, wide, cs);
+  float ga[8], gb[8], ba[8], bb[8];  // (of the norm)
   __nv_bfloat16* y = static_cast<__nv_bfloat16*>(a.q_out) + ((int64_t)token * a.Hq + h0) * D + c8;
 #pragma unroll
   for (int u = 0; u < kHeads; ++u) {
@@ -467,6 +490,13 @@ cache_append_kernel(CacheAppendArgs a, int32_t touched, int64_t kv_units, bool w
     float xa[8], xb[8];
     unpack8(wa[u], xa);
     unpack8(wb[u], xb);
+    if constexpr (kNorm != 0) {
+      if (u == 0 || a.norm.q_heads != 0) {
+        load_gain<D>(a.norm.q_gain, a.norm.q_heads, h0 + u, c8, 1.f, ga, gb);
+        load_gain<D>(a.norm.q_bias, a.norm.q_heads, h0 + u, c8, 0.f, ba, bb);
+      }
+      normalise16<D, kNorm>(a.norm.eps, ga, gb, ba, bb, xa, xb);
+    }
     rotate16(a.rot.interleaved, cs, xa, xb);
     *reinterpret_cast<uint4*>(y + u * D) = pack8(xa);
     *reinterpret_cast<uint4*>(y + u * D + D / 2) = pack8(xb);
@@ -504,10 +534,15 @@ cudaError_t launch_cache_append(const CacheAppendArgs& a, cudaStream_t stream) {
   const int32_t s0 = a.rot.sec[0], s1 = s0 + a.rot.sec[1];
   const bool wide =
       s0 % 4 == 0 && s1 % 4 == 0 && (reinterpret_cast<uintptr_t>(a.rot.table) & 15) == 0;
-  return d == 128 ? launch_kernel(cache_append_kernel<128>, dim3((unsigned)grid), dim3(threads), 0,
-                                  stream, true, a, touched, kv_units, wide)
-                  : launch_kernel(cache_append_kernel<64>, dim3((unsigned)grid), dim3(threads), 0,
-                                  stream, true, a, touched, kv_units, wide);
+  auto launch = [&](auto kernel) {
+    return launch_kernel(kernel, dim3((unsigned)grid), dim3(threads), 0, stream, true, a, touched,
+                         kv_units, wide);
+  };
+  if (a.norm.kind == SSD_NORM_RMS)
+    return launch(d == 128 ? cache_append_kernel<128, 1> : cache_append_kernel<64, 1>);
+  if (a.norm.kind == SSD_NORM_LAYER)
+    return launch(d == 128 ? cache_append_kernel<128, 2> : cache_append_kernel<64, 2>);
+  return launch(d == 128 ? cache_append_kernel<128, 0> : cache_append_kernel<64, 0>);
 }
 
 }  // namespace ssd

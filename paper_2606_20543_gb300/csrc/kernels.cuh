@@ -426,8 +426,22 @@ struct CacheAppendArgs {
   int64_t ldq, ldk, ldv;
   void* q_out;
   int32_t* status;
+  ssd_head_norm norm;  // kind 0: none
 };
 cudaError_t launch_cache_append(const CacheAppendArgs& a, cudaStream_t stream);
+
+// ---- quantize.cu (e4m3 with a scale per 128 entries)
+struct QuantizeArgs {
+  int32_t rows, K, block_rows;
+  const void* x;
+  int32_t bf16;
+  int64_t ldx;
+  void* out;
+  int64_t ldo;
+  float* scale;
+  int64_t lds;
+};
+cudaError_t launch_quantize(const QuantizeArgs& a, cudaStream_t stream);
 
 // ---- cache_attention.cu
 struct CacheAttnArgs {

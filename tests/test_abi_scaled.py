@@ -1,0 +1,77 @@
+"""Host-side argument checks of the 8-bit products and of the head norms: codes come back
+without touching a GPU (every pointer below is a fake that is never read)."""
+import ctypes
+import shutil
+import os
+
+import pytest
+
+F = 0x1000
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if shutil.which("nvcc") is None and not os.path.exists("/usr/local/cuda/bin/nvcc"):
+        pytest.skip("nvcc not available")
+    from paper_2606_20543_gb300 import build
+    build.build()
+    import paper_2606_20543_gb300 as ssd
+    return ssd
+
+
+def test_quantize(lib):
+    so = lib.load()
+
+    def call(rows=200, K=300, block=1, x=F, bf16=1, ldx=304, out=F, ldo=304, scale=F, lds=200):
+        return so.ssd_quantize(rows, K, block, x, bf16, ldx, out, ldo, scale, lds, None)
+
+    assert call(rows=0, lds=0) == 0
+    assert call(rows=-1) == call(K=0) == call(block=0) == call(ldx=296) == call(ldo=288) == 2
+    assert call(ldx=308) == call(ldo=312) == call(lds=199) == call(block=128, lds=1) == 2
+    assert call(block=2) == call(block=64) == call(K=1 << 24, ldx=1 << 24, ldo=1 << 24) == 3
+    for name in ("x", "out", "scale"):
+        assert call(**{name: None}) == 1, name
+    assert call(bf16=2) == call(x=F + 8) == call(out=F + 8) == call(scale=F + 2) == 1
+
+
+def test_append_norm(lib):
+    so = lib.load()
+
+    def call(kind=1, eps=1e-6, gains=(F, F, F, F), heads=(0, 0), Hq=4, B=1, null=False, d=64):
+        c = lib.BlockCache(8, 16, 2, d, F, F, F, F)
+        r = lib.Rotary(F, 9, (ctypes.c_int32 * 3)(16, 8, 8), 0)
+        n = lib.HeadNorm(kind, eps, *gains, *heads)
+        return so.ssd_cache_append_norm(ctypes.byref(c), ctypes.byref(r),
+                                        None if null else ctypes.byref(n), B, 4, Hq, F, F, F, F, 256,
+                                        F, 128, F, 128, F + 4096, F, None)
+
+    assert call(B=0) == call(B=0, kind=2, heads=(4, 2), gains=(None, F, F, None)) == 0
+    assert call(null=True) == call(kind=0) == call(kind=3) == 1
+    for eps in (0.0, -1.0, float("inf"), float("nan")):
+        assert call(eps=eps) == 1
+    assert call(heads=(2, 0)) == call(heads=(0, 4)) == call(heads=(-1, 0)) == call(Hq=3) == 2
+    for i in range(4):
+        assert call(gains=[F + 4 if i == j else F for j in range(4)]) == 1
+
+
+def test_python_side_refusals(lib):
+    import torch
+    g = torch.ones(64)
+    with pytest.raises(ValueError):
+        lib.head_norm("rms", 1e-6, g)  # not on a GPU
+    with pytest.raises(ValueError):
+        lib.head_norm("rms", 1e-6, g.double())
+    with pytest.raises(ValueError):
+        lib.head_norm("rms", 1e-6, torch.ones(4, 64), g)
+    with pytest.raises(ValueError):
+        lib.head_norm("rms", 1e-6, torch.ones(64, 2)[:, 0])
+    with pytest.raises(ValueError):
+        lib.head_norm("rms", 1e-6, None, g, None, torch.ones(128))
+    n = lib.head_norm("layer", 1e-6)
+    assert (n.kind, n.q_heads, n.k_heads) == (2, 0, 0)
+    n.d = 128
+    with pytest.raises(ValueError):
+        lib.ssd_cache_append_norm(lib.BlockCache(8, 16, 2, 64, F, F, F, F), lib.Rotary(), n, 1, 1, 4,
+                                  *[None] * 12)
+    with pytest.raises(ValueError):
+        lib.ssd_quantize(1, 8, 1, torch.zeros((1, 8), dtype=torch.float16), 8, None, 16, None, 1)

@@ -737,6 +737,25 @@ ssd_status ssd_quantize(int32_t rows, int32_t K, int32_t block_rows, const void*
                         int64_t ldx, void* out, int64_t ldo, float* scale, int64_t lds,
                         ssd_stream_t stream);
 
+/* C = A W^T (+ add) of such rows and weights: with g the blocks of 128 of K,
+ *     C[m][n] = sum_g a_scale[g][m] * w_scale[g][n / 128] *
+ *                   sum_{k in g} A[m][k] W[n][k]   + add[m][n]
+ * Both sums in float32; rounded once, to C's type.  A NaN in A goes to its row
+ * of C, one in W to its column.
+ *   a        dev e4m3 [M][K], rows lda bytes apart; w dev e4m3 [N][K], ldw
+ *   a_scale  dev float32 [ceil(K / 128)][ldas], ldas >= M
+ *   w_scale  dev float32 [ceil(K / 128)][ldws], ldws >= ceil(N / 128)
+ *   add      dev bf16 [M][ldadd] or NULL; may be C itself (ldadd = ldc, bf16)
+ *   c        dev float32, or bf16 if c_bf16, [M][ldc] (columns from N on and
+ *            what lies behind K in A and W: untouched and unread)
+ * lda, ldw multiples of 16; a, w 16-byte aligned; any M, N, K and alignment of
+ * add and C to their elements. */
+ssd_status ssd_scaled_matmul(int32_t M, int32_t N, int32_t K, const void* a, int64_t lda,
+                             const float* a_scale, int64_t ldas, const void* w, int64_t ldw,
+                             const float* w_scale, int64_t ldws, const void* add, int64_t ldadd,
+                             void* c, int32_t c_bf16, int64_t ldc, int32_t* status,
+                             ssd_stream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

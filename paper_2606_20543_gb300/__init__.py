@@ -33,7 +33,7 @@ EXPORTED = ["ssd_abi_version", "ssd_status_string", "ssd_set_wait_limit",
             "ssd_verify_accept",
             "ssd_cache_plan", "ssd_rotary_table", "ssd_cache_append", "ssd_cache_append_norm",
             "ssd_cache_attention_workspace", "ssd_cache_attention", "ssd_sample",
-            "ssd_quantize"]
+            "ssd_quantize", "ssd_scaled_matmul"]
 
 
 STRATEGY_ACCEPT_REJECT, STRATEGY_GREEDY, STRATEGY_SAMPLE = 0, 1, 2
@@ -176,6 +176,8 @@ def load(path: Optional[str] = None) -> ctypes.CDLL:
         "ssd_sample": (I32, [I32, I32, P, I32, I64, ctypes.POINTER(Sampling), ctypes.POINTER(Rng),
                              P, P, P, P, P]),
         "ssd_quantize": (I32, [I32, I32, I32, P, I32, I64, P, I64, P, I64, P]),
+        "ssd_scaled_matmul": (I32, [I32, I32, I32, P, I64, P, I64, P, I64, P, I64, P, I64, P, I32,
+                                    I64, P, P]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -507,6 +509,20 @@ def ssd_quantize(rows, K, block_rows, x, ldx, out, ldo, scale, lds, stream=None)
     _check("ssd_quantize", load().ssd_quantize(
         rows, K, block_rows, _ptr(x), _is_bf16(x, "x"), ldx, _ptr(out), ldo, _ptr(scale), lds,
         _stream(stream)))
+
+
+def ssd_scaled_matmul(M, N, K, a, lda, a_scale, ldas, w, ldw, w_scale, ldws, add, ldadd, c, ldc,
+                      status, stream=None) -> None:
+    """C = A W^T (+ add) of e4m3 rows and weights with a scale per 128 (ssd_quantize); C float32
+    or bf16, add bf16 or None."""
+    if add is not None and str(add.dtype) != "torch.bfloat16":
+        raise ValueError("add is bfloat16")
+    for t in (a, w):
+        if t is not None and t.element_size() != 1:
+            raise ValueError("A and W hold 8-bit entries")
+    _check("ssd_scaled_matmul", load().ssd_scaled_matmul(
+        M, N, K, _ptr(a), lda, _ptr(a_scale), ldas, _ptr(w), ldw, _ptr(w_scale), ldws, _ptr(add),
+        ldadd, _ptr(c), _is_bf16(c, "C"), ldc, _ptr(status), _stream(stream)))
 
 
 def ssd_sample(rows, V, logits, ld, p: Sampling, r: Rng, out_tok, prob, kept, status,

@@ -42,4 +42,46 @@ ssd_status ssd_quantize(int32_t rows, int32_t K, int32_t block_rows, const void*
   return from_cuda(launch_quantize(a, (cudaStream_t)stream));
 }
 
+ssd_status ssd_scaled_matmul(int32_t M, int32_t N, int32_t K, const void* a, int64_t lda,
+                             const float* a_scale, int64_t ldas, const void* w, int64_t ldw,
+                             const float* w_scale, int64_t ldws, const void* add, int64_t ldadd,
+                             void* c, int32_t c_bf16, int64_t ldc, int32_t* status,
+                             ssd_stream_t stream) {
+  if (M < 0 || N <= 0 || K <= 0) return SSD_ERR_SHAPE;
+  if (c_bf16 != 0 && c_bf16 != 1) return SSD_ERR_INVALID_ARG;
+  if (lda < K || ldw < K || ldc < N || ldas < M || ldws < ((int64_t)N + kScaleGroup - 1) / kScaleGroup)
+    return SSD_ERR_SHAPE;
+  if (lda % 16 != 0 || ldw % 16 != 0 || (add != nullptr && ldadd < N)) return SSD_ERR_SHAPE;
+  if (M > INT32_MAX / 2 || N > INT32_MAX / 2 || K > INT32_MAX / 2) return SSD_ERR_UNSUPPORTED;
+  // what a tensor map can hold, and what 32-bit counts of tiles can
+  if (lda >= (int64_t)1 << 40 || ldw >= (int64_t)1 << 40) return SSD_ERR_UNSUPPORTED;
+  if (((int64_t)M / 128 + 1) * ((int64_t)N / 64 + 1) > INT32_MAX / 32) return SSD_ERR_UNSUPPORTED;
+  if (M == 0) return SSD_OK;
+  for (const void* p : {a, w, (const void*)a_scale, (const void*)w_scale, (const void*)c,
+                        (const void*)status})
+    if (p == nullptr) return SSD_ERR_INVALID_ARG;
+  if (!aligned(a, 16) || !aligned(w, 16) || !aligned(a_scale, 4) || !aligned(w_scale, 4) ||
+      !aligned(add, 2) || !aligned(c, c_bf16 ? 2 : 4))
+    return SSD_ERR_INVALID_ARG;
+  ScaledMatmulArgs x{};
+  x.M = M;
+  x.N = N;
+  x.K = K;
+  x.a = a;
+  x.lda = lda;
+  x.a_scale = a_scale;
+  x.ldas = ldas;
+  x.w = w;
+  x.ldw = ldw;
+  x.w_scale = w_scale;
+  x.ldws = ldws;
+  x.add = add;
+  x.ldadd = ldadd;
+  x.c = c;
+  x.c_bf16 = c_bf16;
+  x.ldc = ldc;
+  x.status = status;
+  return from_cuda(launch_scaled_matmul(x, (cudaStream_t)stream));
+}
+
 }  // extern "C"

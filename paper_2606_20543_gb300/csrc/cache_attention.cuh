@@ -63,13 +63,6 @@ __host__ __device__ __forceinline__ CacheShares cache_shares(const CacheAttnLaun
                      cut.y - cut.x + 1};
 }
 
-// mbar_wait_warp() with one try ahead of the loop: a wait for what is there already takes a try
-// and a vote (through the loop 220 cycles on a busy SM, of the 2200 that a tile of 64 keys takes).
-__device__ __forceinline__ bool wait_warp(uint64_t* bar, uint32_t parity, int32_t* status) {
-  if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
-  return mbar_wait_warp(bar, parity, status);
-}
-
 // A row's way out.  A row that sees no key has the sum 0, and nothing else has: then it is 0 and
 // -inf, whatever its products are (0 times a NaN of the pool).  A NaN in a key that it sees, or in
 // its query, makes the sum a NaN, and that goes out.

@@ -443,6 +443,26 @@ struct QuantizeArgs {
 };
 cudaError_t launch_quantize(const QuantizeArgs& a, cudaStream_t stream);
 
+// ---- scaled_matmul.cu
+struct ScaledMatmulArgs {
+  int32_t M, N, K;
+  const void* a;         // e4m3 [M][lda]
+  int64_t lda;
+  const float* a_scale;  // [K / 128][ldas]
+  int64_t ldas;
+  const void* w;         // e4m3 [N][ldw]
+  int64_t ldw;
+  const float* w_scale;  // [K / 128][ldws], a scale per 128 rows
+  int64_t ldws;
+  const void* add;       // bf16 [M][ldadd], nullable
+  int64_t ldadd;
+  void* c;               // float32 or bf16 [M][ldc]
+  int32_t c_bf16;
+  int64_t ldc;
+  int32_t* status;
+};
+cudaError_t launch_scaled_matmul(const ScaledMatmulArgs& a, cudaStream_t stream);
+
 // ---- cache_attention.cu
 struct CacheAttnArgs {
   ssd_grid grid;

@@ -34,6 +34,25 @@ def test_quantize(lib):
     assert call(bf16=2) == call(x=F + 8) == call(out=F + 8) == call(scale=F + 2) == 1
 
 
+def test_matmul(lib):
+    so = lib.load()
+
+    def call(M=5, N=200, K=300, a=F, lda=304, sa=F, ldas=5, w=F, ldw=304, sw=F, ldws=2, add=None, ldadd=0,
+             c=F, bf16=1, ldc=200, st=F):
+        return so.ssd_scaled_matmul(M, N, K, a, lda, sa, ldas, w, ldw, sw, ldws, add, ldadd, c, bf16, ldc,
+                                    st, None)
+
+    assert call(M=0) == 0
+    assert call(M=-1) == call(N=0) == call(K=0) == call(lda=288) == call(ldw=288) == call(ldc=199) == 2
+    assert call(ldas=4) == call(ldws=1) == call(lda=312) == call(ldw=308) == call(add=F, ldadd=199) == 2
+    big = 1 << 30
+    assert call(M=big, ldas=big, N=big, ldc=big, ldws=big) == call(lda=1 << 40) == 3
+    for name in ("a", "w", "sa", "sw", "c", "st"):
+        assert call(**{name: None}) == 1, name
+    assert call(a=F + 8) == call(w=F + 8) == call(sa=F + 2) == call(sw=F + 1) == call(c=F + 1) == 1
+    assert call(bf16=0, c=F + 2) == call(bf16=2) == call(add=F + 1, ldadd=200) == 1
+
+
 def test_append_norm(lib):
     so = lib.load()
 
@@ -73,5 +92,11 @@ def test_python_side_refusals(lib):
     with pytest.raises(ValueError):
         lib.ssd_cache_append_norm(lib.BlockCache(8, 16, 2, 64, F, F, F, F), lib.Rotary(), n, 1, 1, 4,
                                   *[None] * 12)
+    with pytest.raises(ValueError):
+        lib.ssd_scaled_matmul(1, 1, 16, None, 16, None, 1, None, 16, None, 1, torch.zeros(1), 1, None, 1,
+                              None)
+    with pytest.raises(ValueError):
+        lib.ssd_scaled_matmul(1, 1, 16, torch.zeros(16), 16, None, 1, None, 16, None, 1, None, 1, None, 1,
+                              None)
     with pytest.raises(ValueError):
         lib.ssd_quantize(1, 8, 1, torch.zeros((1, 8), dtype=torch.float16), 8, None, 16, None, 1)

@@ -5,17 +5,14 @@
 // The scales change along the inner length, so no accumulator of the tensor cores can hold the sum
 // over g: a block of 128 (four tcgen05.mma of kind::f8f6f4) goes into a TMEM buffer of its own, and
 // the epilogue's warps add it, times its scales, to sums in their registers while the tensor
-// cores work on the next block in another buffer.
+// cores work on the next blocks in other buffers.
 //
-// One operand's rows are the 128 lanes of a tile, the other's its TN columns:
-//  - more than 64 rows: the rows of A on the lanes (the scales are then one number a thread), over
-//    64 or 128 rows of W, or a CTA pair (cta_group::2) with 128 lanes each over 256;
-//  - fewer: the rows of W on the lanes and those of A as 16, 32 or 64 columns, so that a decode's
-//    few rows do not leave most of each product empty.  What bounds it is W's way in, so a tile's
-//    inner length is cut over a cluster of CTAs where the tiles alone would leave SMs idle;
-//    they add their sums up through distributed shared memory, in the order of their ranks.
-// Warps of a CTA: the epilogue's four (or eight), one that copies the lanes' operand, one that
-// issues the products, one that copies the columns' operand.
+// More than 64 rows: the rows of A are the 128 lanes of a tile (the scales of a block are then one
+// number a thread), 128 rows of W its columns, or 256 over a CTA pair (cta_group::2) with 128 lanes
+// each.  Up to 64 rows: the other way round (scaled_matmul_few_kernel).
+//
+// Barriers count units of U blocks: a wait that is satisfied already costs a warp about 100
+// cycles, a commit of products as much.
 #include <algorithm>
 
 #include "kernels.cuh"
@@ -28,29 +25,33 @@ constexpr int kGroup = 128;  // entries of a scale, bytes of a stage's rows
 constexpr int kLaneRows = 128;
 constexpr int kPitch = 36;   // floats of a staged row of 32 (rows start four banks apart)
 constexpr int kRaster = 8;   // tiles of lanes that share the columns' tiles in L2
+constexpr int kAhead = 4;    // blocks whose scales are asked for together
+constexpr int kMaxSplits = 8;
 
-template <bool SWAP, bool PAIR, int TN>
+template <bool PAIR, int TN, int U>
 struct Shape {
-  static constexpr int EW = TN > 128 ? 8 : 4;             // epilogue warps
+  static constexpr int EW = TN >= 128 ? 8 : 4;            // epilogue warps
   static constexpr int CW = TN / (EW / 4);                // columns of one
-  static constexpr int kThreads = (EW + 3) * 32;
-  static constexpr int NB = TN >= 128 ? 2 : 4;            // TMEM buffers
-  static constexpr int kLBytes = kLaneRows * kGroup;
+  static constexpr int CR = CW < 64 ? CW : 64;            // columns read from TMEM at a time
+  static constexpr int CH = CW < 32 ? CW : 32;            // columns staged at a time
+  // (a pair's epilogue takes registers from the others, warpgroup by warpgroup)
+  static constexpr int kThreads = (EW + (PAIR ? 4 : 3)) * 32;
+  static constexpr int kCols = 2 * U * TN;                // two units in TMEM
   static constexpr int kCRows = PAIR ? TN / 2 : TN;       // of a CTA's copy
   static constexpr int kCBytes = kCRows * kGroup;
-  static constexpr int kStage = kLBytes + kCBytes;
-  static constexpr int kCtas = SWAP || TN == 64 ? 2 : 1;  // per SM
-  static constexpr int S = PAIR ? 5 : SWAP ? (TN == 16 ? 6 : TN == 32 ? 5 : 4) : TN == 64 ? 3 : 6;
-  static constexpr int P = EW == 8 ? 4 : 8;               // blocks whose scales are under way
-  static constexpr int kRingFloats = SWAP ? EW * P * (TN + 4) : 2 * P * EW * 32;
-  static constexpr int kStaging = SWAP ? 0 : EW * 32 * kPitch * 4;
-  static constexpr int kSmem = 1024 + S * kStage + kStaging + kRingFloats * 4;
-  static_assert(!SWAP || S * kStage >= TN * kLaneRows * 4, "a CTA's sums fit where its stages were");
+  static constexpr int kStaging = EW * 32 * kPitch * 4;
+  static constexpr int kScales = 2 * kAhead * 2 * EW * 32 * 4;
+  static constexpr int kFixed = 1024 + kStaging + kScales;
+  static constexpr int kABytes = kLaneRows * kGroup;
+  static constexpr int kStage = U * (kABytes + kCBytes);
+  static constexpr int S = (224 * 1024 - kFixed) / kStage;
+  static constexpr int kSmem = kFixed + S * kStage;
+  static_assert(kCols <= 512 && kAhead % U == 0 && S >= 2, "");
 };
 
 struct Launch {
-  int32_t tiles_l, tiles_c, splits;
-  int32_t vec;  // C (and add) may be written four columns at a time
+  int32_t tiles_l, tiles_c;
+  int32_t vec;  // C may be written, and add read, 16 bytes of C at a time
 };
 
 __device__ __forceinline__ void cp_async4(uint32_t dst, const float* src, bool live) {
@@ -62,117 +63,274 @@ template <int N>
 __device__ __forceinline__ void cp_async_wait() {
   asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
+// The arrival of the warp's lane 0 at a barrier of the cluster.  Relaxed: what it hands over is tensor
+// memory, ordered by tcgen05.fence; a release would wait for the lanes' own copies of scales
+// (17408 x 12288 x 4096: 1750 us instead of 850).
+__device__ __forceinline__ void arrive_peer_lane0(uint32_t bar, int lane) {
+  asm volatile(
+      "{\n .reg .pred p;\n setp.eq.u32 p, %1, 0;\n"
+      " @p mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];\n}" ::"r"(bar),
+      "r"(lane)
+      : "memory");
+}
 __device__ __forceinline__ float ld_peer(uint32_t addr) {
   float v;
   asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
   return v;
-}
-// An arrival at a barrier of the cluster.
-__device__ __forceinline__ void arrive_peer(uint32_t bar) {
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 // fp32 sums of e4m3 products, M x N, both operands K-major.
 __host__ __device__ constexpr uint32_t idesc_e4m3(int m, int n) {
   return (1u << 4) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
 }
 
-__device__ __forceinline__ float from_bf16(const void* p, int64_t at) {
-  return __uint_as_float((uint32_t)static_cast<const uint16_t*>(p)[at] << 16);
+// Columns of this thread's TMEM lane, without the wait, and the wait for them.
+__device__ __forceinline__ void tmem_ask(uint32_t taddr, uint32_t (&r)[64]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x64.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+      "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,"
+      "%32,%33,%34,%35,%36,%37,%38,%39,%40,%41,%42,%43,%44,%45,%46,%47,"
+      "%48,%49,%50,%51,%52,%53,%54,%55,%56,%57,%58,%59,%60,%61,%62,%63}, [%64];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]),
+        "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]),
+        "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]),
+        "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+        "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]),
+        "=r"(r[30]), "=r"(r[31]), "=r"(r[32]), "=r"(r[33]), "=r"(r[34]), "=r"(r[35]),
+        "=r"(r[36]), "=r"(r[37]), "=r"(r[38]), "=r"(r[39]), "=r"(r[40]), "=r"(r[41]),
+        "=r"(r[42]), "=r"(r[43]), "=r"(r[44]), "=r"(r[45]), "=r"(r[46]), "=r"(r[47]),
+        "=r"(r[48]), "=r"(r[49]), "=r"(r[50]), "=r"(r[51]), "=r"(r[52]), "=r"(r[53]),
+        "=r"(r[54]), "=r"(r[55]), "=r"(r[56]), "=r"(r[57]), "=r"(r[58]), "=r"(r[59]),
+        "=r"(r[60]), "=r"(r[61]), "=r"(r[62]), "=r"(r[63])
+      : "r"(taddr)
+      : "memory");
 }
+__device__ __forceinline__ void tmem_have(uint32_t (&r)[64]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]),
+                 "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]),
+                 "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(r[16]), "+r"(r[17]),
+                 "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]),
+                 "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]),
+                 "+r"(r[30]), "+r"(r[31]), "+r"(r[32]), "+r"(r[33]), "+r"(r[34]), "+r"(r[35]),
+                 "+r"(r[36]), "+r"(r[37]), "+r"(r[38]), "+r"(r[39]), "+r"(r[40]), "+r"(r[41]),
+                 "+r"(r[42]), "+r"(r[43]), "+r"(r[44]), "+r"(r[45]), "+r"(r[46]), "+r"(r[47]),
+                 "+r"(r[48]), "+r"(r[49]), "+r"(r[50]), "+r"(r[51]), "+r"(r[52]), "+r"(r[53]),
+                 "+r"(r[54]), "+r"(r[55]), "+r"(r[56]), "+r"(r[57]), "+r"(r[58]), "+r"(r[59]),
+                 "+r"(r[60]), "+r"(r[61]), "+r"(r[62]), "+r"(r[63])
+               :
+               : "memory");
+}
+__device__ __forceinline__ void tmem_ask(uint32_t taddr, uint32_t (&r)[32]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+      "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]),
+        "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]),
+        "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]),
+        "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+        "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]),
+        "=r"(r[30]), "=r"(r[31])
+      : "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_have(uint32_t (&r)[32]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]),
+                 "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]),
+                 "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(r[16]), "+r"(r[17]),
+                 "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]),
+                 "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]),
+                 "+r"(r[30]), "+r"(r[31])
+               :
+               : "memory");
+}
+__device__ __forceinline__ void tmem_ask(uint32_t taddr, uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]),
+        "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]),
+        "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_have(uint32_t (&r)[16]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]),
+                 "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]),
+                 "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
+               :
+               : "memory");
+}
+// mbar_drain(), inlined: a call has no place beside setmaxnreg.
+__device__ __forceinline__ void drain(uint64_t* bar, uint32_t parity) {
+#pragma unroll 1
+  for (int i = 0; i < (1 << 14) && !mbar_try_wait(bar, parity); ++i) __nanosleep(256);
+}
+
+// A warp's CH columns from n0 on of `rows` rows of C from m0 on: staged with kPitch floats a row, each
+// store whole sectors of a few rows.  vec: 16 bytes a lane, all asked for (of add) before the first
+// is used; else an element.
+template <int CH>
+__device__ __forceinline__ void write_rows(const ScaledMatmulArgs& a, const float* st, int lane,
+                                           int64_t m0, int32_t rows, int32_t n0, bool vec) {
+  const uint16_t* add = static_cast<const uint16_t*>(a.add);
+  vec = vec && n0 + CH <= a.N;
+  if (vec && a.c_bf16) {
+    constexpr int kL = CH / 8, kRows = 32 / kL;  // lanes of a row, rows of a pass
+    const int32_t r0 = lane / kL, c = lane % kL * 8, n = n0 + c;
+    uint4 w[kL];
+#pragma unroll
+    for (int i = 0; i < kL; ++i) {
+      w[i] = make_uint4(0, 0, 0, 0);
+      if (add != nullptr && r0 + i * kRows < rows)
+        w[i] = *reinterpret_cast<const uint4*>(add + (m0 + r0 + i * kRows) * a.ldadd + n);
+    }
+    __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.c) + (m0 + r0) * a.ldc + n;
+#pragma unroll
+    for (int i = 0; i < kL; ++i) {
+      const float4 x = *reinterpret_cast<const float4*>(st + (r0 + i * kRows) * kPitch + c);
+      const float4 y = *reinterpret_cast<const float4*>(st + (r0 + i * kRows) * kPitch + c + 4);
+      const uint32_t* v = &w[i].x;
+      const uint4 z = make_uint4(
+          pack_bf16x2(x.x + __uint_as_float(v[0] << 16), x.y + __uint_as_float(v[0] & 0xffff0000u)),
+          pack_bf16x2(x.z + __uint_as_float(v[1] << 16), x.w + __uint_as_float(v[1] & 0xffff0000u)),
+          pack_bf16x2(y.x + __uint_as_float(v[2] << 16), y.y + __uint_as_float(v[2] & 0xffff0000u)),
+          pack_bf16x2(y.z + __uint_as_float(v[3] << 16), y.w + __uint_as_float(v[3] & 0xffff0000u)));
+      if (r0 + i * kRows < rows) *reinterpret_cast<uint4*>(out) = z;
+      out += kRows * a.ldc;
+    }
+    return;
+  } else if (vec) {
+    constexpr int kL = CH / 4, kRows = 32 / kL;
+    const int32_t r0 = lane / kL, c = lane % kL * 4, n = n0 + c;
+    uint2 w[kL];
+#pragma unroll
+    for (int i = 0; i < kL; ++i) {
+      w[i] = make_uint2(0, 0);
+      if (add != nullptr && r0 + i * kRows < rows)
+        w[i] = *reinterpret_cast<const uint2*>(add + (m0 + r0 + i * kRows) * a.ldadd + n);
+    }
+    float* out = static_cast<float*>(a.c) + (m0 + r0) * a.ldc + n;
+#pragma unroll
+    for (int i = 0; i < kL; ++i) {
+      float4 x = *reinterpret_cast<const float4*>(st + (r0 + i * kRows) * kPitch + c);
+      x.x += __uint_as_float(w[i].x << 16);
+      x.y += __uint_as_float(w[i].x & 0xffff0000u);
+      x.z += __uint_as_float(w[i].y << 16);
+      x.w += __uint_as_float(w[i].y & 0xffff0000u);
+      if (r0 + i * kRows < rows) *reinterpret_cast<float4*>(out) = x;
+      out += kRows * a.ldc;
+    }
+    return;
+  }
+  // an element each, a lane's column of eight rows together
+  const int32_t n = n0 + lane;
+  if (lane >= CH || n >= a.N) return;
+  const int64_t at = m0 * a.ldc + n;
+  const uint16_t* from = add + m0 * a.ldadd + n;
+#pragma unroll 1
+  for (int32_t r = 0; r < rows; r += 8) {
+    float x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      x[i] = st[(r + i) * kPitch + lane];
+      if (add != nullptr && r + i < rows) x[i] += __uint_as_float((uint32_t)from[(r + i) * a.ldadd] << 16);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (r + i >= rows || !dbg_in(at + (r + i) * a.ldc, (a.M - 1) * a.ldc + a.N, a.status)) continue;
+      if (a.c_bf16) static_cast<__nv_bfloat16*>(a.c)[at + (r + i) * a.ldc] = __float2bfloat16_rn(x[i]);
+      else static_cast<float*>(a.c)[at + (r + i) * a.ldc] = x[i];
+    }
+  }
+}
+
 __device__ __forceinline__ void store_one(const ScaledMatmulArgs& a, int64_t m, int32_t n, float x) {
   if (!dbg_in(m * a.ldc + n, (a.M - 1) * a.ldc + a.N, a.status)) return;
-  if (a.add != nullptr) x += from_bf16(a.add, m * a.ldadd + n);
+  if (a.add != nullptr)
+    x += __uint_as_float((uint32_t)static_cast<const uint16_t*>(a.add)[m * a.ldadd + n] << 16);
   if (a.c_bf16) static_cast<__nv_bfloat16*>(a.c)[m * a.ldc + n] = __float2bfloat16_rn(x);
   else static_cast<float*>(a.c)[m * a.ldc + n] = x;
 }
-__device__ __forceinline__ void store_four(const ScaledMatmulArgs& a, int64_t m, int32_t n, float4 x) {
-  if (!dbg_in(m * a.ldc + n + 3, (a.M - 1) * a.ldc + a.N, a.status)) return;
-  if (a.add != nullptr) {
-    const uint2 w = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(a.add) + m * a.ldadd + n);
-    x.x += __uint_as_float(w.x << 16);
-    x.y += __uint_as_float(w.x & 0xffff0000u);
-    x.z += __uint_as_float(w.y << 16);
-    x.w += __uint_as_float(w.y & 0xffff0000u);
-  }
-  if (a.c_bf16)
-    *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.c) + m * a.ldc + n) =
-        make_uint2(pack_bf16x2(x.x, x.y), pack_bf16x2(x.z, x.w));
-  else
-    *reinterpret_cast<float4*>(static_cast<float*>(a.c) + m * a.ldc + n) = x;
-}
 
-template <bool SWAP, bool PAIR, int TN>
-__global__ void __launch_bounds__(Shape<SWAP, PAIR, TN>::kThreads, Shape<SWAP, PAIR, TN>::kCtas)
-scaled_matmul_kernel(const __grid_constant__ CUtensorMap tmL, const __grid_constant__ CUtensorMap tmC,
+// Registers of a pair's CTA: 384 threads of 168 at launch, then 256 of 216 and 128 of 72.
+constexpr int kRegsEpilogue = 216, kRegsOther = 72;
+
+template <bool PAIR, int TN, int U>
+__global__ void __launch_bounds__(Shape<PAIR, TN, U>::kThreads, 1)
+scaled_matmul_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmW,
                      ScaledMatmulArgs a, Launch L) {
-  using H = Shape<SWAP, PAIR, TN>;
-  constexpr int EW = H::EW, CW = H::CW, NB = H::NB, S = H::S, P = H::P;
+  using H = Shape<PAIR, TN, U>;
+  constexpr int EW = H::EW, CW = H::CW, CR = H::CR, CH = H::CH;
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>(
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  float* staging = reinterpret_cast<float*>(smem + S * H::kStage);
-  float* ring = reinterpret_cast<float*>(smem + S * H::kStage + H::kStaging);
-  __shared__ uint64_t full[S], empty[S], tfull[NB], tempty[NB];
+  // a stage: U blocks of A [128][128], U blocks of W [kCRows][128]
+  constexpr int S = H::S, a_bytes = H::kABytes, stage_bytes = H::kStage;
+  float* staging = reinterpret_cast<float*>(smem + S * stage_bytes);
+  float* scales = staging + H::kStaging / 4;
+  __shared__ uint64_t full[S], empty[S], tfull[2], tempty[2];
   __shared__ uint32_t tmem_slot;
   pdl_wait();
 
   const int32_t tid = threadIdx.x, lane = tid & 31, warp = (int32_t)warp_uniform(tid >> 5);
-  const int32_t cluster = PAIR ? 2 : L.splits;
-  const int32_t rank = cluster > 1 ? (int32_t)(blockIdx.x % cluster) : 0;
-  const int32_t first = blockIdx.x / cluster, step = gridDim.x / cluster;
+  const int32_t rank = PAIR ? (int32_t)(blockIdx.x & 1) : 0;
+  const int32_t first = PAIR ? blockIdx.x >> 1 : blockIdx.x, step = PAIR ? gridDim.x >> 1 : gridDim.x;
   const int32_t total = L.tiles_l * L.tiles_c;
   const int32_t blocks = (a.K + kGroup - 1) / kGroup;
-  int32_t kb_lo = 0, kb_hi = blocks;
-  if (SWAP && cluster > 1) {
-    kb_lo = (int32_t)((int64_t)blocks * rank / cluster);
-    kb_hi = (int32_t)((int64_t)blocks * (rank + 1) / cluster);
-  }
-  if (tid == 0) {
+  if (warp == EW && lane < 2) prefetch_tensormap(lane == 0 ? &tmA : &tmW);
+  if (tid == EW * 32) {
     for (int i = 0; i < S; ++i) {
       mbar_init(&full[i], 2);  // the two producers
       mbar_init(&empty[i], 1);
     }
-    for (int i = 0; i < NB; ++i) {
+    for (int i = 0; i < 2; ++i) {
       mbar_init(&tfull[i], 1);
       mbar_init(&tempty[i], PAIR ? 2 * EW : EW);
     }
     fence_barrier_init();
   }
-  if (warp == EW + 1) {
-    if constexpr (PAIR) {
-      tmem_alloc_pair(&tmem_slot, NB * TN);
-      tmem_relinquish_pair();
-    } else {
-      tmem_alloc(&tmem_slot, NB * TN);
-      tmem_relinquish();
-    }
+  if constexpr (PAIR) {
+    __syncwarp();
+    cluster_sync_all();  // (the peer's barriers too are initialised)
+  } else {
+    __syncthreads();
   }
-  if (warp == EW && lane < 2) prefetch_tensormap(lane == 0 ? &tmL : &tmC);
-  tc_fence_before();
-  if constexpr (PAIR) cluster_sync_all();  // (the peer's barriers too are initialised)
-  else __syncthreads();
-  tc_fence_after();
-  const uint32_t tmem = tmem_slot;
-
-  // Tile i: which rows of the lanes' and of the columns' operand.
-  auto tile_of = [&](int32_t i, int32_t& l, int32_t& c) {
-    if constexpr (SWAP) {
-      c = i / L.tiles_l;
-      l = i - c * L.tiles_l;
-    } else {
-      const int32_t per = kRaster * L.tiles_c, g = i / per, r = i - g * per;
-      const int32_t n = min(kRaster, L.tiles_l - g * kRaster);
-      c = r / n;
-      l = g * kRaster + r - c * n;
+  // (the copies begin without tensor memory)
+  uint32_t tmem = 0;
+  if (warp <= EW + 1 && warp != EW) {
+    if (warp == EW + 1) {
+      if constexpr (PAIR) {
+        tmem_alloc_pair(&tmem_slot, H::kCols);
+        tmem_relinquish_pair();
+      } else {
+        tmem_alloc(&tmem_slot, H::kCols);
+        tmem_relinquish();
+      }
+      tc_fence_before();
     }
+    asm volatile("bar.sync 1, %0;" ::"n"((EW + 1) * 32) : "memory");
+    tc_fence_after();
+    tmem = tmem_slot;
+  }
+
+  // Tile i: which rows of A and of W.
+  auto tile_of = [&](int32_t i, int32_t& l, int32_t& c) {
+    const int32_t per = kRaster * L.tiles_c, g = i / per, r = i - g * per;
+    const int32_t n = min(kRaster, L.tiles_l - g * kRaster);
+    c = r / n;
+    l = g * kRaster + r - c * n;
   };
 
+  if (warp >= EW) {
+    if constexpr (PAIR) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOther));
+  }
   if (warp == EW || warp == EW + 2) {
     // ---------------------------------------------------------- producers
-    const bool lanes = warp == EW, leader = elect_one();
-    const uint64_t pol = !SWAP ? policy_evict_normal()
-                               : lanes ? policy_evict_first() : policy_evict_last();
-    const uint32_t bytes = (PAIR ? 2u : 1u) * (lanes ? H::kLBytes : H::kCBytes);
+    const bool of_a = warp == EW, leader = elect_one();
+    const uint64_t pol = policy_evict_normal();
+    const int32_t block_bytes = of_a ? a_bytes : H::kCBytes, at = of_a ? 0 : U * a_bytes;
+    const CUtensorMap* map = of_a ? &tmA : &tmW;
     const uint32_t full0 = PAIR ? peer_addr(smem_u32(full), 0) : 0;
     bool ok = true;
     int32_t n = 0, s = 0;
@@ -181,19 +339,24 @@ scaled_matmul_kernel(const __grid_constant__ CUtensorMap tmL, const __grid_const
     for (int32_t i = first; i < total && ok; i += step) {
       int32_t l, c;
       tile_of(i, l, c);
-      const int32_t row = lanes ? (PAIR ? 2 * l + rank : l) * kLaneRows
-                                : c * TN + (PAIR ? rank * H::kCRows : 0);
+      const int32_t row = of_a ? (PAIR ? 2 * l + rank : l) * kLaneRows
+                               : c * TN + (PAIR ? rank * H::kCRows : 0);
 #pragma unroll 1
-      for (int32_t kb = kb_lo; kb < kb_hi; ++kb, ++n) {
+      for (int32_t kb = 0; kb < blocks; kb += U, ++n) {
         if (n >= S) ok = wait_warp(&empty[s], ph, a.status);
         if (!ok) break;
         if (leader) {
-          unsigned char* dst = smem + s * H::kStage + (lanes ? 0 : H::kLBytes);
-          if (!PAIR || rank == 0) mbar_arrive_expect_tx(&full[s], bytes);
-          if constexpr (PAIR)
-            tma_load_2d_pair(dst, lanes ? &tmL : &tmC, kb * kGroup, row, full0 + 8 * s, pol);
-          else
-            tma_load_2d(dst, lanes ? &tmL : &tmC, kb * kGroup, row, &full[s], pol);
+          unsigned char* dst = smem + s * stage_bytes + at;
+          const int32_t un = min(U, blocks - kb);
+          if (!PAIR || rank == 0) mbar_arrive_expect_tx(&full[s], (PAIR ? 2 : 1) * un * block_bytes);
+#pragma unroll
+          for (int u = 0; u < U; ++u) {
+            if (u >= un) break;
+            if constexpr (PAIR)
+              tma_load_2d_pair(dst + u * block_bytes, map, (kb + u) * kGroup, row, full0 + 8 * s, pol);
+            else
+              tma_load_2d(dst + u * block_bytes, map, (kb + u) * kGroup, row, &full[s], pol);
+          }
         }
         __syncwarp();
         if (++s == S) {
@@ -203,9 +366,9 @@ scaled_matmul_kernel(const __grid_constant__ CUtensorMap tmL, const __grid_const
       }
     }
     // after a wait that gave up, the copies in flight still land here (a pair's are counted by
-    // its even CTA, which waits for both below)
+    // its even CTA, for which the other waits below)
     if (!ok && rank == 0)
-      for (int32_t u = max(0, n - S); u < n; ++u) mbar_drain(&full[u % S], (u / S) & 1);
+      for (int32_t u = max(0, n - S); u < n; ++u) drain(&full[u % S], (u / S) & 1);
   } else if (warp == EW + 1) {
     // ----------------------------------------------------------- products
     if (!PAIR || rank == 0) {
@@ -218,28 +381,35 @@ scaled_matmul_kernel(const __grid_constant__ CUtensorMap tmL, const __grid_const
 #pragma unroll 1
       for (int32_t i = first; i < total && ok; i += step) {
 #pragma unroll 1
-        for (int32_t kb = kb_lo; kb < kb_hi; ++kb, ++n) {
-          const int b = n % NB;
-          if (n >= NB) ok = wait_warp(&tempty[b], ((n / NB) - 1) & 1, a.status);
-          ok = ok && wait_warp(&full[s], ph, a.status);
+        for (int32_t kb = 0; kb < blocks; kb += U, ++n) {
+          const int b = n & 1;
+          ok = wait_warp(&full[s], ph, a.status);
+          // (last: what these products mostly wait for)
+          if (ok && n >= 2) ok = wait_warp(&tempty[b], ((n >> 1) - 1) & 1, a.status);
           if (!ok) break;
           tc_fence_after();
-          const uint64_t dl = smem_desc(base + s * H::kStage, 16, 1024);
-          const uint64_t dc = smem_desc(base + s * H::kStage + H::kLBytes, 16, 1024);
+          const uint64_t da = smem_desc(base + s * stage_bytes, 16, 1024);
+          const uint64_t dw = smem_desc(base + s * stage_bytes + U * a_bytes, 16, 1024);
           if (leader) {
+            // (blocks in turn: a product that adds to the one before it waits for it, 110 cycles
+            // of which 32 columns are work)
 #pragma unroll
             for (int k = 0; k < kGroup / 32; ++k) {
-              if constexpr (PAIR)
-                mma8_ss_pair(tm + b * TN, smem_desc_at(dl, k * 32), smem_desc_at(dc, k * 32), kIdesc, k > 0);
-              else
-                mma8_ss(tm + b * TN, smem_desc_at(dl, k * 32), smem_desc_at(dc, k * 32), kIdesc, k > 0);
+#pragma unroll
+              for (int u = 0; u < U; ++u) {
+                if (U > 1 && kb + u >= blocks) break;
+                const uint64_t x = smem_desc_at(da, u * a_bytes + k * 32);
+                const uint64_t y = smem_desc_at(dw, u * H::kCBytes + k * 32);
+                if constexpr (PAIR) mma8_ss_pair(tm + (b * U + u) * TN, x, y, kIdesc, k > 0);
+                else mma8_ss(tm + (b * U + u) * TN, x, y, kIdesc, k > 0);
+              }
             }
             if constexpr (PAIR) {
-              mma_commit_pair(&empty[s]);
               mma_commit_pair(&tfull[b]);
+              mma_commit_pair(&empty[s]);
             } else {
-              mma_commit(&empty[s]);
               mma_commit(&tfull[b]);
+              mma_commit(&empty[s]);
             }
           }
           __syncwarp();
@@ -249,162 +419,125 @@ scaled_matmul_kernel(const __grid_constant__ CUtensorMap tmL, const __grid_const
           }
         }
       }
-      if (!ok && n > 0) mbar_drain(&tfull[(n - 1) % NB], ((n - 1) / NB) & 1);
+      if (!ok && n > 0) drain(&tfull[(n - 1) & 1], ((n - 1) >> 1) & 1);
     }
-  } else {
+  } else if (warp < EW) {
     // ----------------------------------------------------------- epilogue
+    if constexpr (PAIR) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsEpilogue));
     const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
     const int32_t col = (warp >> 2) * CW;  // the warp's first column of a tile
-    const int32_t my_lane = (warp & 3) * 32 + lane;
     const uint32_t tempty0 = PAIR ? peer_addr(smem_u32(tempty), 0) : 0;
-    // Scales come by cp.async, P - 1 blocks ahead (over the end of a tile, too), into slots that
-    // only this thread reads (lanes are rows of A) or only this warp.
-    int32_t ahead_tile = first, ahead_kb = kb_lo, ahead_slot = 0;
-    int32_t al = 0, ac = 0;
-    tile_of(first, al, ac);
-    const uint32_t ring_at = smem_u32(ring);
+    // Scales come by cp.async, kAhead blocks together and as many ahead (over the end of a tile,
+    // too), into slots that only this thread reads: [2][kAhead][A's, W's][thread].
+    constexpr int kSlot = 2 * EW * 32;
+    const uint32_t scales_at = smem_u32(scales + tid);
+    int32_t next_tile = first, next_kb = blocks;
+    uint32_t next_half = 0;
+    const float* next_a = nullptr;
+    const float* next_w = nullptr;
+    bool live_a = false, live_w = false;
     auto ask = [&]() {
-      if (ahead_tile < total) {
-        if constexpr (SWAP) {
-          const uint32_t to = ring_at + (uint32_t)((warp * P + ahead_slot) * (TN + 4)) * 4;
-#pragma unroll
-          for (int u = 0; u < TN; u += 32) {
-            const int32_t t = u + lane, m = ac * TN + t;
-            if (t < TN) cp_async4(to + t * 4, a.a_scale + ahead_kb * a.ldas + min(m, a.M - 1), m < a.M);
-          }
-          if (lane == 0) cp_async4(to + TN * 4, a.w_scale + ahead_kb * a.ldws + al, true);
-        } else {
-          const uint32_t to = ring_at + (uint32_t)(ahead_slot * 2 * EW * 32 + tid) * 4;
-          const int32_t m = (PAIR ? 2 * al + rank : al) * kLaneRows + my_lane;
-          const int32_t n = ac * TN + col;
-          cp_async4(to, a.a_scale + ahead_kb * a.ldas + min(m, a.M - 1), m < a.M);
-          cp_async4(to + EW * 32 * 4, a.w_scale + ahead_kb * a.ldws + min(n, a.N - 1) / kGroup, n < a.N);
-        }
-        if (++ahead_kb == kb_hi) {
-          ahead_kb = kb_lo;
-          ahead_tile += step;
-          if (ahead_tile < total) tile_of(ahead_tile, al, ac);
-        }
+      if (next_kb >= blocks && next_tile < total) {
+        int32_t l, c;
+        tile_of(next_tile, l, c);
+        next_tile += step;
+        next_kb = 0;
+        const int32_t m = (PAIR ? 2 * l + rank : l) * kLaneRows + (warp & 3) * 32 + lane, n = c * TN + col;
+        live_a = m < a.M;
+        live_w = n < a.N;
+        next_a = a.a_scale + min(m, a.M - 1);
+        next_w = a.w_scale + min(n, a.N - 1) / kGroup;
       }
+      const uint32_t to = scales_at + next_half * (kAhead * kSlot * 4);
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        if (next_kb + u >= blocks) break;
+        cp_async4(to + u * kSlot * 4, next_a, live_a);
+        cp_async4(to + u * kSlot * 4 + EW * 32 * 4, next_w, live_w);
+        next_a += a.ldas;
+        next_w += a.ldws;
+      }
+      next_kb += kAhead;
+      next_half ^= 1u;
       cp_async_commit();
-      ahead_slot = ahead_slot + 1 == P ? 0 : ahead_slot + 1;
     };
-#pragma unroll 1
-    for (int u = 0; u < P - 1; ++u) ask();
+    ask();
 
     bool ok = true;
-    int32_t n = 0, slot = 0;
+    int32_t n = 0;
+    uint32_t half = 0;
 #pragma unroll 1
     for (int32_t i = first; i < total && ok; i += step) {
       int32_t l, c;
       tile_of(i, l, c);
+      const int64_t row0 = (int64_t)(PAIR ? 2 * l + rank : l) * kLaneRows + (warp & 3) * 32;
+      const bool have_rows = row0 < a.M;
       float2 acc[CW / 2];
 #pragma unroll
       for (int e = 0; e < CW / 2; ++e) acc[e] = make_float2(0.f, 0.f);
 #pragma unroll 1
-      for (int32_t kb = kb_lo; kb < kb_hi; ++kb, ++n) {
-        if constexpr (SWAP) __syncwarp();  // (the slot asked for was read by every lane)
-        ask();
-        cp_async_wait<P - 1>();
-        if constexpr (SWAP) __syncwarp();
-        const int b = n % NB;
-        ok = wait_warp(&tfull[b], (n / NB) & 1, a.status);
+      for (int32_t kb = 0; kb < blocks; kb += U, ++n) {
+        if (kb % kAhead == 0) {
+          cp_async_wait<0>();
+          half = next_half ^ 1u;
+          ask();
+        }
+        const float* sc = scales + tid + (half * kAhead + kb % kAhead) * kSlot;
+        const int b = n & 1;
+        ok = wait_warp(&tfull[b], (n >> 1) & 1, a.status);
         if (!ok) break;
         tc_fence_after();
-        const uint32_t from = tmem + lane_off + b * TN + col;
-        if constexpr (SWAP) {
-          const float* sc = ring + (warp * P + slot) * (TN + 4);
-          const float2 ws = make_float2(sc[TN], sc[TN]), zero = make_float2(0.f, 0.f);
-#pragma unroll
-          for (int u = 0; u < TN; u += 16) {
-            float v[16];
-            tmem_ld16(from + u, v);
-#pragma unroll
-            for (int e = 0; e < 16; e += 4) {
-              const float4 s4 = *reinterpret_cast<const float4*>(sc + u + e);
-              float2& x = acc[(u + e) / 2];
-              float2& y = acc[(u + e) / 2 + 1];
-              x = ffma2(make_float2(v[e], v[e + 1]), ffma2(make_float2(s4.x, s4.y), ws, zero), x);
-              y = ffma2(make_float2(v[e + 2], v[e + 3]), ffma2(make_float2(s4.z, s4.w), ws, zero), y);
-            }
-          }
+        const uint32_t from = tmem + lane_off + b * U * TN + col;
+        auto done = [&]() {
           tc_fence_before();
           __syncwarp();
-          arrive_lane0(&tempty[b], lane);
-        } else {
-          const float* sc = ring + slot * 2 * EW * 32 + tid;
-          const float f = sc[0] * sc[EW * 32];
-          const float2 f2 = make_float2(f, f);
-#pragma unroll
-          for (int u = 0; u < CW; u += 32) {
-            float v[32];
-            tmem_ld32(from + u, v);
-            if (u + 32 == CW) {
-              tc_fence_before();
-              __syncwarp();
-              if constexpr (PAIR) {
-                if (lane == 0) arrive_peer(tempty0 + 8 * b);
-                __syncwarp();
-              } else {
-                arrive_lane0(&tempty[b], lane);
-              }
-            }
-#pragma unroll
-            for (int e = 0; e < 32; e += 2)
-              acc[(u + e) / 2] = ffma2(make_float2(v[e], v[e + 1]), f2, acc[(u + e) / 2]);
-          }
+          if constexpr (PAIR) arrive_peer_lane0(tempty0 + 8 * b, lane);
+          else arrive_lane0(&tempty[b], lane);
+        };
+        if (!have_rows) {
+          done();
+          continue;
         }
-        slot = slot + 1 == P ? 0 : slot + 1;
+        // A read of TMEM takes 200 cycles whatever its width (to 64 columns): the widest that the
+        // registers hold, and two warps on a scheduler.  (Of blocks behind the last, whatever the
+        // buffer holds: not added.)
+        constexpr int kPer = CW / CR;
+#pragma unroll
+        for (int q = 0; q < U * kPer; ++q) {
+          const int u = q / kPer, x = q % kPer * CR;
+          uint32_t w[CR];
+          tmem_ask(from + u * TN + x, w);
+          const float f = sc[u * kSlot] * sc[u * kSlot + EW * 32];
+          const float2 f2 = make_float2(f, f);
+          tmem_have(w);
+          if (q + 1 == U * kPer) done();
+          if (U > 1 && kb + u >= blocks) continue;
+#pragma unroll
+          for (int e = 0; e < CR; e += 2)
+            acc[(x + e) / 2] =
+                ffma2(make_float2(__uint_as_float(w[e]), __uint_as_float(w[e + 1])), f2, acc[(x + e) / 2]);
+        }
       }
       if (!ok) break;
-      // ---- the tile's way out
-      if constexpr (SWAP) {
-        if (L.splits > 1) {  // to the cluster's sums, below (one tile a CTA)
-          float* mine = reinterpret_cast<float*>(smem) + my_lane;
-#pragma unroll
-          for (int e = 0; e < TN / 2; ++e) {
-            mine[2 * e * kLaneRows] = acc[e].x;
-            mine[(2 * e + 1) * kLaneRows] = acc[e].y;
-          }
-        } else {
-          const int32_t nn = l * kLaneRows + my_lane;
-          if (nn < a.N) {
-#pragma unroll
-            for (int e = 0; e < TN; ++e) {
-              const int32_t m = c * TN + e;
-              if (m < a.M) store_one(a, m, nn, e & 1 ? acc[e / 2].y : acc[e / 2].x);
-            }
-          }
-        }
-      } else {
-        // a warp's 32 rows turned round in shared memory, 32 columns at a time: each store then
-        // covers whole sectors of four rows
+      // ---- the tile's way out: a warp's 32 rows turned round in shared memory, CH columns at a time
+      if (have_rows) {
         float* st = staging + warp * 32 * kPitch;
-        const int64_t row0 = (int64_t)(PAIR ? 2 * l + rank : l) * kLaneRows + (warp & 3) * 32;
-        const int32_t r8 = lane >> 3, c4 = (lane & 7) * 4;
-#pragma unroll
-        for (int u = 0; u < CW; u += 32) {
-          const int32_t n0 = c * TN + col + u + c4;
+        const int32_t rows = (int32_t)min((int64_t)32, a.M - row0);
+        // (one copy of the code for all pieces: cold, it takes longer to fetch than to run)
+#pragma unroll 1
+        for (int x = 0; x < CW && c * TN + col + x < a.N; x += CH) {
           __syncwarp();
 #pragma unroll
-          for (int e = 0; e < 32; e += 4)
-            *reinterpret_cast<float4*>(st + lane * kPitch + e) =
-                make_float4(acc[(u + e) / 2].x, acc[(u + e) / 2].y, acc[(u + e) / 2 + 1].x,
-                            acc[(u + e) / 2 + 1].y);
-          __syncwarp();
-#pragma unroll 4
-          for (int r = r8; r < 32; r += 4) {
-            if (row0 + r >= a.M) break;
-            const float4 x = *reinterpret_cast<const float4*>(st + r * kPitch + c4);
-            if (L.vec && n0 + 4 <= a.N) {
-              store_four(a, row0 + r, n0, x);
-            } else {
-              if (n0 < a.N) store_one(a, row0 + r, n0, x.x);
-              if (n0 + 1 < a.N) store_one(a, row0 + r, n0 + 1, x.y);
-              if (n0 + 2 < a.N) store_one(a, row0 + r, n0 + 2, x.z);
-              if (n0 + 3 < a.N) store_one(a, row0 + r, n0 + 3, x.w);
-            }
+          for (int y = 0; y < CW; y += CH) {
+            if (x != y) continue;
+#pragma unroll
+            for (int e = 0; e < CH; e += 4)
+              *reinterpret_cast<float4*>(st + lane * kPitch + e) =
+                  make_float4(acc[(y + e) / 2].x, acc[(y + e) / 2].y, acc[(y + e) / 2 + 1].x,
+                              acc[(y + e) / 2 + 1].y);
           }
+          __syncwarp();
+          write_rows<CH>(a, st, lane, row0, rows, c * TN + col + x, L.vec);
         }
       }
     }
@@ -413,30 +546,290 @@ scaled_matmul_kernel(const __grid_constant__ CUtensorMap tmL, const __grid_const
 
   // ---- teardown
   tc_fence_before();
-  if (cluster > 1) cluster_sync_all();
+  if constexpr (PAIR) cluster_sync_all();
   else __syncthreads();
-  if constexpr (SWAP) {
-    if (cluster > 1) {
-      // every CTA of the cluster adds up the rows of A that are its rank's, in the ranks' order
-      int32_t l, c;
-      tile_of(first, l, c);
-      const int32_t n = l * kLaneRows + tid, live = min(TN, a.M - c * TN);
-      if (tid < kLaneRows && n < a.N) {
-        const uint32_t at = smem_u32(smem) + tid * 4;
-        for (int32_t t = rank; t < live; t += cluster) {
-          float x = 0.f;
-#pragma unroll 8
-          for (int32_t r = 0; r < cluster; ++r) x += ld_peer(peer_addr(at + t * kLaneRows * 4, r));
-          store_one(a, c * TN + t, n, x);
-        }
-      }
-      cluster_sync_all();
-    }
-  }
   if (warp == EW + 1) {
     tc_fence_after();
-    if constexpr (PAIR) tmem_dealloc_pair(tmem, NB * TN);
-    else tmem_dealloc(tmem, NB * TN);
+    if constexpr (PAIR) tmem_dealloc_pair(tmem, H::kCols);
+    else tmem_dealloc(tmem, H::kCols);
+  }
+}
+
+// ------------------------------------------------------------------ few rows
+// Up to 64 rows of A as the TN columns of tiles whose lanes are 128 rows of W: the products then read
+// W from shared memory once (with A on the lanes, a tile of 64 rows of W reads 128 of A with it,
+// most of them empty: 16 x 65536 x 4096 56 us, here 43).  W's way in bounds it.  Where the tiles
+// alone would leave SMs idle, the blocks of a tile are cut over a cluster of up to eight CTAs, which
+// add their sums up through distributed shared memory in the order of their ranks.
+template <int TN, int U>
+struct Few {
+  static constexpr int kThreads = 6 * 32;             // epilogue 4, copies, products
+  static constexpr int kCols = 2 * U * TN < 32 ? 32 : 2 * U * TN;
+  static constexpr int kCBytes = TN * kGroup, kWBytes = kLaneRows * kGroup;
+  static constexpr int kStage = U * (kWBytes + kCBytes);
+  static constexpr int kSlot = TN + 4;                // scales of a block: A's, W's
+  static constexpr int kScales = 2 * kAhead * 4 * kSlot * 4;
+  static constexpr int kFixed = 1024 + kScales;
+  static constexpr int S = (112 * 1024 - kFixed) / kStage;
+  static constexpr int kSmem = kFixed + S * kStage;
+  static_assert(S >= 2 && S * kStage >= TN * kLaneRows * 4, "a CTA's sums fit where its stages were");
+};
+
+template <int TN, int U>
+__global__ void __launch_bounds__(Few<TN, U>::kThreads, 2)
+scaled_matmul_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmW,
+                         ScaledMatmulArgs a, int32_t tiles_w, int32_t total, int32_t splits) {
+  using H = Few<TN, U>;
+  constexpr int S = H::S;
+  extern __shared__ __align__(1024) unsigned char smem_raw[];
+  unsigned char* smem = reinterpret_cast<unsigned char*>(
+      (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  float* scales = reinterpret_cast<float*>(smem + S * H::kStage);
+  __shared__ uint64_t full[S], empty[S], tfull[2], tempty[2];
+  __shared__ uint32_t tmem_slot;
+  pdl_wait();
+
+  const int32_t tid = threadIdx.x, lane = tid & 31, warp = (int32_t)warp_uniform(tid >> 5);
+  const int32_t rank = splits > 1 ? (int32_t)(blockIdx.x % splits) : 0;
+  const int32_t first = blockIdx.x / splits, step = gridDim.x / splits;
+  const int32_t blocks = (a.K + kGroup - 1) / kGroup;
+  const int32_t kb_lo = (int32_t)((int64_t)blocks * rank / splits);
+  const int32_t kb_hi = (int32_t)((int64_t)blocks * (rank + 1) / splits);
+  if (warp == 4 && lane < 2) prefetch_tensormap(lane == 0 ? &tmA : &tmW);
+  if (tid == 128) {
+    for (int i = 0; i < S; ++i) {
+      mbar_init(&full[i], 1);
+      mbar_init(&empty[i], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&tfull[i], 1);
+      mbar_init(&tempty[i], 4);
+    }
+    fence_barrier_init();
+  }
+  __syncwarp();
+  uint32_t tmem = 0;
+  if (warp != 4) {  // (the copies begin without the others)
+    if (warp == 5) {
+      tmem_alloc(&tmem_slot, H::kCols);
+      tmem_relinquish();
+      tc_fence_before();
+    }
+    __syncthreads();
+    tc_fence_after();
+    tmem = tmem_slot;
+  }
+  // Tile i: rows (i % tiles_w) * 128 of W and (i / tiles_w) * TN of A.
+  if (warp == 4) {
+    // ------------------------------------------------------------- copies
+    const bool leader = elect_one();
+    const uint64_t once = policy_evict_first(), often = policy_evict_last();
+    bool ok = true, begun = false;
+    int32_t n = 0, s = 0;
+    uint32_t ph = 1;
+#pragma unroll 1
+    for (int32_t i = first; i < total && ok; i += step) {
+      const int32_t c = i / tiles_w, row = (i - c * tiles_w) * kLaneRows;
+#pragma unroll 1
+      for (int32_t kb = kb_lo; kb < kb_hi; kb += U, ++n) {
+        if (n == S) {
+          __syncthreads();
+          begun = true;
+        }
+        if (n >= S) ok = wait_warp(&empty[s], ph, a.status);
+        if (!ok) break;
+        if (leader) {
+          unsigned char* dst = smem + s * H::kStage;
+          const int32_t un = min(U, kb_hi - kb);
+          mbar_arrive_expect_tx(&full[s], un * (H::kWBytes + H::kCBytes));
+#pragma unroll
+          for (int u = 0; u < U; ++u) {
+            if (u >= un) break;
+            tma_load_2d(dst + u * H::kWBytes, &tmW, (kb + u) * kGroup, row, &full[s], once);
+            tma_load_2d(dst + U * H::kWBytes + u * H::kCBytes, &tmA, (kb + u) * kGroup, c * TN, &full[s],
+                        often);
+          }
+        }
+        __syncwarp();
+        if (++s == S) {
+          s = 0;
+          ph ^= 1u;
+        }
+      }
+    }
+    if (!begun) __syncthreads();
+    if (!ok)
+      for (int32_t u = max(0, n - S); u < n; ++u) drain(&full[u % S], (u / S) & 1);
+  } else if (warp == 5) {
+    // ----------------------------------------------------------- products
+    constexpr uint32_t kIdesc = idesc_e4m3(128, TN);
+    const uint32_t base = warp_uniform(smem_u32(smem)), tm = warp_uniform(tmem);
+    const bool leader = elect_one();
+    bool ok = true;
+    int32_t n = 0, s = 0;
+    uint32_t ph = 0;
+#pragma unroll 1
+    for (int32_t i = first; i < total && ok; i += step) {
+#pragma unroll 1
+      for (int32_t kb = kb_lo; kb < kb_hi; kb += U, ++n) {
+        const int b = n & 1;
+        if (n >= 2) ok = wait_warp(&tempty[b], ((n >> 1) - 1) & 1, a.status);
+        // (last: W is what these products wait for)
+        ok = ok && wait_warp(&full[s], ph, a.status);
+        if (!ok) break;
+        tc_fence_after();
+        const uint64_t dw = smem_desc(base + s * H::kStage, 16, 1024);
+        const uint64_t da = smem_desc(base + s * H::kStage + U * H::kWBytes, 16, 1024);
+        if (leader) {
+#pragma unroll
+          for (int k = 0; k < kGroup / 32; ++k) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+              if (U > 1 && kb + u >= kb_hi) break;
+              mma8_ss(tm + (b * U + u) * TN, smem_desc_at(dw, u * H::kWBytes + k * 32),
+                      smem_desc_at(da, u * H::kCBytes + k * 32), kIdesc, k > 0);
+            }
+          }
+          mma_commit(&empty[s]);
+          mma_commit(&tfull[b]);
+        }
+        __syncwarp();
+        if (++s == S) {
+          s = 0;
+          ph ^= 1u;
+        }
+      }
+    }
+    if (!ok && n > 0) drain(&tfull[(n - 1) & 1], ((n - 1) >> 1) & 1);
+  } else {
+    // ----------------------------------------------------------- epilogue
+    const uint32_t lane_off = (uint32_t)(warp * 32) << 16;
+    // Scales come by cp.async, kAhead blocks together and as many ahead, into slots that only this
+    // warp reads: [2][kAhead][warp][A's, W's].
+    const uint32_t scales_at = smem_u32(scales) + warp * H::kSlot * 4;
+    int32_t next_tile = first, next_kb = kb_hi;
+    uint32_t next_half = 0;
+    const float* next_a = nullptr;
+    const float* next_w = nullptr;
+    int32_t live = 0;
+    auto ask = [&]() {
+      if (next_kb >= kb_hi && next_tile < total) {
+        const int32_t c = next_tile / tiles_w;
+        next_w = a.w_scale + kb_lo * a.ldws + (next_tile - c * tiles_w);
+        next_a = a.a_scale + kb_lo * a.ldas + c * TN;
+        live = a.M - c * TN;
+        next_tile += step;
+        next_kb = kb_lo;
+      }
+      const uint32_t to = scales_at + next_half * (kAhead * 4 * H::kSlot * 4);
+#pragma unroll 1
+      for (int u = 0; u < kAhead && next_kb + u < kb_hi; ++u) {
+#pragma unroll
+        for (int t = 0; t < TN; t += 32)
+          if (t + lane < TN)
+            cp_async4(to + u * 4 * H::kSlot * 4 + (t + lane) * 4, next_a + min(t + lane, live - 1),
+                      t + lane < live);
+        if (lane == 0) cp_async4(to + u * 4 * H::kSlot * 4 + TN * 4, next_w, true);
+        next_a += a.ldas;
+        next_w += a.ldws;
+      }
+      next_kb += kAhead;
+      next_half ^= 1u;
+      cp_async_commit();
+    };
+    ask();
+    bool ok = true;
+    int32_t n = 0;
+    uint32_t half = 0;
+#pragma unroll 1
+    for (int32_t i = first; i < total && ok; i += step) {
+      float2 acc[TN / 2];
+#pragma unroll
+      for (int e = 0; e < TN / 2; ++e) acc[e] = make_float2(0.f, 0.f);
+#pragma unroll 1
+      for (int32_t kb = kb_lo; kb < kb_hi; kb += U, ++n) {
+        if ((kb - kb_lo) % kAhead == 0) {
+          cp_async_wait<0>();
+          __syncwarp();  // (every lane's, and every lane has read the other half)
+          half = next_half ^ 1u;
+          ask();
+        }
+        const float* sc = scales + ((half * kAhead + (kb - kb_lo) % kAhead) * 4 + warp) * H::kSlot;
+        const int b = n & 1;
+        ok = wait_warp(&tfull[b], (n >> 1) & 1, a.status);
+        if (!ok) break;
+        tc_fence_after();
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          uint32_t w[TN];
+          tmem_ask(tmem + lane_off + (b * U + u) * TN, w);
+          const float4* s4 = reinterpret_cast<const float4*>(sc + u * 4 * H::kSlot);
+          const float2 ws = make_float2(sc[u * 4 * H::kSlot + TN], sc[u * 4 * H::kSlot + TN]);
+          tmem_have(w);
+          if (u + 1 == U) {
+            tc_fence_before();
+            __syncwarp();
+            arrive_lane0(&tempty[b], lane);
+          }
+          if (U > 1 && kb + u >= kb_hi) continue;
+#pragma unroll
+          for (int e = 0; e < TN; e += 4) {
+            const float4 x = s4[e / 4];
+            const float2 zero = make_float2(0.f, 0.f);
+            const float2 lo = make_float2(__uint_as_float(w[e]), __uint_as_float(w[e + 1]));
+            const float2 hi = make_float2(__uint_as_float(w[e + 2]), __uint_as_float(w[e + 3]));
+            acc[e / 2] = ffma2(lo, ffma2(make_float2(x.x, x.y), ws, zero), acc[e / 2]);
+            acc[e / 2 + 1] = ffma2(hi, ffma2(make_float2(x.z, x.w), ws, zero), acc[e / 2 + 1]);
+          }
+        }
+      }
+      if (!ok) break;
+      if (splits > 1) {  // to the cluster's sums, below (one tile a CTA)
+        float* mine = reinterpret_cast<float*>(smem) + tid;
+#pragma unroll
+        for (int e = 0; e < TN / 2; ++e) {
+          mine[2 * e * kLaneRows] = acc[e].x;
+          mine[(2 * e + 1) * kLaneRows] = acc[e].y;
+        }
+      } else {
+        const int32_t c = i / tiles_w, nn = (i - c * tiles_w) * kLaneRows + tid;
+        if (nn < a.N) {
+#pragma unroll
+          for (int e = 0; e < TN; ++e)
+            if (c * TN + e < a.M) store_one(a, c * TN + e, nn, e & 1 ? acc[e / 2].y : acc[e / 2].x);
+        }
+      }
+    }
+    cp_async_wait<0>();
+  }
+
+  // ---- teardown
+  tc_fence_before();
+  if (splits > 1) {
+    cluster_sync_all();
+    // every CTA of the cluster adds up the rows of A that are its rank's
+    const int32_t c = first / tiles_w, n = (first - c * tiles_w) * kLaneRows + tid;
+    const int32_t live = min(TN, a.M - c * TN);
+    if (tid < kLaneRows && n < a.N) {
+      const uint32_t at = smem_u32(smem) + tid * 4;
+      for (int32_t t = rank; t < live; t += splits) {
+        float v[kMaxSplits];
+#pragma unroll
+        for (int32_t r = 0; r < kMaxSplits; ++r)
+          v[r] = r < splits ? ld_peer(peer_addr(at + t * kLaneRows * 4, r)) : 0.f;
+        float x = 0.f;
+#pragma unroll
+        for (int32_t r = 0; r < kMaxSplits; ++r) x += v[r];
+        store_one(a, c * TN + t, n, x);
+      }
+    }
+    cluster_sync_all();
+  } else {
+    __syncthreads();
+  }
+  if (warp == 5) {
+    tc_fence_after();
+    tmem_dealloc(tmem, H::kCols);
   }
 }
 
@@ -453,59 +846,73 @@ bool rows_map(CUtensorMap* map, const void* base, int32_t K, int64_t rows, int64
 
 int32_t ceil_div(int64_t a, int64_t b) { return (int32_t)((a + b - 1) / b); }
 
-template <bool SWAP, bool PAIR, int TN>
+template <bool PAIR, int TN, int U>
 cudaError_t launch(const ScaledMatmulArgs& a, cudaStream_t stream) {
-  using H = Shape<SWAP, PAIR, TN>;
-  CUtensorMap tl, tc;
-  const bool maps =
-      SWAP ? rows_map(&tl, a.w, a.K, a.N, a.ldw, kLaneRows) && rows_map(&tc, a.a, a.K, a.M, a.lda, H::kCRows)
-           : rows_map(&tl, a.a, a.K, a.M, a.lda, kLaneRows) && rows_map(&tc, a.w, a.K, a.N, a.ldw, H::kCRows);
-  if (!maps) return cudaErrorInvalidValue;
-  auto kernel = scaled_matmul_kernel<SWAP, PAIR, TN>;
+  using H = Shape<PAIR, TN, U>;
+  Launch L{};
+  L.tiles_l = ceil_div(a.M, PAIR ? 2 * kLaneRows : kLaneRows);
+  L.tiles_c = ceil_div(a.N, TN);
+  CUtensorMap ta, tw;
+  if (!rows_map(&ta, a.a, a.K, a.M, a.lda, kLaneRows) || !rows_map(&tw, a.w, a.K, a.N, a.ldw, H::kCRows))
+    return cudaErrorInvalidValue;
+  auto kernel = scaled_matmul_kernel<PAIR, TN, U>;
   const cudaError_t e = allow_smem(kernel, H::kSmem);
   if (e != cudaSuccess) return e;
-  Launch L{};
-  L.tiles_l = ceil_div(SWAP ? a.N : a.M, PAIR ? 2 * kLaneRows : kLaneRows);
-  L.tiles_c = ceil_div(SWAP ? a.M : a.N, TN);
-  L.splits = 1;
-  const int64_t tiles = (int64_t)L.tiles_l * L.tiles_c;
-  const int64_t places = (int64_t)H::kCtas * device_sm_count();
-  if (SWAP) {
-    const int64_t blocks = ceil_div(a.K, kGroup);
-    L.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>({8, places / tiles, blocks / 2}));
-  }
-  auto even = [](const void* p, int64_t ld, uintptr_t bytes) {
-    return ld % 4 == 0 && (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0;
+  auto even = [&](const void* p, int64_t ld, uintptr_t bytes) {
+    return ld % (a.c_bf16 ? 8 : 4) == 0 && (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0;
   };
-  L.vec = even(a.c, a.ldc, a.c_bf16 ? 8 : 16) && (a.add == nullptr || even(a.add, a.ldadd, 8));
-  if (PAIR) {
-    const int64_t pairs = std::min<int64_t>(tiles, places / 2);
-    return launch_clusters(kernel, dim3((unsigned)(2 * pairs)), dim3(H::kThreads), H::kSmem, stream, true,
-                           2, tl, tc, a, L);
-  }
-  if (L.splits > 1)
-    return launch_clusters(kernel, dim3((unsigned)(tiles * L.splits)), dim3(H::kThreads), H::kSmem, stream,
-                           true, L.splits, tl, tc, a, L);
-  return launch_kernel(kernel, dim3((unsigned)std::min<int64_t>(tiles, places)), dim3(H::kThreads), H::kSmem,
-                       stream, true, tl, tc, a, L);
+  L.vec = even(a.c, a.ldc, 16) && (a.add == nullptr || even(a.add, a.ldadd, a.c_bf16 ? 16 : 8));
+  const int64_t tiles = (int64_t)L.tiles_l * L.tiles_c, sms = device_sm_count();
+  if (PAIR)
+    return launch_clusters(kernel, dim3((unsigned)(2 * std::min(tiles, sms / 2))), dim3(H::kThreads), H::kSmem,
+                           stream, true, 2, ta, tw, a, L);
+  return launch_kernel(kernel, dim3((unsigned)std::min(tiles, sms)), dim3(H::kThreads), H::kSmem, stream, true,
+                       ta, tw, a, L);
+}
+
+// CTAs that a tile's blocks are cut over: a power of two (clusters of six leave places of a GPC
+// empty: 48 tiles of 32 blocks 11.9 us, four CTAs each 8.7, two 8.9, one 11.1), and all at work at
+// once (32 tiles of 96 blocks: eight 12.0, four 12.3, one 27.0; 48 of 32: eight 11.0).
+int32_t few_splits(int32_t tiles, int32_t blocks, int32_t sms) {
+  int32_t n = 1;
+  while (n < kMaxSplits && (int64_t)tiles * n * 2 <= sms * 7 / 4 && blocks >= n * 4) n *= 2;
+  return n;
+}
+
+template <int TN, int U>
+cudaError_t launch_few(const ScaledMatmulArgs& a, cudaStream_t stream) {
+  using H = Few<TN, U>;
+  CUtensorMap ta, tw;
+  if (!rows_map(&ta, a.a, a.K, a.M, a.lda, TN) || !rows_map(&tw, a.w, a.K, a.N, a.ldw, kLaneRows))
+    return cudaErrorInvalidValue;
+  auto kernel = scaled_matmul_few_kernel<TN, U>;
+  const cudaError_t e = allow_smem(kernel, H::kSmem);
+  if (e != cudaSuccess) return e;
+  const int32_t tiles_w = ceil_div(a.N, kLaneRows), total = tiles_w * ceil_div(a.M, TN);
+  const int32_t blocks = ceil_div(a.K, kGroup), sms = device_sm_count();
+  const int32_t splits = few_splits(total, blocks, sms);
+  if (splits > 1)
+    return launch_clusters(kernel, dim3((unsigned)(total * splits)), dim3(H::kThreads), H::kSmem, stream, true,
+                           splits, ta, tw, a, tiles_w, total, splits);
+  return launch_kernel(kernel, dim3((unsigned)std::min(total, 2 * sms)), dim3(H::kThreads), H::kSmem, stream,
+                       true, ta, tw, a, tiles_w, total, splits);
 }
 
 }  // namespace
 
 cudaError_t launch_scaled_matmul(const ScaledMatmulArgs& a, cudaStream_t stream) {
-  if (a.M <= 16) return launch<true, false, 16>(a, stream);
-  if (a.M <= 32) return launch<true, false, 32>(a, stream);
-  if (a.M <= 64) return launch<true, false, 64>(a, stream);
+  if (a.M <= 16) return launch_few<16, 2>(a, stream);
+  if (a.M <= 32) return launch_few<32, 2>(a, stream);
+  if (a.M <= 64) return launch_few<64, 2>(a, stream);
   // cycles of a wave of tiles, about: what a block takes and a tile's way in and out
   const int64_t blocks = ceil_div(a.K, kGroup), sms = device_sm_count();
   auto cost = [&](int32_t rows, int32_t cols, int64_t places, int64_t block, int64_t rest) {
     const int64_t tiles = (int64_t)ceil_div(a.M, rows) * ceil_div(a.N, cols);
     return ceil_div(tiles, places) * (blocks * block + rest);
   };
-  const int64_t pair = cost(256, 256, sms / 2, 530, 3000), wide = cost(128, 128, sms, 290, 2000);
-  const int64_t narrow = std::min(cost(128, 64, 2 * sms, 300, 2000), cost(128, 64, sms, 170, 1500));
-  if (pair <= wide && pair <= narrow) return launch<false, true, 256>(a, stream);
-  return wide <= narrow ? launch<false, false, 128>(a, stream) : launch<false, false, 64>(a, stream);
+  if (cost(256, 256, sms / 2, 900, 6000) < cost(128, 128, sms, 550, 5000))
+    return launch<true, 256, 1>(a, stream);
+  return launch<false, 128, 2>(a, stream);
 }
 
 }  // namespace ssd

@@ -523,6 +523,45 @@ scaled_matmul_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
       if (have_rows) {
         float* st = staging + warp * 32 * kPitch;
         const int32_t rows = (int32_t)min((int64_t)32, a.M - row0);
+        if (L.vec && a.c_bf16 && a.add == nullptr) {
+          // rounded first: half of what shared memory carries (as float32 a tile took 9300 cycles)
+          unsigned char* st8 = reinterpret_cast<unsigned char*>(st);
+          constexpr int kBytes = 144;  // of a staged row of 64
+          const int32_t r0 = lane >> 3, c8 = (lane & 7) * 8;
+#pragma unroll 1
+          for (int x = 0; x < CW && c * TN + col + x < a.N; x += 64) {
+            __syncwarp();
+#pragma unroll
+            for (int y = 0; y < CW; y += 64) {
+              if (x != y) continue;
+#pragma unroll
+              for (int e = 0; e < 32; e += 4) {
+                const float2* v = acc + y / 2 + e;
+                *reinterpret_cast<uint4*>(st8 + lane * kBytes + e * 4) =
+                    make_uint4(pack_bf16x2(v[0].x, v[0].y), pack_bf16x2(v[1].x, v[1].y),
+                               pack_bf16x2(v[2].x, v[2].y), pack_bf16x2(v[3].x, v[3].y));
+              }
+            }
+            __syncwarp();
+            const int32_t n = c * TN + col + x + c8;
+            __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.c) + (row0 + r0) * a.ldc + n;
+            const unsigned char* from = st8 + r0 * kBytes + c8 * 2;
+            if (n + 8 <= a.N) {
+#pragma unroll
+              for (int j = 0; j < 8; ++j) {
+                const uint4 v = *reinterpret_cast<const uint4*>(from + j * 4 * kBytes);
+                if (r0 + j * 4 < rows) *reinterpret_cast<uint4*>(out) = v;
+                out += 4 * a.ldc;
+              }
+            } else {
+#pragma unroll 1
+              for (int32_t r = r0; r < rows; r += 4, out += 4 * a.ldc, from += 4 * kBytes)
+                for (int32_t e = 0; n + e < a.N; ++e)
+                  out[e] = reinterpret_cast<const __nv_bfloat16*>(from)[e];
+            }
+          }
+          continue;
+        }
         // (one copy of the code for all pieces: cold, it takes longer to fetch than to run)
 #pragma unroll 1
         for (int x = 0; x < CW && c * TN + col + x < a.N; x += CH) {

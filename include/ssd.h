@@ -678,6 +678,34 @@ ssd_status ssd_cache_attention(const ssd_grid* grid, const ssd_block_cache* cach
                                float scale, void* o, float* lse, void* workspace,
                                size_t workspace_bytes, int32_t* status, ssd_stream_t stream);
 
+/* ssd_cache_attention() for sequences that share the first blocks of a long
+ * prompt: group g holds the sequences group_start[g] <= b < group_start[g + 1],
+ * whose first shared[g] blocks are the same (their tables' first shared[g]
+ * entries are equal; shared[g] may be 0).  The same o and lse, but for the order
+ * of sums; the shared keys are read once for the rows of a group instead of once
+ * a sequence.  Shared blocks hold committed tokens: shared[g] * block <=
+ * cache_len[b] for every sequence of the group that has drafts.
+ *   group_start  dev int32 [groups + 1]: 0 ... B, ascending; shared dev int32
+ *                [groups], at most max_shared (host, at most max_blocks)
+ *   workspace    >= ssd_cache_attention_shared_workspace(..., max_blocks *
+ *                block, max_shared * block) bytes; else as there
+ * Where sharing would not pay (small work, few sequences to a group) each
+ * sequence is worked on by itself, and group_start and shared are not read.
+ * Device errors beside those of ssd_cache_attention(): groups or shared out of
+ * range, more shared tokens than cache_len (DEVICE_BOUNDS; rows of the
+ * sequences concerned untouched, or, where group_start does not ascend, of no
+ * certain value). */
+size_t ssd_cache_attention_shared_workspace(int32_t B, int32_t groups, int32_t Hq, int32_t Hkv, int32_t d,
+                                            int32_t D_max, int32_t L_max, int32_t max_shared);
+ssd_status ssd_cache_attention_shared(const ssd_grid* grid, const ssd_block_cache* cache, int32_t B,
+                                      int32_t groups, const int32_t* group_start, const int32_t* shared,
+                                      int32_t max_shared, int32_t Hq, const int32_t* cache_len,
+                                      const int32_t* n_drafts, const int32_t* draft_pos,
+                                      const int32_t* key_start, int32_t D_max, const int32_t* block_table,
+                                      int32_t max_blocks, const void* q, float scale, void* o, float* lse,
+                                      void* workspace, size_t workspace_bytes, int32_t* status,
+                                      ssd_stream_t stream);
+
 /* ---------------------------------------------------------------------------
  * Sampling with temperature, top-k, top-p and min-p from given uniforms (the
  * paper samples at temperature 1; visual-token models are served with top-k

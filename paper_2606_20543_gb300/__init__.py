@@ -32,7 +32,8 @@ EXPORTED = ["ssd_abi_version", "ssd_status_string", "ssd_set_wait_limit",
             "ssd_verify_step_workspace", "ssd_verify_step_launches", "ssd_verify_step",
             "ssd_verify_accept",
             "ssd_cache_plan", "ssd_rotary_table", "ssd_cache_append", "ssd_cache_append_norm",
-            "ssd_cache_attention_workspace", "ssd_cache_attention", "ssd_sample",
+            "ssd_cache_attention_workspace", "ssd_cache_attention",
+            "ssd_cache_attention_shared_workspace", "ssd_cache_attention_shared", "ssd_sample",
             "ssd_quantize", "ssd_scaled_matmul"]
 
 
@@ -173,6 +174,10 @@ def load(path: Optional[str] = None) -> ctypes.CDLL:
         "ssd_cache_attention_workspace": (SZ, [I32, I32, I32, I32, I32, I32]),
         "ssd_cache_attention": (I32, [ctypes.POINTER(Grid), ctypes.POINTER(BlockCache), I32, I32, P,
                                       P, P, P, I32, P, I32, P, F, P, P, P, SZ, P, P]),
+        "ssd_cache_attention_shared_workspace": (SZ, [I32, I32, I32, I32, I32, I32, I32, I32]),
+        "ssd_cache_attention_shared": (I32, [ctypes.POINTER(Grid), ctypes.POINTER(BlockCache), I32, I32,
+                                             P, P, I32, I32, P, P, P, P, I32, P, I32, P, F, P, P, P, SZ,
+                                             P, P]),
         "ssd_sample": (I32, [I32, I32, P, I32, I64, ctypes.POINTER(Sampling), ctypes.POINTER(Rng),
                              P, P, P, P, P]),
         "ssd_quantize": (I32, [I32, I32, I32, P, I32, I64, P, I64, P, I64, P]),
@@ -493,6 +498,22 @@ def ssd_cache_attention(g: Grid, c: BlockCache, B, Hq, cache_len, n_drafts, draf
         ctypes.byref(g), ctypes.byref(c), B, Hq, _ptr(cache_len), _ptr(n_drafts), _ptr(draft_pos),
         _ptr(key_start), D_max, _ptr(block_table), max_blocks, _ptr(q), scale, _ptr(o), _ptr(lse),
         _ptr(workspace), workspace_bytes, _ptr(status), _stream(stream)))
+
+
+def ssd_cache_attention_shared_workspace(B, groups, Hq, Hkv, d, D_max, L_max, max_shared) -> int:
+    return load().ssd_cache_attention_shared_workspace(B, groups, Hq, Hkv, d, D_max, L_max, max_shared)
+
+
+def ssd_cache_attention_shared(g: Grid, c: BlockCache, B, groups, group_start, shared, max_shared, Hq,
+                               cache_len, n_drafts, draft_pos, key_start, D_max, block_table,
+                               max_blocks, q, scale, o, lse, workspace, workspace_bytes, status,
+                               stream=None) -> None:
+    """ssd_cache_attention() of sequences whose groups share their first blocks."""
+    _check("ssd_cache_attention_shared", load().ssd_cache_attention_shared(
+        ctypes.byref(g), ctypes.byref(c), B, groups, _ptr(group_start), _ptr(shared), max_shared, Hq,
+        _ptr(cache_len), _ptr(n_drafts), _ptr(draft_pos), _ptr(key_start), D_max, _ptr(block_table),
+        max_blocks, _ptr(q), scale, _ptr(o), _ptr(lse), _ptr(workspace), workspace_bytes, _ptr(status),
+        _stream(stream)))
 
 
 def _is_bf16(t, what: str) -> int:

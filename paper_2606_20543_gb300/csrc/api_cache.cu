@@ -99,6 +99,61 @@ ssd_status append(const ssd_block_cache* cache, const ssd_rotary* rotary, const 
   return from_cuda(launch_cache_append(a, (cudaStream_t)stream));
 }
 
+// (groups 0: none)
+ssd_status attention(const ssd_grid* grid, const ssd_block_cache* cache, int32_t B, int32_t groups,
+                     const int32_t* group_start, const int32_t* shared, int32_t max_shared, int32_t Hq,
+                     const int32_t* cache_len, const int32_t* n_drafts, const int32_t* draft_pos,
+                     const int32_t* key_start, int32_t D_max, const int32_t* block_table,
+                     int32_t max_blocks, const void* q, float scale, void* o, float* lse,
+                     void* workspace, size_t workspace_bytes, int32_t* status, ssd_stream_t stream) {
+  ssd_status s = check_grid(grid);
+  if (s != SSD_OK) return s;
+  s = check_cache(cache);
+  if (s != SSD_OK) return s;
+  if (B < 0 || Hq <= 0 || D_max <= 0 || max_blocks <= 0) return SSD_ERR_SHAPE;
+  if (Hq % cache->Hkv != 0) return SSD_ERR_SHAPE;
+  if (max_blocks > INT32_MAX / 2 / cache->block) return SSD_ERR_UNSUPPORTED;
+  if ((int64_t)B * cache->Hkv > 65535) return SSD_ERR_UNSUPPORTED;
+  if ((int64_t)D_max * (Hq / cache->Hkv) > 65535 * 16) return SSD_ERR_UNSUPPORTED;
+  if ((int64_t)B * D_max * Hq > INT32_MAX / 2) return SSD_ERR_UNSUPPORTED;
+  if (B == 0) return SSD_OK;
+  for (const void* p : {(const void*)cache_len, (const void*)n_drafts, (const void*)block_table, q,
+                        (const void*)o, (const void*)status})
+    if (p == nullptr) return SSD_ERR_INVALID_ARG;
+  if (!aligned(q, 16) || !aligned(o, 16)) return SSD_ERR_INVALID_ARG;
+  if (!(scale >= 0.f) || !isfinite(scale)) return SSD_ERR_INVALID_ARG;
+  const int32_t L_max = max_blocks * cache->block;
+  const size_t need =
+      groups > 0 ? cache_attention_shared_workspace(B, groups, Hq, cache->Hkv, cache->d, D_max, L_max,
+                                                    max_shared * cache->block)
+                 : cache_attention_workspace(B, Hq, cache->Hkv, cache->d, D_max, L_max);
+  if (need > 0 && (workspace == nullptr || workspace_bytes < need)) return SSD_ERR_WORKSPACE;
+  if (need > 0 && !aligned(workspace, 16)) return SSD_ERR_INVALID_ARG;
+  CacheAttnArgs a{};
+  a.grid = *grid;
+  a.cache = *cache;
+  a.B = B;
+  a.Hq = Hq;
+  a.D_max = D_max;
+  a.max_blocks = max_blocks;
+  a.cache_len = cache_len;
+  a.n_drafts = n_drafts;
+  a.draft_pos = draft_pos;
+  a.key_start = key_start;
+  a.block_table = block_table;
+  a.q = q;
+  a.scale = scale;
+  a.o = o;
+  a.lse = lse;
+  a.status = status;
+  a.groups = groups;
+  a.max_shared = max_shared;
+  a.group_start = group_start;
+  a.shared = shared;
+  return from_cuda(groups > 0 ? launch_cache_attention_shared(a, workspace, (cudaStream_t)stream)
+                              : launch_cache_attention(a, workspace, (cudaStream_t)stream));
+}
+
 }  // namespace
 
 extern "C" {
@@ -188,44 +243,32 @@ ssd_status ssd_cache_attention(const ssd_grid* grid, const ssd_block_cache* cach
                                const int32_t* block_table, int32_t max_blocks, const void* q,
                                float scale, void* o, float* lse, void* workspace,
                                size_t workspace_bytes, int32_t* status, ssd_stream_t stream) {
-  ssd_status s = check_grid(grid);
-  if (s != SSD_OK) return s;
-  s = check_cache(cache);
-  if (s != SSD_OK) return s;
-  if (B < 0 || Hq <= 0 || D_max <= 0 || max_blocks <= 0) return SSD_ERR_SHAPE;
-  if (Hq % cache->Hkv != 0) return SSD_ERR_SHAPE;
-  if (max_blocks > INT32_MAX / 2 / cache->block) return SSD_ERR_UNSUPPORTED;
-  if ((int64_t)B * cache->Hkv > 65535) return SSD_ERR_UNSUPPORTED;
-  if ((int64_t)D_max * (Hq / cache->Hkv) > 65535 * 16) return SSD_ERR_UNSUPPORTED;
-  if ((int64_t)B * D_max * Hq > INT32_MAX / 2) return SSD_ERR_UNSUPPORTED;
-  if (B == 0) return SSD_OK;
-  for (const void* p : {(const void*)cache_len, (const void*)n_drafts, (const void*)block_table, q,
-                        (const void*)o, (const void*)status})
-    if (p == nullptr) return SSD_ERR_INVALID_ARG;
-  if (!aligned(q, 16) || !aligned(o, 16)) return SSD_ERR_INVALID_ARG;
-  if (!(scale >= 0.f) || !isfinite(scale)) return SSD_ERR_INVALID_ARG;
-  const size_t need = cache_attention_workspace(B, Hq, cache->Hkv, cache->d, D_max,
-                                                max_blocks * cache->block);
-  if (need > 0 && (workspace == nullptr || workspace_bytes < need)) return SSD_ERR_WORKSPACE;
-  if (need > 0 && !aligned(workspace, 16)) return SSD_ERR_INVALID_ARG;
-  CacheAttnArgs a{};
-  a.grid = *grid;
-  a.cache = *cache;
-  a.B = B;
-  a.Hq = Hq;
-  a.D_max = D_max;
-  a.max_blocks = max_blocks;
-  a.cache_len = cache_len;
-  a.n_drafts = n_drafts;
-  a.draft_pos = draft_pos;
-  a.key_start = key_start;
-  a.block_table = block_table;
-  a.q = q;
-  a.scale = scale;
-  a.o = o;
-  a.lse = lse;
-  a.status = status;
-  return from_cuda(launch_cache_attention(a, workspace, (cudaStream_t)stream));
+  return attention(grid, cache, B, 0, nullptr, nullptr, 0, Hq, cache_len, n_drafts, draft_pos, key_start,
+                   D_max, block_table, max_blocks, q, scale, o, lse, workspace, workspace_bytes, status,
+                   stream);
+}
+
+size_t ssd_cache_attention_shared_workspace(int32_t B, int32_t groups, int32_t Hq, int32_t Hkv, int32_t d,
+                                            int32_t D_max, int32_t L_max, int32_t max_shared) {
+  if (groups <= 0 || max_shared < 0 || max_shared > L_max) return 0;
+  if (B <= 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv != 0 || d <= 0 || D_max <= 0 || L_max <= 0) return 0;
+  return cache_attention_shared_workspace(B, groups, Hq, Hkv, d, D_max, L_max, max_shared);
+}
+
+ssd_status ssd_cache_attention_shared(const ssd_grid* grid, const ssd_block_cache* cache, int32_t B,
+                                      int32_t groups, const int32_t* group_start, const int32_t* shared,
+                                      int32_t max_shared, int32_t Hq, const int32_t* cache_len,
+                                      const int32_t* n_drafts, const int32_t* draft_pos,
+                                      const int32_t* key_start, int32_t D_max, const int32_t* block_table,
+                                      int32_t max_blocks, const void* q, float scale, void* o, float* lse,
+                                      void* workspace, size_t workspace_bytes, int32_t* status,
+                                      ssd_stream_t stream) {
+  if (groups <= 0 || max_shared < 0 || max_shared > max_blocks) return SSD_ERR_SHAPE;
+  if (groups > 65535) return SSD_ERR_UNSUPPORTED;
+  if (B > 0 && (group_start == nullptr || shared == nullptr)) return SSD_ERR_INVALID_ARG;
+  return attention(grid, cache, B, groups, group_start, shared, max_shared, Hq, cache_len, n_drafts,
+                   draft_pos, key_start, D_max, block_table, max_blocks, q, scale, o, lse, workspace,
+                   workspace_bytes, status, stream);
 }
 
 ssd_status ssd_sample(int32_t rows, int32_t V, const void* logits, int32_t logits_bf16, int64_t ld,

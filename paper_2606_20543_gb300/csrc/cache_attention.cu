@@ -48,16 +48,9 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kMostP = 256.f;     // a probability beyond it moves its reference
 constexpr float kUnseen = -3.402823466e38f;  // reference of a row that has seen no key
 
-struct Plan {
-  int32_t rows, row_groups;  // rows of a CTA, CTAs with other rows of the same keys
-  int32_t warps;             // of a CTA
-  int32_t per_head, goal, uniform;
-  bool cut(int32_t B) const { return per_head > B; }
-};
-
 // (Of at most 16 rows, or little work.)
-Plan make_plan(int32_t B, int32_t Hq, int32_t Hkv, int32_t D_max, int32_t L_max) {
-  Plan p;
+CacheMmaPlan make_plan(int32_t B, int32_t Hq, int32_t Hkv, int32_t D_max, int32_t L_max) {
+  CacheMmaPlan p;
   const int64_t rows = (int64_t)D_max * (Hq / Hkv);
   const int64_t sms = device_sm_count();
   const bool few = cache_attention_few(B, Hkv, rows, L_max);
@@ -117,7 +110,9 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
 }
 
 // NR: groups of 8 query rows of a warp; W: warps.
-template <int D, int NR, int W>
+// kShared: a sequence's keys begin behind those that it shares with its group, and its rows always
+// go to the part rows.
+template <int D, int NR, int W, bool kShared>
 __global__ void __launch_bounds__(W * 32, W == kWarps ? kCtas : 1)
 cache_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
                   CacheAttnArgs a, CacheAttnLaunch L) {
@@ -148,7 +143,7 @@ cache_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
     fence_barrier_init();
   }
   uint32_t stage = 0, phase = 0;  // of the warp's next step
-  CacheWork work;
+  CacheWork<kShared> work;
   bool more = work.first(a, L, blockIdx.x, first_of && tid < 32);
 #pragma unroll 1
   for (; more; more = work.next(a)) {
@@ -164,8 +159,9 @@ cache_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
       if (work.t_hi == work.tiles) L.info[b].y = blockIdx.x;
     }
     if (row0 >= rows_total) continue;
-    const bool whole = work.t_lo == 0 && work.t_hi == work.tiles, begins = work.t_lo == 0;
-    const int32_t k_lo = work.t_lo * kCacheTile, k_hi = min(Lk, work.t_hi * kCacheTile);
+    const bool whole = !kShared && work.t_lo == 0 && work.t_hi == work.tiles, begins = work.t_lo == 0;
+    const int32_t base = kShared ? cache_base(a, b, cache) : 0;
+    const int32_t k_lo = base + work.t_lo * kCacheTile, k_hi = min(Lk, base + work.t_hi * kCacheTile);
     const int32_t start = a.key_start != nullptr ? min(Lk, max(0, a.key_start[b])) : 0;
 
     // ---- this warp's rows and its share of the steps, and the copies of the first ones
@@ -615,8 +611,8 @@ bool step_map(CUtensorMap* map, const void* base, const ssd_block_cache& c) {
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int D, int NR, int W = kWarps>
-cudaError_t launch_mma(const CacheAttnArgs& a, const Plan& p, const CacheAttnLaunch& L,
+template <int D, int NR, int W, bool kShared>
+cudaError_t launch_mma(const CacheAttnArgs& a, const CacheMmaPlan& p, const CacheAttnLaunch& L,
                        cudaStream_t stream) {
   CUtensorMap tk, tv;
   if (!step_map(&tk, a.cache.k, a.cache) || !step_map(&tv, a.cache.v, a.cache))
@@ -625,9 +621,9 @@ cudaError_t launch_mma(const CacheAttnArgs& a, const Plan& p, const CacheAttnLau
     return 1024 + (size_t)W * kStages * 2 * kStep * D + (size_t)blocks * 12;
   };
   const cudaError_t e =
-      allow_smem(cache_attn_kernel<D, NR, W>, smem(part_blocks(kWorkRoom, kLeastBlock)));
+      allow_smem(cache_attn_kernel<D, NR, W, kShared>, smem(part_blocks(kWorkRoom, kLeastBlock)));
   if (e != cudaSuccess) return e;
-  return launch_kernel(cache_attn_kernel<D, NR, W>, dim3(p.per_head, a.cache.Hkv, p.row_groups),
+  return launch_kernel(cache_attn_kernel<D, NR, W, kShared>, dim3(p.per_head, a.cache.Hkv, p.row_groups),
                        dim3(W * 32), smem(L.max_blocks), stream, true, tk, tv, a, L);
 }
 
@@ -638,11 +634,39 @@ size_t part_bytes(int64_t rows, int32_t d) {
 int64_t tc_part_rows(int32_t B, int32_t Hq, int32_t D_max, int32_t splits) {
   return splits == 1 ? 0 : (int64_t)B * D_max * Hq * splits;
 }
-int64_t mma_part_rows(int32_t B, int32_t Hkv, const Plan& p) {
-  return p.cut(B) ? (int64_t)Hkv * p.row_groups * (p.per_head + B) * p.rows : 0;
+template <int D, bool kShared>
+cudaError_t launch_mma_of(const CacheAttnArgs& a, const CacheMmaPlan& p, const CacheAttnLaunch& L,
+                          cudaStream_t stream) {
+  return p.rows > 8             ? launch_mma<D, 2, kWarps, kShared>(a, p, L, stream)
+         : p.warps == kWarps ? launch_mma<D, 1, kWarps, kShared>(a, p, L, stream)
+                             : launch_mma<D, 1, kManyWarps, kShared>(a, p, L, stream);
 }
 
 }  // namespace
+
+CacheMmaPlan cache_attention_mma_plan(int32_t B, int32_t Hq, int32_t Hkv, int32_t D_max, int32_t L_max) {
+  return make_plan(B, Hq, Hkv, D_max, L_max);
+}
+int64_t cache_attention_mma_rows(int32_t B, int32_t Hkv, const CacheMmaPlan& p, bool all) {
+  return all || p.cut(B) ? (int64_t)Hkv * p.row_groups * (p.per_head + B) * p.rows : 0;
+}
+void cache_attention_mma_fill(CacheAttnLaunch& L, const CacheMmaPlan& p, int32_t L_max, int32_t block) {
+  L.min_tiles = kMinTiles;
+  L.per_head = p.per_head;
+  L.goal = p.goal;
+  L.uniform = p.uniform;
+  L.row_groups = p.row_groups;
+  L.group_rows = p.rows;
+  L.max_blocks = part_blocks(std::min((L_max + kCacheTile - 1) / kCacheTile, kWorkRoom), block);
+}
+cudaError_t launch_cache_attention_mma(const CacheAttnArgs& a, const CacheMmaPlan& p,
+                                       const CacheAttnLaunch& L, cudaStream_t stream) {
+  if (a.groups > 0)
+    return a.cache.d == 128 ? launch_mma_of<128, true>(a, p, L, stream)
+                            : launch_mma_of<64, true>(a, p, L, stream);
+  return a.cache.d == 128 ? launch_mma_of<128, false>(a, p, L, stream)
+                          : launch_mma_of<64, false>(a, p, L, stream);
+}
 
 size_t cache_attention_workspace(int32_t B, int32_t Hq, int32_t Hkv, int32_t d, int32_t D_max,
                                  int32_t L_max) {
@@ -652,7 +676,7 @@ size_t cache_attention_workspace(int32_t B, int32_t Hq, int32_t Hkv, int32_t d, 
     cache_attention_tc_plan(B, Hq, Hkv, D_max, L_max, &splits, &min_tiles);
     rows = tc_part_rows(B, Hq, D_max, splits);
   } else {
-    rows = mma_part_rows(B, Hkv, make_plan(B, Hq, Hkv, D_max, L_max));
+    rows = cache_attention_mma_rows(B, Hkv, make_plan(B, Hq, Hkv, D_max, L_max), false);
   }
   return rows == 0 ? 0 : part_bytes(rows, d) + align256((size_t)B * sizeof(int2));
 }
@@ -661,26 +685,18 @@ cudaError_t launch_cache_attention(const CacheAttnArgs& a, void* ws, cudaStream_
   const int32_t L_max = a.max_blocks * a.cache.block, d = a.cache.d;
   const int32_t tiles = (L_max + kCacheTile - 1) / kCacheTile;
   const bool tc = cache_attention_tc_runs(a.B, a.Hq, a.cache.Hkv, a.D_max, L_max);
-  Plan p{};
+  CacheMmaPlan p{};
   CacheAttnLaunch L{};
   int64_t rows;
-  int32_t part_tiles;
   if (tc) {
     cache_attention_tc_plan(a.B, a.Hq, a.cache.Hkv, a.D_max, L_max, &L.splits, &L.min_tiles);
     rows = tc_part_rows(a.B, a.Hq, a.D_max, L.splits);
-    part_tiles = cache_part_tiles(L.splits, L.min_tiles, tiles);
+    L.max_blocks = part_blocks(cache_part_tiles(L.splits, L.min_tiles, tiles), a.cache.block);
   } else {
     p = make_plan(a.B, a.Hq, a.cache.Hkv, a.D_max, L_max);
-    L.min_tiles = kMinTiles;
-    L.per_head = p.per_head;
-    L.goal = p.goal;
-    L.uniform = p.uniform;
-    L.row_groups = p.row_groups;
-    L.group_rows = p.rows;
-    rows = mma_part_rows(a.B, a.cache.Hkv, p);
-    part_tiles = std::min(tiles, kWorkRoom);
+    cache_attention_mma_fill(L, p, L_max, a.cache.block);
+    rows = cache_attention_mma_rows(a.B, a.cache.Hkv, p, false);
   }
-  L.max_blocks = part_blocks(part_tiles, a.cache.block);
   if (rows > 0) {
     unsigned char* at = static_cast<unsigned char*>(ws);
     L.part_o = reinterpret_cast<float*>(at);
@@ -689,16 +705,7 @@ cudaError_t launch_cache_attention(const CacheAttnArgs& a, void* ws, cudaStream_
     at += align256((size_t)rows * sizeof(float2));
     if (!tc) L.info = reinterpret_cast<int2*>(at);
   }
-  cudaError_t e;
-  if (tc) e = launch_cache_attention_tc(a, L, stream);
-  else if (d == 128)
-    e = p.rows > 8 ? launch_mma<128, 2>(a, p, L, stream)
-        : p.warps == kWarps ? launch_mma<128, 1>(a, p, L, stream)
-                            : launch_mma<128, 1, kManyWarps>(a, p, L, stream);
-  else
-    e = p.rows > 8 ? launch_mma<64, 2>(a, p, L, stream)
-        : p.warps == kWarps ? launch_mma<64, 1>(a, p, L, stream)
-                            : launch_mma<64, 1, kManyWarps>(a, p, L, stream);
+  const cudaError_t e = tc ? launch_cache_attention_tc(a, L, stream) : launch_cache_attention_mma(a, p, L, stream);
   if (e != cudaSuccess || rows == 0) return e;
   const dim3 grid((unsigned)(((int64_t)a.B * a.D_max * a.Hq + 7) / 8));
   return launch_kernel(d == 128 ? cache_attn_combine_kernel<128> : cache_attn_combine_kernel<64>, grid,

@@ -23,6 +23,11 @@ struct CacheAttnLaunch {
   // CacheWork
   int32_t per_head, goal, uniform, row_groups, group_rows;
   int2* info;          // [B]: first and last CTA of a sequence
+  // Groups' shared keys (tensor-core kernel): units of the grid, tiles of rows among them, parts and
+  // their rows [B][D_max][Hq][s_splits]
+  int32_t s_units, s_splits, s_min_tiles;
+  float* s_part_o;
+  float2* s_part_ml;
 };
 
 constexpr int kWorkTiles = 128;  // a CTA's most tiles of one sequence, about (kWorkRoom: at most)
@@ -88,6 +93,20 @@ __device__ __forceinline__ bool cache_lengths_ok(const CacheAttnArgs& a, int32_t
   return cache >= 0 && nd >= 0 && nd <= a.D_max && cache <= a.max_blocks * a.cache.block - nd;
 }
 
+// Tokens of the blocks that sequence b shares with its group: its own keys begin there.  -1: out of
+// range (with cache read).
+__device__ __forceinline__ int32_t cache_base(const CacheAttnArgs& a, int32_t b, int32_t cache) {
+  int32_t lo = 0, hi = a.groups;  // the last group that begins at b or before is in [lo, hi)
+  while (hi - lo > 1) {
+    const int32_t m = (lo + hi) >> 1;
+    if (a.group_start[m] <= b) lo = m;
+    else hi = m;
+  }
+  const int32_t n = a.shared[lo];
+  if (a.group_start[lo] > b || a.group_start[lo + 1] <= b || n < 0 || n > a.max_shared) return -1;
+  return n * a.cache.block <= cache ? n * a.cache.block : -1;
+}
+
 // What CTA x of a KV head's per_head works on: parts of sequences, one after the other.
 //  - The sequences alone fill the GPU (uniform > 0): as many CTAs for every sequence.
 //  - Else a sequence gets a CTA for every `chunk` tiles, with the least chunk for which `goal`
@@ -104,6 +123,7 @@ constexpr int kEvenTiles = 8;
 // A sequence shorter than this many of the shortest parts is not cut: the launch that combines
 // the parts takes 4 us (8 heads over 1200 keys: 12.4 us whole, 14.6 in two).
 constexpr int kCutFrom = 3;
+template <bool kShared>
 struct CacheWork {
   int32_t b, t_lo, t_hi, tiles;  // the part: tiles t_lo .. t_hi - 1 of the tiles of sequence b
   // the line: the CTA's tiles left, and where sequence b begins
@@ -112,11 +132,13 @@ struct CacheWork {
   // Tiles of a sequence; report: bad lengths are recorded.
   static __device__ __forceinline__ int32_t tiles_of(const CacheAttnArgs& a, int32_t b, bool report) {
     const int32_t c = a.cache_len[b], n = a.n_drafts[b];
-    if (!cache_lengths_ok(a, c, n)) {
+    const bool ok = cache_lengths_ok(a, c, n);
+    const int32_t base = kShared && ok && n > 0 ? cache_base(a, b, c) : 0;  // (tiles of its own keys)
+    if (!ok || base < 0) {
       if (report) record_status(a.status, SSD_ERR_DEVICE_BOUNDS);
       return 0;
     }
-    return n == 0 ? 0 : (c + n + kCacheTile - 1) / kCacheTile;
+    return n == 0 ? 0 : (c + n - base + kCacheTile - 1) / kCacheTile;
   }
 
   // The sequence that holds tile x of the line, from sequence b0 = a multiple of 32 on, which
@@ -266,7 +288,23 @@ inline bool cache_attention_few(int64_t B, int64_t Hkv, int64_t rows, int64_t L_
 bool cache_attention_tc_runs(int32_t B, int32_t Hq, int32_t Hkv, int32_t D_max, int32_t L_max);
 void cache_attention_tc_plan(int32_t B, int32_t Hq, int32_t Hkv, int32_t D_max, int32_t L_max,
                              int32_t* splits, int32_t* min_tiles);
+// own: (with groups) the sequences' own keys, too, beside their groups' shared ones
 cudaError_t launch_cache_attention_tc(const CacheAttnArgs& a, const CacheAttnLaunch& L,
-                                      cudaStream_t stream);
+                                      cudaStream_t stream, bool own = true);
+
+// cache_attention.cu: the mma.sync kernel, its plan and its part rows (all: of every sequence, not
+// only of those that are cut)
+struct CacheMmaPlan {
+  int32_t rows, row_groups;  // rows of a CTA, CTAs with other rows of the same keys
+  int32_t warps;             // of a CTA
+  int32_t per_head, goal, uniform;
+  bool cut(int32_t B) const { return per_head > B; }
+};
+CacheMmaPlan cache_attention_mma_plan(int32_t B, int32_t Hq, int32_t Hkv, int32_t D_max, int32_t L_max);
+int64_t cache_attention_mma_rows(int32_t B, int32_t Hkv, const CacheMmaPlan& p, bool all);
+// Fills L's part of the plan (max_blocks among it).
+void cache_attention_mma_fill(CacheAttnLaunch& L, const CacheMmaPlan& p, int32_t L_max, int32_t block);
+cudaError_t launch_cache_attention_mma(const CacheAttnArgs& a, const CacheMmaPlan& p,
+                                       const CacheAttnLaunch& L, cudaStream_t stream);
 
 }  // namespace ssd

@@ -1,0 +1,195 @@
+// cache_attention_shared.cu — attention over the paged 8-bit cache for sequences that share the
+// blocks of a long prompt (include/ssd.h, ssd_cache_attention_shared).  With P the tokens of the
+// blocks that a group shares, a row's softmax over its keys is that over [0, P) joined with that
+// over [P, end): with (m, l, o) the maximum, sum and unnormalised output of each,
+//   M = max m_i,   o = sum o_i 2^(m_i - M) / sum l_i 2^(m_i - M).
+// The keys in [0, P) are the same for all rows of the group, so those rows are stacked into the
+// 128-row tiles of the tensor-core kernel (cache_attention_tc.cu), which reads the keys once a tile
+// instead of once a sequence.  The keys from P on are each sequence's own: on the same kernel, in
+// the same launch, or, for few rows, on the mma.sync one (cache_attention.cu).  Both leave part rows,
+// which the kernel here joins.
+#include <algorithm>
+
+#include "cache_attention.cuh"
+
+namespace ssd {
+
+namespace {
+
+constexpr int kSharedTiles = 6;      // fewest tiles of a part of the shared keys
+constexpr int kSharedPartTiles = 256;
+
+struct SharedPlan {
+  bool plain;   // every sequence by itself: ssd_cache_attention()
+  bool own_tc;  // the own keys on the tensor-core kernel, too
+  CacheMmaPlan mma;
+  int32_t s_units, s_splits, splits, min_tiles;
+  int64_t s_rows, rows;  // part rows
+};
+
+SharedPlan make_plan(int32_t B, int32_t groups, int32_t Hq, int32_t Hkv, int32_t D_max, int32_t L_max,
+                     int32_t max_shared) {
+  SharedPlan p{};
+  const int64_t G = Hq / Hkv, per_seq = D_max * G, rows = (int64_t)B * D_max * Hq;
+  p.plain = max_shared <= 0 || 2 * groups > B || cache_attention_few(B, Hkv, per_seq, L_max);
+  if (p.plain) return p;
+  // (a group's last tile may be part empty)
+  const int64_t tiles_r = (B * per_seq) / 128 + groups, tiles = (max_shared + kCacheTile - 1) / kCacheTile;
+  const int64_t base = tiles_r * Hkv, target = 2 * device_sm_count();
+  const int64_t least = (tiles + kSharedPartTiles - 1) / kSharedPartTiles;
+  p.s_splits = (int32_t)std::max<int64_t>(
+      least, std::min<int64_t>(target / base, std::max<int64_t>(1, tiles / kSharedTiles)));
+  if (base * p.s_splits > INT32_MAX / 2) {
+    p.plain = true;
+    return p;
+  }
+  p.s_units = (int32_t)(base * p.s_splits);
+  p.s_rows = rows * p.s_splits;
+  p.own_tc = per_seq > 16;
+  if (p.own_tc) {
+    cache_attention_tc_plan(B, Hq, Hkv, D_max, L_max, &p.splits, &p.min_tiles);
+    p.rows = rows * p.splits;
+  } else {
+    p.mma = cache_attention_mma_plan(B, Hq, Hkv, D_max, L_max);
+    p.rows = cache_attention_mma_rows(B, Hkv, p.mma, true);
+  }
+  return p;
+}
+
+size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
+size_t part_bytes(int64_t rows, int32_t d) {
+  return align256((size_t)rows * d * sizeof(float)) + align256((size_t)rows * sizeof(float2));
+}
+
+// One warp per (sequence, draft, head): the parts of its row over the shared keys and over its own.
+template <int D>
+__global__ void __launch_bounds__(256) cache_attn_join_kernel(CacheAttnArgs a, CacheAttnLaunch L) {
+  constexpr int PER = D / 32;
+  pdl_wait();
+  const int32_t lane = threadIdx.x & 31;
+  if (blockIdx.x == 0) {  // (groups that are none of the batch's: nothing else looks at all of them)
+    bool bad = false;
+    for (int32_t g = threadIdx.x; g < a.groups; g += blockDim.x)
+      bad |= a.group_start[g] > a.group_start[g + 1];
+    if (threadIdx.x == 0) bad |= a.group_start[0] != 0 || a.group_start[a.groups] != a.B;
+    if (bad) record_status(a.status, SSD_ERR_DEVICE_BOUNDS);
+  }
+  const int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+  if (row >= (int64_t)a.B * a.D_max * a.Hq) return;
+  const int32_t h = (int32_t)(row % a.Hq);
+  const int64_t bj = row / a.Hq;
+  const int32_t b = (int32_t)(bj / a.D_max), j = (int32_t)(bj - (int64_t)b * a.D_max);
+  const int32_t cache = a.cache_len[b], nd = a.n_drafts[b];
+  if (!cache_lengths_ok(a, cache, nd) || j >= nd) return;
+  const int32_t base = cache_base(a, b, cache);
+  if (base < 0) return;
+  const int32_t shared_tiles = (base + kCacheTile - 1) / kCacheTile;
+  const int32_t n_shared = shared_tiles > 0 ? cache_parts(L.s_splits, L.s_min_tiles, shared_tiles) : 0;
+  int32_t n_own;
+  int64_t at, step = 1, room;
+  if (L.info != nullptr) {
+    const int32_t G = a.Hq / a.cache.Hkv, g = h / G;
+    const CacheShares x = cache_shares(L, a.B, b, L.info[b], g, j * G + (h - g * G));
+    n_own = x.parts;
+    step = L.group_rows;
+    at = x.at;
+    room = (int64_t)a.cache.Hkv * L.row_groups * (L.per_head + a.B) * step;
+  } else {
+    n_own = cache_parts(L.splits, L.min_tiles, (cache + nd - base + kCacheTile - 1) / kCacheTile);
+    at = row * L.splits;
+    room = (int64_t)a.B * a.D_max * a.Hq * L.splits;
+  }
+  if (n_own <= 0) return;  // (a wait gave up: no part is known)
+  if (!dbg_in(at + (n_own - 1) * step, room, a.status)) return;
+  const int32_t parts = n_shared + n_own;
+  auto ml_of = [&](int32_t s) {
+    return s < n_shared ? L.s_part_ml[row * L.s_splits + s] : L.part_ml[at + (s - n_shared) * step];
+  };
+  float M = -INFINITY;
+  for (int32_t s = lane; s < parts; s += 32) M = fmaxf(M, ml_of(s).x);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+  float acc[PER], sum = 0.f;
+#pragma unroll
+  for (int k = 0; k < PER; ++k) acc[k] = 0.f;
+  for (int32_t s0 = 0; s0 < parts; s0 += 32) {
+    float mine = 0.f;  // the factor of part s0 + lane
+    if (s0 + lane < parts) {
+      const float2 x = ml_of(s0 + lane);
+      mine = x.x == -INFINITY ? 0.f : exp2f(x.x - M);
+      sum += x.y * mine;
+    }
+    const int32_t n = min(32, parts - s0);
+#pragma unroll 4
+    for (int32_t i = 0; i < n; ++i) {
+      const float f = __shfl_sync(0xffffffffu, mine, i);
+      const int32_t s = s0 + i;
+      const float* po = (s < n_shared ? L.s_part_o + (row * L.s_splits + s) * D
+                                      : L.part_o + (at + (s - n_shared) * step) * D) + lane * PER;
+#pragma unroll
+      for (int k = 0; k < PER; ++k) acc[k] = f == 0.f ? acc[k] : acc[k] + po[k] * f;
+    }
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  const float inv = 1.f / sum;
+  __nv_bfloat16* ob = static_cast<__nv_bfloat16*>(a.o) + row * D + lane * PER;
+#pragma unroll
+  for (int k = 0; k < PER; k += 2)
+    *reinterpret_cast<uint32_t*>(ob + k) =
+        pack_bf16x2(row_value(acc[k], inv, sum), row_value(acc[k + 1], inv, sum));
+  if (a.lse != nullptr && lane == 0) a.lse[((int64_t)b * a.Hq + h) * a.D_max + j] = row_lse(M, sum);
+}
+
+}  // namespace
+
+size_t cache_attention_shared_workspace(int32_t B, int32_t groups, int32_t Hq, int32_t Hkv, int32_t d,
+                                        int32_t D_max, int32_t L_max, int32_t max_shared) {
+  const SharedPlan p = make_plan(B, groups, Hq, Hkv, D_max, L_max, max_shared);
+  if (p.plain) return cache_attention_workspace(B, Hq, Hkv, d, D_max, L_max);
+  return part_bytes(p.s_rows, d) + part_bytes(p.rows, d) + align256((size_t)B * sizeof(int2));
+}
+
+cudaError_t launch_cache_attention_shared(const CacheAttnArgs& a, void* ws, cudaStream_t stream) {
+  const int32_t S = a.cache.block, L_max = a.max_blocks * S, d = a.cache.d;
+  const SharedPlan p = make_plan(a.B, a.groups, a.Hq, a.cache.Hkv, a.D_max, L_max, a.max_shared * S);
+  if (p.plain) {
+    CacheAttnArgs one = a;
+    one.groups = 0;
+    return launch_cache_attention(one, ws, stream);
+  }
+  CacheAttnLaunch L{};
+  const int32_t tiles = (L_max + kCacheTile - 1) / kCacheTile;
+  const int32_t shared_tiles = (a.max_shared * S + kCacheTile - 1) / kCacheTile;
+  const int32_t s_blocks = part_blocks(cache_part_tiles(p.s_splits, kSharedTiles, shared_tiles), S);
+  L.s_units = p.s_units;
+  L.s_splits = p.s_splits;
+  L.s_min_tiles = kSharedTiles;
+  unsigned char* at = static_cast<unsigned char*>(ws);
+  L.s_part_o = reinterpret_cast<float*>(at);
+  at += align256((size_t)p.s_rows * d * sizeof(float));
+  L.s_part_ml = reinterpret_cast<float2*>(at);
+  at += align256((size_t)p.s_rows * sizeof(float2));
+  L.part_o = reinterpret_cast<float*>(at);
+  at += align256((size_t)p.rows * d * sizeof(float));
+  L.part_ml = reinterpret_cast<float2*>(at);
+  at += align256((size_t)p.rows * sizeof(float2));
+  L.splits = p.splits;
+  L.min_tiles = p.min_tiles;
+  L.max_blocks = s_blocks;
+  if (p.own_tc)
+    L.max_blocks = std::max(s_blocks, part_blocks(cache_part_tiles(p.splits, p.min_tiles, tiles), S));
+  cudaError_t e = launch_cache_attention_tc(a, L, stream, p.own_tc);
+  if (e != cudaSuccess) return e;
+  if (!p.own_tc) {
+    L.info = reinterpret_cast<int2*>(at);
+    cache_attention_mma_fill(L, p.mma, L_max, S);
+    e = launch_cache_attention_mma(a, p.mma, L, stream);
+    if (e != cudaSuccess) return e;
+  }
+  const dim3 grid((unsigned)(((int64_t)a.B * a.D_max * a.Hq + 7) / 8));
+  return launch_kernel(d == 128 ? cache_attn_join_kernel<128> : cache_attn_join_kernel<64>, grid, dim3(256),
+                       0, stream, true, a, L);
+}
+
+}  // namespace ssd

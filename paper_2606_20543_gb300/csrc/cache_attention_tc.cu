@@ -159,7 +159,11 @@ struct alignas(16) Shared {
   int32_t len[kLptMax]; // sequences' keys
 };
 
-template <int D>
+// kShared (ssd_cache_attention_shared): the grid's first L.s_units units work on groups' shared keys.
+// A unit stacks 128 rows of a group's sequences (D_max drafts each, those that are none left empty),
+// which all see the keys of the shared blocks, but for a row's key_start and position.  The others
+// work on sequences' own keys, behind the shared ones.  All leave part rows for a combine.
+template <int D, bool kShared>
 __global__ void __launch_bounds__(kThreadsTC, kCtasPerSm)
 cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
                      CacheAttnArgs a, CacheAttnLaunch L, int32_t mtiles) {
@@ -181,68 +185,145 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
   const int32_t tid = threadIdx.x, lane = tid & 31, warp = (int32_t)warp_uniform(tid >> 5);
   const int32_t S = a.cache.block, S_log = 31 - __clz(S), Hkv = a.cache.Hkv, G = a.Hq / Hkv;
   int32_t unit = blockIdx.x;
-  const int32_t split = unit % L.splits;
-  unit /= L.splits;
-  const int32_t mtile = unit % mtiles;
-  unit /= mtiles;
-  const int32_t g = unit % Hkv, rank = unit / Hkv;
-
-  // ---- the sequence: the rank-th longest (batches above 256 keep their order)
-  int32_t b = rank, cache, nd;
-  if (a.B <= 32) {
-    // every warp for itself, a sequence a lane
-    const int32_t c = lane < a.B ? a.cache_len[lane] : 0, n = lane < a.B ? a.n_drafts[lane] : 0;
-    const int32_t mine = lane < a.B ? (cache_lengths_ok(a, c, n) && n > 0 ? c + n : 0) : -1;
-    int32_t r = 0;
+  const bool stacked = kShared && unit < L.s_units;
+  if (kShared && !stacked) unit -= L.s_units;
+  const int32_t splits = stacked ? L.s_splits : L.splits;
+  const int32_t split = unit % splits;
+  unit /= splits;
+  int32_t b, cache, nd, g, mtile, rows_total, base = 0, tiles;
+  int32_t b_first = 0;                       // stacked: the group's first sequence
+  const int32_t per_seq = kShared ? a.D_max * G : 0;  // and a sequence's rows
+  if (stacked) {
+    g = unit % Hkv;
+    // the group that holds row tile unit / Hkv
+    int32_t tile = unit / Hkv, before = 0, group = -1, members = 0;
+    for (int32_t g0 = 0; g0 < a.groups && group < 0; g0 += 32) {
+      const bool in = g0 + lane < a.groups;
+      const int32_t s0 = in ? min(max(a.group_start[g0 + lane], 0), a.B) : 0;
+      const int32_t s1 = in ? min(max(a.group_start[g0 + lane + 1], s0), a.B) : 0;
+      const int32_t t = ((s1 - s0) * per_seq + kBM - 1) / kBM;
+      int32_t upto = t;
 #pragma unroll
-    for (int32_t j = 0; j < 32; ++j) {
-      const int32_t kj = __shfl_sync(0xffffffffu, mine, j);
-      r += kj > mine || (kj == mine && j < lane);
-    }
-    b = __ffs(__ballot_sync(0xffffffffu, r == rank)) - 1;
-    cache = __shfl_sync(0xffffffffu, c, b);
-    nd = __shfl_sync(0xffffffffu, n, b);
-  } else if (a.B <= kLptMax) {
-    int32_t mine = 0, c = 0, n = 0;
-    if (tid < a.B) {
-      c = a.cache_len[tid];
-      n = a.n_drafts[tid];
-      mine = cache_lengths_ok(a, c, n) && n > 0 ? c + n : 0;
-      sh.len[tid] = mine;
-    }
-    __syncthreads();
-    if (tid < a.B) {
-      int32_t r = 0;
-#pragma unroll 4
-      for (int32_t j = 0; j < a.B; ++j) {
-        const int32_t kj = sh.len[j];
-        r += kj > mine || (kj == mine && j < tid);
+      for (int o = 1; o < 32; o <<= 1) {
+        const int32_t y = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += y;
       }
-      if (r == rank) sh.seq = make_int3(tid, c, n);
+      upto += before;
+      const uint32_t here = __ballot_sync(0xffffffffu, tile < upto);
+      if (here != 0) {
+        const int32_t src = __ffs(here) - 1;
+        group = g0 + src;
+        mtile = tile - __shfl_sync(0xffffffffu, upto - t, src);
+        b_first = __shfl_sync(0xffffffffu, s0, src);
+        members = __shfl_sync(0xffffffffu, s1 - s0, src);
+      }
+      before = __shfl_sync(0xffffffffu, upto, 31);
     }
-    __syncthreads();
-    b = sh.seq.x;
-    cache = sh.seq.y;
-    nd = sh.seq.z;
+    if (group < 0) return;
+    const int32_t n = a.shared[group];
+    if (n <= 0 || n > a.max_shared) return;  // (recorded with the sequences' own keys)
+    cache = n * S;
+    nd = 0;
+    rows_total = members * per_seq;
+    b = 0;
   } else {
-    cache = a.cache_len[b];
-    nd = a.n_drafts[b];
+    mtile = unit % mtiles;
+    unit /= mtiles;
+    g = unit % Hkv;
+    const int32_t rank = unit / Hkv;
+
+    // (those behind the shared ones)
+    auto own_keys = [&](int32_t i, int32_t c, int32_t n) {
+      return kShared ? c + n - max(0, cache_base(a, i, c)) : c + n;
+    };
+    // ---- the sequence: the rank-th longest (batches above 256 keep their order)
+    b = rank;
+    if (a.B <= 32) {
+      // every warp for itself, a sequence a lane
+      const int32_t c = lane < a.B ? a.cache_len[lane] : 0, n = lane < a.B ? a.n_drafts[lane] : 0;
+      const int32_t mine = lane < a.B ? (cache_lengths_ok(a, c, n) && n > 0 ? own_keys(lane, c, n) : 0) : -1;
+      int32_t r = 0;
+#pragma unroll
+      for (int32_t j = 0; j < 32; ++j) {
+        const int32_t kj = __shfl_sync(0xffffffffu, mine, j);
+        r += kj > mine || (kj == mine && j < lane);
+      }
+      b = __ffs(__ballot_sync(0xffffffffu, r == rank)) - 1;
+      cache = __shfl_sync(0xffffffffu, c, b);
+      nd = __shfl_sync(0xffffffffu, n, b);
+    } else if (a.B <= kLptMax) {
+      int32_t mine = 0, c = 0, n = 0;
+      if (tid < a.B) {
+        c = a.cache_len[tid];
+        n = a.n_drafts[tid];
+        mine = cache_lengths_ok(a, c, n) && n > 0 ? own_keys(tid, c, n) : 0;
+        sh.len[tid] = mine;
+      }
+      __syncthreads();
+      if (tid < a.B) {
+        int32_t r = 0;
+#pragma unroll 4
+        for (int32_t j = 0; j < a.B; ++j) {
+          const int32_t kj = sh.len[j];
+          r += kj > mine || (kj == mine && j < tid);
+        }
+        if (r == rank) sh.seq = make_int3(tid, c, n);
+      }
+      __syncthreads();
+      b = sh.seq.x;
+      cache = sh.seq.y;
+      nd = sh.seq.z;
+    } else {
+      cache = a.cache_len[b];
+      nd = a.n_drafts[b];
+    }
+    const bool lengths_ok = cache_lengths_ok(a, cache, nd);
+    if (kShared && lengths_ok && nd > 0) base = cache_base(a, b, cache);
+    if (!lengths_ok || base < 0) {
+      if (tid == 0 && split == 0 && g == 0 && mtile == 0) record_status(a.status, SSD_ERR_DEVICE_BOUNDS);
+      return;
+    }
+    rows_total = nd * G;
   }
-  if (!cache_lengths_ok(a, cache, nd)) {
-    if (tid == 0 && split == 0 && g == 0 && mtile == 0) record_status(a.status, SSD_ERR_DEVICE_BOUNDS);
-    return;
-  }
-  const int32_t Lk = cache + nd, rows_total = nd * G, row0 = mtile * kBM;
-  const int32_t tiles = (Lk + KT - 1) / KT;
-  const int32_t parts = cache_parts(L.splits, L.min_tiles, tiles);
+  // A row's sequence, draft and head; false: no row.
+  auto row_of = [&](int32_t r, int32_t& rb, int32_t& j, int32_t& h) {
+    if (stacked) {
+      const int32_t m = r / per_seq;
+      rb = b_first + m;
+      r -= m * per_seq;
+      j = r / G;
+      h = g * G + (r - j * G);
+      if (m * per_seq >= rows_total) return false;
+      const int32_t c = a.cache_len[rb], n = a.n_drafts[rb];
+      return cache_lengths_ok(a, c, n) && j < n && c >= cache;
+    }
+    rb = b;
+    const bool live = r < rows_total;
+    j = live ? r / G : 0;
+    h = g * G + (live ? r - j * G : 0);
+    return live;
+  };
+  const int32_t row0 = mtile * kBM;
+  const int32_t Lk = cache + nd;
+  tiles = (Lk - base + KT - 1) / KT;
+  const int32_t parts = cache_parts(splits, stacked ? L.s_min_tiles : L.min_tiles, tiles);
   if (row0 >= rows_total || split >= parts) return;
+  if (stacked) {  // the first of the tile's sequences names the blocks
+    int32_t least = 0x7fffffff;
+    for (int32_t r = lane; r < kBM; r += 32) {
+      int32_t rb, j, h;
+      if (row_of(row0 + r, rb, j, h)) least = min(least, rb);
+    }
+    b = __reduce_min_sync(0xffffffffu, least);
+    if (b == 0x7fffffff) return;
+  }
   int32_t t_lo = 0, t_hi = tiles;
   if (parts > 1) {
     t_lo = (int32_t)((int64_t)tiles * split / parts);
     t_hi = (int32_t)((int64_t)tiles * (split + 1) / parts);
   }
-  const int32_t k_lo = t_lo * KT, k_hi = min(Lk, t_hi * KT), ntiles = t_hi - t_lo;
-  const int32_t start = a.key_start != nullptr ? min(Lk, max(0, a.key_start[b])) : 0;
+  const int32_t k_lo = base + t_lo * KT, k_hi = min(Lk, base + t_hi * KT), ntiles = t_hi - t_lo;
+  const int32_t start = a.key_start != nullptr && !stacked ? min(Lk, max(0, a.key_start[b])) : 0;
   const int32_t b_lo = k_lo >> S_log, nb = ((k_hi - 1) >> S_log) + 1 - b_lo;
 
   // ---- set-up
@@ -283,7 +364,7 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
     s_blk[i] = make_float4(a.cache.k_scale[at], id >= 0 && vs > 0.f ? log2f(least) : -INFINITY,
                            1.f / least, __int_as_float(id));
   }
-  if (a.draft_pos != nullptr) {
+  if (a.draft_pos != nullptr && !stacked) {
     for (int32_t j = stages ? tid - 128 : nd; j < nd; j += 128) {
       const int32_t p = cache_flat_pos(a, b, cache, j);
       if (p < 0 && split == 0 && g == 0 && mtile == 0) record_status(a.status, SSD_ERR_DEVICE_BOUNDS);
@@ -295,12 +376,12 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
 #pragma unroll 1
   for (int32_t q_row = tid >> 1; !stages && q_row < kBM && row0 + (q_row & ~15) < rows_total;
        q_row += 64) {
-    const int32_t r = row0 + q_row, half = tid & 1;
-    const bool live = r < rows_total;
-    const int32_t j = live ? r / G : 0, h = g * G + (live ? r - j * G : 0);
+    const int32_t half = tid & 1;
+    int32_t rb, j, h;
+    const bool live = row_of(row0 + q_row, rb, j, h);
     const uint4* src = reinterpret_cast<const uint4*>(
                            static_cast<const __nv_bfloat16*>(a.q) +
-                           (((int64_t)b * a.D_max + j) * a.Hq + h) * D) + half * (D / 16);
+                           (((int64_t)rb * a.D_max + j) * a.Hq + h) * D) + half * (D / 16);
     uint4 w[D / 16];
     float m = 0.f;
 #pragma unroll
@@ -496,13 +577,22 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
     // ------------------------------------------------------------- softmax
     take_registers();
     const uint32_t lane_off = (uint32_t)(warp * 32) << 16;
-    const int32_t r = row0 + tid;
-    const bool warp_live = row0 + warp * 32 < rows_total;
+    int32_t rb, j, h;
+    const bool row_live = row_of(row0 + tid, rb, j, h);
+    const bool warp_live = stacked ? __any_sync(0xffffffffu, row_live) : row0 + warp * 32 < rows_total;
     const float rowc = sh.rowc[tid];
-    const int32_t j = r < rows_total ? r / G : 0;
-    int32_t qpos = 0x7fffffff;
+    int32_t qpos = 0x7fffffff, row_start = 0;
     auto flat_of = [&](int32_t i) { return staged ? s_flat[i] : cache_flat_pos(a, b, cache, i); };
-    if (r < rows_total) qpos = flat_of(j);
+    if (row_live) {
+      if (stacked) {
+        qpos = cache_flat_pos(a, rb, a.cache_len[rb], j);
+        if (a.key_start != nullptr) row_start = min(Lk, max(0, a.key_start[rb]));
+      } else {
+        qpos = flat_of(j);
+      }
+    }
+    // keys below this one are hidden from some row of the warp
+    const int32_t hide_to = stacked ? __reduce_max_sync(0xffffffffu, row_start) : start;
     // keys below this one are visible to every row of the warp
     const int32_t mask_from = min(cache, __reduce_min_sync(0xffffffffu, qpos) + 1);
     // references (log2) of the scores, for the sum, and of the scores times their V scales, for
@@ -539,9 +629,11 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
         float sv[64];
         tmem_ld32(tmem + lane_off + sb * KT, sv);
         tmem_ld32(tmem + lane_off + sb * KT + 32, sv + 32);
-        if (c0 + KT > mask_from || c0 < start || c0 + KT > k_hi || any_bad) {
+        if (c0 + KT > mask_from || c0 < hide_to || c0 + KT > k_hi || any_bad) {
           uint64_t keep;
-          if (a.draft_pos == nullptr) {
+          if (stacked) {
+            keep = low_bits(min(Lk, qpos < 0x7fffffff ? qpos + 1 : Lk) - c0) & ~low_bits(row_start - c0);
+          } else if (a.draft_pos == nullptr) {
             keep = low_bits(qpos < 0x7fffffff ? qpos + 1 - c0 : KT);
           } else {
             keep = low_bits(min(cache, qpos < 0x7fffffff ? qpos + 1 : cache) - c0);
@@ -632,13 +724,13 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
     if (ok) ok = wait_warp(&sh.pv_done[(ntiles - 1) & 1], ((ntiles - 1) >> 1) & 1, a.status);
     tc_fence_after();
     if (ok && warp_live) {
-      const bool live = r < rows_total;
-      const int32_t h = g * G + (r - j * G);
-      const int64_t orow = ((int64_t)b * a.D_max + j) * a.Hq + h;
-      const bool direct = parts == 1;
-      const int64_t prow = orow * L.splits + split;
-      const bool store = live && (direct ? dbg_in(orow, (int64_t)a.B * a.D_max * a.Hq, a.status)
-                                         : dbg_in(prow, (int64_t)a.B * a.D_max * a.Hq * L.splits, a.status));
+      const int64_t orow = ((int64_t)rb * a.D_max + j) * a.Hq + h;
+      const bool direct = !kShared && parts == 1;
+      const int64_t prow = orow * splits + split;
+      float* part_o = stacked ? L.s_part_o : L.part_o;
+      float2* part_ml = stacked ? L.s_part_ml : L.part_ml;
+      const bool store = row_live && (direct ? dbg_in(orow, (int64_t)a.B * a.D_max * a.Hq, a.status)
+                                             : dbg_in(prow, (int64_t)a.B * a.D_max * a.Hq * splits, a.status));
       const float inv = v_ref / l_run;
 #pragma unroll 1
       for (int c = 0; c < D / 32; ++c) {
@@ -656,7 +748,7 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
                                pack_bf16x2(x[6], x[7]));
           }
         } else {
-          float4* po = reinterpret_cast<float4*>(L.part_o + prow * D + c * 32);
+          float4* po = reinterpret_cast<float4*>(part_o + prow * D + c * 32);
 #pragma unroll
           for (int i = 0; i < 8; ++i)
             po[i] = make_float4(ov[4 * i] * v_ref, ov[4 * i + 1] * v_ref, ov[4 * i + 2] * v_ref,
@@ -664,7 +756,7 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
         }
       }
       if (store) {
-        if (!direct) L.part_ml[prow] = make_float2(m_run, l_run);
+        if (!direct) part_ml[prow] = make_float2(m_run, l_run);
         else if (a.lse != nullptr)
           a.lse[((int64_t)b * a.Hq + h) * a.D_max + j] = row_lse(m_run, l_run);
       }
@@ -691,8 +783,8 @@ bool cache_map(CUtensorMap* map, const void* base, int64_t rows, int32_t box_row
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int D>
-cudaError_t launch(const CacheAttnArgs& a, const CacheAttnLaunch& L, cudaStream_t stream) {
+template <int D, bool kShared>
+cudaError_t launch(const CacheAttnArgs& a, const CacheAttnLaunch& L, bool own, cudaStream_t stream) {
   const int32_t mtiles = (int32_t)(((int64_t)a.D_max * (a.Hq / a.cache.Hkv) + kBM - 1) / kBM);
   const int64_t rows = (int64_t)a.cache.num_blocks * a.cache.Hkv * a.cache.block;
   const int32_t box = std::min(a.cache.block, KT);
@@ -704,12 +796,12 @@ cudaError_t launch(const CacheAttnArgs& a, const CacheAttnLaunch& L, cudaStream_
            (size_t)blocks * 16 + (size_t)drafts * 4;
   };
   // (a part has at most a tile more than kMaxPartTiles)
-  const cudaError_t e = allow_smem(cache_attn_tc_kernel<D>,
+  const cudaError_t e = allow_smem(cache_attn_tc_kernel<D, kShared>,
                                    smem(part_blocks(kMaxPartTiles + 1, kLeastBlock), kMaxDrafts));
   if (e != cudaSuccess) return e;
-  const int64_t grid = (int64_t)a.B * a.cache.Hkv * mtiles * L.splits;
+  const int64_t grid = (kShared ? L.s_units : 0) + (own ? (int64_t)a.B * a.cache.Hkv * mtiles * L.splits : 0);
   if (grid > INT32_MAX) return cudaErrorInvalidValue;
-  return launch_kernel(cache_attn_tc_kernel<D>, dim3((unsigned)grid), dim3(kThreadsTC),
+  return launch_kernel(cache_attn_tc_kernel<D, kShared>, dim3((unsigned)grid), dim3(kThreadsTC),
                        smem(L.max_blocks, a.draft_pos != nullptr && a.D_max <= kMaxDrafts ? a.D_max : 0),
                        stream, true, tk, tv, a, L, mtiles);
 }
@@ -736,8 +828,10 @@ void cache_attention_tc_plan(int32_t B, int32_t Hq, int32_t Hkv, int32_t D_max, 
 }
 
 cudaError_t launch_cache_attention_tc(const CacheAttnArgs& a, const CacheAttnLaunch& L,
-                                      cudaStream_t stream) {
-  return a.cache.d == 128 ? launch<128>(a, L, stream) : launch<64>(a, L, stream);
+                                      cudaStream_t stream, bool own) {
+  if (a.groups > 0)
+    return a.cache.d == 128 ? launch<128, true>(a, L, own, stream) : launch<64, true>(a, L, own, stream);
+  return a.cache.d == 128 ? launch<128, false>(a, L, true, stream) : launch<64, false>(a, L, true, stream);
 }
 
 }  // namespace ssd

@@ -478,10 +478,18 @@ struct CacheAttnArgs {
   void* o;
   float* lse;  // nullable
   int32_t* status;
+  // ssd_cache_attention_shared: groups of sequences whose first blocks are the same (0: none)
+  int32_t groups, max_shared;
+  const int32_t* group_start;  // [groups + 1]
+  const int32_t* shared;       // [groups], blocks
 };
 size_t cache_attention_workspace(int32_t B, int32_t Hq, int32_t Hkv, int32_t d, int32_t D_max,
                                  int32_t L_max);
 cudaError_t launch_cache_attention(const CacheAttnArgs& a, void* ws, cudaStream_t stream);
+// ---- cache_attention_shared.cu (max_shared: tokens)
+size_t cache_attention_shared_workspace(int32_t B, int32_t groups, int32_t Hq, int32_t Hkv, int32_t d,
+                                        int32_t D_max, int32_t L_max, int32_t max_shared);
+cudaError_t launch_cache_attention_shared(const CacheAttnArgs& a, void* ws, cudaStream_t stream);
 
 // ---- sample.cu
 struct SampleArgs {

@@ -133,7 +133,9 @@ cache_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
   __shared__ uint64_t s_full[W][kStages];
   __shared__ float2 s_ml[W][RW];
   if (threadIdx.x < 2) prefetch_tensormap(threadIdx.x == 0 ? &tmK : &tmV);
-  pdl_wait();
+  // (kShared: beside the kernel before it, on the shared keys, which let it start when all before
+  // that was done; the first CTA waits for it at the end)
+  if (!kShared) pdl_wait();
 
   const int32_t tid = threadIdx.x, lane = tid & 31, warp = (int32_t)warp_uniform(tid >> 5);
   const int32_t g = blockIdx.y, S = a.cache.block, S_log = 31 - __clz(S), G = a.Hq / a.cache.Hkv;
@@ -489,7 +491,7 @@ cache_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
           if (r8 == 0) s_ml[warp][r] = make_float2(m_ref[n][u], l[n][u]);
         }
     }
-    if (__syncthreads_or(!ok)) return;
+    if (__syncthreads_or(!ok)) break;
     constexpr int PER = D / 32;
     for (int32_t r = warp; r < RW && row0 + r < rows_total; r += W) {
       float M = -INFINITY;
@@ -530,6 +532,7 @@ cache_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
       }
     }
   }
+  if (kShared && pdl_first_block()) pdl_wait();
 }
 
 // One warp per (sequence, draft, head): the parts of its row, weighted by their

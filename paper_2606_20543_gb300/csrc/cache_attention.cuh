@@ -26,6 +26,7 @@ struct CacheAttnLaunch {
   // Groups' shared keys (tensor-core kernel): units of the grid, tiles of rows among them, parts and
   // their rows [B][D_max][Hq][s_splits]
   int32_t s_units, s_splits, s_min_tiles;
+  int32_t early;  // the kernel after it may run beside it: the sequences' own keys
   float* s_part_o;
   float2* s_part_ml;
 };
@@ -105,6 +106,26 @@ __device__ __forceinline__ int32_t cache_base(const CacheAttnArgs& a, int32_t b,
   const int32_t n = a.shared[lo];
   if (a.group_start[lo] > b || a.group_start[lo + 1] <= b || n < 0 || n > a.max_shared) return -1;
   return n * a.cache.block <= cache ? n * a.cache.block : -1;
+}
+
+// The same of one sequence, by a converged warp: two loads, one after the other.
+__device__ __forceinline__ int32_t cache_base_warp(const CacheAttnArgs& a, int32_t b, int32_t cache) {
+  const int32_t lane = threadIdx.x & 31;
+  int32_t group = -1, begin = 0, end = 0;
+  for (int32_t g0 = 0; g0 < a.groups; g0 += 32) {
+    const int32_t g = min(g0 + lane, a.groups);
+    const int32_t s0 = a.group_start[g], s1 = a.group_start[min(g + 1, a.groups)];
+    const uint32_t here = __ballot_sync(0xffffffffu, g0 + lane < a.groups && s0 <= b);
+    if (here == 0) break;
+    const int32_t src = 31 - __clz(here);
+    group = g0 + src;
+    begin = __shfl_sync(0xffffffffu, s0, src);
+    end = __shfl_sync(0xffffffffu, s1, src);
+    if (src < 31) break;
+  }
+  if (group < 0 || begin > b || end <= b) return -1;
+  const int32_t n = a.shared[group];
+  return n < 0 || n > a.max_shared || n * a.cache.block > cache ? -1 : n * a.cache.block;
 }
 
 // What CTA x of a KV head's per_head works on: parts of sequences, one after the other.

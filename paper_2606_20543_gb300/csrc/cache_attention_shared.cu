@@ -16,14 +16,16 @@ namespace ssd {
 
 namespace {
 
-constexpr int kSharedTiles = 6;      // fewest tiles of a part of the shared keys
-constexpr int kSharedPartTiles = 256;
+constexpr int kSharedTiles = 6;        // fewest tiles of a part of the shared keys,
+constexpr int kSharedPartTiles = 256;  // and about the most
+constexpr int kSharedWaves = 4;        // units of the shared keys for each place of one, about: groups
+                                       // differ in length, and the longest part is what the end waits for
 
 struct SharedPlan {
   bool plain;   // every sequence by itself: ssd_cache_attention()
   bool own_tc;  // the own keys on the tensor-core kernel, too
   CacheMmaPlan mma;
-  int32_t s_units, s_splits, splits, min_tiles;
+  int32_t s_units, s_splits, s_min_tiles, splits, min_tiles;
   int64_t s_rows, rows;  // part rows
 };
 
@@ -35,10 +37,9 @@ SharedPlan make_plan(int32_t B, int32_t groups, int32_t Hq, int32_t Hkv, int32_t
   if (p.plain) return p;
   // (a group's last tile may be part empty)
   const int64_t tiles_r = (B * per_seq) / 128 + groups, tiles = (max_shared + kCacheTile - 1) / kCacheTile;
-  const int64_t base = tiles_r * Hkv, target = 2 * device_sm_count();
-  const int64_t least = (tiles + kSharedPartTiles - 1) / kSharedPartTiles;
-  p.s_splits = (int32_t)std::max<int64_t>(
-      least, std::min<int64_t>(target / base, std::max<int64_t>(1, tiles / kSharedTiles)));
+  const int64_t base = tiles_r * Hkv, units = (int64_t)kSharedWaves * 2 * device_sm_count();
+  p.s_min_tiles = (int32_t)std::min<int64_t>(kSharedPartTiles / 2, std::max<int64_t>(kSharedTiles, base * tiles / units));
+  p.s_splits = (int32_t)std::max<int64_t>(1, tiles / p.s_min_tiles);
   if (base * p.s_splits > INT32_MAX / 2) {
     p.plain = true;
     return p;
@@ -61,6 +62,12 @@ size_t part_bytes(int64_t rows, int32_t d) {
   return align256((size_t)rows * d * sizeof(float)) + align256((size_t)rows * sizeof(float2));
 }
 
+constexpr int kTogether = 8;
+template <int N>
+struct alignas(4 * N) Lanes {
+  float x[N];
+};
+
 // One warp per (sequence, draft, head): the parts of its row over the shared keys and over its own.
 template <int D>
 __global__ void __launch_bounds__(256) cache_attn_join_kernel(CacheAttnArgs a, CacheAttnLaunch L) {
@@ -80,8 +87,9 @@ __global__ void __launch_bounds__(256) cache_attn_join_kernel(CacheAttnArgs a, C
   const int64_t bj = row / a.Hq;
   const int32_t b = (int32_t)(bj / a.D_max), j = (int32_t)(bj - (int64_t)b * a.D_max);
   const int32_t cache = a.cache_len[b], nd = a.n_drafts[b];
+  const int2 cut = L.info != nullptr ? L.info[b] : make_int2(0, 0);
   if (!cache_lengths_ok(a, cache, nd) || j >= nd) return;
-  const int32_t base = cache_base(a, b, cache);
+  const int32_t base = cache_base_warp(a, b, cache);
   if (base < 0) return;
   const int32_t shared_tiles = (base + kCacheTile - 1) / kCacheTile;
   const int32_t n_shared = shared_tiles > 0 ? cache_parts(L.s_splits, L.s_min_tiles, shared_tiles) : 0;
@@ -89,7 +97,7 @@ __global__ void __launch_bounds__(256) cache_attn_join_kernel(CacheAttnArgs a, C
   int64_t at, step = 1, room;
   if (L.info != nullptr) {
     const int32_t G = a.Hq / a.cache.Hkv, g = h / G;
-    const CacheShares x = cache_shares(L, a.B, b, L.info[b], g, j * G + (h - g * G));
+    const CacheShares x = cache_shares(L, a.B, b, cut, g, j * G + (h - g * G));
     n_own = x.parts;
     step = L.group_rows;
     at = x.at;
@@ -109,9 +117,10 @@ __global__ void __launch_bounds__(256) cache_attn_join_kernel(CacheAttnArgs a, C
   for (int32_t s = lane; s < parts; s += 32) M = fmaxf(M, ml_of(s).x);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
-  float acc[PER], sum = 0.f;
+  Lanes<PER> acc;
 #pragma unroll
-  for (int k = 0; k < PER; ++k) acc[k] = 0.f;
+  for (int k = 0; k < PER; ++k) acc.x[k] = 0.f;
+  float sum = 0.f;
   for (int32_t s0 = 0; s0 < parts; s0 += 32) {
     float mine = 0.f;  // the factor of part s0 + lane
     if (s0 + lane < parts) {
@@ -120,14 +129,21 @@ __global__ void __launch_bounds__(256) cache_attn_join_kernel(CacheAttnArgs a, C
       sum += x.y * mine;
     }
     const int32_t n = min(32, parts - s0);
-#pragma unroll 4
-    for (int32_t i = 0; i < n; ++i) {
-      const float f = __shfl_sync(0xffffffffu, mine, i);
-      const int32_t s = s0 + i;
-      const float* po = (s < n_shared ? L.s_part_o + (row * L.s_splits + s) * D
-                                      : L.part_o + (at + (s - n_shared) * step) * D) + lane * PER;
+    for (int32_t i0 = 0; i0 < n; i0 += kTogether) {  // kTogether parts are asked for at once
+      Lanes<PER> v[kTogether];
 #pragma unroll
-      for (int k = 0; k < PER; ++k) acc[k] = f == 0.f ? acc[k] : acc[k] + po[k] * f;
+      for (int i = 0; i < kTogether; ++i) {
+        const int32_t s = s0 + min(i0 + i, n - 1);
+        v[i] = *reinterpret_cast<const Lanes<PER>*>(
+            (s < n_shared ? L.s_part_o + (row * L.s_splits + s) * D
+                          : L.part_o + (at + (s - n_shared) * step) * D) + lane * PER);
+      }
+#pragma unroll
+      for (int i = 0; i < kTogether; ++i) {
+        const float f = i0 + i < n ? __shfl_sync(0xffffffffu, mine, min(i0 + i, 31)) : 0.f;
+#pragma unroll
+        for (int k = 0; k < PER; ++k) acc.x[k] = f == 0.f ? acc.x[k] : acc.x[k] + v[i].x[k] * f;
+      }
     }
   }
 #pragma unroll
@@ -137,7 +153,7 @@ __global__ void __launch_bounds__(256) cache_attn_join_kernel(CacheAttnArgs a, C
 #pragma unroll
   for (int k = 0; k < PER; k += 2)
     *reinterpret_cast<uint32_t*>(ob + k) =
-        pack_bf16x2(row_value(acc[k], inv, sum), row_value(acc[k + 1], inv, sum));
+        pack_bf16x2(row_value(acc.x[k], inv, sum), row_value(acc.x[k + 1], inv, sum));
   if (a.lse != nullptr && lane == 0) a.lse[((int64_t)b * a.Hq + h) * a.D_max + j] = row_lse(M, sum);
 }
 
@@ -161,10 +177,11 @@ cudaError_t launch_cache_attention_shared(const CacheAttnArgs& a, void* ws, cuda
   CacheAttnLaunch L{};
   const int32_t tiles = (L_max + kCacheTile - 1) / kCacheTile;
   const int32_t shared_tiles = (a.max_shared * S + kCacheTile - 1) / kCacheTile;
-  const int32_t s_blocks = part_blocks(cache_part_tiles(p.s_splits, kSharedTiles, shared_tiles), S);
+  const int32_t s_blocks = part_blocks(cache_part_tiles(p.s_splits, p.s_min_tiles, shared_tiles), S);
   L.s_units = p.s_units;
   L.s_splits = p.s_splits;
-  L.s_min_tiles = kSharedTiles;
+  L.s_min_tiles = p.s_min_tiles;
+  L.early = !p.own_tc;
   unsigned char* at = static_cast<unsigned char*>(ws);
   L.s_part_o = reinterpret_cast<float*>(at);
   at += align256((size_t)p.s_rows * d * sizeof(float));

@@ -149,7 +149,16 @@ __device__ __forceinline__ uint64_t rows_desc(uint32_t saddr) {
   return D == 128 ? d : (d & ~(7ull << 61)) | 4ull << 61;  // 64-byte swizzle
 }
 
-struct alignas(16) Shared {
+// Of a unit of stacked rows: a row's place among the batch's rows [B][D_max][Hq] (-1: no row), its
+// position and its first visible key.
+template <bool kShared>
+struct Rows {};
+template <>
+struct Rows<true> {
+  int32_t at[kBM], pos[kBM], start[kBM], least[4];
+};
+template <bool kShared>
+struct alignas(16) Shared : Rows<kShared> {
   uint64_t k_full[kNK], k_empty[kNK], v_full[kNV], v_empty[kNV];
   uint64_t w_full[2];  // V widened
   uint64_t s_full[2], p_ready[2], pv_done[2];
@@ -175,12 +184,13 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
   unsigned char* sK = sQ + 2 * kQBytes;
   unsigned char* sV = sK + kNK * kTileBytes;
   unsigned char* sW = sV + kNV * kTileBytes;       // V in float16 [2][d / 64][KT][128 bytes]
-  Shared& sh = *reinterpret_cast<Shared*>(sW + 2 * kWideBytes);
+  Shared<kShared>& sh = *reinterpret_cast<Shared<kShared>*>(sW + 2 * kWideBytes);
   // the part's blocks: K scale, log2 of the V scale, its inverse, id (-1: outside the pool)
   float4* s_blk = reinterpret_cast<float4*>(&sh + 1);
   int32_t* s_flat = reinterpret_cast<int32_t*>(s_blk + L.max_blocks);  // the drafts' positions
   const bool staged = a.draft_pos != nullptr && a.D_max <= kMaxDrafts;
   pdl_wait();
+  if (kShared && L.early) pdl_launch_dependents();
 
   const int32_t tid = threadIdx.x, lane = tid & 31, warp = (int32_t)warp_uniform(tid >> 5);
   const int32_t S = a.cache.block, S_log = 31 - __clz(S), Hkv = a.cache.Hkv, G = a.Hq / Hkv;
@@ -196,12 +206,14 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
   if (stacked) {
     g = unit % Hkv;
     // the group that holds row tile unit / Hkv
-    int32_t tile = unit / Hkv, before = 0, group = -1, members = 0;
+    const int32_t tile = unit / Hkv;
+    int32_t before = 0, group = -1, members = 0;
     for (int32_t g0 = 0; g0 < a.groups && group < 0; g0 += 32) {
       const bool in = g0 + lane < a.groups;
       const int32_t s0 = in ? min(max(a.group_start[g0 + lane], 0), a.B) : 0;
       const int32_t s1 = in ? min(max(a.group_start[g0 + lane + 1], s0), a.B) : 0;
-      const int32_t t = ((s1 - s0) * per_seq + kBM - 1) / kBM;
+      const int32_t s_blocks = in ? a.shared[g0 + lane] : 0;
+      const int32_t t = (int32_t)((uint32_t)((s1 - s0) * per_seq + kBM - 1) / kBM);
       int32_t upto = t;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
@@ -216,13 +228,13 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
         mtile = tile - __shfl_sync(0xffffffffu, upto - t, src);
         b_first = __shfl_sync(0xffffffffu, s0, src);
         members = __shfl_sync(0xffffffffu, s1 - s0, src);
+        cache = __shfl_sync(0xffffffffu, s_blocks, src);
       }
       before = __shfl_sync(0xffffffffu, upto, 31);
     }
-    if (group < 0) return;
-    const int32_t n = a.shared[group];
-    if (n <= 0 || n > a.max_shared) return;  // (recorded with the sequences' own keys)
-    cache = n * S;
+    // (what is out of range is recorded with the sequences' own keys)
+    if (group < 0 || cache <= 0 || cache > a.max_shared) return;
+    cache *= S;
     nd = 0;
     rows_total = members * per_seq;
     b = 0;
@@ -285,37 +297,37 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
     }
     rows_total = nd * G;
   }
-  // A row's sequence, draft and head; false: no row.
-  auto row_of = [&](int32_t r, int32_t& rb, int32_t& j, int32_t& h) {
-    if (stacked) {
-      const int32_t m = r / per_seq;
-      rb = b_first + m;
-      r -= m * per_seq;
-      j = r / G;
-      h = g * G + (r - j * G);
-      if (m * per_seq >= rows_total) return false;
-      const int32_t c = a.cache_len[rb], n = a.n_drafts[rb];
-      return cache_lengths_ok(a, c, n) && j < n && c >= cache;
-    }
-    rb = b;
-    const bool live = r < rows_total;
-    j = live ? r / G : 0;
-    h = g * G + (live ? r - j * G : 0);
-    return live;
-  };
   const int32_t row0 = mtile * kBM;
   const int32_t Lk = cache + nd;
   tiles = (Lk - base + KT - 1) / KT;
   const int32_t parts = cache_parts(splits, stacked ? L.s_min_tiles : L.min_tiles, tiles);
   if (row0 >= rows_total || split >= parts) return;
-  if (stacked) {  // the first of the tile's sequences names the blocks
-    int32_t least = 0x7fffffff;
-    for (int32_t r = lane; r < kBM; r += 32) {
-      int32_t rb, j, h;
-      if (row_of(row0 + r, rb, j, h)) least = min(least, rb);
+  if constexpr (kShared) {
+    if (stacked) {
+      int32_t least = 0x7fffffff;
+      if (tid < kBM) {
+        const int32_t r = row0 + tid, m = r / per_seq, in = r - m * per_seq, rb = b_first + m;
+        int32_t at = -1, pos = 0x7fffffff, from = 0;
+        if (r < rows_total) {
+          const int32_t c = a.cache_len[rb], n = a.n_drafts[rb], j = in / G;
+          if (cache_lengths_ok(a, c, n) && j < n && c >= cache) {
+            at = (rb * a.D_max + j) * a.Hq + g * G + (in - j * G);
+            pos = cache_flat_pos(a, rb, c, j);
+            if (a.key_start != nullptr) from = min(cache, max(0, a.key_start[rb]));
+            least = rb;
+          }
+        }
+        sh.at[tid] = at;
+        sh.pos[tid] = pos;
+        sh.start[tid] = from;
+        least = __reduce_min_sync(0xffffffffu, least);
+        if (lane == 0) sh.least[warp] = least;
+      }
+      __syncthreads();
+      // the first of the tile's sequences names the blocks
+      b = min(min(sh.least[0], sh.least[1]), min(sh.least[2], sh.least[3]));
+      if (b == 0x7fffffff) return;
     }
-    b = __reduce_min_sync(0xffffffffu, least);
-    if (b == 0x7fffffff) return;
   }
   int32_t t_lo = 0, t_hi = tiles;
   if (parts > 1) {
@@ -374,14 +386,23 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
   // Q as two terms, two threads a row, the row scaled to [128, 256) (rows behind the last
   // one stay what they were: they reach no other row)
 #pragma unroll 1
-  for (int32_t q_row = tid >> 1; !stages && q_row < kBM && row0 + (q_row & ~15) < rows_total;
-       q_row += 64) {
+  for (int32_t q_row = tid >> 1; (kShared || !stages) && q_row < kBM && row0 + (q_row & ~15) < rows_total;
+       q_row += kShared ? 128 : 64) {
     const int32_t half = tid & 1;
-    int32_t rb, j, h;
-    const bool live = row_of(row0 + q_row, rb, j, h);
-    const uint4* src = reinterpret_cast<const uint4*>(
-                           static_cast<const __nv_bfloat16*>(a.q) +
-                           (((int64_t)rb * a.D_max + j) * a.Hq + h) * D) + half * (D / 16);
+    int32_t at = -1;
+    bool live;
+    if (stacked) {
+      if constexpr (kShared) at = sh.at[q_row];
+      live = at >= 0;
+    } else {
+      const int32_t r = row0 + q_row;
+      live = r < rows_total;
+      const int32_t j = live ? r / G : 0;
+      at = (b * a.D_max + j) * a.Hq + g * G + (live ? r - j * G : 0);
+    }
+    const uint4* src =
+        reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.q) + (int64_t)at * D) +
+        half * (D / 16);
     uint4 w[D / 16];
     float m = 0.f;
 #pragma unroll
@@ -577,19 +598,22 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
     // ------------------------------------------------------------- softmax
     take_registers();
     const uint32_t lane_off = (uint32_t)(warp * 32) << 16;
-    int32_t rb, j, h;
-    const bool row_live = row_of(row0 + tid, rb, j, h);
-    const bool warp_live = stacked ? __any_sync(0xffffffffu, row_live) : row0 + warp * 32 < rows_total;
+    // a row's place among the batch's, its position and its first visible key
+    int32_t orow = -1, qpos = 0x7fffffff, row_start = 0;
+    bool warp_live = row0 + warp * 32 < rows_total;
     const float rowc = sh.rowc[tid];
-    int32_t qpos = 0x7fffffff, row_start = 0;
     auto flat_of = [&](int32_t i) { return staged ? s_flat[i] : cache_flat_pos(a, b, cache, i); };
-    if (row_live) {
-      if (stacked) {
-        qpos = cache_flat_pos(a, rb, a.cache_len[rb], j);
-        if (a.key_start != nullptr) row_start = min(Lk, max(0, a.key_start[rb]));
-      } else {
-        qpos = flat_of(j);
+    if (stacked) {
+      if constexpr (kShared) {
+        orow = sh.at[tid];
+        qpos = sh.pos[tid];
+        row_start = sh.start[tid];
       }
+      warp_live = __any_sync(0xffffffffu, orow >= 0);
+    } else if (row0 + tid < rows_total) {
+      const int32_t r = row0 + tid, j = r / G;
+      orow = (b * a.D_max + j) * a.Hq + g * G + (r - j * G);
+      qpos = flat_of(j);
     }
     // keys below this one are hidden from some row of the warp
     const int32_t hide_to = stacked ? __reduce_max_sync(0xffffffffu, row_start) : start;
@@ -724,21 +748,19 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
     if (ok) ok = wait_warp(&sh.pv_done[(ntiles - 1) & 1], ((ntiles - 1) >> 1) & 1, a.status);
     tc_fence_after();
     if (ok && warp_live) {
-      const int64_t orow = ((int64_t)rb * a.D_max + j) * a.Hq + h;
       const bool direct = !kShared && parts == 1;
-      const int64_t prow = orow * splits + split;
       float* part_o = stacked ? L.s_part_o : L.part_o;
       float2* part_ml = stacked ? L.s_part_ml : L.part_ml;
-      const bool store = row_live && (direct ? dbg_in(orow, (int64_t)a.B * a.D_max * a.Hq, a.status)
-                                             : dbg_in(prow, (int64_t)a.B * a.D_max * a.Hq * splits, a.status));
-      const float inv = v_ref / l_run;
+      const int64_t room = (int64_t)a.B * a.D_max * a.Hq;
+      if (orow >= 0 && !dbg_in(orow, room, a.status)) orow = -1;
+      if (direct) {
+        const float inv = v_ref / l_run;
 #pragma unroll 1
-      for (int c = 0; c < D / 32; ++c) {
-        float ov[32];
-        tmem_ld32(tO + lane_off + c * 32, ov);
-        if (!store) continue;
-        if (direct) {
-          uint4* ob = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(a.o) + orow * D + c * 32);
+        for (int c = 0; c < D / 32; ++c) {
+          float ov[32];
+          tmem_ld32(tO + lane_off + c * 32, ov);
+          if (orow < 0) continue;
+          uint4* ob = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(a.o) + (int64_t)orow * D + c * 32);
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             float x[8];
@@ -747,18 +769,36 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
             ob[i] = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]),
                                pack_bf16x2(x[6], x[7]));
           }
-        } else {
-          float4* po = reinterpret_cast<float4*>(part_o + prow * D + c * 32);
+        }
+        if (orow >= 0 && a.lse != nullptr) {
+          const int32_t bj = orow / a.Hq, h = orow - bj * a.Hq;
+          a.lse[((int64_t)b * a.Hq + h) * a.D_max + (bj - b * a.D_max)] = row_lse(m_run, l_run);
+        }
+      } else {
+        // 32 columns of the warp's rows at a time, turned round where Q was (its products are done):
+        // a store covers 128 bytes of four rows instead of 16 of 32
+        constexpr int kPitch = 36;
+        float* st = reinterpret_cast<float*>(sQ) + warp * 32 * kPitch;
+        const int r8 = lane >> 3, c4 = (lane & 7) * 4;
+#pragma unroll 1
+        for (int c = 0; c < D / 32; ++c) {
+          float ov[32];
+          tmem_ld32(tO + lane_off + c * 32, ov);
 #pragma unroll
           for (int i = 0; i < 8; ++i)
-            po[i] = make_float4(ov[4 * i] * v_ref, ov[4 * i + 1] * v_ref, ov[4 * i + 2] * v_ref,
-                                ov[4 * i + 3] * v_ref);
+            *reinterpret_cast<float4*>(st + lane * kPitch + 4 * i) = make_float4(
+                ov[4 * i] * v_ref, ov[4 * i + 1] * v_ref, ov[4 * i + 2] * v_ref, ov[4 * i + 3] * v_ref);
+          __syncwarp();
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const int32_t to = __shfl_sync(0xffffffffu, orow, i * 4 + r8);
+            const float4 x = *reinterpret_cast<const float4*>(st + (i * 4 + r8) * kPitch + c4);
+            if (to >= 0)
+              *reinterpret_cast<float4*>(part_o + ((int64_t)to * splits + split) * D + c * 32 + c4) = x;
+          }
+          __syncwarp();
         }
-      }
-      if (store) {
-        if (!direct) part_ml[prow] = make_float2(m_run, l_run);
-        else if (a.lse != nullptr)
-          a.lse[((int64_t)b * a.Hq + h) * a.D_max + j] = row_lse(m_run, l_run);
+        if (orow >= 0) part_ml[(int64_t)orow * splits + split] = make_float2(m_run, l_run);
       }
     }
   }
@@ -792,7 +832,7 @@ cudaError_t launch(const CacheAttnArgs& a, const CacheAttnLaunch& L, bool own, c
   if (!cache_map(&tk, a.cache.k, rows, box, D) || !cache_map(&tv, a.cache.v, rows, box, D))
     return cudaErrorInvalidValue;
   auto smem = [](int32_t blocks, int32_t drafts) {
-    return 1024 + 2 * q_bytes(D) + (kNK + kNV) * tile_bytes(D) + 2 * wide_bytes(D) + sizeof(Shared) +
+    return 1024 + 2 * q_bytes(D) + (kNK + kNV) * tile_bytes(D) + 2 * wide_bytes(D) + sizeof(Shared<kShared>) +
            (size_t)blocks * 16 + (size_t)drafts * 4;
   };
   // (a part has at most a tile more than kMaxPartTiles)

@@ -331,15 +331,17 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
   }
   int32_t t_lo = 0, t_hi = tiles;
   if (parts > 1) {
-    t_lo = (int32_t)((int64_t)tiles * split / parts);
-    t_hi = (int32_t)((int64_t)tiles * (split + 1) / parts);
+    // tiles * split / parts and the next, without 64 bits
+    const uint32_t q = (uint32_t)tiles / (uint32_t)parts, r = (uint32_t)tiles - q * parts;
+    t_lo = (int32_t)(q * split + r * split / (uint32_t)parts);
+    t_hi = (int32_t)(q * (split + 1) + r * (split + 1) / (uint32_t)parts);
   }
   const int32_t k_lo = base + t_lo * KT, k_hi = min(Lk, base + t_hi * KT), ntiles = t_hi - t_lo;
   const int32_t start = a.key_start != nullptr && !stacked ? min(Lk, max(0, a.key_start[b])) : 0;
   const int32_t b_lo = k_lo >> S_log, nb = ((k_hi - 1) >> S_log) + 1 - b_lo;
 
   // ---- set-up
-  if (tid == 0) {
+  if (tid == 128) {
     for (int i = 0; i < kNK; ++i) {
       mbar_init(&sh.k_full[i], 1);
       mbar_init(&sh.k_empty[i], 1);
@@ -356,6 +358,7 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
     }
     fence_barrier_init();
   }
+  __syncwarp();
   if (warp == 7) {
     tmem_alloc(&sh.tmem, kCols);
     tmem_relinquish();
@@ -383,6 +386,18 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
       if (staged) s_flat[j] = p;
     }
   }
+  // The copies of a tile's K or V, by one lane of warp 4.  (Blocks behind the last key are not copied:
+  // their rows stay what they were.)
+  auto copy = [&](unsigned char* dst, const CUtensorMap* map, uint64_t* full, int32_t t, uint64_t pol) {
+    const int32_t c0 = k_lo + t * KT, n = min(KT, k_hi - c0), rows = min(S, KT);
+    mbar_arrive_expect_tx(full, (uint32_t)((n + rows - 1) / rows * rows * D));
+#pragma unroll 1
+    for (int32_t k = 0; k < n; k += rows) {
+      const int32_t id = max(__float_as_int(s_blk[((c0 + k) >> S_log) - b_lo].w), 0);
+      const int32_t row = (id * Hkv + g) * S + ((c0 + k) & (S - 1));
+      tma_load_2d(dst + k * D, map, 0, row, full, pol);
+    }
+  };
   // Q as two terms, two threads a row, the row scaled to [128, 256) (rows behind the last
   // one stay what they were: they reach no other row)
 #pragma unroll 1
@@ -390,16 +405,13 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
        q_row += kShared ? 128 : 64) {
     const int32_t half = tid & 1;
     int32_t at = -1;
-    bool live;
     if (stacked) {
       if constexpr (kShared) at = sh.at[q_row];
-      live = at >= 0;
-    } else {
-      const int32_t r = row0 + q_row;
-      live = r < rows_total;
-      const int32_t j = live ? r / G : 0;
-      at = (b * a.D_max + j) * a.Hq + g * G + (live ? r - j * G : 0);
+    } else if (row0 + q_row < rows_total) {
+      const int32_t r = row0 + q_row, j = r / G;
+      at = (b * a.D_max + j) * a.Hq + g * G + (r - j * G);
     }
+    const bool live = at >= 0;
     const uint4* src =
         reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.q) + (int64_t)at * D) +
         half * (D / 16);
@@ -465,34 +477,19 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
     give_registers();
     const bool leader = elect_one();
     const uint64_t pol = policy_evict_first();
-    const int32_t rows = min(S, KT);
     bool ok = true;
     int32_t t = 0, nk = 0, nv = 0;  // tiles; K and V copies issued
 #pragma unroll 1
     for (; t < ntiles && ok; ++t) {
-      const int32_t c0 = k_lo + t * KT;
-      // (blocks behind the last key are not copied: their rows stay what they were)
-      const int32_t n = min(KT, k_hi - c0);
-      const uint32_t bytes = (uint32_t)((n + rows - 1) / rows * rows * D);
-      auto copy = [&](unsigned char* dst, const CUtensorMap* map, uint64_t* full) {
-        if (leader) {
-          mbar_arrive_expect_tx(full, bytes);
-#pragma unroll 1
-          for (int32_t k = 0; k < n; k += rows) {
-            const int32_t id = max(__float_as_int(s_blk[((c0 + k) >> S_log) - b_lo].w), 0);
-            const int32_t row = (id * Hkv + g) * S + ((c0 + k) & (S - 1));
-            tma_load_2d(dst + k * D, map, 0, row, full, pol);
-          }
-        }
-        __syncwarp();
-      };
       if (t >= kNK) ok = wait_warp(&sh.k_empty[t % kNK], ((t / kNK) - 1) & 1, a.status);
       if (!ok) break;
-      copy(sK + t % kNK * kTileBytes, &tmK, &sh.k_full[t % kNK]);
+      if (leader) copy(sK + t % kNK * kTileBytes, &tmK, &sh.k_full[t % kNK], t, pol);
+      __syncwarp();
       nk = t + 1;
       if (t >= kNV) ok = wait_warp(&sh.v_empty[t % kNV], ((t / kNV) - 1) & 1, a.status);
       if (!ok) break;
-      copy(sV + t % kNV * kTileBytes, &tmV, &sh.v_full[t % kNV]);
+      if (leader) copy(sV + t % kNV * kTileBytes, &tmV, &sh.v_full[t % kNV], t, pol);
+      __syncwarp();
       nv = t + 1;
     }
     // after a wait that gave up, the copies in flight still land here
@@ -775,29 +772,23 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
           a.lse[((int64_t)b * a.Hq + h) * a.D_max + (bj - b * a.D_max)] = row_lse(m_run, l_run);
         }
       } else {
-        // 32 columns of the warp's rows at a time, turned round where Q was (its products are done):
-        // a store covers 128 bytes of four rows instead of 16 of 32
-        constexpr int kPitch = 36;
-        float* st = reinterpret_cast<float*>(sQ) + warp * 32 * kPitch;
-        const int r8 = lane >> 3, c4 = (lane & 7) * 4;
+        // A row to shared memory (where Q, K and V were: their products are done), and from there by a
+        // bulk copy of its own: a thread's own stores would be 16 bytes in each of 32 rows.
+        constexpr int kPitch = D + 4;  // floats (rows start four banks apart)
+        static_assert(kBM * kPitch * 4 <= 2 * kQBytes + (kNK + kNV) * kTileBytes + 2 * kWideBytes, "room");
+        float* st = reinterpret_cast<float*>(smem) + tid * kPitch;
 #pragma unroll 1
         for (int c = 0; c < D / 32; ++c) {
           float ov[32];
           tmem_ld32(tO + lane_off + c * 32, ov);
 #pragma unroll
           for (int i = 0; i < 8; ++i)
-            *reinterpret_cast<float4*>(st + lane * kPitch + 4 * i) = make_float4(
+            *reinterpret_cast<float4*>(st + c * 32 + 4 * i) = make_float4(
                 ov[4 * i] * v_ref, ov[4 * i + 1] * v_ref, ov[4 * i + 2] * v_ref, ov[4 * i + 3] * v_ref);
-          __syncwarp();
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const int32_t to = __shfl_sync(0xffffffffu, orow, i * 4 + r8);
-            const float4 x = *reinterpret_cast<const float4*>(st + (i * 4 + r8) * kPitch + c4);
-            if (to >= 0)
-              *reinterpret_cast<float4*>(part_o + ((int64_t)to * splits + split) * D + c * 32 + c4) = x;
-          }
-          __syncwarp();
         }
+        fence_proxy_async_shared();
+        if (orow >= 0) bulk_s2g(part_o + ((int64_t)orow * splits + split) * D, smem_u32(st), D * 4);
+        bulk_s2g_wait();
         if (orow >= 0) part_ml[(int64_t)orow * splits + split] = make_float2(m_run, l_run);
       }
     }

@@ -201,6 +201,17 @@ __device__ __forceinline__ void bulk_g2s_at(uint32_t smem_dst, const void* gmem_
       : "memory");
 }
 
+// The other way, and the wait until what this thread asked for has been read.
+__device__ __forceinline__ void bulk_s2g(void* gmem_dst, uint32_t smem_src, uint32_t bytes) {
+  asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(gmem_dst),
+               "r"(smem_src), "r"(bytes)
+               : "memory");
+}
+__device__ __forceinline__ void bulk_s2g_wait() {
+  asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+  asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+}
+
 // L2 policy: data streamed once (K/V tiles, logit rows).
 __device__ __forceinline__ uint64_t policy_evict_first() {
   uint64_t pol;

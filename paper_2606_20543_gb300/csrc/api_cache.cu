@@ -264,7 +264,7 @@ ssd_status ssd_cache_attention_shared(const ssd_grid* grid, const ssd_block_cach
                                       void* workspace, size_t workspace_bytes, int32_t* status,
                                       ssd_stream_t stream) {
   if (groups <= 0 || max_shared < 0 || max_shared > max_blocks) return SSD_ERR_SHAPE;
-  if (groups > 65535) return SSD_ERR_UNSUPPORTED;
+  if (groups > 65535 || Hq > 65535 * 8) return SSD_ERR_UNSUPPORTED;
   if (B > 0 && (group_start == nullptr || shared == nullptr)) return SSD_ERR_INVALID_ARG;
   return attention(grid, cache, B, groups, group_start, shared, max_shared, Hq, cache_len, n_drafts,
                    draft_pos, key_start, D_max, block_table, max_blocks, q, scale, o, lse, workspace,

@@ -138,7 +138,10 @@ cache_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
   if (!kShared) pdl_wait();
 
   const int32_t tid = threadIdx.x, lane = tid & 31, warp = (int32_t)warp_uniform(tid >> 5);
-  const int32_t g = blockIdx.y, S = a.cache.block, S_log = 31 - __clz(S), G = a.Hq / a.cache.Hkv;
+  // (kShared: a sequence's heads one after the other, the longest sequences first)
+  const int32_t cta = kShared ? blockIdx.x + blockIdx.y * gridDim.x : 0;
+  const int32_t x_cta = kShared ? cta / a.cache.Hkv : blockIdx.x;
+  const int32_t g = kShared ? cta - x_cta * a.cache.Hkv : blockIdx.y, S = a.cache.block, S_log = 31 - __clz(S), G = a.Hq / a.cache.Hkv;
   const bool first_of = g == 0 && blockIdx.z == 0;
   if (lane == 0) {
     for (int t = 0; t < kStages; ++t) mbar_init(&s_full[warp][t], 1);
@@ -146,7 +149,7 @@ cache_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
   }
   uint32_t stage = 0, phase = 0;  // of the warp's next step
   CacheWork<kShared> work;
-  bool more = work.first(a, L, blockIdx.x, first_of && tid < 32);
+  bool more = work.first(a, L, x_cta, first_of && tid < 32);
 #pragma unroll 1
   for (; more; more = work.next(a)) {
     // (the rows of the part before have left the ring's place, and the copies may know it)
@@ -157,8 +160,8 @@ cache_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
     const int32_t Lk = cache + nd, rows_total = nd * G;
     const int32_t row0 = blockIdx.z * RW;
     if (L.info != nullptr && first_of && tid == 0) {
-      if (work.t_lo == 0) L.info[b].x = blockIdx.x;
-      if (work.t_hi == work.tiles) L.info[b].y = blockIdx.x;
+      if (work.t_lo == 0) L.info[b].x = x_cta;
+      if (work.t_hi == work.tiles) L.info[b].y = x_cta;
     }
     if (row0 >= rows_total) continue;
     const bool whole = !kShared && work.t_lo == 0 && work.t_hi == work.tiles, begins = work.t_lo == 0;
@@ -523,7 +526,7 @@ cache_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
       } else {
         // (a CTA leaves a share of several sequences, but of neighbours: slot x + b)
         const int64_t slots = L.per_head + a.B;
-        const int64_t at = (((int64_t)g * L.row_groups + blockIdx.z) * slots + blockIdx.x + b) * RW + r;
+        const int64_t at = (((int64_t)g * L.row_groups + blockIdx.z) * slots + x_cta + b) * RW + r;
         if (!dbg_in(at, (int64_t)a.cache.Hkv * L.row_groups * slots * RW, a.status)) continue;
         float* po = L.part_o + at * D + lane * PER;
 #pragma unroll

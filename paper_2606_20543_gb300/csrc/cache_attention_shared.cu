@@ -62,98 +62,107 @@ size_t part_bytes(int64_t rows, int32_t d) {
   return align256((size_t)rows * d * sizeof(float)) + align256((size_t)rows * sizeof(float2));
 }
 
-constexpr int kTogether = 8;
+constexpr int kTogether = 4;
 template <int N>
 struct alignas(4 * N) Lanes {
   float x[N];
 };
 
 // One warp per (sequence, draft, head): the parts of its row over the shared keys and over its own.
+// CTA: a draft, eight heads.  What bounds it is the chain from the lengths over the parts' places to
+// their rows, and its code, which is fetched cold: no division of 64 bits, four parts at a time (26 KB
+// of code took 3.3 us for a row, this 2).
 template <int D>
 __global__ void __launch_bounds__(256) cache_attn_join_kernel(CacheAttnArgs a, CacheAttnLaunch L) {
   constexpr int PER = D / 32;
   pdl_wait();
   const int32_t lane = threadIdx.x & 31;
-  if (blockIdx.x == 0) {  // (groups that are none of the batch's: nothing else looks at all of them)
+  if (blockIdx.x == 0 && blockIdx.y == 0) {  // (nothing else looks at all of the groups)
     bool bad = false;
     for (int32_t g = threadIdx.x; g < a.groups; g += blockDim.x)
       bad |= a.group_start[g] > a.group_start[g + 1];
     if (threadIdx.x == 0) bad |= a.group_start[0] != 0 || a.group_start[a.groups] != a.B;
     if (bad) record_status(a.status, SSD_ERR_DEVICE_BOUNDS);
   }
-  const int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
-  if (row >= (int64_t)a.B * a.D_max * a.Hq) return;
-  const int32_t h = (int32_t)(row % a.Hq);
-  const int64_t bj = row / a.Hq;
-  const int32_t b = (int32_t)(bj / a.D_max), j = (int32_t)(bj - (int64_t)b * a.D_max);
+  const int32_t h = blockIdx.y * 8 + (threadIdx.x >> 5);
+  if (h >= a.Hq) return;
+  const int32_t b = (int32_t)(blockIdx.x / (uint32_t)a.D_max), j = blockIdx.x - b * a.D_max;
   const int32_t cache = a.cache_len[b], nd = a.n_drafts[b];
   const int2 cut = L.info != nullptr ? L.info[b] : make_int2(0, 0);
+  const CacheGroup group = cache_group_warp(a, b);
   if (!cache_lengths_ok(a, cache, nd) || j >= nd) return;
-  const int32_t base = cache_base_warp(a, b, cache);
+  const int32_t base = group.base(a, b, cache);
   if (base < 0) return;
+  const int64_t row = (int64_t)blockIdx.x * a.Hq + h;
   const int32_t shared_tiles = (base + kCacheTile - 1) / kCacheTile;
   const int32_t n_shared = shared_tiles > 0 ? cache_parts(L.s_splits, L.s_min_tiles, shared_tiles) : 0;
-  int32_t n_own;
-  int64_t at, step = 1, room;
+  int32_t n_own, step = 1;
+  int64_t at;
   if (L.info != nullptr) {
     const int32_t G = a.Hq / a.cache.Hkv, g = h / G;
     const CacheShares x = cache_shares(L, a.B, b, cut, g, j * G + (h - g * G));
     n_own = x.parts;
     step = L.group_rows;
     at = x.at;
-    room = (int64_t)a.cache.Hkv * L.row_groups * (L.per_head + a.B) * step;
+    if (!dbg_in(at + (n_own - 1) * step, (int64_t)a.cache.Hkv * L.row_groups * (L.per_head + a.B) * step,
+                a.status))
+      return;
   } else {
     n_own = cache_parts(L.splits, L.min_tiles, (cache + nd - base + kCacheTile - 1) / kCacheTile);
     at = row * L.splits;
-    room = (int64_t)a.B * a.D_max * a.Hq * L.splits;
   }
   if (n_own <= 0) return;  // (a wait gave up: no part is known)
-  if (!dbg_in(at + (n_own - 1) * step, room, a.status)) return;
   const int32_t parts = n_shared + n_own;
+  const int64_t s_at = row * L.s_splits, own_at = at - (int64_t)n_shared * step;
   auto ml_of = [&](int32_t s) {
-    return s < n_shared ? L.s_part_ml[row * L.s_splits + s] : L.part_ml[at + (s - n_shared) * step];
+    return s < n_shared ? L.s_part_ml[s_at + s] : L.part_ml[own_at + (int64_t)s * step];
   };
-  float M = -INFINITY;
-  for (int32_t s = lane; s < parts; s += 32) M = fmaxf(M, ml_of(s).x);
+  // The first parts' rows are asked for together with the factors of all.
+  Lanes<PER> v[kTogether], acc;
+  auto rows_of = [&](int32_t i0) {
+#pragma unroll
+    for (int i = 0; i < kTogether; ++i) {
+      const int32_t s = min(i0 + i, parts - 1);
+      const float* p = s < n_shared ? L.s_part_o + (s_at + s) * D : L.part_o + (own_at + (int64_t)s * step) * D;
+      v[i] = *reinterpret_cast<const Lanes<PER>*>(p + lane * PER);
+    }
+  };
+  rows_of(0);
+  const float2 first = lane < parts ? ml_of(lane) : make_float2(-INFINITY, 0.f);
+  float M = first.x;
+#pragma unroll 1
+  for (int32_t s = 32 + lane; s < parts; s += 32) M = fmaxf(M, ml_of(s).x);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
-  Lanes<PER> acc;
 #pragma unroll
   for (int k = 0; k < PER; ++k) acc.x[k] = 0.f;
-  float sum = 0.f;
-  for (int32_t s0 = 0; s0 < parts; s0 += 32) {
-    float mine = 0.f;  // the factor of part s0 + lane
-    if (s0 + lane < parts) {
-      const float2 x = ml_of(s0 + lane);
+  float sum = 0.f, mine = 0.f;  // the factor of part (s0 & ~31) + lane
+#pragma unroll 1
+  for (int32_t s0 = 0; s0 < parts; s0 += kTogether) {
+    if ((s0 & 31) == 0) {
+      const float2 x = s0 == 0 ? first : s0 + lane < parts ? ml_of(s0 + lane) : make_float2(-INFINITY, 0.f);
       mine = x.x == -INFINITY ? 0.f : exp2f(x.x - M);
       sum += x.y * mine;
     }
-    const int32_t n = min(32, parts - s0);
-    for (int32_t i0 = 0; i0 < n; i0 += kTogether) {  // kTogether parts are asked for at once
-      Lanes<PER> v[kTogether];
+    if (s0 > 0) rows_of(s0);
 #pragma unroll
-      for (int i = 0; i < kTogether; ++i) {
-        const int32_t s = s0 + min(i0 + i, n - 1);
-        v[i] = *reinterpret_cast<const Lanes<PER>*>(
-            (s < n_shared ? L.s_part_o + (row * L.s_splits + s) * D
-                          : L.part_o + (at + (s - n_shared) * step) * D) + lane * PER);
-      }
+    for (int i = 0; i < kTogether; ++i) {
+      const float f = __shfl_sync(0xffffffffu, mine, (s0 + i) & 31);
+      if (s0 + i >= parts || f == 0.f) continue;
 #pragma unroll
-      for (int i = 0; i < kTogether; ++i) {
-        const float f = i0 + i < n ? __shfl_sync(0xffffffffu, mine, min(i0 + i, 31)) : 0.f;
-#pragma unroll
-        for (int k = 0; k < PER; ++k) acc.x[k] = f == 0.f ? acc.x[k] : acc.x[k] + v[i].x[k] * f;
-      }
+      for (int k = 0; k < PER; ++k) acc.x[k] += v[i].x[k] * f;
     }
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
   const float inv = 1.f / sum;
-  __nv_bfloat16* ob = static_cast<__nv_bfloat16*>(a.o) + row * D + lane * PER;
+  uint32_t w[PER / 2];
 #pragma unroll
   for (int k = 0; k < PER; k += 2)
-    *reinterpret_cast<uint32_t*>(ob + k) =
-        pack_bf16x2(row_value(acc.x[k], inv, sum), row_value(acc.x[k + 1], inv, sum));
+    w[k / 2] = pack_bf16x2(row_value(acc.x[k], inv, sum), row_value(acc.x[k + 1], inv, sum));
+  uint32_t* ob = reinterpret_cast<uint32_t*>(static_cast<__nv_bfloat16*>(a.o) + row * D + lane * PER);
+  if constexpr (PER == 4) *reinterpret_cast<uint2*>(ob) = make_uint2(w[0], w[1]);
+  else ob[0] = w[0];
   if (a.lse != nullptr && lane == 0) a.lse[((int64_t)b * a.Hq + h) * a.D_max + j] = row_lse(M, sum);
 }
 
@@ -204,7 +213,7 @@ cudaError_t launch_cache_attention_shared(const CacheAttnArgs& a, void* ws, cuda
     e = launch_cache_attention_mma(a, p.mma, L, stream);
     if (e != cudaSuccess) return e;
   }
-  const dim3 grid((unsigned)(((int64_t)a.B * a.D_max * a.Hq + 7) / 8));
+  const dim3 grid((unsigned)(a.B * a.D_max), (unsigned)((a.Hq + 7) / 8));
   return launch_kernel(d == 128 ? cache_attn_join_kernel<128> : cache_attn_join_kernel<64>, grid, dim3(256),
                        0, stream, true, a, L);
 }

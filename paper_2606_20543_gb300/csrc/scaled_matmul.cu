@@ -8,8 +8,8 @@
 // cores work on the next blocks in other buffers.
 //
 // More than 64 rows: the rows of A are the 128 lanes of a tile (the scales of a block are then one
-// number a thread), 128 rows of W its columns, or 256 over a CTA pair (cta_group::2) with 128 lanes
-// each.  Up to 64 rows: the other way round (scaled_matmul_few_kernel).
+// number a thread), 128 rows of W its columns; or a CTA pair (cta_group::2) has 128 lanes each and 128
+// or 256 columns.  Up to 64 rows: the other way round (scaled_matmul_few_kernel).
 //
 // Barriers count units of U blocks: a wait that is satisfied already costs a warp about 100
 // cycles, a commit of products as much.
@@ -943,15 +943,19 @@ cudaError_t launch_scaled_matmul(const ScaledMatmulArgs& a, cudaStream_t stream)
   if (a.M <= 16) return launch_few<16, 2>(a, stream);
   if (a.M <= 32) return launch_few<32, 2>(a, stream);
   if (a.M <= 64) return launch_few<64, 2>(a, stream);
-  // cycles of a wave of tiles, about: what a block takes and a tile's way in and out
+  // Nanoseconds of a wave of tiles, about: what a block takes, and a tile's way in and out.  Tiles of a
+  // pair are better for their size and worse where they leave SMs idle.  Measured (us, 256 x 256
+  // and 256 x 128 of a pair, 128 x 128): 1024 x 4096 x 4096 21.9, 25.1, 28.0; 500 x 2000 x 4096 21.3,
+  // 14.3, 15.4; 300 x 5000 x 4096 21.7, 25.0, 16.0; 2000 x 3000 x 4096 40.2, 35.8, 38.3.
   const int64_t blocks = ceil_div(a.K, kGroup), sms = device_sm_count();
   auto cost = [&](int32_t rows, int32_t cols, int64_t places, int64_t block, int64_t rest) {
     const int64_t tiles = (int64_t)ceil_div(a.M, rows) * ceil_div(a.N, cols);
     return ceil_div(tiles, places) * (blocks * block + rest);
   };
-  if (cost(256, 256, sms / 2, 900, 6000) < cost(128, 128, sms, 550, 5000))
-    return launch<true, 256, 1>(a, stream);
-  return launch<false, 128, 2>(a, stream);
+  const int64_t c256 = cost(256, 256, sms / 2, 500, 5500), p128 = cost(256, 128, sms / 2, 315, 4000),
+                c128 = cost(128, 128, sms, 360, 3500);
+  if (c256 < p128 && c256 < c128) return launch<true, 256, 1>(a, stream);
+  return p128 <= c128 ? launch<true, 128, 2>(a, stream) : launch<false, 128, 2>(a, stream);
 }
 
 }  // namespace ssd

@@ -10,8 +10,9 @@ from __future__ import annotations
 import torch
 
 from . import (Grid, Rng, Sampling, cache as make_cache, rotary as make_rotary,
-               ssd_cache_append, ssd_cache_attention, ssd_cache_attention_workspace,
-               ssd_cache_plan, ssd_rotary_table, ssd_sample)
+               ssd_cache_append, ssd_cache_append_norm, ssd_cache_attention,
+               ssd_cache_attention_shared, ssd_cache_attention_shared_workspace,
+               ssd_cache_attention_workspace, ssd_cache_plan, ssd_rotary_table, ssd_sample)
 
 
 def _row_stride(x):
@@ -36,7 +37,11 @@ class PagedDecode:
     says so) is left out of the pass, on the device: n_new is 0, it attends to nothing, its rows of
     o hold what they held and it does not advance.
     ``release(mask)`` gives the blocks of finished sequences back; their next
-    pass starts at length 0."""
+    pass starts at length 0.
+
+    Sequences of one prompt hold its blocks once: after the pass that caches the prompt of the first
+    of each group, ``share(group_start, blocks)`` gives those blocks to the others, and attend()
+    reads them once a group."""
 
     def __init__(self, grid: Grid, B, Hq, Hkv, d, num_blocks, block, max_blocks, N_max, freq,
                  sections, interleaved=False, layers=1, device="cuda"):
@@ -78,13 +83,51 @@ class PagedDecode:
         self.prob, self.kept = new((B * N_max,), torch.float32), new((B * N_max,), torch.int32)
         self.status = new((1,), torch.int32)
         self._ws = {}
+        # groups that share blocks: of every group its blocks and their ids, of every sequence its group
+        self.groups, self.max_shared = 0, 0
 
     def _workspace(self, N):
         if N not in self._ws:
-            n = ssd_cache_attention_workspace(self.B, self.Hq, self.Hkv, self.d, N,
-                                              self.max_blocks * self.block)
+            sizes = (self.Hq, self.Hkv, self.d, N, self.max_blocks * self.block)
+            n = (ssd_cache_attention_shared_workspace(self.B, self.groups, *sizes, self.max_shared * self.block)
+                 if self.groups else ssd_cache_attention_workspace(self.B, *sizes))
             self._ws[N] = torch.empty((max(n, 16),), dtype=torch.uint8, device=self.device), n
         return self._ws[N]
+
+    def share(self, group_start, blocks) -> None:
+        """Group g, the sequences group_start[g] <= b < group_start[g + 1], shares the first blocks[g]
+        blocks of its first sequence, which has cached them whole (0: none); the others, which hold
+        nothing, go on behind them, at length blocks[g] * block.  group_start: 0 ... B; host numbers
+        both.  Called between passes, not while an earlier group's blocks are held; a graph captured
+        before it attends without groups.  A sequence that is released can begin anew once all of
+        its group are (their shared blocks go back with the last of them)."""
+        start, blocks = [int(x) for x in group_start], [int(x) for x in blocks]
+        if len(start) != len(blocks) + 1 or start[0] != 0 or start[-1] != self.B or not blocks \
+                or any(a > b for a, b in zip(start, start[1:])):
+            raise ValueError("group_start: 0 ... B, ascending, one more than blocks")
+        if min(blocks) < 0 or max(blocks) > self.max_blocks:
+            raise ValueError("blocks: between 0 and max_blocks")
+        dev = self.device
+        self.groups, self.max_shared = len(blocks), max(blocks)
+        self.group_start = torch.tensor(start, dtype=torch.int32, device=dev)
+        self.shared = torch.tensor(blocks, dtype=torch.int32, device=dev)
+        sizes = [b - a for a, b in zip(start, start[1:])]
+        self._group = torch.repeat_interleave(torch.arange(self.groups, device=dev),
+                                              torch.tensor(sizes, device=dev))
+        first = torch.tensor([min(a, self.B - 1) for a in start[:-1]], device=dev)
+        firsts = torch.tensor([a for a, n in zip(start, sizes) if n > 0], device=dev)
+        self._shared_ids = self.block_table[first, :max(self.max_shared, 1)].clone()
+        self._shared_own = self.shared * torch.tensor([int(n > 0) for n in sizes], device=dev)
+        base, joins = self.shared[self._group], torch.ones((self.B,), dtype=torch.bool, device=dev)
+        joins[firsts] = False
+        joins &= base > 0
+        at = torch.arange(self._shared_ids.shape[1], device=dev)
+        take = joins[:, None] & (at[None] < base[:, None])
+        part = self.block_table[:, :at.numel()]
+        part.copy_(torch.where(take, self._shared_ids[self._group], part))
+        self.cache_len.copy_(torch.where(joins, base * self.block, self.cache_len))
+        self.held.copy_(torch.where(joins, base, self.held))
+        self._ws = {}
 
     def plan(self, n_new, N=None) -> None:
         """n_new int32 [B] (device), at most N (default N_max) each."""
@@ -101,14 +144,15 @@ class PagedDecode:
         torch.mul(want, self.slots.view(self.B, self.N)[:, 0] >= 0, out=self.n_new)  # (if served)
         self._workspace(self.N)  # (allocated here, not in the middle of a pass)
 
-    def attend(self, layer, q, k, v, draft_pos=None, key_start=None, scale=0.0):
+    def attend(self, layer, q, k, v, draft_pos=None, key_start=None, scale=0.0, norm=None):
         """q bf16 [B * N, Hq * d], k and v bf16 [B * N, Hkv * d]: row b * N + j is new
         token j of sequence b; rows may lie apart (slices of one projection's output).
         draft_pos int32 [B, N]: the new tokens are drafts of these grid indices (y * W + x),
         which give their rotary positions and what they see (without it: the next tokens of the
         flat sequence).  The drafts that advance() keeps become the tokens that follow, so those
         have to be the next ones, in order.  key_start int32 [B]: the first token of a sequence
-        that may be seen.  Returns o bf16 [B * N, Hq * d] (valid until the next
+        that may be seen.  norm: norms of the query and key heads before they are turned
+        (paper_2606_20543_gb300.head_norm).  Returns o bf16 [B * N, Hq * d] (valid until the next
         call; rows without a token hold what they held)."""
         rows, width = self.B * self.N, self.Hq * self.d
         for x, heads in ((q, self.Hq), (k, self.Hkv), (v, self.Hkv)):
@@ -124,13 +168,20 @@ class PagedDecode:
             pos = self._draft_pos[:rows]
             torch.index_select(self._grid_pos, 0, draft_pos.view(-1).clamp(-1, cells).add_(1), out=pos)
         q_rot, o = self._q[:rows * width], self._o[:rows * width]
-        ssd_cache_append(self.caches[layer], self.rotary, self.B, self.N, self.Hq, self.n_new,
-                         self.slots, pos, q, _row_stride(q), k, _row_stride(k), v, _row_stride(v),
-                         q_rot, self.status)
+        new = (self.B, self.N, self.Hq, self.n_new, self.slots, pos, q, _row_stride(q), k, _row_stride(k), v,
+               _row_stride(v), q_rot, self.status)
+        if norm is None:
+            ssd_cache_append(self.caches[layer], self.rotary, *new)
+        else:
+            ssd_cache_append_norm(self.caches[layer], self.rotary, norm, *new)
         ws, n = self._workspace(self.N)
-        ssd_cache_attention(self.g, self.caches[layer], self.B, self.Hq, self.cache_len, self.n_new,
-                            draft_pos, key_start, self.N, self.block_table, self.max_blocks, q_rot,
-                            scale, o, None, ws, n, self.status)
+        rest = (self.Hq, self.cache_len, self.n_new, draft_pos, key_start, self.N, self.block_table,
+                self.max_blocks, q_rot, scale, o, None, ws, n, self.status)
+        if self.groups:
+            ssd_cache_attention_shared(self.g, self.caches[layer], self.B, self.groups, self.group_start,
+                                       self.shared, self.max_shared, *rest)
+        else:
+            ssd_cache_attention(self.g, self.caches[layer], self.B, *rest)
         return o.view(rows, width)
 
     def sample(self, logits, settings: Sampling, rng: Rng):
@@ -149,14 +200,28 @@ class PagedDecode:
         self.held.copy_(self.n_blocks)
         self.head.copy_(self.next_head)
 
-    def release(self, mask) -> None:
-        """Blocks of the sequences with mask [B] (device, bool) go back to the ring."""
-        at = torch.arange(self.max_blocks, device=self.device)
-        own = mask[:, None] & (at[None] < self.held[:, None])
+    def _give_back(self, ids, own) -> None:
+        """Blocks ids[own] to the ring."""
         place = (self.tail + torch.cumsum(own.flatten(), 0) - 1) % self.num_blocks
         place = torch.where(own.flatten(), place, self.num_blocks)
-        self.ring.scatter_(0, place, self.block_table.flatten())
+        self.ring.scatter_(0, place, ids.flatten())
         self.tail.add_(own.sum())
+
+    def release(self, mask) -> None:
+        """Blocks of the sequences with mask [B] (device, bool) go back to the ring, those that a group
+        shares when none of it holds them any more."""
+        at = torch.arange(self.max_blocks, device=self.device)
+        own = mask[:, None] & (at[None] < self.held[:, None])
+        if self.groups:
+            own &= at[None] >= self.shared[self._group][:, None]
+        self._give_back(self.block_table, own)
         self.block_table.masked_fill_(mask[:, None], -1)
         self.cache_len.masked_fill_(mask, 0)
         self.held.masked_fill_(mask, 0)
+        if self.groups:
+            alive = torch.zeros_like(self.shared).index_add_(0, self._group, (self.held > 0).to(torch.int32))
+            done = (alive == 0) & (self._shared_own > 0)
+            here = done[:, None] & (at[None, :self._shared_ids.shape[1]] < self._shared_own[:, None])
+            self._give_back(self._shared_ids, here)
+            self._shared_own.masked_fill_(done, 0)
+            self.shared.masked_fill_(done, 0)

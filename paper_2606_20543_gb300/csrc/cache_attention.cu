@@ -160,8 +160,8 @@ cache_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
     const int32_t Lk = cache + nd, rows_total = nd * G;
     const int32_t row0 = blockIdx.z * RW;
     if (L.info != nullptr && first_of && tid == 0) {
-      if (work.t_lo == 0) L.info[b].x = x_cta;
-      if (work.t_hi == work.tiles) L.info[b].y = x_cta;
+      if (work.t_lo == 0) L.info[b].x = work.x;
+      if (work.t_hi == work.tiles) L.info[b].y = work.x;
     }
     if (row0 >= rows_total) continue;
     const bool whole = !kShared && work.t_lo == 0 && work.t_hi == work.tiles, begins = work.t_lo == 0;
@@ -526,7 +526,7 @@ cache_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
       } else {
         // (a CTA leaves a share of several sequences, but of neighbours: slot x + b)
         const int64_t slots = L.per_head + a.B;
-        const int64_t at = (((int64_t)g * L.row_groups + blockIdx.z) * slots + x_cta + b) * RW + r;
+        const int64_t at = (((int64_t)g * L.row_groups + blockIdx.z) * slots + work.x + b) * RW + r;
         if (!dbg_in(at, (int64_t)a.cache.Hkv * L.row_groups * slots * RW, a.status)) continue;
         float* po = L.part_o + at * D + lane * PER;
 #pragma unroll

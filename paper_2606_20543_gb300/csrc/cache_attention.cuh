@@ -152,6 +152,7 @@ constexpr int kCutFrom = 3;
 template <bool kShared>
 struct CacheWork {
   int32_t b, t_lo, t_hi, tiles;  // the part: tiles t_lo .. t_hi - 1 of the tiles of sequence b
+  int32_t x;  // the CTA's place: never falling from one sequence to the next, so that x + b is its own
   // the line: the CTA's tiles left, and where sequence b begins
   int64_t at, end, start;
 
@@ -244,10 +245,14 @@ struct CacheWork {
   // lengths.
   __device__ __forceinline__ bool first(const CacheAttnArgs& a, const CacheAttnLaunch& L, int32_t x,
                                         bool report) {
+    this->x = x;
     if (L.uniform > 0) {
       b = x / L.uniform;
       const int32_t split = x - b * L.uniform;
-      if (kShared && a.B <= 32 * kRanked) b = ranked(a, b);
+      if (kShared && a.B <= 32 * kRanked) {
+        b = ranked(a, b);
+        this->x = b * L.uniform + split;
+      }
       tiles = tiles_of(a, b, report && split == 0);
       const int32_t parts = (tiles + kWorkTiles - 1) / kWorkTiles;
       if (split >= parts) return false;

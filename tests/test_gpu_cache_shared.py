@@ -187,6 +187,16 @@ def test_many_sequences_and_groups(ssd, B, groups, D):
           wide=20000).check(ssd, rows=[0, D - 1])
 
 
+@pytest.mark.parametrize("B,Hq,Hkv,D", [(64, 16, 8, 1), (60, 8, 8, 2), (300, 4, 2, 1), (40, 24, 12, 3)])
+def test_more_sequences_than_places(ssd, B, Hq, Hkv, D):
+    """A CTA for every sequence and head, the longest first (up to 256 sequences)."""
+    rng = np.random.default_rng(B)
+    start = [0, 1, B // 3, B]
+    Batch(seed=B, start=start, shared=[2, 0, 11], own=rng.integers(0, 500, B).tolist(),
+          nd=rng.integers(0, D + 1, B).tolist(), D=D, Hq=Hq, Hkv=Hkv, d=64, block=16,
+          wide=0).check(ssd, rows=[0, D - 1])
+
+
 def test_small_work_takes_the_path_of_every_sequence_by_itself(ssd):
     kw = dict(seed=3, start=[0, 2, 4], shared=[12, 12], own=[10, 200, 77, 0], nd=[1] * 4, D=1, Hq=8, Hkv=8, d=64,
               block=16)

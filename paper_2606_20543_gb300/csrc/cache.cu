@@ -252,14 +252,25 @@ __device__ __forceinline__ void rotate16(bool interleaved, const float2 (&cs)[8]
   }
 }
 
-// Eight values times their gains plus their biases (null: 1 and 0).
+// Eight values times their gains plus their biases (null: 1 and 0).  kOnce: rounded once, for keys,
+// which e4m3 rounds again: every rounding before that moves a few keys more to a neighbour.
+template <bool kOnce>
 __device__ __forceinline__ void apply8(const float* gain, const float* bias, float (&x)[8]) {
+  const float4* g = reinterpret_cast<const float4*>(gain);
+  const float4* b = reinterpret_cast<const float4*>(bias);
+  if (kOnce && gain != nullptr && bias != nullptr) {
+    const float4 u = __ldg(g), v = __ldg(g + 1), s = __ldg(b), t = __ldg(b + 1);
+    x[0] = fmaf(x[0], u.x, s.x), x[1] = fmaf(x[1], u.y, s.y), x[2] = fmaf(x[2], u.z, s.z);
+    x[3] = fmaf(x[3], u.w, s.w), x[4] = fmaf(x[4], v.x, t.x), x[5] = fmaf(x[5], v.y, t.y);
+    x[6] = fmaf(x[6], v.z, t.z), x[7] = fmaf(x[7], v.w, t.w);
+    return;
+  }
   if (gain != nullptr) {
-    const float4 u = __ldg(reinterpret_cast<const float4*>(gain)), v = __ldg(reinterpret_cast<const float4*>(gain) + 1);
+    const float4 u = __ldg(g), v = __ldg(g + 1);
     x[0] *= u.x, x[1] *= u.y, x[2] *= u.z, x[3] *= u.w, x[4] *= v.x, x[5] *= v.y, x[6] *= v.z, x[7] *= v.w;
   }
   if (bias != nullptr) {
-    const float4 u = __ldg(reinterpret_cast<const float4*>(bias)), v = __ldg(reinterpret_cast<const float4*>(bias) + 1);
+    const float4 u = __ldg(b), v = __ldg(b + 1);
     x[0] += u.x, x[1] += u.y, x[2] += u.z, x[3] += u.w, x[4] += v.x, x[5] += v.y, x[6] += v.z, x[7] += v.w;
   }
 }
@@ -267,7 +278,7 @@ __device__ __forceinline__ void apply8(const float* gain, const float* bias, flo
 // mean (squares of the differences, so a large mean costs no digits); times gain plus bias.  In
 // float32, and not rounded before the rotation.  Called by all lanes of a head together, whatever
 // the warp's other lanes do.  `at`: of the thread's first value in the gains.
-template <int D, int kNorm>
+template <int D, int kNorm, bool kOnce>
 __device__ __forceinline__ void normalise16(float eps, const float* gain, const float* bias, int32_t at,
                                             float (&xa)[8], float (&xb)[8]) {
   constexpr int LPR = D / 16;
@@ -300,10 +311,10 @@ __device__ __forceinline__ void normalise16(float eps, const float* gain, const 
     s = ffma2(x, x, s);
     return x;
   });
-  const float r = rsqrtf(fmaf(sum(s), 1.f / D, eps));
+  const float r = __frsqrt_rn(fmaf(sum(s), 1.f / D, eps));
   each([&](float2 x) { return ffma2(x, make_float2(r, r), zero); });
-  apply8(gain != nullptr ? gain + at : nullptr, bias != nullptr ? bias + at : nullptr, xa);
-  apply8(gain != nullptr ? gain + at + D / 2 : nullptr, bias != nullptr ? bias + at + D / 2 : nullptr, xb);
+  apply8<kOnce>(gain != nullptr ? gain + at : nullptr, bias != nullptr ? bias + at : nullptr, xa);
+  apply8<kOnce>(gain != nullptr ? gain + at + D / 2 : nullptr, bias != nullptr ? bias + at + D / 2 : nullptr, xb);
 }
 
 // A thread holds 16 values of a row, a row takes D / 16 lanes, and a block of
@@ -387,7 +398,7 @@ __device__ __forceinline__ void append_block(const CacheAppendArgs& a, int32_t b
     unpack8(wb[u], xb[u]);
     if (kIsK) {
       if constexpr (kNorm != 0)
-        normalise16<D, kNorm>(a.norm.eps, a.norm.k_gain, a.norm.k_bias,
+        normalise16<D, kNorm, true>(a.norm.eps, a.norm.k_gain, a.norm.k_bias,
                               (a.norm.k_heads != 0 ? g * D : 0) + c8, xa[u], xb[u]);
       float2 cs[8];
       load_turns<D>(a, pos[u], c8, wide, cs);
@@ -493,7 +504,7 @@ cache_append_kernel(CacheAppendArgs a, int32_t touched, int64_t kv_units, bool w
     unpack8(wa[u], xa);
     unpack8(wb[u], xb);
     if constexpr (kNorm != 0)
-      normalise16<D, kNorm>(a.norm.eps, a.norm.q_gain, a.norm.q_bias,
+      normalise16<D, kNorm, false>(a.norm.eps, a.norm.q_gain, a.norm.q_bias,
                             (a.norm.q_heads != 0 ? (h0 + u) * D : 0) + c8, xa, xb);
     rotate16(a.rot.interleaved, cs, xa, xb);
     *reinterpret_cast<uint4*>(y + u * D) = pack8(xa);

@@ -689,12 +689,17 @@ ssd_status ssd_cache_attention(const ssd_grid* grid, const ssd_block_cache* cach
  *                [groups], at most max_shared (host, at most max_blocks)
  *   workspace    >= ssd_cache_attention_shared_workspace(..., max_blocks *
  *                block, max_shared * block) bytes; else as there
- * Where sharing would not pay (small work, few sequences to a group) each
- * sequence is worked on by itself, and group_start and shared are not read.
+ * Where sharing would not pay (small work, few sequences to a group, by an
+ * estimate from the arguments' sizes) each sequence is worked on by itself, and
+ * group_start and shared are not read.  ssd_set_cache_sharing(how) is
+ * process-wide, for callers who know better (tables much wider than their
+ * sequences): 0 by the estimate (the default), 1 always sharing, 2 never; it
+ * holds for workspace queries and calls after it.
  * Device errors beside those of ssd_cache_attention(): groups or shared out of
  * range, more shared tokens than cache_len (DEVICE_BOUNDS; rows of the
  * sequences concerned untouched, or, where group_start does not ascend, of no
  * certain value). */
+ssd_status ssd_set_cache_sharing(int32_t how);
 size_t ssd_cache_attention_shared_workspace(int32_t B, int32_t groups, int32_t Hq, int32_t Hkv, int32_t d,
                                             int32_t D_max, int32_t L_max, int32_t max_shared);
 ssd_status ssd_cache_attention_shared(const ssd_grid* grid, const ssd_block_cache* cache, int32_t B,

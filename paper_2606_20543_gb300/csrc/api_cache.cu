@@ -3,11 +3,15 @@
 // caller's stream.  No allocation, no synchronisation.
 #include <math.h>
 
+#include <atomic>
+
 #include "kernels.cuh"
 
 using namespace ssd;
 
 namespace {
+
+std::atomic<int32_t> g_cache_sharing{kShareByEstimate};
 
 ssd_status from_cuda(cudaError_t e) { return e == cudaSuccess ? SSD_OK : SSD_ERR_CUDA; }
 
@@ -156,7 +160,15 @@ ssd_status attention(const ssd_grid* grid, const ssd_block_cache* cache, int32_t
 
 }  // namespace
 
+int32_t ssd::cache_sharing() { return g_cache_sharing.load(std::memory_order_relaxed); }
+
 extern "C" {
+
+ssd_status ssd_set_cache_sharing(int32_t how) {
+  if (how < kShareByEstimate || how > kShareNever) return SSD_ERR_INVALID_ARG;
+  g_cache_sharing.store(how, std::memory_order_relaxed);
+  return SSD_OK;
+}
 
 ssd_status ssd_cache_plan(const ssd_grid* grid, int32_t B, int32_t block, int32_t max_blocks,
                           int32_t N_max, const int32_t* cache_len, const int32_t* n_new,

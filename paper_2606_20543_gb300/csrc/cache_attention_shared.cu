@@ -9,6 +9,7 @@
 // the same launch, or, for few rows, on the mma.sync one (cache_attention.cu).  Both leave part rows,
 // which the kernel here joins.
 #include <algorithm>
+#include <cmath>
 
 #include "cache_attention.cuh"
 
@@ -29,11 +30,37 @@ struct SharedPlan {
   int64_t s_rows, rows;  // part rows
 };
 
-SharedPlan make_plan(int32_t B, int32_t groups, int32_t Hq, int32_t Hkv, int32_t D_max, int32_t L_max,
-                     int32_t max_shared) {
+// Whether sharing pays, by what both ways take (us, from the largest lengths that the call allows).  A
+// tile of the tensor-core kernel takes an SM 4.8e-3 of a GPU's us where all its warps have rows,
+// less where some have none; the mma.sync kernel streams keys at 5.6 (64-wide heads: 6.4) TB/s; the
+// join reads its parts at 3 TB/s.  Sharing starts three kernels instead of one and sets up units of
+// few tiles: 16 us (14 with the own keys in the same launch) instead of 6 (10).  Measured, shared and
+// not: 64 sequences of one group, 4352 + 1000 keys, 32/8 heads 38 and 102; 50 of 4 drafts over 18000
+// 43 and 138; 8 groups of 4, 48 drafts over 8000 + 600, 16 heads 125 and 152; 7 groups of 7 over 68 +
+// 3900 47 and 40; 8 groups of 2 over 5100 + 1900 50 and 25; 37 of 28 drafts over 290 + 90 48 and 20.
+bool sharing_pays(int32_t B, int32_t groups, int32_t Hq, int32_t Hkv, int32_t d, int32_t D_max,
+                  int32_t L_max, int32_t max_shared, const SharedPlan& p) {
+  const double G = Hq / Hkv, per_seq = D_max * G, rows = (double)B * D_max * Hq;
+  const double shared = std::ceil(max_shared / 64.0), own = std::ceil((L_max - max_shared) / 64.0);
+  const double tiles_r = std::max<double>(groups, B * per_seq / 128 + groups / 2.0);
+  const double stacked = tiles_r * Hkv * shared * 4.8e-3;
+  const double join = rows * (std::min<double>(p.s_splits, shared / p.s_min_tiles) + 1) * d * 4 / 3e6;
+  if (p.own_tc) {
+    const double full = std::ceil(std::min(per_seq, 128.0) / 32) / 4, units = B * Hkv * std::ceil(per_seq / 128);
+    const double tile = 4.8e-3 * (0.4 + 0.6 * full);
+    return 14 + stacked + units * own * tile + join < 0.9 * (10 + units * (shared + own) * tile);
+  }
+  const double us_of_tile = (double)B * Hkv * 2 * d * 64 / (d == 128 ? 5.6e6 : 6.4e6);
+  return 16 + stacked + us_of_tile * own + join < 0.9 * (6 + us_of_tile * (shared + own));
+}
+
+SharedPlan make_plan(int32_t B, int32_t groups, int32_t Hq, int32_t Hkv, int32_t d, int32_t D_max,
+                     int32_t L_max, int32_t max_shared) {
   SharedPlan p{};
   const int64_t G = Hq / Hkv, per_seq = D_max * G, rows = (int64_t)B * D_max * Hq;
-  p.plain = max_shared <= 0 || 2 * groups > B || cache_attention_few(B, Hkv, per_seq, L_max);
+  const int32_t how = cache_sharing();
+  p.plain = max_shared <= 0 || how == kShareNever ||
+            (how != kShareAlways && (2 * (int64_t)groups > B || cache_attention_few(B, Hkv, per_seq, L_max)));
   if (p.plain) return p;
   // (a group's last tile may be part empty)
   const int64_t tiles_r = (B * per_seq) / 128 + groups, tiles = (max_shared + kCacheTile - 1) / kCacheTile;
@@ -47,6 +74,10 @@ SharedPlan make_plan(int32_t B, int32_t groups, int32_t Hq, int32_t Hkv, int32_t
   p.s_units = (int32_t)(base * p.s_splits);
   p.s_rows = rows * p.s_splits;
   p.own_tc = per_seq > 16;
+  if (how != kShareAlways && !sharing_pays(B, groups, Hq, Hkv, d, D_max, L_max, max_shared, p)) {
+    p.plain = true;
+    return p;
+  }
   if (p.own_tc) {
     cache_attention_tc_plan(B, Hq, Hkv, D_max, L_max, &p.splits, &p.min_tiles);
     p.rows = rows * p.splits;
@@ -170,14 +201,14 @@ __global__ void __launch_bounds__(256) cache_attn_join_kernel(CacheAttnArgs a, C
 
 size_t cache_attention_shared_workspace(int32_t B, int32_t groups, int32_t Hq, int32_t Hkv, int32_t d,
                                         int32_t D_max, int32_t L_max, int32_t max_shared) {
-  const SharedPlan p = make_plan(B, groups, Hq, Hkv, D_max, L_max, max_shared);
+  const SharedPlan p = make_plan(B, groups, Hq, Hkv, d, D_max, L_max, max_shared);
   if (p.plain) return cache_attention_workspace(B, Hq, Hkv, d, D_max, L_max);
   return part_bytes(p.s_rows, d) + part_bytes(p.rows, d) + align256((size_t)B * sizeof(int2));
 }
 
 cudaError_t launch_cache_attention_shared(const CacheAttnArgs& a, void* ws, cudaStream_t stream) {
   const int32_t S = a.cache.block, L_max = a.max_blocks * S, d = a.cache.d;
-  const SharedPlan p = make_plan(a.B, a.groups, a.Hq, a.cache.Hkv, a.D_max, L_max, a.max_shared * S);
+  const SharedPlan p = make_plan(a.B, a.groups, a.Hq, a.cache.Hkv, d, a.D_max, L_max, a.max_shared * S);
   if (p.plain) {
     CacheAttnArgs one = a;
     one.groups = 0;

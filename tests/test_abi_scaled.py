@@ -73,6 +73,38 @@ def test_append_norm(lib):
         assert call(gains=[F + 4 if i == j else F for j in range(4)]) == 1
 
 
+def test_shared_attention(lib):
+    so = lib.load()
+    g = ctypes.byref(lib.grid(16, 16, 32))
+
+    def call(grid=g, nb=8, block=16, Hkv=2, d=64, k=F, B=4, groups=2, start=F, shared=F, most=3, Hq=4, cache=F,
+             nd=F, D=4, table=F, M=4, q=F, scale=0.0, o=F, ws=F, n=1 << 40, st=F):
+        c = lib.BlockCache(nb, block, Hkv, d, k, F, F, F)
+        return so.ssd_cache_attention_shared(grid, ctypes.byref(c), B, groups, start, shared, most, Hq, cache, nd,
+                                             None, None, D, table, M, q, scale, o, None, ws, n, st, None)
+
+    assert call(B=0) == 0
+    assert call(groups=0) == call(most=-1) == call(most=5) == call(Hq=3) == call(D=0) == call(B=-1) == 2
+    assert call(groups=70000) == call(d=96) == call(B=1 << 16) == call(M=1 << 30) == 3
+    for name in ("grid", "k", "start", "shared", "cache", "nd", "table", "q", "o", "st"):
+        assert call(**{name: None}) == 1, name
+    assert call(q=F + 8) == call(o=F + 2) == call(scale=-1.0) == 1
+    assert so.ssd_set_cache_sharing(3) == so.ssd_set_cache_sharing(-1) == 1
+    assert so.ssd_set_cache_sharing(1) == 0
+    try:
+        need = so.ssd_cache_attention_shared_workspace(4, 2, 4, 2, 64, 4, 64, 48)
+        assert need > 0 and call(n=need - 1) == call(ws=None) == 7 and call(ws=F + 8) == 1
+    finally:
+        assert so.ssd_set_cache_sharing(0) == 0
+    assert so.ssd_cache_attention_shared_workspace(4, 0, 4, 2, 64, 4, 64, 48) == 0
+    assert so.ssd_cache_attention_shared_workspace(4, 2, 4, 2, 64, 4, 64, 65) == 0
+    # many sequences over a long prompt share by themselves, few do not
+    few = so.ssd_cache_attention_shared_workspace(2, 1, 32, 8, 128, 1, 8192, 8000)
+    assert few == so.ssd_cache_attention_workspace(2, 32, 8, 128, 1, 8192)
+    many = so.ssd_cache_attention_shared_workspace(64, 1, 32, 8, 128, 1, 8192, 8000)
+    assert many != so.ssd_cache_attention_workspace(64, 32, 8, 128, 1, 8192)
+
+
 def test_python_side_refusals(lib):
     import torch
     g = torch.ones(64)

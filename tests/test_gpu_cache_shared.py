@@ -1,7 +1,7 @@
 """ssd_cache_attention_shared against float64 attention over each sequence's keys; tolerances are
 those of the attention without groups (tests/test_gpu_cache_attention.py), whose parts it joins in
-float32.  Tables are wide, so that also small batches take the path that shares (`wide`), but for the
-tests of the path that does not."""
+float32.  Small batches share here, too (ssd_set_cache_sharing), but for the tests of the rule; `shares`
+asks the workspace's size which path it is."""
 import numpy as np
 import pytest
 import torch
@@ -20,17 +20,23 @@ def ssd():
     return m
 
 
+@pytest.fixture(autouse=True)
+def sharing(ssd):
+    ssd.ssd_set_cache_sharing(1)
+    yield
+    ssd.ssd_set_cache_sharing(0)
+
+
 class Batch:
     """Groups of sequences over one pool: start [groups + 1], shared blocks of a group, own tokens
     (cached behind the shared ones) and drafts of a sequence.  Dead entries and unused scales NaN."""
 
-    def __init__(self, *, seed, start, shared, own, nd, D, Hq, Hkv, d, block, wide=2000, spread=0.5,
+    def __init__(self, *, seed, start, shared, own, nd, D, Hq, Hkv, d, block, wide=None, spread=0.5,
                  edit=None, grid=(64, 64, 3, 64), draft_pos=None, key_start=None, max_shared=None):
         rng = np.random.default_rng(seed)
         self.__dict__.update(start=start, shared=shared, nd=nd, D=D, Hq=Hq, Hkv=Hkv, d=d, block=block,
                              grid=grid, draft_pos=draft_pos, key_start=key_start)
         self.B, self.groups = len(own), len(shared)
-        self.max_shared = max(max(shared), 0) if max_shared is None else max_shared
         names, n, self.cache = [], 0, []
         for g in range(self.groups):
             first = list(range(n, n + shared[g]))
@@ -42,7 +48,8 @@ class Batch:
                 n += more
         pool = n + 2
         ids = rng.permutation(pool)
-        self.M = max(max(len(x) for x in names), 1) + wide
+        self.M = max(max(len(x) for x in names), 1) + (2000 if wide is None else wide)
+        self.max_shared = max(max(shared), 0) if max_shared is None else max_shared
         self.table = np.full((self.B, self.M), -1)
         for b, x in enumerate(names):
             self.table[b, :len(x)] = ids[x]
@@ -75,7 +82,7 @@ class Batch:
         wb = ssd.ssd_cache_attention_shared_workspace(B, self.groups, Hq, Hkv, d, D, self.M * self.block,
                                                       self.max_shared * self.block)
         ws = torch.full((max(wb, 16),), 0xff, dtype=torch.uint8, device="cuda")
-        self.ws_bytes = wb
+        self.shares = wb != ssd.ssd_cache_attention_workspace(B, Hq, Hkv, d, D, self.M * self.block)
         opt = lambda x: None if x is None else i32(x)  # noqa: E731
         self.args = (ssd.grid(H, W, prefix, rs), ssd.cache(dev["k"], dev["v"], dsc["k"], dsc["v"]), B,
                      self.groups, i32(self.start), i32(self.shared), self.max_shared, Hq, i32(self.cache),
@@ -116,9 +123,9 @@ class Batch:
             out.append((self.q[b, :n].double().numpy(), per, see, self.d ** -0.5))
         return out
 
-    def check(self, ssd, status=0, **kw):
+    def check(self, ssd, status=0, shares=True, **kw):
         o, ls, st = self.run(ssd)
-        assert st == status
+        assert st == status and self.shares == shares
         check(o, ls, self.refs(), self.nd, **kw)
         return o, ls
 
@@ -175,7 +182,7 @@ def test_padding_on_the_left_and_rows_that_see_nothing(ssd, D, d):
 def test_long_prompts(ssd, D, Hq, Hkv, d):
     """Shared keys of many parts beside short ones."""
     Batch(seed=D + d, start=[0, 4, 9], shared=[320, 3], own=[200, 37, 4000, 0, 0, 900, 64, 63, 1], nd=[D] * 9,
-          D=D, Hq=Hq, Hkv=Hkv, d=d, block=64, wide=500).check(ssd, rows=[0, 1, 17, D - 1])
+          D=D, Hq=Hq, Hkv=Hkv, d=d, block=64).check(ssd, rows=[0, 1, 17, D - 1])
 
 
 @pytest.mark.parametrize("B,groups,D", [(64, 1, 1), (70, 5, 1), (300, 70, 1), (40, 33, 20)])
@@ -187,23 +194,34 @@ def test_many_sequences_and_groups(ssd, B, groups, D):
           wide=20000).check(ssd, rows=[0, D - 1])
 
 
+@pytest.mark.parametrize("wide", [400, 4000])
 @pytest.mark.parametrize("B,Hq,Hkv,D", [(64, 16, 8, 1), (60, 8, 8, 2), (300, 4, 2, 1), (40, 24, 12, 3)])
-def test_more_sequences_than_places(ssd, B, Hq, Hkv, D):
+def test_more_sequences_than_places(ssd, B, Hq, Hkv, D, wide):
     """A CTA for every sequence and head, the longest first (up to 256 sequences)."""
     rng = np.random.default_rng(B)
     start = [0, 1, B // 3, B]
     Batch(seed=B, start=start, shared=[2, 0, 11], own=rng.integers(0, 500, B).tolist(),
           nd=rng.integers(0, D + 1, B).tolist(), D=D, Hq=Hq, Hkv=Hkv, d=64, block=16,
-          wide=0).check(ssd, rows=[0, D - 1])
+          wide=wide).check(ssd, rows=[0, D - 1])
 
 
-def test_small_work_takes_the_path_of_every_sequence_by_itself(ssd):
-    kw = dict(seed=3, start=[0, 2, 4], shared=[12, 12], own=[10, 200, 77, 0], nd=[1] * 4, D=1, Hq=8, Hkv=8, d=64,
-              block=16)
-    small, wide = Batch(wide=0, **kw), Batch(wide=4000, **kw)
-    small.check(ssd)
-    wide.check(ssd)
-    assert small.ws_bytes < wide.ws_bytes
+def test_where_sharing_pays(ssd):
+    """The rule by sizes, the same results on both sides of it."""
+    ssd.ssd_set_cache_sharing(0)
+    small = dict(seed=3, start=[0, 2, 4], shared=[12, 12], own=[10, 200, 77, 0], nd=[1] * 4, D=1, Hq=8, Hkv=8, d=64,
+                 block=16, wide=0)
+    Batch(**small).check(ssd, shares=False)
+    Batch(**dict(small, shared=[0, 0])).check(ssd, shares=False)
+    large = dict(seed=3, start=[0, 48], shared=[40], own=list(range(48)), nd=[1] * 48, D=1, Hq=8, Hkv=8, d=64,
+                 block=128, wide=0)
+    Batch(**large).check(ssd, rows=[0], heads=[0, 5])
+    ssd.ssd_set_cache_sharing(2)
+    Batch(**large).check(ssd, shares=False, rows=[0], heads=[0, 5])
+    ssd.ssd_set_cache_sharing(1)
+    Batch(**small).check(ssd)
+    for how in (-1, 3):
+        with pytest.raises(ssd.SsdError):
+            ssd.ssd_set_cache_sharing(how)
 
 
 def test_scales_that_differ(ssd):
@@ -221,7 +239,7 @@ def test_a_nan_key_reaches_the_rows_that_see_it(ssd):
         b = Batch(seed=D, start=[0, 3, 5], shared=[6, 6], own=[10, 20, 30, 40, 50], nd=[D] * 5, D=D, Hq=4, Hkv=2,
                   d=128, block=16, edit=edit, key_start=[0, 0, 36, 0, 0])
         o, ls, st = b.run(ssd)
-        assert st == 0
+        assert st == 0 and b.shares
         nan = torch.isnan(o).all(-1)
         want = torch.zeros_like(nan)
         want[:2, :, 2:] = True
@@ -240,7 +258,7 @@ def test_the_first_of_a_group_may_be_done(ssd):
         b = Batch(seed=D, start=[0, 4], shared=[6], own=[10, 20, 30, 40], nd=[0, D, 0, D], D=D, Hq=4, Hkv=2,
                   d=128, block=32, edit=edit)
         o, ls, st = b.run(ssd)
-        assert st == 0 and (o[0] == 7).all() and (o[2] == 7).all()
+        assert st == 0 and b.shares and (o[0] == 7).all() and (o[2] == 7).all()
         refs = b.refs()
         for i in (1, 3):
             check(o[i:i + 1], ls[i:i + 1], refs[i:i + 1], [D])
@@ -254,15 +272,15 @@ def test_bad_groups_lengths_and_blocks(ssd):
         b.cache[4] = -2
     b = Batch(nd=[3, 3, 9, 3, 3], edit=edit, **base)
     o, ls, st = b.run(ssd)
-    assert st == 6 and (o[1] == 7).all() and (o[2] == 7).all() and (o[4] == 7).all()
+    assert st == 6 and b.shares and (o[1] == 7).all() and (o[2] == 7).all() and (o[4] == 7).all()
     b.nd, b.cache[1], b.cache[4] = [3, 3, 3, 3, 3], 68, 73
     refs = b.refs()
     for i in (0, 3):
         check(o[i:i + 1], ls[i:i + 1], refs[i:i + 1], [3])
     # blocks that are shared beyond max_shared, or fewer than none
-    for shared, most in (([3, 4], 3), ([3, -1], 4)):
+    for shared in (10 ** 9, -1):
         b = Batch(nd=[3] * 5, **base)
-        b.shared, b.max_shared = shared, most
+        b.shared = [3, b.max_shared + 1 if shared > 0 else shared]
         o, ls, st = b.run(ssd)
         assert st == 6 and (o[3:] == 7).all()
         check(o[:3], ls[:3], b.refs()[:3], [3] * 3)
@@ -270,7 +288,7 @@ def test_bad_groups_lengths_and_blocks(ssd):
     for start in ([0, 3, 4], [1, 3, 5], [0, 6, 5], [0, -7, 5]):
         b = Batch(nd=[3] * 5, **base)
         b.start = start
-        assert b.run(ssd, twice=False)[2] == 6
+        assert b.run(ssd, twice=False)[2] == 6 and b.shares
     # a shared block outside the pool hides its tokens
     for D in (2, 40):
         def hide(b):
@@ -279,7 +297,7 @@ def test_bad_groups_lengths_and_blocks(ssd):
         refs = b.refs()
         hide(b)
         o, ls, st = b.run(ssd)
-        assert st == 6
+        assert st == 6 and b.shares
         for r in refs:
             r[2][:, 16:32] = False
         check(o, ls, refs, [D] * 3)
@@ -292,7 +310,7 @@ def test_another_stream_graphs_and_no_lse(ssd):
     for D in (1, 40):
         b = Batch(seed=4 + D, start=[0, 3], shared=[9], own=[30, 0, 77], nd=[D] * 3, D=D, Hq=4, Hkv=2, d=128, block=32)
         o, _, st = b.run(ssd, stream=s, lse=False)
-        assert st == 0
+        assert st == 0 and b.shares
         check(o, None, b.refs(), b.nd)
         want = o.clone()
         graph = torch.cuda.CUDAGraph()
@@ -314,7 +332,8 @@ def test_workspace_and_refusals(ssd):
     b = Batch(seed=1, start=[0, 3], shared=[3], own=[1, 2, 3], nd=[1] * 3, D=1, Hq=4, Hkv=2, d=64, block=16)
     b.run(ssd)
     a = list(b.args)
-    for i, x in ((3, 0), (6, b.M + 1), (6, -1), (20, b.ws_bytes - 1), (4, None), (5, None)):
+    assert b.shares
+    for i, x in ((3, 0), (6, b.M + 1), (6, -1), (20, a[20] - 1), (4, None), (5, None)):
         bad = list(a)
         bad[i] = x
         with pytest.raises(ssd.SsdError):

@@ -46,6 +46,14 @@ def rows(gen, n, Hq, Hkv, d):
     return x.split([Hq * d, Hkv * d, Hkv * d], 1)
 
 
+@pytest.fixture(autouse=True)
+def sharing(ssd):
+    """Also batches as small as these read shared blocks once."""
+    ssd.ssd_set_cache_sharing(1)
+    yield
+    ssd.ssd_set_cache_sharing(0)
+
+
 @pytest.mark.parametrize("Hq,Hkv,d,block,norm", [(8, 2, 128, 16, None), (4, 4, 64, 32, "rms"),
                                                  (8, 2, 128, 16, "layer")])
 def test_shared_blocks_as_blocks_of_their_own(ssd, Hq, Hkv, d, block, norm):

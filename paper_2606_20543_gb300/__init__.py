@@ -524,13 +524,21 @@ def ssd_cache_attention_shared(g: Grid, c: BlockCache, B, groups, group_start, s
         _stream(stream)))
 
 
+_dtypes = None
+
+
 def _is_bf16(t, what: str) -> int:
     """1 for bfloat16 (or nothing at all), 0 for float32."""
-    if t is None or str(t.dtype) == "torch.bfloat16":
+    global _dtypes
+    if _dtypes is None:
+        import torch
+        _dtypes = {torch.float32: 0, torch.bfloat16: 1}
+    if t is None:
         return 1
-    if str(t.dtype) == "torch.float32":
-        return 0
-    raise ValueError(what + " is float32 or bfloat16")
+    code = _dtypes.get(t.dtype)
+    if code is None:
+        raise ValueError(what + " is float32 or bfloat16")
+    return code
 
 
 def ssd_quantize(rows, K, block_rows, x, ldx, out, ldo, scale, lds, stream=None) -> None:
@@ -544,7 +552,7 @@ def ssd_scaled_matmul(M, N, K, a, lda, a_scale, ldas, w, ldw, w_scale, ldws, add
                       status, stream=None) -> None:
     """C = A W^T (+ add) of e4m3 rows and weights with a scale per 128 (ssd_quantize); C float32
     or bf16, add bf16 or None."""
-    if add is not None and str(add.dtype) != "torch.bfloat16":
+    if add is not None and not _is_bf16(add, "add"):
         raise ValueError("add is bfloat16")
     for t in (a, w):
         if t is not None and t.element_size() != 1:

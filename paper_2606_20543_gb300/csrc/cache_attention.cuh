@@ -26,7 +26,8 @@ struct CacheAttnLaunch {
   // Groups' shared keys (tensor-core kernel): units of the grid, tiles of rows among them, parts and
   // their rows [B][D_max][Hq][s_splits]
   int32_t s_units, s_splits, s_min_tiles;
-  int32_t early;  // the kernel after it may run beside it: the sequences' own keys
+  int32_t early;       // the kernel after it may run beside it: the sequences' own keys
+  int32_t join_heads;  // heads that a warp of the join takes
   float* s_part_o;
   float2* s_part_ml;
 };

@@ -115,8 +115,8 @@ __global__ void __launch_bounds__(256) cache_attn_join_kernel(CacheAttnArgs a, C
     if (threadIdx.x == 0) bad |= a.group_start[0] != 0 || a.group_start[a.groups] != a.B;
     if (bad) record_status(a.status, SSD_ERR_DEVICE_BOUNDS);
   }
-  const int32_t h = blockIdx.y * 8 + (threadIdx.x >> 5);
-  if (h >= a.Hq) return;
+  const int32_t h0 = (blockIdx.y * 8 + (threadIdx.x >> 5)) * L.join_heads;
+  if (h0 >= a.Hq) return;
   const int32_t b = (int32_t)(blockIdx.x / (uint32_t)a.D_max), j = blockIdx.x - b * a.D_max;
   const int32_t cache = a.cache_len[b], nd = a.n_drafts[b];
   const int2 cut = L.info != nullptr ? L.info[b] : make_int2(0, 0);
@@ -124,77 +124,79 @@ __global__ void __launch_bounds__(256) cache_attn_join_kernel(CacheAttnArgs a, C
   if (!cache_lengths_ok(a, cache, nd) || j >= nd) return;
   const int32_t base = group.base(a, b, cache);
   if (base < 0) return;
-  const int64_t row = (int64_t)blockIdx.x * a.Hq + h;
   const int32_t shared_tiles = (base + kCacheTile - 1) / kCacheTile;
   const int32_t n_shared = shared_tiles > 0 ? cache_parts(L.s_splits, L.s_min_tiles, shared_tiles) : 0;
-  int32_t n_own, step = 1;
-  int64_t at;
-  if (L.info != nullptr) {
-    const int32_t G = a.Hq / a.cache.Hkv, g = h / G;
-    const CacheShares x = cache_shares(L, a.B, b, cut, g, j * G + (h - g * G));
-    n_own = x.parts;
-    step = L.group_rows;
-    at = x.at;
-    if (!dbg_in(at + (n_own - 1) * step, (int64_t)a.cache.Hkv * L.row_groups * (L.per_head + a.B) * step,
-                a.status))
-      return;
-  } else {
-    n_own = cache_parts(L.splits, L.min_tiles, (cache + nd - base + kCacheTile - 1) / kCacheTile);
-    at = row * L.splits;
-  }
-  if (n_own <= 0) return;  // (a wait gave up: no part is known)
-  const int32_t parts = n_shared + n_own;
-  const int64_t s_at = row * L.s_splits, own_at = at - (int64_t)n_shared * step;
-  auto ml_of = [&](int32_t s) {
-    return s < n_shared ? L.s_part_ml[s_at + s] : L.part_ml[own_at + (int64_t)s * step];
-  };
-  // The first parts' rows are asked for together with the factors of all.
-  Lanes<PER> v[kTogether], acc;
-  auto rows_of = [&](int32_t i0) {
-#pragma unroll
-    for (int i = 0; i < kTogether; ++i) {
-      const int32_t s = min(i0 + i, parts - 1);
-      const float* p = s < n_shared ? L.s_part_o + (s_at + s) * D : L.part_o + (own_at + (int64_t)s * step) * D;
-      v[i] = *reinterpret_cast<const Lanes<PER>*>(p + lane * PER);
-    }
-  };
-  rows_of(0);
-  const float2 first = lane < parts ? ml_of(lane) : make_float2(-INFINITY, 0.f);
-  float M = first.x;
+  const int32_t n_tiles =
+      L.info != nullptr ? 1 : cache_parts(L.splits, L.min_tiles, (cache + nd - base + kCacheTile - 1) / kCacheTile);
 #pragma unroll 1
-  for (int32_t s = 32 + lane; s < parts; s += 32) M = fmaxf(M, ml_of(s).x);
+  for (int32_t h = h0; h < min(a.Hq, h0 + L.join_heads); ++h) {
+    const int64_t row = (int64_t)blockIdx.x * a.Hq + h;
+    int32_t n_own = n_tiles, step = 1;
+    int64_t at = row * L.splits;
+    if (L.info != nullptr) {
+      const int32_t G = a.Hq / a.cache.Hkv, g = h / G;
+      const CacheShares x = cache_shares(L, a.B, b, cut, g, j * G + (h - g * G));
+      n_own = x.parts;
+      step = L.group_rows;
+      at = x.at;
+      if (!dbg_in(at + (n_own - 1) * step, (int64_t)a.cache.Hkv * L.row_groups * (L.per_head + a.B) * step,
+                  a.status))
+        return;
+    }
+    if (n_own <= 0) return;  // (a wait gave up: no part is known)
+    const int32_t parts = n_shared + n_own;
+    const int64_t s_at = row * L.s_splits, own_at = at - (int64_t)n_shared * step;
+    auto ml_of = [&](int32_t s) {
+      return s < n_shared ? L.s_part_ml[s_at + s] : L.part_ml[own_at + (int64_t)s * step];
+    };
+    // The first parts' rows are asked for together with the factors of all.
+    Lanes<PER> v[kTogether], acc;
+    auto rows_of = [&](int32_t i0) {
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
-#pragma unroll
-  for (int k = 0; k < PER; ++k) acc.x[k] = 0.f;
-  float sum = 0.f, mine = 0.f;  // the factor of part (s0 & ~31) + lane
+      for (int i = 0; i < kTogether; ++i) {
+        const int32_t s = min(i0 + i, parts - 1);
+        const float* p = s < n_shared ? L.s_part_o + (s_at + s) * D : L.part_o + (own_at + (int64_t)s * step) * D;
+        v[i] = *reinterpret_cast<const Lanes<PER>*>(p + lane * PER);
+      }
+    };
+    rows_of(0);
+    const float2 first = lane < parts ? ml_of(lane) : make_float2(-INFINITY, 0.f);
+    float M = first.x;
 #pragma unroll 1
-  for (int32_t s0 = 0; s0 < parts; s0 += kTogether) {
-    if ((s0 & 31) == 0) {
-      const float2 x = s0 == 0 ? first : s0 + lane < parts ? ml_of(s0 + lane) : make_float2(-INFINITY, 0.f);
-      mine = x.x == -INFINITY ? 0.f : exp2f(x.x - M);
-      sum += x.y * mine;
-    }
-    if (s0 > 0) rows_of(s0);
+    for (int32_t s = 32 + lane; s < parts; s += 32) M = fmaxf(M, ml_of(s).x);
 #pragma unroll
-    for (int i = 0; i < kTogether; ++i) {
-      const float f = __shfl_sync(0xffffffffu, mine, (s0 + i) & 31);
-      if (s0 + i >= parts || f == 0.f) continue;
+    for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
 #pragma unroll
-      for (int k = 0; k < PER; ++k) acc.x[k] += v[i].x[k] * f;
+    for (int k = 0; k < PER; ++k) acc.x[k] = 0.f;
+    float sum = 0.f, mine = 0.f;  // the factor of part (s0 & ~31) + lane
+#pragma unroll 1
+    for (int32_t s0 = 0; s0 < parts; s0 += kTogether) {
+      if ((s0 & 31) == 0) {
+        const float2 x = s0 == 0 ? first : s0 + lane < parts ? ml_of(s0 + lane) : make_float2(-INFINITY, 0.f);
+        mine = x.x == -INFINITY ? 0.f : exp2f(x.x - M);
+        sum += x.y * mine;
+      }
+      if (s0 > 0) rows_of(s0);
+#pragma unroll
+      for (int i = 0; i < kTogether; ++i) {
+        const float f = __shfl_sync(0xffffffffu, mine, (s0 + i) & 31);
+        if (s0 + i >= parts || f == 0.f) continue;
+#pragma unroll
+        for (int k = 0; k < PER; ++k) acc.x[k] += v[i].x[k] * f;
+      }
     }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    const float inv = 1.f / sum;
+    uint32_t w[PER / 2];
+#pragma unroll
+    for (int k = 0; k < PER; k += 2)
+      w[k / 2] = pack_bf16x2(row_value(acc.x[k], inv, sum), row_value(acc.x[k + 1], inv, sum));
+    uint32_t* ob = reinterpret_cast<uint32_t*>(static_cast<__nv_bfloat16*>(a.o) + row * D + lane * PER);
+    if constexpr (PER == 4) *reinterpret_cast<uint2*>(ob) = make_uint2(w[0], w[1]);
+    else ob[0] = w[0];
+    if (a.lse != nullptr && lane == 0) a.lse[((int64_t)b * a.Hq + h) * a.D_max + j] = row_lse(M, sum);
   }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-  const float inv = 1.f / sum;
-  uint32_t w[PER / 2];
-#pragma unroll
-  for (int k = 0; k < PER; k += 2)
-    w[k / 2] = pack_bf16x2(row_value(acc.x[k], inv, sum), row_value(acc.x[k + 1], inv, sum));
-  uint32_t* ob = reinterpret_cast<uint32_t*>(static_cast<__nv_bfloat16*>(a.o) + row * D + lane * PER);
-  if constexpr (PER == 4) *reinterpret_cast<uint2*>(ob) = make_uint2(w[0], w[1]);
-  else ob[0] = w[0];
-  if (a.lse != nullptr && lane == 0) a.lse[((int64_t)b * a.Hq + h) * a.D_max + j] = row_lse(M, sum);
 }
 
 }  // namespace
@@ -244,7 +246,10 @@ cudaError_t launch_cache_attention_shared(const CacheAttnArgs& a, void* ws, cuda
     e = launch_cache_attention_mma(a, p.mma, L, stream);
     if (e != cudaSuccess) return e;
   }
-  const dim3 grid((unsigned)(a.B * a.D_max), (unsigned)((a.Hq + 7) / 8));
+  // (with rows for every place of a warp several times over, what a warp looks up serves several heads)
+  const int64_t warps = (int64_t)a.B * a.D_max * a.Hq, places = (int64_t)device_sm_count() * 32;
+  L.join_heads = (int32_t)std::max<int64_t>(1, std::min<int64_t>(4, warps / (2 * places)));
+  const dim3 grid((unsigned)(a.B * a.D_max), (unsigned)((a.Hq + 8 * L.join_heads - 1) / (8 * L.join_heads)));
   return launch_kernel(d == 128 ? cache_attn_join_kernel<128> : cache_attn_join_kernel<64>, grid, dim3(256),
                        0, stream, true, a, L);
 }

@@ -155,7 +155,7 @@ template <bool kShared>
 struct Rows {};
 template <>
 struct Rows<true> {
-  int32_t at[kBM], pos[kBM], start[kBM], least[4];
+  int32_t at[kBM], pos[kBM], start[kBM], least[4], count[8];
 };
 template <bool kShared>
 struct alignas(16) Shared : Rows<kShared> {
@@ -169,8 +169,8 @@ struct alignas(16) Shared : Rows<kShared> {
 };
 
 // kShared (ssd_cache_attention_shared): the grid's first L.s_units units work on groups' shared keys.
-// A unit stacks 128 rows of a group's sequences (D_max drafts each, those that are none left empty),
-// which all see the keys of the shared blocks, but for a row's key_start and position.  The others
+// A unit stacks 128 rows of a group's sequences (tiles are counted as if each had D_max drafts, and
+// those that nothing is left for return), which all see the keys of the shared blocks, but for a row's key_start and position.  The others
 // work on sequences' own keys, behind the shared ones.  All leave part rows for a combine.
 template <int D, bool kShared>
 __global__ void __launch_bounds__(kThreadsTC, kCtasPerSm)
@@ -201,13 +201,13 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
   const int32_t split = unit % splits;
   unit /= splits;
   int32_t b, cache, nd, g, mtile, rows_total, base = 0, tiles;
-  int32_t b_first = 0;                       // stacked: the group's first sequence
+  int32_t b_first = 0, members = 0;          // stacked: the group's first sequence, and how many
   const int32_t per_seq = kShared ? a.D_max * G : 0;  // and a sequence's rows
   if (stacked) {
     g = unit % Hkv;
     // the group that holds row tile unit / Hkv
     const int32_t tile = unit / Hkv;
-    int32_t before = 0, group = -1, members = 0;
+    int32_t before = 0, group = -1;
     for (int32_t g0 = 0; g0 < a.groups && group < 0; g0 += 32) {
       const bool in = g0 + lane < a.groups;
       const int32_t s0 = in ? min(max(a.group_start[g0 + lane], 0), a.B) : 0;
@@ -304,15 +304,57 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
   if (row0 >= rows_total || split >= parts) return;
   if constexpr (kShared) {
     if (stacked) {
+      // Rows are the drafts of the group's sequences, one sequence behind the other: sh.len counts the
+      // drafts up to each (of more than kLptMax sequences, D_max to each).
+      const bool counted = members <= kLptMax;
+      if (counted) {
+        int32_t upto = 0;
+        if (tid < members) {
+          const int32_t c = a.cache_len[b_first + tid], n = a.n_drafts[b_first + tid];
+          upto = cache_lengths_ok(a, c, n) && c >= cache ? n : 0;
+        }
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const int32_t y = __shfl_up_sync(0xffffffffu, upto, o);
+          if (lane >= o) upto += y;
+        }
+        if (lane == 31) sh.count[warp] = upto;
+        __syncthreads();
+        int32_t all = 0;
+#pragma unroll
+        for (int w = 0; w < kThreadsTC / 32; ++w) {
+          if (w < warp) upto += sh.count[w];
+          all += sh.count[w];
+        }
+        sh.len[tid] = upto;
+        __syncthreads();
+        rows_total = all * G;
+        if (row0 >= rows_total) return;
+      }
       int32_t least = 0x7fffffff;
       if (tid < kBM) {
-        const int32_t r = row0 + tid, m = r / per_seq, in = r - m * per_seq, rb = b_first + m;
+        const int32_t r = row0 + tid;
         int32_t at = -1, pos = 0x7fffffff, from = 0;
         if (r < rows_total) {
-          const int32_t c = a.cache_len[rb], n = a.n_drafts[rb], j = in / G;
-          if (cache_lengths_ok(a, c, n) && j < n && c >= cache) {
-            at = (rb * a.D_max + j) * a.Hq + g * G + (in - j * G);
-            pos = cache_flat_pos(a, rb, c, j);
+          int32_t draft = r / G, m;
+          const int32_t h = g * G + (r - draft * G);
+          if (counted) {
+            int32_t lo = 0, hi = members - 1;  // the first sequence that counts beyond the draft
+            while (lo < hi) {
+              const int32_t mid = (lo + hi) >> 1;
+              if (sh.len[mid] > draft) hi = mid;
+              else lo = mid + 1;
+            }
+            m = lo;
+            if (m > 0) draft -= sh.len[m - 1];
+          } else {
+            m = draft / a.D_max;
+            draft -= m * a.D_max;
+          }
+          const int32_t rb = b_first + m, c = a.cache_len[rb], n = a.n_drafts[rb];
+          if (cache_lengths_ok(a, c, n) && draft < n && c >= cache) {
+            at = (rb * a.D_max + draft) * a.Hq + h;
+            pos = cache_flat_pos(a, rb, c, draft);
             if (a.key_start != nullptr) from = min(cache, max(0, a.key_start[rb]));
             least = rb;
           }

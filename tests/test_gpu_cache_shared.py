@@ -185,7 +185,7 @@ def test_long_prompts(ssd, D, Hq, Hkv, d):
           D=D, Hq=Hq, Hkv=Hkv, d=d, block=64).check(ssd, rows=[0, 1, 17, D - 1])
 
 
-@pytest.mark.parametrize("B,groups,D", [(64, 1, 1), (70, 5, 1), (300, 70, 1), (40, 33, 20)])
+@pytest.mark.parametrize("B,groups,D", [(64, 1, 1), (70, 5, 1), (300, 70, 1), (40, 33, 20), (300, 1, 2)])
 def test_many_sequences_and_groups(ssd, B, groups, D):
     rng = np.random.default_rng(B)
     start = [0] + sorted(rng.choice(np.arange(1, B), groups - 1, replace=False).tolist()) + [B]

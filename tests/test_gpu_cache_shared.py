@@ -185,13 +185,21 @@ def test_long_prompts(ssd, D, Hq, Hkv, d):
           D=D, Hq=Hq, Hkv=Hkv, d=d, block=64).check(ssd, rows=[0, 1, 17, D - 1])
 
 
-@pytest.mark.parametrize("B,groups,D", [(64, 1, 1), (70, 5, 1), (300, 70, 1), (40, 33, 20), (300, 1, 2)])
+@pytest.mark.parametrize("B,groups,D", [(64, 1, 1), (70, 5, 1), (300, 70, 1), (40, 33, 20)])
 def test_many_sequences_and_groups(ssd, B, groups, D):
     rng = np.random.default_rng(B)
     start = [0] + sorted(rng.choice(np.arange(1, B), groups - 1, replace=False).tolist()) + [B]
     Batch(seed=B, start=start, shared=rng.integers(0, 9, groups).tolist(), own=rng.integers(0, 200, B).tolist(),
           nd=rng.integers(0, D + 1, B).tolist(), D=D, Hq=4, Hkv=1, d=64, block=16,
           wide=20000).check(ssd, rows=[0, D - 1])
+
+
+@pytest.mark.parametrize("B", [255, 256, 257, 300])
+def test_groups_of_many(ssd, B):
+    """Up to 256 sequences have only their drafts stacked."""
+    rng = np.random.default_rng(B)
+    Batch(seed=B, start=[0, B], shared=[9], own=rng.integers(0, 60, B).tolist(), nd=rng.integers(0, 3, B).tolist(),
+          D=2, Hq=4, Hkv=2, d=64, block=16).check(ssd, rows=[0, 1], heads=[1, 2])
 
 
 @pytest.mark.parametrize("wide", [400, 4000])

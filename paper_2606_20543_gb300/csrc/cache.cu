@@ -196,7 +196,16 @@ __global__ void rotary_table_kernel(int32_t n, int32_t pairs, const float* freq,
 // Rotation of 16 values of a head: 8 from column c8 on in a, 8 from column c8 +
 // d/2 on in b.  Products and sums are rounded one by one (no fused
 // multiply-add), so the result does not depend on how a compiler pairs them.
+// kFused (behind a norm, whose results are rounded in any case): one rounding less, and two
+// instructions of six.
+template <bool kFused>
 __device__ __forceinline__ void turn(float& x, float& y, float2 cs) {
+  if constexpr (kFused) {
+    const float u = fmaf(x, cs.x, -__fmul_rn(y, cs.y));
+    y = fmaf(y, cs.x, __fmul_rn(x, cs.y));
+    x = u;
+    return;
+  }
   const float u = __fsub_rn(__fmul_rn(x, cs.x), __fmul_rn(y, cs.y));
   y = __fadd_rn(__fmul_rn(y, cs.x), __fmul_rn(x, cs.y));
   x = u;
@@ -238,17 +247,18 @@ __device__ __forceinline__ void load_turns(const CacheAppendArgs& a, const int32
     }
   }
 }
+template <bool kFused>
 __device__ __forceinline__ void rotate16(bool interleaved, const float2 (&cs)[8], float (&xa)[8],
                                          float (&xb)[8]) {
   if (interleaved) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      turn(xa[2 * i], xa[2 * i + 1], cs[i]);
-      turn(xb[2 * i], xb[2 * i + 1], cs[4 + i]);
+      turn<kFused>(xa[2 * i], xa[2 * i + 1], cs[i]);
+      turn<kFused>(xb[2 * i], xb[2 * i + 1], cs[4 + i]);
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) turn(xa[i], xb[i], cs[i]);
+    for (int i = 0; i < 8; ++i) turn<kFused>(xa[i], xb[i], cs[i]);
   }
 }
 
@@ -402,7 +412,7 @@ __device__ __forceinline__ void append_block(const CacheAppendArgs& a, int32_t b
                               (a.norm.k_heads != 0 ? g * D : 0) + c8, xa[u], xb[u]);
       float2 cs[8];
       load_turns<D>(a, pos[u], c8, wide, cs);
-      rotate16(a.rot.interleaved, cs, xa[u], xb[u]);
+      rotate16<kNorm != 0>(a.rot.interleaved, cs, xa[u], xb[u]);
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -506,7 +516,7 @@ cache_append_kernel(CacheAppendArgs a, int32_t touched, int64_t kv_units, bool w
     if constexpr (kNorm != 0)
       normalise16<D, kNorm, false>(a.norm.eps, a.norm.q_gain, a.norm.q_bias,
                             (a.norm.q_heads != 0 ? (h0 + u) * D : 0) + c8, xa, xb);
-    rotate16(a.rot.interleaved, cs, xa, xb);
+    rotate16<kNorm != 0>(a.rot.interleaved, cs, xa, xb);
     *reinterpret_cast<uint4*>(y + u * D) = pack8(xa);
     *reinterpret_cast<uint4*>(y + u * D + D / 2) = pack8(xb);
   }

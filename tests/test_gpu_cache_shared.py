@@ -32,10 +32,11 @@ class Batch:
     (cached behind the shared ones) and drafts of a sequence.  Dead entries and unused scales NaN."""
 
     def __init__(self, *, seed, start, shared, own, nd, D, Hq, Hkv, d, block, wide=None, spread=0.5,
-                 edit=None, grid=(64, 64, 3, 64), draft_pos=None, key_start=None, max_shared=None):
+                 edit=None, grid=(64, 64, 3, 64), draft_pos=None, key_start=None, max_shared=None,
+                 offset=0):
         rng = np.random.default_rng(seed)
         self.__dict__.update(start=start, shared=shared, nd=nd, D=D, Hq=Hq, Hkv=Hkv, d=d, block=block,
-                             grid=grid, draft_pos=draft_pos, key_start=key_start)
+                             grid=grid, draft_pos=draft_pos, key_start=key_start, offset=offset)
         self.B, self.groups = len(own), len(shared)
         names, n, self.cache = [], 0, []
         for g in range(self.groups):
@@ -73,8 +74,12 @@ class Batch:
 
     def run(self, ssd, stream=None, lse=True, twice=True):
         B, D, Hq, Hkv, d = self.B, self.D, self.Hq, self.Hkv, self.d
+        off = self.offset  # blocks of the pool before the first that is used
         dev = {x: torch.from_numpy(self.codes[x]).cuda() for x in "kv"}
         dsc = {x: torch.from_numpy(self.scales[x]).cuda() for x in "kv"}
+        if off:
+            dev = {x: torch.cat([t.new_full((off,) + t.shape[1:], 0x7f), t]) for x, t in dev.items()}
+            dsc = {x: torch.cat([t.new_full((off,) + t.shape[1:], float("nan")), t]) for x, t in dsc.items()}
         H, W, prefix, rs = self.grid
         o = torch.full((B, D, Hq, d), 7.0, dtype=torch.bfloat16, device="cuda")
         ls = torch.full((B, Hq, D), 7.0, device="cuda") if lse else None
@@ -86,7 +91,8 @@ class Batch:
         opt = lambda x: None if x is None else i32(x)  # noqa: E731
         self.args = (ssd.grid(H, W, prefix, rs), ssd.cache(dev["k"], dev["v"], dsc["k"], dsc["v"]), B,
                      self.groups, i32(self.start), i32(self.shared), self.max_shared, Hq, i32(self.cache),
-                     i32(self.nd), opt(self.draft_pos), opt(self.key_start), D, i32(self.table), self.M,
+                     i32(self.nd), opt(self.draft_pos), opt(self.key_start), D,
+                     i32(np.where(self.table >= 0, self.table + off, -1)), self.M,
                      self.q.cuda(), 0.0, o, ls, ws, wb, st)
         self.held = dev, dsc
         torch.cuda.synchronize()
@@ -192,6 +198,13 @@ def test_many_sequences_and_groups(ssd, B, groups, D):
     Batch(seed=B, start=start, shared=rng.integers(0, 9, groups).tolist(), own=rng.integers(0, 200, B).tolist(),
           nd=rng.integers(0, D + 1, B).tolist(), D=D, Hq=4, Hkv=1, d=64, block=16,
           wide=20000).check(ssd, rows=[0, D - 1])
+
+
+def test_offsets_beyond_32_bits(ssd):
+    """Blocks behind the first 3 GB of a pool."""
+    for D in (1, 40):
+        Batch(seed=D, start=[0, 4], shared=[5], own=[100, 3, 64, 0], nd=[D] * 4, D=D, Hq=4, Hkv=2, d=128, block=64,
+              offset=200000).check(ssd)
 
 
 @pytest.mark.parametrize("B", [255, 256, 257, 300])

@@ -91,6 +91,26 @@ def test_every_e4m3_value_stays(ssd):
     assert whole.sum() >= 2
 
 
+def test_offsets_beyond_32_bits(ssd):
+    """More than 2^31 entries: the last rows as rows of a small call."""
+    rows, K = 300000, 8192
+    x = torch.zeros((rows, K), dtype=torch.bfloat16, device="cuda")
+    x[-200:].normal_()
+    for block_rows in (1, 128):
+        R = -(-rows // block_rows)
+        out = torch.zeros((rows, K), dtype=torch.uint8, device="cuda")
+        scale = torch.zeros((K // 128, R), device="cuda")
+        ssd.ssd_quantize(rows, K, block_rows, x, K, out, K, scale, R)
+        at = rows // 128 * 128 - 128
+        part, few = torch.zeros((rows - at, K), dtype=torch.uint8, device="cuda"), -(-(rows - at) // block_rows)
+        want = torch.zeros((K // 128, few), device="cuda")
+        ssd.ssd_quantize(rows - at, K, block_rows, x[at:], K, part, K, want, few)
+        torch.cuda.synchronize()
+        assert torch.equal(out[at:], part) and torch.equal(scale[:, -few:], want)
+        assert (part[-100:] != 0).any()
+        del out
+
+
 def test_graph_and_stream(ssd):
     x = torch.randn((64, 512), device="cuda")
     out, scale = torch.zeros((64, 512), dtype=torch.uint8, device="cuda"), torch.zeros((4, 64), device="cuda")

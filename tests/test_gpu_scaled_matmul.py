@@ -30,7 +30,7 @@ def up(x, n):
 class Case:
     """Codes and scales on the GPU, in wider buffers whose rest is NaN."""
 
-    def __init__(self, M, N, K, seed=0, gap=16, offset=0, spread=1.0):
+    def __init__(self, M, N, K, seed=0, gap=16, offset=0, spread=1.0, ldc=None):
         rng = np.random.default_rng(seed)
         self.M, self.N, self.K, C = M, N, K, up(K, 128) // 128
 
@@ -48,12 +48,12 @@ class Case:
         self.sw = np.exp(spread * rng.standard_normal((C, self.ldws))).astype(np.float32)
         self.sa[:, M:], self.sw[:, up(N, 128) // 128:] = np.nan, np.nan
         self.add = torch.from_numpy(rng.standard_normal((M, N)).astype(np.float32)).to(torch.bfloat16)
-        self.gap, self.offset = gap, offset
+        self.offset, self.ldc = offset, N + gap if ldc is None else ldc
         self.dev = {n: torch.from_numpy(getattr(self, n)).cuda() for n in ("a", "w", "sa", "sw")}
 
     def run(self, ssd, bf16=True, add=False, in_place=False):
         M, N = self.M, self.N
-        ldc = N + self.gap
+        ldc = self.ldc
         dtype = torch.bfloat16 if bf16 else torch.float32
         buf = torch.full((M * ldc + self.offset,), 7.0, dtype=dtype, device="cuda")
         c = buf[self.offset:]
@@ -111,6 +111,40 @@ def test_alignment_and_in_place(ssd, M, gap, offset):
     c = Case(M, 2600, 256, 11, gap, offset)
     c.check(ssd, True, in_place=True)
     c.check(ssd, False)
+
+
+@pytest.mark.parametrize("M", [20, 130, 600, 3000])
+@pytest.mark.parametrize("N", [1003, 1540, 2494])
+def test_rows_on_16_bytes_that_end_inside_of_16(ssd, M, N):
+    c = Case(M, N, 400, 19, ldc=N + 8 - N % 8)
+    c.check(ssd, True)
+    c.check(ssd, True, in_place=True)
+    c.check(ssd, False, add=True)
+
+
+def test_offsets_beyond_32_bits(ssd):
+    """More than 2^31 entries of C, and of A: the last rows and columns as in a small product."""
+    for M, N, K in ((40000, 60000, 128), (20, 1 << 25, 256), (1 << 24, 136, 144)):
+        ld = up(K, 16)
+        gen = torch.Generator("cuda").manual_seed(M)
+        rows = lambda n: torch.randint(0, 0x60, (n, ld), generator=gen, device="cuda",  # noqa: E731
+                                       dtype=torch.uint8)
+        a, w, C = rows(M), rows(N), up(K, 128) // 128
+        sa = torch.rand((C, M), generator=gen, device="cuda") + 0.5
+        sw = torch.rand((C, up(N, 128) // 128), generator=gen, device="cuda") + 0.5
+        c, st = torch.zeros((M, N), dtype=torch.bfloat16, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+        ssd.ssd_scaled_matmul(M, N, K, a, ld, sa, M, w, ld, sw, sw.shape[1], None, 0, c, N, st)
+        torch.cuda.synchronize()
+        assert st.item() == 0
+        for i in (slice(0, 3), slice(M // 2, M // 2 + 3), slice(M - 3, M)):
+            for j0 in (0, N // 2 // 128 * 128, (N - 1) // 128 * 128):
+                j = slice(j0, min(N, j0 + 128))
+                x, y = (oc.TABLE[t.cpu().numpy()[:, :K]] for t in (a[i], w[j]))
+                want, mag = oq.matmul(x, sa[:, i].double().cpu().numpy(), y,
+                                      sw[:, j0 // 128:j0 // 128 + 1].double().cpu().numpy())
+                got = c[i, j].double().cpu().numpy()
+                assert (np.abs(got - want) <= (132 + C) * 2.0 ** -23 * mag + 2.0 ** -8 * np.abs(want)).all()
+        del a, w, c, sa, sw
 
 
 @pytest.mark.parametrize("M,N,K", [(3, 200, 900), (40, 300, 300), (200, 520, 300), (4000, 4100, 140)])

@@ -82,24 +82,33 @@ class PagedDecode:
         self.out_tok = new((B * N_max,), torch.int32, -1)
         self.prob, self.kept = new((B * N_max,), torch.float32), new((B * N_max,), torch.int32)
         self.status = new((1,), torch.int32)
-        self._ws = {}
+        self._ws, self._outgrown = {}, []
         # groups that share blocks: of every group its blocks and their ids, of every sequence its group
         self.groups, self.max_shared = 0, 0
 
     def _workspace(self, N):
-        if N not in self._ws:
+        key = N, self.groups, self.max_shared
+        if self._ws.get(N, (None, None))[1] != key:
             sizes = (self.Hq, self.Hkv, self.d, N, self.max_blocks * self.block)
             n = (ssd_cache_attention_shared_workspace(self.B, self.groups, *sizes, self.max_shared * self.block)
                  if self.groups else ssd_cache_attention_workspace(self.B, *sizes))
-            self._ws[N] = torch.empty((max(n, 16),), dtype=torch.uint8, device=self.device), n
-        return self._ws[N]
+            ws = self._ws[N][0] if N in self._ws else None
+            if ws is None or ws.numel() < n:
+                if ws is not None:
+                    self._outgrown.append(ws)  # (graphs may have captured it)
+                ws = torch.empty((max(n, 16),), dtype=torch.uint8, device=self.device)
+            self._ws[N] = ws, key
+        ws = self._ws[N][0]
+        return ws, ws.numel()
 
     def share(self, group_start, blocks) -> None:
         """Group g, the sequences group_start[g] <= b < group_start[g + 1], shares the first blocks[g]
         blocks of its first sequence, which has cached them whole (0: none); the others, which hold
         nothing, go on behind them, at length blocks[g] * block.  group_start: 0 ... B; host numbers
-        both.  Called between passes, not while an earlier group's blocks are held; a graph captured
-        before it attends without groups.  A sequence that is released can begin anew once all of
+        both.  Called between passes, not while an earlier group's blocks are held.  A graph of a pass
+        that was captured before the first share() attends without groups, one captured later serves
+        every share() of as many groups whose blocks are no more than the most when it was captured;
+        for others it is captured anew.  A sequence that is released can begin anew once all of
         its group are (their shared blocks go back with the last of them)."""
         start, blocks = [int(x) for x in group_start], [int(x) for x in blocks]
         if len(start) != len(blocks) + 1 or start[0] != 0 or start[-1] != self.B or not blocks \
@@ -108,16 +117,25 @@ class PagedDecode:
         if min(blocks) < 0 or max(blocks) > self.max_blocks:
             raise ValueError("blocks: between 0 and max_blocks")
         dev = self.device
-        self.groups, self.max_shared = len(blocks), max(blocks)
-        self.group_start = torch.tensor(start, dtype=torch.int32, device=dev)
-        self.shared = torch.tensor(blocks, dtype=torch.int32, device=dev)
+        if len(blocks) != self.groups or max(blocks) > self.max_shared:
+            if self.groups:  # (graphs may have captured them)
+                self._outgrown += [self.group_start, self.shared, self._group, self._shared_ids,
+                                   self._shared_own]
+            self.groups, self.max_shared = len(blocks), max(blocks)
+            new = lambda *shape, t: torch.zeros(shape, dtype=t, device=dev)  # noqa: E731
+            self.group_start = new(self.groups + 1, t=torch.int32)
+            self.shared = new(self.groups, t=torch.int32)
+            self._group = new(self.B, t=torch.int64)
+            self._shared_ids = new(self.groups, max(self.max_shared, 1), t=torch.int32)
+            self._shared_own = new(self.groups, t=torch.int64)
+        self.group_start.copy_(torch.tensor(start, dtype=torch.int32))
+        self.shared.copy_(torch.tensor(blocks, dtype=torch.int32))
         sizes = [b - a for a, b in zip(start, start[1:])]
-        self._group = torch.repeat_interleave(torch.arange(self.groups, device=dev),
-                                              torch.tensor(sizes, device=dev))
+        self._group.copy_(torch.repeat_interleave(torch.arange(self.groups), torch.tensor(sizes)))
         first = torch.tensor([min(a, self.B - 1) for a in start[:-1]], device=dev)
         firsts = torch.tensor([a for a, n in zip(start, sizes) if n > 0], device=dev)
-        self._shared_ids = self.block_table[first, :max(self.max_shared, 1)].clone()
-        self._shared_own = self.shared * torch.tensor([int(n > 0) for n in sizes], device=dev)
+        self._shared_ids.copy_(self.block_table[first, :self._shared_ids.shape[1]])
+        self._shared_own.copy_(self.shared * torch.tensor([int(n > 0) for n in sizes], device=dev))
         base, joins = self.shared[self._group], torch.ones((self.B,), dtype=torch.bool, device=dev)
         joins[firsts] = False
         joins &= base > 0
@@ -127,7 +145,6 @@ class PagedDecode:
         part.copy_(torch.where(take, self._shared_ids[self._group], part))
         self.cache_len.copy_(torch.where(joins, base * self.block, self.cache_len))
         self.held.copy_(torch.where(joins, base, self.held))
-        self._ws = {}
 
     def plan(self, n_new, N=None) -> None:
         """n_new int32 [B] (device), at most N (default N_max) each."""

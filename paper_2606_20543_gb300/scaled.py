@@ -44,9 +44,8 @@ class ScaledLinear:
 
     def __init__(self, weight, status=None):
         N, K = weight.shape
-        if weight.stride(1) != 1 or weight.stride(0) % 8 != 0:
-            weight = torch.nn.functional.pad(weight, (0, -K % 8))
-            weight = weight.contiguous()
+        if weight.stride(1) != 1 or weight.stride(0) % 8 != 0 or weight.stride(0) < K or weight.data_ptr() % 16:
+            weight = torch.cat([weight, weight.new_zeros((N, -K % 8))], 1)  # (a copy in any case)
         self.N, self.K, self.ld = N, K, _up(K, 16)
         dev = weight.device
         self.w = torch.zeros((N, self.ld), dtype=torch.float8_e4m3fn, device=dev)

@@ -118,6 +118,84 @@ def test_shared_blocks_as_blocks_of_their_own(ssd, Hq, Hkv, d, block, norm):
     assert int(b.status.item()) == 0 and (o - o_a.double()).norm() <= 8e-3 * o.norm()
 
 
+def test_graphs_of_earlier_groups(ssd):
+    """A pass captured before any share() attends without groups, in a workspace of its own; one
+    captured after serves the next share() of as many groups."""
+    B, Hq, Hkv, d, block, W, prefix = 4, 8, 2, 128, 16, 8, 1500
+    gen = torch.Generator("cuda").manual_seed(3)
+    a, b = (make(ssd, B, Hq, Hkv, d, block, prefix, W, prefix) for _ in range(2))
+    one, qkv = i32([1] * B), [x.contiguous() for x in rows(gen, B, Hq, Hkv, d)]
+
+    def step(dec):
+        dec.plan(one, 1)
+        return dec.attend(0, *qkv)
+
+    def begin(start, blocks):
+        """The same prompts in both, b's shared (start None: not)."""
+        every = torch.ones((B,), dtype=torch.bool, device="cuda")
+        a.release(every)
+        b.release(every)
+        group = np.zeros(B, int) if start is None else np.repeat(np.arange(len(blocks)), np.diff(start))
+        prompts = [rows(gen, prefix, Hq, Hkv, d) for _ in range(B)]
+        q, k, v = (torch.cat([prompts[g][i] for g in group]) for i in range(3))
+        a.plan(i32([prefix] * B))
+        a.attend(0, q, k, v)
+        a.advance()
+        done = np.zeros(B, int)
+        if start is not None:
+            done = np.array([blocks[g] * block for g in group])
+            b.plan(i32(done * [int(i in start[:-1]) for i in range(B)]))
+            b.attend(0, q, k, v)
+            b.advance()
+            b.share(start, blocks)
+        n = prefix - done
+        part = [torch.cat([x.view(B, prefix, -1)[i, np.r_[done[i]:prefix, 0:done[i]]] for i in range(B)])
+                for x in (q, k, v)]
+        b.plan(i32(n))
+        b.attend(0, *part)
+        b.advance()
+
+    def capture():
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            o = step(b)
+            b.advance()
+        return graph, o
+
+    def check(graph, o):
+        for x in qkv:
+            x.normal_(generator=gen)
+        want = step(a).double()
+        a.advance()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert (o.double() - want).norm() <= 8e-3 * want.norm()
+        assert int(a.status.item()) == 0 and int(b.status.item()) == 0
+        assert torch.equal(a.cache_len, b.cache_len)
+
+    begin(None, None)
+    step(b)
+    size = b._ws[1][0].numel()
+    assert size > 4096
+    alone, o0 = capture()
+    check(alone, o0)
+    begin([0, 2, 4], [40, 7])
+    step(b)
+    shared, o1 = capture()
+    junk = [torch.full((size,), 7, dtype=torch.uint8, device="cuda") for _ in range(4)]
+    for graph, o in ((shared, o1), (alone, o0), (shared, o1)):
+        check(graph, o)
+    assert all((t == 7).all() for t in junk)
+    begin([0, 1, 4], [11, 30])
+    check(shared, o1)
+    check(alone, o0)
+    begin([0, 4], [50])
+    step(b)
+    fewer, o2 = capture()
+    check(fewer, o2)
+    check(alone, o0)
+
+
 def test_share_refuses(ssd):
     dec = make(ssd, 4, 2, 2, 64, 16, 40, 4, 40)
     for start, blocks in (([0, 4], []), ([0, 3], [1]), ([1, 4], [1]), ([0, 3, 2, 4], [1, 1, 1]), ([0, 4], [-1]),
@@ -215,6 +293,13 @@ def test_linear_layers_shapes_and_refusals(ssd):
         buf = torch.zeros((M, 2 * N), dtype=torch.bfloat16, device="cuda")
         assert torch.equal(f(r, out=buf[:, N:]), f(r)) and (buf[:, :N] == 0).all()
         assert int(f.status.item()) == 0
+    # weights that do not lie as the quantiser reads them are copied
+    w = torch.randn((70, 200), generator=gen, device="cuda").to(torch.bfloat16)
+    wide = torch.zeros((70, 208), dtype=torch.bfloat16, device="cuda")
+    wide[:, 1:201] = w
+    for x in (wide[:, 1:201], w.t().contiguous().t(), w[:1].expand(70, 200)):
+        f1, f2 = ScaledLinear(x), ScaledLinear(x.contiguous().clone())
+        assert torch.equal(f1.w.view(torch.uint8), f2.w.view(torch.uint8)) and torch.equal(f1.scale, f2.scale)
     with pytest.raises(ValueError):
         ScaledRows(4, 64).quantize(torch.zeros((5, 64), device="cuda"))
     with pytest.raises(ValueError):

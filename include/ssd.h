@@ -773,7 +773,7 @@ ssd_status ssd_quantize(int32_t rows, int32_t K, int32_t block_rows, const void*
 /* C = A W^T (+ add) of such rows and weights: with g the blocks of 128 of K,
  *     C[m][n] = sum_g a_scale[g][m] * w_scale[g][n / 128] *
  *                   sum_{k in g} A[m][k] W[n][k]   + add[m][n]
- * Both sums in float32; rounded once, to C's type.  A NaN in A goes to its row
+ * The scales' product and both sums in float32; rounded once, to C's type.  A NaN in A goes to its row
  * of C, one in W to its column.
  *   a        dev e4m3 [M][K], rows lda bytes apart; w dev e4m3 [N][K], ldw
  *   a_scale  dev float32 [ceil(K / 128)][ldas], ldas >= M

@@ -443,6 +443,7 @@ def head_norm(kind, eps, q_gain=None, q_bias=None, k_gain=None, k_bias=None) -> 
     n = HeadNorm(NORMS.get(kind, kind), eps, _ptr(q_gain), _ptr(q_bias), _ptr(k_gain), _ptr(k_bias),
                  rows[0][0], rows[1][0])
     n.d = rows[0][1] or rows[1][1]  # (checked against the cache's at the call)
+    n.held = q_gain, q_bias, k_gain, k_bias  # (the struct has addresses only)
     return n
 
 

@@ -170,8 +170,7 @@ struct CacheWork {
   }
 
   // The rank-th longest sequence (own keys beside the shared ones differ in length much more than
-  // whole sequences do, and what starts last should be short: 64 sequences of 100 to 1000 own keys
-  // beside 4352 shared 34 -> 28 us).
+  // whole sequences do, and what starts last should be short).
   static constexpr int kRanked = 8;  // of 32 sequences
   __device__ __noinline__ int32_t ranked(const CacheAttnArgs& a, int32_t rank) {
     const int32_t lane = threadIdx.x & 31;

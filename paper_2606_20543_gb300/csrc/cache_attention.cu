@@ -36,13 +36,19 @@ namespace ssd {
 
 namespace {
 
+constexpr int kStep = 16;           // keys per step
 constexpr int kWarps = 4;           // of a CTA
 constexpr int kManyWarps = 8;       // where no SM has more than one CTA: a warp alone on its
                                     // scheduler takes 900 cycles a step, most of it waiting
                                     // (8 heads over 800 keys: 12.6 us with four, 10.4)
-constexpr int kStages = 4;          // steps in flight per warp
-constexpr int kStep = 16;           // keys per step
 constexpr int kCtas = 3;            // per SM
+// Steps in flight per warp, and CTAs per SM that the registers are for.  Behind shared keys a CTA's keys
+// are few, so its set-up and way out count: more of them at once, also beside a CTA that works on
+// the shared ones (371 sequences of 67 to 712 own keys, 12/4 heads of 64: 61 us, 56).
+template <int NR, int W, bool kShared>
+constexpr int kStagesOf = kShared && NR == 1 && W == kWarps ? 3 : 4;
+template <int NR, int W, bool kShared>
+constexpr int kCtasOf = W != kWarps ? 1 : kShared && NR == 1 ? 4 : kCtas;
 constexpr int kMinTiles = 8;        // a part's fewest tiles
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kMostP = 256.f;     // a probability beyond it moves its reference
@@ -113,9 +119,10 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
 // kShared: a sequence's keys begin behind those that it shares with its group, and its rows always
 // go to the part rows.
 template <int D, int NR, int W, bool kShared>
-__global__ void __launch_bounds__(W * 32, W == kWarps ? kCtas : 1)
+__global__ void __launch_bounds__(W * 32, (kCtasOf<NR, W, kShared>))
 cache_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
                   CacheAttnArgs a, CacheAttnLaunch L) {
+  constexpr int kStages = kStagesOf<NR, W, kShared>;
   constexpr int RW = 8 * NR;          // rows of a warp
   constexpr int NT = D / 16;          // output tiles of 16 columns
   constexpr int KG = D / 64;          // groups of four mma steps of K Q^T
@@ -624,7 +631,7 @@ cudaError_t launch_mma(const CacheAttnArgs& a, const CacheMmaPlan& p, const Cach
   if (!step_map(&tk, a.cache.k, a.cache) || !step_map(&tv, a.cache.v, a.cache))
     return cudaErrorInvalidValue;
   auto smem = [](int32_t blocks) {
-    return 1024 + (size_t)W * kStages * 2 * kStep * D + (size_t)blocks * 12;
+    return 1024 + (size_t)W * kStagesOf<NR, W, kShared> * 2 * kStep * D + (size_t)blocks * 12;
   };
   const cudaError_t e =
       allow_smem(cache_attn_kernel<D, NR, W, kShared>, smem(part_blocks(kWorkRoom, kLeastBlock)));

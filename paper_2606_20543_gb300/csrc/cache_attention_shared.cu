@@ -10,9 +10,9 @@
 // which the kernel here joins.
 //
 // One token of 64 sequences of one group, 4352 shared keys and 100 to 1000 own, 32/8 heads (73 MB):
-// 38 us, 1.9 TB/s: the set-up, first tile and way out of three kernels' CTAs (18000 cycles of a
+// 37 us, 2.0 TB/s: the set-up, first tile and way out of three kernels' CTAs (18000 cycles of a
 // shared unit's 30000), and own keys at 2.5 TB/s beside the shared ones.  48 drafts of 8 groups of 4
-// over 1500 to 8000 shared keys, 16 heads: 119 us, the softmax of the tensor-core kernel.
+// over 1500 to 8000 shared keys, 16 heads: 118 us, the softmax of the tensor-core kernel.
 #include <algorithm>
 #include <cmath>
 
@@ -22,10 +22,9 @@ namespace ssd {
 
 namespace {
 
-constexpr int kSharedTiles = 6;        // fewest tiles of a part of the shared keys,
+constexpr int kSharedTiles = 3;        // fewest tiles of a part of the shared keys,
 constexpr int kSharedPartTiles = 256;  // and about the most
-constexpr int kSharedWaves = 4;        // units of the shared keys for each place of one, about: groups
-                                       // differ in length, and the longest part is what the end waits for
+constexpr double kSharedFixed = 9.5;   // tiles that a unit's set-up, way out and share of the join are worth
 
 struct SharedPlan {
   bool plain;   // every sequence by itself: ssd_cache_attention()
@@ -37,12 +36,14 @@ struct SharedPlan {
 
 // Whether sharing pays, by what both ways take (us, from the largest lengths that the call allows).  A
 // tile of the tensor-core kernel takes an SM 4.8e-3 of a GPU's us where all its warps have rows,
-// less where some have none; the mma.sync kernel streams keys at 5.6 (64-wide heads: 6.4) TB/s; the
-// join reads its parts at 3 TB/s.  Sharing starts three kernels instead of one and sets up units of
-// few tiles: 16 us (14 with the own keys in the same launch) instead of 6 (10).  Measured, shared and
-// not: 64 sequences of one group, 4352 + 1000 keys, 32/8 heads 38 and 102; 50 of 4 drafts over 18000
-// 43 and 138; 8 groups of 4, 48 drafts over 8000 + 600, 16 heads 125 and 152; 7 groups of 7 over 68 +
-// 3900 47 and 40; 8 groups of 2 over 5100 + 1900 50 and 25; 37 of 28 drafts over 290 + 90 48 and 20.
+// less where some have none; the mma.sync kernel streams keys at 5.6 (64-wide heads: 6.4) TB/s; a CTA
+// takes 0.75 us a tile however few there are of them (0.7), and 12 ns more (8, of the own keys); the
+// join reads its parts at 3 TB/s.  Sharing starts three kernels instead of one and sets up units of few tiles: 16 us (14 with
+// the own keys in the same launch) instead of 6 (10; 4 more where sequences are cut).  Measured, shared
+// and not: 64 sequences of one group, 4352 + 1000 keys, 32/8 heads 37 and 102; 50 of 4 drafts over
+// 13000, 33 and 138; 8 groups of 4, 48 drafts over 8000 + 600, 16 heads 118 and 152; 6 of 14, 6 drafts
+// over 2200 + 1400, 6/2 heads 35 and 58; 10 of 3 over 1000, 32 heads 60 and 43; 8 groups of 2 over 4900
+// + 1900, 41 and 25; 3 of 42 drafts over 1800 + 1000, 6/2 heads 22 and 17.
 bool sharing_pays(int32_t B, int32_t groups, int32_t Hq, int32_t Hkv, int32_t d, int32_t D_max,
                   int32_t L_max, int32_t max_shared, const SharedPlan& p) {
   const double G = Hq / Hkv, per_seq = D_max * G, rows = (double)B * D_max * Hq;
@@ -51,12 +52,19 @@ bool sharing_pays(int32_t B, int32_t groups, int32_t Hq, int32_t Hkv, int32_t d,
   const double stacked = tiles_r * Hkv * shared * 4.8e-3;
   const double join = rows * (std::min<double>(p.s_splits, shared / p.s_min_tiles) + 1) * d * 4 / 3e6;
   if (p.own_tc) {
+    int32_t splits, min_tiles;
+    cache_attention_tc_plan(B, Hq, Hkv, D_max, L_max, &splits, &min_tiles);
     const double full = std::ceil(std::min(per_seq, 128.0) / 32) / 4, units = B * Hkv * std::ceil(per_seq / 128);
-    const double tile = 4.8e-3 * (0.4 + 0.6 * full);
-    return 14 + stacked + units * own * tile + join < 0.9 * (10 + units * (shared + own) * tile);
+    const double tile = 4.8e-3 * (0.4 + 0.6 * full), alone = 10 + 12e-3 * units +
+                        std::max(units * (shared + own) * tile, 0.75 * (shared + own) / splits);
+    return 14 + stacked + units * (own * tile + 12e-3) + join < 0.9 * alone;
   }
+  const CacheMmaPlan plan = cache_attention_mma_plan(B, Hq, Hkv, D_max, L_max);
+  const double ctas = plan.uniform > 0 ? (double)B * plan.uniform : plan.goal;
   const double us_of_tile = (double)B * Hkv * 2 * d * 64 / (d == 128 ? 5.6e6 : 6.4e6);
-  return 16 + stacked + us_of_tile * own + join < 0.9 * (6 + us_of_tile * (shared + own));
+  const double alone = 6 + (plan.cut(B) ? 4 : 0) +
+                       std::max(us_of_tile * (shared + own), 0.7 * B * (shared + own) / ctas);
+  return 16 + stacked + us_of_tile * own + 8e-3 * B * Hkv + join < 0.9 * alone;
 }
 
 SharedPlan make_plan(int32_t B, int32_t groups, int32_t Hq, int32_t Hkv, int32_t d, int32_t D_max,
@@ -69,8 +77,16 @@ SharedPlan make_plan(int32_t B, int32_t groups, int32_t Hq, int32_t Hkv, int32_t
   if (p.plain) return p;
   // (a group's last tile may be part empty)
   const int64_t tiles_r = (B * per_seq) / 128 + groups, tiles = (max_shared + kCacheTile - 1) / kCacheTile;
-  const int64_t base = tiles_r * Hkv, units = (int64_t)kSharedWaves * 2 * device_sm_count();
-  p.s_min_tiles = (int32_t)std::min<int64_t>(kSharedPartTiles / 2, std::max<int64_t>(kSharedTiles, base * tiles / units));
+  // Parts of the shared keys: n of them make base * n units, which take an SM's share of base * n *
+  // kSharedFixed tiles beside the tiles themselves, and the end waits for a unit of tiles / n: least for
+  // n = sqrt(tiles * SMs / (base * kSharedFixed)); and no second round for a few units.  Measured (us, by
+  // n): 64 sequences of one group over 4352 keys, 32/8 heads 1: 82, 3: 41, 6: 36, 11: 39, 20: 50; 72 of
+  // two groups over 11900, 32/8 heads 5: 79, 10: 55, 20: 66, 32: 88; 48 drafts, 8 groups of 4 over 1500
+  // to 8000, 16 heads 1: 138, 2: 128, 3: 119, 5: 130, 8: 149.
+  const int64_t base = tiles_r * Hkv, places = 2 * device_sm_count();
+  int64_t n = (int64_t)std::ceil(std::sqrt(0.5 * tiles * places / (kSharedFixed * base)));
+  if (base <= places && base * n > places && 4 * base * n <= 7 * places) n = places / base;
+  p.s_min_tiles = (int32_t)std::min<int64_t>(kSharedPartTiles / 2, std::max<int64_t>(kSharedTiles, tiles / n));
   p.s_splits = (int32_t)std::max<int64_t>(1, tiles / p.s_min_tiles);
   if (base * p.s_splits > INT32_MAX / 2) {
     p.plain = true;
@@ -107,7 +123,7 @@ struct alignas(4 * N) Lanes {
 // One warp per (sequence, draft, head): the parts of its row over the shared keys and over its own.
 // CTA: a draft, eight heads.  What bounds it is the chain from the lengths over the parts' places to
 // their rows, and its code, which is fetched cold: no division of 64 bits, four parts at a time (14 KB
-// of code instead of 26 KB: 64 sequences over 4352 shared keys 39.5 -> 37.1 us, all of the call).
+// of code instead of 26 KB: 64 sequences over 4352 shared keys 39.5 -> 38.2 us, all of the call).
 template <int D>
 __global__ void __launch_bounds__(256) cache_attn_join_kernel(CacheAttnArgs a, CacheAttnLaunch L) {
   constexpr int PER = D / 32;

@@ -24,6 +24,7 @@ namespace {
 constexpr int kGroup = 128;  // entries of a scale, bytes of a stage's rows
 constexpr int kLaneRows = 128;
 constexpr int kPitch = 36;   // floats of a staged row of 32 (rows start four banks apart)
+constexpr int kOddPitch = 33;  // the same where C's rows may begin anywhere
 constexpr int kRaster = 8;   // tiles of lanes that share the columns' tiles in L2
 constexpr int kAhead = 4;    // blocks whose scales are asked for together
 constexpr int kMaxSplits = 8;
@@ -46,12 +47,12 @@ struct Shape {
   static constexpr int kStage = U * (kABytes + kCBytes);
   static constexpr int S = (224 * 1024 - kFixed) / kStage;
   static constexpr int kSmem = kFixed + S * kStage;
-  static_assert(kCols <= 512 && kAhead % U == 0 && S >= 2, "");
+  static_assert(CH == 32 && kCols <= 512 && kAhead % U == 0 && S >= 2, "");
 };
 
 struct Launch {
   int32_t tiles_l, tiles_c;
-  int32_t vec;  // C may be written, and add read, 16 bytes of C at a time
+  int32_t even;  // (C's rows begin anywhere) add's entries lie on four entries where C's do
 };
 
 __device__ __forceinline__ void cp_async4(uint32_t dst, const float* src, bool live) {
@@ -168,13 +169,13 @@ __device__ __forceinline__ void drain(uint64_t* bar, uint32_t parity) {
 }
 
 // A warp's CH columns from n0 on of `rows` rows of C from m0 on: staged with kPitch floats a row, each
-// store whole sectors of a few rows.  vec: 16 bytes a lane, all asked for (of add) before the first
-// is used; else an element.
+// store whole sectors of a few rows: 16 bytes a lane, all asked for (of add) before the first is used;
+// columns up to N that end inside of CH an element a lane.
 template <int CH>
 __device__ __forceinline__ void write_rows(const ScaledMatmulArgs& a, const float* st, int lane,
-                                           int64_t m0, int32_t rows, int32_t n0, bool vec) {
+                                           int64_t m0, int32_t rows, int32_t n0) {
   const uint16_t* add = static_cast<const uint16_t*>(a.add);
-  vec = vec && n0 + CH <= a.N;
+  const bool vec = n0 + CH <= a.N;
   if (vec && a.c_bf16) {
     constexpr int kL = CH / 8, kRows = 32 / kL;  // lanes of a row, rows of a pass
     const int32_t r0 = lane / kL, c = lane % kL * 8, n = n0 + c;
@@ -245,6 +246,110 @@ __device__ __forceinline__ void write_rows(const ScaledMatmulArgs& a, const floa
   }
 }
 
+// The same of rows that begin anywhere: eight lanes a row, four entries a lane from where C is aligned
+// for them (8 or 16 bytes), and the four entries that those leave out at both ends one by one (5848 x
+// 58870 x 172 with a sum, to bf16, rows an odd number of entries apart: an entry a lane 1383 us, this
+// 782; aligned 519; to float32 without a sum 891, 551 and 485).
+template <typename T>
+__device__ __forceinline__ void write_rows_any(const ScaledMatmulArgs& a, const float* st, int lane,
+                                               int64_t m0, int32_t rows, int32_t n0, bool even) {
+  constexpr int kTogether = 4;  // passes whose additions are asked for together
+  const int32_t i = lane & 7, r0 = lane >> 3;
+  const uint16_t* add = static_cast<const uint16_t*>(a.add);
+  if (add != nullptr) add += (m0 + r0) * a.ldadd + n0;
+  T* out = static_cast<T*>(a.c) + (m0 + r0) * a.ldc + n0;
+  st += r0 * kOddPitch;
+  auto value = [](uint32_t x) { return __uint_as_float(x << 16); };
+  auto put = [](T* p, float x) {
+    if constexpr (sizeof(T) == 2) *p = __float2bfloat16_rn(x);
+    else *p = x;
+  };
+  if (n0 + 32 > a.N) {
+#pragma unroll 1
+    for (int32_t r = r0; r < rows; r += 4, out += 4 * a.ldc, st += 4 * kOddPitch) {
+#pragma unroll 1
+      for (int32_t e = i; n0 + e < a.N; e += 8) put(out + e, st[e] + (add != nullptr ? value(add[e]) : 0.f));
+      if (add != nullptr) add += 4 * a.ldadd;
+    }
+    return;
+  }
+#pragma unroll 1
+  for (int32_t r = r0; r < r0 + 32; r += 4 * kTogether) {
+    uint2 w[kTogether];
+    uint32_t we[kTogether];
+    int32_t first[kTogether], edge[kTogether];
+    bool live[kTogether];
+#pragma unroll
+    for (int u = 0; u < kTogether; ++u) {
+      live[u] = r + 4 * u < rows && dbg_in((m0 + r + 4 * u) * a.ldc + n0, (a.M - 1) * a.ldc + a.N, a.status);
+      const int32_t s = (int32_t)(reinterpret_cast<uintptr_t>(out + 4 * u * a.ldc) / sizeof(T)) & 3;
+      first[u] = 4 * i - s;
+      edge[u] = s == 0 || i > 3 ? -1 : i < 4 - s ? i : 28 + i;
+      w[u] = make_uint2(0, 0);
+      we[u] = 0;
+      if (add != nullptr && live[u]) {
+        const uint16_t* from = add + 4 * u * a.ldadd;
+        if (first[u] >= 0) {
+          const uint16_t* f = from + first[u];
+          if (even) w[u] = *reinterpret_cast<const uint2*>(f);
+          else w[u] = make_uint2(f[0] | (uint32_t)f[1] << 16, f[2] | (uint32_t)f[3] << 16);
+        }
+        if (edge[u] >= 0) we[u] = from[edge[u]];
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < kTogether; ++u) {
+      const float* from = st + 4 * u * kOddPitch;
+      const float* f = from + max(first[u], 0);
+      const float x[4] = {f[0] + value(w[u].x), f[1] + __uint_as_float(w[u].x & 0xffff0000u),
+                          f[2] + value(w[u].y), f[3] + __uint_as_float(w[u].y & 0xffff0000u)};
+      const float y = from[max(edge[u], 0)] + value(we[u]);
+      T* to = out + 4 * u * a.ldc;
+      if (!live[u]) continue;
+      if (first[u] >= 0) {
+        if constexpr (sizeof(T) == 2)
+          *reinterpret_cast<uint2*>(to + first[u]) = make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]));
+        else
+          *reinterpret_cast<float4*>(to + first[u]) = make_float4(x[0], x[1], x[2], x[3]);
+      }
+      if (edge[u] >= 0) put(to + edge[u], y);
+    }
+    out += 4 * kTogether * a.ldc;
+    st += 4 * kTogether * kOddPitch;
+    if (add != nullptr) add += 4 * kTogether * a.ldadd;
+  }
+}
+
+// The same of 64 columns staged as bf16 (kOddPitch words a row): eight entries a lane, 16 bytes (without
+// a sum 904 us, 345; aligned 207).
+__device__ __forceinline__ void write_rows_any16(const ScaledMatmulArgs& a, const uint32_t* st, int lane,
+                                                 int64_t m0, int32_t rows, int32_t n0) {
+  const int32_t i = lane & 7, r0 = lane >> 3;
+  uint16_t* out = static_cast<uint16_t*>(a.c) + (m0 + r0) * a.ldc + n0;
+  st += r0 * kOddPitch;
+  auto entry = [&](int32_t e) { return (uint16_t)(st[e >> 1] >> (16 * (e & 1))); };
+  const bool whole = n0 + 64 <= a.N;
+#pragma unroll 2
+  for (int32_t r = r0; r < rows; r += 4, out += 4 * a.ldc, st += 4 * kOddPitch) {
+    if (!dbg_in((m0 + r) * a.ldc + n0, (a.M - 1) * a.ldc + a.N, a.status)) continue;
+    if (!whole) {
+#pragma unroll 1
+      for (int32_t e = i; n0 + e < a.N; e += 8) out[e] = entry(e);
+      continue;
+    }
+    const int32_t s = (int32_t)(reinterpret_cast<uintptr_t>(out) / 2) & 7, first = 8 * i - s;
+    const uint32_t* from = st + (max(first, 0) >> 1);
+    uint32_t w[5], v[4];
+#pragma unroll
+    for (int k = 0; k < 5; ++k) w[k] = from[k];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = __funnelshift_r(w[k], w[k + 1], 16 * (s & 1));
+    if (first >= 0) *reinterpret_cast<uint4*>(out + first) = make_uint4(v[0], v[1], v[2], v[3]);
+    const int32_t edge = i < 8 - s ? i : 56 + i;
+    if (s != 0) out[edge] = entry(edge);
+  }
+}
+
 __device__ __forceinline__ void store_one(const ScaledMatmulArgs& a, int64_t m, int32_t n, float x) {
   if (!dbg_in(m * a.ldc + n, (a.M - 1) * a.ldc + a.N, a.status)) return;
   if (a.add != nullptr)
@@ -256,7 +361,8 @@ __device__ __forceinline__ void store_one(const ScaledMatmulArgs& a, int64_t m, 
 // Registers of a pair's CTA: 384 threads of 168 at launch, then 256 of 216 and 128 of 72.
 constexpr int kRegsEpilogue = 216, kRegsOther = 72;
 
-template <bool PAIR, int TN, int U>
+// kVec: C may be written, and add read, 16 bytes of C at a time.
+template <bool PAIR, int TN, int U, bool kVec>
 __global__ void __launch_bounds__(Shape<PAIR, TN, U>::kThreads, 1)
 scaled_matmul_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmW,
                      ScaledMatmulArgs a, Launch L) {
@@ -531,7 +637,7 @@ scaled_matmul_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
       if (have_rows) {
         float* st = staging + warp * 32 * kPitch;
         const int32_t rows = (int32_t)min((int64_t)32, a.M - row0);
-        if (L.vec && a.c_bf16 && a.add == nullptr) {
+        if (a.c_bf16 && a.add == nullptr) {
           // rounded first: half of what shared memory carries (as float32 a tile took 9300 cycles)
           unsigned char* st8 = reinterpret_cast<unsigned char*>(st);
           constexpr int kBytes = 144;  // of a staged row of 64
@@ -542,15 +648,26 @@ scaled_matmul_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
 #pragma unroll
             for (int y = 0; y < CW; y += 64) {
               if (x != y) continue;
+              if constexpr (kVec) {
 #pragma unroll
-              for (int e = 0; e < 32; e += 4) {
-                const float2* v = acc + y / 2 + e;
-                *reinterpret_cast<uint4*>(st8 + lane * kBytes + e * 4) =
-                    make_uint4(pack_bf16x2(v[0].x, v[0].y), pack_bf16x2(v[1].x, v[1].y),
-                               pack_bf16x2(v[2].x, v[2].y), pack_bf16x2(v[3].x, v[3].y));
+                for (int e = 0; e < 32; e += 4) {
+                  const float2* v = acc + y / 2 + e;
+                  *reinterpret_cast<uint4*>(st8 + lane * kBytes + e * 4) =
+                      make_uint4(pack_bf16x2(v[0].x, v[0].y), pack_bf16x2(v[1].x, v[1].y),
+                                 pack_bf16x2(v[2].x, v[2].y), pack_bf16x2(v[3].x, v[3].y));
+                }
+              } else {
+#pragma unroll
+                for (int e = 0; e < 32; ++e)
+                  reinterpret_cast<uint32_t*>(st8)[lane * kOddPitch + e] =
+                      pack_bf16x2(acc[y / 2 + e].x, acc[y / 2 + e].y);
               }
             }
             __syncwarp();
+            if constexpr (!kVec) {
+              write_rows_any16(a, reinterpret_cast<uint32_t*>(st8), lane, row0, rows, c * TN + col + x);
+              continue;
+            }
             const int32_t n = c * TN + col + x + c8;
             __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.c) + (row0 + r0) * a.ldc + n;
             const unsigned char* from = st8 + r0 * kBytes + c8 * 2;
@@ -577,14 +694,25 @@ scaled_matmul_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
 #pragma unroll
           for (int y = 0; y < CW; y += CH) {
             if (x != y) continue;
+            if constexpr (kVec) {
 #pragma unroll
-            for (int e = 0; e < CH; e += 4)
-              *reinterpret_cast<float4*>(st + lane * kPitch + e) =
-                  make_float4(acc[(y + e) / 2].x, acc[(y + e) / 2].y, acc[(y + e) / 2 + 1].x,
-                              acc[(y + e) / 2 + 1].y);
+              for (int e = 0; e < CH; e += 4)
+                *reinterpret_cast<float4*>(st + lane * kPitch + e) =
+                    make_float4(acc[(y + e) / 2].x, acc[(y + e) / 2].y, acc[(y + e) / 2 + 1].x,
+                                acc[(y + e) / 2 + 1].y);
+            } else {
+#pragma unroll
+              for (int e = 0; e < CH; e += 2) {
+                st[lane * kOddPitch + e] = acc[(y + e) / 2].x;
+                st[lane * kOddPitch + e + 1] = acc[(y + e) / 2].y;
+              }
+            }
           }
           __syncwarp();
-          write_rows<CH>(a, st, lane, row0, rows, c * TN + col + x, L.vec);
+          const int32_t n = c * TN + col + x;
+          if constexpr (kVec) write_rows<CH>(a, st, lane, row0, rows, n);
+          else if (a.c_bf16) write_rows_any<__nv_bfloat16>(a, st, lane, row0, rows, n, L.even);
+          else write_rows_any<float>(a, st, lane, row0, rows, n, L.even);
         }
       }
     }
@@ -893,8 +1021,8 @@ bool rows_map(CUtensorMap* map, const void* base, int32_t K, int64_t rows, int64
 
 int32_t ceil_div(int64_t a, int64_t b) { return (int32_t)((a + b - 1) / b); }
 
-template <bool PAIR, int TN, int U>
-cudaError_t launch(const ScaledMatmulArgs& a, cudaStream_t stream) {
+template <bool PAIR, int TN, int U, bool kVec>
+cudaError_t launch_of(const ScaledMatmulArgs& a, cudaStream_t stream) {
   using H = Shape<PAIR, TN, U>;
   Launch L{};
   L.tiles_l = ceil_div(a.M, PAIR ? 2 * kLaneRows : kLaneRows);
@@ -902,19 +1030,27 @@ cudaError_t launch(const ScaledMatmulArgs& a, cudaStream_t stream) {
   CUtensorMap ta, tw;
   if (!rows_map(&ta, a.a, a.K, a.M, a.lda, kLaneRows) || !rows_map(&tw, a.w, a.K, a.N, a.ldw, H::kCRows))
     return cudaErrorInvalidValue;
-  auto kernel = scaled_matmul_kernel<PAIR, TN, U>;
+  auto kernel = scaled_matmul_kernel<PAIR, TN, U, kVec>;
   const cudaError_t e = allow_smem(kernel, H::kSmem);
   if (e != cudaSuccess) return e;
-  auto even = [&](const void* p, int64_t ld, uintptr_t bytes) {
-    return ld % (a.c_bf16 ? 8 : 4) == 0 && (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0;
-  };
-  L.vec = even(a.c, a.ldc, 16) && (a.add == nullptr || even(a.add, a.ldadd, a.c_bf16 ? 16 : 8));
+  L.even = (a.ldc - a.ldadd) % 4 == 0 && (reinterpret_cast<uintptr_t>(a.c) / (a.c_bf16 ? 2 : 4) -
+                                          reinterpret_cast<uintptr_t>(a.add) / 2) % 4 == 0;
   const int64_t tiles = (int64_t)L.tiles_l * L.tiles_c, sms = device_sm_count();
   if (PAIR)
     return launch_clusters(kernel, dim3((unsigned)(2 * std::min(tiles, sms / 2))), dim3(H::kThreads), H::kSmem,
                            stream, true, 2, ta, tw, a, L);
   return launch_kernel(kernel, dim3((unsigned)std::min(tiles, sms)), dim3(H::kThreads), H::kSmem, stream, true,
                        ta, tw, a, L);
+}
+
+template <bool PAIR, int TN, int U>
+cudaError_t launch(const ScaledMatmulArgs& a, cudaStream_t stream) {
+  auto even = [&](const void* p, int64_t ld, uintptr_t bytes) {
+    return ld % (a.c_bf16 ? 8 : 4) == 0 && (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0;
+  };
+  return even(a.c, a.ldc, 16) && (a.add == nullptr || even(a.add, a.ldadd, a.c_bf16 ? 16 : 8))
+             ? launch_of<PAIR, TN, U, true>(a, stream)
+             : launch_of<PAIR, TN, U, false>(a, stream);
 }
 
 // CTAs that a tile's blocks are cut over: a power of two (clusters of six leave places of a GPC

@@ -122,6 +122,17 @@ def test_rows_on_16_bytes_that_end_inside_of_16(ssd, M, N):
     c.check(ssd, False, add=True)
 
 
+@pytest.mark.parametrize("M,N,K", [(100, 259, 140), (600, 1000, 300), (3000, 2501, 260)])
+@pytest.mark.parametrize("more,offset", [(1, 0), (3, 1), (2, 3), (5, 0), (4, 2), (6, 5)])
+def test_rows_that_begin_anywhere(ssd, M, N, K, more, offset):
+    c = Case(M, N, K, 23, offset=offset, ldc=N + more)
+    c.check(ssd, True)
+    c.check(ssd, True, add=True)
+    c.check(ssd, True, in_place=True)
+    c.check(ssd, False)
+    c.check(ssd, False, add=True)
+
+
 def test_offsets_beyond_32_bits(ssd):
     """More than 2^31 entries of C, and of A: the last rows and columns as in a small product."""
     for M, N, K in ((40000, 60000, 128), (20, 1 << 25, 256), (1 << 24, 136, 144)):

@@ -350,10 +350,12 @@ __device__ __forceinline__ void write_rows_any16(const ScaledMatmulArgs& a, cons
   }
 }
 
+__device__ __forceinline__ float added(const ScaledMatmulArgs& a, int64_t m, int32_t n) {
+  if (a.add == nullptr) return 0.f;
+  return __uint_as_float((uint32_t)static_cast<const uint16_t*>(a.add)[m * a.ldadd + n] << 16);
+}
 __device__ __forceinline__ void store_one(const ScaledMatmulArgs& a, int64_t m, int32_t n, float x) {
   if (!dbg_in(m * a.ldc + n, (a.M - 1) * a.ldc + a.N, a.status)) return;
-  if (a.add != nullptr)
-    x += __uint_as_float((uint32_t)static_cast<const uint16_t*>(a.add)[m * a.ldadd + n] << 16);
   if (a.c_bf16) static_cast<__nv_bfloat16*>(a.c)[m * a.ldc + n] = __float2bfloat16_rn(x);
   else static_cast<float*>(a.c)[m * a.ldc + n] = x;
 }
@@ -918,6 +920,11 @@ scaled_matmul_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_c
     uint32_t half = 0;
 #pragma unroll 1
     for (int32_t i = first; i < total && ok; i += step) {
+      if (a.add != nullptr && tid < 2 * TN) {  // what is added, on its way to L2 meanwhile
+        const int32_t c = i / tiles_w, m = c * TN + (tid >> 1), n = (i - c * tiles_w) * kLaneRows + (tid & 1) * 64;
+        if (m < a.M && n < a.N)
+          asm volatile("prefetch.global.L2 [%0];" ::"l"(static_cast<const uint16_t*>(a.add) + m * a.ldadd + n));
+      }
       float2 acc[TN / 2];
 #pragma unroll
       for (int e = 0; e < TN / 2; ++e) acc[e] = make_float2(0.f, 0.f);
@@ -969,9 +976,17 @@ scaled_matmul_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_c
       } else {
         const int32_t c = i / tiles_w, nn = (i - c * tiles_w) * kLaneRows + tid;
         if (nn < a.N) {
+          // (what is added is asked for 16 rows at a time)
 #pragma unroll
-          for (int e = 0; e < TN; ++e)
-            if (c * TN + e < a.M) store_one(a, c * TN + e, nn, e & 1 ? acc[e / 2].y : acc[e / 2].x);
+          for (int e0 = 0; e0 < TN; e0 += 16) {
+            float x[16];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) x[e] = c * TN + e0 + e < a.M ? added(a, c * TN + e0 + e, nn) : 0.f;
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+              if (c * TN + e0 + e < a.M)
+                store_one(a, c * TN + e0 + e, nn, (e & 1 ? acc[(e0 + e) / 2].y : acc[(e0 + e) / 2].x) + x[e]);
+          }
         }
       }
     }
@@ -989,13 +1004,14 @@ scaled_matmul_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_c
       const uint32_t at = smem_u32(smem) + tid * 4;
       for (int32_t t = rank; t < live; t += splits) {
         float v[kMaxSplits];
+        const float more = added(a, c * TN + t, n);
 #pragma unroll
         for (int32_t r = 0; r < kMaxSplits; ++r)
           v[r] = r < splits ? ld_peer(peer_addr(at + t * kLaneRows * 4, r)) : 0.f;
         float x = 0.f;
 #pragma unroll
         for (int32_t r = 0; r < kMaxSplits; ++r) x += v[r];
-        store_one(a, c * TN + t, n, x);
+        store_one(a, c * TN + t, n, x + more);
       }
     }
     cluster_sync_all();
@@ -1054,12 +1070,16 @@ cudaError_t launch(const ScaledMatmulArgs& a, cudaStream_t stream) {
 }
 
 // CTAs that a tile's blocks are cut over: a power of two (clusters of six leave places of a GPC
-// empty: 48 tiles of 32 blocks 11.9 us, four CTAs each 8.7, two 8.9, one 11.1), and all at work at
-// once (32 tiles of 96 blocks: eight 12.0, four 12.3, one 27.0; 48 of 32: eight 11.0).
+// empty: 48 tiles of 32 blocks 11.9 us, four CTAs each 8.2, two 8.7, one 11.4), and all at work at
+// once (32 tiles of 96 blocks: eight 12.0, four 12.3, one 27.0; 48 of 32: eight 10.0), of short sums on an
+// SM each (30 tiles of 9 blocks: eight 6.2, four 5.2).  The cluster's sums cost about a microsecond:
+// not for fewer than six blocks (52 tiles of 5: two 6.0, one 5.1), and in two only for many (88 tiles of
+// 13: two 11.0, one 7.9; 95 of 57: 19.5 and 22.6).
 int32_t few_splits(int32_t tiles, int32_t blocks, int32_t sms) {
+  const int64_t most = blocks >= 24 ? sms * 7 / 4 : sms;
   int32_t n = 1;
-  while (n < kMaxSplits && (int64_t)tiles * n * 2 <= sms * 7 / 4 && blocks >= n * 4) n *= 2;
-  return n;
+  while (n < kMaxSplits && (int64_t)tiles * n * 2 <= most && blocks >= n * 2) n *= 2;
+  return blocks < 6 || (n == 2 && blocks < 24) ? 1 : n;
 }
 
 template <int TN, int U>
@@ -1096,8 +1116,8 @@ cudaError_t launch_scaled_matmul(const ScaledMatmulArgs& a, cudaStream_t stream)
     const int64_t tiles = (int64_t)ceil_div(a.M, rows) * ceil_div(a.N, cols);
     return ceil_div(tiles, places) * (blocks * block + rest);
   };
-  const int64_t c256 = cost(256, 256, sms / 2, 500, 5500), p128 = cost(256, 128, sms / 2, 315, 4000),
-                c128 = cost(128, 128, sms, 360, 3500);
+  const int64_t c256 = cost(256, 256, sms / 2, 500, 5500), p128 = cost(256, 128, sms / 2, 315, 3000),
+                c128 = cost(128, 128, sms, 340, 2500);
   if (c256 < p128 && c256 < c128) return launch<true, 256, 1>(a, stream);
   return p128 <= c128 ? launch<true, 128, 2>(a, stream) : launch<false, 128, 2>(a, stream);
 }

@@ -28,6 +28,7 @@ constexpr int kOddPitch = 33;  // the same where C's rows may begin anywhere
 constexpr int kRaster = 8;   // tiles of lanes that share the columns' tiles in L2
 constexpr int kAhead = 4;    // blocks whose scales are asked for together
 constexpr int kMaxSplits = 8;
+constexpr int64_t kOftenBytes = 32 << 20;  // most of A to hold in L2, about a quarter
 
 template <bool PAIR, int TN, int U>
 struct Shape {
@@ -52,6 +53,7 @@ struct Shape {
 
 struct Launch {
   int32_t tiles_l, tiles_c;
+  int32_t often;  // A stays in L2
   int32_t even;  // (C's rows begin anywhere) add's entries lie on four entries where C's do
 };
 
@@ -436,7 +438,7 @@ scaled_matmul_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
   if (warp == EW || warp == EW + 2) {
     // ---------------------------------------------------------- producers
     const bool of_a = warp == EW, leader = elect_one();
-    const uint64_t pol = policy_evict_normal();
+    const uint64_t pol = of_a && L.often ? policy_evict_last() : policy_evict_normal();
     const int32_t block_bytes = of_a ? a_bytes : H::kCBytes, at = of_a ? 0 : U * a_bytes;
     const CUtensorMap* map = of_a ? &tmA : &tmW;
     const uint32_t full0 = PAIR ? peer_addr(smem_u32(full), 0) : 0;
@@ -740,12 +742,14 @@ scaled_matmul_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
 // add their sums up through distributed shared memory in the order of their ranks.
 template <int TN, int U>
 struct Few {
-  static constexpr int kThreads = 6 * 32;             // epilogue 4, copies, products
-  static constexpr int kCols = 2 * U * TN < 32 ? 32 : 2 * U * TN;
+  static constexpr int EW = TN < 64 ? 4 : 8;          // epilogue warps,
+  static constexpr int CW = TN / (EW / 4);            // rows of A of one
+  static constexpr int kThreads = (EW + 2) * 32;      // and copies, products
+  static constexpr int kCols = 2 * U * TN;            // two units in TMEM
   static constexpr int kCBytes = TN * kGroup, kWBytes = kLaneRows * kGroup;
   static constexpr int kStage = U * (kWBytes + kCBytes);
-  static constexpr int kSlot = TN + 4;                // scales of a block: A's, W's
-  static constexpr int kScales = 2 * kAhead * 4 * kSlot * 4;
+  static constexpr int kSlot = CW + 4;                // scales of a warp's block: A's, W's
+  static constexpr int kScales = 2 * kAhead * EW * kSlot * 4;
   static constexpr int kFixed = 1024 + kScales;
   static constexpr int S = (112 * 1024 - kFixed) / kStage;
   static constexpr int kSmem = kFixed + S * kStage;
@@ -757,12 +761,12 @@ __global__ void __launch_bounds__(Few<TN, U>::kThreads, 2)
 scaled_matmul_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmW,
                          ScaledMatmulArgs a, int32_t tiles_w, int32_t total, int32_t splits) {
   using H = Few<TN, U>;
-  constexpr int S = H::S;
+  constexpr int S = H::S, B = 2, EW = H::EW, CW = H::CW;
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>(
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   float* scales = reinterpret_cast<float*>(smem + S * H::kStage);
-  __shared__ uint64_t full[S], empty[S], tfull[2], tempty[2];
+  __shared__ uint64_t full[S], empty[S], tfull[B], tempty[B];
   __shared__ uint32_t tmem_slot;
   pdl_wait();
 
@@ -772,22 +776,22 @@ scaled_matmul_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_c
   const int32_t blocks = (a.K + kGroup - 1) / kGroup;
   const int32_t kb_lo = (int32_t)((int64_t)blocks * rank / splits);
   const int32_t kb_hi = (int32_t)((int64_t)blocks * (rank + 1) / splits);
-  if (warp == 4 && lane < 2) prefetch_tensormap(lane == 0 ? &tmA : &tmW);
-  if (tid == 128) {
+  if (warp == EW && lane < 2) prefetch_tensormap(lane == 0 ? &tmA : &tmW);
+  if (tid == EW * 32) {
     for (int i = 0; i < S; ++i) {
       mbar_init(&full[i], 1);
       mbar_init(&empty[i], 1);
     }
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < B; ++i) {
       mbar_init(&tfull[i], 1);
-      mbar_init(&tempty[i], 4);
+      mbar_init(&tempty[i], EW);
     }
     fence_barrier_init();
   }
   __syncwarp();
   uint32_t tmem = 0;
-  if (warp != 4) {  // (the copies begin without the others)
-    if (warp == 5) {
+  if (warp != EW) {  // (the copies begin without the others)
+    if (warp == EW + 1) {
       tmem_alloc(&tmem_slot, H::kCols);
       tmem_relinquish();
       tc_fence_before();
@@ -797,7 +801,7 @@ scaled_matmul_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_c
     tmem = tmem_slot;
   }
   // Tile i: rows (i % tiles_w) * 128 of W and (i / tiles_w) * TN of A.
-  if (warp == 4) {
+  if (warp == EW) {
     // ------------------------------------------------------------- copies
     const bool leader = elect_one();
     const uint64_t once = policy_evict_first(), often = policy_evict_last();
@@ -837,7 +841,7 @@ scaled_matmul_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_c
     if (!begun) __syncthreads();
     if (!ok)
       for (int32_t u = max(0, n - S); u < n; ++u) drain(&full[u % S], (u / S) & 1);
-  } else if (warp == 5) {
+  } else if (warp == EW + 1) {
     // ----------------------------------------------------------- products
     constexpr uint32_t kIdesc = idesc_e4m3(128, TN);
     const uint32_t base = warp_uniform(smem_u32(smem)), tm = warp_uniform(tmem);
@@ -849,8 +853,8 @@ scaled_matmul_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_c
     for (int32_t i = first; i < total && ok; i += step) {
 #pragma unroll 1
       for (int32_t kb = kb_lo; kb < kb_hi; kb += U, ++n) {
-        const int b = n & 1;
-        if (n >= 2) ok = wait_warp(&tempty[b], ((n >> 1) - 1) & 1, a.status);
+        const int b = n % B;
+        if (n >= B) ok = wait_warp(&tempty[b], (n / B - 1) & 1, a.status);
         // (last: W is what these products wait for)
         ok = ok && wait_warp(&full[s], ph, a.status);
         if (!ok) break;
@@ -877,10 +881,12 @@ scaled_matmul_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_c
         }
       }
     }
-    if (!ok && n > 0) drain(&tfull[(n - 1) & 1], ((n - 1) >> 1) & 1);
+    if (!ok && n > 0) drain(&tfull[(n - 1) % B], ((n - 1) / B) & 1);
   } else {
     // ----------------------------------------------------------- epilogue
-    const uint32_t lane_off = (uint32_t)(warp * 32) << 16;
+    // a lane's row of W, the warp's first row of A
+    const int32_t wrow = (warp & 3) * 32 + lane, col = (warp >> 2) * CW;
+    const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
     // Scales come by cp.async, kAhead blocks together and as many ahead, into slots that only this
     // warp reads: [2][kAhead][warp][A's, W's].
     const uint32_t scales_at = smem_u32(scales) + warp * H::kSlot * 4;
@@ -893,20 +899,20 @@ scaled_matmul_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_c
       if (next_kb >= kb_hi && next_tile < total) {
         const int32_t c = next_tile / tiles_w;
         next_w = a.w_scale + kb_lo * a.ldws + (next_tile - c * tiles_w);
-        next_a = a.a_scale + kb_lo * a.ldas + c * TN;
-        live = a.M - c * TN;
+        live = max(0, min(CW, a.M - c * TN - col));
+        next_a = a.a_scale + kb_lo * a.ldas + (live > 0 ? c * TN + col : 0);
         next_tile += step;
         next_kb = kb_lo;
       }
-      const uint32_t to = scales_at + next_half * (kAhead * 4 * H::kSlot * 4);
+      const uint32_t to = scales_at + next_half * (kAhead * EW * H::kSlot * 4);
 #pragma unroll 1
       for (int u = 0; u < kAhead && next_kb + u < kb_hi; ++u) {
 #pragma unroll
-        for (int t = 0; t < TN; t += 32)
-          if (t + lane < TN)
-            cp_async4(to + u * 4 * H::kSlot * 4 + (t + lane) * 4, next_a + min(t + lane, live - 1),
+        for (int t = 0; t < CW; t += 32)
+          if (t + lane < CW)
+            cp_async4(to + u * EW * H::kSlot * 4 + (t + lane) * 4, next_a + max(0, min(t + lane, live - 1)),
                       t + lane < live);
-        if (lane == 0) cp_async4(to + u * 4 * H::kSlot * 4 + TN * 4, next_w, true);
+        if (lane == 0) cp_async4(to + u * EW * H::kSlot * 4 + CW * 4, next_w, true);
         next_a += a.ldas;
         next_w += a.ldws;
       }
@@ -925,9 +931,9 @@ scaled_matmul_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_c
         if (m < a.M && n < a.N)
           asm volatile("prefetch.global.L2 [%0];" ::"l"(static_cast<const uint16_t*>(a.add) + m * a.ldadd + n));
       }
-      float2 acc[TN / 2];
+      float2 acc[CW / 2];
 #pragma unroll
-      for (int e = 0; e < TN / 2; ++e) acc[e] = make_float2(0.f, 0.f);
+      for (int e = 0; e < CW / 2; ++e) acc[e] = make_float2(0.f, 0.f);
 #pragma unroll 1
       for (int32_t kb = kb_lo; kb < kb_hi; kb += U, ++n) {
         if ((kb - kb_lo) % kAhead == 0) {
@@ -936,56 +942,64 @@ scaled_matmul_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_c
           half = next_half ^ 1u;
           ask();
         }
-        const float* sc = scales + ((half * kAhead + (kb - kb_lo) % kAhead) * 4 + warp) * H::kSlot;
-        const int b = n & 1;
-        ok = wait_warp(&tfull[b], (n >> 1) & 1, a.status);
+        const float* sc = scales + ((half * kAhead + (kb - kb_lo) % kAhead) * EW + warp) * H::kSlot;
+        const int b = n % B;
+        ok = wait_warp(&tfull[b], (n / B) & 1, a.status);
         if (!ok) break;
         tc_fence_after();
+        // (a unit's blocks lie side by side: where a warp takes all of their columns, one read)
+        constexpr int kReads = CW == TN && TN > 16 ? 1 : U, kOf = U / kReads;
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-          uint32_t w[TN];
-          tmem_ask(tmem + lane_off + (b * U + u) * TN, w);
-          const float4* s4 = reinterpret_cast<const float4*>(sc + u * 4 * H::kSlot);
-          const float2 ws = make_float2(sc[u * 4 * H::kSlot + TN], sc[u * 4 * H::kSlot + TN]);
+        for (int q = 0; q < kReads; ++q) {
+          uint32_t w[kOf * CW];
+          tmem_ask(tmem + lane_off + (b * U + q) * TN + col, w);
+          float ws[kOf];
+#pragma unroll
+          for (int u = 0; u < kOf; ++u) ws[u] = sc[(q + u) * EW * H::kSlot + CW];
           tmem_have(w);
-          if (u + 1 == U) {
+          if (q + 1 == kReads) {
             tc_fence_before();
             __syncwarp();
             arrive_lane0(&tempty[b], lane);
           }
-          if (U > 1 && kb + u >= kb_hi) continue;
 #pragma unroll
-          for (int e = 0; e < TN; e += 4) {
-            const float4 x = s4[e / 4];
-            const float2 zero = make_float2(0.f, 0.f);
-            const float2 lo = make_float2(__uint_as_float(w[e]), __uint_as_float(w[e + 1]));
-            const float2 hi = make_float2(__uint_as_float(w[e + 2]), __uint_as_float(w[e + 3]));
-            acc[e / 2] = ffma2(lo, ffma2(make_float2(x.x, x.y), ws, zero), acc[e / 2]);
-            acc[e / 2 + 1] = ffma2(hi, ffma2(make_float2(x.z, x.w), ws, zero), acc[e / 2 + 1]);
+          for (int u = 0; u < kOf; ++u) {
+            if (U > 1 && kb + q + u >= kb_hi) continue;
+            const float4* s4 = reinterpret_cast<const float4*>(sc + (q + u) * EW * H::kSlot);
+            const float2 ws2 = make_float2(ws[u], ws[u]), zero = make_float2(0.f, 0.f);
+#pragma unroll
+            for (int e = 0; e < CW; e += 4) {
+              const float4 x = s4[e / 4];
+              const uint32_t* v = w + u * CW + e;
+              const float2 lo = make_float2(__uint_as_float(v[0]), __uint_as_float(v[1]));
+              const float2 hi = make_float2(__uint_as_float(v[2]), __uint_as_float(v[3]));
+              acc[e / 2] = ffma2(lo, ffma2(make_float2(x.x, x.y), ws2, zero), acc[e / 2]);
+              acc[e / 2 + 1] = ffma2(hi, ffma2(make_float2(x.z, x.w), ws2, zero), acc[e / 2 + 1]);
+            }
           }
         }
       }
       if (!ok) break;
       if (splits > 1) {  // to the cluster's sums, below (one tile a CTA)
-        float* mine = reinterpret_cast<float*>(smem) + tid;
+        float* mine = reinterpret_cast<float*>(smem) + col * kLaneRows + wrow;
 #pragma unroll
-        for (int e = 0; e < TN / 2; ++e) {
+        for (int e = 0; e < CW / 2; ++e) {
           mine[2 * e * kLaneRows] = acc[e].x;
           mine[(2 * e + 1) * kLaneRows] = acc[e].y;
         }
       } else {
-        const int32_t c = i / tiles_w, nn = (i - c * tiles_w) * kLaneRows + tid;
+        const int32_t c = i / tiles_w, nn = (i - c * tiles_w) * kLaneRows + wrow, m0 = c * TN + col;
         if (nn < a.N) {
           // (what is added is asked for 16 rows at a time)
 #pragma unroll
-          for (int e0 = 0; e0 < TN; e0 += 16) {
+          for (int e0 = 0; e0 < CW; e0 += 16) {
             float x[16];
 #pragma unroll
-            for (int e = 0; e < 16; ++e) x[e] = c * TN + e0 + e < a.M ? added(a, c * TN + e0 + e, nn) : 0.f;
+            for (int e = 0; e < 16; ++e) x[e] = m0 + e0 + e < a.M ? added(a, m0 + e0 + e, nn) : 0.f;
 #pragma unroll
             for (int e = 0; e < 16; ++e)
-              if (c * TN + e0 + e < a.M)
-                store_one(a, c * TN + e0 + e, nn, (e & 1 ? acc[(e0 + e) / 2].y : acc[(e0 + e) / 2].x) + x[e]);
+              if (m0 + e0 + e < a.M)
+                store_one(a, m0 + e0 + e, nn, (e & 1 ? acc[(e0 + e) / 2].y : acc[(e0 + e) / 2].x) + x[e]);
           }
         }
       }
@@ -998,27 +1012,36 @@ scaled_matmul_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_c
   if (splits > 1) {
     cluster_sync_all();
     // every CTA of the cluster adds up the rows of A that are its rank's
-    const int32_t c = first / tiles_w, n = (first - c * tiles_w) * kLaneRows + tid;
-    const int32_t live = min(TN, a.M - c * TN);
-    if (tid < kLaneRows && n < a.N) {
-      const uint32_t at = smem_u32(smem) + tid * 4;
-      for (int32_t t = rank; t < live; t += splits) {
-        float v[kMaxSplits];
-        const float more = added(a, c * TN + t, n);
+    const int32_t c = first / tiles_w, n = (first - c * tiles_w) * kLaneRows + (tid & 127);
+    const int32_t live = min(TN, a.M - c * TN), step = splits * (EW / 4);
+    if (tid < EW * 32 && n < a.N) {
+      constexpr int kTogether = CW / 16;  // rows whose sums are asked for together
+      const uint32_t at = smem_u32(smem) + (tid & 127) * 4;
+#pragma unroll 1
+      for (int32_t t0 = rank + (tid >> 7) * splits; t0 < live; t0 += kTogether * step) {
+        float v[kTogether][kMaxSplits], more[kTogether];
 #pragma unroll
-        for (int32_t r = 0; r < kMaxSplits; ++r)
-          v[r] = r < splits ? ld_peer(peer_addr(at + t * kLaneRows * 4, r)) : 0.f;
-        float x = 0.f;
+        for (int u = 0; u < kTogether; ++u) {
+          const int32_t t = min(t0 + u * step, live - 1);
+          more[u] = added(a, c * TN + t, n);
 #pragma unroll
-        for (int32_t r = 0; r < kMaxSplits; ++r) x += v[r];
-        store_one(a, c * TN + t, n, x + more);
+          for (int32_t r = 0; r < kMaxSplits; ++r)
+            v[u][r] = r < splits ? ld_peer(peer_addr(at + t * kLaneRows * 4, r)) : 0.f;
+        }
+#pragma unroll
+        for (int u = 0; u < kTogether; ++u) {
+          float x = 0.f;
+#pragma unroll
+          for (int32_t r = 0; r < kMaxSplits; ++r) x += v[u][r];
+          if (t0 + u * step < live) store_one(a, c * TN + t0 + u * step, n, x + more[u]);
+        }
       }
     }
     cluster_sync_all();
   } else {
     __syncthreads();
   }
-  if (warp == 5) {
+  if (warp == EW + 1) {
     tc_fence_after();
     tmem_dealloc(tmem, H::kCols);
   }
@@ -1049,6 +1072,9 @@ cudaError_t launch_of(const ScaledMatmulArgs& a, cudaStream_t stream) {
   auto kernel = scaled_matmul_kernel<PAIR, TN, U, kVec>;
   const cudaError_t e = allow_smem(kernel, H::kSmem);
   if (e != cudaSuccess) return e;
+  // Where all SMs read the same few lines of A at once, L2 serves them much faster under this policy
+  // (152 tiles of 64 rows, K 1024: 15.5 us, 6.9; 128 rows, 512: 6.3, 4.9).
+  L.often = (int64_t)a.M * a.K <= kOftenBytes;
   L.even = (a.ldc - a.ldadd) % 4 == 0 && (reinterpret_cast<uintptr_t>(a.c) / (a.c_bf16 ? 2 : 4) -
                                           reinterpret_cast<uintptr_t>(a.add) / 2) % 4 == 0;
   const int64_t tiles = (int64_t)L.tiles_l * L.tiles_c, sms = device_sm_count();
@@ -1059,14 +1085,16 @@ cudaError_t launch_of(const ScaledMatmulArgs& a, cudaStream_t stream) {
                        ta, tw, a, L);
 }
 
-template <bool PAIR, int TN, int U>
-cudaError_t launch(const ScaledMatmulArgs& a, cudaStream_t stream) {
+// Whether C may be written, and add read, 16 bytes of C at a time.
+bool on_vectors(const ScaledMatmulArgs& a) {
   auto even = [&](const void* p, int64_t ld, uintptr_t bytes) {
     return ld % (a.c_bf16 ? 8 : 4) == 0 && (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0;
   };
-  return even(a.c, a.ldc, 16) && (a.add == nullptr || even(a.add, a.ldadd, a.c_bf16 ? 16 : 8))
-             ? launch_of<PAIR, TN, U, true>(a, stream)
-             : launch_of<PAIR, TN, U, false>(a, stream);
+  return even(a.c, a.ldc, 16) && (a.add == nullptr || even(a.add, a.ldadd, a.c_bf16 ? 16 : 8));
+}
+template <bool PAIR, int TN, int U>
+cudaError_t launch(const ScaledMatmulArgs& a, bool vec, cudaStream_t stream) {
+  return vec ? launch_of<PAIR, TN, U, true>(a, stream) : launch_of<PAIR, TN, U, false>(a, stream);
 }
 
 // CTAs that a tile's blocks are cut over: a power of two (clusters of six leave places of a GPC
@@ -1083,7 +1111,7 @@ int32_t few_splits(int32_t tiles, int32_t blocks, int32_t sms) {
 }
 
 template <int TN, int U>
-cudaError_t launch_few(const ScaledMatmulArgs& a, cudaStream_t stream) {
+cudaError_t launch_few(const ScaledMatmulArgs& a, int32_t splits, cudaStream_t stream) {
   using H = Few<TN, U>;
   CUtensorMap ta, tw;
   if (!rows_map(&ta, a.a, a.K, a.M, a.lda, TN) || !rows_map(&tw, a.w, a.K, a.N, a.ldw, kLaneRows))
@@ -1092,34 +1120,46 @@ cudaError_t launch_few(const ScaledMatmulArgs& a, cudaStream_t stream) {
   const cudaError_t e = allow_smem(kernel, H::kSmem);
   if (e != cudaSuccess) return e;
   const int32_t tiles_w = ceil_div(a.N, kLaneRows), total = tiles_w * ceil_div(a.M, TN);
-  const int32_t blocks = ceil_div(a.K, kGroup), sms = device_sm_count();
-  const int32_t splits = few_splits(total, blocks, sms);
   if (splits > 1)
     return launch_clusters(kernel, dim3((unsigned)(total * splits)), dim3(H::kThreads), H::kSmem, stream, true,
                            splits, ta, tw, a, tiles_w, total, splits);
-  return launch_kernel(kernel, dim3((unsigned)std::min(total, 2 * sms)), dim3(H::kThreads), H::kSmem, stream,
+  return launch_kernel(kernel, dim3((unsigned)std::min(total, 2 * device_sm_count())), dim3(H::kThreads), H::kSmem, stream,
                        true, ta, tw, a, tiles_w, total, splits);
 }
 
 }  // namespace
 
 cudaError_t launch_scaled_matmul(const ScaledMatmulArgs& a, cudaStream_t stream) {
-  if (a.M <= 16) return launch_few<16, 2>(a, stream);
-  if (a.M <= 32) return launch_few<32, 2>(a, stream);
-  if (a.M <= 64) return launch_few<64, 2>(a, stream);
-  // Nanoseconds of a wave of tiles, about: what a block takes, and a tile's way in and out.  Tiles of a
-  // pair are better for their size and worse where they leave SMs idle.  Measured (us, 256 x 256
-  // and 256 x 128 of a pair, 128 x 128): 1024 x 4096 x 4096 21.9, 25.1, 28.0; 500 x 2000 x 4096 21.3,
-  // 14.3, 15.4; 300 x 5000 x 4096 21.7, 25.0, 16.0; 2000 x 3000 x 4096 40.2, 35.8, 38.3.
   const int64_t blocks = ceil_div(a.K, kGroup), sms = device_sm_count();
-  auto cost = [&](int32_t rows, int32_t cols, int64_t places, int64_t block, int64_t rest) {
+  if (a.M <= 64) {
+    // With W's rows on the lanes the blocks are cut, and W is read once at the most tiles; with A's,
+    // a CTA gets going sooner and takes 0.26 us a block instead of 0.24 (16 rows), 0.25 (32), 0.35 (64).
+    // Measured (us, 96 tiles of 128 of W): 64 rows, 2 blocks 5.8 and 4.2, 16 10.6 and 7.8, 32 18.5 and
+    // 12.0, 64 26.7 and 28.8; 48 tiles of 32 rows, 16 9.0 and 7.8, but 152 9.5 and 11.8 (all of them at the
+    // same lines of A); 16 of 64 rows, 64 blocks 11.1 and 21.4; 304 of 32 29.2 and 33.6.
+    const int32_t tiles = ceil_div(a.N, kLaneRows), n = few_splits(tiles, (int32_t)blocks, (int32_t)sms);
+    const bool wide = tiles <= sms && blocks <= 48 && a.M > 16 &&
+                      (a.M > 32 ? n == 1 || blocks < 12 || (n < 4 && blocks <= 32)
+                                : n == 1 && (tiles * blocks <= 1024 || blocks >= 24));
+    if (a.M <= 16) return launch_few<16, 2>(a, n, stream);
+    if (!wide) return a.M <= 32 ? launch_few<32, 2>(a, n, stream) : launch_few<64, 2>(a, n, stream);
+  }
+  // Nanoseconds, about: of a launch, and for every round of tiles what a block takes and a tile's way out
+  // (of 256 and of 128 columns).  Tiles of a pair are better for their size and worse where they leave SMs
+  // idle.  Measured (us, 256 x 256 and 256 x 128 of a pair, 128 x 128): 1024 x 4096 x 4096 with a sum 24.5,
+  // 28, 27; 200 x 5000 x 2050 14.6, 10.3, 9.6; 264 x 24448 x 9134 124, 144, 138; 5848 x 58870 x 172 207, -,
+  // 312; to float32 with rows anywhere 551, -, 520.  Over 200 drawn products 1% above the best of the three.
+  const bool vec = on_vectors(a);
+  const int64_t out256 = a.add != nullptr ? (vec ? 6900 : 10100) : a.c_bf16 ? (vec ? 2700 : 3900) : vec ? 5900 : 6600;
+  const int64_t out128 = a.add != nullptr ? (vec ? 3200 : 4800) : a.c_bf16 ? (vec ? 1800 : 2200) : vec ? 2400 : 3300;
+  auto cost = [&](int32_t rows, int32_t cols, int64_t places, int64_t fixed, int64_t block, int64_t out) {
     const int64_t tiles = (int64_t)ceil_div(a.M, rows) * ceil_div(a.N, cols);
-    return ceil_div(tiles, places) * (blocks * block + rest);
+    return fixed + ceil_div(tiles, places) * (blocks * block + out);
   };
-  const int64_t c256 = cost(256, 256, sms / 2, 500, 5500), p128 = cost(256, 128, sms / 2, 315, 3000),
-                c128 = cost(128, 128, sms, 340, 2500);
-  if (c256 < p128 && c256 < c128) return launch<true, 256, 1>(a, stream);
-  return p128 <= c128 ? launch<true, 128, 2>(a, stream) : launch<false, 128, 2>(a, stream);
+  const int64_t c256 = cost(256, 256, sms / 2, 4000, 500, out256), p128 = cost(256, 128, sms / 2, 3300, 315, out128),
+                c128 = cost(128, 128, sms, 2500, 340, out128);
+  if (c256 < p128 && c256 < c128) return launch<true, 256, 1>(a, vec, stream);
+  return p128 < c128 ? launch<true, 128, 2>(a, vec, stream) : launch<false, 128, 2>(a, vec, stream);
 }
 
 }  // namespace ssd

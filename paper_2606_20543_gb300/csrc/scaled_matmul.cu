@@ -9,7 +9,11 @@
 //
 // More than 64 rows: the rows of A are the 128 lanes of a tile (the scales of a block are then one
 // number a thread), 128 rows of W its columns; or a CTA pair (cta_group::2) has 128 lanes each and 128
-// or 256 columns.  Up to 64 rows: the other way round (scaled_matmul_few_kernel).
+// or 256 columns.  Up to 64 rows, mostly: the other way round (scaled_matmul_few_kernel).
+//
+// 17408 x 12288 x 4096 (1752 GFLOP) 777 us, 2250 TFLOP/s: 560 ns a block of 256 x 256 of a pair, of which
+// the products are 340; two TMEM buffers' round trips bound it, and the copies alone would take 410.
+// 1024 x 4096 x 4096 with a sum 24.2 us; 16 x 65536 x 4096 (273 MB) 42 us, the copy rate.
 //
 // Barriers count units of U blocks: a wait that is satisfied already costs a warp about 100
 // cycles, a commit of products as much.

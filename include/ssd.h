@@ -684,7 +684,8 @@ ssd_status ssd_cache_attention(const ssd_grid* grid, const ssd_block_cache* cach
  * entries are equal; shared[g] may be 0).  The same o and lse, but for the order
  * of sums; the shared keys are read once for the rows of a group instead of once
  * a sequence.  Shared blocks hold committed tokens: shared[g] * block <=
- * cache_len[b] for every sequence of the group that has drafts.
+ * cache_len[b] for every sequence of the group that has drafts.  (A NaN in a
+ * shared token's value: "the rows of its head" there are those of the group.)
  *   group_start  dev int32 [groups + 1]: 0 ... B, ascending; shared dev int32
  *                [groups], at most max_shared (host, at most max_blocks)
  *   workspace    >= ssd_cache_attention_shared_workspace(..., max_blocks *

@@ -155,7 +155,7 @@ template <bool kShared>
 struct Rows {};
 template <>
 struct Rows<true> {
-  int32_t at[kBM], pos[kBM], start[kBM], least[4], count[8];
+  int32_t at[kBM], pos[kBM], start[kBM], least[4], begins[4], count[8];
 };
 template <bool kShared>
 struct alignas(16) Shared : Rows<kShared> {
@@ -331,7 +331,7 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
         rows_total = all * G;
         if (row0 >= rows_total) return;
       }
-      int32_t least = 0x7fffffff;
+      int32_t least = 0x7fffffff, begins = 0x7fffffff;
       if (tid < kBM) {
         const int32_t r = row0 + tid;
         int32_t at = -1, pos = 0x7fffffff, from = 0;
@@ -357,13 +357,15 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
             pos = cache_flat_pos(a, rb, c, draft);
             if (a.key_start != nullptr) from = min(cache, max(0, a.key_start[rb]));
             least = rb;
+            begins = from;
           }
         }
         sh.at[tid] = at;
         sh.pos[tid] = pos;
         sh.start[tid] = from;
         least = __reduce_min_sync(0xffffffffu, least);
-        if (lane == 0) sh.least[warp] = least;
+        begins = __reduce_min_sync(0xffffffffu, begins);
+        if (lane == 0) sh.least[warp] = least, sh.begins[warp] = begins;
       }
       __syncthreads();
       // the first of the tile's sequences names the blocks
@@ -379,7 +381,10 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
     t_hi = (int32_t)(q * (split + 1) + r * (split + 1) / (uint32_t)parts);
   }
   const int32_t k_lo = base + t_lo * KT, k_hi = min(Lk, base + t_hi * KT), ntiles = t_hi - t_lo;
-  const int32_t start = a.key_start != nullptr && !stacked ? min(Lk, max(0, a.key_start[b])) : 0;
+  // (stacked: the first key that any row sees; those before it may be anything)
+  int32_t start = a.key_start != nullptr && !stacked ? min(Lk, max(0, a.key_start[b])) : 0;
+  if constexpr (kShared)
+    if (stacked) start = min(min(sh.begins[0], sh.begins[1]), min(sh.begins[2], sh.begins[3]));
   const int32_t b_lo = k_lo >> S_log, nb = ((k_hi - 1) >> S_log) + 1 - b_lo;
 
   // ---- set-up
@@ -689,9 +694,12 @@ cache_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
       if (!ok) break;
       tc_fence_after();
       if (warp_live) {
+        uint32_t sw[64];  // (one read: it takes 200 cycles whatever its width)
+        tmem_ask(tmem + lane_off + sb * KT, sw);
+        tmem_have(sw);
         float sv[64];
-        tmem_ld32(tmem + lane_off + sb * KT, sv);
-        tmem_ld32(tmem + lane_off + sb * KT + 32, sv + 32);
+#pragma unroll
+        for (int i = 0; i < 64; ++i) sv[i] = __uint_as_float(sw[i]);
         if (c0 + KT > mask_from || c0 < hide_to || c0 + KT > k_hi || any_bad) {
           uint64_t keep;
           if (stacked) {

@@ -268,6 +268,28 @@ def test_a_nan_key_reaches_the_rows_that_see_it(ssd):
         assert torch.equal(torch.isnan(ls), want.transpose(1, 2))
 
 
+def test_padding_of_a_shared_prompt_may_be_anything(ssd):
+    """Before the first token that any sequence of the group may see: NaN in keys, values and scales."""
+    for D, start in ((1, [40] * 4), (1, [64, 37, 100, 51]), (40, [40] * 4), (40, [33, 64, 34, 90]), (1, [128] * 4)):
+        def edit(b):
+            n = min(start)
+            for i in range(-(-n // b.block)):
+                for x in "kv":
+                    b.codes[x][b.table[0, i], :, :n - i * b.block] = 0x7f
+                    if (i + 1) * b.block <= n:
+                        b.scales[x][b.table[0, i]] = np.nan
+
+        b = Batch(seed=D, start=[0, 4], shared=[8], own=[10, 20, 30, 0], nd=[D] * 4, D=D, Hq=4, Hkv=2, d=128,
+                  block=16, edit=edit, key_start=start)
+        o, ls, st = b.run(ssd)
+        assert st == 0 and b.shares
+        refs = b.refs()
+        for _, per, _, _ in refs:
+            for x in per:
+                per[x][:min(start)] = 0.0  # (that nobody sees)
+        check(o, ls, refs, b.nd)
+
+
 def test_the_first_of_a_group_may_be_done(ssd):
     """Blocks are named by a sequence that has drafts, not by one whose table is gone."""
     for D in (1, 33):

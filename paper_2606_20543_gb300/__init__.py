@@ -503,10 +503,15 @@ def ssd_cache_attention(g: Grid, c: BlockCache, B, Hq, cache_len, n_drafts, draf
         _ptr(workspace), workspace_bytes, _ptr(status), _stream(stream)))
 
 
+_cache_sharing = 0
+
+
 def ssd_set_cache_sharing(how: int) -> None:
     """Process-wide: 0 ssd_cache_attention_shared() shares where it pays by its estimate (the
     default), 1 always, 2 never; for workspace queries and calls after it."""
+    global _cache_sharing
     _check("ssd_set_cache_sharing", load().ssd_set_cache_sharing(int(how)))
+    _cache_sharing = int(how)  # (workspaces that callers keep were asked for under it)
 
 
 def ssd_cache_attention_shared_workspace(B, groups, Hq, Hkv, d, D_max, L_max, max_shared) -> int:

@@ -9,6 +9,8 @@ from __future__ import annotations
 
 import torch
 
+import paper_2606_20543_gb300 as _ssd
+
 from . import (Grid, Rng, Sampling, cache as make_cache, rotary as make_rotary,
                ssd_cache_append, ssd_cache_append_norm, ssd_cache_attention,
                ssd_cache_attention_shared, ssd_cache_attention_shared_workspace,
@@ -87,7 +89,7 @@ class PagedDecode:
         self.groups, self.max_shared = 0, 0
 
     def _workspace(self, N):
-        key = N, self.groups, self.max_shared
+        key = N, self.groups, self.max_shared, _ssd._cache_sharing
         if self._ws.get(N, (None, None))[1] != key:
             sizes = (self.Hq, self.Hkv, self.d, N, self.max_blocks * self.block)
             n = (ssd_cache_attention_shared_workspace(self.B, self.groups, *sizes, self.max_shared * self.block)

@@ -196,6 +196,31 @@ def test_graphs_of_earlier_groups(ssd):
     check(alone, o0)
 
 
+def test_sharing_set_between_passes(ssd):
+    """A pass asks for its workspace as sharing is set when it runs; a graph keeps what it was captured with."""
+    B, Hq, Hkv, d, block, W, prefix = 4, 8, 2, 128, 16, 4, 1500
+    gen = torch.Generator("cuda").manual_seed(9)
+    dec = make(ssd, B, Hq, Hkv, d, block, prefix, W, prefix)
+    dec.plan(i32([prefix, 0, 0, 0]))
+    dec.attend(0, *rows(gen, B * prefix, Hq, Hkv, d))
+    dec.advance()
+    dec.share([0, 4], [prefix // block])
+    one, qkv, out = i32([1] * B), [x.contiguous() for x in rows(gen, B, Hq, Hkv, d)], []
+    for how in (2, 1, 0):
+        ssd.ssd_set_cache_sharing(how)
+        dec.plan(one, 1)
+        out.append(dec.attend(0, *qkv).clone())
+        if how == 2:
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph):
+                o = dec.attend(0, *qkv)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert int(dec.status.item()) == 0 and torch.equal(o, out[0])
+    for x in out[1:]:
+        assert (x.double() - out[0].double()).norm() <= 4e-3 * out[0].double().norm()
+
+
 def test_share_refuses(ssd):
     dec = make(ssd, 4, 2, 2, 64, 16, 40, 4, 40)
     for start, blocks in (([0, 4], []), ([0, 3], [1]), ([1, 4], [1]), ([0, 3, 2, 4], [1, 1, 1]), ([0, 4], [-1]),

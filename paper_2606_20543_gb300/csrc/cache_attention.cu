@@ -47,6 +47,7 @@ constexpr int kCtas = 3;            // per SM
 // the shared ones (371 sequences of 67 to 712 own keys, 12/4 heads of 64: 61 us, 56).
 template <int NR, int W, bool kShared>
 constexpr int kStagesOf = kShared && NR == 1 && W == kWarps ? 3 : 4;
+constexpr int kMostPartTiles = 264;  // of shared keys
 template <int NR, int W, bool kShared>
 constexpr int kCtasOf = W != kWarps ? 1 : kShared && NR == 1 ? 4 : kCtas;
 constexpr int kMinTiles = 8;        // a part's fewest tiles
@@ -116,12 +117,14 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
 }
 
 // NR: groups of 8 query rows of a warp; W: warps.
-// kShared: a sequence's keys begin behind those that it shares with its group, and its rows always
-// go to the part rows.
-template <int D, int NR, int W, bool kShared>
-__global__ void __launch_bounds__(W * 32, (kCtasOf<NR, W, kShared>))
+// kMode 1: a sequence's keys begin behind those that it shares with its group, and its rows always
+// go to the part rows.  kMode 2: a group's shared keys, the rows of all its sequences one behind the
+// other, as many at a time as a CTA takes (each time the keys are read again); grid: parts, KV heads, groups.
+template <int D, int NR, int W, int kMode>
+__global__ void __launch_bounds__(W * 32, (kCtasOf<NR, W, kMode == 1>))
 cache_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
                   CacheAttnArgs a, CacheAttnLaunch L) {
+  constexpr bool kShared = kMode == 1, kStack = kMode == 2;
   constexpr int kStages = kStagesOf<NR, W, kShared>;
   constexpr int RW = 8 * NR;          // rows of a warp
   constexpr int NT = D / 16;          // output tiles of 16 columns
@@ -143,38 +146,67 @@ cache_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
   // (kShared: beside the kernel before it, on the shared keys, which let it start when all before
   // that was done; the first CTA waits for it at the end)
   if (!kShared) pdl_wait();
+  if (kStack) pdl_launch_dependents();
 
   const int32_t tid = threadIdx.x, lane = tid & 31, warp = (int32_t)warp_uniform(tid >> 5);
   // (kShared: a sequence's heads one after the other, the longest sequences first)
   const int32_t cta = kShared ? blockIdx.x + blockIdx.y * gridDim.x : 0;
   const int32_t x_cta = kShared ? cta / a.cache.Hkv : blockIdx.x;
-  const int32_t g = kShared ? cta - x_cta * a.cache.Hkv : blockIdx.y, S = a.cache.block, S_log = 31 - __clz(S), G = a.Hq / a.cache.Hkv;
-  const bool first_of = g == 0 && blockIdx.z == 0;
+  const int32_t g = kStack ? blockIdx.x / L.s_splits % a.cache.Hkv : kShared ? cta - x_cta * a.cache.Hkv : blockIdx.y;
+  const int32_t S = a.cache.block, S_log = 31 - __clz(S), G = a.Hq / a.cache.Hkv;
+  const bool first_of = !kStack && g == 0 && blockIdx.z == 0;
+  // kStack: the group's first sequence, the one that names the blocks, rows and shared tokens
+  int32_t g_first = 0, g_named = -1, g_rows = 0, g_len = 0, g_row0 = 0;
+  CacheWork<kShared> work;
+  if constexpr (kStack) {
+    const int32_t group = blockIdx.x / L.s_splits / a.cache.Hkv, split = blockIdx.x % L.s_splits;
+    const int32_t blocks = a.shared[group];
+    g_first = min(max(a.group_start[group], 0), a.B);
+    const int32_t end = min(max(a.group_start[group + 1], g_first), a.B);
+    // (what is out of range is recorded with the sequences' own keys)
+    if (blocks <= 0 || blocks > a.max_shared) return;
+    g_len = blocks * S;
+    g_rows = (end - g_first) * a.D_max * G;
+    for (int32_t b0 = g_first; b0 < end && g_named < 0; b0 += 32) {
+      const int32_t c = b0 + lane < end ? a.cache_len[b0 + lane] : 0, n = b0 + lane < end ? a.n_drafts[b0 + lane] : 0;
+      const uint32_t here = __ballot_sync(0xffffffffu, n > 0 && cache_lengths_ok(a, c, n) && c >= g_len);
+      if (here != 0) g_named = b0 + __ffs(here) - 1;
+    }
+    const int32_t tiles = (g_len + kCacheTile - 1) / kCacheTile, parts = cache_parts(L.s_splits, L.s_min_tiles, tiles);
+    if (g_named < 0 || split >= parts) return;
+    work.t_lo = (int32_t)((int64_t)tiles * split / parts);
+    work.t_hi = (int32_t)((int64_t)tiles * (split + 1) / parts);
+  }
   if (lane == 0) {
     for (int t = 0; t < kStages; ++t) mbar_init(&s_full[warp][t], 1);
     fence_barrier_init();
   }
   uint32_t stage = 0, phase = 0;  // of the warp's next step
-  CacheWork<kShared> work;
-  bool more = work.first(a, L, x_cta, first_of && tid < 32);
+  bool more = true;
+  if constexpr (!kStack) more = work.first(a, L, x_cta, first_of && tid < 32);
+  auto next = [&]() {
+    if constexpr (!kStack) return work.next(a);
+    g_row0 += RW;
+    return g_row0 < g_rows;
+  };
 #pragma unroll 1
-  for (; more; more = work.next(a)) {
+  for (; more; more = next()) {
     // (the rows of the part before have left the ring's place, and the copies may know it)
     fence_proxy_async_shared();
     __syncthreads();
-    const int32_t b = work.b;
-    const int32_t cache = a.cache_len[b], nd = a.n_drafts[b];
-    const int32_t Lk = cache + nd, rows_total = nd * G;
-    const int32_t row0 = blockIdx.z * RW;
-    if (L.info != nullptr && first_of && tid == 0) {
+    const int32_t b = kStack ? g_named : work.b;
+    const int32_t cache = kStack ? g_len : a.cache_len[b], nd = kStack ? 0 : a.n_drafts[b];
+    const int32_t Lk = cache + nd, rows_total = kStack ? g_rows : nd * G;
+    const int32_t row0 = kStack ? g_row0 : blockIdx.z * RW;
+    if (!kStack && L.info != nullptr && first_of && tid == 0) {
       if (work.t_lo == 0) L.info[b].x = work.x;
       if (work.t_hi == work.tiles) L.info[b].y = work.x;
     }
     if (row0 >= rows_total) continue;
-    const bool whole = !kShared && work.t_lo == 0 && work.t_hi == work.tiles, begins = work.t_lo == 0;
+    const bool whole = kMode == 0 && work.t_lo == 0 && work.t_hi == work.tiles, begins = work.t_lo == 0;
     const int32_t base = kShared ? cache_base(a, b, cache) : 0;
     const int32_t k_lo = base + work.t_lo * kCacheTile, k_hi = min(Lk, base + work.t_hi * kCacheTile);
-    const int32_t start = a.key_start != nullptr ? min(Lk, max(0, a.key_start[b])) : 0;
+    int32_t start = !kStack && a.key_start != nullptr ? min(Lk, max(0, a.key_start[b])) : 0;
 
     // ---- this warp's rows and its share of the steps, and the copies of the first ones
     const int32_t q = lane & 3, r8 = lane >> 2;
@@ -222,6 +254,7 @@ cache_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
     uint32_t qf[NR][KG][4][2];
     float rowc_of[NR];
     int32_t qpos_of[NR];
+    int32_t start_of[NR];  // (kStack) the row's first visible key; of no row: INT32_MAX
     const float c2 = (a.scale != 0.f ? a.scale : rsqrtf((float)D)) * kLog2e;
 #pragma unroll
     for (int n = 0; n < NR; ++n) {
@@ -229,9 +262,19 @@ cache_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
       const bool live = r < rows_total;
       const int32_t j = live ? r / G : 0, h = g * G + (live ? r - j * G : 0);
       const uint4* src = reinterpret_cast<const uint4*>(
-          static_cast<const __nv_bfloat16*>(a.q) + (((int64_t)b * a.D_max + j) * a.Hq + h) * D);
-      qpos_of[n] = 0x7fffffff;
-      if (live) {
+          static_cast<const __nv_bfloat16*>(a.q) +
+          (((int64_t)(kStack ? g_first : b) * a.D_max + j) * a.Hq + h) * D);
+      qpos_of[n] = start_of[n] = 0x7fffffff;
+      if constexpr (kStack) {
+        const int32_t rb = g_first + j / a.D_max, jj = j - (rb - g_first) * a.D_max;
+        if (live) {
+          const int32_t c = a.cache_len[rb], n_of = a.n_drafts[rb];
+          if (cache_lengths_ok(a, c, n_of) && jj < n_of && c >= g_len) {
+            qpos_of[n] = cache_flat_pos(a, rb, c, jj);
+            start_of[n] = a.key_start != nullptr ? min(g_len, max(0, a.key_start[rb])) : 0;
+          }
+        }
+      } else if (live) {
         qpos_of[n] = cache_flat_pos(a, b, cache, j);
         if (qpos_of[n] < 0 && begins && g == 0) record_status(a.status, SSD_ERR_DEVICE_BOUNDS);
       }
@@ -272,15 +315,28 @@ cache_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
       if (NR == 2) minq = min(minq, qpos_of[NR - 1]);
       mask_from = min(cache, min(0x7ffffffe, __reduce_min_sync(0xffffffffu, minq)) + 1);
     }
+    int32_t hide_to = start;  // keys below this one are hidden from some row of the warp
+    if constexpr (kStack) {
+      int32_t lo = 0x7fffffff, hi = 0;
+#pragma unroll
+      for (int n = 0; n < NR; ++n) {
+        lo = min(lo, start_of[n]);
+        if (start_of[n] != 0x7fffffff) hi = max(hi, start_of[n]);
+      }
+      start = min(g_len, __reduce_min_sync(0xffffffffu, lo));  // (those before it may be anything)
+      hide_to = __reduce_max_sync(0xffffffffu, hi);
+    }
     // From here on a lane's rows are 8 n + 2 q + u: those of its scores and of O.
     float rowc[NR][2];
     int32_t qpos[NR][2];
+    int32_t row_start[NR][2];
 #pragma unroll
     for (int n = 0; n < NR; ++n)
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         rowc[n][u] = __shfl_sync(0xffffffffu, rowc_of[n], (2 * q + u) * 4);
         qpos[n][u] = __shfl_sync(0xffffffffu, qpos_of[n], (2 * q + u) * 4);
+        if (kStack) row_start[n][u] = __shfl_sync(0xffffffffu, start_of[n], (2 * q + u) * 4);
       }
     __syncthreads();  // ids and scales
 
@@ -342,7 +398,8 @@ cache_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
         }
       }
       const int32_t k0 = key_of(t), bi = (k0 >> S_log) - b_lo;
-      const float ks = s_ks[bi], vs = s_vs[bi];
+      // (kStack: a block that nobody sees may have any scale)
+      const float ks = s_ks[bi], vs = kStack && k0 + kStep <= start ? 0.f : s_vs[bi];
       __syncwarp();
       if (lane == 0 && t + kStages < steps)
         issue(t + kStages, stage, s_id[(key_of(t + kStages) >> S_log) - b_lo]);
@@ -371,7 +428,7 @@ cache_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
           for (int e = 0; e < 4; ++e)
             x[n][e] = (KG == 2 ? sc[0][n][e] + sc[KG - 1][n][e] : sc[0][n][e]) * (rowc[n][e & 1] * ks);
       }
-      if (k0 < start || k0 + kStep > min(mask_from, k_hi) || s_id[bi] < 0) {
+      if (k0 < hide_to || k0 + kStep > min(mask_from, k_hi) || s_id[bi] < 0) {
         const bool in_pool = s_id[bi] >= 0;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -388,7 +445,8 @@ cache_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
           for (int n = 0; n < NR; ++n)
 #pragma unroll
             for (int u = 0; u < 2; ++u)
-              if (kp > qpos[n][u] || kp == 0x7fffffff) x[n][2 * h + u] = -INFINITY;
+              if (kp > qpos[n][u] || kp == 0x7fffffff || (kStack && key < row_start[n][u]))
+                x[n][2 * h + u] = -INFINITY;
         }
         // what lies in no key's place may be anything
 #pragma unroll
@@ -530,6 +588,13 @@ cache_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
           ob[k / 2] = pack_bf16x2(row_value(acc[k], inv, sum), row_value(acc[k + 1], inv, sum));
         if (a.lse != nullptr && lane == 0)
           a.lse[((int64_t)b * a.Hq + h) * a.D_max + j] = row_lse(M, sum);
+      } else if constexpr (kStack) {
+        const int64_t at = (((int64_t)g_first * a.D_max + j) * a.Hq + h) * L.s_splits + blockIdx.x % L.s_splits;
+        if (!dbg_in(at, (int64_t)a.B * a.D_max * a.Hq * L.s_splits, a.status)) continue;
+        float* po = L.s_part_o + at * D + lane * PER;
+#pragma unroll
+        for (int k = 0; k < PER; ++k) po[k] = acc[k];
+        if (lane == 0) L.s_part_ml[at] = make_float2(M, sum);
       } else {
         // (a CTA leaves a share of several sequences, but of neighbours: slot x + b)
         const int64_t slots = L.per_head + a.B;
@@ -624,20 +689,18 @@ bool step_map(CUtensorMap* map, const void* base, const ssd_block_cache& c) {
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int D, int NR, int W, bool kShared>
-cudaError_t launch_mma(const CacheAttnArgs& a, const CacheMmaPlan& p, const CacheAttnLaunch& L,
-                       cudaStream_t stream) {
+template <int D, int NR, int W, int kMode>
+cudaError_t launch_mma(const CacheAttnArgs& a, dim3 grid, const CacheAttnLaunch& L, cudaStream_t stream) {
   CUtensorMap tk, tv;
   if (!step_map(&tk, a.cache.k, a.cache) || !step_map(&tv, a.cache.v, a.cache))
     return cudaErrorInvalidValue;
   auto smem = [](int32_t blocks) {
-    return 1024 + (size_t)W * kStagesOf<NR, W, kShared> * 2 * kStep * D + (size_t)blocks * 12;
+    return 1024 + (size_t)W * kStagesOf<NR, W, kMode == 1> * 2 * kStep * D + (size_t)blocks * 12;
   };
   const cudaError_t e =
-      allow_smem(cache_attn_kernel<D, NR, W, kShared>, smem(part_blocks(kWorkRoom, kLeastBlock)));
+      allow_smem(cache_attn_kernel<D, NR, W, kMode>, smem(part_blocks(kMode == 2 ? kMostPartTiles : kWorkRoom, kLeastBlock)));
   if (e != cudaSuccess) return e;
-  return launch_kernel(cache_attn_kernel<D, NR, W, kShared>, dim3(p.per_head, a.cache.Hkv, p.row_groups),
-                       dim3(W * 32), smem(L.max_blocks), stream, true, tk, tv, a, L);
+  return launch_kernel(cache_attn_kernel<D, NR, W, kMode>, grid, dim3(W * 32), smem(L.max_blocks), stream, true, tk, tv, a, L);
 }
 
 size_t part_bytes(int64_t rows, int32_t d) {
@@ -647,12 +710,13 @@ size_t part_bytes(int64_t rows, int32_t d) {
 int64_t tc_part_rows(int32_t B, int32_t Hq, int32_t D_max, int32_t splits) {
   return splits == 1 ? 0 : (int64_t)B * D_max * Hq * splits;
 }
-template <int D, bool kShared>
+template <int D, int kMode>
 cudaError_t launch_mma_of(const CacheAttnArgs& a, const CacheMmaPlan& p, const CacheAttnLaunch& L,
                           cudaStream_t stream) {
-  return p.rows > 8             ? launch_mma<D, 2, kWarps, kShared>(a, p, L, stream)
-         : p.warps == kWarps ? launch_mma<D, 1, kWarps, kShared>(a, p, L, stream)
-                             : launch_mma<D, 1, kManyWarps, kShared>(a, p, L, stream);
+  const dim3 grid(p.per_head, a.cache.Hkv, p.row_groups);
+  return p.rows > 8          ? launch_mma<D, 2, kWarps, kMode>(a, grid, L, stream)
+         : p.warps == kWarps ? launch_mma<D, 1, kWarps, kMode>(a, grid, L, stream)
+                             : launch_mma<D, 1, kManyWarps, kMode>(a, grid, L, stream);
 }
 
 }  // namespace
@@ -675,10 +739,15 @@ void cache_attention_mma_fill(CacheAttnLaunch& L, const CacheMmaPlan& p, int32_t
 cudaError_t launch_cache_attention_mma(const CacheAttnArgs& a, const CacheMmaPlan& p,
                                        const CacheAttnLaunch& L, cudaStream_t stream) {
   if (a.groups > 0)
-    return a.cache.d == 128 ? launch_mma_of<128, true>(a, p, L, stream)
-                            : launch_mma_of<64, true>(a, p, L, stream);
-  return a.cache.d == 128 ? launch_mma_of<128, false>(a, p, L, stream)
-                          : launch_mma_of<64, false>(a, p, L, stream);
+    return a.cache.d == 128 ? launch_mma_of<128, 1>(a, p, L, stream) : launch_mma_of<64, 1>(a, p, L, stream);
+  return a.cache.d == 128 ? launch_mma_of<128, 0>(a, p, L, stream) : launch_mma_of<64, 0>(a, p, L, stream);
+}
+cudaError_t launch_cache_attention_stack(const CacheAttnArgs& a, const CacheAttnLaunch& L, int32_t rows,
+                                         cudaStream_t stream) {
+  const dim3 grid((unsigned)((int64_t)L.s_splits * a.cache.Hkv * a.groups));
+  if (a.cache.d == 128)
+    return rows > 8 ? launch_mma<128, 2, kWarps, 2>(a, grid, L, stream) : launch_mma<128, 1, kWarps, 2>(a, grid, L, stream);
+  return rows > 8 ? launch_mma<64, 2, kWarps, 2>(a, grid, L, stream) : launch_mma<64, 1, kWarps, 2>(a, grid, L, stream);
 }
 
 size_t cache_attention_workspace(int32_t B, int32_t Hq, int32_t Hkv, int32_t d, int32_t D_max,

@@ -379,5 +379,8 @@ int64_t cache_attention_mma_rows(int32_t B, int32_t Hkv, const CacheMmaPlan& p, 
 void cache_attention_mma_fill(CacheAttnLaunch& L, const CacheMmaPlan& p, int32_t L_max, int32_t block);
 cudaError_t launch_cache_attention_mma(const CacheAttnArgs& a, const CacheMmaPlan& p,
                                        const CacheAttnLaunch& L, cudaStream_t stream);
+// Groups' shared keys on it; rows: of a group, about
+cudaError_t launch_cache_attention_stack(const CacheAttnArgs& a, const CacheAttnLaunch& L, int32_t rows,
+                                         cudaStream_t stream);
 
 }  // namespace ssd

@@ -29,6 +29,7 @@ constexpr double kSharedFixed = 9.5;   // tiles that a unit's set-up, way out an
 struct SharedPlan {
   bool plain;   // every sequence by itself: ssd_cache_attention()
   bool own_tc;  // the own keys on the tensor-core kernel, too
+  int32_t few;  // rows of a group, if the shared keys are on the mma.sync kernel, else 0
   CacheMmaPlan mma;
   int32_t s_units, s_splits, s_min_tiles, splits, min_tiles;
   int64_t s_rows, rows;  // part rows
@@ -95,6 +96,7 @@ SharedPlan make_plan(int32_t B, int32_t groups, int32_t Hq, int32_t Hkv, int32_t
   p.s_units = (int32_t)(base * p.s_splits);
   p.s_rows = rows * p.s_splits;
   p.own_tc = per_seq > 16;
+  p.few = !p.own_tc && B * per_seq <= 16 * (int64_t)groups ? (int32_t)((B * per_seq + groups - 1) / groups) : 0;
   if (how != kShareAlways && !sharing_pays(B, groups, Hq, Hkv, d, D_max, L_max, max_shared, p)) {
     p.plain = true;
     return p;
@@ -259,7 +261,8 @@ cudaError_t launch_cache_attention_shared(const CacheAttnArgs& a, void* ws, cuda
   L.max_blocks = s_blocks;
   if (p.own_tc)
     L.max_blocks = std::max(s_blocks, part_blocks(cache_part_tiles(p.splits, p.min_tiles, tiles), S));
-  cudaError_t e = launch_cache_attention_tc(a, L, stream, p.own_tc);
+  cudaError_t e = p.few > 0 ? launch_cache_attention_stack(a, L, p.few, stream)
+                            : launch_cache_attention_tc(a, L, stream, p.own_tc);
   if (e != cudaSuccess) return e;
   if (!p.own_tc) {
     L.info = reinterpret_cast<int2*>(at);

@@ -47,6 +47,9 @@ constexpr int kCtas = 3;            // per SM
 // the shared ones (371 sequences of 67 to 712 own keys, 12/4 heads of 64: 61 us, 56).
 template <int NR, int W, bool kShared>
 constexpr int kStagesOf = kShared && NR == 1 && W == kWarps ? 3 : 4;
+// (Groups differ in size: 16 sequences in 8 groups of 1 to 7, 8 rows a CTA, 3840 keys 28.6 us with one, 21.6
+// with two; in groups of 2, where the second CTAs have no rows, 19.5 and 21.9.)
+constexpr int kStackTurns = 2;
 constexpr int kMostPartTiles = 264;  // of shared keys
 template <int NR, int W, bool kShared>
 constexpr int kCtasOf = W != kWarps ? 1 : kShared && NR == 1 ? 4 : kCtas;
@@ -119,7 +122,8 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
 // NR: groups of 8 query rows of a warp; W: warps.
 // kMode 1: a sequence's keys begin behind those that it shares with its group, and its rows always
 // go to the part rows.  kMode 2: a group's shared keys, the rows of all its sequences one behind the
-// other, as many at a time as a CTA takes (each time the keys are read again); grid: parts, KV heads, groups.
+// other; grid: parts, KV heads and groups in x, CTAs that take turns at the rows of a group in z (each
+// turn reads the keys again).
 template <int D, int NR, int W, int kMode>
 __global__ void __launch_bounds__(W * 32, (kCtasOf<NR, W, kMode == 1>))
 cache_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
@@ -173,7 +177,8 @@ cache_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
       if (here != 0) g_named = b0 + __ffs(here) - 1;
     }
     const int32_t tiles = (g_len + kCacheTile - 1) / kCacheTile, parts = cache_parts(L.s_splits, L.s_min_tiles, tiles);
-    if (g_named < 0 || split >= parts) return;
+    g_row0 = blockIdx.z * RW;
+    if (g_named < 0 || split >= parts || g_row0 >= g_rows) return;
     work.t_lo = (int32_t)((int64_t)tiles * split / parts);
     work.t_hi = (int32_t)((int64_t)tiles * (split + 1) / parts);
   }
@@ -186,7 +191,7 @@ cache_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
   if constexpr (!kStack) more = work.first(a, L, x_cta, first_of && tid < 32);
   auto next = [&]() {
     if constexpr (!kStack) return work.next(a);
-    g_row0 += RW;
+    g_row0 += gridDim.z * RW;
     return g_row0 < g_rows;
   };
 #pragma unroll 1
@@ -744,7 +749,7 @@ cudaError_t launch_cache_attention_mma(const CacheAttnArgs& a, const CacheMmaPla
 }
 cudaError_t launch_cache_attention_stack(const CacheAttnArgs& a, const CacheAttnLaunch& L, int32_t rows,
                                          cudaStream_t stream) {
-  const dim3 grid((unsigned)((int64_t)L.s_splits * a.cache.Hkv * a.groups));
+  const dim3 grid((unsigned)((int64_t)L.s_splits * a.cache.Hkv * a.groups), 1, kStackTurns);
   if (a.cache.d == 128)
     return rows > 8 ? launch_mma<128, 2, kWarps, 2>(a, grid, L, stream) : launch_mma<128, 1, kWarps, 2>(a, grid, L, stream);
   return rows > 8 ? launch_mma<64, 2, kWarps, 2>(a, grid, L, stream) : launch_mma<64, 1, kWarps, 2>(a, grid, L, stream);

@@ -5,14 +5,16 @@
 //   M = max m_i,   o = sum o_i 2^(m_i - M) / sum l_i 2^(m_i - M).
 // The keys in [0, P) are the same for all rows of the group, so those rows are stacked into the
 // 128-row tiles of the tensor-core kernel (cache_attention_tc.cu), which reads the keys once a tile
-// instead of once a sequence.  The keys from P on are each sequence's own: on the same kernel, in
+// instead of once a sequence; up to 16 rows a group, about, go to the mma.sync kernel
+// (cache_attention.cu), 8 or 16 at a time.  The keys from P on are each sequence's own: on the same kernel, in
 // the same launch, or, for few rows, on the mma.sync one (cache_attention.cu).  Both leave part rows,
 // which the kernel here joins.
 //
 // One token of 64 sequences of one group, 4352 shared keys and 100 to 1000 own, 32/8 heads (73 MB):
 // 37 us, 2.0 TB/s: the set-up, first tile and way out of three kernels' CTAs (18000 cycles of a
 // shared unit's 30000), and own keys at 2.5 TB/s beside the shared ones.  48 drafts of 8 groups of 4
-// over 1500 to 8000 shared keys, 16 heads: 118 us, the softmax of the tensor-core kernel.
+// over 1500 to 8000 shared keys, 16 heads: 118 us, the softmax of the tensor-core kernel.  35 tokens of 7 groups over 6300 shared keys,
+// 8 heads of 64 (46 MB): 19 us, on the tensor-core kernel 45.
 #include <algorithm>
 #include <cmath>
 
@@ -24,7 +26,8 @@ namespace {
 
 constexpr int kSharedTiles = 3;        // fewest tiles of a part of the shared keys,
 constexpr int kSharedPartTiles = 256;  // and about the most
-constexpr double kSharedFixed = 9.5;   // tiles that a unit's set-up, way out and share of the join are worth
+constexpr double kSharedFixed = 9.5;   // tiles that a unit's set-up, way out and share of the join are worth,
+constexpr double kFewFixed = 6;        // and one of few rows on the mma.sync kernel
 
 struct SharedPlan {
   bool plain;   // every sequence by itself: ssd_cache_attention()
@@ -39,10 +42,11 @@ struct SharedPlan {
 // tile of the tensor-core kernel takes an SM 4.8e-3 of a GPU's us where all its warps have rows,
 // less where some have none; the mma.sync kernel streams keys at 5.6 (64-wide heads: 6.4) TB/s; a CTA
 // takes 0.75 us a tile however few there are of them (0.7), and 12 ns more (8, of the own keys); the
-// join reads its parts at 3 TB/s.  Sharing starts three kernels instead of one and sets up units of few tiles: 16 us (14 with
-// the own keys in the same launch) instead of 6 (10; 4 more where sequences are cut).  Measured, shared
-// and not: 64 sequences of one group, 4352 + 1000 keys, 32/8 heads 37 and 102; 50 of 4 drafts over
-// 13000, 33 and 138; 8 groups of 4, 48 drafts over 8000 + 600, 16 heads 118 and 152; 6 of 14, 6 drafts
+// join reads its parts at 3 TB/s.  Sharing starts three kernels instead of one and sets up units of few
+// tiles: 16 us (11 with few rows of a group, 14 with the own keys in the same launch) instead of 6 (10; 4
+// more where sequences are cut).  Measured, shared and not: 64 sequences of one group, 4352 + 1000 keys,
+// 32/8 heads 37 and 102; 50 of 4 drafts over 13000, 33 and 138; 8 groups of 4, 48 drafts over 8000 + 600,
+// 16 heads 117 and 152; 7 groups of 5 over 6300, 8 heads of 64 19 and 46; 6 of 14, 6 drafts
 // over 2200 + 1400, 6/2 heads 35 and 58; 10 of 3 over 1000, 32 heads 60 and 43; 8 groups of 2 over 4900
 // + 1900, 41 and 25; 3 of 42 drafts over 1800 + 1000, 6/2 heads 22 and 17.
 bool sharing_pays(int32_t B, int32_t groups, int32_t Hq, int32_t Hkv, int32_t d, int32_t D_max,
@@ -65,7 +69,8 @@ bool sharing_pays(int32_t B, int32_t groups, int32_t Hq, int32_t Hkv, int32_t d,
   const double us_of_tile = (double)B * Hkv * 2 * d * 64 / (d == 128 ? 5.6e6 : 6.4e6);
   const double alone = 6 + (plan.cut(B) ? 4 : 0) +
                        std::max(us_of_tile * (shared + own), 0.7 * B * (shared + own) / ctas);
-  return 16 + stacked + us_of_tile * own + 8e-3 * B * Hkv + join < 0.9 * alone;
+  const double few = std::max(us_of_tile / B * groups * shared, 0.7 * shared / p.s_splits);
+  return (p.few > 0 ? 11 + few : 16 + stacked) + us_of_tile * own + 8e-3 * B * Hkv + join < 0.9 * alone;
 }
 
 SharedPlan make_plan(int32_t B, int32_t groups, int32_t Hq, int32_t Hkv, int32_t d, int32_t D_max,
@@ -84,8 +89,10 @@ SharedPlan make_plan(int32_t B, int32_t groups, int32_t Hq, int32_t Hkv, int32_t
   // n): 64 sequences of one group over 4352 keys, 32/8 heads 1: 82, 3: 41, 6: 36, 11: 39, 20: 50; 72 of
   // two groups over 11900, 32/8 heads 5: 79, 10: 55, 20: 66, 32: 88; 48 drafts, 8 groups of 4 over 1500
   // to 8000, 16 heads 1: 138, 2: 128, 3: 119, 5: 130, 8: 149.
-  const int64_t base = tiles_r * Hkv, places = 2 * device_sm_count();
-  int64_t n = (int64_t)std::ceil(std::sqrt(0.5 * tiles * places / (kSharedFixed * base)));
+  p.own_tc = per_seq > 16;
+  p.few = !p.own_tc && B * per_seq <= 16 * (int64_t)groups ? (int32_t)((B * per_seq + groups - 1) / groups) : 0;
+  const int64_t sms = device_sm_count(), base = tiles_r * Hkv, places = (p.few > 0 && d == 64 ? 3 : 2) * sms;
+  int64_t n = (int64_t)std::ceil(std::sqrt(tiles * sms / ((p.few > 0 ? kFewFixed : kSharedFixed) * base)));
   if (base <= places && base * n > places && 4 * base * n <= 7 * places) n = places / base;
   p.s_min_tiles = (int32_t)std::min<int64_t>(kSharedPartTiles / 2, std::max<int64_t>(kSharedTiles, tiles / n));
   p.s_splits = (int32_t)std::max<int64_t>(1, tiles / p.s_min_tiles);
@@ -95,8 +102,6 @@ SharedPlan make_plan(int32_t B, int32_t groups, int32_t Hq, int32_t Hkv, int32_t
   }
   p.s_units = (int32_t)(base * p.s_splits);
   p.s_rows = rows * p.s_splits;
-  p.own_tc = per_seq > 16;
-  p.few = !p.own_tc && B * per_seq <= 16 * (int64_t)groups ? (int32_t)((B * per_seq + groups - 1) / groups) : 0;
   if (how != kShareAlways && !sharing_pays(B, groups, Hq, Hkv, d, D_max, L_max, max_shared, p)) {
     p.plain = true;
     return p;

@@ -200,6 +200,27 @@ def test_many_sequences_and_groups(ssd, B, groups, D):
           wide=20000).check(ssd, rows=[0, D - 1])
 
 
+@pytest.mark.parametrize("D,Hq,Hkv,d", [(1, 4, 2, 128), (1, 2, 2, 64), (2, 8, 4, 64), (3, 6, 2, 128)])
+@pytest.mark.parametrize("how", ["", "key_start", "draft_pos"])
+def test_few_rows_of_most_groups_and_many_of_one(ssd, D, Hq, Hkv, d, how):
+    """Shared keys on the kernel for few rows: a group of 23 sequences beside ten of one or none, some
+    sequences without drafts, padding, drafts anywhere on the grid."""
+    rng = np.random.default_rng(D + d)
+    start = [0, 1, 24, 24, 25, 26, 27, 28, 29, 30, 31, 32]
+    shared = [9, 40, 5, 0, 17, 1, 3, 8, 2, 12, 64]
+    B = start[-1]
+    nd = [int(x) for x in rng.integers(0, D + 1, B)]
+    nd[1], nd[0] = 0, D  # (the first of the long group has nothing to do)
+    kw = {}
+    if how == "key_start":
+        kw["key_start"] = [int(x) for x in rng.integers(0, 40, B)]
+    if how == "draft_pos":  # over a grid that reaches from the prompts to behind all tokens
+        kw["grid"] = (64, 64, 0, 64)
+        kw["draft_pos"] = rng.integers(600, 4096, (B, D))
+    Batch(seed=D, start=start, shared=shared, own=[int(x) for x in rng.integers(0, 90, B)], nd=nd, D=D, Hq=Hq,
+          Hkv=Hkv, d=d, block=16, **kw).check(ssd)
+
+
 def test_offsets_beyond_32_bits(ssd):
     """Blocks behind the first 3 GB of a pool."""
     for D in (1, 40):

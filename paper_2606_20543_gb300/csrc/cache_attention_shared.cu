@@ -14,7 +14,7 @@
 // 37 us, 2.0 TB/s: the set-up, first tile and way out of three kernels' CTAs (18000 cycles of a
 // shared unit's 30000), and own keys at 2.5 TB/s beside the shared ones.  48 drafts of 8 groups of 4
 // over 1500 to 8000 shared keys, 16 heads: 118 us, the softmax of the tensor-core kernel.  35 tokens of 7 groups over 6300 shared keys,
-// 8 heads of 64 (46 MB): 19 us, on the tensor-core kernel 45.
+// 8 heads of 64 (46 MB): 20 us, without sharing 54.
 #include <algorithm>
 #include <cmath>
 
@@ -46,7 +46,7 @@ struct SharedPlan {
 // tiles: 16 us (11 with few rows of a group, 14 with the own keys in the same launch) instead of 6 (10; 4
 // more where sequences are cut).  Measured, shared and not: 64 sequences of one group, 4352 + 1000 keys,
 // 32/8 heads 37 and 102; 50 of 4 drafts over 13000, 33 and 138; 8 groups of 4, 48 drafts over 8000 + 600,
-// 16 heads 117 and 152; 7 groups of 5 over 6300, 8 heads of 64 19 and 46; 6 of 14, 6 drafts
+// 16 heads 117 and 152; 7 groups of 5 over 6300, 8 heads of 64 20 and 54; 6 of 14, 6 drafts
 // over 2200 + 1400, 6/2 heads 35 and 58; 10 of 3 over 1000, 32 heads 60 and 43; 8 groups of 2 over 4900
 // + 1900, 41 and 25; 3 of 42 drafts over 1800 + 1000, 6/2 heads 22 and 17.
 bool sharing_pays(int32_t B, int32_t groups, int32_t Hq, int32_t Hkv, int32_t d, int32_t D_max,

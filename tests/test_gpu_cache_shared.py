@@ -402,3 +402,24 @@ def test_workspace_and_refusals(ssd):
         bad[i] = x
         with pytest.raises(ssd.SsdError):
             ssd.ssd_cache_attention_shared(*bad)
+
+
+@pytest.mark.parametrize("D,Hq,Hkv", [(1, 8, 2), (1, 4, 4), (40, 4, 2)])
+def test_two_calls_at_once(ssd, D, Hq, Hkv):
+    """Calls on two streams, each with a workspace of its own, give what each gives alone."""
+    calls = []
+    for seed, n in ((1, 6), (2, 40)):
+        own = [20 + 31 * i % 400 for i in range(n)]
+        b = Batch(seed=seed, start=[0, n // 3, n], shared=[30, 60], own=own, nd=[D] * n, D=D, Hq=Hq, Hkv=Hkv,
+                  d=128, block=16)
+        o, ls, st = b.run(ssd)
+        assert st == 0 and b.shares
+        calls.append((b, o.clone(), ls.clone(), torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for b, _, _, stream in calls:
+            ssd.ssd_cache_attention_shared(*b.args, stream=stream)
+    torch.cuda.synchronize()
+    for b, o, ls, _ in calls:
+        now, lse, st = b.args[17], b.args[18], b.args[21]
+        assert st.item() == 0 and torch.equal(now.view(torch.int16), o.view(torch.int16)) and torch.equal(lse, ls)

@@ -226,3 +226,28 @@ def test_no_rows(ssd):
     ssd.ssd_scaled_matmul(0, 4, 16, t, 16, c, 4, t, 16, c, 4, None, 0, c, 4, st)
     torch.cuda.synchronize()
     assert st.item() == 0 and (c == 3.0).all()
+
+
+def test_products_at_once(ssd):
+    """Products of every kernel on two streams give what each gives alone."""
+    def call(c, out, st, stream=None):
+        ssd.ssd_scaled_matmul(c.M, c.N, c.K, c.dev["a"], c.lda, c.dev["sa"], c.ldas, c.dev["w"], c.ldw,
+                              c.dev["sw"], c.ldws, None, 0, out, c.N, st, stream=stream)
+
+    cases = [Case(M, N, 2100, M) for M, N in ((5, 1500), (40, 3000), (60, 300), (200, 1000), (1500, 2049), (2100, 2304))]
+    st, streams = torch.zeros(1, dtype=torch.int32, device="cuda"), [torch.cuda.Stream() for _ in range(2)]
+    out = [torch.zeros((c.M, c.N), dtype=torch.bfloat16, device="cuda") for c in cases]
+    alone = []
+    for c, o in zip(cases, out):
+        call(c, o, st)
+        torch.cuda.synchronize()
+        alone.append(o.clone())
+        o.zero_()
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for i, (c, o) in enumerate(zip(cases, out)):
+            call(c, o, st, streams[i % 2])
+    torch.cuda.synchronize()
+    assert st.item() == 0
+    for o, a in zip(out, alone):
+        assert torch.equal(o.view(torch.int16), a.view(torch.int16))

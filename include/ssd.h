@@ -695,7 +695,9 @@ ssd_status ssd_cache_attention(const ssd_grid* grid, const ssd_block_cache* cach
  * group_start and shared are not read.  ssd_set_cache_sharing(how) is
  * process-wide, for callers who know better (tables much wider than their
  * sequences): 0 by the estimate (the default), 1 always sharing, 2 never; it
- * holds for workspace queries and calls after it.
+ * holds for workspace queries and calls after it.  A call reads it once; one whose
+ * workspace was asked for under another setting is refused (SSD_ERR_WORKSPACE) if
+ * that is too small for the way it would go now.
  * Device errors beside those of ssd_cache_attention(): groups or shared out of
  * range, more shared tokens than cache_len (DEVICE_BOUNDS; rows of the
  * sequences concerned untouched, or, where group_start does not ascend, of no

@@ -5,7 +5,7 @@
 
 #include <atomic>
 
-#include "kernels.cuh"
+#include "cache_attention.cuh"
 
 using namespace ssd;
 
@@ -127,10 +127,13 @@ ssd_status attention(const ssd_grid* grid, const ssd_block_cache* cache, int32_t
   if (!aligned(q, 16) || !aligned(o, 16)) return SSD_ERR_INVALID_ARG;
   if (!(scale >= 0.f) || !isfinite(scale)) return SSD_ERR_INVALID_ARG;
   const int32_t L_max = max_blocks * cache->block;
-  const size_t need =
-      groups > 0 ? cache_attention_shared_workspace(B, groups, Hq, cache->Hkv, cache->d, D_max, L_max,
-                                                    max_shared * cache->block)
-                 : cache_attention_workspace(B, Hq, cache->Hkv, cache->d, D_max, L_max);
+  CacheSharedPlan plan{};
+  if (groups > 0)
+    plan = cache_attention_shared_plan(cache_sharing(), B, groups, Hq, cache->Hkv, cache->d, D_max, L_max,
+                                       max_shared * cache->block);
+  const size_t need = groups > 0
+                          ? cache_attention_shared_bytes(plan, B, Hq, cache->Hkv, cache->d, D_max, L_max)
+                          : cache_attention_workspace(B, Hq, cache->Hkv, cache->d, D_max, L_max);
   if (need > 0 && (workspace == nullptr || workspace_bytes < need)) return SSD_ERR_WORKSPACE;
   if (need > 0 && !aligned(workspace, 16)) return SSD_ERR_INVALID_ARG;
   CacheAttnArgs a{};
@@ -154,7 +157,7 @@ ssd_status attention(const ssd_grid* grid, const ssd_block_cache* cache, int32_t
   a.max_shared = max_shared;
   a.group_start = group_start;
   a.shared = shared;
-  return from_cuda(groups > 0 ? launch_cache_attention_shared(a, workspace, (cudaStream_t)stream)
+  return from_cuda(groups > 0 ? launch_cache_attention_shared(a, plan, workspace, (cudaStream_t)stream)
                               : launch_cache_attention(a, workspace, (cudaStream_t)stream));
 }
 
@@ -264,7 +267,9 @@ size_t ssd_cache_attention_shared_workspace(int32_t B, int32_t groups, int32_t H
                                             int32_t D_max, int32_t L_max, int32_t max_shared) {
   if (groups <= 0 || max_shared < 0 || max_shared > L_max) return 0;
   if (B <= 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv != 0 || d <= 0 || D_max <= 0 || L_max <= 0) return 0;
-  return cache_attention_shared_workspace(B, groups, Hq, Hkv, d, D_max, L_max, max_shared);
+  return cache_attention_shared_bytes(
+      cache_attention_shared_plan(cache_sharing(), B, groups, Hq, Hkv, d, D_max, L_max, max_shared), B, Hq, Hkv, d,
+      D_max, L_max);
 }
 
 ssd_status ssd_cache_attention_shared(const ssd_grid* grid, const ssd_block_cache* cache, int32_t B,

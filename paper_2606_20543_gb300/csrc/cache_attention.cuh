@@ -383,4 +383,22 @@ cudaError_t launch_cache_attention_mma(const CacheAttnArgs& a, const CacheMmaPla
 cudaError_t launch_cache_attention_stack(const CacheAttnArgs& a, const CacheAttnLaunch& L, int32_t rows,
                                          cudaStream_t stream);
 
+// cache_attention_shared.cu: the way that a call for groups goes.  Made once a call: the workspace is
+// checked against the plan that is launched, whatever another thread sets meanwhile.  how: a
+// kShare...; max_shared: tokens.
+struct CacheSharedPlan {
+  bool plain;   // every sequence by itself: ssd_cache_attention()
+  bool own_tc;  // the own keys on the tensor-core kernel, too
+  int32_t few;  // rows of a group, if the shared keys are on the mma.sync kernel, else 0
+  CacheMmaPlan mma;
+  int32_t s_units, s_splits, s_min_tiles, splits, min_tiles;
+  int64_t s_rows, rows;  // part rows
+};
+CacheSharedPlan cache_attention_shared_plan(int32_t how, int32_t B, int32_t groups, int32_t Hq, int32_t Hkv,
+                                            int32_t d, int32_t D_max, int32_t L_max, int32_t max_shared);
+size_t cache_attention_shared_bytes(const CacheSharedPlan& p, int32_t B, int32_t Hq, int32_t Hkv, int32_t d,
+                                    int32_t D_max, int32_t L_max);
+cudaError_t launch_cache_attention_shared(const CacheAttnArgs& a, const CacheSharedPlan& p, void* ws,
+                                          cudaStream_t stream);
+
 }  // namespace ssd

@@ -29,15 +29,6 @@ constexpr int kSharedPartTiles = 256;  // and about the most
 constexpr double kSharedFixed = 9.5;   // tiles that a unit's set-up, way out and share of the join are worth,
 constexpr double kFewFixed = 6;        // and one of few rows on the mma.sync kernel
 
-struct SharedPlan {
-  bool plain;   // every sequence by itself: ssd_cache_attention()
-  bool own_tc;  // the own keys on the tensor-core kernel, too
-  int32_t few;  // rows of a group, if the shared keys are on the mma.sync kernel, else 0
-  CacheMmaPlan mma;
-  int32_t s_units, s_splits, s_min_tiles, splits, min_tiles;
-  int64_t s_rows, rows;  // part rows
-};
-
 // Whether sharing pays, by what both ways take (us, from the largest lengths that the call allows).  A
 // tile of the tensor-core kernel takes an SM 4.8e-3 of a GPU's us where all its warps have rows,
 // less where some have none; the mma.sync kernel streams keys at 5.6 (64-wide heads: 6.4) TB/s; a CTA
@@ -50,7 +41,7 @@ struct SharedPlan {
 // over 2200 + 1400, 6/2 heads 35 and 58; 10 of 3 over 1000, 32 heads 60 and 43; 8 groups of 2 over 4900
 // + 1900, 41 and 25; 3 of 42 drafts over 1800 + 1000, 6/2 heads 22 and 17.
 bool sharing_pays(int32_t B, int32_t groups, int32_t Hq, int32_t Hkv, int32_t d, int32_t D_max,
-                  int32_t L_max, int32_t max_shared, const SharedPlan& p) {
+                  int32_t L_max, int32_t max_shared, const CacheSharedPlan& p) {
   const double G = Hq / Hkv, per_seq = D_max * G, rows = (double)B * D_max * Hq;
   const double shared = std::ceil(max_shared / 64.0), own = std::ceil((L_max - max_shared) / 64.0);
   const double tiles_r = std::max<double>(groups, B * per_seq / 128 + groups / 2.0);
@@ -71,49 +62,6 @@ bool sharing_pays(int32_t B, int32_t groups, int32_t Hq, int32_t Hkv, int32_t d,
                        std::max(us_of_tile * (shared + own), 0.7 * B * (shared + own) / ctas);
   const double few = std::max(us_of_tile / B * groups * shared, 0.7 * shared / p.s_splits);
   return (p.few > 0 ? 11 + few : 16 + stacked) + us_of_tile * own + 8e-3 * B * Hkv + join < 0.9 * alone;
-}
-
-SharedPlan make_plan(int32_t B, int32_t groups, int32_t Hq, int32_t Hkv, int32_t d, int32_t D_max,
-                     int32_t L_max, int32_t max_shared) {
-  SharedPlan p{};
-  const int64_t G = Hq / Hkv, per_seq = D_max * G, rows = (int64_t)B * D_max * Hq;
-  const int32_t how = cache_sharing();
-  p.plain = max_shared <= 0 || how == kShareNever ||
-            (how != kShareAlways && (2 * (int64_t)groups > B || cache_attention_few(B, Hkv, per_seq, L_max)));
-  if (p.plain) return p;
-  // (a group's last tile may be part empty)
-  const int64_t tiles_r = (B * per_seq) / 128 + groups, tiles = (max_shared + kCacheTile - 1) / kCacheTile;
-  // Parts of the shared keys: n of them make base * n units, which take an SM's share of base * n *
-  // kSharedFixed tiles beside the tiles themselves, and the end waits for a unit of tiles / n: least for
-  // n = sqrt(tiles * SMs / (base * kSharedFixed)); and no second round for a few units.  Measured (us, by
-  // n): 64 sequences of one group over 4352 keys, 32/8 heads 1: 82, 3: 41, 6: 36, 11: 39, 20: 50; 72 of
-  // two groups over 11900, 32/8 heads 5: 79, 10: 55, 20: 66, 32: 88; 48 drafts, 8 groups of 4 over 1500
-  // to 8000, 16 heads 1: 138, 2: 128, 3: 119, 5: 130, 8: 149.
-  p.own_tc = per_seq > 16;
-  p.few = !p.own_tc && B * per_seq <= 16 * (int64_t)groups ? (int32_t)((B * per_seq + groups - 1) / groups) : 0;
-  const int64_t sms = device_sm_count(), base = tiles_r * Hkv, places = (p.few > 0 && d == 64 ? 3 : 2) * sms;
-  int64_t n = (int64_t)std::ceil(std::sqrt(tiles * sms / ((p.few > 0 ? kFewFixed : kSharedFixed) * base)));
-  if (base <= places && base * n > places && 4 * base * n <= 7 * places) n = places / base;
-  p.s_min_tiles = (int32_t)std::min<int64_t>(kSharedPartTiles / 2, std::max<int64_t>(kSharedTiles, tiles / n));
-  p.s_splits = (int32_t)std::max<int64_t>(1, tiles / p.s_min_tiles);
-  if (base * p.s_splits > INT32_MAX / 2) {
-    p.plain = true;
-    return p;
-  }
-  p.s_units = (int32_t)(base * p.s_splits);
-  p.s_rows = rows * p.s_splits;
-  if (how != kShareAlways && !sharing_pays(B, groups, Hq, Hkv, d, D_max, L_max, max_shared, p)) {
-    p.plain = true;
-    return p;
-  }
-  if (p.own_tc) {
-    cache_attention_tc_plan(B, Hq, Hkv, D_max, L_max, &p.splits, &p.min_tiles);
-    p.rows = rows * p.splits;
-  } else {
-    p.mma = cache_attention_mma_plan(B, Hq, Hkv, D_max, L_max);
-    p.rows = cache_attention_mma_rows(B, Hkv, p.mma, true);
-  }
-  return p;
 }
 
 size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
@@ -229,16 +177,57 @@ __global__ void __launch_bounds__(256) cache_attn_join_kernel(CacheAttnArgs a, C
 
 }  // namespace
 
-size_t cache_attention_shared_workspace(int32_t B, int32_t groups, int32_t Hq, int32_t Hkv, int32_t d,
-                                        int32_t D_max, int32_t L_max, int32_t max_shared) {
-  const SharedPlan p = make_plan(B, groups, Hq, Hkv, d, D_max, L_max, max_shared);
+CacheSharedPlan cache_attention_shared_plan(int32_t how, int32_t B, int32_t groups, int32_t Hq, int32_t Hkv,
+                                            int32_t d, int32_t D_max, int32_t L_max, int32_t max_shared) {
+  CacheSharedPlan p{};
+  const int64_t G = Hq / Hkv, per_seq = D_max * G, rows = (int64_t)B * D_max * Hq;
+  p.plain = max_shared <= 0 || how == kShareNever ||
+            (how != kShareAlways && (2 * (int64_t)groups > B || cache_attention_few(B, Hkv, per_seq, L_max)));
+  if (p.plain) return p;
+  // (a group's last tile may be part empty)
+  const int64_t tiles_r = (B * per_seq) / 128 + groups, tiles = (max_shared + kCacheTile - 1) / kCacheTile;
+  // Parts of the shared keys: n of them make base * n units, which take an SM's share of base * n *
+  // kSharedFixed tiles beside the tiles themselves, and the end waits for a unit of tiles / n: least for
+  // n = sqrt(tiles * SMs / (base * kSharedFixed)); and no second round for a few units.  Measured (us, by
+  // n): 64 sequences of one group over 4352 keys, 32/8 heads 1: 82, 3: 41, 6: 36, 11: 39, 20: 50; 72 of
+  // two groups over 11900, 32/8 heads 5: 79, 10: 55, 20: 66, 32: 88; 48 drafts, 8 groups of 4 over 1500
+  // to 8000, 16 heads 1: 138, 2: 128, 3: 119, 5: 130, 8: 149.
+  p.own_tc = per_seq > 16;
+  p.few = !p.own_tc && B * per_seq <= 16 * (int64_t)groups ? (int32_t)((B * per_seq + groups - 1) / groups) : 0;
+  const int64_t sms = device_sm_count(), base = tiles_r * Hkv, places = (p.few > 0 && d == 64 ? 3 : 2) * sms;
+  int64_t n = (int64_t)std::ceil(std::sqrt(tiles * sms / ((p.few > 0 ? kFewFixed : kSharedFixed) * base)));
+  if (base <= places && base * n > places && 4 * base * n <= 7 * places) n = places / base;
+  p.s_min_tiles = (int32_t)std::min<int64_t>(kSharedPartTiles / 2, std::max<int64_t>(kSharedTiles, tiles / n));
+  p.s_splits = (int32_t)std::max<int64_t>(1, tiles / p.s_min_tiles);
+  if (base * p.s_splits > INT32_MAX / 2) {
+    p.plain = true;
+    return p;
+  }
+  p.s_units = (int32_t)(base * p.s_splits);
+  p.s_rows = rows * p.s_splits;
+  if (how != kShareAlways && !sharing_pays(B, groups, Hq, Hkv, d, D_max, L_max, max_shared, p)) {
+    p.plain = true;
+    return p;
+  }
+  if (p.own_tc) {
+    cache_attention_tc_plan(B, Hq, Hkv, D_max, L_max, &p.splits, &p.min_tiles);
+    p.rows = rows * p.splits;
+  } else {
+    p.mma = cache_attention_mma_plan(B, Hq, Hkv, D_max, L_max);
+    p.rows = cache_attention_mma_rows(B, Hkv, p.mma, true);
+  }
+  return p;
+}
+
+size_t cache_attention_shared_bytes(const CacheSharedPlan& p, int32_t B, int32_t Hq, int32_t Hkv, int32_t d,
+                                    int32_t D_max, int32_t L_max) {
   if (p.plain) return cache_attention_workspace(B, Hq, Hkv, d, D_max, L_max);
   return part_bytes(p.s_rows, d) + part_bytes(p.rows, d) + align256((size_t)B * sizeof(int2));
 }
 
-cudaError_t launch_cache_attention_shared(const CacheAttnArgs& a, void* ws, cudaStream_t stream) {
+cudaError_t launch_cache_attention_shared(const CacheAttnArgs& a, const CacheSharedPlan& p, void* ws,
+                                          cudaStream_t stream) {
   const int32_t S = a.cache.block, L_max = a.max_blocks * S, d = a.cache.d;
-  const SharedPlan p = make_plan(a.B, a.groups, a.Hq, a.cache.Hkv, d, a.D_max, L_max, a.max_shared * S);
   if (p.plain) {
     CacheAttnArgs one = a;
     one.groups = 0;

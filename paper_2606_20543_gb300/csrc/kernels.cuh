@@ -486,12 +486,8 @@ struct CacheAttnArgs {
 size_t cache_attention_workspace(int32_t B, int32_t Hq, int32_t Hkv, int32_t d, int32_t D_max,
                                  int32_t L_max);
 cudaError_t launch_cache_attention(const CacheAttnArgs& a, void* ws, cudaStream_t stream);
-// ---- cache_attention_shared.cu (max_shared: tokens)
-size_t cache_attention_shared_workspace(int32_t B, int32_t groups, int32_t Hq, int32_t Hkv, int32_t d,
-                                        int32_t D_max, int32_t L_max, int32_t max_shared);
 enum { kShareByEstimate = 0, kShareAlways = 1, kShareNever = 2 };
 int32_t cache_sharing();  // (ssd_set_cache_sharing)
-cudaError_t launch_cache_attention_shared(const CacheAttnArgs& a, void* ws, cudaStream_t stream);
 
 // ---- sample.cu
 struct SampleArgs {

@@ -703,6 +703,7 @@ ssd_status ssd_cache_attention(const ssd_grid* grid, const ssd_block_cache* cach
  * sequences concerned untouched, or, where group_start does not ascend, of no
  * certain value). */
 ssd_status ssd_set_cache_sharing(int32_t how);
+int32_t ssd_get_cache_sharing(void); /* as it is set now */
 size_t ssd_cache_attention_shared_workspace(int32_t B, int32_t groups, int32_t Hq, int32_t Hkv, int32_t d,
                                             int32_t D_max, int32_t L_max, int32_t max_shared);
 ssd_status ssd_cache_attention_shared(const ssd_grid* grid, const ssd_block_cache* cache, int32_t B,

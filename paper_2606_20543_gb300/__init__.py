@@ -33,7 +33,7 @@ EXPORTED = ["ssd_abi_version", "ssd_status_string", "ssd_set_wait_limit",
             "ssd_verify_accept",
             "ssd_cache_plan", "ssd_rotary_table", "ssd_cache_append", "ssd_cache_append_norm",
             "ssd_cache_attention_workspace", "ssd_cache_attention",
-            "ssd_set_cache_sharing", "ssd_cache_attention_shared_workspace",
+            "ssd_set_cache_sharing", "ssd_get_cache_sharing", "ssd_cache_attention_shared_workspace",
             "ssd_cache_attention_shared", "ssd_sample",
             "ssd_quantize", "ssd_scaled_matmul"]
 
@@ -176,6 +176,7 @@ def load(path: Optional[str] = None) -> ctypes.CDLL:
         "ssd_cache_attention": (I32, [ctypes.POINTER(Grid), ctypes.POINTER(BlockCache), I32, I32, P,
                                       P, P, P, I32, P, I32, P, F, P, P, P, SZ, P, P]),
         "ssd_set_cache_sharing": (I32, [I32]),
+        "ssd_get_cache_sharing": (I32, []),
         "ssd_cache_attention_shared_workspace": (SZ, [I32, I32, I32, I32, I32, I32, I32, I32]),
         "ssd_cache_attention_shared": (I32, [ctypes.POINTER(Grid), ctypes.POINTER(BlockCache), I32, I32,
                                              P, P, I32, I32, P, P, P, P, I32, P, I32, P, F, P, P, P, SZ,
@@ -503,15 +504,15 @@ def ssd_cache_attention(g: Grid, c: BlockCache, B, Hq, cache_len, n_drafts, draf
         _ptr(workspace), workspace_bytes, _ptr(status), _stream(stream)))
 
 
-_cache_sharing = 0
-
-
 def ssd_set_cache_sharing(how: int) -> None:
     """Process-wide: 0 ssd_cache_attention_shared() shares where it pays by its estimate (the
     default), 1 always, 2 never; for workspace queries and calls after it."""
-    global _cache_sharing
     _check("ssd_set_cache_sharing", load().ssd_set_cache_sharing(int(how)))
-    _cache_sharing = int(how)  # (workspaces that callers keep were asked for under it)
+
+
+def ssd_get_cache_sharing() -> int:
+    """What ssd_set_cache_sharing() set last, by whichever caller of the library."""
+    return load().ssd_get_cache_sharing()
 
 
 def ssd_cache_attention_shared_workspace(B, groups, Hq, Hkv, d, D_max, L_max, max_shared) -> int:

@@ -173,6 +173,8 @@ ssd_status ssd_set_cache_sharing(int32_t how) {
   return SSD_OK;
 }
 
+int32_t ssd_get_cache_sharing(void) { return cache_sharing(); }
+
 ssd_status ssd_cache_plan(const ssd_grid* grid, int32_t B, int32_t block, int32_t max_blocks,
                           int32_t N_max, const int32_t* cache_len, const int32_t* n_new,
                           const int32_t* held, const int32_t* ring, int32_t ring_size,

@@ -9,12 +9,11 @@ from __future__ import annotations
 
 import torch
 
-import paper_2606_20543_gb300 as _ssd
-
 from . import (Grid, Rng, Sampling, cache as make_cache, rotary as make_rotary,
                ssd_cache_append, ssd_cache_append_norm, ssd_cache_attention,
                ssd_cache_attention_shared, ssd_cache_attention_shared_workspace,
-               ssd_cache_attention_workspace, ssd_cache_plan, ssd_rotary_table, ssd_sample)
+               ssd_cache_attention_workspace, ssd_cache_plan, ssd_get_cache_sharing,
+               ssd_rotary_table, ssd_sample)
 
 
 def _row_stride(x):
@@ -89,8 +88,8 @@ class PagedDecode:
         self.groups, self.max_shared = 0, 0
 
     def _workspace(self, N):
-        key = N, self.groups, self.max_shared, _ssd._cache_sharing
-        if self._ws.get(N, (None, None))[1] != key:
+        key = N, self.groups, self.max_shared, ssd_get_cache_sharing()
+        while self._ws.get(N, (None, None))[1] != key:
             sizes = (self.Hq, self.Hkv, self.d, N, self.max_blocks * self.block)
             n = (ssd_cache_attention_shared_workspace(self.B, self.groups, *sizes, self.max_shared * self.block)
                  if self.groups else ssd_cache_attention_workspace(self.B, *sizes))
@@ -100,6 +99,7 @@ class PagedDecode:
                     self._outgrown.append(ws)  # (graphs may have captured it)
                 ws = torch.empty((max(n, 16),), dtype=torch.uint8, device=self.device)
             self._ws[N] = ws, key
+            key = key[:3] + (ssd_get_cache_sharing(),)  # (set by another thread meanwhile: asked again)
         ws = self._ws[N][0]
         return ws, ws.numel()
 

@@ -99,11 +99,13 @@ const char* ssd_status_string(ssd_status s);
  * releases its tensor memory and returns, so the context stays usable.  Both
  * controls are process-wide and apply to launches enqueued after the call.
  *  ssd_set_wait_limit(polls): the polls after which each bounded wait of the
- *    kernels with grid-wide waits (the fused lm_head, the draft predictor)
- *    gives up; 0 restores the default, well above a second of waiting.
+ *    kernels with grid-wide waits (the fused lm_head, the draft predictor) and of
+ *    the 8-bit products of few rows gives up; 0 restores the default, well above
+ *    a second of waiting.
  *  ssd_set_barrier_shortfall(n): makes those kernels' grid-wide waits (the
  *    lm_head's grid barriers, the predictor's wait for the previous product)
- *    expect n arrivals more than their CTAs make, so that they cannot
+ *    expect n arrivals more than their CTAs make, and the few-row products'
+ *    wait for their sums one more, so that they cannot
  *    complete and run out after the wait limit: a way to exercise the timeout
  *    path without faulting anything.  0 (the default) turns it off.
  * ------------------------------------------------------------------------- */
@@ -778,7 +780,8 @@ ssd_status ssd_quantize(int32_t rows, int32_t K, int32_t block_rows, const void*
  *     C[m][n] = sum_g a_scale[g][m] * w_scale[g][n / 128] *
  *                   sum_{k in g} A[m][k] W[n][k]   + add[m][n]
  * The scales' product and both sums in float32; rounded once, to C's type.  A NaN in A goes to its row
- * of C, one in W to its column.
+ * of C, one in W to its column.  After a wait that ran out (SSD_ERR_TIMEOUT) tiles whose sums are not known
+ * are not written.
  *   a        dev e4m3 [M][K], rows lda bytes apart; w dev e4m3 [N][K], ldw
  *   a_scale  dev float32 [ceil(K / 128)][ldas], ldas >= M
  *   w_scale  dev float32 [ceil(K / 128)][ldws], ldws >= ceil(N / 128)

@@ -164,9 +164,10 @@ __device__ __forceinline__ bool mbar_wait_warp(uint64_t* bar, uint32_t parity, i
 
 // mbar_wait_warp() with one try ahead of the loop: a wait for what is there already takes a try
 // and a vote (through the loop 220 cycles on a busy SM, of the 2200 that a tile of 64 keys takes).
-__device__ __forceinline__ bool wait_warp(uint64_t* bar, uint32_t parity, int32_t* status) {
+__device__ __forceinline__ bool wait_warp(uint64_t* bar, uint32_t parity, int32_t* status,
+                                          uint32_t max_polls = kMaxPolls) {
   if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
-  return mbar_wait_warp(bar, parity, status);
+  return mbar_wait_warp(bar, parity, status, max_polls);
 }
 
 // After a wait that gave up: this CTA's copies and products still in flight land

@@ -90,10 +90,19 @@ __host__ __device__ constexpr uint32_t idesc_e4m3(int m, int n) {
   return (1u << 4) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
 }
 
-// mbar_drain(), inlined: a call has no place beside setmaxnreg.
+// mbar_drain(), inlined: a call has no place beside setmaxnreg.  Called by whole warps, whose lanes may
+// leave the loop one by one: together again behind it, as the barriers that follow want them.
 __device__ __forceinline__ void drain(uint64_t* bar, uint32_t parity) {
 #pragma unroll 1
   for (int i = 0; i < (1 << 14) && !mbar_try_wait(bar, parity); ++i) __nanosleep(256);
+  __syncwarp();
+}
+// The same of what is on its way in any case: without a sleep at first.
+__device__ __forceinline__ void land(uint64_t* bar, uint32_t parity) {
+  bool here = false;
+#pragma unroll 1
+  for (int i = 0; i < 1024 && !here; ++i) here = __all_sync(0xffffffffu, mbar_try_wait(bar, parity));
+  if (!here) drain(bar, parity);
 }
 
 // A warp's CH columns from n0 on of `rows` rows of C from m0 on: staged with kPitch floats a row, each
@@ -651,6 +660,7 @@ scaled_matmul_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
 
   // ---- teardown
   tc_fence_before();
+  __syncwarp();  // (cluster barriers take whole warps)
   if constexpr (PAIR) cluster_sync_all();
   else __syncthreads();
   if (warp == EW + 1) {
@@ -682,10 +692,15 @@ struct Few {
   static_assert(S >= 2 && S * kStage >= TN * kLaneRows * 4, "a CTA's sums fit where its stages were");
 };
 
+struct FewLaunch {
+  int32_t tiles_w, total, splits;
+  uint32_t max_polls, shortfall;  // (ssd_set_wait_limit, ssd_set_barrier_shortfall)
+};
+
 template <int TN, int U>
 __global__ void __launch_bounds__(Few<TN, U>::kThreads, 2)
 scaled_matmul_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmW,
-                         ScaledMatmulArgs a, int32_t tiles_w, int32_t total, int32_t splits) {
+                         ScaledMatmulArgs a, FewLaunch L) {
   using H = Few<TN, U>;
   constexpr int S = H::S, B = 2, EW = H::EW, CW = H::CW;
   extern __shared__ __align__(1024) unsigned char smem_raw[];
@@ -693,9 +708,10 @@ scaled_matmul_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_c
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   float* scales = reinterpret_cast<float*>(smem + S * H::kStage);
   __shared__ uint64_t full[S], empty[S], tfull[B], tempty[B];
-  __shared__ uint32_t tmem_slot;
+  __shared__ uint32_t tmem_slot, gave_up;  // (a warp of the epilogue: its sums are not known)
   pdl_wait();
 
+  const int32_t tiles_w = L.tiles_w, total = L.total, splits = L.splits;
   const int32_t tid = threadIdx.x, lane = tid & 31, warp = (int32_t)warp_uniform(tid >> 5);
   const int32_t rank = splits > 1 ? (int32_t)(blockIdx.x % splits) : 0;
   const int32_t first = blockIdx.x / splits, step = gridDim.x / splits;
@@ -704,12 +720,13 @@ scaled_matmul_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_c
   const int32_t kb_hi = (int32_t)((int64_t)blocks * (rank + 1) / splits);
   if (warp == EW && lane < 2) prefetch_tensormap(lane == 0 ? &tmA : &tmW);
   if (tid == EW * 32) {
+    gave_up = 0;
     for (int i = 0; i < S; ++i) {
       mbar_init(&full[i], 1);
       mbar_init(&empty[i], 1);
     }
     for (int i = 0; i < B; ++i) {
-      mbar_init(&tfull[i], 1);
+      mbar_init(&tfull[i], 1 + L.shortfall);
       mbar_init(&tempty[i], EW);
     }
     fence_barrier_init();
@@ -743,7 +760,7 @@ scaled_matmul_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_c
           __syncthreads();
           begun = true;
         }
-        if (n >= S) ok = wait_warp(&empty[s], ph, a.status);
+        if (n >= S) ok = wait_warp(&empty[s], ph, a.status, L.max_polls);
         if (!ok) break;
         if (leader) {
           unsigned char* dst = smem + s * H::kStage;
@@ -765,8 +782,8 @@ scaled_matmul_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_c
       }
     }
     if (!begun) __syncthreads();
-    if (!ok)
-      for (int32_t u = max(0, n - S); u < n; ++u) drain(&full[u % S], (u / S) & 1);
+    // the last copies land here, also where nobody waits for them any more
+    for (int32_t u = max(0, n - S); u < n; ++u) land(&full[u % S], (u / S) & 1);
   } else if (warp == EW + 1) {
     // ----------------------------------------------------------- products
     constexpr uint32_t kIdesc = idesc_e4m3(128, TN);
@@ -780,9 +797,9 @@ scaled_matmul_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_c
 #pragma unroll 1
       for (int32_t kb = kb_lo; kb < kb_hi; kb += U, ++n) {
         const int b = n % B;
-        if (n >= B) ok = wait_warp(&tempty[b], (n / B - 1) & 1, a.status);
+        if (n >= B) ok = wait_warp(&tempty[b], (n / B - 1) & 1, a.status, L.max_polls);
         // (last: W is what these products wait for)
-        ok = ok && wait_warp(&full[s], ph, a.status);
+        ok = ok && wait_warp(&full[s], ph, a.status, L.max_polls);
         if (!ok) break;
         tc_fence_after();
         const uint64_t dw = smem_desc(base + s * H::kStage, 16, 1024);
@@ -807,7 +824,7 @@ scaled_matmul_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_c
         }
       }
     }
-    if (!ok && n > 0) drain(&tfull[(n - 1) % B], ((n - 1) / B) & 1);
+    if (n > 0) land(&tfull[(n - 1) % B], ((n - 1) / B) & 1);  // (nor does an epilogue that gave up)
   } else {
     // ----------------------------------------------------------- epilogue
     // a lane's row of W, the warp's first row of A
@@ -870,7 +887,7 @@ scaled_matmul_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_c
         }
         const float* sc = scales + ((half * kAhead + (kb - kb_lo) % kAhead) * EW + warp) * H::kSlot;
         const int b = n % B;
-        ok = wait_warp(&tfull[b], (n / B) & 1, a.status);
+        ok = wait_warp(&tfull[b], (n / B) & 1, a.status, L.max_polls);
         if (!ok) break;
         tc_fence_after();
         // (a unit's blocks lie side by side: where a warp takes all of their columns, one read)
@@ -931,38 +948,44 @@ scaled_matmul_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_c
       }
     }
     cp_async_wait<0>();
+    if (!ok && lane == 0) gave_up = 1;
   }
 
   // ---- teardown
   tc_fence_before();
+  __syncwarp();  // (cluster barriers take whole warps)
   if (splits > 1) {
     cluster_sync_all();
-    // every CTA of the cluster adds up the rows of A that are its rank's
+    // every CTA of the cluster adds up the rows of A that are its rank's (none where a CTA gave up)
     const int32_t c = first / tiles_w, n = (first - c * tiles_w) * kLaneRows + (tid & 127);
     const int32_t live = min(TN, a.M - c * TN), step = splits * (EW / 4);
-    if (tid < EW * 32 && n < a.N) {
+    if (warp < EW) {
       constexpr int kTogether = CW / 16;  // rows whose sums are asked for together
       const uint32_t at = smem_u32(smem) + (tid & 127) * 4;
+      // (asked for ahead of the sums; splits is a power of two)
+      const float unknown = ld_peer(peer_addr(smem_u32(&gave_up), lane & (splits - 1)));
 #pragma unroll 1
       for (int32_t t0 = rank + (tid >> 7) * splits; t0 < live; t0 += kTogether * step) {
         float v[kTogether][kMaxSplits], more[kTogether];
 #pragma unroll
         for (int u = 0; u < kTogether; ++u) {
           const int32_t t = min(t0 + u * step, live - 1);
-          more[u] = added(a, c * TN + t, n);
+          more[u] = n < a.N ? added(a, c * TN + t, n) : 0.f;
 #pragma unroll
           for (int32_t r = 0; r < kMaxSplits; ++r)
             v[u][r] = r < splits ? ld_peer(peer_addr(at + t * kLaneRows * 4, r)) : 0.f;
         }
+        const bool known = !__any_sync(0xffffffffu, __float_as_uint(unknown) != 0);  // (by all lanes)
 #pragma unroll
         for (int u = 0; u < kTogether; ++u) {
           float x = 0.f;
 #pragma unroll
           for (int32_t r = 0; r < kMaxSplits; ++r) x += v[u][r];
-          if (t0 + u * step < live) store_one(a, c * TN + t0 + u * step, n, x + more[u]);
+          if (known && t0 + u * step < live && n < a.N) store_one(a, c * TN + t0 + u * step, n, x + more[u]);
         }
       }
     }
+    __syncwarp();
     cluster_sync_all();
   } else {
     __syncthreads();
@@ -1046,11 +1069,12 @@ cudaError_t launch_few(const ScaledMatmulArgs& a, int32_t splits, cudaStream_t s
   const cudaError_t e = allow_smem(kernel, H::kSmem);
   if (e != cudaSuccess) return e;
   const int32_t tiles_w = ceil_div(a.N, kLaneRows), total = tiles_w * ceil_div(a.M, TN);
+  const FewLaunch L{tiles_w, total, splits, wait_poll_limit(), std::min(barrier_shortfall(), 1u)};
   if (splits > 1)
     return launch_clusters(kernel, dim3((unsigned)(total * splits)), dim3(H::kThreads), H::kSmem, stream, true,
-                           splits, ta, tw, a, tiles_w, total, splits);
+                           splits, ta, tw, a, L);
   return launch_kernel(kernel, dim3((unsigned)std::min(total, 2 * device_sm_count())), dim3(H::kThreads), H::kSmem, stream,
-                       true, ta, tw, a, tiles_w, total, splits);
+                       true, ta, tw, a, L);
 }
 
 }  // namespace

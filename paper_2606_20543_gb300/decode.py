@@ -84,8 +84,9 @@ class PagedDecode:
         self.prob, self.kept = new((B * N_max,), torch.float32), new((B * N_max,), torch.int32)
         self.status = new((1,), torch.int32)
         self._ws, self._outgrown = {}, []
-        # groups that share blocks: of every group its blocks and their ids, of every sequence its group
-        self.groups, self.max_shared = 0, 0
+        # groups that share blocks: of every group its blocks and their ids, of every sequence its group;
+        # by the number of groups, for the graphs that captured them
+        self.groups, self.max_shared, self._groups = 0, 0, {}
 
     def _workspace(self, N):
         key = N, self.groups, self.max_shared, ssd_get_cache_sharing()
@@ -119,32 +120,29 @@ class PagedDecode:
         if min(blocks) < 0 or max(blocks) > self.max_blocks:
             raise ValueError("blocks: between 0 and max_blocks")
         dev = self.device
-        if len(blocks) != self.groups or max(blocks) > self.max_shared:
-            if self.groups:  # (graphs may have captured them)
-                self._outgrown += [self.group_start, self.shared, self._group, self._shared_ids,
-                                   self._shared_own]
-            self.groups, self.max_shared = len(blocks), max(blocks)
+        self.groups = len(blocks)
+        if self.groups not in self._groups:
             new = lambda *shape, t: torch.zeros(shape, dtype=t, device=dev)  # noqa: E731
-            self.group_start = new(self.groups + 1, t=torch.int32)
-            self.shared = new(self.groups, t=torch.int32)
-            self._group = new(self.B, t=torch.int64)
-            self._shared_ids = new(self.groups, max(self.max_shared, 1), t=torch.int32)
-            self._shared_own = new(self.groups, t=torch.int64)
+            self._groups[self.groups] = dict(
+                max_shared=0, group_start=new(self.groups + 1, t=torch.int32), shared=new(self.groups, t=torch.int32),
+                _group=new(self.B, t=torch.int64), _shared_ids=new(self.groups, self.max_blocks, t=torch.int32),
+                _shared_own=new(self.groups, t=torch.int64))
+        kept = self._groups[self.groups]
+        kept["max_shared"] = max(kept["max_shared"], *blocks)
+        self.__dict__.update(kept)
         self.group_start.copy_(torch.tensor(start, dtype=torch.int32))
         self.shared.copy_(torch.tensor(blocks, dtype=torch.int32))
         sizes = [b - a for a, b in zip(start, start[1:])]
         self._group.copy_(torch.repeat_interleave(torch.arange(self.groups), torch.tensor(sizes)))
         first = torch.tensor([min(a, self.B - 1) for a in start[:-1]], device=dev)
         firsts = torch.tensor([a for a, n in zip(start, sizes) if n > 0], device=dev)
-        self._shared_ids.copy_(self.block_table[first, :self._shared_ids.shape[1]])
+        self._shared_ids.copy_(self.block_table[first])
         self._shared_own.copy_(self.shared * torch.tensor([int(n > 0) for n in sizes], device=dev))
         base, joins = self.shared[self._group], torch.ones((self.B,), dtype=torch.bool, device=dev)
         joins[firsts] = False
         joins &= base > 0
-        at = torch.arange(self._shared_ids.shape[1], device=dev)
-        take = joins[:, None] & (at[None] < base[:, None])
-        part = self.block_table[:, :at.numel()]
-        part.copy_(torch.where(take, self._shared_ids[self._group], part))
+        take = joins[:, None] & (torch.arange(self.max_blocks, device=dev)[None] < base[:, None])
+        self.block_table.copy_(torch.where(take, self._shared_ids[self._group], self.block_table))
         self.cache_len.copy_(torch.where(joins, base * self.block, self.cache_len))
         self.held.copy_(torch.where(joins, base, self.held))
 
@@ -240,7 +238,7 @@ class PagedDecode:
         if self.groups:
             alive = torch.zeros_like(self.shared).index_add_(0, self._group, (self.held > 0).to(torch.int32))
             done = (alive == 0) & (self._shared_own > 0)
-            here = done[:, None] & (at[None, :self._shared_ids.shape[1]] < self._shared_own[:, None])
+            here = done[:, None] & (at[None] < self._shared_own[:, None])
             self._give_back(self._shared_ids, here)
             self._shared_own.masked_fill_(done, 0)
             self.shared.masked_fill_(done, 0)

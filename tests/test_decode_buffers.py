@@ -43,3 +43,56 @@ def test_the_workspace_follows_the_switch_whoever_sets_it(ssd):
         assert n >= need() and n == ws.numel()
         sizes.append(need())
     assert sizes[1] > sizes[0]
+
+
+def state(dec, num_blocks):
+    """The tensors that share() and release() work on, of a pool that nothing holds."""
+    import torch
+    i32 = lambda *s: torch.zeros(s, dtype=torch.int32)  # noqa: E731
+    dec.__dict__.update(num_blocks=num_blocks, block_table=i32(dec.B, dec.max_blocks).fill_(-1),
+                        cache_len=i32(dec.B), held=i32(dec.B), status=i32(1),
+                        ring=torch.arange(num_blocks + 1, dtype=torch.int32),
+                        head=torch.zeros(1, dtype=torch.int64), tail=torch.full((1,), num_blocks), _groups={})
+    return dec
+
+
+def cached(dec, b, tokens):
+    """Sequence b caches `tokens` tokens in the pool's next blocks."""
+    n = -(-tokens // dec.block) - int(dec.held[b])
+    at = (int(dec.head) + __import__("torch").arange(n)) % dec.num_blocks
+    dec.block_table[b, int(dec.held[b]):int(dec.held[b]) + n] = dec.ring[at]
+    dec.head += n
+    dec.held[b] += n
+    dec.cache_len[b] = tokens
+
+
+def everyone(dec):
+    import torch
+    return torch.ones((dec.B,), dtype=torch.bool)
+
+
+def free(dec):
+    at = (__import__("torch").arange(int(dec.tail - dec.head)) + int(dec.head)) % dec.num_blocks
+    return sorted(dec.ring[at].tolist())
+
+
+def groups_of(dec, start, blocks):
+    for b, n in zip(start, blocks):
+        cached(dec, b, n * dec.block + 1)
+    dec.share(start, blocks)
+
+
+def test_groups_that_come_again_have_the_buffers_that_graphs_captured(ssd):
+    dec = state(make(0, 0, max_blocks=9), 40)
+    kept, seen = {}, 0
+    for start, blocks in [([0, 2, 4], [3, 2]), ([0, 1, 2, 4], [1, 2, 0]), ([0, 3, 4], [5, 1]), ([0, 4], [2]),
+                          ([0, 1, 4], [1, 3])] * 4:
+        groups_of(dec, start, blocks)
+        here = [t.data_ptr() for t in (dec.group_start, dec.shared)]
+        assert kept.setdefault(len(blocks), here) == here
+        assert dec.group_start.tolist() == start and dec.shared.tolist() == blocks
+        assert dec.max_shared >= max(blocks)
+        dec.release(everyone(dec))
+        assert free(dec) == list(range(40))
+        # nothing is kept beside the buffers of each number of groups
+        assert not dec._outgrown and (seen := max(seen, len(dec._groups))) <= 3

@@ -83,6 +83,7 @@ class PagedDecode:
         self.out_tok = new((B * N_max,), torch.int32, -1)
         self.prob, self.kept = new((B * N_max,), torch.float32), new((B * N_max,), torch.int32)
         self.status = new((1,), torch.int32)
+        # by N; each workspace is larger than the one before by half, so those outgrown take twice the last
         self._ws, self._outgrown = {}, []
         # groups that share blocks: of every group its blocks and their ids, of every sequence its group;
         # by the number of groups, for the graphs that captured them
@@ -98,6 +99,7 @@ class PagedDecode:
             if ws is None or ws.numel() < n:
                 if ws is not None:
                     self._outgrown.append(ws)  # (graphs may have captured it)
+                    n = max(n, ws.numel() * 3 // 2)
                 ws = torch.empty((max(n, 16),), dtype=torch.uint8, device=self.device)
             self._ws[N] = ws, key
             key = key[:3] + (ssd_get_cache_sharing(),)  # (set by another thread meanwhile: asked again)

@@ -96,3 +96,19 @@ def test_groups_that_come_again_have_the_buffers_that_graphs_captured(ssd):
         assert free(dec) == list(range(40))
         # nothing is kept beside the buffers of each number of groups
         assert not dec._outgrown and (seen := max(seen, len(dec._groups))) <= 3
+
+
+def test_outgrown_workspaces_stay_within_twice_the_last(ssd):
+    """Graphs may have captured them, so they are kept; they grow by half at least, so that however often
+    a little more is needed all of them together hold at most twice what the last one does (1 / (1 - 2/3)
+    less itself)."""
+    ssd.ssd_set_cache_sharing(1)
+    so, dec = ssd.load(), make(1, 1, B=16, max_blocks=4000)
+    dec.N_max, sizes = 64, set()
+    for most in list(range(1, 4000, 7)) + [5, 900, 33]:
+        dec.max_shared = most
+        n = dec._workspace(1)[1]
+        assert n >= so.ssd_cache_attention_shared_workspace(16, 1, 8, 2, 128, 1, 64000, 16 * most)
+        sizes.add(n)
+        assert sum(t.numel() for t in dec._outgrown) <= 2 * n
+    assert len(sizes) > 2

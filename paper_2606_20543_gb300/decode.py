@@ -88,6 +88,8 @@ class PagedDecode:
         # groups that share blocks: of every group its blocks and their ids, of every sequence its group;
         # by the number of groups, for the graphs that captured them
         self.groups, self.max_shared, self._groups = 0, 0, {}
+        # blocks that a sequence has of its group; -1 for a place whose group goes on without it, else 1
+        self._base, self._open = new((B,), torch.int32), new((B,), torch.int32, 1)
 
     def _workspace(self, N):
         key = N, self.groups, self.max_shared, ssd_get_cache_sharing()
@@ -113,8 +115,9 @@ class PagedDecode:
         both.  Called between passes, not while an earlier group's blocks are held.  A graph of a pass
         that was captured before the first share() attends without groups, one captured later serves
         every share() of as many groups whose blocks are no more than the most when it was captured;
-        for others it is captured anew.  A sequence that is released can begin anew once all of
-        its group are (their shared blocks go back with the last of them)."""
+        for others it is captured anew.  A place that is released can begin anew once all of its group
+        are (their shared blocks go back with the last of them); a pass with groups that asks tokens of it
+        before leaves it out, as one that plan() cannot serve (status: DEVICE_BOUNDS)."""
         start, blocks = [int(x) for x in group_start], [int(x) for x in blocks]
         if len(start) != len(blocks) + 1 or start[0] != 0 or start[-1] != self.B or not blocks \
                 or any(a > b for a, b in zip(start, start[1:])):
@@ -145,6 +148,8 @@ class PagedDecode:
         joins &= base > 0
         take = joins[:, None] & (torch.arange(self.max_blocks, device=dev)[None] < base[:, None])
         self.block_table.copy_(torch.where(take, self._shared_ids[self._group], self.block_table))
+        self._base.copy_(base)
+        self._open.fill_(1)
         self.cache_len.copy_(torch.where(joins, base * self.block, self.cache_len))
         self.held.copy_(torch.where(joins, base, self.held))
 
@@ -154,6 +159,8 @@ class PagedDecode:
         if not 0 < self.N <= self.N_max:
             raise ValueError("N is between 1 and N_max")
         want = n_new.to(self.n_new).expand(self.B).contiguous()  # (mostly n_new itself)
+        if self.groups:
+            want = torch.minimum(want, want * self._open)  # (less than none, if any, of a place that is not open)
         rows = self.B * self.N
         self.slots, self.pos = self._slots[:rows], self._pos[:rows]
         ssd_cache_plan(self.g, self.B, self.block, self.max_blocks, self.N, self.cache_len,
@@ -232,15 +239,17 @@ class PagedDecode:
         at = torch.arange(self.max_blocks, device=self.device)
         own = mask[:, None] & (at[None] < self.held[:, None])
         if self.groups:
-            own &= at[None] >= self.shared[self._group][:, None]
+            own &= at[None] >= self._base[:, None]
         self._give_back(self.block_table, own)
         self.block_table.masked_fill_(mask[:, None], -1)
         self.cache_len.masked_fill_(mask, 0)
         self.held.masked_fill_(mask, 0)
         if self.groups:
-            alive = torch.zeros_like(self.shared).index_add_(0, self._group, (self.held > 0).to(torch.int32))
+            self._base.masked_fill_(mask, 0)
+            alive = torch.zeros_like(self.shared).index_add_(0, self._group, (self._base > 0).to(torch.int32))
             done = (alive == 0) & (self._shared_own > 0)
             here = done[:, None] & (at[None] < self._shared_own[:, None])
             self._give_back(self._shared_ids, here)
             self._shared_own.masked_fill_(done, 0)
             self.shared.masked_fill_(done, 0)
+            self._open.copy_(1 - 2 * ((self._base == 0) & (self.shared[self._group] > 0)).to(torch.int32))

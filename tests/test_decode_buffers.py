@@ -52,7 +52,8 @@ def state(dec, num_blocks):
     dec.__dict__.update(num_blocks=num_blocks, block_table=i32(dec.B, dec.max_blocks).fill_(-1),
                         cache_len=i32(dec.B), held=i32(dec.B), status=i32(1),
                         ring=torch.arange(num_blocks + 1, dtype=torch.int32),
-                        head=torch.zeros(1, dtype=torch.int64), tail=torch.full((1,), num_blocks), _groups={})
+                        head=torch.zeros(1, dtype=torch.int64), tail=torch.full((1,), num_blocks), _groups={},
+                        _base=i32(dec.B), _open=i32(dec.B).fill_(1))
     return dec
 
 
@@ -112,3 +113,21 @@ def test_outgrown_workspaces_stay_within_twice_the_last(ssd):
         sizes.add(n)
         assert sum(t.numel() for t in dec._outgrown) <= 2 * n
     assert len(sizes) > 2
+
+
+def test_blocks_of_a_place_that_began_anew_come_back(ssd):
+    """Also those in the places of the blocks that its group shares, whichever goes first."""
+    import torch
+    for order in ([1, 0, 2, 3], [0, 2, 1, 3], [3, 2, 1, 0]):
+        dec = state(make(0, 0, max_blocks=9), 40)
+        groups_of(dec, [0, 3, 4], [4, 2])
+        for b in range(3):
+            cached(dec, b, 4 * 16 + 40)
+        dec.release(torch.tensor([False, True, False, False]))
+        assert len(free(dec)) == 40 - 4 - 3 - 3 - 3 and dec._open.tolist() == [1, -1, 1, 1]
+        cached(dec, 1, 50)  # (a pass that was captured before any share())
+        held = [t for t in dec.block_table.flatten().tolist() if t >= 0]
+        assert len(set(held)) + len(free(dec)) == 40
+        for b in order:
+            dec.release(torch.arange(4) == b)
+        assert free(dec) == list(range(40)) and dec.shared.tolist() == [0, 0] and dec._open.tolist() == [1] * 4

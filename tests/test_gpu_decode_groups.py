@@ -102,3 +102,67 @@ def test_graphs_of_as_many_groups_serve_later_groups(ssd):
     p.begin([0, 2, 4], [3, 40])
     p.check(*two)
     p.check(*more)
+
+
+@pytest.mark.parametrize("captured", [False, True])
+def test_a_place_whose_group_goes_on_without_it(ssd, captured):
+    """A pass that asks tokens of it leaves it out and says so; the others' rows are right, and the place
+    begins anew when its group is done."""
+    p = Pair(ssd, 7)
+    p.begin([0, 3, 4], [20, 31])
+    graph = p.capture() if captured else None
+    gone = torch.tensor([False, True, False, False], device="cuda")
+    p.a.release(gone)
+    p.b.release(gone)
+    held = int((p.b.tail - p.b.head).item())
+    # without tokens for it nothing is wrong; with them (or fewer than none) it is left out
+    for n in (0, 1, -1):
+        want = p.step(p.a, i32([1, 0, 1, 1])).clone().double()
+        p.a.advance()
+        p.b._o.fill_(5.0)
+        if captured and n == 1:
+            graph[0].replay()
+            o = graph[1]
+        else:
+            o = p.step(p.b, i32([1, n, 1, 1]))
+            p.b.advance()
+        torch.cuda.synchronize()
+        assert int(p.b.status.item()) == (0 if n == 0 else 6) and int(p.a.status.item()) == 0
+        p.b.status.zero_()
+        keep = [0, 2, 3]
+        assert (o[keep].double() - want[keep]).norm() <= 8e-3 * want[keep].norm() and (o[1] == 5.0).all()
+        assert p.b.n_new.tolist() == [1, 0, 1, 1] and p.b.cache_len.tolist() == p.a.cache_len.tolist()
+        assert int(p.b.held[1].item()) == 0
+    assert held - int((p.b.tail - p.b.head).item()) <= 3  # (blocks that the three others went on into)
+    for b in (2, 0, 3):
+        p.b.release(torch.arange(B, device="cuda") == b)
+    assert int((p.b.tail - p.b.head).item()) == p.b.num_blocks
+    at = (torch.arange(p.b.num_blocks, device="cuda") + p.b.head) % p.b.num_blocks
+    assert torch.equal(p.b.ring[at].sort().values, torch.arange(p.b.num_blocks, dtype=torch.int32, device="cuda"))
+    p.begin([0, 2, 4], [11, 17])
+    p.check(*p.capture())
+
+
+def test_a_place_that_began_anew_without_groups(ssd):
+    """A graph of before any share() serves it; a pass with groups leaves it out until its group is done."""
+    p = Pair(ssd, 8)
+    alone = p.capture()
+    p.b.release(torch.ones((B,), dtype=torch.bool, device="cuda"))
+    p.begin([0, 4], [9])
+    gone = torch.tensor([False, False, True, False], device="cuda")
+    p.a.release(gone)
+    p.b.release(gone)
+    for _ in range(3):
+        p.check(*alone)
+    p.step(p.b)
+    torch.cuda.synchronize()
+    assert int(p.b.status.item()) == 6 and p.b.n_new.tolist() == [1, 1, 0, 1]
+    p.b.status.zero_()
+    rest = torch.tensor([True, True, False, True], device="cuda")
+    p.a.release(rest)
+    p.b.release(rest)
+    want = p.step(p.a).clone().double()
+    o = p.step(p.b)
+    torch.cuda.synchronize()
+    assert int(p.b.status.item()) == 0 and (o.double() - want).norm() <= 8e-3 * want.norm()
+    p.b.release(torch.ones((B,), dtype=torch.bool, device="cuda"))

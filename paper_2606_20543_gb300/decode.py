@@ -112,7 +112,8 @@ class PagedDecode:
         """Group g, the sequences group_start[g] <= b < group_start[g + 1], shares the first blocks[g]
         blocks of its first sequence, which has cached them whole (0: none); the others, which hold
         nothing, go on behind them, at length blocks[g] * block.  group_start: 0 ... B; host numbers
-        both.  Called between passes, not while an earlier group's blocks are held.  A graph of a pass
+        both.  Called between passes, not while an earlier group's blocks are held; what of this does not
+        hold is refused, for which it waits for the device.  A graph of a pass
         that was captured before the first share() attends without groups, one captured later serves
         every share() of as many groups whose blocks are no more than the most when it was captured;
         for others it is captured anew.  A place that is released can begin anew once all of its group
@@ -125,6 +126,16 @@ class PagedDecode:
         if min(blocks) < 0 or max(blocks) > self.max_blocks:
             raise ValueError("blocks: between 0 and max_blocks")
         dev = self.device
+        n = torch.repeat_interleave(torch.tensor(blocks), torch.tensor([b - a for a, b in zip(start, start[1:])])).to(dev)
+        is_first = torch.zeros((self.B,), dtype=torch.bool, device=dev)
+        is_first[[a for a, b in zip(start, start[1:]) if b > a]] = True
+        whole = (self.cache_len >= n * self.block) & (self.held >= n)
+        bad = torch.stack([(self._base > 0).any(), (is_first & ~whole).any(),
+                           (~is_first & (n > 0) & ((self.held > 0) | (self.cache_len > 0))).any()]).tolist()
+        for what, is_so in zip(("an earlier group's blocks are held", "the first of a group has not cached its blocks",
+                                "another sequence of a group holds blocks"), bad):
+            if is_so:
+                raise ValueError(what)
         self.groups = len(blocks)
         if self.groups not in self._groups:
             new = lambda *shape, t: torch.zeros(shape, dtype=t, device=dev)  # noqa: E731

@@ -131,3 +131,31 @@ def test_blocks_of_a_place_that_began_anew_come_back(ssd):
         for b in order:
             dec.release(torch.arange(4) == b)
         assert free(dec) == list(range(40)) and dec.shared.tolist() == [0, 0] and dec._open.tolist() == [1] * 4
+
+
+def test_share_refuses_what_would_lose_blocks(ssd):
+    import torch
+    dec = state(make(0, 0, max_blocks=9), 40)
+    cached(dec, 0, 50)
+    before = dec.block_table.clone()
+    # blocks that are not cached whole, by the first of a group or at all
+    for start, blocks in (([0, 4], [4]), ([0, 2, 4], [3, 1]), ([0, 1, 4], [0, 2])):
+        with pytest.raises(ValueError, match="not cached"):
+            dec.share(start, blocks)
+    # a sequence that would join holds blocks of its own
+    cached(dec, 2, 5)
+    with pytest.raises(ValueError, match="holds blocks"):
+        dec.share([0, 4], [3])
+    assert dec.groups == 0 and torch.equal(dec.block_table[[0, 1, 3]], before[[0, 1, 3]])
+    # groups that share nothing, and empty groups, may hold what they do
+    dec.share([0, 2, 2, 4], [3, 1, 0])
+    assert dec.block_table[1, :3].tolist() == dec.block_table[0, :3].tolist()
+    # an earlier group's blocks
+    with pytest.raises(ValueError, match="earlier"):
+        dec.share([0, 2, 4], [3, 0])
+    dec.release(torch.tensor([True, False, False, False]))
+    with pytest.raises(ValueError, match="earlier"):
+        dec.share([0, 4], [0])
+    dec.release(everyone(dec))
+    assert free(dec) == list(range(40))
+    groups_of(dec, [0, 4], [2])

@@ -27,7 +27,8 @@ namespace {
 
 constexpr int kGroup = 128;  // entries of a scale, bytes of a stage's rows
 constexpr int kLaneRows = 128;
-constexpr int kPitch = 36;   // floats of a staged row of 32 (rows start four banks apart)
+constexpr int kPiece = 32;   // columns staged at a time
+constexpr int kPitch = 36;   // floats of a row of them (rows start four banks apart)
 constexpr int kOddPitch = 33;  // the same where C's rows may begin anywhere
 constexpr int kRaster = 8;   // tiles of lanes that share the columns' tiles in L2
 constexpr int kAhead = 4;    // blocks whose scales are asked for together
@@ -36,10 +37,9 @@ constexpr int64_t kOftenBytes = 32 << 20;  // most of A to hold in L2, about a q
 
 template <bool PAIR, int TN, int U>
 struct Shape {
-  static constexpr int EW = TN >= 128 ? 8 : 4;            // epilogue warps
-  static constexpr int CW = TN / (EW / 4);                // columns of one
-  static constexpr int CR = CW < 64 ? CW : 64;            // columns read from TMEM at a time
-  static constexpr int CH = CW < 32 ? CW : 32;            // columns staged at a time
+  static constexpr int EW = 8;                            // epilogue warps
+  static constexpr int CW = TN / 2;                       // columns of one
+  static constexpr int CR = 64;                           // columns read from TMEM at a time
   // (a pair's epilogue takes registers from the others, warpgroup by warpgroup)
   static constexpr int kThreads = (EW + (PAIR ? 4 : 3)) * 32;
   static constexpr int kCols = 2 * U * TN;                // two units in TMEM
@@ -52,7 +52,7 @@ struct Shape {
   static constexpr int kStage = U * (kABytes + kCBytes);
   static constexpr int S = (224 * 1024 - kFixed) / kStage;
   static constexpr int kSmem = kFixed + S * kStage;
-  static_assert(CH == 32 && kCols <= 512 && kAhead % U == 0 && S >= 2, "");
+  static_assert(CW % CR == 0 && kCols <= 512 && kAhead % U == 0 && S >= 2, "");
 };
 
 struct Launch {
@@ -105,16 +105,15 @@ __device__ __forceinline__ void land(uint64_t* bar, uint32_t parity) {
   if (!here) drain(bar, parity);
 }
 
-// A warp's CH columns from n0 on of `rows` rows of C from m0 on: staged with kPitch floats a row, each
+// A warp's kPiece columns from n0 on of `rows` rows of C from m0 on: staged with kPitch floats a row, each
 // store whole sectors of a few rows: 16 bytes a lane, all asked for (of add) before the first is used;
-// columns up to N that end inside of CH an element a lane.
-template <int CH>
+// columns up to N that end inside of them an element a lane.
 __device__ __forceinline__ void write_rows(const ScaledMatmulArgs& a, const float* st, int lane,
                                            int64_t m0, int32_t rows, int32_t n0) {
   const uint16_t* add = static_cast<const uint16_t*>(a.add);
-  const bool vec = n0 + CH <= a.N;
+  const bool vec = n0 + kPiece <= a.N;
   if (vec && a.c_bf16) {
-    constexpr int kL = CH / 8, kRows = 32 / kL;  // lanes of a row, rows of a pass
+    constexpr int kL = kPiece / 8, kRows = 32 / kL;  // lanes of a row, rows of a pass
     const int32_t r0 = lane / kL, c = lane % kL * 8, n = n0 + c;
     uint4 w[kL];
 #pragma unroll
@@ -139,7 +138,7 @@ __device__ __forceinline__ void write_rows(const ScaledMatmulArgs& a, const floa
     }
     return;
   } else if (vec) {
-    constexpr int kL = CH / 4, kRows = 32 / kL;
+    constexpr int kL = kPiece / 4, kRows = 32 / kL;
     const int32_t r0 = lane / kL, c = lane % kL * 4, n = n0 + c;
     uint2 w[kL];
 #pragma unroll
@@ -163,7 +162,7 @@ __device__ __forceinline__ void write_rows(const ScaledMatmulArgs& a, const floa
   }
   // an element each, a lane's column of eight rows together
   const int32_t n = n0 + lane;
-  if (lane >= CH || n >= a.N) return;
+  if (n >= a.N) return;
   const int64_t at = m0 * a.ldc + n;
   const uint16_t* from = add + m0 * a.ldadd + n;
 #pragma unroll 1
@@ -201,7 +200,7 @@ __device__ __forceinline__ void write_rows_any(const ScaledMatmulArgs& a, const 
     if constexpr (sizeof(T) == 2) *p = __float2bfloat16_rn(x);
     else *p = x;
   };
-  if (n0 + 32 > a.N) {
+  if (n0 + kPiece > a.N) {
 #pragma unroll 1
     for (int32_t r = r0; r < rows; r += 4, out += 4 * a.ldc, st += 4 * kOddPitch) {
 #pragma unroll 1
@@ -306,7 +305,7 @@ __global__ void __launch_bounds__(Shape<PAIR, TN, U>::kThreads, 1)
 scaled_matmul_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmW,
                      ScaledMatmulArgs a, Launch L) {
   using H = Shape<PAIR, TN, U>;
-  constexpr int EW = H::EW, CW = H::CW, CR = H::CR, CH = H::CH;
+  constexpr int EW = H::EW, CW = H::CW, CR = H::CR;
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>(
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -572,7 +571,7 @@ scaled_matmul_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
         }
       }
       if (!ok) break;
-      // ---- the tile's way out: a warp's 32 rows turned round in shared memory, CH columns at a time
+      // ---- the tile's way out: a warp's 32 rows turned round in shared memory, kPiece columns at a time
       if (have_rows) {
         float* st = staging + warp * 32 * kPitch;
         const int32_t rows = (int32_t)min((int64_t)32, a.M - row0);
@@ -628,20 +627,20 @@ scaled_matmul_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
         }
         // (one copy of the code for all pieces: cold, it takes longer to fetch than to run)
 #pragma unroll 1
-        for (int x = 0; x < CW && c * TN + col + x < a.N; x += CH) {
+        for (int x = 0; x < CW && c * TN + col + x < a.N; x += kPiece) {
           __syncwarp();
 #pragma unroll
-          for (int y = 0; y < CW; y += CH) {
+          for (int y = 0; y < CW; y += kPiece) {
             if (x != y) continue;
             if constexpr (kVec) {
 #pragma unroll
-              for (int e = 0; e < CH; e += 4)
+              for (int e = 0; e < kPiece; e += 4)
                 *reinterpret_cast<float4*>(st + lane * kPitch + e) =
                     make_float4(acc[(y + e) / 2].x, acc[(y + e) / 2].y, acc[(y + e) / 2 + 1].x,
                                 acc[(y + e) / 2 + 1].y);
             } else {
 #pragma unroll
-              for (int e = 0; e < CH; e += 2) {
+              for (int e = 0; e < kPiece; e += 2) {
                 st[lane * kOddPitch + e] = acc[(y + e) / 2].x;
                 st[lane * kOddPitch + e + 1] = acc[(y + e) / 2].y;
               }
@@ -649,7 +648,7 @@ scaled_matmul_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
           }
           __syncwarp();
           const int32_t n = c * TN + col + x;
-          if constexpr (kVec) write_rows<CH>(a, st, lane, row0, rows, n);
+          if constexpr (kVec) write_rows(a, st, lane, row0, rows, n);
           else if (a.c_bf16) write_rows_any<__nv_bfloat16>(a, st, lane, row0, rows, n, L.even);
           else write_rows_any<float>(a, st, lane, row0, rows, n, L.even);
         }

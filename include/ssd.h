@@ -684,8 +684,11 @@ ssd_status ssd_cache_attention(const ssd_grid* grid, const ssd_block_cache* cach
  * prompt: group g holds the sequences group_start[g] <= b < group_start[g + 1],
  * whose first shared[g] blocks are the same (their tables' first shared[g]
  * entries are equal; shared[g] may be 0).  The same o and lse, but for the order
- * of sums; the shared keys are read once for the rows of a group instead of once
- * a sequence.  Shared blocks hold committed tokens: shared[g] * block <=
+ * of sums and, where the groups' rows are more than 16 in the mean, for the
+ * queries: as without sharing for more than 16 rows of a sequence, their entries
+ * below 2^-10 of the row's largest are good to 2^-18 of that largest, not to 8
+ * bits of their own.  The shared keys are read once for the rows of a group instead
+ * of once a sequence.  Shared blocks hold committed tokens: shared[g] * block <=
  * cache_len[b] for every sequence of the group that has drafts.  (A NaN in a
  * shared token's value: "the rows of its head" there are those of the group.)
  *   group_start  dev int32 [groups + 1]: 0 ... B, ascending; shared dev int32
@@ -696,10 +699,12 @@ ssd_status ssd_cache_attention(const ssd_grid* grid, const ssd_block_cache* cach
  * estimate from the arguments' sizes) each sequence is worked on by itself, and
  * group_start and shared are not read.  ssd_set_cache_sharing(how) is
  * process-wide, for callers who know better (tables much wider than their
- * sequences): 0 by the estimate (the default), 1 always sharing, 2 never; it
- * holds for workspace queries and calls after it.  A call reads it once; one whose
- * workspace was asked for under another setting is refused (SSD_ERR_WORKSPACE) if
- * that is too small for the way it would go now.
+ * sequences; one group of nearly all sequences beside many of one, whose rows the
+ * estimate, which knows their mean alone, takes for few): 0 by the estimate (the
+ * default), 1 always sharing, 2 never; it holds for workspace queries and calls
+ * after it.  A call reads it once; one whose workspace was asked for under another
+ * setting is refused (SSD_ERR_WORKSPACE) if that is too small for the way it would
+ * go now.
  * Device errors beside those of ssd_cache_attention(): groups or shared out of
  * range, more shared tokens than cache_len (DEVICE_BOUNDS; rows of the
  * sequences concerned untouched, or, where group_start does not ascend, of no

@@ -463,8 +463,10 @@ __device__ __forceinline__ void append_block(const CacheAppendArgs& a, int32_t b
 // Grid: first the (sequence, touched block, head) units of K, then those of V, then
 // those of q: a thread takes 16 columns of up to kHeads heads of a token.
 // 72 registers: with norms the compiler takes 86 to 92, and what is lost in loads under way costs more
-// (16 ragged prompts, layer norms with gains and biases of every head: 66.9 us, 58.5 with 72, 60.3
-// with 64; root-mean-square norms alone 54.9 and 47.6; without norms 66 registers either way).
+// than the 64 to 92 bytes a thread that it spills (16 ragged prompts, layer norms with gains and biases of
+// every head, on the same inputs again and again: 66.9 us, 58.5 with 72, 60.3 with 64; root-mean-square norms
+// alone 54.9 and 47.6).  On inputs that change: 64 and 55 us, one row of gains for all heads 61 and 53; without
+// norms, which spills nothing, 42.
 template <int D, int kNorm>
 __global__ void __maxnreg__(72)
 cache_append_kernel(CacheAppendArgs a, int32_t touched, int64_t kv_units, bool wide) {

@@ -23,7 +23,7 @@ struct CacheAttnLaunch {
   // CacheWork
   int32_t per_head, goal, uniform, row_groups, group_rows;
   int2* info;          // [B]: first and last CTA of a sequence
-  // Groups' shared keys (tensor-core kernel): units of the grid, tiles of rows among them, parts and
+  // Groups' shared keys (either kernel): units of the tensor-core kernel's grid, parts and
   // their rows [B][D_max][Hq][s_splits]
   int32_t s_units, s_splits, s_min_tiles;
   int32_t early;       // the kernel after it may run beside it: the sequences' own keys

@@ -11,10 +11,10 @@
 // which the kernel here joins.
 //
 // One token of 64 sequences of one group, 4352 shared keys and 100 to 1000 own, 32/8 heads (73 MB):
-// 37 us, 2.0 TB/s: the set-up, first tile and way out of three kernels' CTAs (18000 cycles of a
+// 38 us, 1.9 TB/s: the set-up, first tile and way out of three kernels' CTAs (18000 cycles of a
 // shared unit's 30000), and own keys at 2.5 TB/s beside the shared ones.  48 drafts of 8 groups of 4
-// over 1500 to 8000 shared keys, 16 heads: 118 us, the softmax of the tensor-core kernel.  35 tokens of 7 groups over 6300 shared keys,
-// 8 heads of 64 (46 MB): 20 us, without sharing 54.
+// over 1500 to 8000 shared keys, 16 heads: 118 us, the softmax of the tensor-core kernel.  35 tokens of 7
+// groups over 6300 shared keys, 8 heads of 64 (46 MB): 20 us, without sharing 54.
 #include <algorithm>
 #include <cmath>
 
@@ -39,7 +39,12 @@ constexpr double kFewFixed = 6;        // and one of few rows on the mma.sync ke
 // 32/8 heads 37 and 102; 50 of 4 drafts over 13000, 33 and 138; 8 groups of 4, 48 drafts over 8000 + 600,
 // 16 heads 117 and 152; 7 groups of 5 over 6300, 8 heads of 64 20 and 54; 6 of 14, 6 drafts
 // over 2200 + 1400, 6/2 heads 35 and 58; 10 of 3 over 1000, 32 heads 60 and 43; 8 groups of 2 over 4900
-// + 1900, 41 and 25; 3 of 42 drafts over 1800 + 1000, 6/2 heads 22 and 17.
+// + 1900, 41 and 25; 3 of 42 drafts over 1800 + 1000, 6/2 heads 22 and 17.  Where it is wrong: small work, which
+// cache_attention_few() keeps from it (20 sequences of 4 groups over 1408, 8 heads of 64: 13 shared, 16 not,
+// as chosen); many heads of short own keys (182 of 14 groups over 256, 32 heads: 132 as chosen, 87); 380 of 10
+// over 704, 8 heads of 64: 41, 63 as chosen; and groups of very unequal size, whose sizes are on the device: 19 of
+// one and one of 61, over 4096, 32/8 heads 176 as chosen (the large
+// group's 244 rows, 16 a turn, read the keys eight times one after the other), 95 not.
 bool sharing_pays(int32_t B, int32_t groups, int32_t Hq, int32_t Hkv, int32_t d, int32_t D_max,
                   int32_t L_max, int32_t max_shared, const CacheSharedPlan& p) {
   const double G = Hq / Hkv, per_seq = D_max * G, rows = (double)B * D_max * Hq;

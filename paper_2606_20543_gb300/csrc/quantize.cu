@@ -3,7 +3,8 @@
 //   s = max(largest finite |x|, 2^-100) / 448,   q = e4m3(clamp(x * (1 / s), -448, 448)).
 // Every value is read once and held in registers between the search for the largest and the
 // rounding.  Memory bound: an entry is 2 (or 4) bytes in and 1 out.  17408 x 4096 of bf16 (216 MB)
-// 35.4 us, 6.1 TB/s, 0.91 of the measured copy rate; 8 x 4096 2.3 us, a launch.
+// 36.4 us, 5.9 TB/s, 0.89 of the measured copy rate, of float32 57.0; 8 x 4096 2.0 us, a launch; a weight of
+// 12288 x 4096 in blocks of 128 x 128 38.2 us (151 MB).
 #include <algorithm>
 
 #include "e4m3.cuh"

@@ -11,9 +11,9 @@
 // number a thread), 128 rows of W its columns; or a CTA pair (cta_group::2) has 128 lanes each and 128
 // or 256 columns.  Up to 64 rows, mostly: the other way round (scaled_matmul_few_kernel).
 //
-// 17408 x 12288 x 4096 (1752 GFLOP) 777 us, 2250 TFLOP/s: 560 ns a block of 256 x 256 of a pair, of which
-// the products are 340; two TMEM buffers' round trips bound it (without the reads of TMEM 563 us).
-// 1024 x 4096 x 4096 with a sum 24.2 us; 16 x 65536 x 4096 (273 MB) 42 us, the copy rate.
+// 17408 x 12288 x 4096 (1752 GFLOP) 800 us in a graph, 2190 TFLOP/s: 560 ns a block of 256 x 256 of
+// a pair, of which the products are 340; two TMEM buffers' round trips bound it (without the reads of TMEM
+// 563 us).  1024 x 4096 x 4096 with a sum 25.0 us; 16 x 65536 x 4096 (273 MB) 43 us, the copy rate.
 //
 // Barriers count units of U blocks: a wait that is satisfied already costs a warp about 100
 // cycles, a commit of products as much.
@@ -674,7 +674,9 @@ scaled_matmul_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
 // W from shared memory once (with A on the lanes, a tile of 64 rows of W reads 128 of A with it,
 // most of them empty: 16 x 65536 x 4096 56 us, here 43).  W's way in bounds it.  Where the tiles
 // alone would leave SMs idle, the blocks of a tile are cut over a cluster of up to eight CTAs, which
-// add their sums up through distributed shared memory in the order of their ranks.
+// add their sums up through distributed shared memory in the order of their ranks (with each other's word
+// that no wait gave up, 0.15 us: 1 x 4096 x 4096 6.55 us without it, 6.70).  Two CTAs an SM hold the 64-column
+// kernel to 96 registers, which spills nothing.
 template <int TN, int U>
 struct Few {
   static constexpr int EW = TN < 64 ? 4 : 8;          // epilogue warps,
@@ -1072,8 +1074,8 @@ cudaError_t launch_few(const ScaledMatmulArgs& a, int32_t splits, cudaStream_t s
   if (splits > 1)
     return launch_clusters(kernel, dim3((unsigned)(total * splits)), dim3(H::kThreads), H::kSmem, stream, true,
                            splits, ta, tw, a, L);
-  return launch_kernel(kernel, dim3((unsigned)std::min(total, 2 * device_sm_count())), dim3(H::kThreads), H::kSmem, stream,
-                       true, ta, tw, a, L);
+  return launch_kernel(kernel, dim3((unsigned)std::min(total, 2 * device_sm_count())), dim3(H::kThreads),
+                       H::kSmem, stream, true, ta, tw, a, L);
 }
 
 }  // namespace
@@ -1097,7 +1099,7 @@ cudaError_t launch_scaled_matmul(const ScaledMatmulArgs& a, cudaStream_t stream)
   // (of 256 and of 128 columns).  Tiles of a pair are better for their size and worse where they leave SMs
   // idle.  Measured (us, 256 x 256 and 256 x 128 of a pair, 128 x 128): 1024 x 4096 x 4096 with a sum 24.5,
   // 28, 27; 200 x 5000 x 2050 14.6, 10.3, 9.6; 264 x 24448 x 9134 124, 144, 138; 5848 x 58870 x 172 207, -,
-  // 312; to float32 with rows anywhere 551, -, 520.  Over 200 drawn products 1% above the best of the three.
+  // 312; to float32 with rows anywhere 551, -, 520.  Over 350 drawn products 1% above the best of the three.
   const bool vec = on_vectors(a);
   const int64_t out256 = a.add != nullptr ? (vec ? 6900 : 10100) : a.c_bf16 ? (vec ? 2700 : 3900) : vec ? 5900 : 6600;
   const int64_t out128 = a.add != nullptr ? (vec ? 3200 : 4800) : a.c_bf16 ? (vec ? 1800 : 2200) : vec ? 2400 : 3300;

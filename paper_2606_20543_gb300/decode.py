@@ -113,10 +113,9 @@ class PagedDecode:
         blocks of its first sequence, which has cached them whole (0: none); the others, which hold
         nothing, go on behind them, at length blocks[g] * block.  group_start: 0 ... B; host numbers
         both.  Called between passes, not while an earlier group's blocks are held; what of this does not
-        hold is refused, for which it waits for the device.  A graph of a pass
-        that was captured before the first share() attends without groups, one captured later serves
-        every share() of as many groups whose blocks are no more than the most when it was captured;
-        for others it is captured anew.  A place that is released can begin anew once all of its group
+        hold is refused, for which it waits for the device.  A graph of a pass that was captured before the
+        first share() attends without groups, one captured later serves every share() of as many groups
+        whose blocks are no more than the most when it was captured; for others it is captured anew.  A place that is released can begin anew once all of its group
         are (their shared blocks go back with the last of them); a pass with groups that asks tokens of it
         before leaves it out, as one that plan() cannot serve (status: DEVICE_BOUNDS)."""
         start, blocks = [int(x) for x in group_start], [int(x) for x in blocks]
@@ -126,9 +125,10 @@ class PagedDecode:
         if min(blocks) < 0 or max(blocks) > self.max_blocks:
             raise ValueError("blocks: between 0 and max_blocks")
         dev = self.device
-        n = torch.repeat_interleave(torch.tensor(blocks), torch.tensor([b - a for a, b in zip(start, start[1:])])).to(dev)
+        sizes = [b - a for a, b in zip(start, start[1:])]
+        n = torch.repeat_interleave(torch.tensor(blocks), torch.tensor(sizes)).to(dev)
         is_first = torch.zeros((self.B,), dtype=torch.bool, device=dev)
-        is_first[[a for a, b in zip(start, start[1:]) if b > a]] = True
+        is_first[[a for a, size in zip(start, sizes) if size > 0]] = True
         whole = (self.cache_len >= n * self.block) & (self.held >= n)
         bad = torch.stack([(self._base > 0).any(), (is_first & ~whole).any(),
                            (~is_first & (n > 0) & ((self.held > 0) | (self.cache_len > 0))).any()]).tolist()
@@ -148,15 +148,12 @@ class PagedDecode:
         self.__dict__.update(kept)
         self.group_start.copy_(torch.tensor(start, dtype=torch.int32))
         self.shared.copy_(torch.tensor(blocks, dtype=torch.int32))
-        sizes = [b - a for a, b in zip(start, start[1:])]
         self._group.copy_(torch.repeat_interleave(torch.arange(self.groups), torch.tensor(sizes)))
         first = torch.tensor([min(a, self.B - 1) for a in start[:-1]], device=dev)
-        firsts = torch.tensor([a for a, n in zip(start, sizes) if n > 0], device=dev)
         self._shared_ids.copy_(self.block_table[first])
-        self._shared_own.copy_(self.shared * torch.tensor([int(n > 0) for n in sizes], device=dev))
-        base, joins = self.shared[self._group], torch.ones((self.B,), dtype=torch.bool, device=dev)
-        joins[firsts] = False
-        joins &= base > 0
+        self._shared_own.copy_(self.shared * torch.tensor([int(size > 0) for size in sizes], device=dev))
+        base = self.shared[self._group]
+        joins = ~is_first & (base > 0)
         take = joins[:, None] & (torch.arange(self.max_blocks, device=dev)[None] < base[:, None])
         self.block_table.copy_(torch.where(take, self._shared_ids[self._group], self.block_table))
         self._base.copy_(base)

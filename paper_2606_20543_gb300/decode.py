@@ -115,9 +115,10 @@ class PagedDecode:
         both.  Called between passes, not while an earlier group's blocks are held; what of this does not
         hold is refused, for which it waits for the device.  A graph of a pass that was captured before the
         first share() attends without groups, one captured later serves every share() of as many groups
-        whose blocks are no more than the most when it was captured; for others it is captured anew.  A place that is released can begin anew once all of its group
-        are (their shared blocks go back with the last of them); a pass with groups that asks tokens of it
-        before leaves it out, as one that plan() cannot serve (status: DEVICE_BOUNDS)."""
+        whose blocks are no more than the most when it was captured; for others it is captured anew.  A
+        place that is released can begin anew once all of its group are (their shared blocks go back with
+        the last of them); a pass with groups that asks tokens of it before leaves it out, as one that
+        plan() cannot serve (status: DEVICE_BOUNDS)."""
         start, blocks = [int(x) for x in group_start], [int(x) for x in blocks]
         if len(start) != len(blocks) + 1 or start[0] != 0 or start[-1] != self.B or not blocks \
                 or any(a > b for a, b in zip(start, start[1:])):
